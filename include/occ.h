@@ -479,6 +479,66 @@ int occ_overlap_enqueue(const occ_overlap_cfg *cfg, void *comm_stream, void *wor
 #define OCC_NOALLOC_MAX_ITER 1024
 int occ_overlap_enqueue_noalloc(const occ_overlap_cfg *cfg, void *comm_stream, uint32_t *err);
 
+/* ------------------------------------------------ operators of a block
+ *
+ * What a model's block computes between the GEMMs and collectives above:
+ * products of 4-bit operands, the expert layer whose tokens the alltoall
+ * routes, and the norms around a block.  Same conventions as above; every
+ * entry point is asynchronous on `stream` and ordered by it alone.
+ */
+enum { OCC_BF16 = 0, OCC_F32 = 1, OCC_MX4 = 2 };  /* element types */
+
+/*
+ * Microscaled 4-bit floating point (MX4): a rows x cols matrix in blocks of
+ * 32 consecutive columns of a row.  A block has one scale 2^e (a byte, e + 127;
+ * 255 = NaN) and 32 codes of E2M1: sign, two bits of exponent, one of fraction,
+ * the values 0, 0.5, 1, 1.5, 2, 3, 4, 6 for codes 0 .. 7.  Rows are padded with
+ * zero codes to Kp = OCC_MX4_KP(cols) columns, a multiple of 512.
+ *   codes  : rows x Kp/2 bytes; the even column of a pair is the low nibble.
+ *   scales : ceil(rows/16) x Kp/2 bytes, tiles of 16 rows x 512 columns of 256
+ *            bytes each.  Row 16 t + r, block (4 s + j) * 4 + g (s < Kp/512;
+ *            j, g < 4) is byte j of word 16 g + r of tile (t, s): the 64 words
+ *            of a tile are what the 64 lanes of a wave hand to four 16x16x128
+ *            matrix instructions.  Pad rows and blocks have zero bytes.
+ * Both 16-byte aligned.  A batch of matrices is a batch of each.
+ */
+#define OCC_MX4_KP(cols) (((size_t)(cols) + 511) / 512 * 512)
+#define OCC_MX4_CODE_BYTES(rows, cols) ((size_t)(rows) * (OCC_MX4_KP(cols) / 2))
+#define OCC_MX4_SCALE_BYTES(rows, cols) (((size_t)(rows) + 15) / 16 * (OCC_MX4_KP(cols) / 2))
+#define OCC_MX4_MAX_DIM 8388608  /* largest rows or cols (2^23) */
+
+/*
+ * occ_mx4_quantize -- x (rows x cols, OCC_BF16 or OCC_F32, row r at x + r*ld)
+ * to MX4, once or twice from one read:
+ *   codes, scales     : of x, blocks along its rows (null: not made);
+ *   codes_t, scales_t : of x's transpose, cols x rows, blocks along x's
+ *                       columns (null: not made): the operand of a product
+ *                       that sums over x's rows, as a weight gradient does.
+ * A block's scale is 2^e, e = floor(log2(max |x|)) - 2 within [-127, 127] (-127
+ * where all are zero); its codes are x / 2^e rounded to the nearest value,
+ * ties to the even code, magnitudes beyond 6 to 6.  A block that holds an
+ * infinity or a NaN gets the NaN scale and zero codes.  x is aligned to its
+ * elements, ld >= cols.  OCC_EINVAL if both pairs or one half of a pair is null.
+ */
+int occ_mx4_quantize(const void *x, int dtype, int rows, int cols, size_t ld, void *codes, void *scales,
+                     void *codes_t, void *scales_t, void *stream);
+
+/* occ_mx4_dequantize -- the values MX4 codes and scales stand for, to out
+   (OCC_BF16, exact down to its smallest normal scale, or OCC_F32; row r at out + r*ld). */
+int occ_mx4_dequantize(const void *codes, const void *scales, int rows, int cols, void *out, int dtype, size_t ld,
+                       void *stream);
+
+/*
+ * occ_gemm_mx4 -- C = A * B^T of MX4 operands, A M x K, B N x K (a linear
+ * layer's weight), fp32 accumulation on the scaled matrix instructions; C is
+ * M x N row-major, OCC_BF16 (rounded to nearest-even) or OCC_F32.  lds_bytes is
+ * the occupancy pad of occ_gemm: extra LDS per workgroup, never touched;
+ * OCC_ELDS where the tile has no room for it.  Any M, N, K >= 0 up to
+ * OCC_MX4_MAX_DIM; K == 0 writes zeros.  C is aligned to its elements.
+ */
+int occ_gemm_mx4(const void *A, const void *A_scales, const void *B, const void *B_scales, void *C, int dtype,
+                 int M, int N, int K, size_t lds_bytes, void *stream);
+
 /* Static string naming a status code. */
 const char *occ_strerror(int status);
 

@@ -22,6 +22,7 @@ OCC_COMM_REDUCE, OCC_COMM_PERMUTE, OCC_COMM_REDUCE_OWN = 0, 1, 2
 OCC_RUN_SEQ, OCC_RUN_OVL, OCC_RUN_ISO, OCC_RUN_GRAPH, OCC_RUN_PACE_ALL = 1, 2, 4, 8, 16
 OCC_B_KN, OCC_B_NK = 0, 1
 OCC_DEP_EVENT, OCC_DEP_COUNTER = 0, 1
+OCC_BF16, OCC_F32, OCC_MX4 = 0, 1, 2
 # kernel variants of occ.h, by the layout of B they read
 KN_VARIANTS = {
     32: "pp 256x256x64 8w 2st", 33: "skinny M<=16, 32-, 64- or 128-column units",
@@ -109,6 +110,10 @@ _SIGS = {
     "occ_overlap_workspace_bytes": [ctypes.c_int],
     "occ_overlap_enqueue": [ctypes.POINTER(occ_overlap_cfg), _P, _P, ctypes.c_size_t, _P],
     "occ_overlap_enqueue_noalloc": [ctypes.POINTER(occ_overlap_cfg), _P, _P],
+    "occ_mx4_quantize": [_P, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_size_t, _P, _P, _P, _P, _P],
+    "occ_mx4_dequantize": [_P, _P, ctypes.c_int, ctypes.c_int, _P, ctypes.c_int, ctypes.c_size_t, _P],
+    "occ_gemm_mx4": [_P, _P, _P, _P, _P, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                     ctypes.c_size_t, _P],
     "occ_strerror": [ctypes.c_int],
     "occ_version": [],
 }
@@ -491,3 +496,101 @@ def occ_overlap_enqueue_noalloc(A, B, C, *, comm_stream, err=None, bufs=None, ou
         raise ValueError("err must be a 32-bit GPU tensor")
     _check(lib().occ_overlap_enqueue_noalloc(ctypes.byref(cfg), _stream(comm_stream), _ptr(err)),
            "occ_overlap_enqueue_noalloc")
+
+
+# ------------------------------------------------------------------ operators of a block
+
+_FLOAT_TYPES = {torch.bfloat16: OCC_BF16, torch.float32: OCC_F32}
+
+
+def _float_type(name, t):
+    if t.dtype not in _FLOAT_TYPES or not t.is_cuda:
+        raise ValueError("%s must be a bfloat16 or float32 GPU tensor" % name)
+    return _FLOAT_TYPES[t.dtype]
+
+
+def _rows(name, t, shape=None):
+    """(type, row pitch) of a 2-D GPU tensor whose rows are contiguous."""
+    kind = _float_type(name, t)
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError("%s must have shape %s" % (name, "(rows, cols)" if shape is None else tuple(shape)))
+    rows, cols = t.shape
+    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+        raise ValueError("%s must have contiguous rows that do not overlap" % name)
+    return kind, (t.stride(0) if rows > 1 else cols)
+
+
+class Mx4:
+    """A rows x cols matrix, or a batch of them, in microscaled 4-bit floating
+    point (the layout is occ.h's): ``codes`` (..., rows, Kp/2) and ``scales``
+    (..., ceil(rows/16), Kp/2), uint8, with Kp = cols padded to a multiple of 512."""
+
+    __slots__ = ("codes", "scales", "rows", "cols")
+
+    def __init__(self, codes, scales, rows, cols):
+        half = (cols + 511) // 512 * 256
+        for name, t, n in (("codes", codes, rows), ("scales", scales, (rows + 15) // 16)):
+            if t.dtype != torch.uint8 or t.dim() < 2 or tuple(t.shape[-2:]) != (n, half) or not t.is_contiguous():
+                raise ValueError("%s must be a contiguous uint8 tensor of (..., %d, %d)" % (name, n, half))
+        if codes.shape[:-2] != scales.shape[:-2] or codes.device != scales.device:
+            raise ValueError("codes and scales must be of one batch and device")
+        self.codes, self.scales, self.rows, self.cols = codes, scales, int(rows), int(cols)
+
+    def __getitem__(self, i):
+        """Matrix i of a batch (a view)."""
+        if self.codes.dim() < 3:
+            raise IndexError("not a batch")
+        return Mx4(self.codes[i], self.scales[i], self.rows, self.cols)
+
+
+def mx4_empty(rows, cols, batch=(), device="cuda"):
+    """An uninitialised Mx4 of rows x cols matrices."""
+    half = (cols + 511) // 512 * 256
+    batch = (batch,) if isinstance(batch, int) else tuple(batch)
+    return Mx4(torch.empty(batch + (rows, half), dtype=torch.uint8, device=device),
+               torch.empty(batch + ((rows + 15) // 16, half), dtype=torch.uint8, device=device), rows, cols)
+
+
+def _mx4(name, q, rows=None, cols=None):
+    if not isinstance(q, Mx4) or q.codes.dim() != 2 or not q.codes.is_cuda:
+        raise ValueError("%s must be one Mx4 matrix on the GPU" % name)
+    if (rows is not None and q.rows != rows) or (cols is not None and q.cols != cols):
+        raise ValueError("%s must be %s x %s" % (name, rows, cols))
+    return _ptr(q.codes), _ptr(q.scales)
+
+
+def occ_mx4_quantize(x, out=None, out_t=None, stream=None):
+    """x (rows x cols, bf16 or fp32, contiguous rows) to MX4: ``out`` in blocks along
+    its rows and ``out_t`` (cols x rows) in blocks along its columns, either or both
+    from one read.  Returns (out, out_t)."""
+    kind, ld = _rows("x", x)
+    rows, cols = x.shape
+    null = (_P(0), _P(0))
+    q = null if out is None else _mx4("out", out, rows, cols)
+    qt = null if out_t is None else _mx4("out_t", out_t, cols, rows)
+    if out is None and out_t is None:
+        raise ValueError("out or out_t must be given")
+    if x.numel() > 0:
+        _check(lib().occ_mx4_quantize(_ptr(x), kind, rows, cols, ld, *q, *qt, _stream(stream)), "occ_mx4_quantize")
+    return out, out_t
+
+
+def occ_mx4_dequantize(q, out, stream=None):
+    """The values of an Mx4 matrix, to out (rows x cols, bf16 or fp32)."""
+    kind, ld = _rows("out", out, (q.rows, q.cols))
+    if out.numel() > 0:
+        _check(lib().occ_mx4_dequantize(*_mx4("q", q), q.rows, q.cols, _ptr(out), kind, ld, _stream(stream)),
+               "occ_mx4_dequantize")
+    return out
+
+
+def occ_gemm_mx4(A, B, C, lds_bytes=0, stream=None):
+    """C = A @ B.T of MX4 operands (fp32 accumulation): A M x K, B N x K (a linear
+    layer's weight), C M x N bfloat16 or float32."""
+    a, b = _mx4("A", A), _mx4("B", B, cols=A.cols)
+    kind = _float_type("C", C)
+    if tuple(C.shape) != (A.rows, B.rows) or not C.is_contiguous():
+        raise ValueError("C must be a contiguous (M, N) tensor")
+    _check(lib().occ_gemm_mx4(*a, *b, _ptr(C), kind, A.rows, B.rows, A.cols, int(lds_bytes), _stream(stream)),
+           "occ_gemm_mx4")
+    return C

@@ -1,0 +1,120 @@
+// C = A B^T of MX4 operands (occ_gemm_mx4): the tiles, and which call takes which.
+//
+// fp32 accumulation on v_mfma_scale_f32_16x16x128_f8f6f4: exact products of two
+// E2M1 values and two powers of two, 128 a lane group and instruction.  The
+// kernels live in gemm_mx4_pp.h (256x256 tiles), gemm_mx4_rp.h (smaller ones) and
+// gemm_mx4_skinny.h (M <= 16).
+#include "gemm_mx4_pp.h"
+#include "gemm_mx4_rp.h"
+#include "gemm_mx4_skinny.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace occ {
+namespace {
+
+typedef void (*Mx4Fn)(Mx4Operands, int, int);
+
+// A tile and its estimated time on a shape (as gemm.hip's): launch + rounds * (fixed + step per 512 of K).
+struct Mx4Tile {
+  int bm, bn, threads, lds;
+  Mx4Fn bf16, f32;
+  int per_cu;  // workgroups resident on a CU
+  double fixed, step;
+};
+
+template <template <class> class T>
+constexpr Mx4Tile tile_of(Mx4Fn bf16, Mx4Fn f32, int per_cu, double fixed, double step) {
+  typedef T<uint16_t> X;
+  return Mx4Tile{X::BM, X::BN, X::NT, X::LDS_BYTES, bf16, f32, per_cu, fixed, step};
+}
+
+template <class OUT>
+using Rp128x128 = Mx4Rp<128, 128, 2, 4, 2, 1, OUT>;
+template <class OUT>
+using Rp64x64 = Mx4Rp<64, 64, 2, 2, 4, 4, OUT>;
+template <class OUT>
+using Rp32x64 = Mx4Rp<32, 64, 2, 2, 4, 4, OUT>;
+
+const Mx4Tile kTiles[] = {
+    tile_of<Mx4Pp>(gemm_mx4_pp_kernel<Mx4Pp<uint16_t>>, gemm_mx4_pp_kernel<Mx4Pp<float>>, 1, 4.0, 2.2),
+    tile_of<Rp128x128>(gemm_mx4_rp_kernel<Rp128x128<uint16_t>>, gemm_mx4_rp_kernel<Rp128x128<float>>, 1, 2.0, 0.9),
+    tile_of<Rp64x64>(gemm_mx4_rp_kernel<Rp64x64<uint16_t>>, gemm_mx4_rp_kernel<Rp64x64<float>>, 1, 1.6, 0.4),
+    tile_of<Rp32x64>(gemm_mx4_rp_kernel<Rp32x64<uint16_t>>, gemm_mx4_rp_kernel<Rp32x64<float>>, 1, 1.3, 0.33),
+};
+constexpr int kNumTiles = (int)(sizeof kTiles / sizeof kTiles[0]);
+
+int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
+
+// The tile with the least estimated time whose LDS fits in `room`, -1 if none.
+int choose_tile(const Mx4GemmCall &c, int num_cus, int room) {
+  int best = -1;
+  double t_best = 0;
+  for (int i = 0; i < kNumTiles; ++i) {
+    const Mx4Tile &t = kTiles[i];
+    if (t.lds > room) continue;
+    const double tiles = (double)ceil_div(c.M, t.bm) * ceil_div(c.N, t.bn);
+    const double us = std::ceil(tiles / num_cus) * (t.fixed + t.step * ceil_div(c.K, 512));
+    if (best < 0 || us < t_best) {
+      best = i;
+      t_best = us;
+    }
+  }
+  return best;
+}
+
+typedef void (*SkinnyFn)(Mx4Operands, int);
+template <class OUT, bool NT>
+SkinnyFn skinny_fn(int kw, int ut) {
+  if (ut == 2)
+    return kw == 8 ? gemm_mx4_skinny_kernel<8, 2, OUT, NT> : kw == 4 ? gemm_mx4_skinny_kernel<4, 2, OUT, NT>
+         : kw == 2 ? gemm_mx4_skinny_kernel<2, 2, OUT, NT> : gemm_mx4_skinny_kernel<1, 2, OUT, NT>;
+  return kw == 8 ? gemm_mx4_skinny_kernel<8, 1, OUT, NT> : kw == 4 ? gemm_mx4_skinny_kernel<4, 1, OUT, NT>
+       : kw == 2 ? gemm_mx4_skinny_kernel<2, 1, OUT, NT> : gemm_mx4_skinny_kernel<1, 1, OUT, NT>;
+}
+
+int launch_skinny(const Mx4GemmCall &c, const Mx4Operands &o, const DeviceInfo &di, hipStream_t s) {
+  // the largest power of two of waves along K that all have a k-step
+  int kw = 1;
+  while (kw < 8 && kw * 2 <= o.steps512) kw *= 2;
+  // 32-column units share A's loads between two blocks; 16-column ones where those would leave CUs idle
+  const int ut = ceil_div(c.N, 32) * kw >= di.num_cus * 8 ? 2 : 1;
+  const int units = ceil_div(c.N, 16 * ut);
+  const bool nt = (long long)c.N * o.pitch > (256ll << 20);  // B is read once and exceeds the last-level cache
+  const SkinnyFn fn = c.dtype == OCC_BF16 ? (nt ? skinny_fn<uint16_t, true>(kw, ut) : skinny_fn<uint16_t, false>(kw, ut))
+                                          : (nt ? skinny_fn<float, true>(kw, ut) : skinny_fn<float, false>(kw, ut));
+  const int own = 8 * ut * 64 * 16;
+  if ((size_t)own + c.lds_bytes > (size_t)di.max_lds_per_wg) return OCC_ELDS;
+  if (c.lds_bytes > 0 && hipFuncSetAttribute(reinterpret_cast<const void *>(fn), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                             di.max_lds_per_wg - own) != hipSuccess)
+    return OCC_EHIP;
+  hipLaunchKernelGGL(fn, dim3(ceil_div(units, 8 / kw)), dim3(512), (int)c.lds_bytes, s, o, units);
+  return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
+}
+
+}  // namespace
+
+int mx4_gemm_launch(const Mx4GemmCall &c, hipStream_t s) {
+  const DeviceInfo *di = nullptr;
+  int st = current_device_info(&di);
+  if (st != OCC_OK) return st;
+  if (c.M == 0 || c.N == 0) return OCC_OK;
+  const Mx4Operands o{static_cast<const uint8_t *>(c.A), static_cast<const uint8_t *>(c.As),
+                      static_cast<const uint8_t *>(c.B), static_cast<const uint8_t *>(c.Bs),
+                      c.C, c.M, c.N, (uint32_t)(OCC_MX4_KP(c.K) / 2), ceil_div(c.K, 256), ceil_div(c.K, 512)};
+  if (c.M <= 16) return launch_skinny(c, o, *di, s);
+  if (c.lds_bytes > (size_t)di->max_lds_per_wg) return OCC_ELDS;
+  // the pad keeps the tile: it lowers residency and changes nothing else, and is never clamped
+  const Mx4Tile &t = kTiles[choose_tile(c, di->num_cus, di->max_lds_per_wg)];
+  if ((size_t)t.lds + c.lds_bytes > (size_t)di->max_lds_per_wg) return OCC_ELDS;
+  const Mx4Fn fn = c.dtype == OCC_BF16 ? t.bf16 : t.f32;
+  if (hipFuncSetAttribute(reinterpret_cast<const void *>(fn), hipFuncAttributeMaxDynamicSharedMemorySize,
+                          di->max_lds_per_wg) != hipSuccess)
+    return OCC_EHIP;
+  const int tm = ceil_div(c.M, t.bm), tn = ceil_div(c.N, t.bn);
+  hipLaunchKernelGGL(fn, dim3(tm * tn), dim3(t.threads), t.lds + (int)c.lds_bytes, s, o, tm, tn);
+  return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
+}
+
+}  // namespace occ

@@ -82,6 +82,36 @@ int validate_reduce_own(const void *own, const float *const *peers, int npeers, 
 int validate_permute(const void *src, const void *dst, const int32_t *perm, int nchunks,
                      size_t chunk_bytes);
 
+// ---- operators of a block (include/occ.h) ---------------------------------
+struct Mx4QuantCall {
+  const void *x;
+  int dtype, rows, cols;
+  size_t ld;
+  void *codes, *scales;      // of x, or null
+  void *codes_t, *scales_t;  // of its transpose, or null
+};
+int validate_mx4_quant(const Mx4QuantCall &c);
+int mx4_quant_launch(const Mx4QuantCall &c, hipStream_t s);
+
+struct Mx4DequantCall {
+  const void *codes, *scales;
+  int rows, cols;
+  void *out;
+  int dtype;
+  size_t ld;
+};
+int validate_mx4_dequant(const Mx4DequantCall &c);
+int mx4_dequant_launch(const Mx4DequantCall &c, hipStream_t s);
+
+struct Mx4GemmCall {
+  const void *A, *As, *B, *Bs;
+  void *C;
+  int dtype, M, N, K;
+  size_t lds_bytes;
+};
+int validate_mx4_gemm(const Mx4GemmCall &c);
+int mx4_gemm_launch(const Mx4GemmCall &c, hipStream_t s);
+
 // Tracing helper: sets npairs [start, end] pairs to [UINT64_MAX, 0] and the
 // workgroup-record counter wg[0] to 0 (either pointer may be null).
 int trace_reset(uint64_t *stamps, int npairs, uint32_t *wg, hipStream_t s);

@@ -1,0 +1,89 @@
+"""Plain 64-bit implementations of the operators of a block, for the tests.
+
+Written from the definitions in include/occ.h, in numpy, sharing nothing with
+the library."""
+import math
+
+import numpy as np
+
+GRID = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def f64(t):
+    """A torch tensor as float64 on the host."""
+    return t.detach().double().cpu().numpy()
+
+
+# ---------------------------------------------------------------- MX4
+
+def mx4_kp(cols):
+    return (cols + 511) // 512 * 512
+
+
+def mx4_scale_exponent(block):
+    """e of a block's scale 2^e, or None where the block is not finite."""
+    top = np.max(np.abs(block)) if len(block) else 0.0
+    if not np.isfinite(top):
+        return None
+    return -127 if top == 0 else max(-127, min(127, math.frexp(top)[1] - 1 - 2))
+
+
+def mx4_code(a):
+    """Code (without sign) of a magnitude in units of the scale: nearest value, ties to the even code, at most 6."""
+    d = np.abs(GRID - a)
+    best = np.flatnonzero(d == d.min())
+    return 7 if a >= 6 else int(best[0] if len(best) == 1 or best[0] % 2 == 0 else best[1])
+
+
+def mx4_quantize(x):
+    """(codes as (rows, cols) values 0 .. 15, scale bytes as (rows, ceil(cols / 32))) of a float64 matrix."""
+    rows, cols = x.shape
+    nb = (cols + 31) // 32
+    codes = np.zeros((rows, cols), np.uint8)
+    scales = np.zeros((rows, nb), np.uint8)
+    for r in range(rows):
+        for b in range(nb):
+            blk = x[r, 32 * b:32 * b + 32]
+            e = mx4_scale_exponent(blk)
+            scales[r, b] = 255 if e is None else e + 127
+            if e is not None:
+                for i, v in enumerate(blk):
+                    codes[r, 32 * b + i] = mx4_code(abs(v) * 2.0 ** -e) + (8 if np.signbit(v) else 0)
+    return codes, scales
+
+
+def mx4_values(codes, scales):
+    """Values of codes (rows, cols) and scale bytes (rows, blocks)."""
+    v = GRID[codes & 7] * np.where(codes & 8, -1.0, 1.0)
+    s = np.where(scales == 255, np.nan, 2.0 ** (scales.astype(np.float64) - 127))
+    return v * np.repeat(s, 32, axis=1)[:, :codes.shape[1]]
+
+
+def mx4_unpack(code_bytes, scale_bytes, rows, cols):
+    """(codes, scales, what the padding holds) of the library's layout."""
+    kp = mx4_kp(cols)
+    assert code_bytes.shape == (rows, kp // 2) and scale_bytes.shape == ((rows + 15) // 16, kp // 2)
+    codes = np.empty((rows, kp), np.uint8)
+    codes[:, 0::2], codes[:, 1::2] = code_bytes & 15, code_bytes >> 4
+    rp, nb = (rows + 15) // 16 * 16, (cols + 31) // 32
+    scales = np.empty((rp, kp // 32), np.uint8)
+    for r in range(rp):
+        for b in range(kp // 32):
+            s, j, g = b // 16, b % 16 // 4, b % 4
+            scales[r, b] = scale_bytes[r // 16, 256 * s + 4 * (16 * g + r % 16) + j]
+    pads = [codes[:, cols:], scales[rows:], scales[:, nb:]]
+    return codes[:, :cols], scales[:rows, :nb], pads
+
+
+def mx4_pack(codes, scales):
+    """The library's layout of codes (rows, cols) and scale bytes (rows, blocks)."""
+    rows, cols = codes.shape
+    kp = mx4_kp(cols)
+    full = np.zeros((rows, kp), np.uint8)
+    full[:, :cols] = codes
+    out = np.zeros(((rows + 15) // 16, kp // 2), np.uint8)
+    for r in range(rows):
+        for b in range(scales.shape[1]):
+            s, j, g = b // 16, b % 16 // 4, b % 4
+            out[r // 16, 256 * s + 4 * (16 * g + r % 16) + j] = scales[r, b]
+    return full[:, 0::2] | (full[:, 1::2] << 4), out
