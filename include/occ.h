@@ -539,6 +539,57 @@ int occ_mx4_dequantize(const void *codes, const void *scales, int rows, int cols
 int occ_gemm_mx4(const void *A, const void *A_scales, const void *B, const void *B_scales, void *C, int dtype,
                  int M, int N, int K, size_t lds_bytes, void *stream);
 
+/*
+ * occ_norm_gate -- the norms after a block and before the next one, with the
+ * block's gate and the residual's scale, row by row (rows x D):
+ *   n = f * r1 * w_post,  r1 = 1 / sqrt(mean(f^2) + eps)     (post != 0; else n = f)
+ *   y = alpha * x + gate * n                                  (gate null: 1)
+ *   h = y * r2 * w_pre,   r2 = 1 / sqrt(mean(y^2) + eps)      (h null: not made)
+ * f, h, the weights and the gate are of type act; the residual x, y of type
+ * res: (OCC_BF16, OCC_BF16), (OCC_BF16, OCC_F32) or (OCC_F32, OCC_F32).  Sums and
+ * statistics are fp32, h comes from the unrounded y, each output is rounded once.
+ * A null weight is 1; post == 0 takes no w_post.  gate has `groups` rows of D;
+ * row r uses gate row r / (rows / groups): 1 for a gate per channel, `rows` for one
+ * per token, any divisor of rows between.  rstd (rows x 2 fp32, null: not stored)
+ * receives r1 and r2 (1 where a norm is not made), which the backward reads.
+ * ld_* are row pitches in elements, at least D; buffers are aligned to their
+ * elements.  1 <= D <= OCC_NORM_MAX_D, rows >= 0.
+ *
+ * occ_norm_gate_bwd -- gradients of the same from dy (of y, res) and dh (of h,
+ * act), either null for zero (not both), with f, y, rstd, the weights and the gate of
+ * the forward call:
+ *   D = dy + r2 (dh w_pre) - y r2^3 mean(dh w_pre y)
+ *   dx = alpha D,  df = r1 v - f r1^3 mean(v f),  v = gate D w_post
+ * and, summed in fp32 in a fixed order, dw_post, dw_pre (D) and dgate (groups x D).  A null
+ * output is not made.  workspace: occ_norm_gate_bwd_workspace_bytes(rows, D,
+ * groups) bytes, 16-byte aligned, need not be cleared (groups: 1 without a gate).
+ * Outputs must not overlap inputs or each other, except that y may be x, h may be f,
+ * dx may be dy and df may be f or dh (same pitch): each row is read before it is written.
+ */
+#define OCC_NORM_MAX_D 16384
+typedef struct occ_norm_args {
+  int rows, D;
+  int act, res;            /* OCC_BF16 or OCC_F32 */
+  int post;                /* 0: no norm after the block */
+  int groups;              /* rows of gate (ignored without one) */
+  float alpha, eps;
+  const void *f, *x;       /* x: forward only */
+  const void *w_post, *w_pre, *gate;
+  void *y, *h;             /* backward: y is an input, h is ignored */
+  float *rstd;             /* backward: an input */
+  size_t ld_f, ld_x, ld_y, ld_h;
+  /* backward only */
+  const void *dy, *dh;
+  void *df, *dx;
+  float *dw_post, *dw_pre, *dgate;
+  size_t ld_dy, ld_dh, ld_df, ld_dx;
+  void *workspace;
+  size_t workspace_bytes;
+} occ_norm_args;
+int occ_norm_gate(const occ_norm_args *args, void *stream);
+int occ_norm_gate_bwd(const occ_norm_args *args, void *stream);
+size_t occ_norm_gate_bwd_workspace_bytes(int rows, int D, int groups);
+
 /* Static string naming a status code. */
 const char *occ_strerror(int status);
 

@@ -82,6 +82,16 @@ class occ_overlap_result(ctypes.Structure):
                 "t_seq_median_ms", "t_ovl_median_ms", "t_seq_std_ms", "t_ovl_std_ms")]
 
 
+class occ_norm_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("rows", "D", "act", "res", "post", "groups")] + [
+        ("alpha", ctypes.c_float), ("eps", ctypes.c_float)] + [(n, ctypes.c_void_p) for n in (
+            "f", "x", "w_post", "w_pre", "gate", "y", "h", "rstd")] + [(n, ctypes.c_size_t) for n in (
+                "ld_f", "ld_x", "ld_y", "ld_h")] + [(n, ctypes.c_void_p) for n in (
+                    "dy", "dh", "df", "dx", "dw_post", "dw_pre", "dgate")] + [(n, ctypes.c_size_t) for n in (
+                        "ld_dy", "ld_dh", "ld_df", "ld_dx")] + [("workspace", ctypes.c_void_p),
+                                                                ("workspace_bytes", ctypes.c_size_t)]
+
+
 _lib = None
 _P = ctypes.c_void_p
 _SIGS = {
@@ -114,6 +124,9 @@ _SIGS = {
     "occ_mx4_dequantize": [_P, _P, ctypes.c_int, ctypes.c_int, _P, ctypes.c_int, ctypes.c_size_t, _P],
     "occ_gemm_mx4": [_P, _P, _P, _P, _P, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
                      ctypes.c_size_t, _P],
+    "occ_norm_gate": [ctypes.POINTER(occ_norm_args), _P],
+    "occ_norm_gate_bwd": [ctypes.POINTER(occ_norm_args), _P],
+    "occ_norm_gate_bwd_workspace_bytes": [ctypes.c_int, ctypes.c_int, ctypes.c_int],
     "occ_strerror": [ctypes.c_int],
     "occ_version": [],
 }
@@ -131,7 +144,7 @@ def lib():
             f = getattr(L, name)
             f.argtypes = args
             f.restype = (ctypes.c_char_p if name == "occ_strerror" else
-                         ctypes.c_size_t if name == "occ_overlap_workspace_bytes" else ctypes.c_int)
+                         ctypes.c_size_t if name.endswith("_workspace_bytes") else ctypes.c_int)
         v = L.occ_version()
         if (v >> 16, v & 0xFFFF) != ABI_VERSION:
             raise RuntimeError("%s has ABI version %d.%d, this binding expects %d.%d; rebuild it with "
@@ -594,3 +607,81 @@ def occ_gemm_mx4(A, B, C, lds_bytes=0, stream=None):
     _check(lib().occ_gemm_mx4(*a, *b, _ptr(C), kind, A.rows, B.rows, A.cols, int(lds_bytes), _stream(stream)),
            "occ_gemm_mx4")
     return C
+
+
+def _norm_args(f, res, w_post, w_pre, gate, alpha, eps, post):
+    """The fields forward and backward share; `res` is a tensor of the residual's type."""
+    n = occ_norm_args()
+    n.act, n.ld_f = _rows("f", f)
+    n.rows, n.D = f.shape
+    n.res = _float_type("the residual", res)
+    n.post, n.alpha, n.eps, n.groups = int(bool(post)), float(alpha), float(eps), 1
+    n.f = _ptr(f).value
+    for name, t in (("w_post", w_post), ("w_pre", w_pre)):
+        if t is not None:
+            if t.dtype != f.dtype or not t.is_cuda or tuple(t.shape) != (n.D,) or not t.is_contiguous():
+                raise ValueError("%s must be a contiguous (D,) GPU tensor of f's type" % name)
+            setattr(n, name, _ptr(t).value)
+    if gate is not None:
+        if gate.dtype != f.dtype or not gate.is_cuda or gate.dim() != 2 or gate.shape[1] != n.D \
+                or not gate.is_contiguous():
+            raise ValueError("gate must be a contiguous (groups, D) GPU tensor of f's type")
+        n.groups, n.gate = gate.shape[0], _ptr(gate).value
+    return n
+
+
+def _norm_rows(n, name, t, like):
+    """Row tensor `name` of like's type and (rows, D) into the arguments."""
+    if t is None:
+        return
+    if t.dtype != like.dtype:
+        raise ValueError("%s must be of type %s" % (name, like.dtype))
+    setattr(n, "ld_" + name, _rows(name, t, (n.rows, n.D))[1])
+    setattr(n, name, _ptr(t).value)
+
+
+def _f32(name, t, shape):
+    if t.dtype != torch.float32 or not t.is_cuda or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous float32 GPU tensor of shape %s" % (name, tuple(shape)))
+    return _ptr(t).value
+
+
+def occ_norm_gate(f, x, y, h=None, *, w_post=None, w_pre=None, gate=None, alpha=1.0, eps=1e-6, post=True, rstd=None,
+                  stream=None):
+    """y = alpha x + gate * norm(f) w_post and, with ``h``, h = norm(y) w_pre, for rows of f (a
+    block's output) and x (the residual).  gate: (groups, D), row r's is row r // (rows / groups).
+    ``rstd`` (rows, 2 fp32) receives what the backward needs.  Returns (y, h)."""
+    n = _norm_args(f, x, w_post, w_pre, gate, alpha, eps, post)
+    _norm_rows(n, "x", x, x)
+    _norm_rows(n, "y", y, x)
+    _norm_rows(n, "h", h, f)
+    if rstd is not None:
+        n.rstd = _f32("rstd", rstd, (n.rows, 2))
+    _check(lib().occ_norm_gate(ctypes.byref(n), _stream(stream)), "occ_norm_gate")
+    return y, h
+
+
+def occ_norm_gate_bwd_workspace_bytes(rows, D, groups=1):
+    """Device bytes occ_norm_gate_bwd needs."""
+    return int(lib().occ_norm_gate_bwd_workspace_bytes(int(rows), int(D), int(groups)))
+
+
+def occ_norm_gate_bwd(dy, dh, f, y, rstd, df=None, dx=None, *, w_post=None, w_pre=None, gate=None, alpha=1.0, post=True,
+                      dw_post=None, dw_pre=None, dgate=None, workspace=None, stream=None):
+    """Gradients of occ_norm_gate from dy and dh (either None for zero), with the forward's f,
+    y, rstd, weights and gate; each output None is not made.  df is of f's type, dx of
+    y's, the parameters' gradients are fp32.  Returns (df, dx)."""
+    n = _norm_args(f, y, w_post, w_pre, gate, alpha, 0.0, post)
+    _norm_rows(n, "y", y, y)
+    for name, t, like in (("dy", dy, y), ("dh", dh, f), ("df", df, f), ("dx", dx, y)):
+        _norm_rows(n, name, t, like)
+    n.rstd = _f32("rstd", rstd, (n.rows, 2))
+    for name, t, shape in (("dw_post", dw_post, (n.D,)), ("dw_pre", dw_pre, (n.D,)), ("dgate", dgate, (n.groups, n.D))):
+        if t is not None:
+            setattr(n, name, _f32(name, t, shape))
+    if workspace is not None:
+        if not workspace.is_cuda or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous GPU tensor")
+        n.workspace, n.workspace_bytes = _ptr(workspace).value, workspace.numel() * workspace.element_size()
+    _check(lib().occ_norm_gate_bwd(ctypes.byref(n), _stream(stream)), "occ_norm_gate_bwd")
+    return df, dx

@@ -95,6 +95,72 @@ int validate_mx4_gemm(const Mx4GemmCall &c) {
   return disjoint(out, in) ? OCC_OK : OCC_EALIAS;
 }
 
+namespace {
+
+// out may also be exactly one of the inputs (same pitch): in place, row by row.
+bool in_place(const Range &out, const Range &in, size_t ld_out, size_t ld_in) {
+  return out.p != nullptr && out.p == in.p && ld_out == ld_in;
+}
+
+}  // namespace
+
+int validate_norm(const occ_norm_args &n, bool backward) {
+  if (!float_type(n.act) || !float_type(n.res) || (n.act == OCC_F32 && n.res != OCC_F32)) return OCC_EINVAL;
+  if (n.rows < 0 || n.rows > (1 << 30) || n.D < 1 || n.D > OCC_NORM_MAX_D) return OCC_EINVAL;
+  if (n.post == 0 && (n.w_post != nullptr || (backward && n.dw_post != nullptr))) return OCC_EINVAL;
+  if (n.gate != nullptr &&
+      (n.groups < 1 || (n.rows > 0 ? n.groups > n.rows || n.rows % n.groups != 0 : n.groups > 65533)))
+    return OCC_EINVAL;
+  if (backward && n.gate == nullptr && n.dgate != nullptr) return OCC_EINVAL;
+  const size_t ea = type_bytes(n.act), er = type_bytes(n.res), D = (size_t)n.D;
+  const size_t gates = n.gate != nullptr ? (size_t)n.groups * D * ea : 0;
+  if (!aligned(n.w_post, ea) || !aligned(n.w_pre, ea) || !aligned(n.gate, ea)) return OCC_EINVAL;
+  struct Rows {
+    const void *p;
+    size_t ld, elem;
+    bool needed;
+  };
+  auto bad = [&](const Rows &r) {
+    return n.rows > 0 && ((r.needed && r.p == nullptr) || (r.p != nullptr && (!aligned(r.p, r.elem) || r.ld < D)));
+  };
+  auto range = [&](const Rows &r) {
+    return Range{r.p, n.rows == 0 ? 0 : ((size_t)(n.rows - 1) * r.ld + D) * r.elem};
+  };
+  const Rows f{n.f, n.ld_f, ea, true}, y{n.y, n.ld_y, er, !backward || n.dh != nullptr};
+  const Range wp{n.w_post, D * ea}, wq{n.w_pre, D * ea}, g{n.gate, gates};
+  const Range rstd{n.rstd, (size_t)n.rows * 8};
+  if (!aligned(n.rstd, 4) || bad(f) || bad(y)) return OCC_EINVAL;
+  if (!backward) {
+    const Rows x{n.x, n.ld_x, er, true}, h{n.h, n.ld_h, ea, false};
+    if (bad(x) || bad(h)) return OCC_EINVAL;
+    const Range none{nullptr, 0};
+    const Range in[] = {in_place(range(h), range(f), h.ld, f.ld) ? none : range(f),
+                        in_place(range(y), range(x), y.ld, x.ld) ? none : range(x), wp, wq, g};
+    const Range out[] = {range(y), range(h), rstd};
+    // in place or not, y stays off f and h off x
+    if (overlaps(range(y), range(f)) || overlaps(range(h), range(x))) return OCC_EALIAS;
+    return disjoint(out, in) ? OCC_OK : OCC_EALIAS;
+  }
+  const Rows dy{n.dy, n.ld_dy, er, false}, dh{n.dh, n.ld_dh, ea, false};
+  const Rows df{n.df, n.ld_df, ea, false}, dx{n.dx, n.ld_dx, er, false};
+  if (n.rows > 0 && ((n.dy == nullptr && n.dh == nullptr) || n.rstd == nullptr)) return OCC_EINVAL;
+  if (bad(dy) || bad(dh) || bad(df) || bad(dx)) return OCC_EINVAL;
+  if (!aligned(n.dw_post, 4) || !aligned(n.dw_pre, 4) || !aligned(n.dgate, 4)) return OCC_EINVAL;
+  const size_t need = norm_bwd_workspace(n.rows, n.D, n.gate != nullptr ? n.groups : 1);
+  if (need > 0 && (n.workspace == nullptr || !aligned(n.workspace, 16) || n.workspace_bytes < need)) return OCC_EINVAL;
+  const Range out[] = {range(df), range(dx), {n.dw_post, D * 4}, {n.dw_pre, D * 4},
+                       {n.dgate, n.gate != nullptr ? (size_t)n.groups * D * 4 : 0}, {n.workspace, need}};
+  const Range none{nullptr, 0};
+  const Range rest[] = {range(y), wp, wq, g, rstd, none};
+  if (!disjoint(out, rest)) return OCC_EALIAS;
+  for (const Range &o : out) {
+    if (overlaps(o, range(f)) && !(o.p == n.df && in_place(o, range(f), n.ld_df, n.ld_f))) return OCC_EALIAS;
+    if (overlaps(o, range(dh)) && !(o.p == n.df && in_place(o, range(dh), n.ld_df, n.ld_dh))) return OCC_EALIAS;
+    if (overlaps(o, range(dy)) && !(o.p == n.dx && in_place(o, range(dy), n.ld_dx, n.ld_dy))) return OCC_EALIAS;
+  }
+  return OCC_OK;
+}
+
 }  // namespace occ
 
 extern "C" {
@@ -120,6 +186,23 @@ int occ_gemm_mx4(const void *A, const void *A_scales, const void *B, const void 
   const occ::Mx4GemmCall c{A, A_scales, B, B_scales, C, dtype, M, N, K, lds_bytes};
   const int st = occ::validate_mx4_gemm(c);
   return st == OCC_OK ? occ::mx4_gemm_launch(c, static_cast<hipStream_t>(stream)) : st;
+}
+
+int occ_norm_gate(const occ_norm_args *args, void *stream) {
+  if (args == nullptr) return OCC_EINVAL;
+  const int st = occ::validate_norm(*args, false);
+  return st == OCC_OK ? occ::norm_gate_launch(*args, static_cast<hipStream_t>(stream)) : st;
+}
+
+int occ_norm_gate_bwd(const occ_norm_args *args, void *stream) {
+  if (args == nullptr) return OCC_EINVAL;
+  const int st = occ::validate_norm(*args, true);
+  return st == OCC_OK ? occ::norm_gate_bwd_launch(*args, static_cast<hipStream_t>(stream)) : st;
+}
+
+size_t occ_norm_gate_bwd_workspace_bytes(int rows, int D, int groups) {
+  if (rows < 0 || D < 1 || D > OCC_NORM_MAX_D || groups < 1 || groups > (rows > 0 ? rows : 1)) return 0;
+  return occ::norm_bwd_workspace(rows, D, groups);
 }
 
 }  // extern "C"

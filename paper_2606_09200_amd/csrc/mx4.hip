@@ -3,54 +3,13 @@
 // q(x)_b = RNE_e2m1(x_b / 2^e), e = floor(log2(max |x_b|)) - 2 over blocks of 32.
 // All that is computed is a maximum of exponents; both kernels are bound by the
 // bytes they move (2 or 4 in, 17/32 out per value and orientation).
-#include "gemm_common.h"
+#include "block_util.h"
 #include "mx4.h"
 
 namespace occ {
 namespace {
 
-typedef uint32_t u32x4_e2 __attribute__((ext_vector_type(4), aligned(2)));  // 16 bytes at any element
-typedef uint32_t u32x4_e4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-// By value: a bit cast of a vector's element itself would read its first.
-__device__ __forceinline__ float as_float(uint32_t w) { return __builtin_bit_cast(float, w); }
-__device__ __forceinline__ float bf16_lo(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t w) { return __builtin_bit_cast(float, w & 0xFFFF0000u); }
-
-// 8 consecutive values of a row as binary32, `left` of them exist (the others are zero).
-__device__ __forceinline__ void load8(const uint16_t *p, int left, float (&v)[8]) {
-  if (left >= 8) {
-    const u32x4_e2 w = *reinterpret_cast<const u32x4_e2 *>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = bf16_lo(w[i]);
-      v[2 * i + 1] = bf16_hi(w[i]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? bf16_lo(p[i]) : 0.f;
-  }
-}
-__device__ __forceinline__ void load8(const float *p, int left, float (&v)[8]) {
-  u32x4 a = {0u, 0u, 0u, 0u}, b = {0u, 0u, 0u, 0u};
-  if (left >= 8) {
-    a = *reinterpret_cast<const u32x4_e4 *>(p);
-    b = *reinterpret_cast<const u32x4_e4 *>(p + 4);
-  } else {
-    const uint32_t *w = reinterpret_cast<const uint32_t *>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (i < left) a[i] = w[i];
-      if (4 + i < left) b[i] = w[4 + i];
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[i] = as_float(a[i]);
-    v[4 + i] = as_float(b[i]);
-  }
-}
 
 __device__ __forceinline__ uint32_t mag(float f) { return __builtin_bit_cast(uint32_t, f) & 0x7FFFFFFFu; }
 
@@ -204,35 +163,7 @@ __global__ __launch_bounds__(256) void mx4_dequant_kernel(const uint8_t *__restr
       const uint32_t b = m >= 2u ? ((m >> 1) + 126u) << 23 | (m & 1u) << 22 : m == 1u ? 0x3F000000u : 0u;
       v[e] = __builtin_bit_cast(float, b | (q >> 3) << 31) * sc;
     }
-    E *o = out + (size_t)row * ld + c;
-    const int left = cols - c;
-    if constexpr (sizeof(E) == 2) {
-      if (left >= 8) {
-        u32x4 p;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-        __builtin_nontemporal_store(p, reinterpret_cast<u32x4_e2 *>(o));
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e < left) o[e] = to_bf16(v[e]);
-      }
-    } else {
-      if (left >= 8) {
-        u32x4 p, q;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[e] = __builtin_bit_cast(uint32_t, v[e]);
-          q[e] = __builtin_bit_cast(uint32_t, v[4 + e]);
-        }
-        __builtin_nontemporal_store(p, reinterpret_cast<u32x4_e4 *>(o));
-        __builtin_nontemporal_store(q, reinterpret_cast<u32x4_e4 *>(o + 4));
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e < left) o[e] = v[e];
-      }
-    }
+    store8(out + (size_t)row * ld + c, cols - c, v);
   }
 }
 

@@ -112,6 +112,42 @@ struct Mx4GemmCall {
 int validate_mx4_gemm(const Mx4GemmCall &c);
 int mx4_gemm_launch(const Mx4GemmCall &c, hipStream_t s);
 
+struct NormFwd {
+  int rows, D;
+  bool post;
+  float alpha, eps;
+  const void *f, *x, *w_post, *w_pre, *gate;
+  int rows_per_gate;
+  void *y, *h;
+  float *rstd;
+  size_t ld_f, ld_x, ld_y, ld_h;
+};
+struct NormBwd {
+  int rows, D;
+  bool post;
+  float alpha;
+  const void *f, *y, *dy, *dh, *w_post, *w_pre, *gate;
+  const float *rstd;
+  void *df, *dx;
+  float *dw_post, *dw_pre, *dgate;
+  size_t ld_f, ld_y, ld_dy, ld_dh, ld_df, ld_dx;
+  int rows_per_gate, run, per_gate, gates;  // see NormSplit
+  float *part1, *part2, *part3;             // runs x D each; part3 only where several gates have several runs
+};
+// The backward's runs of rows: either `per_gate` runs of at most `run` rows within each gate's
+// rows, or (direct) runs of `gates` whole gates.  rt: threads a run.
+struct NormSplit {
+  int rt, runs, rows_per_gate;
+  bool direct;
+  int run, per_gate, gates;
+};
+constexpr int kNormRuns = 256;
+NormSplit norm_split(int rows, int D, int groups);
+size_t norm_bwd_workspace(int rows, int D, int groups);
+int validate_norm(const occ_norm_args &n, bool backward);
+int norm_gate_launch(const occ_norm_args &n, hipStream_t s);
+int norm_gate_bwd_launch(const occ_norm_args &n, hipStream_t s);
+
 // Tracing helper: sets npairs [start, end] pairs to [UINT64_MAX, 0] and the
 // workgroup-record counter wg[0] to 0 (either pointer may be null).
 int trace_reset(uint64_t *stamps, int npairs, uint32_t *wg, hipStream_t s);

@@ -87,3 +87,44 @@ def mx4_pack(codes, scales):
             s, j, g = b // 16, b % 16 // 4, b % 4
             out[r // 16, 256 * s + 4 * (16 * g + r % 16) + j] = scales[r, b]
     return full[:, 0::2] | (full[:, 1::2] << 4), out
+
+
+# ---------------------------------------------------------------- norms around a block
+
+def gate_rows(gate, rows, D):
+    """One gate row per row (ones without a gate)."""
+    return np.ones((rows, D)) if gate is None else np.repeat(gate, rows // gate.shape[0], axis=0) if rows else np.ones((0, D))
+
+
+def norm_gate(f, x, w_post, w_pre, gate, alpha, eps, post=True):
+    """y, h, rstd (rows, 2) in 64 bits."""
+    rows, D = f.shape
+    one = np.ones(D)
+    r1 = 1 / np.sqrt((f * f).mean(1) + eps) if post else np.ones(rows)
+    n = f * r1[:, None] * (one if w_post is None else w_post)
+    y = alpha * x + gate_rows(gate, rows, D) * n
+    r2 = 1 / np.sqrt((y * y).mean(1) + eps)
+    return y, y * r2[:, None] * (one if w_pre is None else w_pre), np.stack([r1, r2], 1)
+
+
+def norm_gate_bwd(dy, dh, f, y, rstd, w_post, w_pre, gate, alpha, post=True):
+    """Gradients and, for each, the sum of the magnitudes it is made of."""
+    rows, D = f.shape
+    w1, w2 = (np.ones(D) if w is None else w for w in (w_post, w_pre))
+    g = gate_rows(gate, rows, D)
+    r1, r2 = rstd[:, :1], rstd[:, 1:]
+    dy, dh = (np.zeros((rows, D)) if t is None else t for t in (dy, dh))
+    u, yn, fn = dh * w2, y * r2, f * r1
+    mean = lambda t: t.mean(1, keepdims=True)
+    d = dy + r2 * (u - yn * mean(u * yn))
+    d_mag = abs(dy) + r2 * (abs(u) + abs(yn) * mean(abs(u * yn)))
+    v, v_mag = d * g * w1, d_mag * abs(g * w1)
+    out = {"dx": alpha * d, "df": r1 * (v - fn * mean(v * fn)) if post else v,
+           "dw_post": (d * g * fn).sum(0), "dw_pre": (dh * yn).sum(0)}
+    mag = {"dx": abs(alpha) * d_mag, "df": r1 * (v_mag + (abs(fn) * mean(v_mag * abs(fn)) if post else 0)),
+           "dw_post": (d_mag * abs(g * fn)).sum(0), "dw_pre": abs(dh * yn).sum(0)}
+    if gate is not None:
+        k = gate.shape[0]
+        out["dgate"] = (d * fn).reshape(k, -1, D).sum(1) * w1
+        mag["dgate"] = (d_mag * abs(fn)).reshape(k, -1, D).sum(1) * abs(w1)
+    return out, mag
