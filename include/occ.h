@@ -590,6 +590,49 @@ int occ_norm_gate(const occ_norm_args *args, void *stream);
 int occ_norm_gate_bwd(const occ_norm_args *args, void *stream);
 size_t occ_norm_gate_bwd_workspace_bytes(int rows, int D, int groups);
 
+/*
+ * occ_moe -- a whole mixture-of-experts layer for a few tokens (decoding), as one
+ * GPU that holds the experts runs it:
+ *   l = x router^T (fp32);  the top_k largest of l (ties to the lower index)
+ *   p = softmax(l);  w_j = p_j, or p_j over the sum of the top_k (renorm != 0)
+ *   y = sum_j w_j w_down_j (silu(w_gate_j x) * (w_up_j x))
+ * x, router and y are bf16, the router's logits, softmax and all sums fp32; the
+ * hidden activations are rounded to bf16 between the two products.  Weights are
+ * bf16 or MX4 (weight_type OCC_BF16 or OCC_MX4; MX4 scales in s_*), gate and up
+ * experts x I x H, down experts x H x I; bf16 matrices lie stride_* elements apart
+ * (0: packed), MX4 ones packed.  mask (tokens bytes, null: all ones): a token with
+ * 0 takes no part, its y is 0, its ids -1 and its weights 0.  ids and weights
+ * (tokens x top_k, in descending order; null: not stored) receive the routing.
+ * A NaN logit is below every other; its token's weights are NaN.
+ * Limits: tokens <= 64, experts <= 512, top_k <= 16 and <= experts; H and I
+ * multiples of 8 up to 65536; x, router and bf16 weights 16-byte aligned with ld_x
+ * and stride_* multiples of 8; y aligned to its elements.
+ * workspace: occ_moe_workspace_bytes(...) bytes, 16-byte aligned, zeroed once
+ * before its first use (a complete call leaves it ready for the next, of any
+ * sizes it is large enough for); calls that share one must not overlap.  Neither
+ * kernel waits for one that has not started, so calls on several streams, each with its
+ * own workspace, can share the GPU.
+ */
+#define OCC_MOE_MAX_TOKENS 64
+typedef struct occ_moe_args {
+  int tokens, H, I, experts, top_k;
+  int weight_type;
+  int renorm;
+  const void *x, *router;
+  const void *w_gate, *w_up, *w_down;
+  const void *s_gate, *s_up, *s_down;
+  size_t stride_gate, stride_up, stride_down;
+  const void *mask;
+  void *y;
+  int32_t *ids;
+  float *weights;
+  size_t ld_x, ld_y;
+  void *workspace;
+  size_t workspace_bytes;
+} occ_moe_args;
+int occ_moe(const occ_moe_args *args, void *stream);
+size_t occ_moe_workspace_bytes(int tokens, int H, int I, int experts, int top_k);
+
 /* Static string naming a status code. */
 const char *occ_strerror(int status);
 

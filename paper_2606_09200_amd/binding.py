@@ -92,6 +92,15 @@ class occ_norm_args(ctypes.Structure):
                                                                 ("workspace_bytes", ctypes.c_size_t)]
 
 
+class occ_moe_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("tokens", "H", "I", "experts", "top_k", "weight_type", "renorm")] + [
+        (n, ctypes.c_void_p) for n in ("x", "router", "w_gate", "w_up", "w_down", "s_gate", "s_up", "s_down")] + [
+            (n, ctypes.c_size_t) for n in ("stride_gate", "stride_up", "stride_down")] + [
+                (n, ctypes.c_void_p) for n in ("mask", "y", "ids", "weights")] + [
+                    ("ld_x", ctypes.c_size_t), ("ld_y", ctypes.c_size_t), ("workspace", ctypes.c_void_p),
+                    ("workspace_bytes", ctypes.c_size_t)]
+
+
 _lib = None
 _P = ctypes.c_void_p
 _SIGS = {
@@ -127,6 +136,8 @@ _SIGS = {
     "occ_norm_gate": [ctypes.POINTER(occ_norm_args), _P],
     "occ_norm_gate_bwd": [ctypes.POINTER(occ_norm_args), _P],
     "occ_norm_gate_bwd_workspace_bytes": [ctypes.c_int, ctypes.c_int, ctypes.c_int],
+    "occ_moe": [ctypes.POINTER(occ_moe_args), _P],
+    "occ_moe_workspace_bytes": [ctypes.c_int] * 5,
     "occ_strerror": [ctypes.c_int],
     "occ_version": [],
 }
@@ -685,3 +696,60 @@ def occ_norm_gate_bwd(dy, dh, f, y, rstd, df=None, dx=None, *, w_post=None, w_pr
         n.workspace, n.workspace_bytes = _ptr(workspace).value, workspace.numel() * workspace.element_size()
     _check(lib().occ_norm_gate_bwd(ctypes.byref(n), _stream(stream)), "occ_norm_gate_bwd")
     return df, dx
+
+
+def occ_moe_workspace_bytes(tokens, H, I, experts, top_k):
+    """Device bytes occ_moe needs (zeroed once)."""
+    return int(lib().occ_moe_workspace_bytes(int(tokens), int(H), int(I), int(experts), int(top_k)))
+
+
+def occ_moe(x, router, w_gate, w_up, w_down, y, *, top_k, workspace, ids=None, weights=None, renorm=True, mask=None,
+            stream=None):
+    """y = a mixture-of-experts layer of x (tokens x H, bf16, up to 64 tokens): softmax router
+    (experts x H), top_k experts of silu(w_gate x) * (w_up x) and w_down.  Weights are bf16
+    tensors (experts, I, H), (experts, I, H), (experts, H, I) or Mx4 batches of the same.
+    ids / weights (tokens, top_k; int32 / float32) receive the routing; mask: a bool or uint8
+    per token.  workspace: a GPU tensor zeroed once.  Returns y."""
+    a = occ_moe_args()
+    if x.dtype != torch.bfloat16 or y.dtype != torch.bfloat16:
+        raise ValueError("x and y must be bfloat16 GPU tensors")
+    _, a.ld_x = _rows("x", x)
+    a.tokens, a.H = x.shape
+    _, a.ld_y = _rows("y", y, x.shape)
+    if router.dtype != torch.bfloat16 or not router.is_cuda or router.dim() != 2 or router.shape[1] != a.H \
+            or not router.is_contiguous():
+        raise ValueError("router must be a contiguous (experts, H) bfloat16 GPU tensor")
+    a.experts, a.top_k, a.renorm = router.shape[0], int(top_k), int(bool(renorm))
+    mx = isinstance(w_gate, Mx4)
+    a.weight_type = OCC_MX4 if mx else OCC_BF16
+    a.I = w_gate.rows if mx else w_gate.shape[1] if w_gate.dim() == 3 else -1
+    for name, w, rows, cols in (("gate", w_gate, a.I, a.H), ("up", w_up, a.I, a.H), ("down", w_down, a.H, a.I)):
+        if mx:
+            if not isinstance(w, Mx4) or (w.rows, w.cols) != (rows, cols) or tuple(w.codes.shape[:-2]) != (a.experts,) \
+                    or not w.codes.is_cuda:
+                raise ValueError("w_%s must be an Mx4 batch of %d matrices %d x %d" % (name, a.experts, rows, cols))
+            setattr(a, "w_" + name, _ptr(w.codes).value)
+            setattr(a, "s_" + name, _ptr(w.scales).value)
+        else:
+            if not isinstance(w, torch.Tensor) or w.dtype != torch.bfloat16 or not w.is_cuda \
+                    or tuple(w.shape) != (a.experts, rows, cols) or w.stride(2) != 1 or w.stride(1) != cols:
+                raise ValueError("w_%s must be a bfloat16 GPU tensor (%d, %d, %d) of contiguous matrices"
+                                 % (name, a.experts, rows, cols))
+            setattr(a, "w_" + name, _ptr(w).value)
+            setattr(a, "stride_" + name, w.stride(0) if a.experts > 1 else 0)
+    for name, t, dtype in (("ids", ids, torch.int32), ("weights", weights, torch.float32)):
+        if t is not None:
+            if t.dtype != dtype or not t.is_cuda or tuple(t.shape) != (a.tokens, a.top_k) or not t.is_contiguous():
+                raise ValueError("%s must be a contiguous (tokens, top_k) %s GPU tensor" % (name, dtype))
+            setattr(a, name, _ptr(t).value)
+    if mask is not None:
+        if mask.dtype not in (torch.bool, torch.uint8) or not mask.is_cuda or tuple(mask.shape) != (a.tokens,) \
+                or not mask.is_contiguous():
+            raise ValueError("mask must be a contiguous bool or uint8 GPU tensor, one per token")
+        a.mask = _ptr(mask).value
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous GPU tensor")
+    a.x, a.router, a.y = _ptr(x).value, _ptr(router).value, _ptr(y).value
+    a.workspace, a.workspace_bytes = _ptr(workspace).value, workspace.numel() * workspace.element_size()
+    _check(lib().occ_moe(ctypes.byref(a), _stream(stream)), "occ_moe")
+    return y

@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libocc.so")
 SOURCES = ["abi.hip", "gemm.hip", "comm.hip", "overlap.hip", "abi_block.hip", "mx4.hip", "gemm_mx4.hip",
-           "norm.hip"]
+           "norm.hip", "moe.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

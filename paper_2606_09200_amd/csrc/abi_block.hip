@@ -161,6 +161,42 @@ int validate_norm(const occ_norm_args &n, bool backward) {
   return OCC_OK;
 }
 
+int validate_moe(const occ_moe_args &a) {
+  const int st = validate_moe_sizes(a.tokens, a.H, a.I, a.experts, a.top_k);
+  if (st != OCC_OK) return st;
+  const bool mx = a.weight_type == OCC_MX4;
+  if (!mx && a.weight_type != OCC_BF16) return OCC_EINVAL;
+  if (a.tokens == 0) return OCC_OK;
+  const size_t H = (size_t)a.H, I = (size_t)a.I, E = (size_t)a.experts, T = (size_t)a.tokens, k = (size_t)a.top_k;
+  if (a.x == nullptr || a.router == nullptr || a.y == nullptr || !aligned(a.x, 16) || !aligned(a.router, 16) ||
+      !aligned(a.y, 2) || !aligned(a.ids, 4) || !aligned(a.weights, 4))
+    return OCC_EINVAL;
+  // rows of x are addressed with 32-bit byte offsets
+  if (a.ld_x < H || a.ld_x % 8 != 0 || a.ld_x > (1u << 23) || a.ld_y < H) return OCC_EINVAL;
+  struct {
+    const void *w, *s;
+    size_t stride, rows, cols;
+  } m[3] = {{a.w_gate, a.s_gate, a.stride_gate, I, H}, {a.w_up, a.s_up, a.stride_up, I, H}, {a.w_down, a.s_down, a.stride_down, H, I}};
+  Range in[9] = {{a.x, ((T - 1) * a.ld_x + H) * 2}, {a.router, E * H * 2}, {a.mask, T}};
+  for (int i = 0; i < 3; ++i) {
+    if (m[i].w == nullptr || !aligned(m[i].w, 16)) return OCC_EINVAL;
+    if (mx) {
+      if (m[i].s == nullptr || !aligned(m[i].s, 16) || m[i].stride != 0) return OCC_EINVAL;
+      in[3 + 2 * i] = {m[i].w, E * OCC_MX4_CODE_BYTES(m[i].rows, m[i].cols)};
+      in[4 + 2 * i] = {m[i].s, E * OCC_MX4_SCALE_BYTES(m[i].rows, m[i].cols)};
+    } else {
+      const size_t one = m[i].rows * m[i].cols, stride = m[i].stride == 0 ? one : m[i].stride;
+      if (stride < one || stride % 8 != 0) return OCC_EINVAL;
+      in[3 + 2 * i] = {m[i].w, ((E - 1) * stride + one) * 2};
+      in[4 + 2 * i] = {nullptr, 0};
+    }
+  }
+  const size_t need = moe_workspace(a.tokens, a.H, a.I, a.experts, a.top_k);
+  if (a.workspace == nullptr || !aligned(a.workspace, 16) || a.workspace_bytes < need) return OCC_EINVAL;
+  const Range out[] = {{a.y, ((T - 1) * a.ld_y + H) * 2}, {a.ids, T * k * 4}, {a.weights, T * k * 4}, {a.workspace, need}};
+  return disjoint(out, in) ? OCC_OK : OCC_EALIAS;
+}
+
 }  // namespace occ
 
 extern "C" {
@@ -203,6 +239,17 @@ int occ_norm_gate_bwd(const occ_norm_args *args, void *stream) {
 size_t occ_norm_gate_bwd_workspace_bytes(int rows, int D, int groups) {
   if (rows < 0 || D < 1 || D > OCC_NORM_MAX_D || groups < 1 || groups > (rows > 0 ? rows : 1)) return 0;
   return occ::norm_bwd_workspace(rows, D, groups);
+}
+
+int occ_moe(const occ_moe_args *args, void *stream) {
+  if (args == nullptr) return OCC_EINVAL;
+  const int st = occ::validate_moe(*args);
+  return st == OCC_OK ? occ::moe_launch(*args, static_cast<hipStream_t>(stream)) : st;
+}
+
+size_t occ_moe_workspace_bytes(int tokens, int H, int I, int experts, int top_k) {
+  if (tokens == 0 || occ::validate_moe_sizes(tokens, H, I, experts, top_k) != OCC_OK) return 0;
+  return occ::moe_workspace(tokens, H, I, experts, top_k);
 }
 
 }  // extern "C"

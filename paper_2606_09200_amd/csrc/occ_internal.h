@@ -148,6 +148,47 @@ int validate_norm(const occ_norm_args &n, bool backward);
 int norm_gate_launch(const occ_norm_args &n, hipStream_t s);
 int norm_gate_bwd_launch(const occ_norm_args &n, hipStream_t s);
 
+struct MoeCounters {
+  uint32_t arrived;  // router workgroups that are done; zero between calls
+  uint32_t ticket;   // next task of the experts' queue
+  uint32_t up_done;  // finished tasks of the first kind
+  uint32_t active;   // experts that some token picked
+};
+struct MoeExpert {
+  uint32_t id, first;  // its index, and its first row of the hidden activations
+  uint32_t tokens[2];  // its tokens, a bit each
+};
+struct MoeMatrix {
+  const void *w;
+  const uint8_t *scales;
+  size_t stride, scale_stride;  // bytes from expert to expert
+};
+struct MoeCall {
+  int T, H, I, E, k;
+  bool renorm;
+  int slices, row_blocks, max_segments, ld_x;
+  const uint16_t *x, *router;
+  MoeMatrix gate, up, down;
+  const uint8_t *mask;
+  uint16_t *y;
+  size_t ld_y;
+  int32_t *ids;
+  float *weights;
+  // workspace
+  MoeCounters *count;
+  MoeExpert *plan;
+  int *token_of;     // token of each row of the hidden activations
+  float *gate_of;    // experts x 64: a token's weight
+  uint32_t *joined;  // per 16 rows of y: finished parts
+  float *part;       // partial logits
+  uint16_t *hidden;  // rows x I, bf16
+  float *sums;       // parts x T x H
+};
+int validate_moe_sizes(int T, int H, int I, int E, int k);
+int validate_moe(const occ_moe_args &a);
+size_t moe_workspace(int T, int H, int I, int E, int k);
+int moe_launch(const occ_moe_args &a, hipStream_t s);
+
 // Tracing helper: sets npairs [start, end] pairs to [UINT64_MAX, 0] and the
 // workgroup-record counter wg[0] to 0 (either pointer may be null).
 int trace_reset(uint64_t *stamps, int npairs, uint32_t *wg, hipStream_t s);

@@ -128,3 +128,41 @@ def norm_gate_bwd(dy, dh, f, y, rstd, w_post, w_pre, gate, alpha, post=True):
         out["dgate"] = (d * fn).reshape(k, -1, D).sum(1) * w1
         mag["dgate"] = (d_mag * abs(fn)).reshape(k, -1, D).sum(1) * abs(w1)
     return out, mag
+
+
+# ---------------------------------------------------------------- expert layer
+
+def route(logits, top_k, renorm, mask):
+    """ids (-1 for masked tokens) and weights: the largest logits, a tie to the lower index, a NaN last."""
+    T, E = logits.shape
+    ids, w = np.full((T, top_k), -1), np.zeros((T, top_k))
+    for t in range(T):
+        if mask is not None and not mask[t]:
+            continue
+        l = logits[t]
+        pick = sorted(range(E), key=lambda e: (-l[e] if l[e] == l[e] else np.inf, l[e] != l[e], e))[:top_k]
+        with np.errstate(all="ignore"):
+            p = np.exp(l - l[pick[0]])
+            p = p / p.sum()
+            ids[t], w[t] = pick, p[pick] / p[pick].sum() if renorm else p[pick]
+    return ids, w
+
+
+def moe(x, ids, w, gate, up, down):
+    """y, and how far rounding may take it: the sums of magnitudes of its binary32 sums and of the
+    hidden activations' bf16 rounding.  gate, up, down: lists of matrices."""
+    T, H = x.shape
+    y, tol = np.zeros((T, H)), np.zeros((T, H))
+    for t in range(T):
+        for j, e in enumerate(ids[t]):
+            if e < 0:
+                continue
+            g, u = gate[e] @ x[t], up[e] @ x[t]
+            eg, eu = (H * 2.0 ** -23 * (abs(m[e]) @ abs(x[t])) for m in (gate, up))
+            s = g / (1 + np.exp(-g))
+            h = s * u
+            # |silu'| < 1.1; a few roundings of the epilogue; one to bf16
+            eh = 1.1 * abs(u) * eg + abs(s) * eu + (2.0 ** -8 + 2.0 ** -20) * abs(h)
+            y[t] += w[t, j] * (down[e] @ h)
+            tol[t] += w[t, j] * (abs(down[e]) @ (eh + (len(h) * 2.0 ** -23 + 2.0 ** -16) * abs(h)))
+    return y, tol + 2.0 ** -8 * abs(y)
