@@ -4,10 +4,12 @@
 //   y = sum_j w_j Wd_j (silu(Wg_j x) * Wu_j x),  w_j = p_j, or p_j / sum of the k
 //
 // With at most 64 tokens the layer is bound by reading the router and the weights of
-// the experts that some token picked, once.  Two kernels: the router, whose last
-// workgroup picks the experts and lists each one's tokens, and the experts, whose
-// workgroups take tasks from a queue: first all (expert, 16 rows of Wg and Wu), then
-// all (16 rows of Wd, experts).
+// the experts that some token picked, once.  Three launches: the router, whose last
+// workgroup picks the experts and lists each one's tokens, and the two products of the
+// picked experts, the host not knowing which.  The two products in one launch, the second
+// waiting on the device for the first, were slower: tasks then have to come from a
+// queue (a workgroup may wait only for work that a running one holds), whose counter
+// answers one workgroup every 11 ns (512 of them: 5.8 us), and a kernel's start costs 2.3.
 #include "block_util.h"
 #include "mx4.h"
 
@@ -66,17 +68,25 @@ __device__ __forceinline__ uint32_t wave_pick(uint32_t v) {
 
 // ---------------------------------------------------------------------------
 // Router.  A workgroup multiplies 16 experts' rows with all tokens over one of `slices`
-// slices of H, its 8 waves 128 columns each in turn; the partial logits go to
+// slices of H, its 16 waves 128 columns each in turn; the partial logits go to
 // part[slice][token][expert].  The workgroup that arrives last adds the slices in
 // order and picks: a wave per token at a time, lane l holding experts l, l + 64, ...
-// Logits order as integers, a NaN below everything (its token's weights become NaN
-// with the sum); equal ones go to the lower index.
-template <int TB>
-__global__ __launch_bounds__(kThreads) void moe_route_kernel(MoeCall c) {
-  __shared__ f32x4 partial[kWaves][TB][64];
+// (PER of them), with the logits of GROUP tokens on their way at once: they come from
+// other XCDs' writes through memory, and waiting for each token's in turn made this
+// kernel 33 us long for 64 tokens.  Logits order as integers, a NaN below everything
+// (its token's weights become NaN with the sum); equal ones go to the lower index.
+constexpr int kRouteThreads = 1024, kRouteWaves = kRouteThreads / 64;
+
+template <int TB, int PER>
+__global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(MoeCall c) {
+  constexpr int GROUP = PER == 1 ? 4 : PER == 2 ? 2 : 1;
+  __shared__ f32x4 partial[kRouteWaves][TB][64];
   __shared__ uint32_t last;
   __shared__ uint32_t picked[kMaxExperts][2];  // the tokens of an expert, a bit each
-  __shared__ uint32_t wave_active[kWaves], wave_pairs[kWaves];
+  __shared__ uint32_t first_of[kMaxExperts];   // its first row of the hidden activations
+  __shared__ uint32_t wave_active[kRouteWaves], wave_pairs[kRouteWaves];
+  __shared__ float weight_of[kMaxTokens][kMaxTopK];
+  __shared__ int id_of[kMaxTokens][kMaxTopK];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, g = lane >> 4;
   const int eb = blockIdx.x / c.slices, slice = blockIdx.x % c.slices;
@@ -91,7 +101,7 @@ __global__ __launch_bounds__(kThreads) void moe_route_kernel(MoeCall c) {
 #pragma unroll
     for (int b = 0; b < TB; ++b) xo[b] = b * 16 + l16 < c.T ? (uint32_t)(b * 16 + l16) * (uint32_t)c.ld_x * 2u : kNowhere;
     const int steps = (c.H + 127) / 128;
-    for (int s = slice * kWaves + wave; s < steps; s += c.slices * kWaves) {
+    for (int s = slice * kRouteWaves + wave; s < steps; s += c.slices * kRouteWaves) {
       u32x4 w[4], x[TB][4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -112,7 +122,7 @@ __global__ __launch_bounds__(kThreads) void moe_route_kernel(MoeCall c) {
     if (wave < TB) {
       f32x4 v = partial[0][wave][lane];
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) v = v + partial[w][wave][lane];
+      for (int w = 1; w < kRouteWaves; ++w) v = v + partial[w][wave][lane];
       const int t = wave * 16 + l16;
       if (t < c.T) {
         float *p = c.part + ((size_t)slice * c.T + t) * c.E;
@@ -127,70 +137,86 @@ __global__ __launch_bounds__(kThreads) void moe_route_kernel(MoeCall c) {
   __syncthreads();
   if (!last) return;
 
-  if (threadIdx.x == 0) {  // for the next call's router and this call's experts
-    put_device(&c.count->arrived, 0u);
-    c.count->ticket = 0;
-    c.count->up_done = 0;
-  }
-  for (int i = threadIdx.x; i < c.row_blocks; i += kThreads) c.joined[i] = 0;
-  for (int i = threadIdx.x; i < c.E; i += kThreads) picked[i][0] = picked[i][1] = 0u;
+  if (threadIdx.x == 0) put_device(&c.count->arrived, 0u);  // for the next call
+  for (int i = threadIdx.x; i < c.row_blocks; i += kRouteThreads) c.joined[i] = 0;
+  for (int i = threadIdx.x; i < c.E; i += kRouteThreads) picked[i][0] = picked[i][1] = 0u;
   __syncthreads();
-  constexpr int PER = kMaxExperts / 64;
-  for (int t = wave; t < c.T; t += kWaves) {
-    if (c.mask != nullptr && c.mask[t] == 0) {
-      if (lane < c.k) {
-        if (c.ids != nullptr) c.ids[t * c.k + lane] = -1;
-        if (c.weights != nullptr) c.weights[t * c.k + lane] = 0.f;
-      }
-      continue;
-    }
-    float l[PER];
-    uint32_t key[PER];
+  for (int t0 = wave * GROUP; t0 < c.T; t0 += kRouteWaves * GROUP) {
+    float logit[GROUP][PER];
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const int e = j * 64 + lane;
-      l[j] = 0.f;
-      key[j] = 0u;
-      if (j * 64 < c.E && e < c.E) {
-        const float *p = c.part + (size_t)t * c.E + e;
-        for (int s = 0; s < c.slices; ++s) l[j] = l[j] + get_device(p + (size_t)s * c.T * c.E);
+    for (int q = 0; q < GROUP; ++q)
+#pragma unroll
+      for (int j = 0; j < PER; ++j) logit[q][j] = 0.f;
+#pragma unroll 2
+    for (int s = 0; s < c.slices; ++s) {
+      float v[GROUP][PER];
+#pragma unroll
+      for (int q = 0; q < GROUP; ++q)
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+          const int t = min(t0 + q, c.T - 1), e = min(j * 64 + lane, c.E - 1);
+          v[q][j] = get_device(c.part + ((size_t)s * c.T + t) * c.E + e);
+        }
+#pragma unroll
+      for (int q = 0; q < GROUP; ++q)
+#pragma unroll
+        for (int j = 0; j < PER; ++j) logit[q][j] = logit[q][j] + v[q][j];
+    }
+#pragma unroll
+    for (int q = 0; q < GROUP; ++q) {
+      const int t = t0 + q;
+      if (t >= c.T) break;
+      if (c.mask != nullptr && c.mask[t] == 0) {
+        if (lane < c.k) {
+          if (c.ids != nullptr) c.ids[t * c.k + lane] = -1;
+          if (c.weights != nullptr) c.weights[t * c.k + lane] = 0.f;
+          id_of[t][lane] = -1;
+        }
+        continue;
+      }
+      float l[PER];
+      uint32_t key[PER];
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        l[j] = logit[q][j];
         // ascending integers, 1 and above; what is taken or missing is 0
         const uint32_t u = __builtin_bit_cast(uint32_t, l[j]);
-        key[j] = l[j] != l[j] ? 1u : (u >> 31 ? ~u : u | 0x80000000u);
+        key[j] = j * 64 + lane >= c.E ? 0u : l[j] != l[j] ? 1u : (u >> 31 ? ~u : u | 0x80000000u);
       }
-    }
-    float top = 0.f, mine = 0.f;  // mine: lane j < k holds pick j's logit, then its weight
-    int my_id = 0;
-    for (int j = 0; j < c.k; ++j) {
-      uint32_t best = 0u;
-      int at = 0;
+      float top = 0.f, mine = 0.f;  // mine: lane j < k holds pick j's logit, then its weight
+      int my_id = 0;
+      for (int j = 0; j < c.k; ++j) {
+        uint32_t best = 0u;
+        int at = 0;
 #pragma unroll
-      for (int i = PER - 1; i >= 0; --i)
-        if (key[i] >= best) best = key[i], at = i;  // the lowest index among this lane's equals
-      const uint32_t win = wave_pick<true>(best);
-      const uint32_t e = wave_pick<false>(best == win ? (uint32_t)(at * 64 + lane) : 0xFFFFFFFFu);
-      float v = 0.f;
+        for (int i = PER - 1; i >= 0; --i)
+          if (key[i] >= best) best = key[i], at = i;  // the lowest index among this lane's equals
+        const uint32_t win = wave_pick<true>(best);
+        const uint32_t e = wave_pick<false>(best == win ? (uint32_t)(at * 64 + lane) : 0xFFFFFFFFu);
+        float v = 0.f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          if ((uint32_t)(i * 64 + lane) == e) v = l[i], key[i] = 0u;
+        v = as_float((uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, v), (int)(e & 63u)));
+        if (j == 0) top = v;
+        if (lane == j) mine = v, my_id = (int)e;
+      }
+      float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < PER; ++i)
-        if ((uint32_t)(i * 64 + lane) == e) v = l[i], key[i] = 0u;
-      v = as_float((uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, v), (int)(e & 63u)));
-      if (j == 0) top = v;
-      if (lane == j) mine = v, my_id = (int)e;
-    }
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-      if (i * 64 + lane < c.E) sum = sum + expf(l[i] - top);
-    sum = wave_sum(sum);
-    mine = lane < c.k ? expf(mine - top) : 0.f;
-    const float kept = wave_sum(mine);
-    // a NaN among the logits is in `sum`, whichever experts were picked
-    mine = c.renorm ? (sum == sum ? mine / kept : sum) : mine / sum;
-    if (lane < c.k) {
-      if (c.ids != nullptr) c.ids[t * c.k + lane] = my_id;
-      if (c.weights != nullptr) c.weights[t * c.k + lane] = mine;
-      c.gate_of[(size_t)my_id * kMaxTokens + t] = mine;
-      atomicOr(&picked[my_id][t >> 5], 1u << (t & 31));
+        if (i * 64 + lane < c.E) sum = sum + expf(l[i] - top);
+      sum = wave_sum(sum);
+      mine = lane < c.k ? expf(mine - top) : 0.f;
+      const float kept = wave_sum(mine);
+      // a NaN among the logits is in `sum`, whichever experts were picked
+      mine = c.renorm ? (sum == sum ? mine / kept : sum) : mine / sum;
+      if (lane < c.k) {
+        if (c.ids != nullptr) c.ids[t * c.k + lane] = my_id;
+        if (c.weights != nullptr) c.weights[t * c.k + lane] = mine;
+        id_of[t][lane] = my_id;
+        weight_of[t][lane] = mine;
+        atomicOr(&picked[my_id][t >> 5], 1u << (t & 31));
+      }
     }
   }
   __syncthreads();
@@ -210,15 +236,23 @@ __global__ __launch_bounds__(kThreads) void moe_route_kernel(MoeCall c) {
   before -= n;
   __syncthreads();
   int slot = __popcll(act & ((1ull << lane) - 1)), total = 0;
-  for (int w = 0; w < kWaves; ++w) {
+#pragma unroll
+  for (int w = 0; w < kRouteWaves; ++w) {
     if (w < wave) slot += wave_active[w], before += wave_pairs[w];
     total += wave_active[w];
   }
   if (threadIdx.x == 0) c.count->active = total;
   if (n > 0) {
-    c.plan[slot] = MoeExpert{(uint32_t)e, (uint32_t)before, {m0, m1}};
-    int r = before;
-    for (uint64_t m = (uint64_t)m1 << 32 | m0; m != 0; m &= m - 1) c.token_of[r++] = __builtin_ctzll(m);
+    c.plan[slot] = MoeExpert{(uint32_t)e, (uint32_t)before, (uint32_t)n, 0u};
+    first_of[e] = (uint32_t)before;
+  }
+  __syncthreads();
+  // an expert's rows are its tokens in order
+  for (int i = threadIdx.x; i < c.T * c.k; i += kRouteThreads) {
+    const int t = i / c.k, id = id_of[t][i % c.k];
+    if (id < 0) continue;
+    const uint64_t m = (uint64_t)picked[id][1] << 32 | picked[id][0];
+    c.rows[first_of[id] + __popcll(m & ((1ull << t) - 1))] = MoeRow{t, weight_of[t][i % c.k]};
   }
 }
 
@@ -288,197 +322,285 @@ struct Rows16<true> {
   }
 };
 
-// Experts.  Tasks are taken in order from a queue, so a task is held by a workgroup that
-// runs, and workgroups that wait for all tasks of the first kind hold none of them:
-// the wait ends whatever else occupies the GPU.
+// What the router left, read through the scalar cache: the kernels below only read it.
+__device__ __forceinline__ MoeExpert expert_at(const MoeCall &c, uint32_t i) {
+  typedef const __attribute__((address_space(4))) MoeExpert *Constant;
+  const Constant p = (Constant)(uintptr_t)c.plan;
+  MoeExpert e;
+  e.id = __builtin_amdgcn_readfirstlane(p[i].id);
+  e.first = __builtin_amdgcn_readfirstlane(p[i].first);
+  e.n = __builtin_amdgcn_readfirstlane(p[i].n);
+  return e;
+}
+
+// The other factor's operands of steps b U .. b U + U - 1: rows at byte offset `from`.
+template <class Rows, int U>
+__device__ __forceinline__ void factor(u32x4 (&x)[U][4], __amdgpu_buffer_rsrc_t r, uint32_t from, int b, int cols, int g) {
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t k = (uint32_t)(b * U + u) * 128u + Rows::column(i, g);
+      x[u][i] = load16(r, k < (uint32_t)cols ? from + k * 2u : kNowhere);
+    }
+}
+
+template <bool MX>
+constexpr int kBatch = MX ? 2 : 1;  // 128-column steps of a batch
+
+// ---------------------------------------------------------------------------
+// silu(Wg x) * (Wu x).  A task is 16 rows of Wg and of Wu of one expert with that expert's
+// tokens (16 to an MFMA); the 8 waves split H, the sums meet in LDS in wave order, and
+// the result is rounded to bf16, the next product's operand.
 //
-// First kind: 16 rows of Wg and of Wu of one expert with that expert's tokens (16 to an
-// MFMA); the 8 waves split H, the sums meet in LDS, silu(g) u is rounded to bf16, the
-// next product's operand, and stored at device scope.  Second kind: 16 rows of Wd for
-// the experts of one of `segments` parts of the list; the waves split I, an MFMA's
-// columns are the tokens themselves, and a token's weighted sum over its experts
-// stays in the lane's registers.  With several segments the last one to finish a row
-// block adds them in order.  No sum depends on timing.
+// What bounds it is the stream of weights, so it must not stop: a wave has the next
+// batch's weights in flight while it multiplies (loads return in order: the other
+// factor's and the next task's rows are asked for before them), also across the end of a
+// task, and two workgroups share a CU.
 template <bool MX, int TB>
-__global__ __launch_bounds__(kThreads) void moe_experts_kernel(MoeCall c) {
-  constexpr int U = MX ? 4 : 2;  // 128-column steps in flight
+__global__ __launch_bounds__(kThreads, TB > 2 ? 2 : 4) void moe_up_kernel(MoeCall c) {
+  constexpr int U = kBatch<MX>;
   typedef Rows16<MX> Rows;
-  __shared__ f32x4 partial[kWaves][2 * TB][64];
-  __shared__ uint32_t ticket, last;
+  __shared__ f32x4 sums[TB > 2 ? 1 : 2][kWaves][TB][2][64];  // used in turn where two fit beside another workgroup's
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, g = lane >> 4;
-  const int active = __builtin_amdgcn_readfirstlane((int)c.count->active);
-  const int up_blocks = (c.I + 15) / 16;
-  const uint32_t ups = (uint32_t)active * up_blocks;
-  // enough second-kind tasks for every workgroup, but no more parts than experts
-  const int segments = max(1, min(min(active, c.max_segments), ((int)gridDim.x + c.row_blocks - 1) / c.row_blocks));
-  const uint32_t tasks = ups + (uint32_t)(c.row_blocks * segments);
+  const uint32_t blocks = (uint32_t)(c.I + 15) / 16;
+  const uint32_t tasks = __builtin_amdgcn_readfirstlane(c.count->active) * blocks;
+  if (blockIdx.x >= tasks) return;
   const auto rx = rsrc_of(c.x, ((uint32_t)(c.T - 1) * (uint32_t)c.ld_x + (uint32_t)c.H) * 2u);
-  const auto rh = rsrc_of(c.hidden, (uint32_t)(c.T * c.k) * (uint32_t)c.I * 2u);
-  bool waited = false;
-
-  if (threadIdx.x == 0) ticket = add_device(&c.count->ticket);
-  __syncthreads();
-  for (uint32_t task = ticket; task < tasks;) {
-    uint32_t next = 0;
-    if (threadIdx.x == 0) next = add_device(&c.count->ticket);  // arrives while this task runs
-    if (task < ups) {
-      const MoeExpert ex = c.plan[task / up_blocks];
-      const int row0 = (int)(task % up_blocks) * 16;
-      const int n = __popc(ex.tokens[0]) + __popc(ex.tokens[1]), nb = (n + 15) / 16;
-      const Rows wg(c.gate, ex.id, row0, c.I, c.H, lane), wu(c.up, ex.id, row0, c.I, c.H, lane);
-      uint32_t xo[TB];
+  const int batches = (c.H + 128 * U - 1) / (128 * U);
+  const int b0 = wave * batches / kWaves, b1 = (wave + 1) * batches / kWaves;
+  typename Rows::Step wg[U], wu[U];
+  auto load = [&](const MoeExpert &e, uint32_t task, int b) {
+    const int row0 = (int)(task % blocks) * 16;
+    const Rows rg(c.gate, (int)e.id, row0, c.I, c.H, lane), ru(c.up, (int)e.id, row0, c.I, c.H, lane);
 #pragma unroll
-      for (int b = 0; b < TB; ++b)
-        xo[b] = b * 16 + l16 < n ? (uint32_t)c.token_of[ex.first + b * 16 + l16] * (uint32_t)c.ld_x * 2u : kNowhere;
-      f32x4 ag[TB], au[TB];
+    for (int u = 0; u < U; ++u) {
+      rg.load(wg[u], b * U + u, lane, (b * U + u) * 128 < c.H);
+      ru.load(wu[u], b * U + u, lane, (b * U + u) * 128 < c.H);
+    }
+  };
+  int token[TB];  // of this lane's column in each 16, -1 past the last
+  auto tokens_of = [&](const MoeExpert &e) {
 #pragma unroll
-      for (int b = 0; b < TB; ++b) ag[b] = au[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-      const int steps = (c.H + 127) / 128;
-      for (int s = wave * U; s < steps; s += kWaves * U) {
-        typename Rows::Step fg[U], fu[U];
+    for (int at = 0; at < TB; ++at) token[at] = at * 16 + l16 < (int)e.n ? c.rows[e.first + at * 16 + l16].token : -1;
+  };
+  MoeExpert ex = expert_at(c, blockIdx.x / blocks);
+  tokens_of(ex);
+  if (b0 < b1) load(ex, blockIdx.x, b0);
+  int turn = 0;
+  for (uint32_t task = blockIdx.x; task < tasks; task += gridDim.x) {
+    const uint32_t nxt = task + gridDim.x;
+    const MoeExpert en = nxt < tasks ? expert_at(c, nxt / blocks) : ex;
+    const int n = (int)ex.n, nb = (n + 15) / 16;
+    f32x4 ag[TB], au[TB];
+    uint32_t xo[TB];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          wg.load(fg[u], s + u, lane, s + u < steps);
-          wu.load(fu[u], s + u, lane, s + u < steps);
+    for (int at = 0; at < TB; ++at) {
+      ag[at] = au[at] = f32x4{0.f, 0.f, 0.f, 0.f};
+      xo[at] = token[at] >= 0 ? (uint32_t)token[at] * (uint32_t)c.ld_x * 2u : kNowhere;
+    }
+    for (int b = b0; b < b1; ++b) {
+      u32x4 x[U][4];
+      factor<Rows, U>(x, rx, xo[0], b, c.H, g);
+      typename Rows::Step fg[U], fu[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) fg[u] = wg[u], fu[u] = wu[u];
+      if (b + 1 == b1 && nxt < tasks) tokens_of(en);
+      __builtin_amdgcn_sched_barrier(0);
+      if (b + 1 < b1) load(ex, task, b + 1);
+      else if (nxt < tasks) load(en, nxt, b0);
+      __builtin_amdgcn_sched_barrier(0);
+      auto multiply = [&](int at) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            ag[at] = mfma_bf16(Rows::operand(fg[u], i), x[u][i], ag[at]);
+            au[at] = mfma_bf16(Rows::operand(fu[u], i), x[u][i], au[at]);
+          }
+      };
+      multiply(0);
+#pragma unroll
+      for (int at = 1; at < TB; ++at)
+        if (at < nb) {
+          factor<Rows, U>(x, rx, xo[at], b, c.H, g);
+          multiply(at);
         }
+    }
+    if (b0 == b1 && nxt < tasks) tokens_of(en);
+    auto &part = sums[turn];
 #pragma unroll
-        for (int b = 0; b < TB; ++b)
-          if (b < nb) {
+    for (int at = 0; at < TB; ++at)
+      if (at < nb) {
+        part[wave][at][0][lane] = ag[at];
+        part[wave][at][1][lane] = au[at];
+      }
+    __syncthreads();
+    if (wave < nb) {
+      f32x4 gs = part[0][wave][0][lane], us = part[0][wave][1][lane];
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+      for (int w = 1; w < kWaves; ++w) {
+        gs = gs + part[w][wave][0][lane];
+        us = us + part[w][wave][1][lane];
+      }
+      float v[4];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const uint32_t k = (uint32_t)(s + u) * 128u + Rows::column(i, g);
-                const u32x4 x = load16(rx, k < (uint32_t)c.H ? xo[b] + k * 2u : kNowhere);
-                ag[b] = mfma_bf16(Rows::operand(fg[u], i), x, ag[b]);
-                au[b] = mfma_bf16(Rows::operand(fu[u], i), x, au[b]);
-              }
+      for (int i = 0; i < 4; ++i) v[i] = gs[i] / (1.f + expf(-gs[i])) * us[i];
+      const int row = (int)(task % blocks) * 16 + g * 4;  // I is a multiple of 8: all four exist or none
+      if (wave * 16 + l16 < n && row < c.I)
+        *reinterpret_cast<uint64_t *>(c.hidden + (size_t)(ex.first + wave * 16 + l16) * c.I + row) =
+            (uint64_t)pack_bf16(v[2], v[3]) << 32 | pack_bf16(v[0], v[1]);
+    }
+    if constexpr (TB > 2) __syncthreads();
+    else turn ^= 1;
+    ex = en;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// y = sum_j w_j Wd_j h_j.  A task is 16 rows of Wd for the experts of one of `segments` parts
+// of the list; the waves split those experts' columns end to end, each adding its
+// experts' weighted sums to its own rows of y in LDS, one per token (a token that did not
+// pick an expert gets nothing from it, whatever its weights hold).  With several segments
+// the last one to finish a row block adds them in order: no sum depends on timing.
+// The weights' stream is kept up as above.
+template <bool MX, int TB>
+__global__ __launch_bounds__(kThreads, TB > 2 ? 2 : 4) void moe_down_kernel(MoeCall c) {
+  constexpr int U = 2;  // 128-column steps of a batch
+  typedef Rows16<MX> Rows;
+  extern __shared__ __align__(16) unsigned char smem[];  // two areas [wave][token][16 rows], used in turn
+  __shared__ uint32_t last;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const int active = (int)__builtin_amdgcn_readfirstlane(c.count->active);
+  const int segments = max(1, min(active, c.max_segments));
+  const int tasks = c.row_blocks * segments;
+  if ((int)blockIdx.x >= tasks) return;
+  const auto rh = rsrc_of(c.hidden, (uint32_t)(c.T * c.k) * (uint32_t)c.I * 2u);
+  const int batches = (c.I + 128 * U - 1) / (128 * U);  // of one expert
+  const int area_floats = kWaves * c.T * 16;
+  typename Rows::Step wd[U];
+  struct Part {  // of a task: its rows, its first expert, and this wave's batches of all its experts, end to end
+    int row0, a0, b0, b1;
+  };
+  auto part_of = [&](int task) {
+    const int seg = task % segments;
+    Part p;
+    p.row0 = task / segments * 16;
+    p.a0 = seg * active / segments;
+    const int all = ((seg + 1) * active / segments - p.a0) * batches;
+    p.b0 = wave * all / kWaves;
+    p.b1 = (wave + 1) * all / kWaves;
+    return p;
+  };
+  auto load = [&](const Part &p, int b) {
+    const Rows rd(c.down, (int)expert_at(c, p.a0 + b / batches).id, p.row0, c.H, c.I, lane);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = b % batches * U + u;
+      rd.load(wd[u], s, lane, s * 128 < c.I);
+    }
+  };
+  Part p = part_of(blockIdx.x);
+  if (p.b0 < p.b1) load(p, p.b0);
+  int turn = 0;
+  for (int task = blockIdx.x; task < tasks; task += gridDim.x, turn ^= 1) {
+    Part q{0, 0, 0, 0};
+    if (task + (int)gridDim.x < tasks) q = part_of(task + gridDim.x);
+    float *area = reinterpret_cast<float *>(smem) + turn * area_floats, *mine = area + wave * c.T * 16;
+    for (int i = lane; i < c.T * 4; i += 64) reinterpret_cast<f32x4 *>(mine)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int b = p.b0; b < p.b1;) {
+      const MoeExpert ex = expert_at(c, p.a0 + b / batches);
+      const int n = (int)ex.n, nb = (n + 15) / 16;
+      const int end = min(p.b1, (b / batches + 1) * batches);
+      f32x4 acc[TB];
+      uint32_t ho[TB];
+#pragma unroll
+      for (int at = 0; at < TB; ++at) {
+        acc[at] = f32x4{0.f, 0.f, 0.f, 0.f};
+        ho[at] = at * 16 + l16 < n ? (ex.first + at * 16 + l16) * (uint32_t)c.I * 2u : kNowhere;
+      }
+      MoeRow row[TB];
+      for (; b < end; ++b) {
+        u32x4 x[U][4];
+        factor<Rows, U>(x, rh, ho[0], b % batches, c.I, g);
+        typename Rows::Step fd[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) fd[u] = wd[u];
+        if (b + 1 == end) {
+#pragma unroll
+          for (int at = 0; at < TB; ++at)
+            if (at * 16 + l16 < n) row[at] = c.rows[ex.first + at * 16 + l16];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (b + 1 < p.b1) load(p, b + 1);
+        else if (q.b0 < q.b1) load(q, q.b0);
+        __builtin_amdgcn_sched_barrier(0);
+        auto multiply = [&](int at) {
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[at] = mfma_bf16(Rows::operand(fd[u], i), x[u][i], acc[at]);
+        };
+        multiply(0);
+#pragma unroll
+        for (int at = 1; at < TB; ++at)
+          if (at < nb) {
+            factor<Rows, U>(x, rh, ho[at], b % batches, c.I, g);
+            multiply(at);
           }
       }
+      // this wave's part of the expert is whole: into its tokens' rows
 #pragma unroll
-      for (int b = 0; b < TB; ++b)
-        if (b < nb) {
-          partial[wave][2 * b][lane] = ag[b];
-          partial[wave][2 * b + 1][lane] = au[b];
+      for (int at = 0; at < TB; ++at)
+        if (at * 16 + l16 < n) {
+          f32x4 *y = reinterpret_cast<f32x4 *>(mine + row[at].token * 16 + g * 4);
+          f32x4 v = *y;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = __builtin_fmaf(row[at].weight, acc[at][i], v[i]);
+          *y = v;
         }
-      __syncthreads();
-      if (wave < nb) {
-        f32x4 gs = partial[0][2 * wave][lane], us = partial[0][2 * wave + 1][lane];
+    }
+    if (p.b0 == p.b1 && q.b0 < q.b1) load(q, q.b0);
+    __syncthreads();
+    const int rb = p.row0 / 16, seg = task % segments;
+    const int tok = threadIdx.x >> 2, row = p.row0 + (threadIdx.x & 3) * 4;  // H is a multiple of 8
+    const bool has = tok < c.T && row < c.H;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (has) {
+      const f32x4 *in = reinterpret_cast<const f32x4 *>(area) + threadIdx.x;
+      v = in[0];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) {
-          gs = gs + partial[w][2 * wave][lane];
-          us = us + partial[w][2 * wave + 1][lane];
-        }
-        float v[4];
+      for (int w = 1; w < kWaves; ++w) v = v + in[w * c.T * 4];
+    }
+    bool store = has;
+    if (segments > 1) {
+      const size_t at = (size_t)tok * c.H + row, whole = (size_t)c.T * c.H;
+      if (has) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = gs[i] / (1.f + expf(-gs[i])) * us[i];
-        const int row = row0 + g * 4;  // I is a multiple of 8: all four exist or none
-        if (wave * 16 + l16 < n && row < c.I)
-          put_device(reinterpret_cast<uint64_t *>(c.hidden + (size_t)(ex.first + wave * 16 + l16) * c.I + row),
-                     (uint64_t)pack_bf16(v[2], v[3]) << 32 | pack_bf16(v[0], v[1]));
+        for (int i = 0; i < 4; ++i) put_device(c.sums + seg * whole + at + i, v[i]);
       }
       stores_done();
-      if (threadIdx.x == 0) add_device(&c.count->up_done);
-    } else {
-      if (!waited) {
-        if (threadIdx.x == 0)
-          while (get_device(&c.count->up_done) < ups) __builtin_amdgcn_s_sleep(2);
-        __syncthreads();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");  // once a workgroup
-        waited = true;
-      }
-      const int rb = (int)(task - ups) / segments, seg = (int)(task - ups) % segments;
-      const int row0 = rb * 16;
-      const int a0 = seg * active / segments, a1 = (seg + 1) * active / segments;
-      f32x4 y[TB];
-#pragma unroll
-      for (int b = 0; b < TB; ++b) y[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-      const int steps = (c.I + 127) / 128;
-      for (int a = a0; a < a1; ++a) {
-        const MoeExpert ex = c.plan[a];
-        const uint64_t tokens = (uint64_t)ex.tokens[1] << 32 | ex.tokens[0];
-        const Rows wd(c.down, ex.id, row0, c.H, c.I, lane);
-        uint32_t ho[TB];
-        float w[TB];
-        f32x4 t[TB];
-#pragma unroll
-        for (int b = 0; b < TB; ++b) {
-          const int tok = b * 16 + l16;
-          const bool mine = (tokens >> tok) & 1;
-          const int r = (int)ex.first + __popcll(tokens & ((1ull << tok) - 1));
-          ho[b] = mine ? (uint32_t)r * (uint32_t)c.I * 2u : kNowhere;
-          w[b] = mine ? c.gate_of[(size_t)ex.id * kMaxTokens + tok] : 0.f;
-          t[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-        for (int s = wave * U; s < steps; s += kWaves * U) {
-          typename Rows::Step fd[U];
-#pragma unroll
-          for (int u = 0; u < U; ++u) wd.load(fd[u], s + u, lane, s + u < steps);
-#pragma unroll
-          for (int b = 0; b < TB; ++b)
-            if (TB == 1 || ((tokens >> (b * 16)) & 0xFFFFull) != 0) {
-#pragma unroll
-              for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const uint32_t k = (uint32_t)(s + u) * 128u + Rows::column(i, g);
-                  const u32x4 h = load16(rh, k < (uint32_t)c.I ? ho[b] + k * 2u : kNowhere);
-                  t[b] = mfma_bf16(Rows::operand(fd[u], i), h, t[b]);
-                }
-            }
-        }
-        // a token that did not pick this expert adds nothing, whatever the weights hold
-#pragma unroll
-        for (int b = 0; b < TB; ++b)
-          if (ho[b] != kNowhere) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[b][i] = __builtin_fmaf(w[b], t[b][i], y[b][i]);
-          }
-      }
-#pragma unroll
-      for (int b = 0; b < TB; ++b) partial[wave][b][lane] = y[b];
+      if (threadIdx.x == 0) last = add_device(c.joined + rb) + 1 == (uint32_t)segments;
       __syncthreads();
-      const int row = row0 + g * 4, tok = wave * 16 + l16;  // H is a multiple of 8
-      const bool mine = wave < TB && tok < c.T && row < c.H;
-      f32x4 v = {0.f, 0.f, 0.f, 0.f};
-      if (mine) {
-        v = partial[0][wave][lane];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) v = v + partial[w][wave][lane];
-      }
-      bool store = mine;
-      if (segments > 1) {
-        float *out = c.sums + ((size_t)seg * c.T + tok) * c.H + row;
-        if (mine) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) put_device(out + i, v[i]);
-        }
-        stores_done();
-        if (threadIdx.x == 0) last = add_device(c.joined + rb) + 1 == (uint32_t)segments;
-        __syncthreads();
-        store = mine && last;
-        if (store) {
-          const float *in = c.sums + (size_t)tok * c.H + row;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = get_device(in + i);
-          for (int s = 1; s < segments; ++s)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = v[i] + get_device(in + (size_t)s * c.T * c.H + i);
-        }
-      }
+      store = has && last;
       if (store) {
-        typedef uint32_t u32x2_e2 __attribute__((ext_vector_type(2), aligned(2)));
-        u32x2_e2 o;
-        o[0] = pack_bf16(v[0], v[1]);
-        o[1] = pack_bf16(v[2], v[3]);
-        *reinterpret_cast<u32x2_e2 *>(c.y + (size_t)tok * c.ld_y + row) = o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = get_device(c.sums + at + i);
+        for (int s = 1; s < segments; ++s)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = v[i] + get_device(c.sums + s * whole + at + i);
       }
     }
-    if (threadIdx.x == 0) ticket = next;
-    __syncthreads();  // `partial` and `last` are read, `ticket` is written
-    task = ticket;
-    __syncthreads();
+    if (store) {
+      typedef uint32_t u32x2_e2 __attribute__((ext_vector_type(2), aligned(2)));
+      u32x2_e2 o;
+      o[0] = pack_bf16(v[0], v[1]);
+      o[1] = pack_bf16(v[2], v[3]);
+      *reinterpret_cast<u32x2_e2 *>(c.y + (size_t)tok * c.ld_y + row) = o;
+    }
+    p = q;
   }
 }
 
@@ -486,19 +608,19 @@ size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
 // The workspace's parts; the counters come first.
 struct MoeLayout {
-  size_t plan, token_of, gate_of, joined, part, hidden, sums, end;
+  size_t plan, rows, joined, part, hidden, sums, end;
   int slices, segments, row_blocks;
 };
 MoeLayout layout_of(int T, int H, int I, int E, int k) {
   MoeLayout l{};
-  // slices of H: a router workgroup's 8 waves take 128 columns each at a time
-  l.slices = std::max(1, std::min(16, (H + 1023) / 1024));
+  l.slices = std::max(1, std::min(16, (H + 128 * kRouteWaves - 1) / (128 * kRouteWaves)));  // one step a wave
   l.row_blocks = (H + 15) / 16;
+  // parts of the second kind's tasks: two tasks a workgroup or more, so that the last ones to end
+  // are short, with at most E experts to share
   l.segments = std::max(1, std::min(std::min(E, T * k), (1024 + l.row_blocks - 1) / l.row_blocks));
   size_t at = up16(sizeof(MoeCounters));
   l.plan = at, at += up16((size_t)E * sizeof(MoeExpert));
-  l.token_of = at, at += up16((size_t)T * k * 4);
-  l.gate_of = at, at += up16((size_t)E * kMaxTokens * 4);
+  l.rows = at, at += up16((size_t)T * k * sizeof(MoeRow));
   l.joined = at, at += up16((size_t)l.row_blocks * 4);
   l.part = at, at += up16((size_t)l.slices * T * E * 4);
   l.hidden = at, at += up16((size_t)T * k * I * 2);
@@ -508,9 +630,17 @@ MoeLayout layout_of(int T, int H, int I, int E, int k) {
 }
 
 typedef void (*MoeFn)(MoeCall);
+template <int PER>
+MoeFn route_fn(int tb) {
+  return tb == 1 ? moe_route_kernel<1, PER> : tb == 2 ? moe_route_kernel<2, PER> : moe_route_kernel<4, PER>;
+}
 template <bool MX>
-MoeFn experts_fn(int tb) {
-  return tb == 1 ? moe_experts_kernel<MX, 1> : tb == 2 ? moe_experts_kernel<MX, 2> : moe_experts_kernel<MX, 4>;
+MoeFn up_fn(int tb) {
+  return tb == 1 ? moe_up_kernel<MX, 1> : tb == 2 ? moe_up_kernel<MX, 2> : moe_up_kernel<MX, 4>;
+}
+template <bool MX>
+MoeFn down_fn(int tb) {
+  return tb == 1 ? moe_down_kernel<MX, 1> : tb == 2 ? moe_down_kernel<MX, 2> : moe_down_kernel<MX, 4>;
 }
 
 }  // namespace
@@ -542,17 +672,19 @@ int moe_launch(const occ_moe_args &a, hipStream_t s) {
   c.y = static_cast<uint16_t *>(a.y), c.ld_y = a.ld_y, c.ids = a.ids, c.weights = a.weights;
   c.count = reinterpret_cast<MoeCounters *>(ws);
   c.plan = reinterpret_cast<MoeExpert *>(ws + l.plan);
-  c.token_of = reinterpret_cast<int *>(ws + l.token_of);
-  c.gate_of = reinterpret_cast<float *>(ws + l.gate_of);
+  c.rows = reinterpret_cast<MoeRow *>(ws + l.rows);
   c.joined = reinterpret_cast<uint32_t *>(ws + l.joined);
   c.part = reinterpret_cast<float *>(ws + l.part);
   c.hidden = reinterpret_cast<uint16_t *>(ws + l.hidden);
   c.sums = reinterpret_cast<float *>(ws + l.sums);
   const int tb = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
-  const MoeFn route = tb == 1 ? moe_route_kernel<1> : tb == 2 ? moe_route_kernel<2> : moe_route_kernel<4>;
-  hipLaunchKernelGGL(route, dim3((a.experts + 15) / 16 * l.slices), dim3(kThreads), 0, s, c);
+  const MoeFn route = a.experts <= 64 ? route_fn<1>(tb) : a.experts <= 128 ? route_fn<2>(tb) : route_fn<8>(tb);
+  hipLaunchKernelGGL(route, dim3((a.experts + 15) / 16 * l.slices), dim3(kRouteThreads), 0, s, c);
   if (hipGetLastError() != hipSuccess) return OCC_EHIP;
-  hipLaunchKernelGGL(mx ? experts_fn<true>(tb) : experts_fn<false>(tb), dim3(di->num_cus * 2), dim3(kThreads), 0, s, c);
+  const unsigned grid = (unsigned)di->num_cus * 2;
+  hipLaunchKernelGGL(mx ? up_fn<true>(tb) : up_fn<false>(tb), dim3(grid), dim3(kThreads), 0, s, c);
+  if (hipGetLastError() != hipSuccess) return OCC_EHIP;
+  hipLaunchKernelGGL(mx ? down_fn<true>(tb) : down_fn<false>(tb), dim3(grid), dim3(kThreads), 2 * kWaves * a.tokens * 64, s, c);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
 }
 

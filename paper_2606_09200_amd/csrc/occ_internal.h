@@ -150,13 +150,15 @@ int norm_gate_bwd_launch(const occ_norm_args &n, hipStream_t s);
 
 struct MoeCounters {
   uint32_t arrived;  // router workgroups that are done; zero between calls
-  uint32_t ticket;   // next task of the experts' queue
-  uint32_t up_done;  // finished tasks of the first kind
   uint32_t active;   // experts that some token picked
 };
 struct MoeExpert {
-  uint32_t id, first;  // its index, and its first row of the hidden activations
-  uint32_t tokens[2];  // its tokens, a bit each
+  uint32_t id, first, n;  // its index, its first row of the hidden activations, their number
+  uint32_t unused;
+};
+struct MoeRow {  // of the hidden activations: a token's with one of its experts
+  int token;
+  float weight;
 };
 struct MoeMatrix {
   const void *w;
@@ -177,8 +179,7 @@ struct MoeCall {
   // workspace
   MoeCounters *count;
   MoeExpert *plan;
-  int *token_of;     // token of each row of the hidden activations
-  float *gate_of;    // experts x 64: a token's weight
+  MoeRow *rows;
   uint32_t *joined;  // per 16 rows of y: finished parts
   float *part;       // partial logits
   uint16_t *hidden;  // rows x I, bf16
