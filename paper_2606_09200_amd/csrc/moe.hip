@@ -22,8 +22,9 @@ constexpr int kMaxTokens = 64, kMaxTopK = 16, kMaxExperts = 512;
 constexpr int kThreads = 512, kWaves = kThreads / 64;
 constexpr uint32_t kNowhere = 0x80000000u;  // a byte offset beyond every descriptor
 
-__device__ __forceinline__ u32x4 load16(__amdgpu_buffer_rsrc_t r, uint32_t off) {
-  return __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0);
+// 16 bytes at `off` (checked against the descriptor's end) plus `uniform` (which stays within a row).
+__device__ __forceinline__ u32x4 load16(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t uniform = 0) {
+  return __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, (int)uniform, 0);
 }
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void *p, uint32_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, 0x00020000);
@@ -68,19 +69,21 @@ __device__ __forceinline__ uint32_t wave_pick(uint32_t v) {
 
 // ---------------------------------------------------------------------------
 // Router.  A workgroup multiplies 16 experts' rows with all tokens over one of `slices`
-// slices of H, its 16 waves 128 columns each in turn; the partial logits go to
-// part[slice][token][expert].  The workgroup that arrives last adds the slices in
+// slices of H, a wave 16 tokens and 128 columns at a time; the partial logits go to
+// part[16 experts, slice][token][expert].  The workgroup that arrives last adds the slices in
 // order and picks: a wave per token at a time, lane l holding experts l, l + 64, ...
-// (PER of them), with the logits of GROUP tokens on their way at once: they come from
-// other XCDs' writes through memory, and waiting for each token's in turn made this
-// kernel 33 us long for 64 tokens.  Logits order as integers, a NaN below everything
-// (its token's weights become NaN with the sum); equal ones go to the lower index.
+// (PER of them), the next token's logits on their way: they come from other XCDs'
+// writes through memory.  Logits order as integers, a NaN below everything (its
+// token's weights become NaN with the sum); equal ones go to the lower index.
+//
+// What bounds it is latency: two trips to memory and one workgroup's tail.  Most of
+// that workgroup's instructions run once and come from memory too (80 ns per 64
+// bytes), so its loops stay rolled.
 constexpr int kRouteThreads = 1024, kRouteWaves = kRouteThreads / 64;
 
 template <int TB, int PER>
 __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(MoeCall c) {
-  constexpr int GROUP = PER == 1 ? 4 : PER == 2 ? 2 : 1;
-  __shared__ f32x4 partial[kRouteWaves][TB][64];
+  __shared__ f32x4 partial[kRouteWaves / TB][TB][64];
   __shared__ uint32_t last;
   __shared__ uint32_t picked[kMaxExperts][2];  // the tokens of an expert, a bit each
   __shared__ uint32_t first_of[kMaxExperts];   // its first row of the hidden activations
@@ -91,45 +94,37 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(MoeCall c) {
   const int l16 = lane & 15, g = lane >> 4;
   const int eb = blockIdx.x / c.slices, slice = blockIdx.x % c.slices;
   {
-    const int e0 = eb * 16, rows = min(16, c.E - e0);
+    constexpr int STEPS = kRouteWaves / TB;
+    const int e0 = eb * 16, rows = min(16, c.E - e0), t = wave % TB * 16 + l16;
     const auto rw = rsrc_of(c.router + (size_t)e0 * c.H, (uint32_t)rows * (uint32_t)c.H * 2u);
     const auto rx = rsrc_of(c.x, ((uint32_t)(c.T - 1) * (uint32_t)c.ld_x + (uint32_t)c.H) * 2u);
-    f32x4 acc[TB];
-#pragma unroll
-    for (int b = 0; b < TB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    uint32_t xo[TB];
-#pragma unroll
-    for (int b = 0; b < TB; ++b) xo[b] = b * 16 + l16 < c.T ? (uint32_t)(b * 16 + l16) * (uint32_t)c.ld_x * 2u : kNowhere;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     const int steps = (c.H + 127) / 128;
-    for (int s = slice * kRouteWaves + wave; s < steps; s += c.slices * kRouteWaves) {
-      u32x4 w[4], x[TB][4];
+#pragma unroll 1
+    for (int s = slice * STEPS + wave / TB; s < steps; s += c.slices * STEPS) {
+      u32x4 w[4], x[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint32_t k = (uint32_t)(s * 128 + i * 32 + g * 8);
         const bool in = k < (uint32_t)c.H;
         w[i] = load16(rw, in ? ((uint32_t)l16 * (uint32_t)c.H + k) * 2u : kNowhere);
-#pragma unroll
-        for (int b = 0; b < TB; ++b) x[b][i] = load16(rx, in ? xo[b] + k * 2u : kNowhere);
+        x[i] = load16(rx, in && t < c.T ? ((uint32_t)t * (uint32_t)c.ld_x + k) * 2u : kNowhere);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int b = 0; b < TB; ++b) acc[b] = mfma_bf16(w[i], x[b][i], acc[b]);
+      for (int i = 0; i < 4; ++i) acc = mfma_bf16(w[i], x[i], acc);
     }
-#pragma unroll
-    for (int b = 0; b < TB; ++b) partial[wave][b][lane] = acc[b];
+    partial[wave / TB][wave % TB][lane] = acc;
     __syncthreads();
-    if (wave < TB) {
-      f32x4 v = partial[0][wave][lane];
+    // a thread per 4 experts (g) of a token
+    if (threadIdx.x < TB * 64) {
+      const int b = threadIdx.x >> 6, t = b * 16 + l16;
+      f32x4 v = partial[0][b][lane];
 #pragma unroll
-      for (int w = 1; w < kRouteWaves; ++w) v = v + partial[w][wave][lane];
-      const int t = wave * 16 + l16;
-      if (t < c.T) {
-        float *p = c.part + ((size_t)slice * c.T + t) * c.E;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (e0 + g * 4 + i < c.E) put_device(p + e0 + g * 4 + i, v[i]);
-      }
+      for (int w = 1; w < STEPS; ++w) v = v + partial[w][b][lane];
+      if (t < c.T)
+        __builtin_amdgcn_raw_buffer_store_b128(
+            __builtin_bit_cast(u32x4, v), rsrc_of(c.part + (size_t)blockIdx.x * c.T * 16, (uint32_t)c.T * 64u),
+            t * 64 + g * 16, 0, 16);  // device scope, as put_device
     }
   }
   stores_done();
@@ -141,82 +136,67 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(MoeCall c) {
   for (int i = threadIdx.x; i < c.row_blocks; i += kRouteThreads) c.joined[i] = 0;
   for (int i = threadIdx.x; i < c.E; i += kRouteThreads) picked[i][0] = picked[i][1] = 0u;
   __syncthreads();
-  for (int t0 = wave * GROUP; t0 < c.T; t0 += kRouteWaves * GROUP) {
-    float logit[GROUP][PER];
+  float ahead[PER];  // the next token's logits
+  auto fetch = [&](int t) {
 #pragma unroll
-    for (int q = 0; q < GROUP; ++q)
-#pragma unroll
-      for (int j = 0; j < PER; ++j) logit[q][j] = 0.f;
-#pragma unroll 2
+    for (int j = 0; j < PER; ++j) ahead[j] = 0.f;
+#pragma unroll 4
     for (int s = 0; s < c.slices; ++s) {
-      float v[GROUP][PER];
-#pragma unroll
-      for (int q = 0; q < GROUP; ++q)
-#pragma unroll
-        for (int j = 0; j < PER; ++j) {
-          const int t = min(t0 + q, c.T - 1), e = min(j * 64 + lane, c.E - 1);
-          v[q][j] = get_device(c.part + ((size_t)s * c.T + t) * c.E + e);
-        }
-#pragma unroll
-      for (int q = 0; q < GROUP; ++q)
-#pragma unroll
-        for (int j = 0; j < PER; ++j) logit[q][j] = logit[q][j] + v[q][j];
-    }
-#pragma unroll
-    for (int q = 0; q < GROUP; ++q) {
-      const int t = t0 + q;
-      if (t >= c.T) break;
-      if (c.mask != nullptr && c.mask[t] == 0) {
-        if (lane < c.k) {
-          if (c.ids != nullptr) c.ids[t * c.k + lane] = -1;
-          if (c.weights != nullptr) c.weights[t * c.k + lane] = 0.f;
-          id_of[t][lane] = -1;
-        }
-        continue;
-      }
-      float l[PER];
-      uint32_t key[PER];
 #pragma unroll
       for (int j = 0; j < PER; ++j) {
-        l[j] = logit[q][j];
-        // ascending integers, 1 and above; what is taken or missing is 0
-        const uint32_t u = __builtin_bit_cast(uint32_t, l[j]);
-        key[j] = j * 64 + lane >= c.E ? 0u : l[j] != l[j] ? 1u : (u >> 31 ? ~u : u | 0x80000000u);
+        const int e = min(j * 64 + lane, c.E - 1);
+        ahead[j] = ahead[j] + get_device(c.part + ((size_t)((e >> 4) * c.slices + s) * c.T + t) * 16 + (e & 15));
       }
-      float top = 0.f, mine = 0.f;  // mine: lane j < k holds pick j's logit, then its weight
-      int my_id = 0;
-      for (int j = 0; j < c.k; ++j) {
-        uint32_t best = 0u;
-        int at = 0;
+    }
+  };
+  if (wave < c.T) fetch(wave);
+#pragma unroll 1
+  for (int t = wave; t < c.T; t += kRouteWaves) {
+    const bool live = c.mask == nullptr || c.mask[t] != 0;
+    float l[PER];
+    uint32_t key[PER];
 #pragma unroll
-        for (int i = PER - 1; i >= 0; --i)
-          if (key[i] >= best) best = key[i], at = i;  // the lowest index among this lane's equals
-        const uint32_t win = wave_pick<true>(best);
-        const uint32_t e = wave_pick<false>(best == win ? (uint32_t)(at * 64 + lane) : 0xFFFFFFFFu);
-        float v = 0.f;
+    for (int j = 0; j < PER; ++j) {
+      l[j] = ahead[j];
+      // ascending integers, 1 and above; what is taken or missing is 0
+      const uint32_t u = __builtin_bit_cast(uint32_t, l[j]);
+      key[j] = j * 64 + lane >= c.E ? 0u : l[j] != l[j] ? 1u : (u >> 31 ? ~u : u | 0x80000000u);
+    }
+    if (t + kRouteWaves < c.T) fetch(t + kRouteWaves);
+    float top = 0.f, mine = 0.f;  // mine: lane j < k holds pick j's logit, then its weight
+    int my_id = 0;
+#pragma unroll 1
+    for (int j = 0; j < c.k; ++j) {
+      uint32_t best = 0u;
+      int at = 0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i)
-          if ((uint32_t)(i * 64 + lane) == e) v = l[i], key[i] = 0u;
-        v = as_float((uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, v), (int)(e & 63u)));
-        if (j == 0) top = v;
-        if (lane == j) mine = v, my_id = (int)e;
-      }
-      float sum = 0.f;
+      for (int i = PER - 1; i >= 0; --i)
+        if (key[i] >= best) best = key[i], at = i;  // the lowest index among this lane's equals
+      const uint32_t win = wave_pick<true>(best);
+      const uint32_t e = wave_pick<false>(best == win ? (uint32_t)(at * 64 + lane) : 0xFFFFFFFFu);
+      float v = 0.f;
 #pragma unroll
       for (int i = 0; i < PER; ++i)
-        if (i * 64 + lane < c.E) sum = sum + expf(l[i] - top);
-      sum = wave_sum(sum);
-      mine = lane < c.k ? expf(mine - top) : 0.f;
-      const float kept = wave_sum(mine);
-      // a NaN among the logits is in `sum`, whichever experts were picked
-      mine = c.renorm ? (sum == sum ? mine / kept : sum) : mine / sum;
-      if (lane < c.k) {
-        if (c.ids != nullptr) c.ids[t * c.k + lane] = my_id;
-        if (c.weights != nullptr) c.weights[t * c.k + lane] = mine;
-        id_of[t][lane] = my_id;
-        weight_of[t][lane] = mine;
-        atomicOr(&picked[my_id][t >> 5], 1u << (t & 31));
-      }
+        if ((uint32_t)(i * 64 + lane) == e) v = l[i], key[i] = 0u;
+      v = as_float((uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, v), (int)(e & 63u)));
+      if (j == 0) top = v;
+      if (lane == j) mine = v, my_id = (int)e;
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sum = sum + (i * 64 + lane < c.E ? expf(l[i] - top) : 0.f);
+    sum = wave_sum(sum);
+    float w = lane < c.k ? expf(mine - top) : 0.f;
+    // a NaN among the logits is in `sum`, whichever experts were picked
+    if (c.renorm) sum = sum == sum ? wave_sum(w) : sum;
+    w = w / sum;
+    if (lane < c.k) {
+      if (!live) my_id = -1, w = 0.f;
+      if (c.ids != nullptr) c.ids[t * c.k + lane] = my_id;
+      if (c.weights != nullptr) c.weights[t * c.k + lane] = w;
+      id_of[t][lane] = my_id;
+      weight_of[t][lane] = w;
+      if (live) atomicOr(&picked[my_id][t >> 5], 1u << (t & 31));
     }
   }
   __syncthreads();
@@ -257,70 +237,108 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(MoeCall c) {
 }
 
 // ---------------------------------------------------------------------------
-// A 16-row block of an expert's matrix, read in steps of 128 columns: four MFMA
-// operands of 32 columns.  bf16: operand i is columns 32 i + 8 g .. + 7 of lane (row, g).
-// MX4: a lane's 16 bytes are the block of columns 32 g .. + 31, operand i its columns
-// 8 i .. + 7, converted to bf16 exactly (E2M1 has two bits of precision) with the block's
-// scale; the other factor is read in the same order.
+// A 16-row block of an expert's matrix, read in units of 256 bytes a row of bf16 (128 columns) and
+// 128 of MX4 (256 columns; the other factor's operands for more would halve the waves on a
+// CU).  A load takes whole pieces of 4 or 8 rows, and the unit turns into operands through
+// LDS of the wave's own (chunks of 16 bytes spread by row, no bank conflicts, no
+// barriers): loads of 64 bytes from each of 16 rows, as an MFMA's operand lies in memory,
+// are 10 % slower over the layer.
+//
+// STEPS steps of 128 columns, each four MFMA operands of 32.  bf16: operand i of a step is
+// columns 32 i + 8 g .. + 7 of lane (row, g).  MX4: a lane's 16 bytes are the block of columns
+// 32 g .. + 31 of the step, operand i its columns 8 i .. + 7, converted to bf16 (exactly:
+// E2M1 has two bits of precision) with the block's scale; the other factor is read
+// in the same order.
 template <bool MX>
-struct Rows16;
-template <>
-struct Rows16<false> {
-  struct Step {
-    u32x4 w[4];
-  };
-  __amdgpu_buffer_rsrc_t r;
-  uint32_t at, cols;
-  static __device__ __forceinline__ uint32_t column(int i, int g) { return 32 * i + 8 * g; }
-  __device__ __forceinline__ Rows16(const MoeMatrix &m, int e, int row0, int rows, int cols_, int lane) : cols(cols_) {
-    r = rsrc_of(static_cast<const uint8_t *>(m.w) + (size_t)e * m.stride + (size_t)row0 * cols * 2,
-                (uint32_t)min(16, rows - row0) * cols * 2u);
-    at = (uint32_t)(lane & 15) * cols * 2u;
-  }
-  __device__ __forceinline__ void load(Step &s, int step, int lane, bool in) const {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t k = (uint32_t)step * 128u + column(i, lane >> 4);
-      s.w[i] = load16(r, in && k < cols ? at + k * 2u : kNowhere);
-    }
-  }
-  static __device__ __forceinline__ u32x4 operand(const Step &s, int i) { return s.w[i]; }
+struct Unit {
+  u32x4 w[MX ? 2 : 4];  // load i: CH lanes to a row, rows 64 / CH apart
+  uint32_t scale;       // MX4: the lane's word of the scale tile, its first two bytes the unit's steps
 };
-template <>
-struct Rows16<true> {
-  struct Step {
-    u32x4 w;
-    uint32_t s;
-  };
+
+template <bool MX>
+struct Rows16 {
+  static constexpr int STEPS = MX ? 2 : 1, COLS = 128 * STEPS;
+  static constexpr int CH = MX ? 8 : 16, LOADS = CH / 4;  // 16-byte chunks of a row, loads of a unit
+  static constexpr int LDS = 16 * CH;                     // chunks of a staged unit
   __amdgpu_buffer_rsrc_t r, rs;
-  uint32_t at;
-  static __device__ __forceinline__ uint32_t column(int i, int g) { return 32 * g + 8 * i; }
+  uint32_t at, pitch, left;  // left: bytes of a row past the lane's first chunk
   __device__ __forceinline__ Rows16(const MoeMatrix &m, int e, int row0, int rows, int cols, int lane) {
-    const uint32_t P = (uint32_t)(OCC_MX4_KP(cols) / 2);
-    r = rsrc_of(static_cast<const uint8_t *>(m.w) + (size_t)e * m.stride + (size_t)row0 * P, (uint32_t)min(16, rows - row0) * P);
-    rs = rsrc_of(m.scales + (size_t)e * m.scale_stride + (size_t)(row0 >> 4) * P, P);
-    at = (uint32_t)(lane & 15) * P + (uint32_t)(lane >> 4) * 16u;
+    pitch = MX ? (uint32_t)(OCC_MX4_KP(cols) / 2) : (uint32_t)cols * 2u;
+    r = rsrc_of(static_cast<const uint8_t *>(m.w) + (size_t)e * m.stride + (size_t)row0 * pitch,
+                (uint32_t)min(16, rows - row0) * pitch);
+    if constexpr (MX) rs = rsrc_of(m.scales + (size_t)e * m.scale_stride + (size_t)(row0 >> 4) * pitch, pitch);
+    at = (uint32_t)(lane / CH) * pitch + (uint32_t)(lane % CH) * 16u;
+    left = pitch - (uint32_t)(lane % CH) * 16u;
   }
-  __device__ __forceinline__ void load(Step &s, int step, int lane, bool in) const {
-    s.w = load16(r, in ? at + (uint32_t)step * 64u : kNowhere);
-    s.s = __builtin_amdgcn_raw_buffer_load_b8(rs, (int)(in ? (uint32_t)(step >> 2) * 256u + lane * 4u + (step & 3) : kNowhere), 0, 0);
-  }
-  static __device__ __forceinline__ u32x4 operand(const Step &s, int i) {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    const float sc = mx4_scale_value(s.s);
-    const uint32_t w = s.w[i];
-    u32x4 o;
-    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 1);
-    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 3);
-    o[0] = __builtin_bit_cast(uint32_t, a);
-    o[1] = __builtin_bit_cast(uint32_t, b);
-    o[2] = __builtin_bit_cast(uint32_t, c);
-    o[3] = __builtin_bit_cast(uint32_t, d);
-    // the conversion takes the scale's exponent alone; a NaN scale (a block that held one) stays NaN
-    if (s.s == 255u) o = u32x4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
-    return o;
+  __device__ __forceinline__ void load(Unit<MX> &q, int unit, int lane) const {
+    const uint32_t k = (uint32_t)unit * (CH * 16u), step = 64u / CH * pitch;
+    if (MX || k + CH * 16u <= pitch) {  // MX4 rows are whole units
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) q.w[i] = load16(r, at + i * step, k);
+    } else {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) q.w[i] = load16(r, (int)(left - k) > 0 ? at + i * step + k : kNowhere);
+    }
+    if constexpr (MX)  // a tile is two units; the second one's bytes are the upper half of its words
+      q.scale = __builtin_amdgcn_raw_buffer_load_b16(rs, lane * 4, (int)((uint32_t)(unit >> 1) * 256u + (unit & 1) * 2u), 0);
   }
 };
+
+// Where chunk c of a row of a staged unit lies.
+template <bool MX>
+__device__ __forceinline__ int slot_of(int row, int c) {
+  return MX ? row * 8 + swz<8>(row, c) : row * 16 + (c ^ row);
+}
+template <bool MX>
+__device__ __forceinline__ void stage(u32x4 *lds, const Unit<MX> &q, int lane) {
+  constexpr int CH = Rows16<MX>::CH;
+#pragma unroll
+  for (int i = 0; i < Rows16<MX>::LOADS; ++i) lds[slot_of<MX>(i * (64 / CH) + lane / CH, lane % CH)] = q.w[i];
+}
+// A lane's part of step s of a staged unit: operand i of bf16, or four operands' MX4 codes.
+template <bool MX>
+__device__ __forceinline__ u32x4 chunk(const u32x4 *lds, int i, int lane) {
+  return lds[slot_of<MX>(lane & 15, 4 * i + (lane >> 4))];
+}
+// 8 MX4 codes with scale byte `s`.  The conversion takes the byte as a binary32 exponent: 0 is 2^-127, 255
+// makes NaN (checked on every scale and code).
+__device__ __forceinline__ u32x4 mx4_operand(uint32_t codes, uint32_t s) {
+  const float sc = as_float(s << 23);
+  u32x4 o;
+  o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, sc, 0));
+  o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, sc, 1));
+  o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, sc, 2));
+  o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, sc, 3));
+  return o;
+}
+
+// The other factor's operands of a unit: rows (bf16) at byte offset `from` (kNowhere: none),
+// which holds the lane's part already.
+template <bool MX>
+__device__ __forceinline__ uint32_t lane_bytes(int g) {
+  return (MX ? 64u : 16u) * (uint32_t)g;
+}
+template <bool MX>
+__device__ __forceinline__ void factor(u32x4 (&x)[Rows16<MX>::STEPS][4], __amdgpu_buffer_rsrc_t r, uint32_t from, int unit,
+                                       int cols, int g) {
+  constexpr uint32_t kNext = MX ? 16 : 64;  // bytes from operand to operand
+  const uint32_t k = (uint32_t)unit * Rows16<MX>::COLS * 2u;
+  if (k + Rows16<MX>::COLS * 2u <= (uint32_t)cols * 2u) {
+#pragma unroll
+    for (int s = 0; s < Rows16<MX>::STEPS; ++s)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[s][i] = load16(r, from + 256u * s + kNext * i, k);
+  } else {
+    const uint32_t end = (uint32_t)cols * 2u - lane_bytes<MX>(g);
+#pragma unroll
+    for (int s = 0; s < Rows16<MX>::STEPS; ++s)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t at = k + 256u * s + kNext * i;
+        x[s][i] = load16(r, (int)(end - at) > 0 ? from + at : kNowhere);
+      }
+  }
+}
 
 // What the router left, read through the scalar cache: the kernels below only read it.
 __device__ __forceinline__ MoeExpert expert_at(const MoeCall &c, uint32_t i) {
@@ -333,246 +351,240 @@ __device__ __forceinline__ MoeExpert expert_at(const MoeCall &c, uint32_t i) {
   return e;
 }
 
-// The other factor's operands of steps b U .. b U + U - 1: rows at byte offset `from`.
-template <class Rows, int U>
-__device__ __forceinline__ void factor(u32x4 (&x)[U][4], __amdgpu_buffer_rsrc_t r, uint32_t from, int b, int cols, int g) {
-#pragma unroll
-  for (int u = 0; u < U; ++u)
+// Two 16-row blocks times one unit of the other factor's columns: acc0 += A x, acc1 += B x.
+template <bool MX>
+__device__ __forceinline__ void multiply(f32x4 &acc0, f32x4 &acc1, const u32x4 *lds, uint32_t scale0, uint32_t scale1,
+                                         const u32x4 (&x)[Rows16<MX>::STEPS][4], int lane) {
+  if constexpr (!MX) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t k = (uint32_t)(b * U + u) * 128u + Rows::column(i, g);
-      x[u][i] = load16(r, k < (uint32_t)cols ? from + k * 2u : kNowhere);
+      acc0 = mfma_bf16(chunk<MX>(lds, i, lane), x[0][i], acc0);
+      acc1 = mfma_bf16(chunk<MX>(lds + Rows16<MX>::LDS, i, lane), x[0][i], acc1);
     }
-}
-
-template <bool MX>
-constexpr int kBatch = MX ? 2 : 1;  // 128-column steps of a batch
-
-// ---------------------------------------------------------------------------
-// silu(Wg x) * (Wu x).  A task is 16 rows of Wg and of Wu of one expert with that expert's
-// tokens (16 to an MFMA); the 8 waves split H, the sums meet in LDS in wave order, and
-// the result is rounded to bf16, the next product's operand.
-//
-// What bounds it is the stream of weights, so it must not stop: a wave has the next
-// batch's weights in flight while it multiplies (loads return in order: the other
-// factor's and the next task's rows are asked for before them), also across the end of a
-// task, and two workgroups share a CU.
-template <bool MX, int TB>
-__global__ __launch_bounds__(kThreads, TB > 2 ? 2 : 4) void moe_up_kernel(MoeCall c) {
-  constexpr int U = kBatch<MX>;
-  typedef Rows16<MX> Rows;
-  __shared__ f32x4 sums[TB > 2 ? 1 : 2][kWaves][TB][2][64];  // used in turn where two fit beside another workgroup's
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int l16 = lane & 15, g = lane >> 4;
-  const uint32_t blocks = (uint32_t)(c.I + 15) / 16;
-  const uint32_t tasks = __builtin_amdgcn_readfirstlane(c.count->active) * blocks;
-  if (blockIdx.x >= tasks) return;
-  const auto rx = rsrc_of(c.x, ((uint32_t)(c.T - 1) * (uint32_t)c.ld_x + (uint32_t)c.H) * 2u);
-  const int batches = (c.H + 128 * U - 1) / (128 * U);
-  const int b0 = wave * batches / kWaves, b1 = (wave + 1) * batches / kWaves;
-  typename Rows::Step wg[U], wu[U];
-  auto load = [&](const MoeExpert &e, uint32_t task, int b) {
-    const int row0 = (int)(task % blocks) * 16;
-    const Rows rg(c.gate, (int)e.id, row0, c.I, c.H, lane), ru(c.up, (int)e.id, row0, c.I, c.H, lane);
+  } else {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      rg.load(wg[u], b * U + u, lane, (b * U + u) * 128 < c.H);
-      ru.load(wu[u], b * U + u, lane, (b * U + u) * 128 < c.H);
-    }
-  };
-  int token[TB];  // of this lane's column in each 16, -1 past the last
-  auto tokens_of = [&](const MoeExpert &e) {
+    for (int s = 0; s < Rows16<MX>::STEPS; ++s) {
+      const u32x4 a = chunk<MX>(lds, s, lane), b = chunk<MX>(lds + Rows16<MX>::LDS, s, lane);
+      const uint32_t sa = scale0 >> (8 * s) & 255u, sb = scale1 >> (8 * s) & 255u;
 #pragma unroll
-    for (int at = 0; at < TB; ++at) token[at] = at * 16 + l16 < (int)e.n ? c.rows[e.first + at * 16 + l16].token : -1;
-  };
-  MoeExpert ex = expert_at(c, blockIdx.x / blocks);
-  tokens_of(ex);
-  if (b0 < b1) load(ex, blockIdx.x, b0);
-  int turn = 0;
-  for (uint32_t task = blockIdx.x; task < tasks; task += gridDim.x) {
-    const uint32_t nxt = task + gridDim.x;
-    const MoeExpert en = nxt < tasks ? expert_at(c, nxt / blocks) : ex;
-    const int n = (int)ex.n, nb = (n + 15) / 16;
-    f32x4 ag[TB], au[TB];
-    uint32_t xo[TB];
-#pragma unroll
-    for (int at = 0; at < TB; ++at) {
-      ag[at] = au[at] = f32x4{0.f, 0.f, 0.f, 0.f};
-      xo[at] = token[at] >= 0 ? (uint32_t)token[at] * (uint32_t)c.ld_x * 2u : kNowhere;
-    }
-    for (int b = b0; b < b1; ++b) {
-      u32x4 x[U][4];
-      factor<Rows, U>(x, rx, xo[0], b, c.H, g);
-      typename Rows::Step fg[U], fu[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) fg[u] = wg[u], fu[u] = wu[u];
-      if (b + 1 == b1 && nxt < tasks) tokens_of(en);
-      __builtin_amdgcn_sched_barrier(0);
-      if (b + 1 < b1) load(ex, task, b + 1);
-      else if (nxt < tasks) load(en, nxt, b0);
-      __builtin_amdgcn_sched_barrier(0);
-      auto multiply = [&](int at) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            ag[at] = mfma_bf16(Rows::operand(fg[u], i), x[u][i], ag[at]);
-            au[at] = mfma_bf16(Rows::operand(fu[u], i), x[u][i], au[at]);
-          }
-      };
-      multiply(0);
-#pragma unroll
-      for (int at = 1; at < TB; ++at)
-        if (at < nb) {
-          factor<Rows, U>(x, rx, xo[at], b, c.H, g);
-          multiply(at);
-        }
-    }
-    if (b0 == b1 && nxt < tasks) tokens_of(en);
-    auto &part = sums[turn];
-#pragma unroll
-    for (int at = 0; at < TB; ++at)
-      if (at < nb) {
-        part[wave][at][0][lane] = ag[at];
-        part[wave][at][1][lane] = au[at];
+      for (int i = 0; i < 4; ++i) {
+        acc0 = mfma_bf16(mx4_operand(a[i], sa), x[s][i], acc0);
+        acc1 = mfma_bf16(mx4_operand(b[i], sb), x[s][i], acc1);
       }
-    __syncthreads();
-    if (wave < nb) {
-      f32x4 gs = part[0][wave][0][lane], us = part[0][wave][1][lane];
-#pragma unroll
-      for (int w = 1; w < kWaves; ++w) {
-        gs = gs + part[w][wave][0][lane];
-        us = us + part[w][wave][1][lane];
-      }
-      float v[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = gs[i] / (1.f + expf(-gs[i])) * us[i];
-      const int row = (int)(task % blocks) * 16 + g * 4;  // I is a multiple of 8: all four exist or none
-      if (wave * 16 + l16 < n && row < c.I)
-        *reinterpret_cast<uint64_t *>(c.hidden + (size_t)(ex.first + wave * 16 + l16) * c.I + row) =
-            (uint64_t)pack_bf16(v[2], v[3]) << 32 | pack_bf16(v[0], v[1]);
+      __builtin_amdgcn_sched_barrier(0);  // a step's operands at a time: registers
     }
-    if constexpr (TB > 2) __syncthreads();
-    else turn ^= 1;
-    ex = en;
   }
 }
 
 // ---------------------------------------------------------------------------
-// y = sum_j w_j Wd_j h_j.  A task is 16 rows of Wd for the experts of one of `segments` parts
+// silu(Wg x) * (Wu x).  A task is `rbs` blocks of 16 rows of Wg and of Wu of one expert with that
+// expert's tokens (16 to an MFMA).  8 / rbs waves split H (more blocks where H has fewer
+// units than there are waves), the sums meet in LDS in wave order, and the result is
+// rounded to bf16, the next product's operand.
+//
+// What bounds it is the stream of weights, so it must not stop: a wave has the next
+// unit's weights in flight while it multiplies (loads return in order: the other
+// factor's are asked for before them), also across the end of a task, and two
+// workgroups share a CU.
+template <bool MX, int TB>
+__global__ __launch_bounds__(kThreads, TB > 2 ? 2 : 4) void moe_up_kernel(MoeCall c) {
+  typedef Rows16<MX> Rows;
+  // a wave's units of Wg and Wu; its sums at the end of a task
+  constexpr int AREA = 2 * Rows::LDS > 128 * TB ? 2 * Rows::LDS : 128 * TB;
+  __shared__ u32x4 staged[kWaves][AREA];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  u32x4 *lds = staged[wave];
+  const int kws = kWaves / c.rbs;           // waves along H
+  const int kw = wave % kws, rsub = wave / kws;
+  const uint32_t groups = (uint32_t)(c.I + 16 * c.rbs - 1) / (uint32_t)(16 * c.rbs);
+  // the first task's expert is read beside the number of tasks, not after it
+  MoeExpert ex = expert_at(c, min(blockIdx.x / groups, (uint32_t)c.E - 1u));
+  const uint32_t tasks = __builtin_amdgcn_readfirstlane(c.count->active) * groups;
+  if (blockIdx.x >= tasks) return;
+  const auto rx = rsrc_of(c.x, ((uint32_t)(c.T - 1) * (uint32_t)c.ld_x + (uint32_t)c.H) * 2u);
+  const int units = (c.H + Rows::COLS - 1) / Rows::COLS;
+  const int u0 = kw * units / kws, u1 = (kw + 1) * units / kws;
+  auto row_of = [&](uint32_t task) { return min(((int)(task % groups) * c.rbs + rsub) * 16, c.I); };  // I: no rows
+  Unit<MX> wg, wu;
+  auto load = [&](const MoeExpert &e, int row0, int u) {
+    Rows(c.gate, (int)e.id, row0, c.I, c.H, lane).load(wg, u, lane);
+    Rows(c.up, (int)e.id, row0, c.I, c.H, lane).load(wu, u, lane);
+  };
+  auto from_of = [&](const MoeExpert &e, int at) {  // where the lane's token of the at-th 16 lies
+    return at * 16 + l16 < (int)e.n
+               ? (uint32_t)c.rows[e.first + at * 16 + l16].token * (uint32_t)c.ld_x * 2u + lane_bytes<MX>(g) : kNowhere;
+  };
+  if (u0 < u1) load(ex, row_of(blockIdx.x), u0);
+  uint32_t xo = from_of(ex, 0);
+#pragma unroll 1
+  for (uint32_t task = blockIdx.x; task < tasks; task += gridDim.x) {
+    const uint32_t nxt = task + gridDim.x;
+    const MoeExpert en = nxt < tasks ? expert_at(c, nxt / groups) : ex;
+    const int n = (int)ex.n, nb = (n + 15) / 16, row0 = row_of(task);
+    const uint32_t xn = from_of(en, 0);
+    f32x4 ag[TB], au[TB];
+#pragma unroll
+    for (int at = 0; at < TB; ++at) ag[at] = au[at] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int u = u0; u < u1; ++u) {
+      u32x4 x[Rows::STEPS][4];
+      factor<MX>(x, rx, xo, u, c.H, g);
+      // this unit's weights leave the registers, the next one's are on their way into them
+      const uint32_t sg = wg.scale, su = wu.scale;
+      stage<MX>(lds, wg, lane);
+      stage<MX>(lds + Rows::LDS, wu, lane);
+      __builtin_amdgcn_sched_barrier(0);
+      if (u + 1 < u1) load(ex, row0, u + 1);
+      else if (nxt < tasks) load(en, row_of(nxt), u0);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply<MX>(ag[0], au[0], lds, sg, su, x, lane);
+#pragma unroll
+      for (int at = 1; at < TB; ++at)
+        if (at < nb) {
+          factor<MX>(x, rx, from_of(ex, at), u, c.H, g);
+          multiply<MX>(ag[at], au[at], lds, sg, su, x, lane);
+        }
+    }
+    f32x4 *sums = reinterpret_cast<f32x4 *>(lds);  // [16 tokens][Wg, Wu][lane]
+#pragma unroll
+    for (int at = 0; at < TB; ++at)
+      if (at < nb) {
+        sums[at * 128 + lane] = ag[at];
+        sums[at * 128 + 64 + lane] = au[at];
+      }
+    __syncthreads();
+    // wave: 16 rows of the task and 16 tokens
+    for (int v = wave; v < c.rbs * nb; v += kWaves) {
+      const int rs = v % c.rbs, at = v / c.rbs;
+      const f32x4 *in = reinterpret_cast<const f32x4 *>(staged[rs * kws]) + at * 128 + lane;
+      f32x4 gs = in[0], us = in[64];
+      for (int w = 1; w < kws; ++w) {
+        gs = gs + in[w * AREA];
+        us = us + in[w * AREA + 64];
+      }
+      float h[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[i] = gs[i] / (1.f + expf(-gs[i])) * us[i];
+      const int row = ((int)(task % groups) * c.rbs + rs) * 16 + g * 4;  // I is a multiple of 8: all four exist or none
+      if (at * 16 + l16 < n && row < c.I)
+        *reinterpret_cast<uint64_t *>(c.hidden + (size_t)(ex.first + at * 16 + l16) * c.I + row) =
+            (uint64_t)pack_bf16(h[2], h[3]) << 32 | pack_bf16(h[0], h[1]);
+    }
+    __syncthreads();  // before the sums' place is staged into again
+    ex = en;
+    xo = xn;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// y = sum_j w_j Wd_j h_j.  A task is 32 rows of Wd for the experts of one of `segments` parts
 // of the list; the waves split those experts' columns end to end, each adding its
 // experts' weighted sums to its own rows of y in LDS, one per token (a token that did not
 // pick an expert gets nothing from it, whatever its weights hold).  With several segments
-// the last one to finish a row block adds them in order: no sum depends on timing.
+// the last one to finish a block of rows adds them in order: no sum depends on timing.
 // The weights' stream is kept up as above.
 template <bool MX, int TB>
 __global__ __launch_bounds__(kThreads, TB > 2 ? 2 : 4) void moe_down_kernel(MoeCall c) {
-  constexpr int U = 2;  // 128-column steps of a batch
   typedef Rows16<MX> Rows;
-  extern __shared__ __align__(16) unsigned char smem[];  // two areas [wave][token][16 rows], used in turn
-  __shared__ uint32_t last;
+  __shared__ u32x4 staged[kWaves][2 * Rows::LDS];        // a wave's units of the two row blocks
+  extern __shared__ __align__(16) unsigned char smem[];  // y: [wave][token][32 rows]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, g = lane >> 4;
+  u32x4 *lds = staged[wave];
   const int active = (int)__builtin_amdgcn_readfirstlane(c.count->active);
   const int segments = max(1, min(active, c.max_segments));
   const int tasks = c.row_blocks * segments;
   if ((int)blockIdx.x >= tasks) return;
   const auto rh = rsrc_of(c.hidden, (uint32_t)(c.T * c.k) * (uint32_t)c.I * 2u);
-  const int batches = (c.I + 128 * U - 1) / (128 * U);  // of one expert
-  const int area_floats = kWaves * c.T * 16;
-  typename Rows::Step wd[U];
-  struct Part {  // of a task: its rows, its first expert, and this wave's batches of all its experts, end to end
-    int row0, a0, b0, b1;
+  const int units = (c.I + Rows::COLS - 1) / Rows::COLS;  // of one expert
+  Unit<MX> w0, w1;
+  struct Part {  // of a task: its rows, its first expert, and this wave's units of all its experts, end to end
+    int row0, a0, u0, u1;
   };
   auto part_of = [&](int task) {
     const int seg = task % segments;
     Part p;
-    p.row0 = task / segments * 16;
+    p.row0 = task / segments * 32;
     p.a0 = seg * active / segments;
-    const int all = ((seg + 1) * active / segments - p.a0) * batches;
-    p.b0 = wave * all / kWaves;
-    p.b1 = (wave + 1) * all / kWaves;
+    const int all = ((seg + 1) * active / segments - p.a0) * units;
+    p.u0 = wave * all / kWaves;
+    p.u1 = (wave + 1) * all / kWaves;
     return p;
   };
-  auto load = [&](const Part &p, int b) {
-    const Rows rd(c.down, (int)expert_at(c, p.a0 + b / batches).id, p.row0, c.H, c.I, lane);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int s = b % batches * U + u;
-      rd.load(wd[u], s, lane, s * 128 < c.I);
-    }
+  auto load = [&](const Part &p, int u) {
+    const int e = (int)expert_at(c, p.a0 + u / units).id;
+    Rows(c.down, e, p.row0, c.H, c.I, lane).load(w0, u % units, lane);
+    Rows(c.down, e, min(p.row0 + 16, c.H), c.H, c.I, lane).load(w1, u % units, lane);
   };
   Part p = part_of(blockIdx.x);
-  if (p.b0 < p.b1) load(p, p.b0);
-  int turn = 0;
-  for (int task = blockIdx.x; task < tasks; task += gridDim.x, turn ^= 1) {
+  if (p.u0 < p.u1) load(p, p.u0);
+  float *y = reinterpret_cast<float *>(smem), *mine = y + wave * c.T * 32;
+#pragma unroll 1
+  for (int task = blockIdx.x; task < tasks; task += gridDim.x) {
     Part q{0, 0, 0, 0};
     if (task + (int)gridDim.x < tasks) q = part_of(task + gridDim.x);
-    float *area = reinterpret_cast<float *>(smem) + turn * area_floats, *mine = area + wave * c.T * 16;
-    for (int i = lane; i < c.T * 4; i += 64) reinterpret_cast<f32x4 *>(mine)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int b = p.b0; b < p.b1;) {
-      const MoeExpert ex = expert_at(c, p.a0 + b / batches);
+    for (int i = lane; i < c.T * 8; i += 64) reinterpret_cast<f32x4 *>(mine)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int u = p.u0; u < p.u1;) {
+      const MoeExpert ex = expert_at(c, p.a0 + u / units);
       const int n = (int)ex.n, nb = (n + 15) / 16;
-      const int end = min(p.b1, (b / batches + 1) * batches);
-      f32x4 acc[TB];
-      uint32_t ho[TB];
+      const int end = min(p.u1, (u / units + 1) * units);
+      auto from_of = [&](int at) {
+        return at * 16 + l16 < n ? (ex.first + at * 16 + l16) * (uint32_t)c.I * 2u + lane_bytes<MX>(g) : kNowhere;
+      };
+      f32x4 a0[TB], a1[TB];
+      MoeRow row[TB];
 #pragma unroll
       for (int at = 0; at < TB; ++at) {
-        acc[at] = f32x4{0.f, 0.f, 0.f, 0.f};
-        ho[at] = at * 16 + l16 < n ? (ex.first + at * 16 + l16) * (uint32_t)c.I * 2u : kNowhere;
+        a0[at] = a1[at] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (at * 16 + l16 < n) row[at] = c.rows[ex.first + at * 16 + l16];
       }
-      MoeRow row[TB];
-      for (; b < end; ++b) {
-        u32x4 x[U][4];
-        factor<Rows, U>(x, rh, ho[0], b % batches, c.I, g);
-        typename Rows::Step fd[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) fd[u] = wd[u];
-        if (b + 1 == end) {
-#pragma unroll
-          for (int at = 0; at < TB; ++at)
-            if (at * 16 + l16 < n) row[at] = c.rows[ex.first + at * 16 + l16];
-        }
+#pragma unroll 1
+      for (; u < end; ++u) {
+        u32x4 x[Rows::STEPS][4];
+        factor<MX>(x, rh, from_of(0), u % units, c.I, g);
+        const uint32_t s0 = w0.scale, s1 = w1.scale;
+        stage<MX>(lds, w0, lane);
+        stage<MX>(lds + Rows::LDS, w1, lane);
         __builtin_amdgcn_sched_barrier(0);
-        if (b + 1 < p.b1) load(p, b + 1);
-        else if (q.b0 < q.b1) load(q, q.b0);
+        if (u + 1 < p.u1) load(p, u + 1);
+        else if (q.u0 < q.u1) load(q, q.u0);
         __builtin_amdgcn_sched_barrier(0);
-        auto multiply = [&](int at) {
-#pragma unroll
-          for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[at] = mfma_bf16(Rows::operand(fd[u], i), x[u][i], acc[at]);
-        };
-        multiply(0);
+        multiply<MX>(a0[0], a1[0], lds, s0, s1, x, lane);
 #pragma unroll
         for (int at = 1; at < TB; ++at)
           if (at < nb) {
-            factor<Rows, U>(x, rh, ho[at], b % batches, c.I, g);
-            multiply(at);
+            factor<MX>(x, rh, from_of(at), u % units, c.I, g);
+            multiply<MX>(a0[at], a1[at], lds, s0, s1, x, lane);
           }
       }
       // this wave's part of the expert is whole: into its tokens' rows
 #pragma unroll
       for (int at = 0; at < TB; ++at)
         if (at * 16 + l16 < n) {
-          f32x4 *y = reinterpret_cast<f32x4 *>(mine + row[at].token * 16 + g * 4);
-          f32x4 v = *y;
+          f32x4 *to = reinterpret_cast<f32x4 *>(mine + row[at].token * 32 + g * 4);
+          f32x4 v0 = to[0], v1 = to[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = __builtin_fmaf(row[at].weight, acc[at][i], v[i]);
-          *y = v;
+          for (int i = 0; i < 4; ++i) {
+            v0[i] = __builtin_fmaf(row[at].weight, a0[at][i], v0[i]);
+            v1[i] = __builtin_fmaf(row[at].weight, a1[at][i], v1[i]);
+          }
+          to[0] = v0;
+          to[4] = v1;
         }
     }
-    if (p.b0 == p.b1 && q.b0 < q.b1) load(q, q.b0);
+    if (p.u0 == p.u1 && q.u0 < q.u1) load(q, q.u0);
     __syncthreads();
-    const int rb = p.row0 / 16, seg = task % segments;
-    const int tok = threadIdx.x >> 2, row = p.row0 + (threadIdx.x & 3) * 4;  // H is a multiple of 8
+    const int rb = task / segments, seg = task % segments;
+    const int tok = threadIdx.x >> 3, row = p.row0 + (threadIdx.x & 7) * 4;  // H is a multiple of 8
     const bool has = tok < c.T && row < c.H;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
     if (has) {
-      const f32x4 *in = reinterpret_cast<const f32x4 *>(area) + threadIdx.x;
+      const f32x4 *in = reinterpret_cast<const f32x4 *>(y) + threadIdx.x;
       v = in[0];
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) v = v + in[w * c.T * 4];
+      for (int w = 1; w < kWaves; ++w) v = v + in[w * c.T * 8];
     }
     bool store = has;
     if (segments > 1) {
@@ -582,9 +594,10 @@ __global__ __launch_bounds__(kThreads, TB > 2 ? 2 : 4) void moe_down_kernel(MoeC
         for (int i = 0; i < 4; ++i) put_device(c.sums + seg * whole + at + i, v[i]);
       }
       stores_done();
-      if (threadIdx.x == 0) last = add_device(c.joined + rb) + 1 == (uint32_t)segments;
+      uint32_t *last = reinterpret_cast<uint32_t *>(y);  // y has been read
+      if (threadIdx.x == 0) *last = add_device(c.joined + rb) + 1 == (uint32_t)segments;
       __syncthreads();
-      store = has && last;
+      store = has && *last != 0u;
       if (store) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = get_device(c.sums + at + i);
@@ -600,6 +613,7 @@ __global__ __launch_bounds__(kThreads, TB > 2 ? 2 : 4) void moe_down_kernel(MoeC
       o[1] = pack_bf16(v[2], v[3]);
       *reinterpret_cast<u32x2_e2 *>(c.y + (size_t)tok * c.ld_y + row) = o;
     }
+    __syncthreads();  // before y is cleared for the next task
     p = q;
   }
 }
@@ -613,16 +627,18 @@ struct MoeLayout {
 };
 MoeLayout layout_of(int T, int H, int I, int E, int k) {
   MoeLayout l{};
-  l.slices = std::max(1, std::min(16, (H + 128 * kRouteWaves - 1) / (128 * kRouteWaves)));  // one step a wave
-  l.row_blocks = (H + 15) / 16;
-  // parts of the second kind's tasks: two tasks a workgroup or more, so that the last ones to end
-  // are short, with at most E experts to share
-  l.segments = std::max(1, std::min(std::min(E, T * k), (1024 + l.row_blocks - 1) / l.row_blocks));
+  const int steps = kRouteWaves / (T <= 16 ? 1 : T <= 32 ? 2 : 4);  // of 128 columns, that a router workgroup takes at once
+  l.slices = std::max(1, std::min(16, (H + 128 * steps - 1) / (128 * steps)));
+  l.row_blocks = (H + 31) / 32;
+  // parts of the second product's tasks: one task a workgroup with few experts, two with many, so
+  // that the last ones to end are short
+  const int want = T * k <= 16 ? 512 : 1024;
+  l.segments = std::max(1, std::min(std::min(E, T * k), (want + l.row_blocks - 1) / l.row_blocks));
   size_t at = up16(sizeof(MoeCounters));
   l.plan = at, at += up16((size_t)E * sizeof(MoeExpert));
   l.rows = at, at += up16((size_t)T * k * sizeof(MoeRow));
   l.joined = at, at += up16((size_t)l.row_blocks * 4);
-  l.part = at, at += up16((size_t)l.slices * T * E * 4);
+  l.part = at, at += up16((size_t)l.slices * ((E + 15) / 16) * T * 64);
   l.hidden = at, at += up16((size_t)T * k * I * 2);
   l.sums = at, at += up16(l.segments > 1 ? (size_t)l.segments * T * H * 4 : 0);
   l.end = at;
@@ -681,10 +697,13 @@ int moe_launch(const occ_moe_args &a, hipStream_t s) {
   const MoeFn route = a.experts <= 64 ? route_fn<1>(tb) : a.experts <= 128 ? route_fn<2>(tb) : route_fn<8>(tb);
   hipLaunchKernelGGL(route, dim3((a.experts + 15) / 16 * l.slices), dim3(kRouteThreads), 0, s, c);
   if (hipGetLastError() != hipSuccess) return OCC_EHIP;
+  // the waves of a task of the first product split H in units; where it has fewer, more rows
+  const int units = mx ? (a.H + 255) / 256 : (a.H + 127) / 128;
+  c.rbs = units >= 8 ? 1 : units >= 4 ? 2 : units >= 2 ? 4 : 8;
   const unsigned grid = (unsigned)di->num_cus * 2;
   hipLaunchKernelGGL(mx ? up_fn<true>(tb) : up_fn<false>(tb), dim3(grid), dim3(kThreads), 0, s, c);
   if (hipGetLastError() != hipSuccess) return OCC_EHIP;
-  hipLaunchKernelGGL(mx ? down_fn<true>(tb) : down_fn<false>(tb), dim3(grid), dim3(kThreads), 2 * kWaves * a.tokens * 64, s, c);
+  hipLaunchKernelGGL(mx ? down_fn<true>(tb) : down_fn<false>(tb), dim3(grid), dim3(kThreads), kWaves * a.tokens * 128, s, c);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
 }
 

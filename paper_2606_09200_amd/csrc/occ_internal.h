@@ -168,7 +168,7 @@ struct MoeMatrix {
 struct MoeCall {
   int T, H, I, E, k;
   bool renorm;
-  int slices, row_blocks, max_segments, ld_x;
+  int slices, row_blocks, max_segments, ld_x, rbs;
   const uint16_t *x, *router;
   MoeMatrix gate, up, down;
   const uint8_t *mask;
@@ -180,7 +180,7 @@ struct MoeCall {
   MoeCounters *count;
   MoeExpert *plan;
   MoeRow *rows;
-  uint32_t *joined;  // per 16 rows of y: finished parts
+  uint32_t *joined;  // per 32 rows of y: finished parts
   float *part;       // partial logits
   uint16_t *hidden;  // rows x I, bf16
   float *sums;       // parts x T x H
