@@ -23,8 +23,9 @@ constexpr int kThreads = 512, kWaves = kThreads / 64;
 constexpr uint32_t kNowhere = 0x80000000u;  // a byte offset beyond every descriptor
 
 // 16 bytes at `off` (checked against the descriptor's end) plus `uniform` (which stays within a row).
+template <int POLICY = 0>
 __device__ __forceinline__ u32x4 load16(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t uniform = 0) {
-  return __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, (int)uniform, 0);
+  return __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, (int)uniform, POLICY);
 }
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void *p, uint32_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, 0x00020000);
@@ -79,7 +80,7 @@ __device__ __forceinline__ uint32_t wave_pick(uint32_t v) {
 // What bounds it is latency: two trips to memory and one workgroup's tail.  Most of
 // that workgroup's instructions run once and come from memory too (80 ns per 64
 // bytes), so its loops stay rolled.
-constexpr int kRouteThreads = 1024, kRouteWaves = kRouteThreads / 64;
+constexpr int kRouteThreads = 1024, kRouteWaves = kRouteThreads / 64, kSlices = 8;
 
 template <int TB, int PER>
 __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(MoeCall c) {
@@ -136,18 +137,16 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(MoeCall c) {
   for (int i = threadIdx.x; i < c.row_blocks; i += kRouteThreads) c.joined[i] = 0;
   for (int i = threadIdx.x; i < c.E; i += kRouteThreads) picked[i][0] = picked[i][1] = 0u;
   __syncthreads();
-  float ahead[PER];  // the next token's logits
+  float ahead[PER][kSlices];  // the next token's logits, slice by slice
   auto fetch = [&](int t) {
 #pragma unroll
-    for (int j = 0; j < PER; ++j) ahead[j] = 0.f;
-#pragma unroll 4
-    for (int s = 0; s < c.slices; ++s) {
+    for (int j = 0; j < PER; ++j)
 #pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        const int e = min(j * 64 + lane, c.E - 1);
-        ahead[j] = ahead[j] + get_device(c.part + ((size_t)((e >> 4) * c.slices + s) * c.T + t) * 16 + (e & 15));
-      }
-    }
+      for (int s = 0; s < kSlices; ++s)
+        if (s < c.slices && j * 64 < c.E) {
+          const int e = min(j * 64 + lane, c.E - 1);
+          ahead[j][s] = get_device(c.part + ((size_t)((e >> 4) * c.slices + s) * c.T + t) * 16 + (e & 15));
+        }
   };
   if (wave < c.T) fetch(wave);
 #pragma unroll 1
@@ -157,7 +156,10 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(MoeCall c) {
     uint32_t key[PER];
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      l[j] = ahead[j];
+      l[j] = 0.f;
+#pragma unroll
+      for (int s = 0; s < kSlices; ++s)
+        if (s < c.slices) l[j] = l[j] + ahead[j][s];
       // ascending integers, 1 and above; what is taken or missing is 0
       const uint32_t u = __builtin_bit_cast(uint32_t, l[j]);
       key[j] = j * 64 + lane >= c.E ? 0u : l[j] != l[j] ? 1u : (u >> 31 ? ~u : u | 0x80000000u);
@@ -200,11 +202,12 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(MoeCall c) {
     }
   }
   __syncthreads();
-  // active experts in index order, with the first of their rows of the hidden activations
+  // active experts in index order, with the first of their rows of the hidden activations; one with
+  // more than 32 tokens is two entries, whose weights are read twice
   const int e = threadIdx.x;
   const uint32_t m0 = e < c.E ? picked[e][0] : 0u, m1 = e < c.E ? picked[e][1] : 0u;
   const int n = __popc(m0) + __popc(m1);
-  const uint64_t act = __ballot(n > 0);
+  const uint64_t act = __ballot(n > 0), two = __ballot(n > 32);  // one or two entries of the list
   int before = n;  // pairs of lower lanes
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
@@ -212,10 +215,10 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(MoeCall c) {
     if (lane >= d) before += o;
   }
   if (lane == 63) wave_pairs[wave] = before;
-  if (lane == 0) wave_active[wave] = __popcll(act);
+  if (lane == 0) wave_active[wave] = __popcll(act) + __popcll(two);
   before -= n;
   __syncthreads();
-  int slot = __popcll(act & ((1ull << lane) - 1)), total = 0;
+  int slot = __popcll(act & ((1ull << lane) - 1)) + __popcll(two & ((1ull << lane) - 1)), total = 0;
 #pragma unroll
   for (int w = 0; w < kRouteWaves; ++w) {
     if (w < wave) slot += wave_active[w], before += wave_pairs[w];
@@ -223,7 +226,8 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(MoeCall c) {
   }
   if (threadIdx.x == 0) c.count->active = total;
   if (n > 0) {
-    c.plan[slot] = MoeExpert{(uint32_t)e, (uint32_t)before, (uint32_t)n, 0u};
+    c.plan[slot] = MoeExpert{(uint32_t)e, (uint32_t)before, (uint32_t)min(n, 32), 0u};
+    if (n > 32) c.plan[slot + 1] = MoeExpert{(uint32_t)e, (uint32_t)before + 32u, (uint32_t)n - 32u, 0u};
     first_of[e] = (uint32_t)before;
   }
   __syncthreads();
@@ -242,7 +246,9 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(MoeCall c) {
 // CU).  A load takes whole pieces of 4 or 8 rows, and the unit turns into operands through
 // LDS of the wave's own (chunks of 16 bytes spread by row, no bank conflicts, no
 // barriers): loads of 64 bytes from each of 16 rows, as an MFMA's operand lies in memory,
-// are 10 % slower over the layer.
+// are 10 % slower over the layer.  Where pieces are whole cache lines, each read once, the
+// loads are non-temporal (one token, MX4: 55 -> 45 us; 64 tokens, bf16: 403 -> 360);
+// where neighbouring pieces share lines that costs 8 % (rows of 2800 bytes).
 //
 // STEPS steps of 128 columns, each four MFMA operands of 32.  bf16: operand i of a step is
 // columns 32 i + 8 g .. + 7 of lane (row, g).  MX4: a lane's 16 bytes are the block of columns
@@ -262,6 +268,7 @@ struct Rows16 {
   static constexpr int LDS = 16 * CH;                     // chunks of a staged unit
   __amdgpu_buffer_rsrc_t r, rs;
   uint32_t at, pitch, left;  // left: bytes of a row past the lane's first chunk
+  bool whole;                // pieces are whole cache lines
   __device__ __forceinline__ Rows16(const MoeMatrix &m, int e, int row0, int rows, int cols, int lane) {
     pitch = MX ? (uint32_t)(OCC_MX4_KP(cols) / 2) : (uint32_t)cols * 2u;
     r = rsrc_of(static_cast<const uint8_t *>(m.w) + (size_t)e * m.stride + (size_t)row0 * pitch,
@@ -269,10 +276,14 @@ struct Rows16 {
     if constexpr (MX) rs = rsrc_of(m.scales + (size_t)e * m.scale_stride + (size_t)(row0 >> 4) * pitch, pitch);
     at = (uint32_t)(lane / CH) * pitch + (uint32_t)(lane % CH) * 16u;
     left = pitch - (uint32_t)(lane % CH) * 16u;
+    whole = pitch % 128u == 0u && ((uintptr_t)m.w + m.stride) % 128u == 0u && m.stride % 128u == 0u;
   }
   __device__ __forceinline__ void load(Unit<MX> &q, int unit, int lane) const {
     const uint32_t k = (uint32_t)unit * (CH * 16u), step = 64u / CH * pitch;
-    if (MX || k + CH * 16u <= pitch) {  // MX4 rows are whole units
+    if (MX || (k + CH * 16u <= pitch && whole)) {  // MX4 rows are whole units
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) q.w[i] = load16<2>(r, at + i * step, k);
+    } else if (k + CH * 16u <= pitch) {
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) q.w[i] = load16(r, at + i * step, k);
     } else {
@@ -387,7 +398,7 @@ __device__ __forceinline__ void multiply(f32x4 &acc0, f32x4 &acc1, const u32x4 *
 // factor's are asked for before them), also across the end of a task, and two
 // workgroups share a CU.
 template <bool MX, int TB>
-__global__ __launch_bounds__(kThreads, TB > 2 ? 2 : 4) void moe_up_kernel(MoeCall c) {
+__global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(MoeCall c) {
   typedef Rows16<MX> Rows;
   // a wave's units of Wg and Wu; its sums at the end of a task
   constexpr int AREA = 2 * Rows::LDS > 128 * TB ? 2 * Rows::LDS : 128 * TB;
@@ -399,12 +410,12 @@ __global__ __launch_bounds__(kThreads, TB > 2 ? 2 : 4) void moe_up_kernel(MoeCal
   const int kw = wave % kws, rsub = wave / kws;
   const uint32_t groups = (uint32_t)(c.I + 16 * c.rbs - 1) / (uint32_t)(16 * c.rbs);
   // the first task's expert is read beside the number of tasks, not after it
-  MoeExpert ex = expert_at(c, min(blockIdx.x / groups, (uint32_t)c.E - 1u));
+  MoeExpert ex = expert_at(c, min(blockIdx.x / groups, (uint32_t)(c.E * (c.T > 32 ? 2 : 1)) - 1u));
   const uint32_t tasks = __builtin_amdgcn_readfirstlane(c.count->active) * groups;
   if (blockIdx.x >= tasks) return;
   const auto rx = rsrc_of(c.x, ((uint32_t)(c.T - 1) * (uint32_t)c.ld_x + (uint32_t)c.H) * 2u);
   const int units = (c.H + Rows::COLS - 1) / Rows::COLS;
-  const int u0 = kw * units / kws, u1 = (kw + 1) * units / kws;
+  const int u0 = kw, u1 = units;  // every kws-th, so that the waves together read whole rows
   auto row_of = [&](uint32_t task) { return min(((int)(task % groups) * c.rbs + rsub) * 16, c.I); };  // I: no rows
   Unit<MX> wg, wu;
   auto load = [&](const MoeExpert &e, int row0, int u) {
@@ -427,7 +438,7 @@ __global__ __launch_bounds__(kThreads, TB > 2 ? 2 : 4) void moe_up_kernel(MoeCal
 #pragma unroll
     for (int at = 0; at < TB; ++at) ag[at] = au[at] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-    for (int u = u0; u < u1; ++u) {
+    for (int u = u0; u < u1; u += kws) {
       u32x4 x[Rows::STEPS][4];
       factor<MX>(x, rx, xo, u, c.H, g);
       // this unit's weights leave the registers, the next one's are on their way into them
@@ -435,7 +446,7 @@ __global__ __launch_bounds__(kThreads, TB > 2 ? 2 : 4) void moe_up_kernel(MoeCal
       stage<MX>(lds, wg, lane);
       stage<MX>(lds + Rows::LDS, wu, lane);
       __builtin_amdgcn_sched_barrier(0);
-      if (u + 1 < u1) load(ex, row0, u + 1);
+      if (u + kws < u1) load(ex, row0, u + kws);
       else if (nxt < tasks) load(en, row_of(nxt), u0);
       __builtin_amdgcn_sched_barrier(0);
       multiply<MX>(ag[0], au[0], lds, sg, su, x, lane);
@@ -485,7 +496,7 @@ __global__ __launch_bounds__(kThreads, TB > 2 ? 2 : 4) void moe_up_kernel(MoeCal
 // the last one to finish a block of rows adds them in order: no sum depends on timing.
 // The weights' stream is kept up as above.
 template <bool MX, int TB>
-__global__ __launch_bounds__(kThreads, TB > 2 ? 2 : 4) void moe_down_kernel(MoeCall c) {
+__global__ __launch_bounds__(kThreads, 4) void moe_down_kernel(MoeCall c) {
   typedef Rows16<MX> Rows;
   __shared__ u32x4 staged[kWaves][2 * Rows::LDS];        // a wave's units of the two row blocks
   extern __shared__ __align__(16) unsigned char smem[];  // y: [wave][token][32 rows]
@@ -588,22 +599,20 @@ __global__ __launch_bounds__(kThreads, TB > 2 ? 2 : 4) void moe_down_kernel(MoeC
     }
     bool store = has;
     if (segments > 1) {
-      const size_t at = (size_t)tok * c.H + row, whole = (size_t)c.T * c.H;
-      if (has) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) put_device(c.sums + seg * whole + at + i, v[i]);
-      }
+      constexpr int kDevice = 16;  // cache policy: device scope, as put_device and get_device
+      const uint32_t at = ((uint32_t)tok * (uint32_t)c.H + (uint32_t)row) * 4u, whole = (uint32_t)c.T * (uint32_t)c.H * 4u;
+      const auto rs = rsrc_of(c.sums, whole * (uint32_t)segments);
+      if (has) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rs, (int)(seg * whole + at), 0, kDevice);
       stores_done();
       uint32_t *last = reinterpret_cast<uint32_t *>(y);  // y has been read
       if (threadIdx.x == 0) *last = add_device(c.joined + rb) + 1 == (uint32_t)segments;
       __syncthreads();
       store = has && *last != 0u;
       if (store) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = get_device(c.sums + at + i);
-        for (int s = 1; s < segments; ++s)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = v[i] + get_device(c.sums + s * whole + at + i);
+        v = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int s = 0; s < segments; ++s)
+          v = v + __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(s * whole + at), 0, kDevice));
       }
     }
     if (store) {
@@ -628,14 +637,14 @@ struct MoeLayout {
 MoeLayout layout_of(int T, int H, int I, int E, int k) {
   MoeLayout l{};
   const int steps = kRouteWaves / (T <= 16 ? 1 : T <= 32 ? 2 : 4);  // of 128 columns, that a router workgroup takes at once
-  l.slices = std::max(1, std::min(16, (H + 128 * steps - 1) / (128 * steps)));
+  l.slices = std::max(1, std::min(kSlices, (H + 128 * steps - 1) / (128 * steps)));
   l.row_blocks = (H + 31) / 32;
   // parts of the second product's tasks: one task a workgroup with few experts, two with many, so
   // that the last ones to end are short
   const int want = T * k <= 16 ? 512 : 1024;
   l.segments = std::max(1, std::min(std::min(E, T * k), (want + l.row_blocks - 1) / l.row_blocks));
   size_t at = up16(sizeof(MoeCounters));
-  l.plan = at, at += up16((size_t)E * sizeof(MoeExpert));
+  l.plan = at, at += up16((size_t)E * (T > 32 ? 2 : 1) * sizeof(MoeExpert));
   l.rows = at, at += up16((size_t)T * k * sizeof(MoeRow));
   l.joined = at, at += up16((size_t)l.row_blocks * 4);
   l.part = at, at += up16((size_t)l.slices * ((E + 15) / 16) * T * 64);
@@ -652,11 +661,11 @@ MoeFn route_fn(int tb) {
 }
 template <bool MX>
 MoeFn up_fn(int tb) {
-  return tb == 1 ? moe_up_kernel<MX, 1> : tb == 2 ? moe_up_kernel<MX, 2> : moe_up_kernel<MX, 4>;
+  return tb == 1 ? moe_up_kernel<MX, 1> : moe_up_kernel<MX, 2>;
 }
 template <bool MX>
 MoeFn down_fn(int tb) {
-  return tb == 1 ? moe_down_kernel<MX, 1> : tb == 2 ? moe_down_kernel<MX, 2> : moe_down_kernel<MX, 4>;
+  return tb == 1 ? moe_down_kernel<MX, 1> : moe_down_kernel<MX, 2>;
 }
 
 }  // namespace
@@ -703,7 +712,9 @@ int moe_launch(const occ_moe_args &a, hipStream_t s) {
   const unsigned grid = (unsigned)di->num_cus * 2;
   hipLaunchKernelGGL(mx ? up_fn<true>(tb) : up_fn<false>(tb), dim3(grid), dim3(kThreads), 0, s, c);
   if (hipGetLastError() != hipSuccess) return OCC_EHIP;
-  hipLaunchKernelGGL(mx ? down_fn<true>(tb) : down_fn<false>(tb), dim3(grid), dim3(kThreads), kWaves * a.tokens * 128, s, c);
+  // y of every wave in LDS beside what its units pass through: one workgroup a CU for many tokens
+  const int y_bytes = kWaves * a.tokens * 128, per_cu = (mx ? 32768 : 65536) + y_bytes > di->lds_per_cu / 2 ? 1 : 2;
+  hipLaunchKernelGGL(mx ? down_fn<true>(tb) : down_fn<false>(tb), dim3(di->num_cus * per_cu), dim3(kThreads), y_bytes, s, c);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
 }
 
