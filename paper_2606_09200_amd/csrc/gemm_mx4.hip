@@ -64,32 +64,46 @@ int choose_tile(const Mx4GemmCall &c, int num_cus, int room) {
   return best;
 }
 
+// A B that is read once and exceeds the eight 4 MB L2s goes past them.
+constexpr long long kNtBytes = 32ll << 20;
+
 typedef void (*SkinnyFn)(Mx4Operands, int);
-template <class OUT, bool NT>
-SkinnyFn skinny_fn(int kw, int ut) {
-  if (ut == 2)
-    return kw == 8 ? gemm_mx4_skinny_kernel<8, 2, OUT, NT> : kw == 4 ? gemm_mx4_skinny_kernel<4, 2, OUT, NT>
-         : kw == 2 ? gemm_mx4_skinny_kernel<2, 2, OUT, NT> : gemm_mx4_skinny_kernel<1, 2, OUT, NT>;
-  return kw == 8 ? gemm_mx4_skinny_kernel<8, 1, OUT, NT> : kw == 4 ? gemm_mx4_skinny_kernel<4, 1, OUT, NT>
-       : kw == 2 ? gemm_mx4_skinny_kernel<2, 1, OUT, NT> : gemm_mx4_skinny_kernel<1, 1, OUT, NT>;
+
+template <class OUT>
+SkinnyFn skinny_fn(int kw, int xs, bool nt) {
+  if (xs == 2) return nt ? gemm_mx4_skinny_kernel<8, 2, OUT, true> : gemm_mx4_skinny_kernel<8, 2, OUT, false>;
+  if (kw == 8) return nt ? gemm_mx4_skinny_kernel<8, 1, OUT, true> : gemm_mx4_skinny_kernel<8, 1, OUT, false>;
+  return kw == 4 ? gemm_mx4_skinny_kernel<4, 1, OUT, false> : kw == 2 ? gemm_mx4_skinny_kernel<2, 1, OUT, false>
+                                                                    : gemm_mx4_skinny_kernel<1, 1, OUT, false>;
+}
+
+// The pad's limit, once it is known to fit: an attribute that matters to pads only.
+int allow_lds(const void *fn, size_t lds_bytes, int own, const DeviceInfo &di) {
+  if ((size_t)own + lds_bytes > (size_t)di.max_lds_per_wg) return OCC_ELDS;
+  if (lds_bytes == 0) return OCC_OK;
+  return hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, di.max_lds_per_wg - own) == hipSuccess ? OCC_OK
+                                                                                                                   : OCC_EHIP;
 }
 
 int launch_skinny(const Mx4GemmCall &c, const Mx4Operands &o, const DeviceInfo &di, hipStream_t s) {
-  // the largest power of two of waves along K that all have a k-step
+  // waves along K: one a k-step, up to 8
   int kw = 1;
-  while (kw < 8 && kw * 2 <= o.steps512) kw *= 2;
-  // 32-column units share A's loads between two blocks; 16-column ones where those would leave CUs idle
-  const int ut = ceil_div(c.N, 32) * kw >= di.num_cus * 8 ? 2 : 1;
-  const int units = ceil_div(c.N, 16 * ut);
-  const bool nt = (long long)c.N * o.pitch > (256ll << 20);  // B is read once and exceeds the last-level cache
-  const SkinnyFn fn = c.dtype == OCC_BF16 ? (nt ? skinny_fn<uint16_t, true>(kw, ut) : skinny_fn<uint16_t, false>(kw, ut))
-                                          : (nt ? skinny_fn<float, true>(kw, ut) : skinny_fn<float, false>(kw, ut));
-  const int own = 8 * ut * 64 * 16;
-  if ((size_t)own + c.lds_bytes > (size_t)di.max_lds_per_wg) return OCC_ELDS;
-  if (c.lds_bytes > 0 && hipFuncSetAttribute(reinterpret_cast<const void *>(fn), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                             di.max_lds_per_wg - own) != hipSuccess)
-    return OCC_EHIP;
-  hipLaunchKernelGGL(fn, dim3(ceil_div(units, 8 / kw)), dim3(512), (int)c.lds_bytes, s, o, units);
+  while (kw < 8 && kw < o.steps512) kw *= 2;
+  const int xs = std::max(1, ceil_div(o.steps512, kw));
+  if (xs > 2) {  // A does not fit in registers
+    typedef void (*LongFn)(Mx4Operands);
+    const LongFn fn = c.dtype == OCC_BF16 ? gemm_mx4_skinny_long_kernel<uint16_t> : gemm_mx4_skinny_long_kernel<float>;
+    const int st = allow_lds(reinterpret_cast<const void *>(fn), c.lds_bytes, 8 * 2 * 1024, di);
+    if (st != OCC_OK) return st;
+    hipLaunchKernelGGL(fn, dim3(ceil_div(c.N, 32)), dim3(512), (int)c.lds_bytes, s, o);
+    return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
+  }
+  const bool nt = (long long)c.N * o.pitch > kNtBytes;
+  const SkinnyFn fn = c.dtype == OCC_BF16 ? skinny_fn<uint16_t>(kw, xs, nt) : skinny_fn<float>(kw, xs, nt);
+  const int st = allow_lds(reinterpret_cast<const void *>(fn), c.lds_bytes, 8 * 4096 + 16 * 1024, di);
+  if (st != OCC_OK) return st;
+  const int units = ceil_div(c.N, 16);
+  hipLaunchKernelGGL(fn, dim3(std::min(ceil_div(units, 8 / kw), 2 * di.num_cus)), dim3(512), (int)c.lds_bytes, s, o, units);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
 }
 
