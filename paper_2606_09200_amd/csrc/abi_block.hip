@@ -46,11 +46,6 @@ bool mx4_pointers(const void *codes, const void *scales) {
   return codes != nullptr && scales != nullptr && aligned(codes, 16) && aligned(scales, 16);
 }
 
-int current_device() {
-  const DeviceInfo *di = nullptr;
-  return current_device_info(&di);
-}
-
 }  // namespace
 
 int validate_mx4_quant(const Mx4QuantCall &c) {
@@ -204,16 +199,14 @@ extern "C" {
 int occ_mx4_quantize(const void *x, int dtype, int rows, int cols, size_t ld, void *codes, void *scales,
                      void *codes_t, void *scales_t, void *stream) {
   const occ::Mx4QuantCall c{x, dtype, rows, cols, ld, codes, scales, codes_t, scales_t};
-  int st = occ::validate_mx4_quant(c);
-  if (st == OCC_OK) st = occ::current_device();
+  const int st = occ::validate_mx4_quant(c);
   return st == OCC_OK ? occ::mx4_quant_launch(c, static_cast<hipStream_t>(stream)) : st;
 }
 
 int occ_mx4_dequantize(const void *codes, const void *scales, int rows, int cols, void *out, int dtype, size_t ld,
                        void *stream) {
   const occ::Mx4DequantCall c{codes, scales, rows, cols, out, dtype, ld};
-  int st = occ::validate_mx4_dequant(c);
-  if (st == OCC_OK) st = occ::current_device();
+  const int st = occ::validate_mx4_dequant(c);
   return st == OCC_OK ? occ::mx4_dequant_launch(c, static_cast<hipStream_t>(stream)) : st;
 }
 

@@ -26,19 +26,5 @@ __device__ __forceinline__ float mx4_scale_value(uint32_t s) {
   return __builtin_bit_cast(float, bits);
 }
 
-// Codes of 8 values whose block has scale byte s: the hardware's conversion
-// divides by the scale and rounds to nearest-even with saturation, as the format
-// asks (checked on every scale and on ties).
-__device__ __forceinline__ uint32_t mx4_codes8(const float (&v)[8], uint32_t s) {
-  if (s == 255u) return 0u;
-  const float sc = mx4_scale_value(s);
-  uint32_t w = 0;
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], sc, 0);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], sc, 1);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], sc, 2);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], sc, 3);
-  return w;
-}
-
 }  // namespace
 }  // namespace occ
