@@ -172,20 +172,21 @@ __global__ __launch_bounds__(T::NT) void gemm_mx4_pp_kernel(Mx4Operands o, int t
     wait_vmcnt<0>();  // the DMA issued past the last k-step, before the stages get other use
     barrier();
 
+    typedef TileOut<T::BN, typename T::Out> Out;
+    static_assert(128 * Out::PITCH <= T::LDS_BYTES, "half a tile of C");
     int el = lane;
     asm volatile("" : "+v"(el));  // keeps the addresses below out of the k-loop's registers
-    const int em = el & 15;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int mb = m0 + h * 128 + half * 64 + i * 16;  // first row of the block
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb)
-          store_mx4_pair(static_cast<typename T::Out *>(o.C), M, N, mb, em, n0 + hb * 128 + wn * 32, el,
-                         acc[h][i][2 * hb], acc[h][i][2 * hb + 1]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+        for (int j = 0; j < 4; ++j)
+          Out::put(smem, half * 64 + i * 16, (j >> 1) * 128 + wn * 32 + (j & 1) * 16, el, acc[h][i][j]);
+      __syncthreads();
+      Out::template store<128, T::NT>(smem, static_cast<typename T::Out *>(o.C), M, N, m0 + h * 128, n0);
+      __syncthreads();
+    }
   }
 }
 

@@ -41,7 +41,6 @@ struct Mx4Rp {
   static constexpr int LDS_BYTES = STAGES * STAGE_BYTES;
   static constexpr int NG = KS / GS;                // fragment groups per k-step
   static_assert(KS % GS == 0 && (NG == 1 || NG % 2 == 0), "groups alternate between two register sets");
-  static_assert(FN % 2 == 0, "16-column blocks are stored in pairs");
   static_assert(BM % RPP == 0 && BN % RPP == 0 && RPP % 16 == 0, "uneven load passes, or a swizzle that changes between them");
   static_assert((STAGES - 1) * LOADS <= 63, "vmcnt holds at most 63");
 };
@@ -198,14 +197,17 @@ __global__ __launch_bounds__(T::NT) void gemm_mx4_rp_kernel(Mx4Operands o, int t
     wait_vmcnt<0>();  // the DMA issued past the last k-step, before the stages get other use
     publish();
 
+    typedef TileOut<T::BN, typename T::Out> Out;
+    static_assert(T::BM * Out::PITCH <= T::LDS_BYTES, "a tile of C");
     int el = lane;
     asm volatile("" : "+v"(el));  // keeps the addresses below out of the k-loop's registers
 #pragma unroll
     for (int i = 0; i < T::FM; ++i)
 #pragma unroll
-      for (int jp = 0; jp < T::FN / 2; ++jp)
-        store_mx4_pair(static_cast<typename T::Out *>(o.C), M, N, m0 + (wm * T::FM + i) * 16, el & 15,
-                       n0 + wn * T::FN * 16 + jp * 32, el, acc[i][2 * jp], acc[i][2 * jp + 1]);
+      for (int j = 0; j < T::FN; ++j) Out::put(smem, (wm * T::FM + i) * 16, (wn * T::FN + j) * 16, el, acc[i][j]);
+    __syncthreads();
+    Out::template store<T::BM, T::NT>(smem, static_cast<typename T::Out *>(o.C), M, N, m0, n0);
+    __syncthreads();
   }
 }
 
