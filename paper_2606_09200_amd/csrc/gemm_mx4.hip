@@ -33,6 +33,8 @@ constexpr Mx4Tile tile_of(Mx4Fn bf16, Mx4Fn f32, int per_cu, double fixed, doubl
 template <class OUT>
 using Rp128x128 = Mx4Rp<128, 128, 2, 4, 2, 1, OUT>;
 template <class OUT>
+using Rp128x64 = Mx4Rp<128, 64, 4, 2, 3, 2, OUT>;
+template <class OUT>
 using Rp64x64 = Mx4Rp<64, 64, 2, 2, 4, 4, OUT>;
 template <class OUT>
 using Rp32x64 = Mx4Rp<32, 64, 2, 2, 4, 4, OUT>;
@@ -40,9 +42,11 @@ using Rp32x64 = Mx4Rp<32, 64, 2, 2, 4, 4, OUT>;
 const Mx4Tile kTiles[] = {
     tile_of<Mx4Pp>(gemm_mx4_pp_kernel<Mx4Pp<uint16_t>>, gemm_mx4_pp_kernel<Mx4Pp<float>>, 1, 4.0, 2.2),
     tile_of<Rp128x128>(gemm_mx4_rp_kernel<Rp128x128<uint16_t>>, gemm_mx4_rp_kernel<Rp128x128<float>>, 1, 2.0, 0.9),
+    tile_of<Rp128x64>(gemm_mx4_rp_kernel<Rp128x64<uint16_t>>, gemm_mx4_rp_kernel<Rp128x64<float>>, 1, 1.8, 0.6),
     tile_of<Rp64x64>(gemm_mx4_rp_kernel<Rp64x64<uint16_t>>, gemm_mx4_rp_kernel<Rp64x64<float>>, 1, 1.6, 0.4),
     tile_of<Rp32x64>(gemm_mx4_rp_kernel<Rp32x64<uint16_t>>, gemm_mx4_rp_kernel<Rp32x64<float>>, 1, 1.3, 0.33),
 };
+constexpr int kMaxDevices = 64;
 constexpr int kNumTiles = (int)(sizeof kTiles / sizeof kTiles[0]);
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
@@ -120,12 +124,21 @@ int mx4_gemm_launch(const Mx4GemmCall &c, hipStream_t s) {
   if (c.M <= 16) return launch_skinny(c, o, *di, s);
   if (c.lds_bytes > (size_t)di->max_lds_per_wg) return OCC_ELDS;
   // the pad keeps the tile: it lowers residency and changes nothing else, and is never clamped
-  const Mx4Tile &t = kTiles[choose_tile(c, di->num_cus, di->max_lds_per_wg)];
+  const int id = choose_tile(c, di->num_cus, di->max_lds_per_wg);
+  const Mx4Tile &t = kTiles[id];
   if ((size_t)t.lds + c.lds_bytes > (size_t)di->max_lds_per_wg) return OCC_ELDS;
   const Mx4Fn fn = c.dtype == OCC_BF16 ? t.bf16 : t.f32;
-  if (hipFuncSetAttribute(reinterpret_cast<const void *>(fn), hipFuncAttributeMaxDynamicSharedMemorySize,
-                          di->max_lds_per_wg) != hipSuccess)
-    return OCC_EHIP;
+  // the dynamic-LDS limit is a per-device attribute of each kernel: set once
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return OCC_ENODEV;
+  static bool attr_set[kMaxDevices][kNumTiles][2] = {};
+  bool &set = attr_set[dev][id][c.dtype == OCC_F32];
+  if (!set) {
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(fn), hipFuncAttributeMaxDynamicSharedMemorySize,
+                            di->max_lds_per_wg) != hipSuccess)
+      return OCC_EHIP;
+    set = true;
+  }
   const int tm = ceil_div(c.M, t.bm), tn = ceil_div(c.N, t.bn);
   hipLaunchKernelGGL(fn, dim3(tm * tn), dim3(t.threads), t.lds + (int)c.lds_bytes, s, o, tm, tn);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
