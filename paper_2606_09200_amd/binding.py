@@ -524,24 +524,42 @@ def occ_overlap_enqueue_noalloc(A, B, C, *, comm_stream, err=None, bufs=None, ou
 
 # ------------------------------------------------------------------ operators of a block
 
+# These calls are short (a decode step's run for 5 us), so their checks ask a tensor for little: the
+# contiguous case first, sizes as one tuple, addresses as plain integers.
 _FLOAT_TYPES = {torch.bfloat16: OCC_BF16, torch.float32: OCC_F32}
 
 
+def _raw_stream(stream):
+    """The hipStream_t as an integer; the current one where CUDA is known to be in use."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
 def _float_type(name, t):
-    if t.dtype not in _FLOAT_TYPES or not t.is_cuda:
+    kind = _FLOAT_TYPES.get(t.dtype)
+    if kind is None or not t.is_cuda:
         raise ValueError("%s must be a bfloat16 or float32 GPU tensor" % name)
-    return _FLOAT_TYPES[t.dtype]
+    return kind
 
 
-def _rows(name, t, shape=None):
-    """(type, row pitch) of a 2-D GPU tensor whose rows are contiguous."""
-    kind = _float_type(name, t)
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
-        raise ValueError("%s must have shape %s" % (name, "(rows, cols)" if shape is None else tuple(shape)))
-    rows, cols = t.shape
-    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+def _pitch(name, t, rows, cols):
+    """Row pitch of a (rows, cols) tensor whose rows are contiguous."""
+    if t.shape != (rows, cols):
+        raise ValueError("%s must have shape (%d, %d)" % (name, rows, cols))
+    if t.is_contiguous():
+        return cols
+    ld, one = t.stride()
+    if (cols > 1 and one != 1) or (rows > 1 and ld < cols):
         raise ValueError("%s must have contiguous rows that do not overlap" % name)
-    return kind, (t.stride(0) if rows > 1 else cols)
+    return ld if rows > 1 else cols
+
+
+def _sizes(name, t):
+    """(rows, cols) of a 2-D tensor."""
+    if t.dim() != 2:
+        raise ValueError("%s must have two dimensions" % name)
+    return t.shape
 
 
 class Mx4:
@@ -575,86 +593,90 @@ def mx4_empty(rows, cols, batch=(), device="cuda"):
                torch.empty(batch + ((rows + 15) // 16, half), dtype=torch.uint8, device=device), rows, cols)
 
 
-def _mx4(name, q, rows=None, cols=None):
+def _mx4(name, q, rows, cols):
+    """Addresses of the codes and scales of one matrix."""
     if not isinstance(q, Mx4) or q.codes.dim() != 2 or not q.codes.is_cuda:
         raise ValueError("%s must be one Mx4 matrix on the GPU" % name)
-    if (rows is not None and q.rows != rows) or (cols is not None and q.cols != cols):
-        raise ValueError("%s must be %s x %s" % (name, rows, cols))
-    return _ptr(q.codes), _ptr(q.scales)
+    if q.rows != rows or q.cols != cols:
+        raise ValueError("%s must be %d x %d" % (name, rows, cols))
+    return q.codes.data_ptr(), q.scales.data_ptr()
 
 
 def occ_mx4_quantize(x, out=None, out_t=None, stream=None):
     """x (rows x cols, bf16 or fp32, contiguous rows) to MX4: ``out`` in blocks along
     its rows and ``out_t`` (cols x rows) in blocks along its columns, either or both
     from one read.  Returns (out, out_t)."""
-    kind, ld = _rows("x", x)
-    rows, cols = x.shape
-    null = (_P(0), _P(0))
-    q = null if out is None else _mx4("out", out, rows, cols)
-    qt = null if out_t is None else _mx4("out_t", out_t, cols, rows)
-    if out is None and out_t is None:
+    kind = _float_type("x", x)
+    rows, cols = _sizes("x", x)
+    ld = _pitch("x", x, rows, cols)
+    codes = scales = codes_t = scales_t = None
+    if out is not None:
+        codes, scales = _mx4("out", out, rows, cols)
+    if out_t is not None:
+        codes_t, scales_t = _mx4("out_t", out_t, cols, rows)
+    elif out is None:
         raise ValueError("out or out_t must be given")
-    if x.numel() > 0:
-        _check(lib().occ_mx4_quantize(_ptr(x), kind, rows, cols, ld, *q, *qt, _stream(stream)), "occ_mx4_quantize")
+    if rows and cols:
+        st = lib().occ_mx4_quantize(x.data_ptr(), kind, rows, cols, ld, codes, scales, codes_t, scales_t,
+                                    _raw_stream(stream))
+        if st:
+            raise OccError(st, "occ_mx4_quantize")
     return out, out_t
 
 
 def occ_mx4_dequantize(q, out, stream=None):
     """The values of an Mx4 matrix, to out (rows x cols, bf16 or fp32)."""
-    kind, ld = _rows("out", out, (q.rows, q.cols))
-    if out.numel() > 0:
-        _check(lib().occ_mx4_dequantize(*_mx4("q", q), q.rows, q.cols, _ptr(out), kind, ld, _stream(stream)),
-               "occ_mx4_dequantize")
+    kind = _float_type("out", out)
+    rows, cols = _sizes("out", out)
+    codes, scales = _mx4("q", q, rows, cols)
+    ld = _pitch("out", out, rows, cols)
+    if rows and cols:
+        st = lib().occ_mx4_dequantize(codes, scales, rows, cols, out.data_ptr(), kind, ld, _raw_stream(stream))
+        if st:
+            raise OccError(st, "occ_mx4_dequantize")
     return out
 
 
 def occ_gemm_mx4(A, B, C, lds_bytes=0, stream=None):
     """C = A @ B.T of MX4 operands (fp32 accumulation): A M x K, B N x K (a linear
     layer's weight), C M x N bfloat16 or float32."""
-    a, b = _mx4("A", A), _mx4("B", B, cols=A.cols)
     kind = _float_type("C", C)
-    if tuple(C.shape) != (A.rows, B.rows) or not C.is_contiguous():
+    M, N = _sizes("C", C)
+    K = A.cols if isinstance(A, Mx4) else -1
+    a, a_scales = _mx4("A", A, M, K)
+    b, b_scales = _mx4("B", B, N, K)
+    if not C.is_contiguous():
         raise ValueError("C must be a contiguous (M, N) tensor")
-    _check(lib().occ_gemm_mx4(*a, *b, _ptr(C), kind, A.rows, B.rows, A.cols, int(lds_bytes), _stream(stream)),
-           "occ_gemm_mx4")
+    st = lib().occ_gemm_mx4(a, a_scales, b, b_scales, C.data_ptr(), kind, M, N, K, lds_bytes, _raw_stream(stream))
+    if st:
+        raise OccError(st, "occ_gemm_mx4")
     return C
 
 
-def _norm_args(f, res, w_post, w_pre, gate, alpha, eps, post):
-    """The fields forward and backward share; `res` is a tensor of the residual's type."""
-    n = occ_norm_args()
-    n.act, n.ld_f = _rows("f", f)
-    n.rows, n.D = f.shape
-    n.res = _float_type("the residual", res)
-    n.post, n.alpha, n.eps, n.groups = int(bool(post)), float(alpha), float(eps), 1
-    n.f = _ptr(f).value
-    for name, t in (("w_post", w_post), ("w_pre", w_pre)):
-        if t is not None:
-            if t.dtype != f.dtype or not t.is_cuda or tuple(t.shape) != (n.D,) or not t.is_contiguous():
-                raise ValueError("%s must be a contiguous (D,) GPU tensor of f's type" % name)
-            setattr(n, name, _ptr(t).value)
-    if gate is not None:
-        if gate.dtype != f.dtype or not gate.is_cuda or gate.dim() != 2 or gate.shape[1] != n.D \
-                or not gate.is_contiguous():
-            raise ValueError("gate must be a contiguous (groups, D) GPU tensor of f's type")
-        n.groups, n.gate = gate.shape[0], _ptr(gate).value
-    return n
-
-
-def _norm_rows(n, name, t, like):
-    """Row tensor `name` of like's type and (rows, D) into the arguments."""
+def _param(name, t, dtype, shape):
+    """Address of a contiguous GPU tensor of that type and shape, None for None."""
     if t is None:
-        return
-    if t.dtype != like.dtype:
-        raise ValueError("%s must be of type %s" % (name, like.dtype))
-    setattr(n, "ld_" + name, _rows(name, t, (n.rows, n.D))[1])
-    setattr(n, name, _ptr(t).value)
+        return None
+    if t.dtype != dtype or not t.is_cuda or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s GPU tensor of shape %s" % (name, dtype, shape))
+    return t.data_ptr()
 
 
-def _f32(name, t, shape):
-    if t.dtype != torch.float32 or not t.is_cuda or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous float32 GPU tensor of shape %s" % (name, tuple(shape)))
-    return _ptr(t).value
+def _row_arg(name, t, dtype, rows, cols):
+    """(address, pitch) of a row tensor, (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if t.dtype != dtype or not t.is_cuda:
+        raise ValueError("%s must be a %s GPU tensor" % (name, dtype))
+    return t.data_ptr(), _pitch(name, t, rows, cols)
+
+
+def _gate_arg(gate, dtype, D):
+    """(address, groups)."""
+    if gate is None:
+        return None, 1
+    groups = _sizes("gate", gate)[0]
+    return _param("gate", gate, dtype, (groups, D)), groups
 
 
 def occ_norm_gate(f, x, y, h=None, *, w_post=None, w_pre=None, gate=None, alpha=1.0, eps=1e-6, post=True, rstd=None,
@@ -662,13 +684,19 @@ def occ_norm_gate(f, x, y, h=None, *, w_post=None, w_pre=None, gate=None, alpha=
     """y = alpha x + gate * norm(f) w_post and, with ``h``, h = norm(y) w_pre, for rows of f (a
     block's output) and x (the residual).  gate: (groups, D), row r's is row r // (rows / groups).
     ``rstd`` (rows, 2 fp32) receives what the backward needs.  Returns (y, h)."""
-    n = _norm_args(f, x, w_post, w_pre, gate, alpha, eps, post)
-    _norm_rows(n, "x", x, x)
-    _norm_rows(n, "y", y, x)
-    _norm_rows(n, "h", h, f)
-    if rstd is not None:
-        n.rstd = _f32("rstd", rstd, (n.rows, 2))
-    _check(lib().occ_norm_gate(ctypes.byref(n), _stream(stream)), "occ_norm_gate")
+    act, res = _float_type("f", f), _float_type("x", x)
+    rows, D = _sizes("f", f)
+    one, two = f.dtype, x.dtype
+    g, groups = _gate_arg(gate, one, D)
+    x_ptr, ld_x = _row_arg("x", x, two, rows, D)
+    y_ptr, ld_y = _row_arg("y", y, two, rows, D)
+    h_ptr, ld_h = _row_arg("h", h, one, rows, D)
+    n = occ_norm_args(rows, D, act, res, 1 if post else 0, groups, alpha, eps, f.data_ptr(), x_ptr,
+                      _param("w_post", w_post, one, (D,)), _param("w_pre", w_pre, one, (D,)), g, y_ptr, h_ptr,
+                      _param("rstd", rstd, torch.float32, (rows, 2)), _pitch("f", f, rows, D), ld_x, ld_y, ld_h)
+    st = lib().occ_norm_gate(ctypes.byref(n), _raw_stream(stream))
+    if st:
+        raise OccError(st, "occ_norm_gate")
     return y, h
 
 
@@ -682,25 +710,55 @@ def occ_norm_gate_bwd(dy, dh, f, y, rstd, df=None, dx=None, *, w_post=None, w_pr
     """Gradients of occ_norm_gate from dy and dh (either None for zero), with the forward's f,
     y, rstd, weights and gate; each output None is not made.  df is of f's type, dx of
     y's, the parameters' gradients are fp32.  Returns (df, dx)."""
-    n = _norm_args(f, y, w_post, w_pre, gate, alpha, 0.0, post)
-    _norm_rows(n, "y", y, y)
-    for name, t, like in (("dy", dy, y), ("dh", dh, f), ("df", df, f), ("dx", dx, y)):
-        _norm_rows(n, name, t, like)
-    n.rstd = _f32("rstd", rstd, (n.rows, 2))
-    for name, t, shape in (("dw_post", dw_post, (n.D,)), ("dw_pre", dw_pre, (n.D,)), ("dgate", dgate, (n.groups, n.D))):
-        if t is not None:
-            setattr(n, name, _f32(name, t, shape))
-    if workspace is not None:
-        if not workspace.is_cuda or not workspace.is_contiguous():
-            raise ValueError("workspace must be a contiguous GPU tensor")
-        n.workspace, n.workspace_bytes = _ptr(workspace).value, workspace.numel() * workspace.element_size()
-    _check(lib().occ_norm_gate_bwd(ctypes.byref(n), _stream(stream)), "occ_norm_gate_bwd")
+    act, res = _float_type("f", f), _float_type("y", y)
+    rows, D = _sizes("f", f)
+    one, two, f32 = f.dtype, y.dtype, torch.float32
+    g, groups = _gate_arg(gate, one, D)
+    y_ptr, ld_y = _row_arg("y", y, two, rows, D)
+    dy_ptr, ld_dy = _row_arg("dy", dy, two, rows, D)
+    dh_ptr, ld_dh = _row_arg("dh", dh, one, rows, D)
+    df_ptr, ld_df = _row_arg("df", df, one, rows, D)
+    dx_ptr, ld_dx = _row_arg("dx", dx, two, rows, D)
+    ws, ws_bytes = _workspace_arg(workspace)
+    n = occ_norm_args(rows, D, act, res, 1 if post else 0, groups, alpha, 0.0, f.data_ptr(), None,
+                      _param("w_post", w_post, one, (D,)), _param("w_pre", w_pre, one, (D,)), g, y_ptr, None,
+                      _param("rstd", rstd, f32, (rows, 2)), _pitch("f", f, rows, D), 0, ld_y, 0, dy_ptr, dh_ptr, df_ptr,
+                      dx_ptr, _param("dw_post", dw_post, f32, (D,)), _param("dw_pre", dw_pre, f32, (D,)),
+                      _param("dgate", dgate, f32, (groups, D)), ld_dy, ld_dh, ld_df, ld_dx, ws, ws_bytes)
+    st = lib().occ_norm_gate_bwd(ctypes.byref(n), _raw_stream(stream))
+    if st:
+        raise OccError(st, "occ_norm_gate_bwd")
     return df, dx
+
+
+def _workspace_arg(workspace):
+    """(address, bytes), (None, 0) for None."""
+    if workspace is None:
+        return None, 0
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous GPU tensor")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def occ_moe_workspace_bytes(tokens, H, I, experts, top_k):
     """Device bytes occ_moe needs (zeroed once)."""
     return int(lib().occ_moe_workspace_bytes(int(tokens), int(H), int(I), int(experts), int(top_k)))
+
+
+def _expert_weights(name, w, mx, experts, rows, cols):
+    """(weights, scales, elements from expert to expert) of a batch of matrices."""
+    if mx:
+        if not isinstance(w, Mx4) or w.rows != rows or w.cols != cols or w.codes.dim() != 3 or len(w.codes) != experts \
+                or not w.codes.is_cuda:
+            raise ValueError("w_%s must be an Mx4 batch of %d matrices %d x %d" % (name, experts, rows, cols))
+        return w.codes.data_ptr(), w.scales.data_ptr(), 0
+    if not isinstance(w, torch.Tensor) or w.dtype != torch.bfloat16 or not w.is_cuda or w.shape != (experts, rows, cols):
+        raise ValueError("w_%s must be a bfloat16 GPU tensor (%d, %d, %d)" % (name, experts, rows, cols))
+    if w.is_contiguous():
+        return w.data_ptr(), None, 0
+    if w.stride(2) != 1 or w.stride(1) != cols:
+        raise ValueError("w_%s must be of contiguous matrices" % name)
+    return w.data_ptr(), None, w.stride(0) if experts > 1 else 0
 
 
 def occ_moe(x, router, w_gate, w_up, w_down, y, *, top_k, workspace, ids=None, weights=None, renorm=True, mask=None,
@@ -710,46 +768,26 @@ def occ_moe(x, router, w_gate, w_up, w_down, y, *, top_k, workspace, ids=None, w
     tensors (experts, I, H), (experts, I, H), (experts, H, I) or Mx4 batches of the same.
     ids / weights (tokens, top_k; int32 / float32) receive the routing; mask: a bool or uint8
     per token.  workspace: a GPU tensor zeroed once.  Returns y."""
-    a = occ_moe_args()
-    if x.dtype != torch.bfloat16 or y.dtype != torch.bfloat16:
-        raise ValueError("x and y must be bfloat16 GPU tensors")
-    _, a.ld_x = _rows("x", x)
-    a.tokens, a.H = x.shape
-    _, a.ld_y = _rows("y", y, x.shape)
-    if router.dtype != torch.bfloat16 or not router.is_cuda or router.dim() != 2 or router.shape[1] != a.H \
-            or not router.is_contiguous():
-        raise ValueError("router must be a contiguous (experts, H) bfloat16 GPU tensor")
-    a.experts, a.top_k, a.renorm = router.shape[0], int(top_k), int(bool(renorm))
+    bf16 = torch.bfloat16
+    tokens, H = _sizes("x", x)
+    x_ptr, ld_x = _row_arg("x", x, bf16, tokens, H)
+    y_ptr, ld_y = _row_arg("y", y, bf16, tokens, H)
+    experts = _sizes("router", router)[0]
+    r_ptr = _param("router", router, bf16, (experts, H))
     mx = isinstance(w_gate, Mx4)
-    a.weight_type = OCC_MX4 if mx else OCC_BF16
-    a.I = w_gate.rows if mx else w_gate.shape[1] if w_gate.dim() == 3 else -1
-    for name, w, rows, cols in (("gate", w_gate, a.I, a.H), ("up", w_up, a.I, a.H), ("down", w_down, a.H, a.I)):
-        if mx:
-            if not isinstance(w, Mx4) or (w.rows, w.cols) != (rows, cols) or tuple(w.codes.shape[:-2]) != (a.experts,) \
-                    or not w.codes.is_cuda:
-                raise ValueError("w_%s must be an Mx4 batch of %d matrices %d x %d" % (name, a.experts, rows, cols))
-            setattr(a, "w_" + name, _ptr(w.codes).value)
-            setattr(a, "s_" + name, _ptr(w.scales).value)
-        else:
-            if not isinstance(w, torch.Tensor) or w.dtype != torch.bfloat16 or not w.is_cuda \
-                    or tuple(w.shape) != (a.experts, rows, cols) or w.stride(2) != 1 or w.stride(1) != cols:
-                raise ValueError("w_%s must be a bfloat16 GPU tensor (%d, %d, %d) of contiguous matrices"
-                                 % (name, a.experts, rows, cols))
-            setattr(a, "w_" + name, _ptr(w).value)
-            setattr(a, "stride_" + name, w.stride(0) if a.experts > 1 else 0)
-    for name, t, dtype in (("ids", ids, torch.int32), ("weights", weights, torch.float32)):
-        if t is not None:
-            if t.dtype != dtype or not t.is_cuda or tuple(t.shape) != (a.tokens, a.top_k) or not t.is_contiguous():
-                raise ValueError("%s must be a contiguous (tokens, top_k) %s GPU tensor" % (name, dtype))
-            setattr(a, name, _ptr(t).value)
-    if mask is not None:
-        if mask.dtype not in (torch.bool, torch.uint8) or not mask.is_cuda or tuple(mask.shape) != (a.tokens,) \
-                or not mask.is_contiguous():
-            raise ValueError("mask must be a contiguous bool or uint8 GPU tensor, one per token")
-        a.mask = _ptr(mask).value
-    if not workspace.is_cuda or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous GPU tensor")
-    a.x, a.router, a.y = _ptr(x).value, _ptr(router).value, _ptr(y).value
-    a.workspace, a.workspace_bytes = _ptr(workspace).value, workspace.numel() * workspace.element_size()
-    _check(lib().occ_moe(ctypes.byref(a), _stream(stream)), "occ_moe")
+    I = w_gate.rows if mx else w_gate.shape[1] if w_gate.dim() == 3 else -1
+    g, g_scales, g_stride = _expert_weights("gate", w_gate, mx, experts, I, H)
+    u, u_scales, u_stride = _expert_weights("up", w_up, mx, experts, I, H)
+    d, d_scales, d_stride = _expert_weights("down", w_down, mx, experts, H, I)
+    if mask is not None and mask.dtype != torch.bool and mask.dtype != torch.uint8:
+        raise ValueError("mask must be a bool or uint8 GPU tensor, one per token")
+    ws, ws_bytes = _workspace_arg(workspace)
+    a = occ_moe_args(tokens, H, I, experts, top_k, OCC_MX4 if mx else OCC_BF16, 1 if renorm else 0, x_ptr, r_ptr, g, u, d,
+                     g_scales, u_scales, d_scales, g_stride, u_stride, d_stride,
+                     None if mask is None else _param("mask", mask, mask.dtype, (tokens,)), y_ptr,
+                     _param("ids", ids, torch.int32, (tokens, top_k)),
+                     _param("weights", weights, torch.float32, (tokens, top_k)), ld_x, ld_y, ws, ws_bytes)
+    st = lib().occ_moe(ctypes.byref(a), _raw_stream(stream))
+    if st:
+        raise OccError(st, "occ_moe")
     return y
