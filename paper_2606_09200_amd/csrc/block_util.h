@@ -8,6 +8,9 @@ namespace {
 
 typedef uint32_t u32x4_e2 __attribute__((ext_vector_type(4), aligned(2)));  // 16 bytes at any element
 typedef uint32_t u32x4_e4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_e2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x2_e4 __attribute__((ext_vector_type(2), aligned(4)));
+typedef uint32_t u32_e2 __attribute__((aligned(2)));
 
 // By value: a bit cast of a vector's element itself would read its first.
 __device__ __forceinline__ float as_float(uint32_t w) { return __builtin_bit_cast(float, w); }
@@ -17,8 +20,6 @@ __device__ __forceinline__ float bf16_hi(uint32_t w) { return __builtin_bit_cast
 __device__ __forceinline__ float value(uint16_t h) { return as_float((uint32_t)h << 16); }
 __device__ __forceinline__ float value(float f) { return f; }
 
-// 8 consecutive values of a row as they are stored (bf16: 4 words, binary32: 8); the first
-// `left` of them exist, the others are zero.  Rows start at any element.
 // Element `at` of a row: a 32-bit byte offset from a uniform base costs one register, a pointer per
 // lane two.
 template <class E>
@@ -27,85 +28,150 @@ __device__ __forceinline__ E *element(E *row, uint32_t at) {
   return reinterpret_cast<E *>(reinterpret_cast<Byte *>(row) + at * (uint32_t)sizeof(E));
 }
 
+// 8 consecutive values of a row as they are stored (bf16: 4 words, binary32: 8), zeros where they do
+// not exist.  Rows start at any element.  load: all of them or none; load_part: the first
+// `left`, the end of a row of `cols` values: the lane there takes the row's last 8 and shifts
+// out those it does not own (one load and a few selects).
 template <class E>
 struct Raw8;
 template <>
 struct Raw8<uint16_t> {
   u32x4 w;
-  __device__ __forceinline__ void load(const uint16_t *p, int left) {
+  __device__ __forceinline__ void load(const uint16_t *p, bool in) {
     w = u32x4{0u, 0u, 0u, 0u};
-    if (left >= 8) {
-      w = *reinterpret_cast<const u32x4_e2 *>(p);
-    } else {
+    if (in) w = *reinterpret_cast<const u32x4_e2 *>(p);
+  }
+  __device__ __forceinline__ void load_rest(const uint16_t *p, int cols) {  // see store_rest
+    if (cols & 4) {
+      const u32x2_e2 v = *reinterpret_cast<const u32x2_e2 *>(p);
+      w[0] = v[0], w[1] = v[1];
+      p += 4;
+    }
+    if (cols & 2) {
+      w[2] = *reinterpret_cast<const u32_e2 *>(p);
+      p += 2;
+    }
+    if (cols & 1) w[3] = *p;
+  }
+  __device__ __forceinline__ void load_part(const uint16_t *p, int left, int cols) {
+    w = u32x4{0u, 0u, 0u, 0u};
+    if (cols >= 8) {
+      const int drop = 8 - (cols & 7);  // the same for every row
+      const bool part = left < 8;
+      if (left > 0) w = *reinterpret_cast<const u32x4_e2 *>(part ? p - drop : p);
+      const bool d4 = part && (drop & 4), d2 = part && (drop & 2), d1 = part && (drop & 1);
+      w[0] = d4 ? w[2] : w[0];
+      w[1] = d4 ? w[3] : w[1];
+      w[2] = d4 ? 0u : w[2];
+      w[3] = d4 ? 0u : w[3];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = d2 ? (i < 3 ? w[i + 1] : 0u) : w[i];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = d1 ? __builtin_amdgcn_alignbit(i < 3 ? w[i + 1] : 0u, w[i], 16) : w[i];
+    } else if (left > 0) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        uint32_t lo = 0u, hi = 0u;
-        if (2 * i < left) lo = p[2 * i];
-        if (2 * i + 1 < left) hi = p[2 * i + 1];
-        w[i] = lo | hi << 16;
+        const uint32_t lo = p[min(2 * i, left - 1)], hi = p[min(2 * i + 1, left - 1)];
+        w[i] = (2 * i < left ? lo : 0u) | (2 * i + 1 < left ? hi << 16 : 0u);
       }
     }
   }
   __device__ __forceinline__ float at(int e) const { return e & 1 ? bf16_hi(w[e >> 1]) : bf16_lo(w[e >> 1]); }
+  // What was computed from the words so far is computed again, not kept in registers.
+  __device__ __forceinline__ void forget() { asm volatile("" : "+v"(w)); }
 };
 template <>
 struct Raw8<float> {
   u32x4 a, b;
-  __device__ __forceinline__ void load(const float *p, int left) {
+  __device__ __forceinline__ void load(const float *p, bool in) {
     a = b = u32x4{0u, 0u, 0u, 0u};
-    if (left >= 8) {
+    if (in) {
       a = *reinterpret_cast<const u32x4_e4 *>(p);
       b = *reinterpret_cast<const u32x4_e4 *>(p + 4);
-    } else {
+    }
+  }
+  __device__ __forceinline__ void load_rest(const float *p, int cols) {
+    if (cols & 4) {
+      a = *reinterpret_cast<const u32x4_e4 *>(p);
+      p += 4;
+    }
+    if (cols & 2) {
+      const u32x2_e4 v = *reinterpret_cast<const u32x2_e4 *>(p);
+      b[0] = v[0], b[1] = v[1];
+      p += 2;
+    }
+    if (cols & 1) b[2] = *reinterpret_cast<const uint32_t *>(p);
+  }
+  __device__ __forceinline__ void load_part(const float *p, int left, int cols) {
+    a = b = u32x4{0u, 0u, 0u, 0u};
+    if (cols >= 8) {
+      const int drop = 8 - (cols & 7);
+      const bool part = left < 8;
+      if (left > 0) {
+        const float *q = part ? p - drop : p;
+        a = *reinterpret_cast<const u32x4_e4 *>(q);
+        b = *reinterpret_cast<const u32x4_e4 *>(q + 4);
+      }
+      const u32x4 none = {0u, 0u, 0u, 0u};
+      const bool d4 = part && (drop & 4), d2 = part && (drop & 2), d1 = part && (drop & 1);
+      a = d4 ? b : a;
+      b = d4 ? none : b;
+      a = d2 ? u32x4{a[2], a[3], b[0], b[1]} : a;
+      b = d2 ? u32x4{b[2], b[3], 0u, 0u} : b;
+      a = d1 ? u32x4{a[1], a[2], a[3], b[0]} : a;
+      b = d1 ? u32x4{b[1], b[2], b[3], 0u} : b;
+    } else if (left > 0) {
       const uint32_t *w = reinterpret_cast<const uint32_t *>(p);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (i < left) a[i] = w[i];
-        if (4 + i < left) b[i] = w[4 + i];
+        const uint32_t lo = w[min(i, left - 1)], hi = w[min(4 + i, left - 1)];
+        a[i] = i < left ? lo : 0u;
+        b[i] = 4 + i < left ? hi : 0u;
       }
     }
   }
   __device__ __forceinline__ float at(int e) const { return e < 4 ? as_float(a[e]) : as_float(b[e - 4]); }
+  __device__ __forceinline__ void forget() { asm volatile("" : "+v"(a), "+v"(b)); }
 };
 
-// The same as binary32 values.
-template <class E>
-__device__ __forceinline__ void load8(const E *p, int left, float (&v)[8]) {
-  Raw8<E> r;
-  r.load(p, left);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = r.at(e);
-}
-
-// 8 consecutive values of a row, rounded to the row's type; the first `left` of them exist.
+// 8 consecutive values of a row, rounded to the row's type, where they exist.
 // Non-temporal: outputs as large as these are not read again before they leave the L2.
-__device__ __forceinline__ void store8(uint16_t *p, int left, const float (&v)[8]) {
-  if (left >= 8) {
-    u32x4 w;
+__device__ __forceinline__ void store8(uint16_t *p, bool in, const float (&v)[8]) {
+  u32x4 w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-    __builtin_nontemporal_store(w, reinterpret_cast<u32x4_e2 *>(p));
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < left) p[i] = to_bf16(v[i]);
-  }
+  for (int i = 0; i < 4; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+  if (in) __builtin_nontemporal_store(w, reinterpret_cast<u32x4_e2 *>(p));
 }
-__device__ __forceinline__ void store8(float *p, int left, const float (&v)[8]) {
-  if (left >= 8) {
-    u32x4 a, b;
+__device__ __forceinline__ void store8(float *p, bool in, const float (&v)[8]) {
+  u32x4 a, b;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      a[i] = __builtin_bit_cast(uint32_t, v[i]);
-      b[i] = __builtin_bit_cast(uint32_t, v[4 + i]);
-    }
+  for (int i = 0; i < 4; ++i) {
+    a[i] = __builtin_bit_cast(uint32_t, v[i]);
+    b[i] = __builtin_bit_cast(uint32_t, v[4 + i]);
+  }
+  if (in) {
     __builtin_nontemporal_store(a, reinterpret_cast<u32x4_e4 *>(p));
     __builtin_nontemporal_store(b, reinterpret_cast<u32x4_e4 *>(p + 4));
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < left) p[i] = v[i];
   }
+}
+
+// The end of a row of `cols` values, cols % 8 of them, taken by fours, twos and ones: as far as there
+// are any, elements 0 to 3, then 4 and 5, then 6.
+template <class E>
+__device__ __forceinline__ void store_rest(E *p, int cols, const float (&v)[8]) {
+  auto put = [&](float x) {
+    if constexpr (sizeof(E) == 2) *p++ = to_bf16(x);
+    else *p++ = x;
+  };
+  if (cols & 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) put(v[i]);
+  }
+  if (cols & 2) {
+    put(v[4]);
+    put(v[5]);
+  }
+  if (cols & 1) put(v[6]);
 }
 
 template <int CTRL>

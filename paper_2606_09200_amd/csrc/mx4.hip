@@ -86,7 +86,7 @@ __global__ __launch_bounds__(256) void mx4_quant_rows_kernel(const E *__restrict
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int row = t * 16 + wave * 4 + i;
-      v[i].load(x + (size_t)min(row, rows - 1) * ld + min(c, cols), row < rows ? cols - c : 0);
+      v[i].load_part(x + (size_t)min(row, rows - 1) * ld + min(c, cols), row < rows ? cols - c : 0, cols);
     }
   };
   load(blockIdx.x);
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(256) void mx4_quant_both_kernel(const E *__restrict
 #pragma unroll
   for (int p = 0; p < 8; ++p) {
     const int row = r0 + p * 16 + (threadIdx.x >> 4);
-    v[p].load(x + (size_t)min(row, rows - 1) * ld + min(c, cols), row < rows ? cols - c : 0);
+    v[p].load_part(x + (size_t)min(row, rows - 1) * ld + min(c, cols), row < rows ? cols - c : 0, cols);
   }
 #pragma unroll
   for (int p = 0; p < 8; ++p) {
@@ -273,7 +273,13 @@ __global__ __launch_bounds__(256) void mx4_dequant_kernel(const uint8_t *__restr
         const auto v0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[i], sc, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[i], sc, 1);
         const auto v2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[i], sc, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[i], sc, 3);
         v[0] = v0[0], v[1] = v0[1], v[2] = v1[0], v[3] = v1[1], v[4] = v2[0], v[5] = v2[1], v[6] = v3[0], v[7] = v3[1];
-        store8(o, cols - c, v);
+        if (cols - c >= 8) {
+          store8(o, true, v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (e < cols - c) o[e] = v[e];
+        }
       }
     }
   }
