@@ -16,9 +16,10 @@
 // loads and stores of one lane and no selects.
 //
 // 8192 rows of 8192 bf16: forward 100 us (5.4 TB/s of what it must read and write), backward 164
-// us with its sums joined (4.9 TB/s); binary32: 215 and 341 us (5.0, 4.7).  12004 ragged rows of 5003
+// us with its sums joined (4.9 TB/s); binary32: 215 and 341 us (5.0, 4.6).  12004 ragged rows of 5003
 // with a binary32 residual: 169 and 260 us (4.3, 4.2).  16 rows of 8192: 6.4 us, of which a
-// launch is 2.3 and the rest the way through two sums.
+// launch is 2.3 and the rest the way through two sums.  Rows beyond 8192 columns go backward at
+// 4.0 (bf16) and 2.9 TB/s (binary32): one row a CU in flight, nothing fetched ahead.
 #include "block_util.h"
 
 #include <algorithm>
@@ -56,6 +57,12 @@ struct Chunks {
       in[c] = at[c] < whole;
       end[c] = REST && at[c] == whole;
     }
+  }
+  // Keeps the offsets from being folded into 64-bit addresses of each tensor's chunks, which would live
+  // across rows: the backward pass spilled them (4096 rows of 16384 binary32: 681 us, now 551).
+  __device__ __forceinline__ void fresh() {
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) asm volatile("" : "+v"(at[c]));
   }
   template <class E>
   __device__ __forceinline__ void load(Raw8<E> &v, const E *row, int c) const {
@@ -206,24 +213,18 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
     row_begin = gate_at * a.rows_per_gate + (int)(blockIdx.x % a.per_gate) * a.run;
     row_end = min((gate_at + 1) * a.rows_per_gate, row_begin + a.run);
   }
-  const Chunks<NCH, REST> cols(D);
+  Chunks<NCH, REST> cols(D);
   const ACT *w_post = static_cast<const ACT *>(a.w_post), *w_pre = static_cast<const ACT *>(a.w_pre);
   const ACT *gate = static_cast<const ACT *>(a.gate);
   Raw8<ACT> w1[NCH], w2[NCH], gv[NCH];
-  auto load_gate = [&]() {
-    if (gate != nullptr)
-#pragma unroll
-      for (int c = 0; c < NCH; ++c) cols.load(gv[c], gate + (size_t)gate_at * D, c);
+  auto load_gate = [&](int c) {
+    if (gate != nullptr) cols.load(gv[c], gate + (size_t)gate_at * D, c);
   };
-  auto load_post = [&]() {
-    if (w_post != nullptr)
-#pragma unroll
-      for (int c = 0; c < NCH; ++c) cols.load(w1[c], w_post, c);
+  auto load_post = [&](int c) {
+    if (w_post != nullptr) cols.load(w1[c], w_post, c);
   };
-  auto load_pre = [&]() {
-    if (w_pre != nullptr)
-#pragma unroll
-      for (int c = 0; c < NCH; ++c) cols.load(w2[c], w_pre, c);
+  auto load_pre = [&](int c) {
+    if (w_pre != nullptr) cols.load(w2[c], w_pre, c);
   };
   auto post = [&](int c, int e) { return w_post != nullptr ? w1[c].at(e) : 1.f; };
   auto gated = [&](int c, int e) { return gate != nullptr ? gv[c].at(e) : 1.f; };
@@ -235,9 +236,9 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
   ColumnSums<8 * NCH, WIDE> s2(lds + 8 * NCH * 1024);
   ColumnSums<8 * NCH, WIDE && DIRECT> dw1(lds);
   if (!WIDE) {
-    load_post();
-    load_pre();
-    if (!DIRECT) load_gate();
+    load_post(0);
+    load_pre(0);
+    if (!DIRECT) load_gate(0);
   }
   struct Rows {
     Raw8<ACT> f[NCH], dh[NCH];
@@ -262,6 +263,7 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
   int par = 0, in_gate = 0;
   for (int row = row_begin; row < row_end; ++row, par ^= 1) {
     Rows ahead;
+    cols.fresh();
     if (WIDE) fetch(q, row);
     else fetch(ahead, min(row + 1, row_end - 1));
     float d[NCH][8];
@@ -274,11 +276,11 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
       return w_pre != nullptr ? u * w2[c].at(e) : u;
     };
     if (a.dh != nullptr) {
-      if (WIDE) load_pre();
       float dot = 0.f;
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
         fence();
+        if (WIDE) load_pre(c);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float yn = q.y[c].at(e) * q.r2;
@@ -291,17 +293,20 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
       for (int c = 0; c < NCH; ++c) {
         q.y[c].forget();
         q.dh[c].forget();
+        if (WIDE) load_pre(c);
 #pragma unroll
         for (int e = 0; e < 8; ++e) d[c][e] = q.r2 * (pre(c, e) - dot * (q.y[c].at(e) * q.r2));
       }
     }
-    fence();
-    if (WIDE) load_post();
-    if (DIRECT ? WIDE || in_gate == 0 : WIDE) load_gate();
+    if (!WIDE && DIRECT && in_gate == 0) load_gate(0);
     float dot = 0.f;
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
       fence();
+      if (WIDE) {
+        load_gate(c);
+        load_post(c);
+      }
       if (a.dy != nullptr)
 #pragma unroll
         for (int e = 0; e < 8; ++e) d[c][e] = d[c][e] + q.dy[c].at(e);
@@ -334,6 +339,10 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
         float m[8];
+        if (WIDE) {
+          load_gate(c);
+          load_post(c);
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float s = s1.get(8 * c + e);
@@ -350,7 +359,6 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
   }
   const size_t mine = (size_t)blockIdx.x * D;
   const bool three = !DIRECT && a.part3 != nullptr;
-  if (WIDE && three) load_gate();
 #pragma unroll
   for (int c = 0; c < NCH; ++c) {
     float m[8], n[8];
@@ -361,6 +369,7 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
     }
     cols.store(a.part2 + mine, c, n);
     if (three) {
+      if (WIDE) load_gate(c);
       cols.store(a.part3 + mine, c, m);
 #pragma unroll
       for (int e = 0; e < 8; ++e) m[e] = m[e] * gated(c, e);
