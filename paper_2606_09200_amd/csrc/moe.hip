@@ -494,9 +494,10 @@ __global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(MoeCall c) {
 // experts' weighted sums to its own rows of y in LDS, one per token (a token that did not
 // pick an expert gets nothing from it, whatever its weights hold).  With several segments
 // the last one to finish a block of rows adds them in order: no sum depends on timing.
-// The weights' stream is kept up as above.
-template <bool MX, int TB>
-__global__ __launch_bounds__(kThreads, 4) void moe_down_kernel(MoeCall c) {
+// The weights' stream is kept up as above; a cursor runs AHEAD units in front of the
+// multiplications, across experts and tasks.  AHEAD is 2 where y leaves room for one workgroup a CU.
+template <bool MX, int TB, int AHEAD>
+__global__ __launch_bounds__(kThreads, AHEAD == 1 ? 4 : 2) void moe_down_kernel(MoeCall c) {
   typedef Rows16<MX> Rows;
   __shared__ u32x4 staged[kWaves][2 * Rows::LDS];        // a wave's units of the two row blocks
   extern __shared__ __align__(16) unsigned char smem[];  // y: [wave][token][32 rows]
@@ -509,7 +510,7 @@ __global__ __launch_bounds__(kThreads, 4) void moe_down_kernel(MoeCall c) {
   if ((int)blockIdx.x >= tasks) return;
   const auto rh = rsrc_of(c.hidden, (uint32_t)(c.T * c.k) * (uint32_t)c.I * 2u);
   const int units = (c.I + Rows::COLS - 1) / Rows::COLS;  // of one expert
-  Unit<MX> w0, w1;
+  Unit<MX> w0[AHEAD], w1[AHEAD];
   struct Part {  // of a task: its rows, its first expert, and this wave's units of all its experts, end to end
     int row0, a0, u0, u1;
   };
@@ -523,18 +524,33 @@ __global__ __launch_bounds__(kThreads, 4) void moe_down_kernel(MoeCall c) {
     p.u1 = (wave + 1) * all / kWaves;
     return p;
   };
-  auto load = [&](const Part &p, int u) {
-    const int e = (int)expert_at(c, p.a0 + u / units).id;
-    Rows(c.down, e, p.row0, c.H, c.I, lane).load(w0, u % units, lane);
-    Rows(c.down, e, min(p.row0 + 16, c.H), c.H, c.I, lane).load(w1, u % units, lane);
+  struct Cursor {  // the unit to load next: `left` units of the task, unit `k` of list entry `a`
+    int task, row0, left, a, k;
+  } cur;
+  auto enter = [&](int task) {  // the first task from this one on in which the wave has a unit
+    cur.left = 0;
+    for (; task < tasks && cur.left == 0; task += gridDim.x) {
+      const Part p = part_of(task);
+      cur.task = task, cur.row0 = p.row0, cur.left = p.u1 - p.u0;
+      cur.a = p.a0 + p.u0 / units, cur.k = p.u0 % units;
+    }
   };
-  Part p = part_of(blockIdx.x);
-  if (p.u0 < p.u1) load(p, p.u0);
+  auto load = [&](Unit<MX> &q0, Unit<MX> &q1) {
+    if (cur.left == 0) return;
+    const int e = (int)expert_at(c, cur.a).id;
+    Rows(c.down, e, cur.row0, c.H, c.I, lane).load(q0, cur.k, lane);
+    Rows(c.down, e, min(cur.row0 + 16, c.H), c.H, c.I, lane).load(q1, cur.k, lane);
+    if (++cur.k == units) cur.k = 0, ++cur.a;
+    if (--cur.left == 0) enter(cur.task + gridDim.x);
+  };
+  enter(blockIdx.x);
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) load(w0[i], w1[i]);
+  int slot = 0;
   float *y = reinterpret_cast<float *>(smem), *mine = y + wave * c.T * 32;
 #pragma unroll 1
   for (int task = blockIdx.x; task < tasks; task += gridDim.x) {
-    Part q{0, 0, 0, 0};
-    if (task + (int)gridDim.x < tasks) q = part_of(task + gridDim.x);
+    const Part p = part_of(task);
     for (int i = lane; i < c.T * 8; i += 64) reinterpret_cast<f32x4 *>(mine)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
     for (int u = p.u0; u < p.u1;) {
@@ -555,13 +571,18 @@ __global__ __launch_bounds__(kThreads, 4) void moe_down_kernel(MoeCall c) {
       for (; u < end; ++u) {
         u32x4 x[Rows::STEPS][4];
         factor<MX>(x, rh, from_of(0), u % units, c.I, g);
-        const uint32_t s0 = w0.scale, s1 = w1.scale;
-        stage<MX>(lds, w0, lane);
-        stage<MX>(lds + Rows::LDS, w1, lane);
-        __builtin_amdgcn_sched_barrier(0);
-        if (u + 1 < p.u1) load(p, u + 1);
-        else if (q.u0 < q.u1) load(q, q.u0);
-        __builtin_amdgcn_sched_barrier(0);
+        uint32_t s0, s1;
+        auto turn = [&](Unit<MX> &q0, Unit<MX> &q1) {
+          s0 = q0.scale, s1 = q1.scale;
+          stage<MX>(lds, q0, lane);
+          stage<MX>(lds + Rows::LDS, q1, lane);
+          __builtin_amdgcn_sched_barrier(0);
+          load(q0, q1);
+          __builtin_amdgcn_sched_barrier(0);
+        };
+        if (AHEAD == 1 || slot == 0) turn(w0[0], w1[0]);
+        else turn(w0[AHEAD - 1], w1[AHEAD - 1]);
+        if (AHEAD > 1) slot ^= 1;
         multiply<MX>(a0[0], a1[0], lds, s0, s1, x, lane);
 #pragma unroll
         for (int at = 1; at < TB; ++at)
@@ -585,7 +606,6 @@ __global__ __launch_bounds__(kThreads, 4) void moe_down_kernel(MoeCall c) {
           to[4] = v1;
         }
     }
-    if (p.u0 == p.u1 && q.u0 < q.u1) load(q, q.u0);
     __syncthreads();
     const int rb = task / segments, seg = task % segments;
     const int tok = threadIdx.x >> 3, row = p.row0 + (threadIdx.x & 7) * 4;  // H is a multiple of 8
@@ -623,7 +643,6 @@ __global__ __launch_bounds__(kThreads, 4) void moe_down_kernel(MoeCall c) {
       *reinterpret_cast<u32x2_e2 *>(c.y + (size_t)tok * c.ld_y + row) = o;
     }
     __syncthreads();  // before y is cleared for the next task
-    p = q;
   }
 }
 
@@ -663,9 +682,9 @@ template <bool MX>
 MoeFn up_fn(int tb) {
   return tb == 1 ? moe_up_kernel<MX, 1> : moe_up_kernel<MX, 2>;
 }
-template <bool MX>
-MoeFn down_fn(int tb) {
-  return tb == 1 ? moe_down_kernel<MX, 1> : moe_down_kernel<MX, 2>;
+MoeFn down_fn(bool mx, int tb, int per_cu) {
+  if (mx) return tb == 1 ? moe_down_kernel<true, 1, 1> : per_cu > 1 ? moe_down_kernel<true, 2, 1> : moe_down_kernel<true, 2, 2>;
+  return tb == 1 ? moe_down_kernel<false, 1, 1> : moe_down_kernel<false, 2, 2>;
 }
 
 }  // namespace
@@ -713,8 +732,9 @@ int moe_launch(const occ_moe_args &a, hipStream_t s) {
   hipLaunchKernelGGL(mx ? up_fn<true>(tb) : up_fn<false>(tb), dim3(grid), dim3(kThreads), 0, s, c);
   if (hipGetLastError() != hipSuccess) return OCC_EHIP;
   // y of every wave in LDS beside what its units pass through: one workgroup a CU for many tokens
-  const int y_bytes = kWaves * a.tokens * 128, per_cu = (mx ? 32768 : 65536) + y_bytes > di->lds_per_cu / 2 ? 1 : 2;
-  hipLaunchKernelGGL(mx ? down_fn<true>(tb) : down_fn<false>(tb), dim3(di->num_cus * per_cu), dim3(kThreads), y_bytes, s, c);
+  const int y_bytes = kWaves * a.tokens * 128;
+  const int per_cu = (mx ? 32768 : 65536) + y_bytes > di->lds_per_cu / 2 || (!mx && tb > 1) ? 1 : 2;
+  hipLaunchKernelGGL(down_fn(mx, tb, per_cu), dim3(di->num_cus * per_cu), dim3(kThreads), y_bytes, s, c);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
 }
 
