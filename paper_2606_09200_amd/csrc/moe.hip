@@ -397,8 +397,8 @@ __device__ __forceinline__ void multiply(f32x4 &acc0, f32x4 &acc1, const u32x4 *
 // unit's weights in flight while it multiplies (loads return in order: the other
 // factor's are asked for before them), also across the end of a task, and two
 // workgroups share a CU.
-template <bool MX, int TB>
-__global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(MoeCall c) {
+template <bool MX, int TB, int AHEAD>
+__global__ __launch_bounds__(kThreads, !MX && AHEAD > 1 ? 2 : 4) void moe_up_kernel(MoeCall c) {
   typedef Rows16<MX> Rows;
   // a wave's units of Wg and Wu; its sums at the end of a task
   constexpr int AREA = 2 * Rows::LDS > 128 * TB ? 2 * Rows::LDS : 128 * TB;
@@ -417,22 +417,36 @@ __global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(MoeCall c) {
   const int units = (c.H + Rows::COLS - 1) / Rows::COLS;
   const int u0 = kw, u1 = units;  // every kws-th, so that the waves together read whole rows
   auto row_of = [&](uint32_t task) { return min(((int)(task % groups) * c.rbs + rsub) * 16, c.I); };  // I: no rows
-  Unit<MX> wg, wu;
-  auto load = [&](const MoeExpert &e, int row0, int u) {
-    Rows(c.gate, (int)e.id, row0, c.I, c.H, lane).load(wg, u, lane);
-    Rows(c.up, (int)e.id, row0, c.I, c.H, lane).load(wu, u, lane);
+  Unit<MX> wg[AHEAD], wu[AHEAD];
+  struct Cursor {  // the unit to load next
+    uint32_t task;
+    int expert, row0, u;
+  } cur{blockIdx.x, (int)ex.id, row_of(blockIdx.x), u0};
+  auto load = [&](Unit<MX> &qg, Unit<MX> &qu) {
+    if (cur.task >= tasks || u0 >= u1) return;
+    Rows(c.gate, cur.expert, cur.row0, c.I, c.H, lane).load(qg, cur.u, lane);
+    Rows(c.up, cur.expert, cur.row0, c.I, c.H, lane).load(qu, cur.u, lane);
+    cur.u += kws;
+    if (cur.u >= u1) {
+      cur.task += gridDim.x;
+      if (cur.task < tasks) cur.expert = (int)expert_at(c, cur.task / groups).id;
+      cur.row0 = row_of(cur.task);
+      cur.u = u0;
+    }
   };
   auto from_of = [&](const MoeExpert &e, int at) {  // where the lane's token of the at-th 16 lies
     return at * 16 + l16 < (int)e.n
                ? (uint32_t)c.rows[e.first + at * 16 + l16].token * (uint32_t)c.ld_x * 2u + lane_bytes<MX>(g) : kNowhere;
   };
-  if (u0 < u1) load(ex, row_of(blockIdx.x), u0);
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) load(wg[i], wu[i]);
+  int slot = 0;
   uint32_t xo = from_of(ex, 0);
 #pragma unroll 1
   for (uint32_t task = blockIdx.x; task < tasks; task += gridDim.x) {
     const uint32_t nxt = task + gridDim.x;
     const MoeExpert en = nxt < tasks ? expert_at(c, nxt / groups) : ex;
-    const int n = (int)ex.n, nb = (n + 15) / 16, row0 = row_of(task);
+    const int n = (int)ex.n, nb = (n + 15) / 16;
     const uint32_t xn = from_of(en, 0);
     f32x4 ag[TB], au[TB];
 #pragma unroll
@@ -442,13 +456,18 @@ __global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(MoeCall c) {
       u32x4 x[Rows::STEPS][4];
       factor<MX>(x, rx, xo, u, c.H, g);
       // this unit's weights leave the registers, the next one's are on their way into them
-      const uint32_t sg = wg.scale, su = wu.scale;
-      stage<MX>(lds, wg, lane);
-      stage<MX>(lds + Rows::LDS, wu, lane);
-      __builtin_amdgcn_sched_barrier(0);
-      if (u + kws < u1) load(ex, row0, u + kws);
-      else if (nxt < tasks) load(en, row_of(nxt), u0);
-      __builtin_amdgcn_sched_barrier(0);
+      uint32_t sg, su;
+      auto turn = [&](Unit<MX> &qg, Unit<MX> &qu) {
+        sg = qg.scale, su = qu.scale;
+        stage<MX>(lds, qg, lane);
+        stage<MX>(lds + Rows::LDS, qu, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        load(qg, qu);
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      if (AHEAD == 1 || slot == 0) turn(wg[0], wu[0]);
+      else turn(wg[AHEAD - 1], wu[AHEAD - 1]);
+      if (AHEAD > 1) slot ^= 1;
       multiply<MX>(ag[0], au[0], lds, sg, su, x, lane);
 #pragma unroll
       for (int at = 1; at < TB; ++at)
@@ -678,9 +697,9 @@ template <int PER>
 MoeFn route_fn(int tb) {
   return tb == 1 ? moe_route_kernel<1, PER> : tb == 2 ? moe_route_kernel<2, PER> : moe_route_kernel<4, PER>;
 }
-template <bool MX>
-MoeFn up_fn(int tb) {
-  return tb == 1 ? moe_up_kernel<MX, 1> : moe_up_kernel<MX, 2>;
+MoeFn up_fn(bool mx, int tb) {
+  if (mx) return tb == 1 ? moe_up_kernel<true, 1, 2> : moe_up_kernel<true, 2, 1>;
+  return tb == 1 ? moe_up_kernel<false, 1, 1> : moe_up_kernel<false, 2, 2>;
 }
 MoeFn down_fn(bool mx, int tb, int per_cu) {
   if (mx) return tb == 1 ? moe_down_kernel<true, 1, 1> : per_cu > 1 ? moe_down_kernel<true, 2, 1> : moe_down_kernel<true, 2, 2>;
@@ -728,8 +747,8 @@ int moe_launch(const occ_moe_args &a, hipStream_t s) {
   // the waves of a task of the first product split H in units; where it has fewer, more rows
   const int units = mx ? (a.H + 255) / 256 : (a.H + 127) / 128;
   c.rbs = units >= 8 ? 1 : units >= 4 ? 2 : units >= 2 ? 4 : 8;
-  const unsigned grid = (unsigned)di->num_cus * 2;
-  hipLaunchKernelGGL(mx ? up_fn<true>(tb) : up_fn<false>(tb), dim3(grid), dim3(kThreads), 0, s, c);
+  const unsigned grid = (unsigned)di->num_cus * (!mx && tb > 1 ? 1 : 2);
+  hipLaunchKernelGGL(up_fn(mx, tb), dim3(grid), dim3(kThreads), 0, s, c);
   if (hipGetLastError() != hipSuccess) return OCC_EHIP;
   // y of every wave in LDS beside what its units pass through: one workgroup a CU for many tokens
   const int y_bytes = kWaves * a.tokens * 128;
