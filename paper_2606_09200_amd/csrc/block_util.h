@@ -135,13 +135,19 @@ struct Raw8<float> {
 };
 
 // 8 consecutive values of a row, rounded to the row's type, where they exist.
-// Non-temporal: outputs as large as these are not read again before they leave the L2.
+// NT: non-temporal.
+template <bool NT = true>
 __device__ __forceinline__ void store8(uint16_t *p, bool in, const float (&v)[8]) {
   u32x4 w;
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-  if (in) __builtin_nontemporal_store(w, reinterpret_cast<u32x4_e2 *>(p));
+  if (NT) {
+    if (in) __builtin_nontemporal_store(w, reinterpret_cast<u32x4_e2 *>(p));
+  } else {
+    if (in) *reinterpret_cast<u32x4_e2 *>(p) = w;
+  }
 }
+template <bool NT = true>
 __device__ __forceinline__ void store8(float *p, bool in, const float (&v)[8]) {
   u32x4 a, b;
 #pragma unroll
@@ -150,8 +156,13 @@ __device__ __forceinline__ void store8(float *p, bool in, const float (&v)[8]) {
     b[i] = __builtin_bit_cast(uint32_t, v[4 + i]);
   }
   if (in) {
-    __builtin_nontemporal_store(a, reinterpret_cast<u32x4_e4 *>(p));
-    __builtin_nontemporal_store(b, reinterpret_cast<u32x4_e4 *>(p + 4));
+    if (NT) {
+      __builtin_nontemporal_store(a, reinterpret_cast<u32x4_e4 *>(p));
+      __builtin_nontemporal_store(b, reinterpret_cast<u32x4_e4 *>(p + 4));
+    } else {
+      *reinterpret_cast<u32x4_e4 *>(p) = a;
+      *reinterpret_cast<u32x4_e4 *>(p + 4) = b;
+    }
   }
 }
 

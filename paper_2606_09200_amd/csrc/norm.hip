@@ -15,9 +15,9 @@
 // with its values by fours, twos and ones at fixed places (Chunks), which takes two more
 // loads and stores of one lane and no selects.
 //
-// 8192 rows of 8192 bf16: forward 100 us (5.4 TB/s of what it must read and write), backward 164
-// us with its sums joined (4.9 TB/s); binary32: 215 and 341 us (5.0, 4.6).  12004 ragged rows of 5003
-// with a binary32 residual: 169 and 260 us (4.3, 4.2).  16 rows of 8192: 6.4 us, of which a
+// 8192 rows of 8192 bf16: forward 100 us (5.4 TB/s of what it must read and write), backward 165
+// us with its sums joined (4.9 TB/s); binary32: 212 and 324 us (5.1, 5.0).  12004 ragged rows of 5003
+// with a binary32 residual: 169 and 247 us (4.3, 4.4).  16 rows of 8192: 6.4 us, of which a
 // launch is 2.3 and the rest the way through two sums.  Rows beyond 8192 columns go backward at
 // 4.0 (bf16) and 2.9 TB/s (binary32): one row a CU in flight, nothing fetched ahead.
 #include "block_util.h"
@@ -69,9 +69,11 @@ struct Chunks {
     v.load(element(row, at[c]), in[c]);
     if (REST && end[c]) v.load_rest(element(row, at[c]), D);
   }
-  template <class E>
+  // NT for the forward rows (8192 rows of 8191 bf16: 140 us, without 145); the backward pass's are
+  // stored plainly (8192 rows of 8192 binary32: 324 us, with 355).
+  template <bool NT, class E>
   __device__ __forceinline__ void store(E *row, int c, const float (&v)[8]) const {
-    store8(element(row, at[c]), in[c], v);
+    store8<NT>(element(row, at[c]), in[c], v);
     if (REST && end[c]) store_rest(element(row, at[c]), D, v);
   }
 };
@@ -133,7 +135,7 @@ __global__ __launch_bounds__(1024) void norm_gate_kernel(NormFwd a) {
         y[c][e] = __builtin_fmaf(a.alpha, xv[c].at(e), y[c][e]);
         ss = __builtin_fmaf(y[c][e], y[c][e], ss);
       }
-      cols.store(yo, c, y[c]);
+      cols.template store<true>(yo, c, y[c]);
     }
     float r2 = 1.f;
     if (a.h != nullptr) {
@@ -148,7 +150,7 @@ __global__ __launch_bounds__(1024) void norm_gate_kernel(NormFwd a) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) y[c][e] = y[c][e] * w.at(e);
         }
-        cols.store(ho, c, y[c]);
+        cols.template store<true>(ho, c, y[c]);
       }
     }
     if (a.rstd != nullptr && threadIdx.x == 0) {
@@ -314,7 +316,7 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
         float m[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) m[e] = a.alpha * d[c][e];
-        cols.store(static_cast<RES *>(a.dx) + (size_t)row * a.ld_dx, c, m);
+        cols.template store<false>(static_cast<RES *>(a.dx) + (size_t)row * a.ld_dx, c, m);
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -332,7 +334,7 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
         q.f[c].forget();
 #pragma unroll
         for (int e = 0; e < 8; ++e) m[e] = q.r1 * (d[c][e] - dot * (q.f[c].at(e) * q.r1));
-        cols.store(static_cast<ACT *>(a.df) + (size_t)row * a.ld_df, c, m);
+        cols.template store<false>(static_cast<ACT *>(a.df) + (size_t)row * a.ld_df, c, m);
       }
     }
     if (DIRECT && ++in_gate == a.rows_per_gate) {
@@ -350,7 +352,7 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
           dw1.set(8 * c + e, __builtin_fmaf(gated(c, e), s, dw1.get(8 * c + e)));
           s1.set(8 * c + e, 0.f);
         }
-        if (a.dgate != nullptr) cols.store(a.dgate + (size_t)gate_at * D, c, m);
+        if (a.dgate != nullptr) cols.template store<false>(a.dgate + (size_t)gate_at * D, c, m);
       }
       in_gate = 0;
       ++gate_at;
@@ -367,14 +369,14 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
       m[e] = DIRECT ? dw1.get(8 * c + e) : s1.get(8 * c + e);
       n[e] = s2.get(8 * c + e);
     }
-    cols.store(a.part2 + mine, c, n);
+    cols.template store<false>(a.part2 + mine, c, n);
     if (three) {
       if (WIDE) load_gate(c);
-      cols.store(a.part3 + mine, c, m);
+      cols.template store<false>(a.part3 + mine, c, m);
 #pragma unroll
       for (int e = 0; e < 8; ++e) m[e] = m[e] * gated(c, e);
     }
-    cols.store(a.part1 + mine, c, m);
+    cols.template store<false>(a.part1 + mine, c, m);
   }
 }
 
