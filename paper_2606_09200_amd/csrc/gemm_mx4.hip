@@ -16,35 +16,47 @@ namespace {
 
 typedef void (*Mx4Fn)(Mx4Operands, int, int);
 
-// A tile and its estimated time on a shape (as gemm.hip's): launch + rounds * (fixed + step per 512 of K).
+// A tile and its estimated time on a shape: rounds of up to per_cu workgroups a CU, each of them a
+// fixed part and a step per 512 of K, in us, where the CUs are lightly loaded and where they are full.
 struct Mx4Tile {
   int bm, bn, threads, lds;
   Mx4Fn bf16, f32;
   int per_cu;  // workgroups resident on a CU
-  double fixed, step;
+  double fixed, step, full_fixed, full_step;
+  // n tiles at once.  A full chip slows a tile of one workgroup a CU with what all CUs store and load
+  // together and with its clock, which a part of it does little; one of two a CU from
+  // where CUs have two.
+  double round_us(double n, double num_cus, double k) const {
+    const double x = per_cu == 2 ? std::max(0.0, n / num_cus - 1) : n / num_cus * (n / num_cus);
+    return (1 - x) * (fixed + step * k) + x * (full_fixed + full_step * k);
+  }
 };
 
 template <template <class> class T>
-constexpr Mx4Tile tile_of(Mx4Fn bf16, Mx4Fn f32, int per_cu, double fixed, double step) {
+constexpr Mx4Tile tile_of(Mx4Fn bf16, Mx4Fn f32, int per_cu, double fixed, double step, double full_fixed, double full_step) {
   typedef T<uint16_t> X;
-  return Mx4Tile{X::BM, X::BN, X::NT, X::LDS_BYTES, bf16, f32, per_cu, fixed, step};
+  return Mx4Tile{X::BM, X::BN, X::NT, X::LDS_BYTES, bf16, f32, per_cu, fixed, step, full_fixed, full_step};
 }
 
 template <class OUT>
-using Rp128x128 = Mx4Rp<128, 128, 2, 4, 2, 1, OUT>;
+using Rp128x128 = Mx4Rp<128, 128, 2, 2, 256, 2, 1, OUT>;
 template <class OUT>
-using Rp128x64 = Mx4Rp<128, 64, 4, 2, 3, 2, OUT>;
+using Rp128x64 = Mx4Rp<128, 64, 4, 2, 512, 3, 2, OUT>;
 template <class OUT>
-using Rp64x64 = Mx4Rp<64, 64, 2, 2, 4, 4, OUT>;
+using Rp64x64 = Mx4Rp<64, 64, 2, 2, 512, 4, 4, OUT>;
 template <class OUT>
-using Rp32x64 = Mx4Rp<32, 64, 2, 2, 4, 4, OUT>;
+using Rp32x64 = Mx4Rp<32, 64, 2, 2, 512, 4, 4, OUT>;
 
+// Fitted to 39 shapes from 17 x 512 x 512 to 16384 x 8192 x 512; the tile chosen is within 8 % of
+// the best one or half a microsecond.  128x128 at two workgroups a CU passes 256x256 where K is short
+// (16384 x 8192 x 512: 84 us, 92) or the larger tiles leave CUs idle (2500 x 2500 x 8192:
+// 31, 46; 3001 x 2504 x 5003: 25, 33), and is passed by it on the large ones (8192^3: 269, 234).
 const Mx4Tile kTiles[] = {
-    tile_of<Mx4Pp>(gemm_mx4_pp_kernel<Mx4Pp<uint16_t>>, gemm_mx4_pp_kernel<Mx4Pp<float>>, 1, 4.0, 2.2),
-    tile_of<Rp128x128>(gemm_mx4_rp_kernel<Rp128x128<uint16_t>>, gemm_mx4_rp_kernel<Rp128x128<float>>, 1, 2.0, 0.9),
-    tile_of<Rp128x64>(gemm_mx4_rp_kernel<Rp128x64<uint16_t>>, gemm_mx4_rp_kernel<Rp128x64<float>>, 1, 1.8, 0.6),
-    tile_of<Rp64x64>(gemm_mx4_rp_kernel<Rp64x64<uint16_t>>, gemm_mx4_rp_kernel<Rp64x64<float>>, 1, 1.6, 0.4),
-    tile_of<Rp32x64>(gemm_mx4_rp_kernel<Rp32x64<uint16_t>>, gemm_mx4_rp_kernel<Rp32x64<float>>, 1, 1.3, 0.33),
+    tile_of<Mx4Pp>(gemm_mx4_pp_kernel<Mx4Pp<uint16_t>>, gemm_mx4_pp_kernel<Mx4Pp<float>>, 1, 4.0, 2.2, 9.0, 2.75),
+    tile_of<Rp128x128>(gemm_mx4_rp_kernel<Rp128x128<uint16_t>>, gemm_mx4_rp_kernel<Rp128x128<float>>, 2, 1.5, 0.95, 3.1, 1.9),
+    tile_of<Rp128x64>(gemm_mx4_rp_kernel<Rp128x64<uint16_t>>, gemm_mx4_rp_kernel<Rp128x64<float>>, 1, 1.8, 0.6, 1.8, 0.6),
+    tile_of<Rp64x64>(gemm_mx4_rp_kernel<Rp64x64<uint16_t>>, gemm_mx4_rp_kernel<Rp64x64<float>>, 1, 1.6, 0.4, 1.6, 0.4),
+    tile_of<Rp32x64>(gemm_mx4_rp_kernel<Rp32x64<uint16_t>>, gemm_mx4_rp_kernel<Rp32x64<float>>, 1, 1.3, 0.33, 1.3, 0.33),
 };
 constexpr int kMaxDevices = 64;
 constexpr int kNumTiles = (int)(sizeof kTiles / sizeof kTiles[0]);
@@ -59,7 +71,8 @@ int choose_tile(const Mx4GemmCall &c, int num_cus, int room) {
     const Mx4Tile &t = kTiles[i];
     if (t.lds > room) continue;
     const double tiles = (double)ceil_div(c.M, t.bm) * ceil_div(c.N, t.bn);
-    const double us = std::ceil(tiles / num_cus) * (t.fixed + t.step * ceil_div(c.K, 512));
+    const double k = ceil_div(c.K, 512), slots = (double)t.per_cu * num_cus, rounds = std::floor(tiles / slots);
+    const double us = rounds * t.round_us(slots, num_cus, k) + (tiles > rounds * slots ? t.round_us(tiles - rounds * slots, num_cus, k) : 0);
     if (best < 0 || us < t_best) {
       best = i;
       t_best = us;

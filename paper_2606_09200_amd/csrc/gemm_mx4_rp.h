@@ -24,29 +24,41 @@ __device__ __forceinline__ void lds_dma4(i32x4 rsrc, uint32_t lds_addr, uint32_t
 // group's fragments are read and a later k-step's DMA is issued, and a k-step has
 // one barrier, before its last group.  Scale tiles are fetched 256 bytes per
 // DMA and read as one word per 16 rows and k-step, with the k-step's first group.
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int GS_, class OUT>
+// BK = 256 halves the k-steps: rows of 128 bytes, each scale tile fetched with both
+// steps that use it (four tiles per DMA), so that two workgroups share a CU.
+template <int BM_, int BN_, int WM_, int WN_, int BK_, int STAGES_, int GS_, class OUT>
 struct Mx4Rp {
   typedef OUT Out;
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, GS = GS_, BK = 512;
-  static constexpr int ROW = 256, KS = 4;           // bytes of a row, 128-wide substeps of a k-step
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, GS = GS_, BK = BK_;
+  static constexpr int ROW = BK / 2, KS = BK / 128;  // bytes of a row, 128-wide substeps of a k-step
+  static constexpr bool HALF = BK == 256;            // a k-step is half a scale tile
   static constexpr int WAVES = WM * WN, NT = 64 * WAVES;
   static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
-  static constexpr int RPP = NT / 16;               // rows per DMA pass
+  static constexpr int CHUNKS = ROW / 16, RPP = NT / CHUNKS;  // 16-byte chunks of a row, rows per DMA pass
   static constexpr int A_LOADS = BM / RPP, B_LOADS = BN / RPP;
   static constexpr int TILES = (BM + BN) / 16;      // scale tiles
-  static constexpr int S_LOADS = (TILES + WAVES - 1) / WAVES;
+  static constexpr int S_LOADS = HALF ? TILES / 4 / WAVES : (TILES + WAVES - 1) / WAVES;
   static constexpr int LOADS = A_LOADS + B_LOADS + S_LOADS;
   static constexpr int A_BYTES = BM * ROW, CODE_BYTES = A_BYTES + BN * ROW;
-  static constexpr int STAGE_BYTES = CODE_BYTES + S_LOADS * WAVES * 256;
+  static constexpr int STAGE_BYTES = CODE_BYTES + S_LOADS * WAVES * (HALF ? 1024 : 256);
   static constexpr int LDS_BYTES = STAGES * STAGE_BYTES;
   static constexpr int NG = KS / GS;                // fragment groups per k-step
   static_assert(KS % GS == 0 && (NG == 1 || NG % 2 == 0), "groups alternate between two register sets");
   static_assert(BM % RPP == 0 && BN % RPP == 0 && RPP % 16 == 0, "uneven load passes, or a swizzle that changes between them");
+  static_assert(BK == 512 || (HALF && BM % (64 * S_LOADS) == 0 && TILES == 4 * WAVES * S_LOADS && NG % 2 == 0),
+                "a wave's scale DMA is of one operand's tiles");
   static_assert((STAGES - 1) * LOADS <= 63, "vmcnt holds at most 63");
 };
 
+// Chunk c of row r of a staged operand lies at (and the chunk there is) this one of the row.
 template <class T>
-__global__ __launch_bounds__(T::NT) void gemm_mx4_rp_kernel(Mx4Operands o, int tiles_m, int tiles_n) {
+__device__ __forceinline__ int mx4_rp_chunk(int r, int c) {
+  if constexpr (T::HALF) return swz<8>(r, c);
+  else return c ^ (r & 15);
+}
+
+template <class T>
+__global__ __launch_bounds__(T::NT, 2) void gemm_mx4_rp_kernel(Mx4Operands o, int tiles_m, int tiles_n) {
   extern __shared__ __align__(16) unsigned char smem[];  // tile stages, then the unused pad
   constexpr int S = T::STAGES;
   const int M = o.M, N = o.N;
@@ -56,20 +68,20 @@ __global__ __launch_bounds__(T::NT) void gemm_mx4_rp_kernel(Mx4Operands o, int t
   const int wm = wave / T::WN, wn = wave % T::WN;
   const int l16 = lane & 15, g = lane >> 4;
   const int ntiles = tiles_m * tiles_n;
-  const int nk = o.steps512;
+  const int nk = T::HALF ? o.steps256 : o.steps512;
   const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char *)smem;
   const uint32_t wave_lds = (uint32_t)wave * 1024u;
 
-  // DMA slots: rows are one 256-byte bank line each, chunks spread by the row (the same in every pass)
-  const int r_in = threadIdx.x >> 4;
-  const uint32_t lane_off = (uint32_t)r_in * P + 16u * (uint32_t)((threadIdx.x & 15) ^ (r_in & 15));
+  // DMA slots: chunks spread by the row (the same in every pass)
+  const int r_in = threadIdx.x / T::CHUNKS;
+  const uint32_t lane_off = (uint32_t)r_in * P + 16u * (uint32_t)mx4_rp_chunk<T>(r_in, threadIdx.x % T::CHUNKS);
   const uint32_t pass_step = (uint32_t)T::RPP * P;
 
   int a_rd[T::KS], b_rd[T::KS];
 #pragma unroll
   for (int ks = 0; ks < T::KS; ++ks) {
-    a_rd[ks] = (wm * T::FM * 16 + l16) * T::ROW + ((ks * 4 + g) ^ l16) * 16;
-    b_rd[ks] = T::A_BYTES + (wn * T::FN * 16 + l16) * T::ROW + ((ks * 4 + g) ^ l16) * 16;
+    a_rd[ks] = (wm * T::FM * 16 + l16) * T::ROW + mx4_rp_chunk<T>(l16, ks * 4 + g) * 16;
+    b_rd[ks] = T::A_BYTES + (wn * T::FN * 16 + l16) * T::ROW + mx4_rp_chunk<T>(l16, ks * 4 + g) * 16;
   }
 
   for (int t = blockIdx.x; t < ntiles; t += gridDim.x) {
@@ -83,7 +95,7 @@ __global__ __launch_bounds__(T::NT) void gemm_mx4_rp_kernel(Mx4Operands o, int t
     const int at = min(T::BM / 16, (M - m0 + 15) >> 4), bt = min(T::BN / 16, (N - n0 + 15) >> 4);  // tiles that exist
     // DMA pass p of k-step kt (A's, B's, then scales) into stage `slot`
     auto issue_pass = [&](int kt, uint32_t slot, int p) {
-      const uint32_t k0 = (uint32_t)kt * 256u;
+      const uint32_t k0 = (uint32_t)kt * T::ROW;
       const bool in = kt < nk;
       if (p < T::A_LOADS) {
         const i32x4 rs = make_rsrc(Am + k0, in ? a_bytes - k0 : 0u);
@@ -92,6 +104,12 @@ __global__ __launch_bounds__(T::NT) void gemm_mx4_rp_kernel(Mx4Operands o, int t
         const int q = p - T::A_LOADS;
         const i32x4 rs = make_rsrc(Bn + k0, in ? b_bytes - k0 : 0u);
         lds_dma16(rs, slot + wave_lds + (uint32_t)(T::A_BYTES + q * T::NT * 16), lane_off + (uint32_t)q * pass_step);
+      } else if constexpr (T::HALF) {
+        const int x = ((p - T::A_LOADS - T::B_LOADS) * T::WAVES + wave) * 4;  // first of four scale tiles, A's then B's
+        const bool b = x >= T::BM / 16;
+        const uint32_t y = (uint32_t)(b ? x - T::BM / 16 : x), s0 = (uint32_t)(kt >> 1) * 256u;
+        const i32x4 rs = make_rsrc((b ? Sb : Sa) + s0, in ? (uint32_t)(b ? bt : at) * P - s0 : 0u);
+        lds_dma16(rs, slot + (uint32_t)(T::CODE_BYTES + x * 256), (y + g) * P + (uint32_t)l16 * 16u);
       } else {
         const int x = (p - T::A_LOADS - T::B_LOADS) * T::WAVES + wave;  // scale tile, A's then B's
         const bool b = x >= T::BM / 16;
@@ -125,9 +143,9 @@ __global__ __launch_bounds__(T::NT) void gemm_mx4_rp_kernel(Mx4Operands o, int t
       for (int j = 0; j < T::FN; ++j)
         bs_next[j] = *reinterpret_cast<const int *>(sc + (T::BM / 16 + wn * T::FN + j) * 256);
     };
-    auto mfma = [&](int gi, int set, int x) {
+    auto mfma = [&](int byte0, int gi, int set, int x) {
       const int s = x / (T::FM * T::FN), i = x / T::FN % T::FM, j = x % T::FN;
-      switch (gi * T::GS + s) {  // a constant once unrolled
+      switch (byte0 + gi * T::GS + s) {  // a constant once unrolled
         case 0: acc[i][j] = mfma_mx4<0>(bf[set][s][j], af[set][s][i], acc[i][j], bs[j], as[i]); break;
         case 1: acc[i][j] = mfma_mx4<1>(bf[set][s][j], af[set][s][i], acc[i][j], bs[j], as[i]); break;
         case 2: acc[i][j] = mfma_mx4<2>(bf[set][s][j], af[set][s][i], acc[i][j], bs[j], as[i]); break;
@@ -152,7 +170,7 @@ __global__ __launch_bounds__(T::NT) void gemm_mx4_rp_kernel(Mx4Operands o, int t
 #pragma unroll
     for (int x = 0; x < NR; ++x) read_frag(smem, 0, 0, x);
     int stage = 0;  // stage of the k-step being multiplied
-    auto step = [&](int kt, int set0) {
+    auto step = [&](int kt, int set0, int byte0) {
       const int next = stage + 1 == S ? 0 : stage + 1;
       const unsigned char *cur = smem + stage * T::STAGE_BYTES, *nxt = smem + next * T::STAGE_BYTES;
       const uint32_t slot = slot_of(stage);
@@ -171,7 +189,7 @@ __global__ __launch_bounds__(T::NT) void gemm_mx4_rp_kernel(Mx4Operands o, int t
         }
 #pragma unroll
         for (int x = 0; x < NM; ++x) {
-          mfma(gi, set, x);
+          mfma(byte0, gi, set, x);
           // the reads behind the first half of the MFMAs, the DMA behind all of them
 #pragma unroll
           for (int y = 0; y < NR; ++y)
@@ -184,15 +202,15 @@ __global__ __launch_bounds__(T::NT) void gemm_mx4_rp_kernel(Mx4Operands o, int t
       }
       stage = next;
     };
-    if constexpr (T::NG == 1) {
+    if constexpr (T::NG == 1 || T::HALF) {  // the register sets or the scales' bytes alternate
       int kt = 0;
       for (; kt + 1 < nk; kt += 2) {
-        step(kt, 0);
-        step(kt + 1, 1);
+        step(kt, 0, 0);
+        step(kt + 1, T::NG == 1, T::HALF ? 2 : 0);
       }
-      if (kt < nk) step(kt, 0);
+      if (kt < nk) step(kt, 0, 0);
     } else {
-      for (int kt = 0; kt < nk; ++kt) step(kt, 0);
+      for (int kt = 0; kt < nk; ++kt) step(kt, 0, 0);
     }
     wait_vmcnt<0>();  // the DMA issued past the last k-step, before the stages get other use
     publish();
