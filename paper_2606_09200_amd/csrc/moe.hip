@@ -14,6 +14,7 @@
 #include "mx4.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace occ {
 namespace {
@@ -530,8 +531,12 @@ __global__ __launch_bounds__(kThreads, AHEAD == 1 ? 4 : 2) void moe_down_kernel(
   const auto rh = rsrc_of(c.hidden, (uint32_t)(c.T * c.k) * (uint32_t)c.I * 2u);
   const int units = (c.I + Rows::COLS - 1) / Rows::COLS;  // of one expert
   Unit<MX> w0[AHEAD], w1[AHEAD];
-  struct Part {  // of a task: its rows, its first expert, and this wave's units of all its experts, end to end
-    int row0, a0, u0, u1;
+  // Of a task: its rows, its first expert, and this wave's units of all its experts, end to end, from
+  // `start` round.  Long tasks start at different columns: with all at the same ones, and rows a power of
+  // two apart, only some of the memory's channels answer (64 tokens, 32 experts of 4096 x 2048
+  // bf16 in tasks of 16 experts: 113 us, now 84).  It gains nothing with MX4's shorter rows.
+  struct Part {
+    int row0, a0, u0, u1, start;
   };
   auto part_of = [&](int task) {
     const int seg = task % segments;
@@ -541,17 +546,20 @@ __global__ __launch_bounds__(kThreads, AHEAD == 1 ? 4 : 2) void moe_down_kernel(
     const int all = ((seg + 1) * active / segments - p.a0) * units;
     p.u0 = wave * all / kWaves;
     p.u1 = (wave + 1) * all / kWaves;
+    p.start = !MX && p.u1 - p.u0 >= 8 ? p.u0 + task / segments % (p.u1 - p.u0) : p.u0;
     return p;
   };
   struct Cursor {  // the unit to load next: `left` units of the task, unit `k` of list entry `a`
-    int task, row0, left, a, k;
+    int task, row0, left, to_end, a, k, a0, k0;
   } cur;
   auto enter = [&](int task) {  // the first task from this one on in which the wave has a unit
     cur.left = 0;
     for (; task < tasks && cur.left == 0; task += gridDim.x) {
       const Part p = part_of(task);
       cur.task = task, cur.row0 = p.row0, cur.left = p.u1 - p.u0;
-      cur.a = p.a0 + p.u0 / units, cur.k = p.u0 % units;
+      cur.to_end = p.u1 - p.start;
+      cur.a = p.a0 + p.start / units, cur.k = p.start % units;
+      cur.a0 = p.a0 + p.u0 / units, cur.k0 = p.u0 % units;
     }
   };
   auto load = [&](Unit<MX> &q0, Unit<MX> &q1) {
@@ -560,6 +568,7 @@ __global__ __launch_bounds__(kThreads, AHEAD == 1 ? 4 : 2) void moe_down_kernel(
     Rows(c.down, e, cur.row0, c.H, c.I, lane).load(q0, cur.k, lane);
     Rows(c.down, e, min(cur.row0 + 16, c.H), c.H, c.I, lane).load(q1, cur.k, lane);
     if (++cur.k == units) cur.k = 0, ++cur.a;
+    if (--cur.to_end == 0) cur.a = cur.a0, cur.k = cur.k0;
     if (--cur.left == 0) enter(cur.task + gridDim.x);
   };
   enter(blockIdx.x);
@@ -572,10 +581,11 @@ __global__ __launch_bounds__(kThreads, AHEAD == 1 ? 4 : 2) void moe_down_kernel(
     const Part p = part_of(task);
     for (int i = lane; i < c.T * 8; i += 64) reinterpret_cast<f32x4 *>(mine)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-    for (int u = p.u0; u < p.u1;) {
+    for (int u = p.start, left = p.u1 - p.u0; left > 0;) {
       const MoeExpert ex = expert_at(c, p.a0 + u / units);
       const int n = (int)ex.n, nb = (n + 15) / 16;
-      const int end = min(p.u1, (u / units + 1) * units);
+      const int end = min(min(p.u1, (u / units + 1) * units), u + left);
+      left -= end - u;
       auto from_of = [&](int at) {
         return at * 16 + l16 < n ? (ex.first + at * 16 + l16) * (uint32_t)c.I * 2u + lane_bytes<MX>(g) : kNowhere;
       };
@@ -610,7 +620,8 @@ __global__ __launch_bounds__(kThreads, AHEAD == 1 ? 4 : 2) void moe_down_kernel(
             multiply<MX>(a0[at], a1[at], lds, s0, s1, x, lane);
           }
       }
-      // this wave's part of the expert is whole: into its tokens' rows
+      if (u == p.u1) u = p.u0;
+      // this part of the expert is whole: into its tokens' rows
 #pragma unroll
       for (int at = 0; at < TB; ++at)
         if (at * 16 + l16 < n) {
@@ -667,27 +678,48 @@ __global__ __launch_bounds__(kThreads, AHEAD == 1 ? 4 : 2) void moe_down_kernel(
 
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
+// Workgroups of the second product on a CU: y of every wave is in LDS beside what its units pass through.
+// More than 16 tokens with bf16 weights and more than 48 with MX4 leave room for one.
+int down_per_cu(int T, bool mx) { return T <= (mx ? 48 : 16) ? 2 : 1; }
+
+// Parts of the list of experts that the second product's tasks take: the split of the least estimated
+// time.  A task costs 2 us beside its units, 3 where parts have to be joined, and eight units (one a
+// wave) what 32 rows of 512 bytes a wave take at a CU's share of 6 TB/s; tasks run in rounds of
+// as many as the chip holds.  (Four tasks a workgroup whatever the sizes: 55 tokens of 8 experts, 6144 x
+// 1264 MX4, 35 us, now 16; 37 tokens of 60 experts, 2504 x 1400 bf16, 93 us, now 69.)
+int down_segments(int T, int H, int I, int E, int k, bool mx) {
+  constexpr double kCus = 256;
+  const double active = E * (1 - std::pow(1 - (double)k / E, T));  // expected
+  const int blocks = (H + 31) / 32, units = mx ? (I + 255) / 256 : (I + 127) / 128, per_cu = down_per_cu(T, mx);
+  const double unit_us = (mx ? 1.4 : 2.8) * per_cu;
+  int best = 1;
+  double t_best = 0;
+  for (int seg = 1; seg <= std::min(E, T * k); ++seg) {
+    const double n = std::min((double)seg, std::max(1.0, active));
+    const double us = std::ceil(blocks * n / (kCus * per_cu)) * ((seg > 1 ? 3 : 2) + unit_us * std::max(1.0, active * units / n / kWaves));
+    if (seg == 1 || us < t_best) best = seg, t_best = us;
+  }
+  return best;
+}
+
 // The workspace's parts; the counters come first.
 struct MoeLayout {
   size_t plan, rows, joined, part, hidden, sums, end;
-  int slices, segments, row_blocks;
+  int slices, row_blocks;
 };
 MoeLayout layout_of(int T, int H, int I, int E, int k) {
   MoeLayout l{};
   const int steps = kRouteWaves / (T <= 16 ? 1 : T <= 32 ? 2 : 4);  // of 128 columns, that a router workgroup takes at once
   l.slices = std::max(1, std::min(kSlices, (H + 128 * steps - 1) / (128 * steps)));
   l.row_blocks = (H + 31) / 32;
-  // parts of the second product's tasks: one task a workgroup with few experts, two with many, so
-  // that the last ones to end are short
-  const int want = T * k <= 16 ? 512 : 1024;
-  l.segments = std::max(1, std::min(std::min(E, T * k), (want + l.row_blocks - 1) / l.row_blocks));
+  const int segments = std::max(down_segments(T, H, I, E, k, false), down_segments(T, H, I, E, k, true));
   size_t at = up16(sizeof(MoeCounters));
   l.plan = at, at += up16((size_t)E * (T > 32 ? 2 : 1) * sizeof(MoeExpert));
   l.rows = at, at += up16((size_t)T * k * sizeof(MoeRow));
   l.joined = at, at += up16((size_t)l.row_blocks * 4);
   l.part = at, at += up16((size_t)l.slices * ((E + 15) / 16) * T * 64);
   l.hidden = at, at += up16((size_t)T * k * I * 2);
-  l.sums = at, at += up16(l.segments > 1 ? (size_t)l.segments * T * H * 4 : 0);
+  l.sums = at, at += up16(segments > 1 ? (size_t)segments * T * H * 4 : 0);
   l.end = at;
   return l;
 }
@@ -719,7 +751,7 @@ int moe_launch(const occ_moe_args &a, hipStream_t s) {
   unsigned char *ws = static_cast<unsigned char *>(a.workspace);
   MoeCall c{};
   c.T = a.tokens, c.H = a.H, c.I = a.I, c.E = a.experts, c.k = a.top_k, c.renorm = a.renorm != 0;
-  c.slices = l.slices, c.row_blocks = l.row_blocks, c.max_segments = l.segments;
+  c.slices = l.slices, c.row_blocks = l.row_blocks, c.max_segments = down_segments(a.tokens, a.H, a.I, a.experts, a.top_k, a.weight_type == OCC_MX4);
   c.x = static_cast<const uint16_t *>(a.x), c.ld_x = (int)a.ld_x;
   c.router = static_cast<const uint16_t *>(a.router);
   const bool mx = a.weight_type == OCC_MX4;
@@ -750,9 +782,7 @@ int moe_launch(const occ_moe_args &a, hipStream_t s) {
   const unsigned grid = (unsigned)di->num_cus * (!mx && tb > 1 ? 1 : 2);
   hipLaunchKernelGGL(up_fn(mx, tb), dim3(grid), dim3(kThreads), 0, s, c);
   if (hipGetLastError() != hipSuccess) return OCC_EHIP;
-  // y of every wave in LDS beside what its units pass through: one workgroup a CU for many tokens
-  const int y_bytes = kWaves * a.tokens * 128;
-  const int per_cu = (mx ? 32768 : 65536) + y_bytes > di->lds_per_cu / 2 || (!mx && tb > 1) ? 1 : 2;
+  const int y_bytes = kWaves * a.tokens * 128, per_cu = down_per_cu(a.tokens, mx);
   hipLaunchKernelGGL(down_fn(mx, tb, per_cu), dim3(di->num_cus * per_cu), dim3(kThreads), y_bytes, s, c);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
 }
