@@ -36,10 +36,6 @@ template <class V>
 __device__ __forceinline__ void put_device(V *p, V v) {  // through the XCD's L2, for readers on other XCDs
   __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-template <class V>
-__device__ __forceinline__ V get_device(const V *p) {
-  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
 __device__ __forceinline__ uint32_t add_device(uint32_t *p) {
   return __hip_atomic_fetch_add(p, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -55,27 +51,25 @@ __device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// Largest / smallest of 32-bit words over a wave, in every lane.
-template <bool MAX>
-__device__ __forceinline__ uint32_t wave_pick(uint32_t v) {
-  auto pick = [](uint32_t a, uint32_t b) { return MAX ? max(a, b) : min(a, b); };
-  v = pick(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true));
-  v = pick(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true));
-  v = pick(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true));
-  v = pick(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xF, 0xF, true));
+// Largest of 32-bit words over a wave, in every lane.
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xF, 0xF, true));
   const auto s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  v = pick(s[0], s[1]);
+  v = max(s[0], s[1]);
   const auto t = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return pick(t[0], t[1]);
+  return max(t[0], t[1]);
 }
 
 // ---------------------------------------------------------------------------
 // Router.  A workgroup multiplies 16 experts' rows with all tokens over one of `slices`
 // slices of H, a wave 16 tokens and 128 columns at a time; the partial logits go to
 // part[16 experts, slice][token][expert].  The workgroup that arrives last adds the slices in
-// order and picks: a wave per token at a time, lane l holding experts l, l + 64, ...
-// (PER of them), the next token's logits on their way: they come from other XCDs'
-// writes through memory.  Logits order as integers, a NaN below everything (its
+// order, all tokens at once (they come from other XCDs' writes through memory), and picks:
+// a wave per token at a time, lane l holding experts l, l + 64, ... (PER of them).
+// Logits order as integers, a NaN below everything (its
 // token's weights become NaN with the sum); equal ones go to the lower index.
 //
 // What bounds it is latency: two trips to memory and one workgroup's tail.  Most of
@@ -138,18 +132,27 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(MoeCall c) {
   for (int i = threadIdx.x; i < c.row_blocks; i += kRouteThreads) c.joined[i] = 0;
   for (int i = threadIdx.x; i < c.E; i += kRouteThreads) picked[i][0] = picked[i][1] = 0u;
   __syncthreads();
-  float ahead[PER][kSlices];  // the next token's logits, slice by slice
-  auto fetch = [&](int t) {
-#pragma unroll
-    for (int j = 0; j < PER; ++j)
+  extern __shared__ __align__(16) unsigned char smem[];
+  float *logits = reinterpret_cast<float *>(smem);  // [token][pitch]
+  const int pitch = (c.E + 15) / 16 * 16;
+  {
+    const auto rp = rsrc_of(c.part, (uint32_t)(pitch * c.slices * c.T) * 4u);
+    const int per_block = c.T * 4;  // 16-byte pieces of 16 experts' logits
+    for (int i = threadIdx.x; i < pitch * c.T / 4; i += kRouteThreads) {
+      const int b = i / per_block, in = i % per_block;
+      f32x4 part[kSlices];
 #pragma unroll
       for (int s = 0; s < kSlices; ++s)
-        if (s < c.slices && j * 64 < c.E) {
-          const int e = min(j * 64 + lane, c.E - 1);
-          ahead[j][s] = get_device(c.part + ((size_t)((e >> 4) * c.slices + s) * c.T + t) * 16 + (e & 15));
-        }
-  };
-  if (wave < c.T) fetch(wave);
+        if (s < c.slices)
+          part[s] = __builtin_bit_cast(f32x4, load16<16>(rp, (uint32_t)((b * c.slices + s) * per_block + in) * 16u));
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < kSlices; ++s)
+        if (s < c.slices) v = v + part[s];
+      *reinterpret_cast<f32x4 *>(logits + (in >> 2) * pitch + b * 16 + (in & 3) * 4) = v;
+    }
+  }
+  __syncthreads();
 #pragma unroll 1
   for (int t = wave; t < c.T; t += kRouteWaves) {
     const bool live = c.mask == nullptr || c.mask[t] != 0;
@@ -157,33 +160,35 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(MoeCall c) {
     uint32_t key[PER];
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      l[j] = 0.f;
-#pragma unroll
-      for (int s = 0; s < kSlices; ++s)
-        if (s < c.slices) l[j] = l[j] + ahead[j][s];
+      l[j] = j * 64 + lane < c.E ? logits[t * pitch + j * 64 + lane] : 0.f;
       // ascending integers, 1 and above; what is taken or missing is 0
       const uint32_t u = __builtin_bit_cast(uint32_t, l[j]);
       key[j] = j * 64 + lane >= c.E ? 0u : l[j] != l[j] ? 1u : (u >> 31 ? ~u : u | 0x80000000u);
     }
-    if (t + kRouteWaves < c.T) fetch(t + kRouteWaves);
     float top = 0.f, mine = 0.f;  // mine: lane j < k holds pick j's logit, then its weight
     int my_id = 0;
 #pragma unroll 1
     for (int j = 0; j < c.k; ++j) {
-      uint32_t best = 0u;
-      int at = 0;
+      uint32_t best = key[0];
 #pragma unroll
-      for (int i = PER - 1; i >= 0; --i)
-        if (key[i] >= best) best = key[i], at = i;  // the lowest index among this lane's equals
-      const uint32_t win = wave_pick<true>(best);
-      const uint32_t e = wave_pick<false>(best == win ? (uint32_t)(at * 64 + lane) : 0xFFFFFFFFu);
+      for (int i = 1; i < PER; ++i) best = max(best, key[i]);
+      const uint32_t win = wave_max(best);
+      int e = 0;  // the lowest index among equals
       float v = 0.f;
 #pragma unroll
+      for (int i = PER - 1; i >= 0; --i) {
+        const uint64_t has = __ballot(key[i] == win);
+        if (has != 0) {
+          const int at = __builtin_ctzll(has);
+          e = i * 64 + at;
+          v = as_float((uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, l[i]), at));
+        }
+      }
+#pragma unroll
       for (int i = 0; i < PER; ++i)
-        if ((uint32_t)(i * 64 + lane) == e) v = l[i], key[i] = 0u;
-      v = as_float((uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, v), (int)(e & 63u)));
+        if (i * 64 + lane == e) key[i] = 0u;
       if (j == 0) top = v;
-      if (lane == j) mine = v, my_id = (int)e;
+      if (lane == j) mine = v, my_id = e;
     }
     float sum = 0.f;
 #pragma unroll
@@ -397,7 +402,9 @@ __device__ __forceinline__ void multiply(f32x4 &acc0, f32x4 &acc1, const u32x4 *
 // What bounds it is the stream of weights, so it must not stop: a wave has the next
 // unit's weights in flight while it multiplies (loads return in order: the other
 // factor's are asked for before them), also across the end of a task, and two
-// workgroups share a CU.
+// workgroups share a CU.  With AHEAD = 2 a wave has two units in flight: one workgroup a CU of
+// them keeps up a stream of bf16 weights for many tokens better (64 tokens: 204 us, now 180),
+// and two of them MX4's for few.
 template <bool MX, int TB, int AHEAD>
 __global__ __launch_bounds__(kThreads, !MX && AHEAD > 1 ? 2 : 4) void moe_up_kernel(MoeCall c) {
   typedef Rows16<MX> Rows;
@@ -649,7 +656,7 @@ __global__ __launch_bounds__(kThreads, AHEAD == 1 ? 4 : 2) void moe_down_kernel(
     }
     bool store = has;
     if (segments > 1) {
-      constexpr int kDevice = 16;  // cache policy: device scope, as put_device and get_device
+      constexpr int kDevice = 16;  // cache policy: device scope, as put_device
       const uint32_t at = ((uint32_t)tok * (uint32_t)c.H + (uint32_t)row) * 4u, whole = (uint32_t)c.T * (uint32_t)c.H * 4u;
       const auto rs = rsrc_of(c.sums, whole * (uint32_t)segments);
       if (has) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rs, (int)(seg * whole + at), 0, kDevice);
@@ -678,6 +685,20 @@ __global__ __launch_bounds__(kThreads, AHEAD == 1 ? 4 : 2) void moe_down_kernel(
 
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
+// Experts that T tokens pick, on average.
+double expected_active(int T, int E, int k) { return E * (1 - std::pow(1 - (double)k / E, T)); }
+
+// Blocks of 16 rows in a task of the first product, whose waves split H between them: more where H has fewer
+// units than there are waves.  Beside that, four with many bf16 tokens, which have one workgroup a CU, for
+// fewer ends of tasks (64 tokens, 32 experts of 4096 x 2048: 177 us, now 167; 2504 x 2048: 141, 126; 16
+// experts of 4096 x 4096 lose: 181, 187), and two with MX4 as long as every workgroup has a
+// task (one token, 8 of 64 experts of 4096 x 2048: 17.9 us, now 16.4; 64 tokens: 122, 113).
+int up_row_blocks(int T, int H, int I, int E, int k, bool mx, int workgroups) {
+  const int units = mx ? (H + 255) / 256 : (H + 127) / 128, least = units >= 8 ? 1 : units >= 4 ? 2 : units >= 2 ? 4 : 8;
+  if (!mx) return T > 16 ? std::max(least, 4) : least;
+  return expected_active(T, E, k) * ((I + 31) / 32) >= workgroups ? std::max(least, 2) : least;
+}
+
 // Workgroups of the second product on a CU: y of every wave is in LDS beside what its units pass through.
 // More than 16 tokens with bf16 weights and more than 48 with MX4 leave room for one.
 int down_per_cu(int T, bool mx) { return T <= (mx ? 48 : 16) ? 2 : 1; }
@@ -689,7 +710,7 @@ int down_per_cu(int T, bool mx) { return T <= (mx ? 48 : 16) ? 2 : 1; }
 // 1264 MX4, 35 us, now 16; 37 tokens of 60 experts, 2504 x 1400 bf16, 93 us, now 69.)
 int down_segments(int T, int H, int I, int E, int k, bool mx) {
   constexpr double kCus = 256;
-  const double active = E * (1 - std::pow(1 - (double)k / E, T));  // expected
+  const double active = expected_active(T, E, k);
   const int blocks = (H + 31) / 32, units = mx ? (I + 255) / 256 : (I + 127) / 128, per_cu = down_per_cu(T, mx);
   const double unit_us = (mx ? 1.4 : 2.8) * per_cu;
   int best = 1;
@@ -774,12 +795,14 @@ int moe_launch(const occ_moe_args &a, hipStream_t s) {
   c.sums = reinterpret_cast<float *>(ws + l.sums);
   const int tb = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
   const MoeFn route = a.experts <= 64 ? route_fn<1>(tb) : a.experts <= 128 ? route_fn<2>(tb) : route_fn<8>(tb);
-  hipLaunchKernelGGL(route, dim3((a.experts + 15) / 16 * l.slices), dim3(kRouteThreads), 0, s, c);
+  const int logits = a.tokens * ((a.experts + 15) / 16 * 16) * 4;
+  if (logits > 32768 &&  // with the kernel's own 30 KB past what a launch may have unasked
+      hipFuncSetAttribute(reinterpret_cast<const void *>(route), hipFuncAttributeMaxDynamicSharedMemorySize, logits) != hipSuccess)
+    return OCC_EHIP;
+  hipLaunchKernelGGL(route, dim3((a.experts + 15) / 16 * l.slices), dim3(kRouteThreads), logits, s, c);
   if (hipGetLastError() != hipSuccess) return OCC_EHIP;
-  // the waves of a task of the first product split H in units; where it has fewer, more rows
-  const int units = mx ? (a.H + 255) / 256 : (a.H + 127) / 128;
-  c.rbs = units >= 8 ? 1 : units >= 4 ? 2 : units >= 2 ? 4 : 8;
   const unsigned grid = (unsigned)di->num_cus * (!mx && tb > 1 ? 1 : 2);
+  c.rbs = up_row_blocks(a.tokens, a.H, a.I, a.experts, a.top_k, mx, (int)grid);
   hipLaunchKernelGGL(up_fn(mx, tb), dim3(grid), dim3(kThreads), 0, s, c);
   if (hipGetLastError() != hipSuccess) return OCC_EHIP;
   const int y_bytes = kWaves * a.tokens * 128, per_cu = down_per_cu(a.tokens, mx);
