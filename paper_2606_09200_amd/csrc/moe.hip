@@ -690,13 +690,15 @@ double expected_active(int T, int E, int k) { return E * (1 - std::pow(1 - (doub
 
 // Blocks of 16 rows in a task of the first product, whose waves split H between them: more where H has fewer
 // units than there are waves.  Beside that, four with many bf16 tokens, which have one workgroup a CU, for
-// fewer ends of tasks (64 tokens, 32 experts of 4096 x 2048: 177 us, now 167; 2504 x 2048: 141, 126; 16
-// experts of 4096 x 4096 lose: 181, 187), and two with MX4 as long as every workgroup has a
-// task (one token, 8 of 64 experts of 4096 x 2048: 17.9 us, now 16.4; 64 tokens: 122, 113).
+// fewer ends of tasks, where two rounds of such tasks are left (64 tokens, 32 experts of 4096 x
+// 2048: 177 us, now 167; 2504 x 2048: 141, 126; 16 experts of 4096 x 4096 lose: 181, 187), and two
+// with MX4 where every workgroup has a task (one token, 8 of 64 experts of 4096 x 2048: 17.9 us,
+// now 16.4; 64 tokens: 122, 113).
 int up_row_blocks(int T, int H, int I, int E, int k, bool mx, int workgroups) {
   const int units = mx ? (H + 255) / 256 : (H + 127) / 128, least = units >= 8 ? 1 : units >= 4 ? 2 : units >= 2 ? 4 : 8;
-  if (!mx) return T > 16 ? std::max(least, 4) : least;
-  return expected_active(T, E, k) * ((I + 31) / 32) >= workgroups ? std::max(least, 2) : least;
+  const double active = expected_active(T, E, k);
+  if (!mx) return T > 16 && active * ((I + 63) / 64) >= 1.9 * workgroups ? std::max(least, 4) : least;
+  return active * ((I + 31) / 32) >= 0.95 * workgroups ? std::max(least, 2) : least;
 }
 
 // Workgroups of the second product on a CU: y of every wave is in LDS beside what its units pass through.

@@ -85,6 +85,14 @@ def test_layer(T, H, I, E, k, kind):
     assert all(torch.equal(a, b) for a, b in zip(out, again))
 
 
+# the most logits a routing can have; long runs of units in the second product; several units of four row blocks in the
+# first; one token to every expert
+@pytest.mark.parametrize("kind", ["bf16", "mx4"])
+@pytest.mark.parametrize("T,H,I,E,k", [(64, 64, 32, 512, 16), (20, 72, 8200, 6, 3), (24, 1160, 264, 4, 2), (1, 96, 40, 16, 16)])
+def test_layer_at_the_ends_of_its_splits(T, H, I, E, k, kind):
+    test_layer(T, H, I, E, k, kind)
+
+
 def test_equal_logits_go_to_the_lower_index():
     m = Layer(3, 64, 32, 100, 6, "bf16")
     m.router[:] = m.router[7]
