@@ -15,11 +15,11 @@
 // with its values by fours, twos and ones at fixed places (Chunks), which takes two more
 // loads and stores of one lane and no selects.
 //
-// 8192 rows of 8192 bf16: forward 100 us (5.4 TB/s of what it must read and write), backward 165
-// us with its sums joined (4.9 TB/s); binary32: 212 and 324 us (5.1, 5.0).  12004 ragged rows of 5003
-// with a binary32 residual: 169 and 247 us (4.3, 4.4).  16 rows of 8192: 6.4 us, of which a
+// 8192 rows of 8192 bf16: forward 95 us (5.6 TB/s of what it must read and write), backward 165
+// us with its sums joined (4.9 TB/s); binary32: 198 and 324 us (5.4, 5.0).  12004 ragged rows of 5003
+// with a binary32 residual: 144 and 250 us (5.0, 4.3).  16 rows of 8192: 6.4 us, of which a
 // launch is 2.3 and the rest the way through two sums.  Rows beyond 8192 columns go backward at
-// 4.0 (bf16) and 2.9 TB/s (binary32): one row a CU in flight, nothing fetched ahead.
+// 4.1 (bf16) and 2.9 TB/s (binary32): one row a CU in flight, nothing fetched ahead.
 #include "block_util.h"
 
 #include <algorithm>
@@ -81,82 +81,81 @@ int chunks(int D) { return (D + 7) / 8; }
 
 // ---------------------------------------------------------------------------
 // Forward.  A workgroup of as many waves as a row needs at NCH chunks of 8 columns a thread (chunk c
-// of thread t: columns 8 (c threads + t)) walks rows with the grid's stride; one wave
-// needs no barrier.
+// of thread t: columns 8 (c threads + t)) has one row; one wave needs no barrier.  As many
+// workgroups as the chip holds, each walking rows, were slower: their rows go in step (12004 rows of
+// 5120: 161 us, now 132; 16384 of 4096: 100, 94).
 template <int NCH, bool REST, class ACT, class RES>
 __global__ __launch_bounds__(1024) void norm_gate_kernel(NormFwd a) {
-  __shared__ float slots[2][2][16];
+  __shared__ float slots[2][16];
   const Chunks<NCH, REST> cols(a.D);
   const float inv_d = 1.0f / (float)a.D;
   const ACT *w1 = static_cast<const ACT *>(a.w_post), *w2 = static_cast<const ACT *>(a.w_pre);
-  int par = 0;
-  for (int row = blockIdx.x; row < a.rows; row += gridDim.x, par ^= 1) {
-    const ACT *f = static_cast<const ACT *>(a.f) + (size_t)row * a.ld_f;
-    const RES *x = static_cast<const RES *>(a.x) + (size_t)row * a.ld_x;
-    RES *yo = static_cast<RES *>(a.y) + (size_t)row * a.ld_y;
-    ACT *ho = static_cast<ACT *>(a.h) + (a.h != nullptr ? (size_t)row * a.ld_h : 0);
-    const ACT *gate = static_cast<const ACT *>(a.gate);
-    if (gate != nullptr) gate += (size_t)(row / a.rows_per_gate) * a.D;
-    Raw8<ACT> fv[NCH];
-    Raw8<RES> xv[NCH];
+  const int row = blockIdx.x;
+  const ACT *f = static_cast<const ACT *>(a.f) + (size_t)row * a.ld_f;
+  const RES *x = static_cast<const RES *>(a.x) + (size_t)row * a.ld_x;
+  RES *yo = static_cast<RES *>(a.y) + (size_t)row * a.ld_y;
+  ACT *ho = static_cast<ACT *>(a.h) + (a.h != nullptr ? (size_t)row * a.ld_h : 0);
+  const ACT *gate = static_cast<const ACT *>(a.gate);
+  if (gate != nullptr) gate += (size_t)(row / a.rows_per_gate) * a.D;
+  Raw8<ACT> fv[NCH];
+  Raw8<RES> xv[NCH];
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) cols.load(fv[c], f, c);
+  for (int c = 0; c < NCH; ++c) cols.load(fv[c], f, c);
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) cols.load(xv[c], x, c);
-    float r1 = 1.f;
-    if (a.post) {
-      float ss = 0.f;
-#pragma unroll
-      for (int c = 0; c < NCH; ++c)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(fv[c].at(e), fv[c].at(e), ss);
-      r1 = 1.0f / __builtin_sqrtf(row_sum(ss, slots[par][0]) * inv_d + a.eps);
-    }
+  for (int c = 0; c < NCH; ++c) cols.load(xv[c], x, c);
+  float r1 = 1.f;
+  if (a.post) {
     float ss = 0.f;
-    float y[NCH][8];
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(fv[c].at(e), fv[c].at(e), ss);
+    r1 = 1.0f / __builtin_sqrtf(row_sum(ss, slots[0]) * inv_d + a.eps);
+  }
+  float ss = 0.f;
+  float y[NCH][8];
+#pragma unroll
+  for (int c = 0; c < NCH; ++c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[c][e] = fv[c].at(e) * r1;
+    if (w1 != nullptr) {
+      Raw8<ACT> w;
+      cols.load(w, w1, c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[c][e] = y[c][e] * w.at(e);
+    }
+    if (gate != nullptr) {
+      Raw8<ACT> w;
+      cols.load(w, gate, c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[c][e] = y[c][e] * w.at(e);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      y[c][e] = __builtin_fmaf(a.alpha, xv[c].at(e), y[c][e]);
+      ss = __builtin_fmaf(y[c][e], y[c][e], ss);
+    }
+    cols.template store<true>(yo, c, y[c]);
+  }
+  float r2 = 1.f;
+  if (a.h != nullptr) {
+    r2 = 1.0f / __builtin_sqrtf(row_sum(ss, slots[1]) * inv_d + a.eps);
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[c][e] = fv[c].at(e) * r1;
-      if (w1 != nullptr) {
+      for (int e = 0; e < 8; ++e) y[c][e] = y[c][e] * r2;
+      if (w2 != nullptr) {
         Raw8<ACT> w;
-        cols.load(w, w1, c);
+        cols.load(w, w2, c);
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[c][e] = y[c][e] * w.at(e);
       }
-      if (gate != nullptr) {
-        Raw8<ACT> w;
-        cols.load(w, gate, c);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[c][e] = y[c][e] * w.at(e);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        y[c][e] = __builtin_fmaf(a.alpha, xv[c].at(e), y[c][e]);
-        ss = __builtin_fmaf(y[c][e], y[c][e], ss);
-      }
-      cols.template store<true>(yo, c, y[c]);
+      cols.template store<true>(ho, c, y[c]);
     }
-    float r2 = 1.f;
-    if (a.h != nullptr) {
-      r2 = 1.0f / __builtin_sqrtf(row_sum(ss, slots[par][1]) * inv_d + a.eps);
-#pragma unroll
-      for (int c = 0; c < NCH; ++c) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[c][e] = y[c][e] * r2;
-        if (w2 != nullptr) {
-          Raw8<ACT> w;
-          cols.load(w, w2, c);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[c][e] = y[c][e] * w.at(e);
-        }
-        cols.template store<true>(ho, c, y[c]);
-      }
-    }
-    if (a.rstd != nullptr && threadIdx.x == 0) {
-      a.rstd[2 * (size_t)row] = r1;
-      a.rstd[2 * (size_t)row + 1] = r2;
-    }
+  }
+  if (a.rstd != nullptr && threadIdx.x == 0) {
+    a.rstd[2 * (size_t)row] = r1;
+    a.rstd[2 * (size_t)row + 1] = r2;
   }
 }
 
@@ -430,13 +429,14 @@ FwdFn fwd_fn(int nch) {
 }
 template <class ACT, class RES>
 int launch_fwd(const NormFwd &a, int num_cus, hipStream_t s) {
-  // 16 columns a thread; 8 where rows are fewer than the CUs, which shortens a row's way through its
+  // 16 columns a thread of a bf16 residual (8192 rows of 8192: 95 us, with 8 columns 112), 8 of a binary32 one
+  // (20000 rows of 1505: 72 us, with 16 80); 8 too where rows are fewer than the CUs, for a row's way through its
   // two sums, and up to 512 columns, a wave's
-  const int nch = a.D <= 512 || (a.rows <= num_cus && a.D <= 8192) ? 1 : 2;
+  const bool one = sizeof(RES) == 4 || a.D <= 512 || a.rows <= num_cus;
+  const int nch = one && a.D <= 8192 ? 1 : 2;
   const int rt = row_threads(a.D, nch);
   const FwdFn fn = a.D % 8 != 0 ? fwd_fn<true, ACT, RES>(nch) : fwd_fn<false, ACT, RES>(nch);
-  const int grid = std::min(a.rows, num_cus * std::max(1, 2048 / rt));  // 32 waves a CU
-  hipLaunchKernelGGL(fn, dim3(grid), dim3(rt), 0, s, a);
+  hipLaunchKernelGGL(fn, dim3(a.rows), dim3(rt), 0, s, a);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
 }
 
