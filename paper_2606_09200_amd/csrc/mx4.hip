@@ -274,7 +274,7 @@ __global__ __launch_bounds__(256) void mx4_dequant_kernel(const uint8_t *__restr
         const auto v2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[i], sc, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[i], sc, 3);
         v[0] = v0[0], v[1] = v0[1], v[2] = v1[0], v[3] = v1[1], v[4] = v2[0], v[5] = v2[1], v[6] = v3[0], v[7] = v3[1];
         if (cols - c >= 8) {
-          store8(o, true, v);
+          store8<false>(o, true, v);
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
