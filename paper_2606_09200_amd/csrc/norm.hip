@@ -15,9 +15,9 @@
 // with its values by fours, twos and ones at fixed places (Chunks), which takes two more
 // loads and stores of one lane and no selects.
 //
-// 8192 rows of 8192 bf16: forward 95 us (5.6 TB/s of what it must read and write), backward 165
-// us with its sums joined (4.9 TB/s); binary32: 198 and 324 us (5.4, 5.0).  12004 ragged rows of 5003
-// with a binary32 residual: 144 and 250 us (5.0, 4.3).  16 rows of 8192: 6.4 us, of which a
+// 8192 rows of 8192 bf16: forward 95 us (5.6 TB/s of what it must read and write), backward 153
+// us with its sums joined (5.3 TB/s); binary32: 198 and 311 us (5.4, 5.2).  12004 ragged rows of 5003
+// with a binary32 residual: 144 and 221 us (5.0, 4.9).  16 rows of 8192: 6.4 us, of which a
 // launch is 2.3 and the rest the way through two sums.  Rows beyond 8192 columns go backward at
 // 4.1 (bf16) and 2.9 TB/s (binary32): one row a CU in flight, nothing fetched ahead.
 #include "block_util.h"
@@ -69,7 +69,7 @@ struct Chunks {
     v.load(element(row, at[c]), in[c]);
     if (REST && end[c]) v.load_rest(element(row, at[c]), D);
   }
-  // NT for the forward rows (8192 rows of 8191 bf16: 140 us, without 145); the backward pass's are
+  // NT for the forward rows (8192 rows of 8192 bf16: 94 us, without 100); the backward pass's are
   // stored plainly (8192 rows of 8192 binary32: 324 us, with 355).
   template <bool NT, class E>
   __device__ __forceinline__ void store(E *row, int c, const float (&v)[8]) const {
@@ -165,9 +165,10 @@ __global__ __launch_bounds__(1024) void norm_gate_kernel(NormFwd a) {
 // row is worked on.
 //
 // Where gates are shared by many rows (or there is none), a run stays within one
-// gate's rows (`per_gate` runs each).  S and dw2's sum leave as one row each of the
+// gate's rows: every per_gate-th of them, so that all runs together walk through memory (runs of
+// neighbouring rows: 8192 x 8192 bf16 165 us instead of 153, binary32 324 and 311).  S and dw2's sum leave as one row each of the
 // partial arrays; with several gates g S does too, as the first.  Where gates are not
-// shared so (DIRECT), a run is `gates` whole gates: at the end of each, dg is
+// shared so (DIRECT), a run is every runs-th whole gate: at the end of each, dg is
 // complete and stored, and g S goes into the run's sum of dw1, the first array's row.
 //
 // Up to 8192 columns (NCH = 1) the sums, the weights and two rows fit in registers.
@@ -206,13 +207,13 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
   const float inv_d = 1.0f / (float)D;
   int row_begin, row_end, gate_at;
   if (DIRECT) {
-    gate_at = blockIdx.x * a.gates;
+    gate_at = blockIdx.x;
     row_begin = gate_at * a.rows_per_gate;
-    row_end = min(a.rows, row_begin + a.gates * a.rows_per_gate);
+    row_end = a.rows;
   } else {
     gate_at = blockIdx.x / a.per_gate;
-    row_begin = gate_at * a.rows_per_gate + (int)(blockIdx.x % a.per_gate) * a.run;
-    row_end = min((gate_at + 1) * a.rows_per_gate, row_begin + a.run);
+    row_begin = gate_at * a.rows_per_gate + (int)(blockIdx.x % a.per_gate);
+    row_end = (gate_at + 1) * a.rows_per_gate;
   }
   Chunks<NCH, REST> cols(D);
   const ACT *w_post = static_cast<const ACT *>(a.w_post), *w_pre = static_cast<const ACT *>(a.w_pre);
@@ -262,11 +263,13 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
   Rows q;
   if (!WIDE && row_begin < row_end) fetch(q, row_begin);
   int par = 0, in_gate = 0;
-  for (int row = row_begin; row < row_end; ++row, par ^= 1) {
+  for (int row = row_begin, next; row < row_end; row = next, par ^= 1) {
+    if (DIRECT) next = in_gate + 1 < a.rows_per_gate ? row + 1 : row + 1 + ((int)gridDim.x - 1) * a.rows_per_gate;
+    else next = row + a.per_gate;
     Rows ahead;
     cols.fresh();
     if (WIDE) fetch(q, row);
-    else fetch(ahead, min(row + 1, row_end - 1));
+    else if (next < row_end) fetch(ahead, next);
     float d[NCH][8];
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
@@ -354,7 +357,7 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
         if (a.dgate != nullptr) cols.template store<false>(a.dgate + (size_t)gate_at * D, c, m);
       }
       in_gate = 0;
-      ++gate_at;
+      gate_at += gridDim.x;
     }
     if (!WIDE) q = ahead;
   }
@@ -457,10 +460,10 @@ NormSplit norm_split(int rows, int D, int groups) {
   NormSplit p{};
   p.rt = row_threads(D, wide_row(D) ? 2 : 1);
   if (rows == 0) return p;
-  // at most kNormRuns * 1024 / rt runs: a workgroup of 1024 threads per CU or its equal in
-  // threads; more would write more partial rows than they gain in load balance.  Few rows make no
-  // more than one run a CU, of up to 4 rows.
-  const int target = kNormRuns * 1024 / p.rt;
+  // at most one run a CU, or as many as make 512 threads: more fill the CUs no better, start unevenly and write
+  // more partial rows (up to 1024 threads a CU: 16384 rows of 4096 bf16 165 us instead of 152,
+  // 12004 of 5003 241 and 221, 32768 of 512 53 and 48).  Few rows make runs of up to 4.
+  const int target = kNormRuns * std::max(1, 512 / p.rt);
   p.rows_per_gate = rows / groups;
   const int run = std::max((rows + target - 1) / target, std::min(4, (rows + kNormRuns - 1) / kNormRuns));
   p.direct = groups > 1 && p.rows_per_gate < run * 2;
@@ -506,7 +509,7 @@ int norm_gate_bwd_launch(const occ_norm_args &n, hipStream_t s) {
   a.f = n.f, a.y = n.y, a.dy = n.dy, a.dh = n.dh, a.w_post = n.w_post, a.w_pre = n.w_pre, a.gate = n.gate;
   a.rstd = n.rstd, a.df = n.df, a.dx = n.dx, a.dw_post = n.dw_post, a.dw_pre = n.dw_pre, a.dgate = n.dgate;
   a.ld_f = n.ld_f, a.ld_y = n.ld_y, a.ld_dy = n.ld_dy, a.ld_dh = n.ld_dh, a.ld_df = n.ld_df, a.ld_dx = n.ld_dx;
-  a.rows_per_gate = p.rows_per_gate, a.run = p.run, a.per_gate = p.per_gate, a.gates = p.gates;
+  a.rows_per_gate = p.rows_per_gate, a.per_gate = p.per_gate;
   a.part1 = static_cast<float *>(n.workspace);
   a.part2 = a.part1 + (size_t)p.runs * n.D;
   const bool three = groups > 1 && !p.direct;

@@ -131,11 +131,11 @@ struct NormBwd {
   void *df, *dx;
   float *dw_post, *dw_pre, *dgate;
   size_t ld_f, ld_y, ld_dy, ld_dh, ld_df, ld_dx;
-  int rows_per_gate, run, per_gate, gates;  // see NormSplit
-  float *part1, *part2, *part3;             // runs x D each; part3 only where several gates have several runs
+  int rows_per_gate, per_gate;  // see NormSplit
+  float *part1, *part2, *part3;  // runs x D each; part3 only where several gates have several runs
 };
 // The backward's runs of rows: either `per_gate` runs of at most `run` rows within each gate's
-// rows, or (direct) runs of `gates` whole gates.  rt: threads a run.
+// rows, or (direct) runs of up to `gates` whole gates.  rt: threads a run.
 struct NormSplit {
   int rt, runs, rows_per_gate;
   bool direct;
