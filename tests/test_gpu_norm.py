@@ -106,6 +106,19 @@ def test_forward_options(act, res):
                 assert (yw[:, D:] == 77).all() and (hw[:, D:] == 77).all() and (with_h or (h == 77).all())
 
 
+@pytest.mark.parametrize("act,res", TYPES)
+@pytest.mark.parametrize("rows,D", [(1, 5), (700, 333), (300, 8190), (40, 16381)])
+def test_forward_in_place(rows, D, act, res):
+    """y over x and h over f: the same bits as in buffers of their own."""
+    p = problem(rows, D, act, res, 1, seed=D)
+    args = dict(w_post=p["w_post"], w_pre=p["w_pre"], gate=p["gate"], alpha=ALPHA, eps=EPS)
+    (y, _), (h, _) = blank((rows, D), res), blank((rows, D), act)
+    occ.occ_norm_gate(p["f"], p["x"], y, h, **args)
+    f, x = p["f"].clone(), p["x"].clone()
+    occ.occ_norm_gate(f, x, x, f, **args)
+    assert torch.equal(x, y) and torch.equal(f, h)
+
+
 @pytest.mark.parametrize("D", [96, 3001, 9000])
 def test_zero_and_nonfinite_rows_stay_their_own(D):
     p = problem(6, D, BF16, F32, 1, seed=5)
