@@ -23,7 +23,7 @@ namespace {
 //
 // K is padded by the format: rows of codes have whole 512-column pieces of zeros.
 //
-// 8192^3: 234 to 250 us, 4.4 to 4.7 PFLOP/s.  A k-step takes 1800 cycles of LDS (20 fragments a wave read, 68 KiB
+// 8192^3: 234 to 250 us, 4.4 to 4.7 PFLOP/s.  A k-step takes 2100 cycles of LDS (24 KiB a wave read, 68 KiB
 // written) beside 2048 of the matrix pipes, which are 57 % busy at the 1.8 to 1.9 GHz the
 // board's power leaves; a tile's first loads and last stores are 10 us of 60.
 template <class OUT>

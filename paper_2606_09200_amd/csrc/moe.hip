@@ -714,16 +714,15 @@ int down_per_cu(int T, bool mx) { return T <= (mx ? 48 : 16) ? 2 : 1; }
 // wave) what 32 rows of 512 bytes a wave take at a CU's share of 6 TB/s; tasks run in rounds of
 // as many as the chip holds.  (Four tasks a workgroup whatever the sizes: 55 tokens of 8 experts, 6144 x
 // 1264 MX4, 35 us, now 16; 37 tokens of 60 experts, 2504 x 1400 bf16, 93 us, now 69.)
-int down_segments(int T, int H, int I, int E, int k, bool mx) {
-  constexpr double kCus = 256;
-  const double active = expected_active(T, E, k);
-  const int blocks = (H + 31) / 32, units = mx ? (I + 255) / 256 : (I + 127) / 128, per_cu = down_per_cu(T, mx);
-  const double unit_us = (mx ? 1.4 : 2.8) * per_cu;
+int down_segments(int T, int H, int I, double active, int most, bool mx) {
+  const double slots = 256.0 * down_per_cu(T, mx), per_slot = 1 / slots;
+  const int blocks = (H + 31) / 32, units = mx ? (I + 255) / 256 : (I + 127) / 128;
+  const double unit_us = (mx ? 1.4 : 2.8) * down_per_cu(T, mx), work = std::max(1.0, active) * units / kWaves;
   int best = 1;
   double t_best = 0;
-  for (int seg = 1; seg <= std::min(E, T * k); ++seg) {
-    const double n = std::min((double)seg, std::max(1.0, active));
-    const double us = std::ceil(blocks * n / (kCus * per_cu)) * ((seg > 1 ? 3 : 2) + unit_us * std::max(1.0, active * units / n / kWaves));
+  // past the last split that leaves a wave a unit, or four rounds of tasks, nothing is gained
+  for (int seg = 1; seg <= most && (seg == 1 || (seg <= active && work >= seg && blocks * seg <= 4 * slots)); ++seg) {
+    const double us = std::ceil(blocks * seg * per_slot) * ((seg > 1 ? 3 : 2) + unit_us * std::max(1.0, work / seg));
     if (seg == 1 || us < t_best) best = seg, t_best = us;
   }
   return best;
@@ -732,14 +731,16 @@ int down_segments(int T, int H, int I, int E, int k, bool mx) {
 // The workspace's parts; the counters come first.
 struct MoeLayout {
   size_t plan, rows, joined, part, hidden, sums, end;
-  int slices, row_blocks;
+  int slices, row_blocks, segments[2];  // of the second product with bf16 and with MX4 weights
 };
 MoeLayout layout_of(int T, int H, int I, int E, int k) {
   MoeLayout l{};
   const int steps = kRouteWaves / (T <= 16 ? 1 : T <= 32 ? 2 : 4);  // of 128 columns, that a router workgroup takes at once
   l.slices = std::max(1, std::min(kSlices, (H + 128 * steps - 1) / (128 * steps)));
   l.row_blocks = (H + 31) / 32;
-  const int segments = std::max(down_segments(T, H, I, E, k, false), down_segments(T, H, I, E, k, true));
+  const double active = expected_active(T, E, k);
+  for (int mx = 0; mx < 2; ++mx) l.segments[mx] = down_segments(T, H, I, active, std::min(E, T * k), mx != 0);
+  const int segments = std::max(l.segments[0], l.segments[1]);
   size_t at = up16(sizeof(MoeCounters));
   l.plan = at, at += up16((size_t)E * (T > 32 ? 2 : 1) * sizeof(MoeExpert));
   l.rows = at, at += up16((size_t)T * k * sizeof(MoeRow));
@@ -778,7 +779,7 @@ int moe_launch(const occ_moe_args &a, hipStream_t s) {
   unsigned char *ws = static_cast<unsigned char *>(a.workspace);
   MoeCall c{};
   c.T = a.tokens, c.H = a.H, c.I = a.I, c.E = a.experts, c.k = a.top_k, c.renorm = a.renorm != 0;
-  c.slices = l.slices, c.row_blocks = l.row_blocks, c.max_segments = down_segments(a.tokens, a.H, a.I, a.experts, a.top_k, a.weight_type == OCC_MX4);
+  c.slices = l.slices, c.row_blocks = l.row_blocks, c.max_segments = l.segments[a.weight_type == OCC_MX4];
   c.x = static_cast<const uint16_t *>(a.x), c.ld_x = (int)a.ld_x;
   c.router = static_cast<const uint16_t *>(a.router);
   const bool mx = a.weight_type == OCC_MX4;
