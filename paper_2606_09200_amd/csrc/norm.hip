@@ -19,7 +19,7 @@
 // us with its sums joined (5.3 TB/s); binary32: 198 and 311 us (5.4, 5.2).  12004 ragged rows of 5003
 // with a binary32 residual: 144 and 221 us (5.0, 4.9).  16 rows of 8192: 6.4 us, of which a
 // launch is 2.3 and the rest the way through two sums.  Rows beyond 8192 columns go backward at
-// 4.1 (bf16) and 2.9 TB/s (binary32): one row a CU in flight, nothing fetched ahead.
+// 4.5 TB/s: one row a CU in flight, nothing fetched ahead.
 #include "block_util.h"
 
 #include <algorithm>
@@ -59,7 +59,7 @@ struct Chunks {
     }
   }
   // Keeps the offsets from being folded into 64-bit addresses of each tensor's chunks, which would live
-  // across rows: the backward pass spilled them (4096 rows of 16384 binary32: 681 us, now 551).
+  // across rows: the backward pass spilled them.
   __device__ __forceinline__ void fresh() {
 #pragma unroll
     for (int c = 0; c < NCH; ++c) asm volatile("" : "+v"(at[c]));
@@ -173,7 +173,7 @@ __global__ __launch_bounds__(1024) void norm_gate_kernel(NormFwd a) {
 //
 // Up to 8192 columns (NCH = 1) the sums, the weights and two rows fit in registers.
 // Beyond (NCH = 2, 1024 threads of 128 registers) the sums live in LDS, the
-// weights come from the caches for each row, and rows are not fetched ahead.
+// binary32 weights come from the caches for each row, and rows are not fetched ahead.
 template <int N, bool LDS>
 struct ColumnSums;  // N sums a thread
 template <int N>
@@ -200,6 +200,7 @@ struct ColumnSums<N, true> {
 template <int NCH, bool REST, class ACT, class RES, bool DIRECT>
 __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
   constexpr bool WIDE = NCH > 1;
+  constexpr bool KEEP = !WIDE || sizeof(ACT) == 2;  // weights stay in registers
   __shared__ float slots[2][2][16];
   extern __shared__ __align__(16) unsigned char smem[];  // WIDE: two arrays of 8 NCH 1024 sums
   float *lds = reinterpret_cast<float *>(smem);
@@ -219,13 +220,18 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
   const ACT *w_post = static_cast<const ACT *>(a.w_post), *w_pre = static_cast<const ACT *>(a.w_pre);
   const ACT *gate = static_cast<const ACT *>(a.gate);
   Raw8<ACT> w1[NCH], w2[NCH], gv[NCH];
+  // loaded again for each row: what a null pointer leaves is cleared, or the last row's registers would stay live
+  // (and 80 of them in scratch memory: 4096 rows of 16384 binary32 546 us, now 354)
   auto load_gate = [&](int c) {
+    if (!KEEP) gv[c] = Raw8<ACT>{};
     if (gate != nullptr) cols.load(gv[c], gate + (size_t)gate_at * D, c);
   };
   auto load_post = [&](int c) {
+    if (!KEEP) w1[c] = Raw8<ACT>{};
     if (w_post != nullptr) cols.load(w1[c], w_post, c);
   };
   auto load_pre = [&](int c) {
+    if (!KEEP) w2[c] = Raw8<ACT>{};
     if (w_pre != nullptr) cols.load(w2[c], w_pre, c);
   };
   auto post = [&](int c, int e) { return w_post != nullptr ? w1[c].at(e) : 1.f; };
@@ -237,11 +243,13 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
   ColumnSums<8 * NCH, WIDE && !DIRECT> s1(lds);
   ColumnSums<8 * NCH, WIDE> s2(lds + 8 * NCH * 1024);
   ColumnSums<8 * NCH, WIDE && DIRECT> dw1(lds);
-  if (!WIDE) {
-    load_post(0);
-    load_pre(0);
-    if (!DIRECT) load_gate(0);
-  }
+  if (KEEP)
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+      load_post(c);
+      load_pre(c);
+      if (!DIRECT) load_gate(c);
+    }
   struct Rows {
     Raw8<ACT> f[NCH], dh[NCH];
     Raw8<RES> y[NCH], dy[NCH];
@@ -268,8 +276,11 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
     else next = row + a.per_gate;
     Rows ahead;
     cols.fresh();
-    if (WIDE) fetch(q, row);
-    else if (next < row_end) fetch(ahead, next);
+    if (WIDE) {
+      q = Rows{};
+      fetch(q, row);
+    }
+    if (!WIDE && next < row_end) fetch(ahead, next);
     float d[NCH][8];
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
@@ -284,7 +295,7 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
         fence();
-        if (WIDE) load_pre(c);
+        if (!KEEP) load_pre(c);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float yn = q.y[c].at(e) * q.r2;
@@ -297,17 +308,19 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
       for (int c = 0; c < NCH; ++c) {
         q.y[c].forget();
         q.dh[c].forget();
-        if (WIDE) load_pre(c);
+        if (!KEEP) load_pre(c);
 #pragma unroll
         for (int e = 0; e < 8; ++e) d[c][e] = q.r2 * (pre(c, e) - dot * (q.y[c].at(e) * q.r2));
       }
     }
-    if (!WIDE && DIRECT && in_gate == 0) load_gate(0);
+    if (KEEP && DIRECT && in_gate == 0)
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) load_gate(c);
     float dot = 0.f;
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
       fence();
-      if (WIDE) {
+      if (!KEEP) {
         load_gate(c);
         load_post(c);
       }
@@ -343,7 +356,7 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
         float m[8];
-        if (WIDE) {
+        if (!KEEP) {
           load_gate(c);
           load_post(c);
         }
@@ -373,7 +386,7 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
     }
     cols.template store<false>(a.part2 + mine, c, n);
     if (three) {
-      if (WIDE) load_gate(c);
+      if (!KEEP) load_gate(c);
       cols.template store<false>(a.part3 + mine, c, m);
 #pragma unroll
       for (int e = 0; e < 8; ++e) m[e] = m[e] * gated(c, e);
