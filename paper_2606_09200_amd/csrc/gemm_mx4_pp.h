@@ -23,9 +23,11 @@ namespace {
 //
 // K is padded by the format: rows of codes have whole 512-column pieces of zeros.
 //
-// 8192^3: 234 to 250 us, 4.4 to 4.7 PFLOP/s.  A k-step takes 2100 cycles of LDS (24 KiB a wave read, 68 KiB
-// written) beside 2048 of the matrix pipes, which are 57 % busy at the 1.8 to 1.9 GHz the
-// board's power leaves; a tile's first loads and last stores are 10 us of 60.
+// 8192^3: 234 to 260 us, 4.2 to 4.7 PFLOP/s; K = 32768: 4.9.  Power bounds it: the board's cap leaves 1.8 to 1.9
+// GHz (operands of zeros run 1.4 times as fast), at which the matrix pipes are 57 % busy.  Next are the
+// reads and barriers between the phases (with a quarter of the MFMAs the loop still takes two thirds of
+// its time; LDS itself is 30 % busy) and a tile's first loads and last stores, 10 us of 60.  Memory
+// is not: with every k-step in the L2 it gains 3 %.
 template <class OUT>
 struct Mx4Pp {
   typedef OUT Out;
