@@ -283,7 +283,8 @@ struct Rows16 {
     pitch = MX ? (uint32_t)(OCC_MX4_KP(cols) / 2) : (uint32_t)cols * 2u;
     r = rsrc_of(static_cast<const uint8_t *>(m.w) + (size_t)e * m.stride + (size_t)row0 * pitch,
                 (uint32_t)min(16, rows - row0) * pitch);
-    if constexpr (MX) rs = rsrc_of(m.scales + (size_t)e * m.scale_stride + (size_t)(row0 >> 4) * pitch, pitch);
+    // row0 = rows (no rows) may lie past the last scale tile
+    if constexpr (MX) rs = rsrc_of(m.scales + (size_t)e * m.scale_stride + (size_t)(row0 >> 4) * pitch, row0 < rows ? pitch : 0u);
     at = (uint32_t)(lane / CH) * pitch + (uint32_t)(lane % CH) * 16u;
     left = pitch - (uint32_t)(lane % CH) * 16u;
     whole = pitch % 128u == 0u && ((uintptr_t)m.w + m.stride) % 128u == 0u && m.stride % 128u == 0u;

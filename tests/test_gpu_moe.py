@@ -93,6 +93,21 @@ def test_layer_at_the_ends_of_its_splits(T, H, I, E, k, kind):
     test_layer(T, H, I, E, k, kind)
 
 
+# the last expert's last task has blocks past its rows, in both products: nothing is read for them
+@pytest.mark.parametrize("T,H,I,E,k", [(2, 48, 80, 3, 3), (18, 1072, 208, 2, 2)])
+def test_blocks_past_the_last_experts_rows(T, H, I, E, k):
+    m = Layer(T, H, I, E, k, "mx4", seed=11)
+    own = m.run()
+    m.check(*own)
+    for name in ("gate", "up", "down"):   # NaN scales follow the last expert's
+        q = m.w[name]
+        more = occ.mx4_empty(q.rows, q.cols, batch=E + 1, device=DEV)
+        more.codes[:E], more.scales[:E] = q.codes, q.scales
+        more.codes[E], more.scales[E] = 0, 255
+        m.w[name] = occ.Mx4(more.codes[:E], more.scales[:E], q.rows, q.cols)
+    assert all(torch.equal(a, b) for a, b in zip(own, m.run()))
+
+
 def test_equal_logits_go_to_the_lower_index():
     m = Layer(3, 64, 32, 100, 6, "bf16")
     m.router[:] = m.router[7]
