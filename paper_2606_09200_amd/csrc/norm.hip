@@ -90,7 +90,8 @@ __global__ __launch_bounds__(1024) void norm_gate_kernel(NormFwd a) {
   const Chunks<NCH, REST> cols(a.D);
   const float inv_d = 1.0f / (float)a.D;
   const ACT *w1 = static_cast<const ACT *>(a.w_post), *w2 = static_cast<const ACT *>(a.w_pre);
-  const int row = blockIdx.x;
+  const int row = blockIdx.y * gridDim.x + blockIdx.x;
+  if (row >= a.rows) return;
   const ACT *f = static_cast<const ACT *>(a.f) + (size_t)row * a.ld_f;
   const RES *x = static_cast<const RES *>(a.x) + (size_t)row * a.ld_x;
   RES *yo = static_cast<RES *>(a.y) + (size_t)row * a.ld_y;
@@ -452,7 +453,9 @@ int launch_fwd(const NormFwd &a, int num_cus, hipStream_t s) {
   const int nch = one && a.D <= 8192 ? 1 : 2;
   const int rt = row_threads(a.D, nch);
   const FwdFn fn = a.D % 8 != 0 ? fwd_fn<true, ACT, RES>(nch) : fwd_fn<false, ACT, RES>(nch);
-  hipLaunchKernelGGL(fn, dim3(a.rows), dim3(rt), 0, s, a);
+  // a grid's dimension counts at most 2^32 work-items: rows beyond 2^21 go on in the second one
+  const int across = std::min(a.rows, 1 << 21);
+  hipLaunchKernelGGL(fn, dim3(across, (a.rows + across - 1) / across), dim3(rt), 0, s, a);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
 }
 

@@ -274,3 +274,19 @@ def test_refusals():
         occ.occ_norm_gate_bwd(y, None, p["f"], y.clone(), torch.empty((6, 2), device=DEV), dx=torch.empty_like(y),
                               workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
     assert e.value.status == occ.OCC_EINVAL
+
+
+def test_forward_of_more_rows_than_one_grid_dimension():
+    """2^26 + 3 rows of 2: a wave a row is past 2^32 work-items; every row's formula is checked on the GPU."""
+    rows, D = 2 ** 26 + 3, 2
+    base = torch.arange(rows, dtype=torch.int32, device=DEV)
+    f = torch.stack((base % 7 - 3, base % 5 + 1), 1).to(BF16)
+    x = torch.stack((base % 11 - 5, base % 3), 1).to(BF16)
+    y = torch.full((rows, D), float("nan"), dtype=BF16, device=DEV)
+    occ.occ_norm_gate(f, x, y, alpha=ALPHA, eps=EPS)
+    for lo in range(0, rows, 2 ** 24):
+        part = f[lo:lo + 2 ** 24].double()
+        n = part / (part.square().mean(1, keepdim=True) + EPS).sqrt()
+        ax = ALPHA * x[lo:lo + 2 ** 24].double()
+        tol = 2.0 ** -16 * (ax.abs() + n.abs()) + 2.0 ** -8 * (ax + n).abs() + 1e-30
+        assert ((y[lo:lo + 2 ** 24].double() - (ax + n)).abs() <= tol).all(), lo
