@@ -597,7 +597,8 @@ size_t occ_norm_gate_bwd_workspace_bytes(int rows, int D, int groups);
  *   p = softmax(l);  w_j = p_j, or p_j over the sum of the top_k (renorm != 0)
  *   y = sum_j w_j w_down_j (silu(w_gate_j x) * (w_up_j x))
  * x, router and y are bf16, the router's logits, softmax and all sums fp32; the
- * hidden activations are rounded to bf16 between the two products.  Weights are
+ * hidden activations pass between the two products as sums of two bf16 values
+ * (15 bits or more), so y has one rounding to speak of, its own.  Weights are
  * bf16 or MX4 (weight_type OCC_BF16 or OCC_MX4; MX4 scales in s_*), gate and up
  * experts x I x H, down experts x H x I; bf16 matrices lie stride_* elements apart
  * (0: packed), MX4 ones packed.  mask (tokens bytes, null: all ones): a token with

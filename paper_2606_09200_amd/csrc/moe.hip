@@ -11,8 +11,8 @@
 // queue (a workgroup may wait only for work that a running one holds), whose counter
 // answers one workgroup every 11 ns (512 of them: 5.8 us), and a kernel's start costs 2.3.
 //
-// 64 tokens, 32 experts of 4096 x 2048 bf16, top 4: 267 us, 6.0 TB/s (16 for the router, 167 and 84 for the
-// products, 6.4 TB/s both).  37 tokens, 60 of 2504 x 1400: 220 us (12, 138, 70; 5.2 TB/s).  One token, 8
+// 64 tokens, 32 experts of 4096 x 2048 bf16, top 4: 277 us, 5.8 TB/s (16 for the router, 167 and 93 for the
+// products, 6.4 and 5.8 TB/s).  37 tokens, 60 of 2504 x 1400: 220 us (12, 138, 70; 5.2 TB/s).  One token, 8
 // of 64 experts of 4096 x 2048 MX4: 40 us (9, 18, 12; 3.9 and 3.0 TB/s), latency.
 #include "block_util.h"
 #include "mx4.h"
@@ -373,15 +373,19 @@ __device__ __forceinline__ MoeExpert expert_at(const MoeCall &c, uint32_t i) {
   return e;
 }
 
-// Two 16-row blocks times one unit of the other factor's columns: acc0 += A x, acc1 += B x.
-template <bool MX>
-__device__ __forceinline__ void multiply(f32x4 &acc0, f32x4 &acc1, const u32x4 *lds, uint32_t scale0, uint32_t scale1,
-                                         const u32x4 (&x)[Rows16<MX>::STEPS][4], int lane) {
+// Two 16-row blocks times one unit of the other factor's columns, NB times 16 of them: acc0 += A x, acc1 += B x.
+template <bool MX, int NB>
+__device__ __forceinline__ void multiply(f32x4 *acc0, f32x4 *acc1, const u32x4 *lds, uint32_t scale0, uint32_t scale1,
+                                         const u32x4 (*x)[Rows16<MX>::STEPS][4], int lane) {
   if constexpr (!MX) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      acc0 = mfma_bf16(chunk<MX>(lds, i, lane), x[0][i], acc0);
-      acc1 = mfma_bf16(chunk<MX>(lds + Rows16<MX>::LDS, i, lane), x[0][i], acc1);
+      const u32x4 a = chunk<MX>(lds, i, lane), b = chunk<MX>(lds + Rows16<MX>::LDS, i, lane);
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        acc0[n] = mfma_bf16(a, x[n][0][i], acc0[n]);
+        acc1[n] = mfma_bf16(b, x[n][0][i], acc1[n]);
+      }
     }
   } else {
 #pragma unroll
@@ -390,19 +394,37 @@ __device__ __forceinline__ void multiply(f32x4 &acc0, f32x4 &acc1, const u32x4 *
       const uint32_t sa = scale0 >> (8 * s) & 255u, sb = scale1 >> (8 * s) & 255u;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        acc0 = mfma_bf16(mx4_operand(a[i], sa), x[s][i], acc0);
-        acc1 = mfma_bf16(mx4_operand(b[i], sb), x[s][i], acc1);
+        const u32x4 wa = mx4_operand(a[i], sa), wb = mx4_operand(b[i], sb);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          acc0[n] = mfma_bf16(wa, x[n][s][i], acc0[n]);
+          acc1[n] = mfma_bf16(wb, x[n][s][i], acc1[n]);
+        }
       }
       __builtin_amdgcn_sched_barrier(0);  // a step's operands at a time: registers
     }
   }
 }
 
+// A hidden activation h as two bf16 values, a row of each: h cut off after 8 bits, and what is left, rounded; together
+// 15 bits or more.  Rounded to one bf16 value instead, y of every case of 1 to 64 tokens was off by 0.0023 of its size,
+// with two by 0.0016, which is y's own rounding.  The second product takes as long up to 16 tokens and longer
+// beyond (32 experts of 4096 x 2048: 24 tokens MX4 37 -> 40 us, 64 tokens MX4 39 -> 55, bf16 84 -> 93).
+// The lower half has the upper one's sign and is not zero beside it (2^-24 of it instead), and an
+// infinity or NaN is both: an infinite weight gives an infinity, as it does with h in one piece.
+__device__ __forceinline__ uint32_t upper_halves(float lo, float hi) {
+  return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
+}
+__device__ __forceinline__ float lower_half(float h) {
+  const float top = as_float(__builtin_bit_cast(uint32_t, h) & 0xFFFF0000u), r = h - top;
+  return __builtin_fabsf(h) < __builtin_inff() ? (r == 0.f ? top * 0x1p-24f : r) : h;
+}
+
 // ---------------------------------------------------------------------------
 // silu(Wg x) * (Wu x).  A task is `rbs` blocks of 16 rows of Wg and of Wu of one expert with that
 // expert's tokens (16 to an MFMA).  8 / rbs waves split H (more blocks where H has fewer
-// units than there are waves), the sums meet in LDS in wave order, and the result is
-// rounded to bf16, the next product's operand.
+// units than there are waves), the sums meet in LDS in wave order, and the result becomes
+// two bf16 values, the next product's operands.
 //
 // What bounds it is the stream of weights, so it must not stop: a wave has the next
 // unit's weights in flight while it multiplies (loads return in order: the other
@@ -466,8 +488,8 @@ __global__ __launch_bounds__(kThreads, !MX && AHEAD > 1 ? 2 : 4) void moe_up_ker
     for (int at = 0; at < TB; ++at) ag[at] = au[at] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
     for (int u = u0; u < u1; u += kws) {
-      u32x4 x[Rows::STEPS][4];
-      factor<MX>(x, rx, xo, u, c.H, g);
+      u32x4 x[1][Rows::STEPS][4];
+      factor<MX>(x[0], rx, xo, u, c.H, g);
       // this unit's weights leave the registers, the next one's are on their way into them
       uint32_t sg, su;
       auto turn = [&](Unit<MX> &qg, Unit<MX> &qu) {
@@ -481,12 +503,12 @@ __global__ __launch_bounds__(kThreads, !MX && AHEAD > 1 ? 2 : 4) void moe_up_ker
       if (AHEAD == 1 || slot == 0) turn(wg[0], wu[0]);
       else turn(wg[AHEAD - 1], wu[AHEAD - 1]);
       if (AHEAD > 1) slot ^= 1;
-      multiply<MX>(ag[0], au[0], lds, sg, su, x, lane);
+      multiply<MX, 1>(&ag[0], &au[0], lds, sg, su, x, lane);
 #pragma unroll
       for (int at = 1; at < TB; ++at)
         if (at < nb) {
-          factor<MX>(x, rx, from_of(ex, at), u, c.H, g);
-          multiply<MX>(ag[at], au[at], lds, sg, su, x, lane);
+          factor<MX>(x[0], rx, from_of(ex, at), u, c.H, g);
+          multiply<MX, 1>(&ag[at], &au[at], lds, sg, su, x, lane);
         }
     }
     f32x4 *sums = reinterpret_cast<f32x4 *>(lds);  // [16 tokens][Wg, Wu][lane]
@@ -510,9 +532,14 @@ __global__ __launch_bounds__(kThreads, !MX && AHEAD > 1 ? 2 : 4) void moe_up_ker
 #pragma unroll
       for (int i = 0; i < 4; ++i) h[i] = gs[i] / (1.f + expf(-gs[i])) * us[i];
       const int row = ((int)(task % groups) * c.rbs + rs) * 16 + g * 4;  // I is a multiple of 8: all four exist or none
-      if (at * 16 + l16 < n && row < c.I)
-        *reinterpret_cast<uint64_t *>(c.hidden + (size_t)(ex.first + at * 16 + l16) * c.I + row) =
-            (uint64_t)pack_bf16(h[2], h[3]) << 32 | pack_bf16(h[0], h[1]);
+      if (at * 16 + l16 < n && row < c.I) {
+        float r[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = lower_half(h[i]);
+        uint16_t *to = c.hidden + (size_t)(ex.first + at * 16 + l16) * 2 * c.I + row;
+        *reinterpret_cast<uint64_t *>(to) = (uint64_t)upper_halves(h[2], h[3]) << 32 | upper_halves(h[0], h[1]);
+        *reinterpret_cast<uint64_t *>(to + c.I) = (uint64_t)pack_bf16(r[2], r[3]) << 32 | pack_bf16(r[0], r[1]);
+      }
     }
     __syncthreads();  // before the sums' place is staged into again
     ex = en;
@@ -524,15 +551,17 @@ __global__ __launch_bounds__(kThreads, !MX && AHEAD > 1 ? 2 : 4) void moe_up_ker
 // y = sum_j w_j Wd_j h_j.  A task is 32 rows of Wd for the experts of one of `segments` parts
 // of the list; the waves split those experts' columns end to end, each adding its
 // experts' weighted sums to its own rows of y in LDS, one per token (a token that did not
-// pick an expert gets nothing from it, whatever its weights hold).  With several segments
+// pick an expert gets nothing from it, whatever its weights hold).  An activation's two halves are
+// neighbouring columns of a 16-column block, up to TB of them, and their lanes add up at the end.  With several segments
 // the last one to finish a block of rows adds them in order: no sum depends on timing.
 // The weights' stream is kept up as above; a cursor runs AHEAD units in front of the
-// multiplications, across experts and tasks.  AHEAD is 2 where y leaves room for one workgroup a CU.
+// multiplications, across experts and tasks.  AHEAD is 2 where a CU has one workgroup.
 template <bool MX, int TB, int AHEAD>
 __global__ __launch_bounds__(kThreads, AHEAD == 1 ? 4 : 2) void moe_down_kernel(MoeCall c) {
   typedef Rows16<MX> Rows;
   __shared__ u32x4 staged[kWaves][2 * Rows::LDS];        // a wave's units of the two row blocks
   extern __shared__ __align__(16) unsigned char smem[];  // y: [wave][token][32 rows]
+  constexpr int XA = TB > 1 ? 2 : 1;  // blocks of 16 columns asked for ahead of the next weights
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, g = lane >> 4;
   u32x4 *lds = staged[wave];
@@ -540,7 +569,7 @@ __global__ __launch_bounds__(kThreads, AHEAD == 1 ? 4 : 2) void moe_down_kernel(
   const int segments = max(1, min(active, c.max_segments));
   const int tasks = c.row_blocks * segments;
   if ((int)blockIdx.x >= tasks) return;
-  const auto rh = rsrc_of(c.hidden, (uint32_t)(c.T * c.k) * (uint32_t)c.I * 2u);
+  const auto rh = rsrc_of(c.hidden, (uint32_t)(c.T * c.k) * (uint32_t)c.I * 4u);
   const int units = (c.I + Rows::COLS - 1) / Rows::COLS;  // of one expert
   Unit<MX> w0[AHEAD], w1[AHEAD];
   // Of a task: its rows, its first expert, and this wave's units of all its experts, end to end, from
@@ -595,23 +624,25 @@ __global__ __launch_bounds__(kThreads, AHEAD == 1 ? 4 : 2) void moe_down_kernel(
 #pragma unroll 1
     for (int u = p.start, left = p.u1 - p.u0; left > 0;) {
       const MoeExpert ex = expert_at(c, p.a0 + u / units);
-      const int n = (int)ex.n, nb = (n + 15) / 16;
+      const int n = 2 * (int)ex.n, nb = (n + 15) / 16;  // columns: an activation's two halves
       const int end = min(min(p.u1, (u / units + 1) * units), u + left);
       left -= end - u;
       auto from_of = [&](int at) {
-        return at * 16 + l16 < n ? (ex.first + at * 16 + l16) * (uint32_t)c.I * 2u + lane_bytes<MX>(g) : kNowhere;
+        return at * 16 + l16 < n ? (2 * ex.first + at * 16 + l16) * (uint32_t)c.I * 2u + lane_bytes<MX>(g) : kNowhere;
       };
       f32x4 a0[TB], a1[TB];
       MoeRow row[TB];
 #pragma unroll
       for (int at = 0; at < TB; ++at) {
         a0[at] = a1[at] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (at * 16 + l16 < n) row[at] = c.rows[ex.first + at * 16 + l16];
+        if (at * 16 + l16 < n) row[at] = c.rows[ex.first + (at * 16 + l16) / 2];
       }
 #pragma unroll 1
       for (; u < end; ++u) {
-        u32x4 x[Rows::STEPS][4];
-        factor<MX>(x, rh, from_of(0), u % units, c.I, g);
+        u32x4 x[XA][Rows::STEPS][4];
+#pragma unroll
+        for (int at = 0; at < XA; ++at)
+          if (at < nb) factor<MX>(x[at], rh, from_of(at), u % units, c.I, g);
         uint32_t s0, s1;
         auto turn = [&](Unit<MX> &q0, Unit<MX> &q1) {
           s0 = q0.scale, s1 = q1.scale;
@@ -624,28 +655,28 @@ __global__ __launch_bounds__(kThreads, AHEAD == 1 ? 4 : 2) void moe_down_kernel(
         if (AHEAD == 1 || slot == 0) turn(w0[0], w1[0]);
         else turn(w0[AHEAD - 1], w1[AHEAD - 1]);
         if (AHEAD > 1) slot ^= 1;
-        multiply<MX>(a0[0], a1[0], lds, s0, s1, x, lane);
+        if (XA == 1 || nb == 1) multiply<MX, 1>(&a0[0], &a1[0], lds, s0, s1, x, lane);
+        else multiply<MX, XA>(&a0[0], &a1[0], lds, s0, s1, x, lane);
+        if (TB > 2 && nb > 2) {
 #pragma unroll
-        for (int at = 1; at < TB; ++at)
-          if (at < nb) {
-            factor<MX>(x, rh, from_of(at), u % units, c.I, g);
-            multiply<MX>(a0[at], a1[at], lds, s0, s1, x, lane);
-          }
+          for (int at = 0; at < XA; ++at) factor<MX>(x[at], rh, from_of(XA + at), u % units, c.I, g);
+          multiply<MX, XA>(&a0[TB - XA], &a1[TB - XA], lds, s0, s1, x, lane);
+        }
       }
       if (u == p.u1) u = p.u0;
       // this part of the expert is whole: into its tokens' rows
 #pragma unroll
       for (int at = 0; at < TB; ++at)
         if (at * 16 + l16 < n) {
-          f32x4 *to = reinterpret_cast<f32x4 *>(mine + row[at].token * 32 + g * 4);
-          f32x4 v0 = to[0], v1 = to[4];
+          // both halves' lanes have both sums; the upper's takes the first 16 rows, the lower's the others
+          f32x4 *to = reinterpret_cast<f32x4 *>(mine + row[at].token * 32 + (l16 & 1) * 16 + g * 4);
+          f32x4 v = *to;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            v0[i] = __builtin_fmaf(row[at].weight, a0[at][i], v0[i]);
-            v1[i] = __builtin_fmaf(row[at].weight, a1[at][i], v1[i]);
+            const float s0 = a0[at][i] + dpp<0xB1>(a0[at][i]), s1 = a1[at][i] + dpp<0xB1>(a1[at][i]);
+            v[i] = __builtin_fmaf(row[at].weight, l16 & 1 ? s1 : s0, v[i]);
           }
-          to[0] = v0;
-          to[4] = v1;
+          *to = v;
         }
     }
     __syncthreads();
@@ -707,8 +738,9 @@ int up_row_blocks(int T, int H, int I, int E, int k, bool mx, int workgroups) {
 }
 
 // Workgroups of the second product on a CU: y of every wave is in LDS beside what its units pass through.
-// More than 16 tokens with bf16 weights and more than 48 with MX4 leave room for one.
-int down_per_cu(int T, bool mx) { return T <= (mx ? 48 : 16) ? 2 : 1; }
+// Beyond 16 tokens with bf16 weights and 48 with MX4 that leaves room for one; beyond 8, an expert's tokens may be
+// more than one block of 16 columns, whose operands do not fit in half a CU's registers (14 spilled).
+int down_per_cu(int T) { return T <= 8 ? 2 : 1; }
 
 // Parts of the list of experts that the second product's tasks take: the split of the least estimated
 // time.  A task costs 2 us beside its units, 3 where parts have to be joined, and eight units (one a
@@ -716,9 +748,9 @@ int down_per_cu(int T, bool mx) { return T <= (mx ? 48 : 16) ? 2 : 1; }
 // as many as the chip holds.  (Four tasks a workgroup whatever the sizes: 55 tokens of 8 experts, 6144 x
 // 1264 MX4, 35 us, now 16; 37 tokens of 60 experts, 2504 x 1400 bf16, 93 us, now 69.)
 int down_segments(int T, int H, int I, double active, int most, bool mx) {
-  const double slots = 256.0 * down_per_cu(T, mx), per_slot = 1 / slots;
+  const double slots = 256.0 * down_per_cu(T), per_slot = 1 / slots;
   const int blocks = (H + 31) / 32, units = mx ? (I + 255) / 256 : (I + 127) / 128;
-  const double unit_us = (mx ? 1.4 : 2.8) * down_per_cu(T, mx), work = std::max(1.0, active) * units / kWaves;
+  const double unit_us = (mx ? 1.4 : 2.8) * down_per_cu(T), work = std::max(1.0, active) * units / kWaves;
   int best = 1;
   double t_best = 0;
   // past the last split that leaves a wave a unit, or four rounds of tasks, nothing is gained
@@ -747,7 +779,7 @@ MoeLayout layout_of(int T, int H, int I, int E, int k) {
   l.rows = at, at += up16((size_t)T * k * sizeof(MoeRow));
   l.joined = at, at += up16((size_t)l.row_blocks * 4);
   l.part = at, at += up16((size_t)l.slices * ((E + 15) / 16) * T * 64);
-  l.hidden = at, at += up16((size_t)T * k * I * 2);
+  l.hidden = at, at += up16((size_t)T * k * I * 4);
   l.sums = at, at += up16(segments > 1 ? (size_t)segments * T * H * 4 : 0);
   l.end = at;
   return l;
@@ -762,9 +794,9 @@ MoeFn up_fn(bool mx, int tb) {
   if (mx) return tb == 1 ? moe_up_kernel<true, 1, 2> : moe_up_kernel<true, 2, 1>;
   return tb == 1 ? moe_up_kernel<false, 1, 1> : moe_up_kernel<false, 2, 2>;
 }
-MoeFn down_fn(bool mx, int tb, int per_cu) {
-  if (mx) return tb == 1 ? moe_down_kernel<true, 1, 1> : per_cu > 1 ? moe_down_kernel<true, 2, 1> : moe_down_kernel<true, 2, 2>;
-  return tb == 1 ? moe_down_kernel<false, 1, 1> : moe_down_kernel<false, 2, 2>;
+template <bool MX>
+MoeFn down_fn(int tokens) {
+  return tokens <= 8 ? moe_down_kernel<MX, 1, 1> : tokens <= 16 ? moe_down_kernel<MX, 2, 2> : moe_down_kernel<MX, 4, 2>;
 }
 
 }  // namespace
@@ -813,8 +845,8 @@ int moe_launch(const occ_moe_args &a, hipStream_t s) {
   c.rbs = up_row_blocks(a.tokens, a.H, a.I, a.experts, a.top_k, mx, (int)grid);
   hipLaunchKernelGGL(up_fn(mx, tb), dim3(grid), dim3(kThreads), 0, s, c);
   if (hipGetLastError() != hipSuccess) return OCC_EHIP;
-  const int y_bytes = kWaves * a.tokens * 128, per_cu = down_per_cu(a.tokens, mx);
-  hipLaunchKernelGGL(down_fn(mx, tb, per_cu), dim3(di->num_cus * per_cu), dim3(kThreads), y_bytes, s, c);
+  const int y_bytes = kWaves * a.tokens * 128, per_cu = down_per_cu(a.tokens);
+  hipLaunchKernelGGL(mx ? down_fn<true>(a.tokens) : down_fn<false>(a.tokens), dim3(di->num_cus * per_cu), dim3(kThreads), y_bytes, s, c);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
 }
 

@@ -182,7 +182,7 @@ struct MoeCall {
   MoeRow *rows;
   uint32_t *joined;  // per 32 rows of y: finished parts
   float *part;       // partial logits
-  uint16_t *hidden;  // rows x I, bf16
+  uint16_t *hidden;  // rows x 2 x I, bf16: the upper and lower halves
   float *sums;       // parts x T x H
 };
 int validate_moe_sizes(int T, int H, int I, int E, int k);

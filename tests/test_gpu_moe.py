@@ -215,3 +215,47 @@ def test_refusals():
         a = dict(x=m.x, router=m.router, w_gate=w["gate"], w_up=w["up"], w_down=w["down"], y=y, top_k=2, workspace=m.workspace)
         with pytest.raises(ValueError):
             occ.occ_moe(**dict(a, **bad))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "mx4"])
+@pytest.mark.parametrize("T,H,I,E,k", [(1, 64, 264, 4, 2), (7, 136, 520, 3, 2), (12, 64, 264, 2, 2), (40, 128, 200, 2, 2),
+                                       (64, 64, 1032, 5, 3)])
+def test_hidden_activations_keep_their_bits(T, H, I, E, k, kind):
+    """y's own rounding (2^-8) is the only one to bf16 in sight: a hidden activation is good to 2^-15 besides what its
+    sums cost, so y's tolerance has that of the sums of magnitudes.  8, 16 and 32 tokens of an expert among them."""
+    m = Layer(T, H, I, E, k, kind, seed=31 + T)
+    y, ids, w = m.run()
+    x, want, tol = ref.f64(m.x), np.zeros((T, H)), np.zeros((T, H))
+    ids, w = ref.route(x @ ref.f64(m.router).T, k, True, None)
+    for t in range(T):
+        for e, p in zip(ids[t], w[t]):
+            wg, wu, wd = (m.values[n][e] for n in ("gate", "up", "down"))
+            g, u = wg @ x[t], wu @ x[t]
+            s = g / (1 + np.exp(-g))
+            eg, eu = (H * 2.0 ** -23 * (abs(v) @ abs(x[t])) for v in (wg, wu))
+            eh = 1.1 * abs(u) * eg + abs(s) * eu + (2.0 ** -15 + 2.0 ** -20) * abs(s * u)
+            want[t] += p * (wd @ (s * u))
+            tol[t] += p * (abs(wd) @ (eh + (I * 2.0 ** -23 + 2.0 ** -16) * abs(s * u)))
+    err = np.abs(ref.f64(y) - want)
+    assert (err <= tol + 2.0 ** -8 * np.abs(want)).all(), float((err - tol - 2.0 ** -8 * np.abs(want)).max())
+
+
+@pytest.mark.parametrize("T", [6, 40])
+def test_an_infinite_weight_gives_an_infinity(T):
+    """In one place of each expert's last product: its row of y is that infinity, no NaN, and nothing else changes."""
+    m = Layer(T, 128, 72, 3, 2, "bf16", seed=4)
+    clean, ids, _ = m.run()
+    x = ref.f64(m.x)
+    for e in range(3):
+        m.w["down"][e, 17 + e, 33] = float("inf")
+    y = m.run()[0].cpu()
+    for t in range(T):
+        rows = {}
+        for e in ids[t].tolist():
+            g, u = m.values["gate"][e] @ x[t], m.values["up"][e] @ x[t]
+            rows[17 + e] = float(np.sign((g / (1 + np.exp(-g)) * u)[33]))
+        for r in range(128):
+            if r in rows:
+                assert rows[r] != 0 and float(y[t, r]) == rows[r] * float("inf"), (t, r)
+            else:
+                assert y[t, r] == clean[t, r].cpu(), (t, r)
