@@ -766,8 +766,10 @@ def _expert_weights(name, w, mx, experts, rows, cols):
         raise ValueError("w_%s must be a bfloat16 GPU tensor (%d, %d, %d)" % (name, experts, rows, cols))
     if w.is_contiguous():
         return w.data_ptr(), 0, 0
-    if w.stride(2) != 1 or w.stride(1) != cols:
-        raise ValueError("w_%s must be of contiguous matrices" % name)
+    # experts that share memory (an expanded weight's stride is 0, which to the library means packed) would be read past
+    # what there is of them
+    if w.stride(2) != 1 or w.stride(1) != cols or (experts > 1 and w.stride(0) < rows * cols):
+        raise ValueError("w_%s must be of contiguous matrices that do not overlap" % name)
     return w.data_ptr(), 0, w.stride(0) if experts > 1 else 0
 
 

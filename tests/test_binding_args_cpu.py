@@ -53,3 +53,21 @@ def test_row_pointers_only_for_rows_that_can_be_read_as_chunks():
     for v in (t.t(), t[:, ::2], t[:0], t[:, :0], t[0], t[0].expand(3, 11)):
         assert occ._row_ptrs(Fake(v)) is None
     assert occ._row_ptrs(t) is None and occ._row_ptrs(t.double()) is None
+
+
+def test_expert_weights_only_of_matrices_that_lie_apart():
+    # a stand-in that says it is on the GPU; nothing is launched
+    class Gpu(torch.Tensor):
+        is_cuda = property(lambda self: True)
+
+    E, I, H = 3, 16, 8
+    w = torch.zeros(E, 2 * I, H, dtype=torch.bfloat16)
+    for t, stride in ((w[:, :I], 2 * I * H), (w[:, I:], 2 * I * H), (w[:, :I].contiguous(), 0)):
+        assert occ._expert_weights("gate", t.as_subclass(Gpu), False, E, I, H) == (t.data_ptr(), 0, stride)
+    one = w[:1, :I]
+    assert occ._expert_weights("gate", one.expand(1, I, H).as_subclass(Gpu), False, 1, I, H) == (one.data_ptr(), 0, 0)
+    flat = w.view(-1)
+    for t in (one.expand(E, I, H), flat.as_strided((E, I, H), (I * H - H, H, 1)), flat.as_strided((E, I, H), (H, H, 1)),
+              w[:, ::2], flat.as_strided((E, I, H), (I * H, 1, I))):
+        with pytest.raises(ValueError):
+            occ._expert_weights("gate", t.as_subclass(Gpu), False, E, I, H)

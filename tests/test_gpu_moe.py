@@ -259,3 +259,14 @@ def test_an_infinite_weight_gives_an_infinity(T):
                 assert rows[r] != 0 and float(y[t, r]) == rows[r] * float("inf"), (t, r)
             else:
                 assert y[t, r] == clean[t, r].cpu(), (t, r)
+
+
+def test_refuses_experts_that_share_memory():
+    """An expanded weight has one matrix; the call raises before anything is launched."""
+    m = Layer(4, 64, 32, 8, 2, "bf16")
+    y = torch.full((4, 64), 5.0, dtype=BF16, device=DEV)
+    for name in ("gate", "up", "down"):
+        w = dict(m.w, **{name: m.w[name][:1].expand(8, -1, -1)})
+        with pytest.raises(ValueError):
+            occ.occ_moe(m.x, m.router, w["gate"], w["up"], w["down"], y, top_k=2, workspace=m.workspace)
+    assert (y == 5).all()
