@@ -540,6 +540,18 @@ int occ_gemm_mx4(const void *A, const void *A_scales, const void *B, const void 
                  int M, int N, int K, size_t lds_bytes, void *stream);
 
 /*
+ * occ_gemm_mx4_plan_query -- the kernel occ_gemm_mx4 takes for M x N x K on a GPU
+ * of num_cus compute units (0: the current device's, OCC_ENODEV without one).
+ */
+typedef struct occ_gemm_mx4_plan {
+  int tile_m, tile_n;  /* its tile of C; 16 x 16 and, beyond K = 8192, 16 x 32 for M <= 16 */
+  int tiles;           /* that C has */
+  int grid;            /* workgroups launched; 0 where C is empty */
+  int nontemporal;     /* 1: B is read past the caches */
+} occ_gemm_mx4_plan;
+int occ_gemm_mx4_plan_query(int M, int N, int K, int num_cus, occ_gemm_mx4_plan *plan);
+
+/*
  * occ_norm_gate -- the norms after a block and before the next one, with the
  * block's gate and the residual's scale, row by row (rows x D):
  *   n = f * r1 * w_post,  r1 = 1 / sqrt(mean(f^2) + eps)     (post != 0; else n = f)

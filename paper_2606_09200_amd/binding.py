@@ -102,6 +102,10 @@ class occ_moe_args(ctypes.Structure):
                     ("workspace_bytes", ctypes.c_size_t)]
 
 
+class occ_gemm_mx4_plan(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("tile_m", "tile_n", "tiles", "grid", "nontemporal")]
+
+
 # The same structures packed in one go, 0 for NULL: filling a ctypes structure costs a short call 1.2 us more.
 _pack_norm = struct.Struct("@6i2f8P4N7P4NPN")
 _pack_moe = struct.Struct("@7i8P3N4P2NPN")
@@ -139,6 +143,7 @@ _SIGS = {
     "occ_mx4_dequantize": [_P, _P, ctypes.c_int, ctypes.c_int, _P, ctypes.c_int, ctypes.c_size_t, _P],
     "occ_gemm_mx4": [_P, _P, _P, _P, _P, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
                      ctypes.c_size_t, _P],
+    "occ_gemm_mx4_plan_query": [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, _P],
     "occ_norm_gate": [_P, _P],
     "occ_norm_gate_bwd": [_P, _P],
     "occ_norm_gate_bwd_workspace_bytes": [ctypes.c_int, ctypes.c_int, ctypes.c_int],
@@ -657,6 +662,13 @@ def occ_gemm_mx4(A, B, C, lds_bytes=0, stream=None):
     if st:
         raise OccError(st, "occ_gemm_mx4")
     return C
+
+
+def occ_gemm_mx4_plan_query(M, N, K, num_cus=0):
+    """The kernel occ_gemm_mx4 takes on a GPU of num_cus compute units (0: the current one), as a dict."""
+    p = occ_gemm_mx4_plan()
+    _check(lib().occ_gemm_mx4_plan_query(int(M), int(N), int(K), int(num_cus), ctypes.byref(p)), "occ_gemm_mx4_plan_query")
+    return {f: getattr(p, f) for f, _ in occ_gemm_mx4_plan._fields_}
 
 
 def _param(name, t, dtype, shape):

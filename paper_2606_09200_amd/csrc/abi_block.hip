@@ -77,11 +77,15 @@ int validate_mx4_dequant(const Mx4DequantCall &c) {
   return disjoint(out, in) ? OCC_OK : OCC_EALIAS;
 }
 
-int validate_mx4_gemm(const Mx4GemmCall &c) {
-  if (!float_type(c.dtype) || !mx4_dims(c.M, c.N) || !mx4_dims(c.M, c.K)) return OCC_EINVAL;
-  if (c.M == 0 || c.N == 0) return OCC_OK;
+int validate_mx4_gemm_dims(int M, int N, int K) {
+  if (!mx4_dims(M, N) || !mx4_dims(M, K)) return OCC_EINVAL;
   // the grid of the smallest tile (32 x 64) in work-items, as above
-  if (((c.M + 31ull) / 32) * ((c.N + 63ull) / 64) >= (1ull << 23)) return OCC_EINVAL;
+  return ((M + 31ull) / 32) * ((N + 63ull) / 64) >= (1ull << 23) ? OCC_EINVAL : OCC_OK;
+}
+
+int validate_mx4_gemm(const Mx4GemmCall &c) {
+  if (!float_type(c.dtype) || validate_mx4_gemm_dims(c.M, c.N, c.K) != OCC_OK) return OCC_EINVAL;
+  if (c.M == 0 || c.N == 0) return OCC_OK;
   if (c.C == nullptr || !aligned(c.C, type_bytes(c.dtype))) return OCC_EINVAL;
   if (c.K > 0 && (!mx4_pointers(c.A, c.As) || !mx4_pointers(c.B, c.Bs))) return OCC_EINVAL;
   const Range in[] = {{c.A, OCC_MX4_CODE_BYTES(c.M, c.K)}, {c.As, OCC_MX4_SCALE_BYTES(c.M, c.K)},
@@ -215,6 +219,18 @@ int occ_gemm_mx4(const void *A, const void *A_scales, const void *B, const void 
   const occ::Mx4GemmCall c{A, A_scales, B, B_scales, C, dtype, M, N, K, lds_bytes};
   const int st = occ::validate_mx4_gemm(c);
   return st == OCC_OK ? occ::mx4_gemm_launch(c, static_cast<hipStream_t>(stream)) : st;
+}
+
+int occ_gemm_mx4_plan_query(int M, int N, int K, int num_cus, occ_gemm_mx4_plan *plan) {
+  if (plan == nullptr || num_cus < 0 || occ::validate_mx4_gemm_dims(M, N, K) != OCC_OK) return OCC_EINVAL;
+  if (num_cus == 0) {
+    const occ::DeviceInfo *di = nullptr;
+    const int st = occ::current_device_info(&di);
+    if (st != OCC_OK) return st;
+    num_cus = di->num_cus;
+  }
+  occ::mx4_gemm_plan(M, N, K, num_cus, plan);
+  return OCC_OK;
 }
 
 int occ_norm_gate(const occ_norm_args *args, void *stream) {

@@ -63,15 +63,14 @@ constexpr int kNumTiles = (int)(sizeof kTiles / sizeof kTiles[0]);
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-// The tile with the least estimated time whose LDS fits in `room`, -1 if none.
-int choose_tile(const Mx4GemmCall &c, int num_cus, int room) {
+// The tile with the least estimated time.
+int choose_tile(int M, int N, int K, int num_cus) {
   int best = -1;
   double t_best = 0;
   for (int i = 0; i < kNumTiles; ++i) {
     const Mx4Tile &t = kTiles[i];
-    if (t.lds > room) continue;
-    const double tiles = (double)ceil_div(c.M, t.bm) * ceil_div(c.N, t.bn);
-    const double k = ceil_div(c.K, 512), slots = (double)t.per_cu * num_cus, rounds = std::floor(tiles / slots);
+    const double tiles = (double)ceil_div(M, t.bm) * ceil_div(N, t.bn);
+    const double k = ceil_div(K, 512), slots = (double)t.per_cu * num_cus, rounds = std::floor(tiles / slots);
     const double us = rounds * t.round_us(slots, num_cus, k) + (tiles > rounds * slots ? t.round_us(tiles - rounds * slots, num_cus, k) : 0);
     if (best < 0 || us < t_best) {
       best = i;
@@ -102,29 +101,57 @@ int allow_lds(const void *fn, size_t lds_bytes, int own, const DeviceInfo &di) {
                                                                                                                    : OCC_EHIP;
 }
 
+// Of a call with M <= 16.
+struct SkinnyPlan {
+  int kw, xs;  // waves along K, one a k-step, up to 8; k-steps of A that each keeps
+  bool fits;   // A in registers
+  bool nt;
+  int units, grid;
+};
+SkinnyPlan skinny_plan(int N, int K, int num_cus) {
+  SkinnyPlan p{};
+  const int steps512 = ceil_div(K, 512);
+  p.kw = 1;
+  while (p.kw < 8 && p.kw < steps512) p.kw *= 2;
+  p.xs = std::max(1, ceil_div(steps512, p.kw));
+  p.fits = p.xs <= 2;
+  p.nt = p.fits && (long long)N * (long long)(OCC_MX4_KP(K) / 2) > kNtBytes;
+  p.units = ceil_div(N, p.fits ? 16 : 32);
+  p.grid = p.fits ? std::min(ceil_div(p.units, 8 / p.kw), 2 * num_cus) : p.units;
+  return p;
+}
+
 int launch_skinny(const Mx4GemmCall &c, const Mx4Operands &o, const DeviceInfo &di, hipStream_t s) {
-  // waves along K: one a k-step, up to 8
-  int kw = 1;
-  while (kw < 8 && kw < o.steps512) kw *= 2;
-  const int xs = std::max(1, ceil_div(o.steps512, kw));
-  if (xs > 2) {  // A does not fit in registers
+  const SkinnyPlan p = skinny_plan(c.N, c.K, di.num_cus);
+  if (!p.fits) {
     typedef void (*LongFn)(Mx4Operands);
     const LongFn fn = c.dtype == OCC_BF16 ? gemm_mx4_skinny_long_kernel<uint16_t> : gemm_mx4_skinny_long_kernel<float>;
     const int st = allow_lds(reinterpret_cast<const void *>(fn), c.lds_bytes, 8 * 2 * 1024, di);
     if (st != OCC_OK) return st;
-    hipLaunchKernelGGL(fn, dim3(ceil_div(c.N, 32)), dim3(512), (int)c.lds_bytes, s, o);
+    hipLaunchKernelGGL(fn, dim3(p.grid), dim3(512), (int)c.lds_bytes, s, o);
     return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
   }
-  const bool nt = (long long)c.N * o.pitch > kNtBytes;
-  const SkinnyFn fn = c.dtype == OCC_BF16 ? skinny_fn<uint16_t>(kw, xs, nt) : skinny_fn<float>(kw, xs, nt);
+  const SkinnyFn fn = c.dtype == OCC_BF16 ? skinny_fn<uint16_t>(p.kw, p.xs, p.nt) : skinny_fn<float>(p.kw, p.xs, p.nt);
   const int st = allow_lds(reinterpret_cast<const void *>(fn), c.lds_bytes, 8 * 4096 + 16 * 1024, di);
   if (st != OCC_OK) return st;
-  const int units = ceil_div(c.N, 16);
-  hipLaunchKernelGGL(fn, dim3(std::min(ceil_div(units, 8 / kw), 2 * di.num_cus)), dim3(512), (int)c.lds_bytes, s, o, units);
+  hipLaunchKernelGGL(fn, dim3(p.grid), dim3(512), (int)c.lds_bytes, s, o, p.units);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
 }
 
 }  // namespace
+
+void mx4_gemm_plan(int M, int N, int K, int num_cus, occ_gemm_mx4_plan *plan) {
+  *plan = occ_gemm_mx4_plan{};
+  if (M == 0 || N == 0) return;
+  if (M <= 16) {
+    const SkinnyPlan p = skinny_plan(N, K, num_cus);
+    *plan = occ_gemm_mx4_plan{16, p.fits ? 16 : 32, p.units, p.grid, p.nt};
+    return;
+  }
+  const Mx4Tile &t = kTiles[choose_tile(M, N, K, num_cus)];
+  const int tiles = ceil_div(M, t.bm) * ceil_div(N, t.bn);
+  *plan = occ_gemm_mx4_plan{t.bm, t.bn, tiles, tiles, 0};
+}
 
 int mx4_gemm_launch(const Mx4GemmCall &c, hipStream_t s) {
   const DeviceInfo *di = nullptr;
@@ -137,7 +164,7 @@ int mx4_gemm_launch(const Mx4GemmCall &c, hipStream_t s) {
   if (c.M <= 16) return launch_skinny(c, o, *di, s);
   if (c.lds_bytes > (size_t)di->max_lds_per_wg) return OCC_ELDS;
   // the pad keeps the tile: it lowers residency and changes nothing else, and is never clamped
-  const int id = choose_tile(c, di->num_cus, di->max_lds_per_wg);
+  const int id = choose_tile(c.M, c.N, c.K, di->num_cus);
   const Mx4Tile &t = kTiles[id];
   if ((size_t)t.lds + c.lds_bytes > (size_t)di->max_lds_per_wg) return OCC_ELDS;
   const Mx4Fn fn = c.dtype == OCC_BF16 ? t.bf16 : t.f32;

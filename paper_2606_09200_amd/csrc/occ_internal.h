@@ -109,8 +109,10 @@ struct Mx4GemmCall {
   int dtype, M, N, K;
   size_t lds_bytes;
 };
+int validate_mx4_gemm_dims(int M, int N, int K);
 int validate_mx4_gemm(const Mx4GemmCall &c);
 int mx4_gemm_launch(const Mx4GemmCall &c, hipStream_t s);
+void mx4_gemm_plan(int M, int N, int K, int num_cus, occ_gemm_mx4_plan *plan);
 
 struct NormFwd {
   int rows, D;

@@ -128,7 +128,7 @@ def check_product(C, a, b, dtype):
     assert (err <= tol).all(), (float(err.max()), np.argwhere(err > tol)[:4].tolist())
 
 
-# one row to two tiles of every kind, ragged in each dimension; K of one block to several k-steps
+# one row to many tiles, ragged in each dimension; K of one block to several k-steps (each kernel: test_gpu_mx4_tiles.py)
 PRODUCTS = [(1, 1, 1), (1, 40, 600), (3, 17, 32), (16, 33, 5000), (16, 300, 1024), (5, 8200, 2100), (2, 9001, 512),
             (17, 64, 512), (40, 70, 2000), (64, 1000, 1030), (130, 260, 257), (300, 513, 1537), (257, 100, 4100),
             (1025, 2050, 700), (2100, 2310, 300)]
