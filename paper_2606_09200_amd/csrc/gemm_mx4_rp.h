@@ -88,149 +88,146 @@ __global__ __launch_bounds__(T::NT, 2) void gemm_mx4_rp_kernel(Mx4Operands o, in
     b_rd[ks] = T::A_BYTES + (wn * T::FN * 16 + l16) * T::ROW + mx4_rp_chunk<T>(l16, ks * 4 + g) * 16;
   }
 
-  for (int t = blockIdx.x; t < ntiles; t += gridDim.x) {
-    int tm, tn;
-    tile_coords<8>(xcd_remap(t, ntiles), tiles_m, tiles_n, tm, tn);
-    const int m0 = tm * T::BM;
-    const int n0 = tn * T::BN;
-    const uint32_t a_bytes = (uint32_t)min(T::BM, M - m0) * P, b_bytes = (uint32_t)min(T::BN, N - n0) * P;
-    const uint8_t *Am = o.A + (size_t)m0 * P, *Bn = o.B + (size_t)n0 * P;
-    const uint8_t *Sa = o.As + (size_t)(m0 >> 4) * P, *Sb = o.Bs + (size_t)(n0 >> 4) * P;
-    const int at = min(T::BM / 16, (M - m0 + 15) >> 4), bt = min(T::BN / 16, (N - n0 + 15) >> 4);  // tiles that exist
-    // DMA pass p of k-step kt (A's, B's, then scales) into stage `slot`
-    auto issue_pass = [&](int kt, uint32_t slot, int p) {
-      const uint32_t k0 = (uint32_t)kt * T::ROW;
-      const bool in = kt < nk;
-      if (p < T::A_LOADS) {
-        const i32x4 rs = make_rsrc(Am + k0, in ? a_bytes - k0 : 0u);
-        lds_dma16(rs, slot + wave_lds + (uint32_t)(p * T::NT * 16), lane_off + (uint32_t)p * pass_step);
-      } else if (p < T::A_LOADS + T::B_LOADS) {
-        const int q = p - T::A_LOADS;
-        const i32x4 rs = make_rsrc(Bn + k0, in ? b_bytes - k0 : 0u);
-        lds_dma16(rs, slot + wave_lds + (uint32_t)(T::A_BYTES + q * T::NT * 16), lane_off + (uint32_t)q * pass_step);
-      } else if constexpr (T::HALF) {
-        const int x = ((p - T::A_LOADS - T::B_LOADS) * T::WAVES + wave) * 4;  // first of four scale tiles, A's then B's
-        const bool b = x >= T::BM / 16;
-        const uint32_t y = (uint32_t)(b ? x - T::BM / 16 : x), s0 = (uint32_t)(kt >> 1) * 256u;
-        const i32x4 rs = make_rsrc((b ? Sb : Sa) + s0, in ? (uint32_t)(b ? bt : at) * P - s0 : 0u);
-        lds_dma16(rs, slot + (uint32_t)(T::CODE_BYTES + x * 256), (y + g) * P + (uint32_t)l16 * 16u);
-      } else {
-        const int x = (p - T::A_LOADS - T::B_LOADS) * T::WAVES + wave;  // scale tile, A's then B's
-        const bool b = x >= T::BM / 16;
-        const int y = b ? x - T::BM / 16 : x;
-        const bool exists = in && y < (b ? bt : at);
-        const i32x4 rs = make_rsrc((b ? Sb : Sa) + (exists ? (size_t)y * P + k0 : 0), exists ? 256u : 0u);
-        lds_dma4(rs, slot + (uint32_t)(T::CODE_BYTES + x * 256), (uint32_t)lane * 4u);
-      }
-    };
-
-    f32x4 acc[T::FM][T::FN];
-#pragma unroll
-    for (int i = 0; i < T::FM; ++i)
-#pragma unroll
-      for (int j = 0; j < T::FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-    u32x4 af[2][T::GS][T::FM], bf[2][T::GS][T::FN];
-    int as[T::FM], bs[T::FN], as_next[T::FM], bs_next[T::FN];
-    constexpr int NR = T::GS * (T::FM + T::FN);   // fragments of a group
-    constexpr int NM = T::GS * T::FM * T::FN;     // MFMAs of a group
-    auto read_frag = [&](const unsigned char *cur, int gi, int set, int x) {
-      const int s = x / (T::FM + T::FN), y = x % (T::FM + T::FN), ks = gi * T::GS + s;
-      if (y < T::FM) af[set][s][y] = *reinterpret_cast<const u32x4 *>(cur + a_rd[ks] + y * 16 * T::ROW);
-      else bf[set][s][y - T::FM] = *reinterpret_cast<const u32x4 *>(cur + b_rd[ks] + (y - T::FM) * 16 * T::ROW);
-    };
-    auto read_scales = [&](const unsigned char *cur) {
-      const unsigned char *sc = cur + T::CODE_BYTES + lane * 4;
-#pragma unroll
-      for (int i = 0; i < T::FM; ++i) as_next[i] = *reinterpret_cast<const int *>(sc + (wm * T::FM + i) * 256);
-#pragma unroll
-      for (int j = 0; j < T::FN; ++j)
-        bs_next[j] = *reinterpret_cast<const int *>(sc + (T::BM / 16 + wn * T::FN + j) * 256);
-    };
-    auto mfma = [&](int byte0, int gi, int set, int x) {
-      const int s = x / (T::FM * T::FN), i = x / T::FN % T::FM, j = x % T::FN;
-      switch (byte0 + gi * T::GS + s) {  // a constant once unrolled
-        case 0: acc[i][j] = mfma_mx4<0>(bf[set][s][j], af[set][s][i], acc[i][j], bs[j], as[i]); break;
-        case 1: acc[i][j] = mfma_mx4<1>(bf[set][s][j], af[set][s][i], acc[i][j], bs[j], as[i]); break;
-        case 2: acc[i][j] = mfma_mx4<2>(bf[set][s][j], af[set][s][i], acc[i][j], bs[j], as[i]); break;
-        default: acc[i][j] = mfma_mx4<3>(bf[set][s][j], af[set][s][i], acc[i][j], bs[j], as[i]); break;
-      }
-    };
-    auto slot_of = [&](int s) { return lds0 + (uint32_t)s * T::STAGE_BYTES; };
-    auto publish = [&]() {  // this wave's reads are done; then every wave's, and its DMA has landed
-      __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
-      __builtin_amdgcn_sched_barrier(0);
-      __builtin_amdgcn_s_barrier();
-      __builtin_amdgcn_sched_barrier(0);
-    };
-
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-#pragma unroll
-      for (int p = 0; p < T::LOADS; ++p) issue_pass(s, slot_of(s), p);
-    wait_vmcnt<(S - 1) * T::LOADS>();
-    publish();
-    read_scales(smem);
-#pragma unroll
-    for (int x = 0; x < NR; ++x) read_frag(smem, 0, 0, x);
-    int stage = 0;  // stage of the k-step being multiplied
-    auto step = [&](int kt, int set0, int byte0) {
-      const int next = stage + 1 == S ? 0 : stage + 1;
-      const unsigned char *cur = smem + stage * T::STAGE_BYTES, *nxt = smem + next * T::STAGE_BYTES;
-      const uint32_t slot = slot_of(stage);
-#pragma unroll
-      for (int i = 0; i < T::FM; ++i) as[i] = as_next[i];
-#pragma unroll
-      for (int j = 0; j < T::FN; ++j) bs[j] = bs_next[j];
-#pragma unroll
-      for (int gi = 0; gi < T::NG; ++gi) {
-        const int set = (set0 + gi) & 1;
-        const bool last = gi + 1 == T::NG;
-        if (last) {
-          wait_vmcnt<(S - 2) * T::LOADS>();
-          publish();
-          read_scales(nxt);
-        }
-#pragma unroll
-        for (int x = 0; x < NM; ++x) {
-          mfma(byte0, gi, set, x);
-          // the reads behind the first half of the MFMAs, the DMA behind all of them
-#pragma unroll
-          for (int y = 0; y < NR; ++y)
-            if (y * (NM / 2) / NR == x) read_frag(last ? nxt : cur, last ? 0 : gi + 1, set ^ 1, y);
-#pragma unroll
-          for (int p = 0; p < T::LOADS; ++p)
-            if (last && p * NM / T::LOADS == x) issue_pass(kt + S, slot, p);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
-      stage = next;
-    };
-    if constexpr (T::NG == 1 || T::HALF) {  // the register sets or the scales' bytes alternate
-      int kt = 0;
-      for (; kt + 1 < nk; kt += 2) {
-        step(kt, 0, 0);
-        step(kt + 1, T::NG == 1, T::HALF ? 2 : 0);
-      }
-      if (kt < nk) step(kt, 0, 0);
+  int tm, tn;
+  tile_coords<8>(xcd_remap(blockIdx.x, ntiles), tiles_m, tiles_n, tm, tn);
+  const int m0 = tm * T::BM;
+  const int n0 = tn * T::BN;
+  const uint32_t a_bytes = (uint32_t)min(T::BM, M - m0) * P, b_bytes = (uint32_t)min(T::BN, N - n0) * P;
+  const uint8_t *Am = o.A + (size_t)m0 * P, *Bn = o.B + (size_t)n0 * P;
+  const uint8_t *Sa = o.As + (size_t)(m0 >> 4) * P, *Sb = o.Bs + (size_t)(n0 >> 4) * P;
+  const int at = min(T::BM / 16, (M - m0 + 15) >> 4), bt = min(T::BN / 16, (N - n0 + 15) >> 4);  // tiles that exist
+  // DMA pass p of k-step kt (A's, B's, then scales) into stage `slot`
+  auto issue_pass = [&](int kt, uint32_t slot, int p) {
+    const uint32_t k0 = (uint32_t)kt * T::ROW;
+    const bool in = kt < nk;
+    if (p < T::A_LOADS) {
+      const i32x4 rs = make_rsrc(Am + k0, in ? a_bytes - k0 : 0u);
+      lds_dma16(rs, slot + wave_lds + (uint32_t)(p * T::NT * 16), lane_off + (uint32_t)p * pass_step);
+    } else if (p < T::A_LOADS + T::B_LOADS) {
+      const int q = p - T::A_LOADS;
+      const i32x4 rs = make_rsrc(Bn + k0, in ? b_bytes - k0 : 0u);
+      lds_dma16(rs, slot + wave_lds + (uint32_t)(T::A_BYTES + q * T::NT * 16), lane_off + (uint32_t)q * pass_step);
+    } else if constexpr (T::HALF) {
+      const int x = ((p - T::A_LOADS - T::B_LOADS) * T::WAVES + wave) * 4;  // first of four scale tiles, A's then B's
+      const bool b = x >= T::BM / 16;
+      const uint32_t y = (uint32_t)(b ? x - T::BM / 16 : x), s0 = (uint32_t)(kt >> 1) * 256u;
+      const i32x4 rs = make_rsrc((b ? Sb : Sa) + s0, in ? (uint32_t)(b ? bt : at) * P - s0 : 0u);
+      lds_dma16(rs, slot + (uint32_t)(T::CODE_BYTES + x * 256), (y + g) * P + (uint32_t)l16 * 16u);
     } else {
-      for (int kt = 0; kt < nk; ++kt) step(kt, 0, 0);
+      const int x = (p - T::A_LOADS - T::B_LOADS) * T::WAVES + wave;  // scale tile, A's then B's
+      const bool b = x >= T::BM / 16;
+      const int y = b ? x - T::BM / 16 : x;
+      const bool exists = in && y < (b ? bt : at);
+      const i32x4 rs = make_rsrc((b ? Sb : Sa) + (exists ? (size_t)y * P + k0 : 0), exists ? 256u : 0u);
+      lds_dma4(rs, slot + (uint32_t)(T::CODE_BYTES + x * 256), (uint32_t)lane * 4u);
     }
-    wait_vmcnt<0>();  // the DMA issued past the last k-step, before the stages get other use
-    publish();
+  };
 
-    typedef TileOut<T::BN, typename T::Out> Out;
-    static_assert(T::BM * Out::PITCH <= T::LDS_BYTES, "a tile of C");
-    int el = lane;
-    asm volatile("" : "+v"(el));  // keeps the addresses below out of the k-loop's registers
+  f32x4 acc[T::FM][T::FN];
 #pragma unroll
-    for (int i = 0; i < T::FM; ++i)
+  for (int i = 0; i < T::FM; ++i)
 #pragma unroll
-      for (int j = 0; j < T::FN; ++j) Out::put(smem, (wm * T::FM + i) * 16, (wn * T::FN + j) * 16, el, acc[i][j]);
-    __syncthreads();
-    Out::template store<T::BM, T::NT>(smem, static_cast<typename T::Out *>(o.C), M, N, m0, n0);
-    __syncthreads();
+    for (int j = 0; j < T::FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  u32x4 af[2][T::GS][T::FM], bf[2][T::GS][T::FN];
+  int as[T::FM], bs[T::FN], as_next[T::FM], bs_next[T::FN];
+  constexpr int NR = T::GS * (T::FM + T::FN);   // fragments of a group
+  constexpr int NM = T::GS * T::FM * T::FN;     // MFMAs of a group
+  auto read_frag = [&](const unsigned char *cur, int gi, int set, int x) {
+    const int s = x / (T::FM + T::FN), y = x % (T::FM + T::FN), ks = gi * T::GS + s;
+    if (y < T::FM) af[set][s][y] = *reinterpret_cast<const u32x4 *>(cur + a_rd[ks] + y * 16 * T::ROW);
+    else bf[set][s][y - T::FM] = *reinterpret_cast<const u32x4 *>(cur + b_rd[ks] + (y - T::FM) * 16 * T::ROW);
+  };
+  auto read_scales = [&](const unsigned char *cur) {
+    const unsigned char *sc = cur + T::CODE_BYTES + lane * 4;
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i) as_next[i] = *reinterpret_cast<const int *>(sc + (wm * T::FM + i) * 256);
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j)
+      bs_next[j] = *reinterpret_cast<const int *>(sc + (T::BM / 16 + wn * T::FN + j) * 256);
+  };
+  auto mfma = [&](int byte0, int gi, int set, int x) {
+    const int s = x / (T::FM * T::FN), i = x / T::FN % T::FM, j = x % T::FN;
+    switch (byte0 + gi * T::GS + s) {  // a constant once unrolled
+      case 0: acc[i][j] = mfma_mx4<0>(bf[set][s][j], af[set][s][i], acc[i][j], bs[j], as[i]); break;
+      case 1: acc[i][j] = mfma_mx4<1>(bf[set][s][j], af[set][s][i], acc[i][j], bs[j], as[i]); break;
+      case 2: acc[i][j] = mfma_mx4<2>(bf[set][s][j], af[set][s][i], acc[i][j], bs[j], as[i]); break;
+      default: acc[i][j] = mfma_mx4<3>(bf[set][s][j], af[set][s][i], acc[i][j], bs[j], as[i]); break;
+    }
+  };
+  auto slot_of = [&](int s) { return lds0 + (uint32_t)s * T::STAGE_BYTES; };
+  auto publish = [&]() {  // this wave's reads are done; then every wave's, and its DMA has landed
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+#pragma unroll
+  for (int s = 0; s < S; ++s)
+#pragma unroll
+    for (int p = 0; p < T::LOADS; ++p) issue_pass(s, slot_of(s), p);
+  wait_vmcnt<(S - 1) * T::LOADS>();
+  publish();
+  read_scales(smem);
+#pragma unroll
+  for (int x = 0; x < NR; ++x) read_frag(smem, 0, 0, x);
+  int stage = 0;  // stage of the k-step being multiplied
+  auto step = [&](int kt, int set0, int byte0) {
+    const int next = stage + 1 == S ? 0 : stage + 1;
+    const unsigned char *cur = smem + stage * T::STAGE_BYTES, *nxt = smem + next * T::STAGE_BYTES;
+    const uint32_t slot = slot_of(stage);
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i) as[i] = as_next[i];
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) bs[j] = bs_next[j];
+#pragma unroll
+    for (int gi = 0; gi < T::NG; ++gi) {
+      const int set = (set0 + gi) & 1;
+      const bool last = gi + 1 == T::NG;
+      if (last) {
+        wait_vmcnt<(S - 2) * T::LOADS>();
+        publish();
+        read_scales(nxt);
+      }
+#pragma unroll
+      for (int x = 0; x < NM; ++x) {
+        mfma(byte0, gi, set, x);
+        // the reads behind the first half of the MFMAs, the DMA behind all of them
+#pragma unroll
+        for (int y = 0; y < NR; ++y)
+          if (y * (NM / 2) / NR == x) read_frag(last ? nxt : cur, last ? 0 : gi + 1, set ^ 1, y);
+#pragma unroll
+        for (int p = 0; p < T::LOADS; ++p)
+          if (last && p * NM / T::LOADS == x) issue_pass(kt + S, slot, p);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    stage = next;
+  };
+  if constexpr (T::NG == 1 || T::HALF) {  // the register sets or the scales' bytes alternate
+    int kt = 0;
+    for (; kt + 1 < nk; kt += 2) {
+      step(kt, 0, 0);
+      step(kt + 1, T::NG == 1, T::HALF ? 2 : 0);
+    }
+    if (kt < nk) step(kt, 0, 0);
+  } else {
+    for (int kt = 0; kt < nk; ++kt) step(kt, 0, 0);
   }
+  wait_vmcnt<0>();  // the DMA issued past the last k-step, before the stages get other use
+  publish();
+
+  typedef TileOut<T::BN, typename T::Out> Out;
+  static_assert(T::BM * Out::PITCH <= T::LDS_BYTES, "a tile of C");
+  int el = lane;
+  asm volatile("" : "+v"(el));  // keeps the addresses below out of the k-loop's registers
+#pragma unroll
+  for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) Out::put(smem, (wm * T::FM + i) * 16, (wn * T::FN + j) * 16, el, acc[i][j]);
+  __syncthreads();
+  Out::template store<T::BM, T::NT>(smem, static_cast<typename T::Out *>(o.C), M, N, m0, n0);
 }
 
 }  // namespace

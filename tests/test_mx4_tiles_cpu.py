@@ -41,3 +41,10 @@ def test_plan_of_odd_calls():
         assert e.value.status == occ.OCC_EINVAL
     with pytest.raises(occ.OccError):
         plan(5, 5, 64, -1)
+
+
+def test_a_workgroup_has_one_tile():
+    """The tiled kernels have no loop over tiles."""
+    for tile, M, N, K in tiles.CASES:
+        p = plan(M, N, K)
+        assert p["grid"] == p["tiles"] or tile == (16, 16)
