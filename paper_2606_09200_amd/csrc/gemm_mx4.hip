@@ -115,7 +115,7 @@ SkinnyPlan skinny_plan(int N, int K, int num_cus) {
   while (p.kw < 8 && p.kw < steps512) p.kw *= 2;
   p.xs = std::max(1, ceil_div(steps512, p.kw));
   p.fits = p.xs <= 2;
-  p.nt = p.fits && (long long)N * (long long)(OCC_MX4_KP(K) / 2) > kNtBytes;
+  p.nt = p.fits && p.kw == 8 && (long long)N * (long long)(OCC_MX4_KP(K) / 2) > kNtBytes;
   p.units = ceil_div(N, p.fits ? 16 : 32);
   p.grid = p.fits ? std::min(ceil_div(p.units, 8 / p.kw), 2 * num_cus) : p.units;
   return p;

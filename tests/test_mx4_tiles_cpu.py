@@ -48,3 +48,9 @@ def test_a_workgroup_has_one_tile():
     for tile, M, N, K in tiles.CASES:
         p = plan(M, N, K)
         assert p["grid"] == p["tiles"] or tile == (16, 16)
+
+
+def test_plan_names_the_loads_that_are_made():
+    """Short rows are read through the caches, whatever their number."""
+    assert plan(16, 40000, 2048)["nontemporal"] == 0 and plan(16, 40000, 2049)["nontemporal"] == 1
+    assert plan(16, 40000, 8193)["nontemporal"] == 0
