@@ -1,6 +1,7 @@
 // Public C entry points: argument validation (host only, before any HIP
 // call), device facts, and dispatch to the kernels.
 #include "occ_internal.h"
+#include "once.h"
 
 #include <string.h>
 
@@ -75,10 +76,11 @@ int validate_permute(const void *src, const void *dst, const int32_t *perm, int 
 }
 
 const DeviceInfo &device_info(int device) {
+  static Once filled[kMaxDevices];
   DeviceInfo &d = g_info[device];
-  if (!d.ok) {
+  const bool ok = filled[device].run([&] {
     hipDeviceProp_t prop;
-    if (hipGetDeviceProperties(&prop, device) != hipSuccess) return d;
+    if (hipGetDeviceProperties(&prop, device) != hipSuccess) return false;
     int v = 0;
     d.num_cus = prop.multiProcessorCount;
     d.lds_per_cu = hipDeviceGetAttribute(&v, hipDeviceAttributeMaxSharedMemoryPerMultiprocessor, device) == hipSuccess ? v : 0;
@@ -86,8 +88,10 @@ const DeviceInfo &device_info(int device) {
     d.clock_khz = hipDeviceGetAttribute(&v, hipDeviceAttributeClockRate, device) == hipSuccess ? v : 0;
     d.gfx950 = strncmp(prop.gcnArchName, "gfx950", 6) == 0;
     d.ok = d.num_cus > 0 && d.max_lds_per_wg > 0;
-  }
-  return d;
+    return d.ok != 0;
+  });
+  static const DeviceInfo unknown{};
+  return ok ? d : unknown;
 }
 
 int current_device_info(const DeviceInfo **out) {

@@ -25,6 +25,7 @@
 #include "gemm_skinny_kn.h"
 #include "gemm_skinny_ldsb.h"
 #include "gemm_tiled.h"
+#include "once.h"
 
 #include <algorithm>
 #include <cmath>
@@ -411,15 +412,13 @@ int gemm_launch(const GemmCall &c, hipStream_t s) {
     const bool nt = v->fn_nt != nullptr && tiles_m == 1 && b_exceeds_llc(c.N, c.K);
     const bool through = c.trace.release && v->fn_through != nullptr;
     const TiledFn fn = nt ? v->fn_nt : through ? v->fn_through : v->fn;
-    static bool attr_set[kMaxDevices][kMaxVariantId + 1][2] = {};
+    static Once attr_set[kMaxDevices][kMaxVariantId + 1][2];
     const int form = nt || through;  // a variant has at most one of the two
-    if (!attr_set[dev][v->id][form]) {
-      if (hipFuncSetAttribute(reinterpret_cast<const void *>(fn),
-                              hipFuncAttributeMaxDynamicSharedMemorySize,
-                              p.max_lds_per_wg) != hipSuccess)
-        return OCC_EHIP;
-      attr_set[dev][v->id][form] = true;
-    }
+    if (!attr_set[dev][v->id][form].run([&] {
+          return hipFuncSetAttribute(reinterpret_cast<const void *>(fn), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                     p.max_lds_per_wg) == hipSuccess;
+        }))
+      return OCC_EHIP;
     hipLaunchKernelGGL(fn, dim3(p.grid), dim3(v->threads), dyn, s, A, B, C, c.M, c.N, c.K,
                        tiles_m, tiles_n, c.priority, c.trace);
   } else {
@@ -427,13 +426,12 @@ int gemm_launch(const GemmCall &c, hipStream_t s) {
     const bool through = c.trace.release && v->skinny_through != nullptr;
     const SkinnyFn fn = through ? v->skinny_through : v->skinny;
     const int width = v->bn >= 128 ? 0 : v->bn >= 64 ? 1 : 2;  // variant 33's forms
-    static bool attr_set_skinny[kMaxDevices][kMaxVariantId + 1][2][3] = {};
-    if (c.lds_bytes > 0 && !attr_set_skinny[dev][v->id][through][width]) {
-      if (hipFuncSetAttribute(reinterpret_cast<const void *>(fn), hipFuncAttributeMaxDynamicSharedMemorySize,
-                              p.max_lds_per_wg - v->lds) != hipSuccess)
-        return OCC_EHIP;
-      attr_set_skinny[dev][v->id][through][width] = true;
-    }
+    static Once attr_set_skinny[kMaxDevices][kMaxVariantId + 1][2][3];
+    if (c.lds_bytes > 0 && !attr_set_skinny[dev][v->id][through][width].run([&] {
+          return hipFuncSetAttribute(reinterpret_cast<const void *>(fn), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                     p.max_lds_per_wg - v->lds) == hipSuccess;
+        }))
+      return OCC_EHIP;
     hipLaunchKernelGGL(fn, dim3(p.grid), dim3(v->threads), (int)c.lds_bytes, s, A, B, C, c.M, c.N, c.K,
                        c.priority, c.trace);
   }

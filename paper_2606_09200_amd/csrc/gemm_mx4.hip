@@ -7,6 +7,7 @@
 #include "gemm_mx4_pp.h"
 #include "gemm_mx4_rp.h"
 #include "gemm_mx4_skinny.h"
+#include "once.h"
 
 #include <algorithm>
 #include <cmath>
@@ -171,14 +172,12 @@ int mx4_gemm_launch(const Mx4GemmCall &c, hipStream_t s) {
   // the dynamic-LDS limit is a per-device attribute of each kernel: set once
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return OCC_ENODEV;
-  static bool attr_set[kMaxDevices][kNumTiles][2] = {};
-  bool &set = attr_set[dev][id][c.dtype == OCC_F32];
-  if (!set) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void *>(fn), hipFuncAttributeMaxDynamicSharedMemorySize,
-                            di->max_lds_per_wg) != hipSuccess)
-      return OCC_EHIP;
-    set = true;
-  }
+  static Once attr_set[kMaxDevices][kNumTiles][2];
+  if (!attr_set[dev][id][c.dtype == OCC_F32].run([&] {
+        return hipFuncSetAttribute(reinterpret_cast<const void *>(fn), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                   di->max_lds_per_wg) == hipSuccess;
+      }))
+    return OCC_EHIP;
   const int tm = ceil_div(c.M, t.bm), tn = ceil_div(c.N, t.bn);
   hipLaunchKernelGGL(fn, dim3(tm * tn), dim3(t.threads), t.lds + (int)c.lds_bytes, s, o, tm, tn);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
