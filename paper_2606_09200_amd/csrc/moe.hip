@@ -16,6 +16,7 @@
 // of 64 experts of 4096 x 2048 MX4: 40 us (9, 18, 12; 3.9 and 3.0 TB/s), latency.
 #include "block_util.h"
 #include "mx4.h"
+#include "once.h"
 
 #include <algorithm>
 #include <cmath>
@@ -23,7 +24,7 @@
 namespace occ {
 namespace {
 
-constexpr int kMaxTokens = 64, kMaxTopK = 16, kMaxExperts = 512;
+constexpr int kMaxTokens = 64, kMaxTopK = 16, kMaxExperts = 512, kMaxDevices = 64;
 constexpr int kThreads = 512, kWaves = kThreads / 64;
 constexpr uint32_t kNowhere = 0x80000000u;  // a byte offset beyond every descriptor
 
@@ -834,10 +835,18 @@ int moe_launch(const occ_moe_args &a, hipStream_t s) {
   c.hidden = reinterpret_cast<uint16_t *>(ws + l.hidden);
   c.sums = reinterpret_cast<float *>(ws + l.sums);
   const int tb = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
-  const MoeFn route = a.experts <= 64 ? route_fn<1>(tb) : a.experts <= 128 ? route_fn<2>(tb) : route_fn<8>(tb);
+  const int per = a.experts <= 64 ? 0 : a.experts <= 128 ? 1 : 2;
+  const MoeFn route = per == 0 ? route_fn<1>(tb) : per == 1 ? route_fn<2>(tb) : route_fn<8>(tb);
   const int logits = a.tokens * ((a.experts + 15) / 16 * 16) * 4;
-  if (logits > 32768 &&  // with the kernel's own 30 KB past what a launch may have unasked
-      hipFuncSetAttribute(reinterpret_cast<const void *>(route), hipFuncAttributeMaxDynamicSharedMemorySize, logits) != hipSuccess)
+  // with the kernel's own 30 KB past what a launch may have unasked; the limit is the kernel's for all host threads, so
+  // it is what any call needs
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return OCC_ENODEV;
+  static Once limit_set[kMaxDevices][3][3];
+  if (!limit_set[dev][per][tb >> 1].run([&] {
+        return hipFuncSetAttribute(reinterpret_cast<const void *>(route), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                   kMaxTokens * kMaxExperts * 4) == hipSuccess;
+      }))
     return OCC_EHIP;
   hipLaunchKernelGGL(route, dim3((a.experts + 15) / 16 * l.slices), dim3(kRouteThreads), logits, s, c);
   if (hipGetLastError() != hipSuccess) return OCC_EHIP;

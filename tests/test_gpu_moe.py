@@ -270,3 +270,29 @@ def test_refuses_experts_that_share_memory():
         with pytest.raises(ValueError):
             occ.occ_moe(m.x, m.router, w["gate"], w["up"], w["down"], y, top_k=2, workspace=m.workspace)
     assert (y == 5).all()
+
+
+def test_host_threads_with_layers_of_different_sizes():
+    """The router's logits of the two are 128 and 36 KiB of LDS: each thread's calls give what they give alone."""
+    import threading
+    layers = [Layer(64, 64, 32, 512, 2, "bf16", seed=1), Layer(64, 72, 40, 140, 2, "bf16", seed=2)]
+    want = [m.run() for m in layers]
+    streams, bad = [torch.cuda.Stream() for _ in layers], []
+    torch.cuda.synchronize()
+
+    def work(m, s, expected):
+        try:
+            with torch.cuda.stream(s):
+                for _ in range(50):
+                    if not all(torch.equal(a, b) for a, b in zip(m.run(stream=s), expected)):
+                        bad.append("other results")
+        except Exception as e:   # a refused launch among them
+            bad.append(repr(e))
+
+    threads = [threading.Thread(target=work, args=a) for a in zip(layers, streams, want)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not bad, bad[:3]

@@ -56,3 +56,15 @@ def test_launchers_keep_no_plain_flags():
     for path in sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "*.h"))):
         plain = re.findall(r"^\s+static (?:bool|int|float|double|char|void \*)\s*\w+(?:\[[^\]]*\])*\s*(?:=[^(]*)?;", open(path).read(), re.M)
         assert not plain, (path, plain)
+
+
+def test_dynamic_lds_limits_do_not_depend_on_the_call():
+    """The limit is the kernel's, for every host thread: one call's own size would lower what another is about to launch
+    with.  Only device facts, constants and a kernel's own bytes may be in it."""
+    asked = []
+    for path in sorted(glob.glob(os.path.join(CSRC, "*.hip"))):
+        for m in re.finditer(r"hipFuncAttributeMaxDynamicSharedMemorySize,\s*([^;]*?)\)\s*(?:==|!=) hipSuccess", open(path).read()):
+            asked.append((os.path.basename(path), " ".join(m.group(1).split())))
+    known = {"di->max_lds_per_wg", "p.max_lds_per_wg", "p.max_lds_per_wg - v->lds", "di.max_lds_per_wg - own",
+             "kMaxTokens * kMaxExperts * 4", "lds"}   # lds: the wide norms' 2 x 64 KiB
+    assert len(asked) >= 6 and {a for _, a in asked} <= known, asked
