@@ -15,6 +15,7 @@
 // products, 6.4 and 5.8 TB/s).  37 tokens, 60 of 2504 x 1400: 220 us (12, 138, 70; 5.2 TB/s).  One token, 8
 // of 64 experts of 4096 x 2048 MX4: 40 us (9, 18, 12; 3.9 and 3.0 TB/s), latency.
 #include "block_util.h"
+#include "moe_extent.h"
 #include "mx4.h"
 #include "once.h"
 
@@ -282,10 +283,9 @@ struct Rows16 {
   bool whole;                // pieces are whole cache lines
   __device__ __forceinline__ Rows16(const MoeMatrix &m, int e, int row0, int rows, int cols, int lane) {
     pitch = MX ? (uint32_t)(OCC_MX4_KP(cols) / 2) : (uint32_t)cols * 2u;
-    r = rsrc_of(static_cast<const uint8_t *>(m.w) + (size_t)e * m.stride + (size_t)row0 * pitch,
-                (uint32_t)min(16, rows - row0) * pitch);
-    // row0 = rows (no rows) may lie past the last scale tile
-    if constexpr (MX) rs = rsrc_of(m.scales + (size_t)e * m.scale_stride + (size_t)(row0 >> 4) * pitch, row0 < rows ? pitch : 0u);
+    const MoeExtent w = moe_rows_extent(pitch, row0, rows), s = moe_scales_extent(pitch, row0, rows);
+    r = rsrc_of(static_cast<const uint8_t *>(m.w) + (size_t)e * m.stride + w.at, w.bytes);
+    if constexpr (MX) rs = rsrc_of(m.scales + (size_t)e * m.scale_stride + s.at, s.bytes);
     at = (uint32_t)(lane / CH) * pitch + (uint32_t)(lane % CH) * 16u;
     left = pitch - (uint32_t)(lane % CH) * 16u;
     whole = pitch % 128u == 0u && ((uintptr_t)m.w + m.stride) % 128u == 0u && m.stride % 128u == 0u;
@@ -452,7 +452,7 @@ __global__ __launch_bounds__(kThreads, !MX && AHEAD > 1 ? 2 : 4) void moe_up_ker
   const auto rx = rsrc_of(c.x, ((uint32_t)(c.T - 1) * (uint32_t)c.ld_x + (uint32_t)c.H) * 2u);
   const int units = (c.H + Rows::COLS - 1) / Rows::COLS;
   const int u0 = kw, u1 = units;  // every kws-th, so that the waves together read whole rows
-  auto row_of = [&](uint32_t task) { return min(((int)(task % groups) * c.rbs + rsub) * 16, c.I); };  // I: no rows
+  auto row_of = [&](uint32_t task) { return moe_block_row((int)(task % groups) * c.rbs * 16, rsub, c.I); };
   Unit<MX> wg[AHEAD], wu[AHEAD];
   struct Cursor {  // the unit to load next
     uint32_t task;
@@ -608,7 +608,7 @@ __global__ __launch_bounds__(kThreads, AHEAD == 1 ? 4 : 2) void moe_down_kernel(
     if (cur.left == 0) return;
     const int e = (int)expert_at(c, cur.a).id;
     Rows(c.down, e, cur.row0, c.H, c.I, lane).load(q0, cur.k, lane);
-    Rows(c.down, e, min(cur.row0 + 16, c.H), c.H, c.I, lane).load(q1, cur.k, lane);
+    Rows(c.down, e, moe_block_row(cur.row0, 1, c.H), c.H, c.I, lane).load(q1, cur.k, lane);
     if (++cur.k == units) cur.k = 0, ++cur.a;
     if (--cur.to_end == 0) cur.a = cur.a0, cur.k = cur.k0;
     if (--cur.left == 0) enter(cur.task + gridDim.x);

@@ -93,7 +93,8 @@ def test_layer_at_the_ends_of_its_splits(T, H, I, E, k, kind):
     test_layer(T, H, I, E, k, kind)
 
 
-# the last expert's last task has blocks past its rows, in both products: nothing is read for them
+# the last expert's last task has blocks past its rows, in both products: what follows them reaches no output (that
+# nothing of it is read either is test_moe_extent_cpu.py's)
 @pytest.mark.parametrize("T,H,I,E,k", [(2, 48, 80, 3, 3), (18, 1072, 208, 2, 2)])
 def test_blocks_past_the_last_experts_rows(T, H, I, E, k):
     m = Layer(T, H, I, E, k, "mx4", seed=11)
