@@ -48,8 +48,9 @@ using Rp64x64 = Mx4Rp<64, 64, 2, 2, 512, 4, 4, OUT>;
 template <class OUT>
 using Rp32x64 = Mx4Rp<32, 64, 2, 2, 512, 4, 4, OUT>;
 
-// Fitted to 39 shapes from 17 x 512 x 512 to 16384 x 8192 x 512; the tile chosen is within 8 % of
-// the best one or half a microsecond.  128x128 at two workgroups a CU passes 256x256 where K is short
+// Fitted to shapes from 17 x 512 x 512 to 16384 x 8192 x 512.  They hold no bytes: where few rows read a large
+// B once (64 x 28672 x 8192: 16 us by them, 31 measured, of which B's bytes are 21) every estimate is too low,
+// and the choice rests on the tiles' order alone.  128x128 at two workgroups a CU passes 256x256 where K is short
 // (16384 x 8192 x 512: 84 us, 92) or the larger tiles leave CUs idle (2500 x 2500 x 8192:
 // 31, 46; 3001 x 2504 x 5003: 25, 33), and is passed by it on the large ones (8192^3: 269, 234).
 const Mx4Tile kTiles[] = {

@@ -23,11 +23,11 @@ namespace {
 //
 // K is padded by the format: rows of codes have whole 512-column pieces of zeros.
 //
-// 8192^3: 234 to 260 us, 4.2 to 4.7 PFLOP/s; K = 32768: 4.9.  Power bounds it: the board's cap leaves 1.8 to 1.9
-// GHz (operands of zeros run 1.4 times as fast), at which the matrix pipes are 57 % busy.  Next are the
-// reads and barriers between the phases (with a quarter of the MFMAs the loop still takes two thirds of
-// its time; LDS itself is 30 % busy) and a tile's first loads and last stores, 10 us of 60.  Memory
-// is not: with every k-step in the L2 it gains 3 %.
+// 8192^3: 234 to 260 us, 4.2 to 4.7 PFLOP/s; K = 32768: 5.1.  Two bounds multiply.  Power: near the board's cap the
+// clock is 1.84 GHz (operands of zeros run at 2.39, 1.33 times as fast).  And at either clock the matrix
+// pipes are 58 % busy: the reads and barriers between the phases (with a quarter of the MFMAs the loop still
+// takes two thirds of its time; LDS itself is 30 % busy) and a tile's first loads and last stores, 10 us of
+// 60.  Memory is no bound: with every k-step in the L2 it gains 3 %.
 template <class OUT>
 struct Mx4Pp {
   typedef OUT Out;

@@ -28,7 +28,7 @@ __device__ __forceinline__ void lds_dma4(i32x4 rsrc, uint32_t lds_addr, uint32_t
 // steps that use it (four tiles per DMA), so that two workgroups share a CU.
 // One's first loads and last stores then pass beside the other's products (128x128 with eight
 // waves, k-steps of 512 and a CU to itself: 3001 x 2504 x 5003 30 us, now 25; 2500 x 2500 x 8192 41,
-// now 31).  At 8192^3 it is 12 % behind the 256x256 tile, which reads a quarter less from LDS
+// now 31).  At 8192^3 it takes 15 % longer than the 256x256 tile, which reads a quarter less from LDS
 // for the same MFMAs.
 template <int BM_, int BN_, int WM_, int WN_, int BK_, int STAGES_, int GS_, class OUT>
 struct Mx4Rp {

@@ -12,8 +12,9 @@
 // answers one workgroup every 11 ns (512 of them: 5.8 us), and a kernel's start costs 2.3.
 //
 // 64 tokens, 32 experts of 4096 x 2048 bf16, top 4: 277 us, 5.8 TB/s (16 for the router, 167 and 93 for the
-// products, 6.4 and 5.8 TB/s).  37 tokens, 60 of 2504 x 1400: 220 us (12, 138, 70; 5.2 TB/s).  One token, 8
-// of 64 experts of 4096 x 2048 MX4: 40 us (9, 18, 12; 3.9 and 3.0 TB/s), latency.
+// products, 6.4 and 5.8 TB/s).  37 tokens, 60 of 2504 x 1400: 227 us (12, 142, 73; 5.0 TB/s).  One token, 8
+// of 64 experts of 4096 x 2048: MX4 40 us (9, 18, 12; 3.9 and 3.0 TB/s), latency; bf16 82 (9, 49, 24; 5.6 TB/s).
+// 64 tokens, 32 of them MX4: 142 us (16, 72, 54; 4.0 and 2.6 TB/s).
 #include "block_util.h"
 #include "moe_extent.h"
 #include "mx4.h"
@@ -431,8 +432,8 @@ __device__ __forceinline__ float lower_half(float h) {
 // unit's weights in flight while it multiplies (loads return in order: the other
 // factor's are asked for before them), also across the end of a task, and two
 // workgroups share a CU.  With AHEAD = 2 a wave has two units in flight: one workgroup a CU of
-// them keeps up a stream of bf16 weights for many tokens better (64 tokens: 204 us, now 180),
-// and two of them MX4's for few.
+// them keeps up a stream of bf16 weights for many tokens better (64 tokens: 204 us, with it 180; 167 with
+// up_row_blocks()'s four blocks a task), and two of them MX4's for few.
 template <bool MX, int TB, int AHEAD>
 __global__ __launch_bounds__(kThreads, !MX && AHEAD > 1 ? 2 : 4) void moe_up_kernel(MoeCall c) {
   typedef Rows16<MX> Rows;
@@ -749,6 +750,7 @@ int down_per_cu(int T) { return T <= 8 ? 2 : 1; }
 // as many as the chip holds.  (Four tasks a workgroup whatever the sizes: 55 tokens of 8 experts, 6144 x
 // 1264 MX4, 35 us, now 16; 37 tokens of 60 experts, 2504 x 1400 bf16, 93 us, now 69.)
 int down_segments(int T, int H, int I, double active, int most, bool mx) {
+  // 256 CUs, whatever the device: the workspace's size follows from the split and is asked for without one
   const double slots = 256.0 * down_per_cu(T), per_slot = 1 / slots;
   const int blocks = (H + 31) / 32, units = mx ? (I + 255) / 256 : (I + 127) / 128;
   const double unit_us = (mx ? 1.4 : 2.8) * down_per_cu(T), work = std::max(1.0, active) * units / kWaves;

@@ -155,7 +155,7 @@ __global__ __launch_bounds__(256) void mx4_quant_both_kernel(const E *__restrict
   const size_t step = 16 * ld;
   Raw8<E> v[8];
   // tiles whose columns all exist are spared a load's 24 selects: instructions bound this kernel (8192^2
-  // bf16: 57 us with them and with every address multiplied out, now 46)
+  // bf16: 57 us with them and with every address multiplied out, now 44)
   if (c0 + 128 <= cols) {
 #pragma unroll
     for (int p = 0; p < 8; ++p) v[p].load(from + p * step, r0 + p * 16 + rl < rows);

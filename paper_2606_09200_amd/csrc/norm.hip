@@ -9,7 +9,9 @@
 //
 // Both are bound by the bytes of the rows they read and write once; a row stays in
 // registers between its two sums.  Sums, statistics and gradients of the
-// parameters are binary32; rows are rounded once, when stored (h from the unrounded y).
+// parameters are binary32; rows are rounded once, when stored.  h is made from the unrounded y, while the gradients
+// read y as it is stored: with a bf16 residual they are those of a row that is off by up to 2^-8 of itself, the
+// price of storing nothing beside y.
 //
 // A row is chunks of 8 columns.  One that ends inside a chunk leaves that chunk's 8 registers
 // with its values by fours, twos and ones at fixed places (Chunks), which takes two more
@@ -172,9 +174,11 @@ __global__ __launch_bounds__(1024) void norm_gate_kernel(NormFwd a) {
 // shared so (DIRECT), a run is every runs-th whole gate: at the end of each, dg is
 // complete and stored, and g S goes into the run's sum of dw1, the first array's row.
 //
-// Up to 8192 columns (NCH = 1) the sums, the weights and two rows fit in registers.
+// Up to 8192 columns (NCH = 1) the sums, the weights and two rows fit in registers, but for 4 or 5 a thread that
+// binary32 rows spill with DIRECT.
 // Beyond (NCH = 2, 1024 threads of 128 registers) the sums live in LDS, the
-// binary32 weights come from the caches for each row, and rows are not fetched ahead.
+// binary32 weights come from the caches for each row, and rows are not fetched ahead.  bf16 weights,
+// which stay, leave 13 to 16 registers spilled with DIRECT, and one without where the residual is binary32.
 template <int N, bool LDS>
 struct ColumnSums;  // N sums a thread
 template <int N>
@@ -222,7 +226,7 @@ __global__ __launch_bounds__(1024) void norm_gate_bwd_kernel(NormBwd a) {
   const ACT *gate = static_cast<const ACT *>(a.gate);
   Raw8<ACT> w1[NCH], w2[NCH], gv[NCH];
   // loaded again for each row: what a null pointer leaves is cleared, or the last row's registers would stay live
-  // (and 80 of them in scratch memory: 4096 rows of 16384 binary32 546 us, now 354)
+  // (80 of them in scratch memory, now none: 4096 rows of 16384 binary32 546 us, now 354)
   auto load_gate = [&](int c) {
     if (!KEEP) gv[c] = Raw8<ACT>{};
     if (gate != nullptr) cols.load(gv[c], gate + (size_t)gate_at * D, c);
