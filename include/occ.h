@@ -646,6 +646,107 @@ typedef struct occ_moe_args {
 int occ_moe(const occ_moe_args *args, void *stream);
 size_t occ_moe_workspace_bytes(int tokens, int H, int I, int experts, int top_k);
 
+/* ------------------------------------------------ a paged cache and its attention
+ *
+ * Keys and values of all requests lie in two caches of `pages` pages of `page` rows, a row being Hkv heads of
+ * D values.  Row `off` of page `id` is slot id * page + off.  A request's keys are those of its row of the
+ * table (requests x width, page ids, rows ld_table apart): key j lies in page table[i][j / page].
+ * All lengths live on the GPU, so that a captured graph serves every step.
+ */
+#define OCC_KV_MAX_REQUESTS 65536
+#define OCC_KV_MAX_PAGE 65536
+#define OCC_ATTN_MAX_KEYS 2147418112   /* keys of a request: 2^31 - 2^16 */
+
+/*
+ * occ_kv_tables -- a step's block tables, slots and positions from the lengths of its requests.
+ * Request i has cached[i] keys.  fresh[i] >= 0: it brings as many new tokens; fresh[i] < 0: it is over, its pages go
+ * back.  Free pages are a ring: free[0] is the place of the first, free[1] how many follow, in `ring`
+ * (ring_size entries).  With sums over the requests in order,
+ *   start = sum of tokens before,  have = ceil(cached / page),  need = ceil((cached + fresh) / page) - have
+ * request i is served if its tokens end within `rows`, its pages within `width` and, where it needs any, its
+ * sum of needs (of the requests up to it that pass the first two) within free[1].  Then table[i][have ...] get its new
+ * pages, in the ring's order; other entries of the table stay as they are.
+ *   lens[i]   : cached + fresh; -1 for a request that is not served, 0 for one that is over
+ *   starts    : requests + 1; its rows are starts[i] .. starts[i + 1] - 1 (none beyond `rows`)
+ *   slots     : rows; of each token, -1 where its request is not served or its page is not in [0, pages), and for
+ *               rows behind the last token
+ *   positions : rows; cached + 0, 1, ..; 0 for rows without a served request
+ *   free_after: as free, for the next call; pages that come back are behind the others, and are not given out by this call
+ * Only `table` and `ring` are read and written; the others must not overlap.  A program keeps lens as the next step's
+ * cached and free_after as its free.  Everything is exact; int32 buffers, 4-byte aligned.  No workspace.
+ */
+typedef struct occ_kv_tables_args {
+  int requests, rows, width, page, pages, ring_size;
+  const int32_t *cached, *fresh, *free;
+  int32_t *table, *ring;
+  size_t ld_table;
+  int32_t *lens, *starts, *slots, *positions, *free_after;
+} occ_kv_tables_args;
+int occ_kv_tables(const occ_kv_tables_args *args, void *stream);
+
+/*
+ * occ_rope -- rotary positions of q (rows x Hq heads of D) and k (rows x Hkv heads), either may be null:
+ *   (y_0, y_1) = scale (x_0 cos a - x_1 sin a, x_1 cos a + x_0 sin a),  a = 2 pi positions[row] turns[i] / 2^64
+ * for i < pairs; pair i is elements i and i + pairs, or 2 i and 2 i + 1 (interleaved != 0).  Elements from 2 pairs on are
+ * passed through.  turns[i] is the i-th frequency over 2 pi as a fraction of 2^64 (int64, wrapping): angles
+ * are exact to 2^-32 of a turn at every position, negative ones too.  inverse != 0 turns the other way: the
+ * gradient of the same call.  Sums are fp32, outputs are rounded once.
+ * q_out may be q and k_out k (the same pitches).  With caches (both or none; k is needed), row r's turned keys
+ * and its rows of v go to slot slots[r] of k_cache and v_cache, and to none where that is not in [0, pages * page);
+ * k_out may then be null.  dtype, of all tensors: OCC_BF16 or OCC_F32.  *_row, *_head: pitches in elements of rows and
+ * heads, cache_page, cache_row, cache_head of both caches.  Values of a head are contiguous.  1 <= D <= OCC_ROPE_MAX_D,
+ * even, 0 <= 2 pairs <= D; page * pages < 2^31; rows <= 2^24.  Pitches, D / 2 and pairs that are multiples of 8 (4 with
+ * OCC_F32), on 16-byte aligned buffers, are the fast case.
+ * Two rows with one slot: either may be what is kept.  A head's rows must not overlap another's.
+ */
+#define OCC_ROPE_MAX_D 1024
+typedef struct occ_rope_args {
+  int rows, Hq, Hkv, D, pairs, dtype;
+  int interleaved, inverse, page, pages;
+  float scale;
+  const void *q, *k, *v;
+  void *q_out, *k_out, *k_cache, *v_cache;
+  const int32_t *positions, *slots;
+  const int64_t *turns;
+  size_t q_row, q_head, k_row, k_head, v_row, v_head, qo_row, qo_head, ko_row, ko_head;
+  size_t cache_page, cache_row, cache_head;
+} occ_rope_args;
+int occ_rope(const occ_rope_args *args, void *stream);
+
+/*
+ * occ_attn_paged -- attention of each request's new tokens over its pages, after its own keys are there.  Request i has
+ * rows starts[i] .. starts[i + 1] - 1 of q (rows x Hq heads of D, bf16) and keys 0 .. lens[i] - 1; its last row is
+ * its last key's.  With pos the row's key and head h sharing keys of head h / (Hq / Hkv),
+ *   o = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q . k_j),  lse = log sum_j p_j
+ * over j < lens[i], j <= pos (causal != 0) and j > pos - window (window > 0), but not keys whose page is not in [0, pages).
+ * Where nothing is left, o is 0 and lse -inf; what is not seen has no influence, infinities and NaN neither.  lens[i] <= 0
+ * leaves nothing; rows of no request keep what out and lse hold; lengths beyond width * page (or OCC_ATTN_MAX_KEYS) are cut.
+ * Logits, sums and o are fp32; weights p take part in the sum with v as bf16 (two of them where a request has few
+ * rows), out is bf16 and lse (rows x Hq, null: not stored) fp32.
+ * max_fresh: the most rows of a request; what the choice of kernels goes by (results hold for any).
+ * D: a multiple of 8 up to 256; Hq a multiple of Hkv; pitches (elements) multiples of 8, buffers 16-byte aligned,
+ * starts, lens, table and lse 4.  rows * Hq < 2^31.
+ * workspace: occ_attn_paged_workspace_bytes(Hq, Hkv, D) bytes, 16-byte aligned, zeroed once before its first use (a
+ * complete call leaves it ready for the next, of any sizes with this D); calls that share one must not overlap.
+ * No workgroup waits for another.
+ */
+typedef struct occ_attn_args {
+  int requests, rows, Hq, Hkv, D;
+  int page, pages, width, max_fresh;
+  int causal, window;
+  float scale;
+  const void *q, *k_cache, *v_cache;
+  const int32_t *table, *starts, *lens;
+  void *out;
+  float *lse;
+  size_t ld_table, q_row, q_head, out_row, out_head;
+  size_t cache_page, cache_row, cache_head;
+  void *workspace;
+  size_t workspace_bytes;
+} occ_attn_args;
+int occ_attn_paged(const occ_attn_args *args, void *stream);
+size_t occ_attn_paged_workspace_bytes(int Hq, int Hkv, int D);
+
 /* Static string naming a status code. */
 const char *occ_strerror(int status);
 

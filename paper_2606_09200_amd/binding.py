@@ -10,6 +10,7 @@ torch must be imported before the library is loaded so that both use the one
 HIP runtime already in the process (torch's; same soname).
 """
 import ctypes
+import math
 import os
 import struct
 
@@ -106,10 +107,38 @@ class occ_gemm_mx4_plan(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int) for n in ("tile_m", "tile_n", "tiles", "grid", "nontemporal")]
 
 
+class occ_kv_tables_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("requests", "rows", "width", "page", "pages", "ring_size")] + [
+        (n, ctypes.c_void_p) for n in ("cached", "fresh", "free", "table", "ring")] + [("ld_table", ctypes.c_size_t)] + [
+            (n, ctypes.c_void_p) for n in ("lens", "starts", "slots", "positions", "free_after")]
+
+
+class occ_rope_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("rows", "Hq", "Hkv", "D", "pairs", "dtype", "interleaved", "inverse", "page",
+                                            "pages")] + [("scale", ctypes.c_float)] + [(n, ctypes.c_void_p) for n in (
+                                                "q", "k", "v", "q_out", "k_out", "k_cache", "v_cache", "positions", "slots",
+                                                "turns")] + [(n, ctypes.c_size_t) for n in (
+                                                    "q_row", "q_head", "k_row", "k_head", "v_row", "v_head", "qo_row", "qo_head",
+                                                    "ko_row", "ko_head", "cache_page", "cache_row", "cache_head")]
+
+
+class occ_attn_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("requests", "rows", "Hq", "Hkv", "D", "page", "pages", "width", "max_fresh",
+                                            "causal", "window")] + [("scale", ctypes.c_float)] + [(n, ctypes.c_void_p) for n in (
+                                                "q", "k_cache", "v_cache", "table", "starts", "lens", "out", "lse")] + [
+        (n, ctypes.c_size_t) for n in ("ld_table", "q_row", "q_head", "out_row", "out_head", "cache_page", "cache_row",
+                                       "cache_head")] + [("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
 # The same structures packed in one go, 0 for NULL: filling a ctypes structure costs a short call 1.2 us more.
 _pack_norm = struct.Struct("@6i2f8P4N7P4NPN")
 _pack_moe = struct.Struct("@7i8P3N4P2NPN")
+_pack_tables = struct.Struct("@6i5PN5P")
+_pack_rope = struct.Struct("@10if10P13N")
+_pack_attn = struct.Struct("@11if8P8NPN")
 assert _pack_norm.size == ctypes.sizeof(occ_norm_args) and _pack_moe.size == ctypes.sizeof(occ_moe_args)
+assert _pack_tables.size == ctypes.sizeof(occ_kv_tables_args) and _pack_rope.size == ctypes.sizeof(occ_rope_args)
+assert _pack_attn.size == ctypes.sizeof(occ_attn_args)
 
 _lib = None
 _P = ctypes.c_void_p
@@ -149,6 +178,10 @@ _SIGS = {
     "occ_norm_gate_bwd_workspace_bytes": [ctypes.c_int, ctypes.c_int, ctypes.c_int],
     "occ_moe": [_P, _P],
     "occ_moe_workspace_bytes": [ctypes.c_int] * 5,
+    "occ_kv_tables": [_P, _P],
+    "occ_rope": [_P, _P],
+    "occ_attn_paged": [_P, _P],
+    "occ_attn_paged_workspace_bytes": [ctypes.c_int] * 3,
     "occ_strerror": [ctypes.c_int],
     "occ_version": [],
 }
@@ -815,3 +848,170 @@ def occ_moe(x, router, w_gate, w_up, w_down, y, *, top_k, workspace, ids=None, w
     if st:
         raise OccError(st, "occ_moe")
     return y
+
+
+# ------------------------------------------------------------------ a paged cache and its attention
+
+def _int_param(name, t, shape):
+    """Address of a contiguous int32 GPU tensor of that shape."""
+    if t.dtype != torch.int32 or not t.is_cuda or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 GPU tensor of shape %s" % (name, tuple(shape)))
+    return t.data_ptr()
+
+
+def _table_arg(t):
+    """(address, requests, width, pitch) of a block table."""
+    if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 2:
+        raise ValueError("table must be an int32 GPU tensor (requests, width)")
+    n, width = t.shape
+    return t.data_ptr(), n, width, width if t.is_contiguous() else _pitch("table", t, n, width)
+
+
+def occ_kv_tables(cached, fresh, table, ring, free, *, page, pages, lens, starts, slots, positions, free_after, stream=None):
+    """A step's block tables and slots from its requests' lengths (int32 GPU tensors; see occ.h).  cached, fresh, lens
+    (requests); fresh < 0 gives a request's pages back.  table (requests, width) takes new pages from the ring of free ones,
+    whose place and number are free (2), after the call free_after (2).  starts (requests + 1); slots and positions (rows)
+    of each new token.  pages: the cache's, of `page` rows."""
+    t_ptr, n, width, ld = _table_arg(table)
+    one = (n,)
+    if ring.dim() != 1 or slots.dim() != 1:
+        raise ValueError("ring and slots must have one dimension")
+    rows = slots.shape
+    a = _pack_tables.pack(n, rows[0], width, page, pages, ring.shape[0], _int_param("cached", cached, one),
+                          _int_param("fresh", fresh, one), _int_param("free", free, (2,)), t_ptr,
+                          _int_param("ring", ring, ring.shape), ld, _int_param("lens", lens, one),
+                          _int_param("starts", starts, (n + 1,)), _int_param("slots", slots, rows),
+                          _int_param("positions", positions, rows), _int_param("free_after", free_after, (2,)))
+    st = lib().occ_kv_tables(a, _raw_stream(stream))
+    if st:
+        raise OccError(st, "occ_kv_tables")
+    return lens, starts, slots, positions, free_after
+
+
+def rope_turns(pairs, base=10000.0, *, linear=1.0, bands=None, device="cuda"):
+    """Frequencies of rotary positions for occ_rope: base^(-i / pairs) radians a position for pair i, as 64-bit fractions of
+    a turn (int64).  Longer contexts: ``linear`` divides all of them (positions closer together); ``bands`` =
+    (factor, low, high, length) divides by factor those that make fewer than `low` turns in `length` positions, leaves
+    those that make more than `high`, and goes from one to the other linearly in the turns between."""
+    values = []
+    for i in range(int(pairs)):
+        turns = base ** (-i / pairs) / (2 * math.pi) / linear
+        if bands is not None:
+            factor, low, high, length = bands
+            keep = min(1.0, max(0.0, (turns * length - low) / (high - low)))
+            turns = turns * (keep + (1 - keep) / factor)
+        v = int(turns * 2.0 ** 64) % (1 << 64)
+        values.append(v - (1 << 64) if v >= 1 << 63 else v)
+    return torch.tensor(values, dtype=torch.int64, device=device)
+
+
+def _heads_arg(name, t, dtype, rows, heads, D):
+    """(address, row pitch, head pitch) of a (rows, heads, D) tensor whose heads are contiguous."""
+    if t.dtype != dtype or not t.is_cuda or t.shape != (rows, heads, D):
+        raise ValueError("%s must be a %s GPU tensor of shape (%d, %d, %d)" % (name, dtype, rows, heads, D))
+    row, head, one = t.stride()
+    if D > 1 and one != 1:
+        raise ValueError("%s must have contiguous heads" % name)
+    # a dimension of one has any stride
+    head = head if heads > 1 else D
+    return t.data_ptr(), row if rows > 1 else heads * head, head
+
+
+def _cache_arg(k_cache, v_cache, dtype, heads, D):
+    """(addresses, pages, page, pitches) of two caches (pages, page, heads, D) of the same strides."""
+    if k_cache.dtype != dtype or v_cache.dtype != dtype or not k_cache.is_cuda or not v_cache.is_cuda:
+        raise ValueError("k_cache and v_cache must be %s GPU tensors" % dtype)
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.shape[2:] != (heads, D):
+        raise ValueError("k_cache and v_cache must have one shape (pages, page, %d, %d)" % (heads, D))
+    if k_cache.stride() != v_cache.stride() or (D > 1 and k_cache.stride(3) != 1):
+        raise ValueError("k_cache and v_cache must have the same strides, and contiguous heads")
+    pages, page = k_cache.shape[:2]
+    by_page, by_row, by_head, _ = k_cache.stride()
+    by_head = by_head if heads > 1 else D
+    by_row = by_row if page > 1 else heads * by_head
+    return k_cache.data_ptr(), v_cache.data_ptr(), pages, page, by_page if pages > 1 else page * by_row, by_row, by_head
+
+
+def occ_rope(q, k, positions, turns, *, q_out=None, k_out=None, interleaved=False, scale=1.0, inverse=False, v=None, k_cache=None,
+             v_cache=None, slots=None, stream=None):
+    """Rotary positions of q (rows, Hq, D) and k (rows, Hkv, D), either None, by positions (rows, int32) and frequencies
+    turns (pairs, int64; see rope_turns): pair i is elements i and i + pairs, or 2 i and 2 i + 1; elements past 2 pairs pass.
+    inverse: the other way, the gradient.  q_out and k_out: where to, None for in place -- but with k_cache and v_cache
+    (pages, page, Hkv, D), into whose slots (rows, int32) the turned k and v go, no k_out is written for None.
+    bf16 or fp32.  Returns (q_out, k_out)."""
+    some = q if q is not None else k
+    if some is None or some.dim() != 3:
+        raise ValueError("q or k must be given, (rows, heads, D)")
+    dtype, (rows, _, D) = some.dtype, some.shape
+    kind = _float_type("q or k", some)
+    if turns.dim() != 1 or turns.dtype != torch.int64 or not turns.is_cuda or not turns.is_contiguous():
+        raise ValueError("turns must be a contiguous int64 GPU tensor of one dimension")
+    Hq = Hkv = q_ptr = q_row = q_head = qo_ptr = qo_row = qo_head = 0
+    k_ptr = k_row = k_head = ko_ptr = ko_row = ko_head = v_ptr = v_row = v_head = 0
+    kc = vc = pages = page = by_page = by_row = by_head = s_ptr = 0
+    if q is not None:
+        Hq = q.shape[1]
+        q_out = q if q_out is None else q_out
+        q_ptr, q_row, q_head = _heads_arg("q", q, dtype, rows, Hq, D)
+        qo_ptr, qo_row, qo_head = _heads_arg("q_out", q_out, dtype, rows, Hq, D)
+    elif q_out is not None:
+        raise ValueError("q_out needs q")
+    if k is not None:
+        if k.dim() != 3:
+            raise ValueError("k must have shape (rows, heads, D)")
+        Hkv = k.shape[1]
+        if k_out is None and k_cache is None:
+            k_out = k
+        k_ptr, k_row, k_head = _heads_arg("k", k, dtype, rows, Hkv, D)
+        if k_out is not None:
+            ko_ptr, ko_row, ko_head = _heads_arg("k_out", k_out, dtype, rows, Hkv, D)
+    elif k_out is not None:
+        raise ValueError("k_out needs k")
+    if k_cache is not None or v_cache is not None or v is not None or slots is not None:
+        if k is None or v is None or k_cache is None or v_cache is None or slots is None:
+            raise ValueError("a cache needs k, v, k_cache, v_cache and slots")
+        v_ptr, v_row, v_head = _heads_arg("v", v, dtype, rows, Hkv, D)
+        kc, vc, pages, page, by_page, by_row, by_head = _cache_arg(k_cache, v_cache, dtype, Hkv, D)
+        s_ptr = _int_param("slots", slots, (rows,))
+    a = _pack_rope.pack(rows, Hq, Hkv, D, turns.shape[0], kind, 1 if interleaved else 0, 1 if inverse else 0, page, pages, scale,
+                        q_ptr, k_ptr, v_ptr, qo_ptr, ko_ptr, kc, vc, _int_param("positions", positions, (rows,)), s_ptr,
+                        turns.data_ptr(), q_row, q_head, k_row, k_head, v_row, v_head, qo_row, qo_head, ko_row, ko_head,
+                        by_page, by_row, by_head)
+    st = lib().occ_rope(a, _raw_stream(stream))
+    if st:
+        raise OccError(st, "occ_rope")
+    return q_out, k_out
+
+
+def occ_attn_paged_workspace_bytes(Hq, Hkv, D):
+    """Device bytes occ_attn_paged needs (zeroed once)."""
+    return int(lib().occ_attn_paged_workspace_bytes(int(Hq), int(Hkv), int(D)))
+
+
+def occ_attn_paged(q, k_cache, v_cache, table, starts, lens, out, *, max_fresh, workspace, scale=None, causal=True, window=0, lse=None,
+                   stream=None):
+    """Attention of each request's new tokens over its pages: rows starts[i] .. starts[i + 1] - 1 of q (rows, Hq, D) are
+    request i's, its keys the first lens[i] that table (requests, width) leads to in k_cache and v_cache (pages, page, Hkv,
+    D), its last row being its last key's.  scale: D^-0.5 if None.  window: keys a row sees at most, 0 for all.
+    max_fresh: the most rows a request has (for the choice of kernels).  lse (rows, Hq, fp32) receives the log of
+    each row's sum.  workspace: a GPU tensor zeroed once.  Rows of no request are left alone.  Returns out."""
+    if q.dim() != 3:
+        raise ValueError("q must have shape (rows, heads, D)")
+    rows, Hq, D = q.shape
+    bf16 = torch.bfloat16
+    q_ptr, q_row, q_head = _heads_arg("q", q, bf16, rows, Hq, D)
+    o_ptr, o_row, o_head = _heads_arg("out", out, bf16, rows, Hq, D)
+    if k_cache.dim() != 4:
+        raise ValueError("k_cache must have shape (pages, page, heads, D)")
+    Hkv = k_cache.shape[2]
+    kc, vc, pages, page, by_page, by_row, by_head = _cache_arg(k_cache, v_cache, bf16, Hkv, D)
+    t_ptr, n, width, ld = _table_arg(table)
+    ws, ws_bytes = _workspace_arg(workspace)
+    a = _pack_attn.pack(n, rows, Hq, Hkv, D, page, pages, width, max_fresh, 1 if causal else 0, window,
+                        D ** -0.5 if scale is None else scale, q_ptr, kc, vc, t_ptr, _int_param("starts", starts, (n + 1,)),
+                        _int_param("lens", lens, (n,)), o_ptr, _param("lse", lse, torch.float32, (rows, Hq)), ld, q_row, q_head,
+                        o_row, o_head, by_page, by_row, by_head, ws, ws_bytes)
+    st = lib().occ_attn_paged(a, _raw_stream(stream))
+    if st:
+        raise OccError(st, "occ_attn_paged")
+    return out

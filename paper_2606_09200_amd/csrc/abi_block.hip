@@ -196,6 +196,150 @@ int validate_moe(const occ_moe_args &a) {
   return disjoint(out, in) ? OCC_OK : OCC_EALIAS;
 }
 
+namespace {
+
+// Bytes that heads of D values at these pitches span.
+size_t span3(int rows, size_t row, int heads, size_t head, int D, size_t elem) {
+  return rows == 0 || heads == 0 ? 0 : ((size_t)(rows - 1) * row + (size_t)(heads - 1) * head + D) * elem;
+}
+// Heads that do not overlap, in rows that do not: one pitch goes past what the other covers.
+bool apart(int rows, size_t row, int heads, size_t head, int D) {
+  const size_t d = (size_t)D;
+  if (heads > 1 && head < d) return false;
+  if (rows > 1 && row < d) return false;
+  if (heads <= 1 || rows <= 1) return true;
+  return row >= (size_t)(heads - 1) * head + d || head >= (size_t)(rows - 1) * row + d;
+}
+// The same of a cache's rows in pages; pages are outermost, then rows or heads.
+bool cache_apart(int pages, size_t cache_page, int page, size_t row, int heads, size_t head, int D) {
+  return apart(page, row, heads, head, D) && (pages <= 1 || cache_page >= span3(page, row, heads, head, D, 1));
+}
+
+}  // namespace
+
+int validate_kv_tables(const occ_kv_tables_args &a) {
+  if (a.requests < 0 || a.requests > OCC_KV_MAX_REQUESTS || a.rows < 0 || a.rows > (1 << 24)) return OCC_EINVAL;
+  if (a.width < 0 || a.page < 1 || a.page > OCC_KV_MAX_PAGE || a.pages < 0 || a.ring_size < 1) return OCC_EINVAL;
+  if ((long long)a.pages * a.page > INT32_MAX || a.ring_size > (1 << 30)) return OCC_EINVAL;
+  if (a.requests == 0) return OCC_OK;
+  if (a.requests > 1 && a.ld_table < (size_t)a.width) return OCC_EINVAL;
+  const void *needed[] = {a.cached, a.fresh, a.free, a.ring, a.lens, a.starts, a.free_after};
+  for (const void *p : needed)
+    if (p == nullptr || !aligned(p, 4)) return OCC_EINVAL;
+  if ((a.width > 0 && a.table == nullptr) || !aligned(a.table, 4)) return OCC_EINVAL;
+  if (a.rows > 0 && (a.slots == nullptr || a.positions == nullptr)) return OCC_EINVAL;
+  if (!aligned(a.slots, 4) || !aligned(a.positions, 4)) return OCC_EINVAL;
+  const size_t n = (size_t)a.requests * 4, t = (size_t)a.rows * 4;
+  const Range in[] = {{a.cached, n}, {a.fresh, n}, {a.free, 8}};
+  const Range out[] = {{a.table, a.width == 0 ? 0 : ((size_t)(a.requests - 1) * a.ld_table + a.width) * 4},
+                       {a.ring, (size_t)a.ring_size * 4}, {a.lens, n}, {a.starts, n + 4}, {a.slots, t}, {a.positions, t},
+                       {a.free_after, 8}};
+  return disjoint(out, in) ? OCC_OK : OCC_EALIAS;
+}
+
+int validate_rope(const occ_rope_args &a) {
+  if (!float_type(a.dtype) || a.rows < 0 || a.rows > (1 << 24) || a.Hq < 0 || a.Hkv < 0) return OCC_EINVAL;
+  if (a.Hq > 65536 || a.Hkv > 65536 || a.D < 2 || a.D > OCC_ROPE_MAX_D || a.D % 2 != 0) return OCC_EINVAL;
+  if (a.pairs < 0 || 2 * a.pairs > a.D || !(a.scale - a.scale == 0.f)) return OCC_EINVAL;
+  const bool cache = a.k_cache != nullptr;
+  if (cache != (a.v_cache != nullptr)) return OCC_EINVAL;
+  if (a.rows == 0) return OCC_OK;
+  const size_t e = type_bytes(a.dtype);
+  const bool q = a.q != nullptr && a.Hq > 0, k = a.k != nullptr && a.Hkv > 0;
+  if (a.positions == nullptr || !aligned(a.positions, 4) || (a.pairs > 0 && a.turns == nullptr) || !aligned(a.turns, 8)) return OCC_EINVAL;
+  if ((q && a.q_out == nullptr) || (k && a.k_out == nullptr && !cache) || (cache && (!k || a.v == nullptr || a.slots == nullptr)))
+    return OCC_EINVAL;
+  const void *all[] = {a.q, a.k, a.v, a.q_out, a.k_out, a.k_cache, a.v_cache};
+  for (const void *p : all)
+    if (!aligned(p, e)) return OCC_EINVAL;
+  if (!aligned(a.slots, 4)) return OCC_EINVAL;
+  if ((q && (!apart(a.rows, a.q_row, a.Hq, a.q_head, a.D) || !apart(a.rows, a.qo_row, a.Hq, a.qo_head, a.D))) ||
+      (k && !apart(a.rows, a.k_row, a.Hkv, a.k_head, a.D)) ||
+      (k && a.k_out != nullptr && !apart(a.rows, a.ko_row, a.Hkv, a.ko_head, a.D)))
+    return OCC_EINVAL;
+  if (cache && (a.page < 1 || a.page > OCC_KV_MAX_PAGE || a.pages < 1 || (long long)a.page * a.pages > INT32_MAX ||
+                !apart(a.rows, a.v_row, a.Hkv, a.v_head, a.D) ||
+                !cache_apart(a.pages, a.cache_page, a.page, a.cache_row, a.Hkv, a.cache_head, a.D)))
+    return OCC_EINVAL;
+  // rows of the joint projection interleave q, k and v: only tensors that begin within another's head overlap, so
+  // in place is told by the pointer and other overlaps of outputs with inputs by whole ranges where these are packed
+  const Range rq{q ? a.q : nullptr, span3(a.rows, a.q_row, a.Hq, a.q_head, a.D, e)};
+  const Range rk{k ? a.k : nullptr, span3(a.rows, a.k_row, a.Hkv, a.k_head, a.D, e)};
+  const Range rv{cache ? a.v : nullptr, span3(a.rows, a.v_row, a.Hkv, a.v_head, a.D, e)};
+  const Range qo{q ? a.q_out : nullptr, span3(a.rows, a.qo_row, a.Hq, a.qo_head, a.D, e)};
+  const Range ko{k ? a.k_out : nullptr, span3(a.rows, a.ko_row, a.Hkv, a.ko_head, a.D, e)};
+  const size_t cached = cache ? ((size_t)(a.pages - 1) * a.cache_page) * e + span3(a.page, a.cache_row, a.Hkv, a.cache_head, a.D, e) : 0;
+  const Range kc{a.k_cache, cached}, vc{a.v_cache, cached};
+  const Range pos{a.positions, (size_t)a.rows * 4}, turns{a.turns, (size_t)a.pairs * 8}, slots{cache ? a.slots : nullptr, (size_t)a.rows * 4};
+  // Rows of one matrix (q, k and v side by side, as a joint projection leaves them): disjoint where their columns are.
+  auto beside = [&](const Range &x, size_t x_row, int hx, size_t x_head, const Range &y, size_t y_row, int hy, size_t y_head) {
+    if (!overlaps(x, y)) return true;
+    if (x_row != y_row || a.rows < 2) return false;
+    const size_t wx = ((size_t)(hx - 1) * x_head + a.D) * e, wy = ((size_t)(hy - 1) * y_head + a.D) * e, pitch = x_row * e;
+    const uintptr_t px = reinterpret_cast<uintptr_t>(x.p), py = reinterpret_cast<uintptr_t>(y.p);
+    const size_t off = (px > py ? px - py : pitch - (py - px) % pitch) % pitch;  // of x's columns behind y's
+    return off >= wy && off + wx <= pitch;
+  };
+  const bool same_q = a.q_out == a.q && a.qo_row == a.q_row && a.qo_head == a.q_head;
+  const bool same_k = a.k_out == a.k && a.ko_row == a.k_row && a.ko_head == a.k_head;
+  if (q && !same_q && !beside(qo, a.qo_row, a.Hq, a.qo_head, rq, a.q_row, a.Hq, a.q_head)) return OCC_EALIAS;
+  if (q && k && !beside(qo, a.qo_row, a.Hq, a.qo_head, rk, a.k_row, a.Hkv, a.k_head)) return OCC_EALIAS;
+  if (q && cache && !beside(qo, a.qo_row, a.Hq, a.qo_head, rv, a.v_row, a.Hkv, a.v_head)) return OCC_EALIAS;
+  if (k && a.k_out != nullptr) {
+    if (!same_k && !beside(ko, a.ko_row, a.Hkv, a.ko_head, rk, a.k_row, a.Hkv, a.k_head)) return OCC_EALIAS;
+    if (q && !beside(ko, a.ko_row, a.Hkv, a.ko_head, rq, a.q_row, a.Hq, a.q_head)) return OCC_EALIAS;
+    if (q && !beside(ko, a.ko_row, a.Hkv, a.ko_head, qo, a.qo_row, a.Hq, a.qo_head)) return OCC_EALIAS;
+    if (cache && !beside(ko, a.ko_row, a.Hkv, a.ko_head, rv, a.v_row, a.Hkv, a.v_head)) return OCC_EALIAS;
+  }
+  // keys and values may be planes of one cache: disjoint where their heads, rows or pages lie apart
+  if (cache && overlaps(kc, vc)) {
+    const size_t one = span3(a.page, a.cache_row, a.Hkv, a.cache_head, a.D, e), pitch = a.cache_page * e;
+    const uintptr_t pk = reinterpret_cast<uintptr_t>(a.k_cache), pv = reinterpret_cast<uintptr_t>(a.v_cache);
+    const size_t off = (pk > pv ? pk - pv : pv - pk);
+    if (a.pages < 2 || off < one || off + one > pitch) return OCC_EALIAS;
+  }
+  const Range in[] = {pos, turns, slots}, wide[] = {rq, rk, rv};
+  const Range out[] = {kc};
+  const Range out_v[] = {vc};
+  for (const Range &o : {qo, ko, kc, vc})
+    for (const Range &i : in)
+      if (overlaps(o, i)) return OCC_EALIAS;
+  if (!disjoint(out, wide) || !disjoint(out_v, wide)) return OCC_EALIAS;
+  for (const Range &c : {kc, vc})
+    if (overlaps(c, qo) || overlaps(c, ko)) return OCC_EALIAS;
+  return OCC_OK;
+}
+
+bool attn_heads(int Hq, int Hkv, int D) {
+  return Hkv >= 1 && Hq >= Hkv && Hq <= 65536 && Hq % Hkv == 0 && D >= 8 && D <= 256 && D % 8 == 0;
+}
+
+int validate_attn(const occ_attn_args &a) {
+  if (!attn_heads(a.Hq, a.Hkv, a.D)) return OCC_EINVAL;
+  if (a.requests < 0 || a.requests > OCC_KV_MAX_REQUESTS || a.rows < 0 || (long long)a.rows * a.Hq > INT32_MAX) return OCC_EINVAL;
+  if (a.page < 1 || a.page > OCC_KV_MAX_PAGE || a.width < 0 || a.max_fresh < 0 || a.window < 0) return OCC_EINVAL;
+  if (!(a.scale > 0.f) || !(a.scale - a.scale == 0.f)) return OCC_EINVAL;
+  if (a.requests == 0 || a.rows == 0) return OCC_OK;
+  if (a.pages < 1 || (long long)a.pages * a.page > INT32_MAX) return OCC_EINVAL;
+  const void *wide[] = {a.q, a.k_cache, a.v_cache, a.out, a.workspace};
+  for (const void *p : wide)
+    if (p == nullptr || !aligned(p, 16)) return OCC_EINVAL;
+  if (a.starts == nullptr || a.lens == nullptr || (a.width > 0 && a.table == nullptr)) return OCC_EINVAL;
+  if (!aligned(a.starts, 4) || !aligned(a.lens, 4) || !aligned(a.table, 4) || !aligned(a.lse, 4)) return OCC_EINVAL;
+  if ((a.q_row | a.q_head | a.out_row | a.out_head | a.cache_page | a.cache_row | a.cache_head) % 8 != 0) return OCC_EINVAL;
+  if (a.requests > 1 && a.ld_table < (size_t)a.width) return OCC_EINVAL;
+  if (!apart(a.rows, a.q_row, a.Hq, a.q_head, a.D) || !apart(a.rows, a.out_row, a.Hq, a.out_head, a.D)) return OCC_EINVAL;
+  if (!cache_apart(a.pages, a.cache_page, a.page, a.cache_row, a.Hkv, a.cache_head, a.D)) return OCC_EINVAL;
+  const size_t need = attn_workspace(a.D);
+  if (a.workspace_bytes < need) return OCC_EINVAL;
+  const size_t cached = (size_t)(a.pages - 1) * a.cache_page * 2 + span3(a.page, a.cache_row, a.Hkv, a.cache_head, a.D, 2);
+  const Range in[] = {{a.q, span3(a.rows, a.q_row, a.Hq, a.q_head, a.D, 2)}, {a.k_cache, cached}, {a.v_cache, cached},
+                      {a.table, a.width == 0 ? 0 : ((size_t)(a.requests - 1) * a.ld_table + a.width) * 4},
+                      {a.starts, (size_t)(a.requests + 1) * 4}, {a.lens, (size_t)a.requests * 4}};
+  const Range out[] = {{a.out, span3(a.rows, a.out_row, a.Hq, a.out_head, a.D, 2)}, {a.lse, (size_t)a.rows * a.Hq * 4}, {a.workspace, need}};
+  return disjoint(out, in) ? OCC_OK : OCC_EALIAS;
+}
+
 }  // namespace occ
 
 extern "C" {
@@ -259,6 +403,28 @@ int occ_moe(const occ_moe_args *args, void *stream) {
 size_t occ_moe_workspace_bytes(int tokens, int H, int I, int experts, int top_k) {
   if (tokens == 0 || occ::validate_moe_sizes(tokens, H, I, experts, top_k) != OCC_OK) return 0;
   return occ::moe_workspace(tokens, H, I, experts, top_k);
+}
+
+int occ_kv_tables(const occ_kv_tables_args *args, void *stream) {
+  if (args == nullptr) return OCC_EINVAL;
+  const int st = occ::validate_kv_tables(*args);
+  return st == OCC_OK ? occ::kv_tables_launch(*args, static_cast<hipStream_t>(stream)) : st;
+}
+
+int occ_rope(const occ_rope_args *args, void *stream) {
+  if (args == nullptr) return OCC_EINVAL;
+  const int st = occ::validate_rope(*args);
+  return st == OCC_OK ? occ::rope_launch(*args, static_cast<hipStream_t>(stream)) : st;
+}
+
+int occ_attn_paged(const occ_attn_args *args, void *stream) {
+  if (args == nullptr) return OCC_EINVAL;
+  const int st = occ::validate_attn(*args);
+  return st == OCC_OK ? occ::attn_launch(*args, static_cast<hipStream_t>(stream)) : st;
+}
+
+size_t occ_attn_paged_workspace_bytes(int Hq, int Hkv, int D) {
+  return occ::attn_heads(Hq, Hkv, D) ? occ::attn_workspace(D) : 0;
 }
 
 }  // extern "C"

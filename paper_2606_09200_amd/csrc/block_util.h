@@ -185,6 +185,32 @@ __device__ __forceinline__ void store_rest(E *p, int cols, const float (&v)[8]) 
   if (cols & 1) put(v[6]);
 }
 
+constexpr uint32_t kNowhere = 0x80000000u;  // a byte offset beyond every descriptor
+
+// 16 bytes at `off` (checked against the descriptor's end) plus `uniform` (which stays within a row).
+template <int POLICY = 0>
+__device__ __forceinline__ u32x4 load16(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t uniform = 0) {
+  return __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, (int)uniform, POLICY);
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void *p, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, 0x00020000);
+}
+
+template <class V>
+__device__ __forceinline__ void put_device(V *p, V v) {  // through the XCD's L2, for readers on other XCDs
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint32_t add_device(uint32_t *p) {
+  return __hip_atomic_fetch_add(p, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// The workgroup's device-scope stores have completed before thread 0 goes on.
+__device__ __forceinline__ void stores_done() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0);
+  asm volatile("" ::: "memory");
+  __syncthreads();
+}
+
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
   return as_float((uint32_t)__builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));

@@ -1,0 +1,387 @@
+// What a paged cache needs before its attention: block tables and slots from lengths (occ_kv_tables), rotary positions
+// with keys and values put into the cache (occ_rope).
+#include "block_util.h"
+#include "divider.h"
+
+#include <algorithm>
+
+namespace occ {
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4;
+
+// ------------------------------------------------------------------ tables
+//
+// All sums are over requests: tokens, pages to get, pages that go back.  One launch: every workgroup makes the sums of all
+// requests for itself (8 bytes a request from the L2) and then does its share of the requests (pages) and of the tokens.
+// Pages come from the ring's head and go back behind its tail, so nothing that one workgroup reads is written by another.
+struct TablesCall {
+  int n, T, width, pages, size;
+  int64_t keys;              // width * page
+  Divider by_page;
+  int page;
+  const int32_t *cached, *fresh, *free;
+  int32_t *table, *ring;
+  size_t ld;
+  int32_t *lens, *starts, *slots, *positions, *free_after;
+  int requests, tokens;      // of a workgroup
+};
+
+// A request by itself: its tokens, its pages before and after, whether it is over.
+struct Asked {
+  int64_t tokens;  // 0 for one that is over
+  int have, need, back;
+  bool fits;       // into its row of the table
+};
+__device__ __forceinline__ Asked asked(const TablesCall &c, int cached, int fresh) {
+  Asked a;
+  a.tokens = fresh < 0 ? 0 : fresh;
+  const int64_t total = (int64_t)cached + a.tokens;
+  a.fits = fresh >= 0 && cached >= 0 && total <= c.keys;
+  const int known = (int)min((int64_t)max(cached, 0), c.keys);
+  // (x + page - 1) / page without passing 2^31
+  a.have = known == 0 ? 0 : c.by_page(known - 1) + 1;
+  a.need = a.fits ? (total == 0 ? 0 : c.by_page((int)total - 1) + 1) - a.have : 0;
+  a.back = fresh < 0 ? a.have : 0;
+  return a;
+}
+
+// What requests before one have asked for.
+struct Before {
+  int64_t tokens, need, back;
+};
+// `need` counts only for requests whose tokens fit into the step's buffers.
+__device__ __forceinline__ bool within(const TablesCall &c, const Asked &a, const Before &b) {
+  return a.fits && b.tokens + a.tokens <= c.T;
+}
+__device__ __forceinline__ void pass(const TablesCall &c, Before &b, const Asked &a) {
+  if (within(c, a, b)) b.need += a.need;
+  b.tokens += a.tokens;
+  b.back += a.back;
+}
+
+__global__ __launch_bounds__(kThreads) void kv_tables_kernel(TablesCall c) {
+  __shared__ int64_t sums[3][kWaves];
+  __shared__ Before before[kThreads + 1];   // of each thread's requests
+  struct Share {
+    int64_t first;  // its first page's place behind the ring's head, or behind its tail
+    int have, need, back;
+  };
+  __shared__ Share shares[64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int per = (c.n + kThreads - 1) / kThreads;
+  const int r0 = min((int)threadIdx.x * per, c.n), r1 = min(r0 + per, c.n);
+  const int size = c.size;
+  const int count = min(max(c.free[1], 0), size);
+  const int head = c.free[0] < 0 || c.free[0] >= size ? 0 : c.free[0];
+
+  // Sums before each thread's requests: tokens first, for which requests need pages depends on them.
+  auto scan = [&](int64_t own, int which) {
+    int64_t upto = own;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int64_t v = __shfl_up(upto, d);
+      if (lane >= d) upto += v;
+    }
+    if (lane == 63) sums[which][wave] = upto;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) upto += sums[which][w];
+    return upto - own;
+  };
+  Before own{0, 0, 0};
+  for (int i = r0; i < r1; ++i) own.tokens += max(c.fresh[i], 0);
+  Before b{scan(own.tokens, 0), 0, 0};
+  Before mine = b;
+  for (int i = r0; i < r1; ++i) pass(c, mine, asked(c, c.cached[i], c.fresh[i]));
+  own = mine;
+  b.need = scan(own.need, 1);
+  b.back = scan(own.back, 2);
+  before[threadIdx.x] = b;
+  if (threadIdx.x == kThreads - 1) before[kThreads] = Before{own.tokens, b.need + own.need, b.back + own.back};
+  __syncthreads();
+
+  // the workgroup's requests: lengths, and what their pages need
+  const int first = min((int)blockIdx.x * c.requests, c.n), last = min(first + c.requests, c.n);
+  {
+    Before at = b;
+    for (int i = r0; i < r1; ++i) {
+      const Asked a = asked(c, c.cached[i], c.fresh[i]);
+      if (i >= first && i < last) {
+        const bool ok = within(c, a, at) && (a.need == 0 || at.need + a.need <= count);
+        c.lens[i] = c.fresh[i] < 0 ? 0 : ok ? (int)(c.cached[i] + a.tokens) : -1;
+        c.starts[i] = (int)min(at.tokens, (int64_t)c.T);
+        if (i == c.n - 1) c.starts[c.n] = (int)min(at.tokens + a.tokens, (int64_t)c.T);
+        shares[i - first] = Share{a.back ? at.back : at.need, a.have, ok ? a.need : 0, a.back};
+      }
+      pass(c, at, a);
+    }
+  }
+  __syncthreads();
+  for (int i = first + wave; i < last; i += kWaves) {
+    const Share s = shares[i - first];
+    int32_t *row = c.table + (size_t)i * c.ld;
+    for (int j = lane; j < s.need; j += 64) {
+      const int64_t at = head + s.first + j;
+      row[s.have + j] = c.ring[at < size ? at : at - size];
+    }
+    for (int j = lane; j < s.back; j += 64) {
+      const int64_t at = (int64_t)count + s.first + j;  // behind what was free, as far as the ring has room
+      if (at < size) c.ring[head + at < size ? head + at : head + at - size] = row[j];
+    }
+  }
+  if (blockIdx.x == 0) {
+    // pages taken: the sum up to the last request that got its own, which is the last whose sum the free pages cover
+    __shared__ int64_t taken;
+    if (threadIdx.x == 0) taken = 0;
+    __syncthreads();
+    Before at = b;
+    int64_t most = 0;
+    for (int i = r0; i < r1; ++i) {
+      const Asked a = asked(c, c.cached[i], c.fresh[i]);
+      if (within(c, a, at) && a.need > 0 && at.need + a.need <= count) most = at.need + a.need;
+      pass(c, at, a);
+    }
+    if (most > 0) atomicMax(reinterpret_cast<long long *>(&taken), (long long)most);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      const int64_t next = head + taken, back = before[kThreads].back;
+      c.free_after[0] = (int)(next < size ? next : next - size);
+      c.free_after[1] = (int)min(count - taken + back, size - taken);
+    }
+  }
+
+  // the workgroup's tokens
+  const int64_t all = before[kThreads].tokens;
+  for (int64_t t = (int64_t)blockIdx.x * c.tokens + threadIdx.x; t < min((int64_t)(blockIdx.x + 1) * c.tokens, (int64_t)c.T); t += kThreads) {
+    int slot = -1, position = 0;
+    if (t < all) {
+      int lo = 0, hi = kThreads - 1;   // the last thread whose requests begin at or before t
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (before[mid].tokens <= t) lo = mid;
+        else hi = mid - 1;
+      }
+      // threads behind the requests' end begin at the sum of all, which is past t; of several that begin at t's
+      // request, the last has it
+      Before at = before[lo];
+      int i = lo * per;
+      Asked a = asked(c, c.cached[i], c.fresh[i]);
+      while (at.tokens + a.tokens <= t) {
+        pass(c, at, a);
+        ++i;
+        a = asked(c, c.cached[i], c.fresh[i]);
+      }
+      if (within(c, a, at) && (a.need == 0 || at.need + a.need <= count)) {
+        position = c.cached[i] + (int)(t - at.tokens);
+        const int index = c.by_page(position);
+        int id;
+        if (index < a.have) {
+          id = c.table[(size_t)i * c.ld + index];
+        } else {
+          const int64_t from = head + at.need + (index - a.have);
+          id = c.ring[from < size ? from : from - size];
+        }
+        if ((uint32_t)id < (uint32_t)c.pages) slot = id * c.page + (position - index * c.page);
+      }
+    }
+    c.slots[t] = slot;
+    c.positions[t] = position;
+  }
+}
+
+// ------------------------------------------------------------------ rotary positions
+//
+//   (y_0, y_1) = m (x_0 cos a - x_1 sin a, x_1 cos a + x_0 sin a),  a = 2 pi position turns_i
+//
+// for pair i of a head.  turns is a 64-bit fraction of a turn, so that position * turns modulo 2^64 is the exact
+// remainder of the angle, however far the position.  A workgroup makes its tokens' cosines and sines once, in LDS, and
+// passes over their heads: bound by reading and writing q, k and v once.
+struct RopeCall {
+  int T, Hq, Hkv, D, half, interleaved;
+  const void *q, *k, *v;
+  void *q_out, *k_out, *k_cache, *v_cache;
+  size_t q_row, q_head, k_row, k_head, v_row, v_head, qo_row, qo_head, ko_row, ko_head, cache_page, cache_row, cache_head;
+  const int32_t *positions, *slots;
+  const int64_t *turns;
+  float scale, sign;
+  int page, slots_end;
+  Divider by_page, by_item, by_chunk;
+  int tokens;           // of a workgroup
+  int per_token;        // items: pieces of 2 PAIRS elements
+  int per_head;
+};
+
+template <class E>
+__device__ __forceinline__ E rounded(float v) {
+  if constexpr (sizeof(E) == 2) return to_bf16(v);
+  else return v;
+}
+
+template <class E, int N>
+struct Piece {
+  typedef E V __attribute__((ext_vector_type(N)));
+  __device__ static __forceinline__ void load(const E *p, E (&x)[N]) {
+    if constexpr (N == 1) {
+      x[0] = *p;
+    } else {
+      const V v = *reinterpret_cast<const V *>(p);
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = v[i];
+    }
+  }
+  __device__ static __forceinline__ void store(E *p, const E (&x)[N]) {
+    if constexpr (N == 1) {
+      *p = x[0];
+    } else {
+      V v;
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = x[i];
+      *reinterpret_cast<V *>(p) = v;
+    }
+  }
+};
+
+template <class E, int PAIRS>
+__global__ __launch_bounds__(kThreads) void rope_kernel(RopeCall c) {
+  extern __shared__ __align__(16) float2 angles[];  // [token][pair]: (cos, sin), scaled
+  const int t0 = blockIdx.x * c.tokens, tokens = min(c.tokens, c.T - t0);
+  for (int i = threadIdx.x; i < tokens * c.half; i += kThreads) {
+    const int t = i / c.half, pair = i - t * c.half;
+    const int64_t phase = (int64_t)((uint64_t)(int64_t)c.positions[t0 + t] * (uint64_t)c.turns[pair]);
+    float s, co;
+    sincospif((float)phase * 0x1p-63f, &s, &co);
+    angles[i] = float2{co * c.scale, s * c.scale * c.sign};
+  }
+  __syncthreads();
+  const int stride = kThreads * gridDim.y;
+  for (int e = blockIdx.y * kThreads + threadIdx.x; e < tokens * c.per_token; e += stride) {
+    const int t = c.by_item(e), in = e - t * c.per_token;
+    const int h = c.by_chunk(in), piece = in - h * c.per_head;
+    const size_t token = (size_t)(t0 + t);
+    // the caches' row, where the token has one
+    const int slot = c.slots != nullptr && h >= c.Hq ? c.slots[token] : -1;
+    const bool kept = slot >= 0 && slot < c.slots_end;
+    const int index = kept ? c.by_page(slot) : 0;
+    const size_t row = (size_t)index * c.cache_page + (size_t)(slot - index * c.page) * c.cache_row;
+    // elements of a piece: pairs of the turned part, then plain ones
+    const int first = piece * PAIRS;
+    const bool turned = first < c.half;
+    const int a0 = turned && !c.interleaved ? first : 2 * first;
+    const int a1 = turned && !c.interleaved ? first + c.half : 2 * first + PAIRS;
+    E x[2][PAIRS], y[2][PAIRS];
+    if (h >= c.Hq + c.Hkv) {
+      if (!kept) continue;
+      const int head = h - c.Hq - c.Hkv;
+      const E *from = static_cast<const E *>(c.v) + token * c.v_row + (size_t)head * c.v_head + 2 * first;
+      E *to = static_cast<E *>(c.v_cache) + row + (size_t)head * c.cache_head + 2 * first;
+      Piece<E, PAIRS>::load(from, x[0]);
+      Piece<E, PAIRS>::load(from + PAIRS, x[1]);
+      Piece<E, PAIRS>::store(to, x[0]);
+      Piece<E, PAIRS>::store(to + PAIRS, x[1]);
+      continue;
+    }
+    const bool key = h >= c.Hq;
+    const int head = key ? h - c.Hq : h;
+    const E *from = key ? static_cast<const E *>(c.k) + token * c.k_row + (size_t)head * c.k_head
+                        : static_cast<const E *>(c.q) + token * c.q_row + (size_t)head * c.q_head;
+    Piece<E, PAIRS>::load(from + a0, x[0]);
+    Piece<E, PAIRS>::load(from + a1, x[1]);
+    if (turned) {
+      const float2 *cs = angles + t * c.half + first;
+#pragma unroll
+      for (int i = 0; i < PAIRS; ++i) {
+        const float2 w = cs[i];
+        if (c.interleaved) {
+          E *xs = &x[0][0], *ys = &y[0][0];
+          const float u = value(xs[2 * i]), v = value(xs[2 * i + 1]);
+          ys[2 * i] = rounded<E>(__builtin_fmaf(u, w.x, -(v * w.y)));
+          ys[2 * i + 1] = rounded<E>(__builtin_fmaf(v, w.x, u * w.y));
+        } else {
+          const float u = value(x[0][i]), v = value(x[1][i]);
+          y[0][i] = rounded<E>(__builtin_fmaf(u, w.x, -(v * w.y)));
+          y[1][i] = rounded<E>(__builtin_fmaf(v, w.x, u * w.y));
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < PAIRS; ++i) y[0][i] = x[0][i], y[1][i] = x[1][i];
+    }
+    auto put = [&](E *to) {
+      Piece<E, PAIRS>::store(to + a0, y[0]);
+      Piece<E, PAIRS>::store(to + a1, y[1]);
+    };
+    if (!key) {
+      put(static_cast<E *>(c.q_out) + token * c.qo_row + (size_t)head * c.qo_head);
+    } else {
+      if (c.k_out != nullptr) put(static_cast<E *>(c.k_out) + token * c.ko_row + (size_t)head * c.ko_head);
+      if (kept) put(static_cast<E *>(c.k_cache) + row + (size_t)head * c.cache_head);
+    }
+  }
+}
+
+typedef void (*RopeFn)(RopeCall);
+
+}  // namespace
+
+int kv_tables_launch(const occ_kv_tables_args &a, hipStream_t s) {
+  const DeviceInfo *di = nullptr;
+  const int st = current_device_info(&di);
+  if (st != OCC_OK) return st;
+  if (a.requests == 0) return OCC_OK;
+  TablesCall c{};
+  c.n = a.requests, c.T = a.rows, c.width = a.width, c.pages = a.pages, c.size = a.ring_size, c.page = a.page;
+  c.keys = std::min<int64_t>((int64_t)a.width * a.page, OCC_ATTN_MAX_KEYS);
+  c.by_page = Divider(a.page);
+  c.cached = a.cached, c.fresh = a.fresh, c.free = a.free, c.table = a.table, c.ring = a.ring, c.ld = a.ld_table;
+  c.lens = a.lens, c.starts = a.starts, c.slots = a.slots, c.positions = a.positions, c.free_after = a.free_after;
+  const int grid = std::max((a.rows + 1023) / 1024, (a.requests + 63) / 64);
+  c.requests = (a.requests + grid - 1) / grid;
+  c.tokens = (a.rows + grid - 1) / grid;
+  hipLaunchKernelGGL(kv_tables_kernel, dim3(grid), dim3(kThreads), 0, s, c);
+  return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
+}
+
+int rope_launch(const occ_rope_args &a, hipStream_t s) {
+  const DeviceInfo *di = nullptr;
+  const int st = current_device_info(&di);
+  if (st != OCC_OK) return st;
+  const int Hq = a.q != nullptr ? a.Hq : 0, Hkv = a.k != nullptr ? a.Hkv : 0;
+  if (a.rows == 0 || Hq + Hkv == 0) return OCC_OK;
+  const bool cache = a.k_cache != nullptr;
+  RopeCall c{};
+  c.T = a.rows, c.Hq = Hq, c.Hkv = Hkv, c.D = a.D, c.half = a.pairs, c.interleaved = a.interleaved != 0;
+  c.q = a.q, c.k = a.k, c.v = a.v, c.q_out = a.q_out, c.k_out = a.k_out, c.k_cache = a.k_cache, c.v_cache = a.v_cache;
+  c.q_row = a.q_row, c.q_head = a.q_head, c.k_row = a.k_row, c.k_head = a.k_head, c.v_row = a.v_row, c.v_head = a.v_head;
+  c.qo_row = a.qo_row, c.qo_head = a.qo_head, c.ko_row = a.ko_row, c.ko_head = a.ko_head;
+  c.cache_page = a.cache_page, c.cache_row = a.cache_row, c.cache_head = a.cache_head;
+  c.positions = a.positions, c.slots = cache ? a.slots : nullptr, c.turns = a.turns;
+  c.scale = a.scale, c.sign = a.inverse ? -1.f : 1.f;
+  c.page = cache ? a.page : 1, c.slots_end = cache ? a.page * a.pages : 0, c.by_page = Divider(c.page);
+  // Pieces of as many pairs as 16 bytes hold, where sizes, pitches and addresses are multiples; of one pair otherwise.
+  const int elem = a.dtype == OCC_F32 ? 4 : 2;
+  auto fits = [&](int pairs) {
+    const size_t n = (size_t)pairs, bytes = n * elem;
+    size_t all = (size_t)a.pairs | (size_t)a.D / 2;   // both parts are whole pieces
+    uintptr_t at = 0;
+    if (Hq) all |= a.q_row | a.q_head | a.qo_row | a.qo_head, at |= (uintptr_t)a.q | (uintptr_t)a.q_out;
+    if (Hkv) all |= a.k_row | a.k_head, at |= (uintptr_t)a.k;
+    if (Hkv && a.k_out) all |= a.ko_row | a.ko_head, at |= (uintptr_t)a.k_out;
+    if (cache) all |= a.cache_page | a.cache_row | a.cache_head | a.v_row | a.v_head, at |= (uintptr_t)a.v | (uintptr_t)a.k_cache | (uintptr_t)a.v_cache;
+    return a.D % 2 == 0 && all % n == 0 && at % bytes == 0;
+  };
+  const int pairs = elem == 2 ? (fits(8) ? 8 : fits(4) ? 4 : 1) : (fits(4) ? 4 : 1);
+  RopeFn fn = elem == 2 ? (pairs == 8 ? rope_kernel<uint16_t, 8> : pairs == 4 ? rope_kernel<uint16_t, 4> : rope_kernel<uint16_t, 1>)
+                        : (pairs == 4 ? rope_kernel<float, 4> : rope_kernel<float, 1>);
+  c.per_head = a.D / 2 / pairs;
+  c.per_token = c.per_head * (Hq + Hkv + (cache ? Hkv : 0));
+  c.by_item = Divider(c.per_token), c.by_chunk = Divider(c.per_head);
+  // several tokens share a workgroup where there are plenty, a token's heads are dealt out where there are few
+  c.tokens = a.rows >= 4 * 4 * di->num_cus ? 4 : 1;
+  const int x = (a.rows + c.tokens - 1) / c.tokens;
+  const int passes = (int)(((int64_t)c.tokens * c.per_token + kThreads - 1) / kThreads);
+  const int y = std::max(1, std::min({passes, 4 * di->num_cus / x, 64}));
+  hipLaunchKernelGGL(fn, dim3(x, y), dim3(kThreads), (size_t)c.tokens * c.half * sizeof(float2), s, c);
+  return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
+}
+
+}  // namespace occ

@@ -192,6 +192,15 @@ int validate_moe(const occ_moe_args &a);
 size_t moe_workspace(int T, int H, int I, int E, int k);
 int moe_launch(const occ_moe_args &a, hipStream_t s);
 
+int validate_kv_tables(const occ_kv_tables_args &a);
+int kv_tables_launch(const occ_kv_tables_args &a, hipStream_t s);
+int validate_rope(const occ_rope_args &a);
+int rope_launch(const occ_rope_args &a, hipStream_t s);
+bool attn_heads(int Hq, int Hkv, int D);
+int validate_attn(const occ_attn_args &a);
+size_t attn_workspace(int D);
+int attn_launch(const occ_attn_args &a, hipStream_t s);
+
 // Tracing helper: sets npairs [start, end] pairs to [UINT64_MAX, 0] and the
 // workgroup-record counter wg[0] to 0 (either pointer may be null).
 int trace_reset(uint64_t *stamps, int npairs, uint32_t *wg, hipStream_t s);
