@@ -166,9 +166,8 @@ def _prepare_tables(c, s, g):
     s["cached"], s["fresh"], s["pages"] = _ints(cached), _ints(fresh), pages
     s["T"] = T + 7   # a program's buffers hold its largest step
     if own:
-        s["lens"], s["starts"] = torch.empty_like(s["cached"]), _ints([0] * (c["n"] + 1))
-        s["slots"], s["positions"] = _ints([0] * s["T"]), _ints([0] * s["T"])
-        s["free_after"] = _ints([0, 0])
+        for name, n in (("lens", c["n"]), ("starts", c["n"] + 1), ("slots", s["T"]), ("positions", s["T"]), ("free_after", 2)):
+            s[name] = torch.empty(n, device=DEV, dtype=torch.int32)
 
 
 def _prepare_rope(c, s, g):
