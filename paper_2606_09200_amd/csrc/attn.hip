@@ -18,7 +18,6 @@
 namespace occ {
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;
 constexpr int kDevice = 16;  // cache policy: device scope, as put_device
 constexpr int kCus = 256;    // the workspace's size is asked for without a device
 constexpr int kMaxDevices = 64;
@@ -77,6 +76,8 @@ __device__ __forceinline__ float sum_quarters(float v) {
 __device__ __forceinline__ bool pair_nonfinite(uint32_t w) {
   return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
 }
+// Bits 0x80008000 are set where either is.
+__device__ __forceinline__ uint32_t pair_exponents(uint32_t w) { return (w & 0x7F807F80u) + 0x00800080u; }
 __device__ __forceinline__ uint32_t pair_finite(uint32_t w) {
   return ((w & 0x7F80u) == 0x7F80u ? 0u : w & 0xFFFFu) | ((w & 0x7F800000u) == 0x7F800000u ? 0u : w & 0xFFFF0000u);
 }
@@ -88,6 +89,8 @@ struct AttnCall {
   float *lse;
   int n, rows, Hq, Hkv, D, group;
   int heads;           // of a tile, with its tokens cut.tokens of them
+  int groups;          // of heads that share keys, tiles' heads at a time
+  Divider by_heads, by_groups;
   int page, width, pages, keys;   // keys: width * page
   Divider by_page;
   size_t table_pitch;
@@ -113,39 +116,40 @@ struct KeyRow {
   int64_t at;
   bool bad;
 };
-__device__ __forceinline__ KeyRow key_row(const AttnCall &c, const int32_t *table, int key) {
+__device__ __forceinline__ KeyRow key_row(const AttnCall &c, int key, int id) {
   const int index = c.by_page(key);
-  const int id = table[index];
   const bool bad = (uint32_t)id >= (uint32_t)c.pages;
   return KeyRow{(int64_t)(bad ? 0 : id) * (int64_t)c.cache_page + (int64_t)(key - index * c.page) * (int64_t)c.cache_row, bad};
 }
 
+template <int THREADS>
 struct WalkShared {
-  int64_t wave[kWaves];
+  int64_t wave[THREADS / 64];
   int64_t at;
   int request;
-  AttnSeq seq[kThreads];
+  uint32_t last_one;
+  AttnSeq seq[THREADS];
 };
 
-// What a workgroup computes of an item: blocks [b0, b1) of 32 (64) keys from key `first` on, of which `last` is the end.
+// What a workgroup computes of an item: blocks [b0, b1) of the keys from `first` on, of which `last` is the end.
 struct Piece {
-  int request, part, tile;
+  int request, kv, group, tile;
   AttnSeq s;
+  AttnItem it;
   int first, last, b0, b1;
-  AttnOwners owners;
   bool began;  // the item begins in this share
   bool alone;  // nobody else has a part of it
-  bool first_began;  // it begins in the first share that has blocks of it
 };
 
-// Calls work(piece) for every item of this workgroup's share of the line.
-template <class F>
-__device__ __forceinline__ void walk(const AttnCall &c, WalkShared &sh, int me, int workgroups, F work) {
+// Calls work(piece, share) for every item of share `me` of the line.
+template <int THREADS, class F>
+__device__ __forceinline__ void walk(const AttnCall &c, WalkShared<THREADS> &sh, int me, int shares, F work) {
   const AttnCut &cut = c.cut;
   // units of all requests before each thread's own
-  const int per = (c.n + kThreads - 1) / kThreads;
+  const int per = (c.n + THREADS - 1) / THREADS;
   const int r0 = min((int)threadIdx.x * per, c.n), r1 = min(r0 + per, c.n);
   int64_t own = 0;
+#pragma unroll 1
   for (int i = r0; i < r1; ++i) {
     const AttnSeq s = seq_of(c, i);
     if (per == 1) sh.seq[threadIdx.x] = s;
@@ -161,19 +165,21 @@ __device__ __forceinline__ void walk(const AttnCall &c, WalkShared &sh, int me, 
   __syncthreads();
   int64_t total = 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < THREADS / 64; ++w) {
     if (w < (int)(threadIdx.x >> 6)) upto += sh.wave[w];
     total += sh.wave[w];
   }
   total = uniform(total);
-  const int64_t share = max((int64_t)c.min_share, (total + workgroups - 1) / workgroups);
-  const int64_t lo = me * share, hi = min(lo + share, total);
+  AttnShare share = attn_share(total, shares, c.min_share);
+  share.units = uniform(share.units);
+  const int64_t lo = me * share.units, hi = min(lo + share.units, total);
   if (lo >= total) return;
   if (upto - own <= lo && lo < upto) {
     int64_t at = upto - own;
     int i = r0;
+#pragma unroll 1
     for (; i < r1 - 1; ++i) {
-      const int64_t u = attn_units(cut, per == 1 ? sh.seq[threadIdx.x] : seq_of(c, i));
+      const int64_t u = attn_units(cut, seq_of(c, i));
       if (lo < at + u) break;
       at += u;
     }
@@ -184,55 +190,74 @@ __device__ __forceinline__ void walk(const AttnCall &c, WalkShared &sh, int me, 
   int i = uniform(sh.request), cached = 0;
   int64_t at_request = uniform(sh.at);
   bool filled = per == 1;
+#pragma unroll 1
   for (; at_request < hi; ++i) {
-    if (!filled || i >= cached + kThreads) {  // the next requests' lengths, one a thread
+    if (!filled || i >= cached + THREADS) {  // the next requests' lengths, one a thread
       __syncthreads();
       cached = i;
       if (cached + (int)threadIdx.x < c.n) sh.seq[threadIdx.x] = seq_of(c, cached + threadIdx.x);
       __syncthreads();
       filled = true;
     }
-    AttnSeq s = sh.seq[i - cached];
-    s.first = uniform(s.first), s.fresh = uniform(s.fresh), s.len = uniform(s.len);
-    const int tiles = attn_tiles(cut, s);
+    Piece p;
+    p.s = sh.seq[i - cached];
+    p.s.first = uniform(p.s.first), p.s.fresh = uniform(p.s.fresh), p.s.len = uniform(p.s.len);
+    const int tiles = attn_tiles(cut, p.s);
     if (tiles == 0) continue;
-    const int64_t units = attn_units_before(cut, s, tiles);
-    const int64_t x = max(lo, at_request) - at_request;
-    int part = x == 0 ? 0 : (int)(x / units);
-    int m = x == 0 ? 0 : attn_tile_at(cut, s, x - part * units);
-    AttnItem it;
-    it.at = at_request + part * units + (m == 0 ? 0 : attn_units_before(cut, s, m));
-    while (it.at < hi && part < cut.parts) {
-      Piece p;
-      p.request = i, p.part = part, p.tile = m, p.s = s;
-      p.first = attn_first_key(cut, s, m), p.last = attn_last_key(cut, s, m);
-      it.keys = p.last - p.first;
-      p.b0 = attn_blocks_before(cut, it, lo), p.b1 = attn_blocks_before(cut, it, hi);
-      p.owners = attn_owners(cut, it, share);
-      p.began = it.at >= lo;
-      p.first_began = it.at >= (int64_t)p.owners.from * share;
-      p.alone = it.keys == 0 || p.owners.to - p.owners.from == 1;
-      if (p.b0 < p.b1 || (it.keys == 0 && p.began)) work(p);
-      it.at += cut.fixed + it.keys;
+    const int64_t units = attn_units_before(cut, p.s, tiles);
+    int part = 0, m = 0;
+    p.it.at = at_request;
+    if (lo > at_request) {  // the first request: from within it
+      while (p.it.at + units <= lo) p.it.at += units, ++part;
+      m = attn_tile_at(cut, p.s, lo - p.it.at);
+      if (m > 0) p.it.at += attn_units_before(cut, p.s, m);
+    }
+    p.request = i;
+#pragma unroll 1
+    while (p.it.at < hi && part < cut.parts) {
+      p.kv = c.by_groups(part), p.group = part - p.kv * c.groups, p.tile = m;
+      p.first = attn_first_key(cut, p.s, m), p.last = attn_last_key(cut, p.s, m);
+      p.it.keys = p.last - p.first;
+      p.b0 = attn_blocks_before(cut, p.it, lo), p.b1 = attn_blocks_before(cut, p.it, hi);
+      p.began = p.it.at >= lo;
+      p.alone = p.b0 == 0 && p.b1 * cut.block >= p.it.keys;
+      if (p.b0 < p.b1 || (p.it.keys == 0 && p.began)) work(p, share);
+      p.it.at += cut.fixed + p.it.keys;
       if (++m == tiles) m = 0, ++part;
     }
     at_request += units * cut.parts;
   }
 }
 
+// Whether this workgroup, its part of the item stored, is the last of those that have one (the same in all threads).
+template <int THREADS>
+__device__ __forceinline__ bool last_of(const AttnCall &c, WalkShared<THREADS> &sh, const AttnOwners &o) {
+  stores_done();
+  if (threadIdx.x == 0) {
+    const bool last = add_device(c.joined + o.from) + 1 == (uint32_t)(o.to - o.from);
+    if (last) put_device(c.joined + o.from, 0u);  // for the next call
+    sh.last_one = last;
+  }
+  __syncthreads();
+  return sh.last_one != 0u;
+}
+
+// Places of partial results: two a share, for an item that began before it and for one that begins in it.
+__device__ __forceinline__ uint32_t place_of(int share, bool began, int floats) { return (uint32_t)(2 * share + (began ? 1 : 0)) * (uint32_t)(floats * 4); }
+
 // A row of a tile: its token and head, and the keys [lo, hi) that it sees.
 struct Row {
   int token, head, lo, hi;
   bool valid;
 };
-__device__ __forceinline__ Row row_of(const AttnCall &c, const Piece &p, int groups, int r) {
-  const int t = r / c.heads, h = r - t * c.heads;
+__device__ __forceinline__ Row row_of(const AttnCall &c, const Piece &p, int r) {
+  const int t = c.by_heads(r), h = r - t * c.heads;
   const int token = p.tile * c.cut.tokens + t;
-  const int kv = p.part / groups, in = (p.part - kv * groups) * c.heads + h;
+  const int in = p.group * c.heads + h;
   Row row;
   row.valid = t < c.cut.tokens && token < p.s.fresh && in < c.group;
   row.token = p.s.first + token;
-  row.head = kv * c.group + in;
+  row.head = p.kv * c.group + in;
   const int pos = p.s.len - p.s.fresh + token;
   row.hi = !row.valid ? 0 : c.cut.causal ? min(pos + 1, p.s.len) : p.s.len;
   row.lo = c.cut.window ? pos - c.cut.window + 1 : 0;
@@ -249,20 +274,21 @@ __device__ __forceinline__ void seen_by_all(const AttnCall &c, const Piece &p, i
 // ------------------------------------------------------------------ few rows
 //
 // Decoding: up to 16 rows (heads that share keys, times tokens) and many keys.  What bounds it is reading keys and
-// values once.  Each of the workgroup's 4 waves takes every 4th block of 32 keys by itself, with no barrier: keys go
+// values once.  Each of the workgroup's 8 waves takes every 8th block of 32 keys by itself, with no barrier: keys go
 // from memory to the registers of S^T = K Q^T as they are (16x16x32 MFMAs: a lane holds 8 keys' scores of one row, which
 // are what the second product wants of it), values pass through the wave's own LDS to be read transposed for O^T = V^T
 // P^T.  P goes in as the sum of two bf16 values: matrix instructions are in plenty here, and o then has
 // its own rounding alone.
 template <int DP>
 struct FewTile {
-  static constexpr int ROWS = 16, KEYS = 32;
+  static constexpr int WAVES = 8, THREADS = 64 * WAVES;
+  static constexpr int ROWS = 16, TILES = DP > 128 ? 1 : 2, KEYS = 16 * TILES;
   static constexpr int KS = DP / 32, DT = DP / 16;
   static constexpr int PITCH = DP * 2;                 // bytes of a row of V in LDS
   static constexpr int O_PITCH = DP + 4;               // floats of a row of O there
-  static constexpr int WAVE_BYTES = 64 * DP + 256;     // 32 rows of V, later 16 of O
+  static constexpr int WAVE_BYTES = 64 * DP + 256;     // KEYS rows of V, later 16 of O
   static constexpr int PART = ROWS * (DP + 2);         // floats of a partial result: O, then (m, l) of each row
-  static constexpr int PER_CU = DP > 128 ? 1 : 2;
+  static constexpr int PER_CU = 1;
 };
 
 // Physical 16-byte chunk of chunk c in row r of the V tile.  Values are written 16 rows at a time at one chunk, and
@@ -274,27 +300,60 @@ __device__ __forceinline__ int few_swizzle(int r, int c) {
 }
 
 template <int DP>
-__global__ __launch_bounds__(kThreads, FewTile<DP>::PER_CU) void attn_few_kernel(AttnCall c) {
+__global__ __launch_bounds__(FewTile<DP>::THREADS, FewTile<DP>::PER_CU) void attn_few_kernel(AttnCall c) {
   using T = FewTile<DP>;
-  constexpr int KS = T::KS, DT = T::DT;
+  constexpr int KS = T::KS, DT = T::DT, TILES = T::TILES;
   extern __shared__ __align__(256) unsigned char smem[];  // WAVE_BYTES a wave
-  __shared__ WalkShared sh;
-  __shared__ float ml[kWaves][2][16];
-  __shared__ uint32_t last_one;
+  __shared__ WalkShared<T::THREADS> sh;
+  __shared__ float ml[T::WAVES][2][16];
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
   const int l16 = lane & 15, g = lane >> 4;
   unsigned char *mine = smem + wave * T::WAVE_BYTES;
   const uint32_t mine_lds = lds_address(mine);
-  const int groups = c.cut.parts / c.Hkv;
+  const int me = (int)xcd_remap(blockIdx.x, gridDim.x);
 
-  walk(c, sh, (int)xcd_remap(blockIdx.x, gridDim.x), (int)gridDim.x, [&](const Piece &p) {
-    const int kv = p.part / groups;
-    const Row row = row_of(c, p, groups, l16);
+  walk(c, sh, me, (int)gridDim.x, [&](const Piece &p, const AttnShare &share) {
+    const Row row = row_of(c, p, l16);
     int all_lo, all_hi;
     seen_by_all(c, p, 0, c.cut.tokens, all_lo, all_hi);
     const int32_t *table = c.table + (size_t)p.request * c.table_pitch;
-    const uint16_t *kc = c.k + (size_t)kv * c.cache_head + 8 * g, *vc = c.v + (size_t)kv * c.cache_head + 8 * g;
+    const uint16_t *kc = c.k + (size_t)p.kv * c.cache_head + 8 * g, *vc = c.v + (size_t)p.kv * c.cache_head + 8 * g;
 
+    // A block's keys are asked for when the ones before have been multiplied, its values when those have gone to LDS: one
+    // set of registers each, and something in flight at all times.  The page numbers of the block after
+    // are asked for before either, so that waiting for them does not wait for these.
+    u32x4 k[TILES][KS], v[TILES][KS];
+    int ids[TILES], keys[TILES];
+    int64_t at[TILES];
+    uint32_t bad = 0, next_bad = 0;  // a bit for each key of the block whose page is none
+    auto ask = [&](int b) {
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) {
+        keys[t] = min(p.first + b * T::KEYS + 16 * t + l16, p.last - 1);
+        ids[t] = table[c.by_page(keys[t])];
+      }
+    };
+    auto load = [&](u32x4 (&to)[TILES][KS], const uint16_t *from) {
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          to[t][s] = u32x4{0u, 0u, 0u, 0u};
+          if (32 * s + 8 * g < c.D) to[t][s] = *reinterpret_cast<const u32x4 *>(from + at[t] + 32 * s);
+        }
+    };
+    auto load_keys = [&](int b) {
+      next_bad = 0;
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) {
+        const KeyRow r = key_row(c, keys[t], ids[t]);
+        at[t] = r.at;
+        next_bad |= ((uint32_t)__ballot(r.bad) & 0xFFFFu) << (16 * t);
+      }
+      if (b + T::WAVES < p.b1) ask(b + T::WAVES);
+      load(k, kc);
+    };
+    if (p.b0 + wave < p.b1) ask(p.b0 + wave);
     u32x4 q[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
@@ -302,58 +361,50 @@ __global__ __launch_bounds__(kThreads, FewTile<DP>::PER_CU) void attn_few_kernel
       if (row.valid && 32 * s + 8 * g < c.D)
         q[s] = *reinterpret_cast<const u32x4 *>(c.q + (size_t)row.token * c.q_row + (size_t)row.head * c.q_head + 32 * s + 8 * g);
     }
+    if (p.b0 + wave < p.b1) {
+      load_keys(p.b0 + wave);
+      load(v, vc);
+    }
     f32x4 acc[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
 
-    for (int b = p.b0 + wave; b < p.b1; b += kWaves) {
+#pragma unroll 1
+    for (int b = p.b0 + wave; b < p.b1; b += T::WAVES) {
       const int kb = p.first + b * T::KEYS;
-      u32x4 k[2][KS], v[2][KS];
-      uint64_t bad[2];
+      const bool more = b + T::WAVES < p.b1;
+      bad = next_bad;
+      f32x4 x[TILES];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const KeyRow r = key_row(c, table, min(kb + 16 * t + l16, p.last - 1));
-        bad[t] = __ballot(r.bad);
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-          k[t][s] = v[t][s] = u32x4{0u, 0u, 0u, 0u};
-          if (32 * s + 8 * g < c.D) {
-            k[t][s] = *reinterpret_cast<const u32x4 *>(kc + r.at + 32 * s);
-            v[t][s] = *reinterpret_cast<const u32x4 *>(vc + r.at + 32 * s);
-          }
-        }
-      }
-      f32x4 x[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
+      for (int t = 0; t < TILES; ++t) {
         x[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < KS; ++s) x[t] = mfma16(k[t][s], q[s], x[t]);
       }
+      if (more) load_keys(b + T::WAVES);
       // a lane's scores are of keys 16 t + 4 g + i
-      const bool masked = kb < all_lo || kb + T::KEYS > all_hi || ((bad[0] | bad[1]) & 0xFFFFu) != 0;
-      if (masked) {
+      if (kb < all_lo || kb + T::KEYS > all_hi || bad != 0) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < TILES; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int at = 16 * t + 4 * g + i;
-            const bool seen = kb + at >= row.lo && kb + at < row.hi && !((bad[t] >> (4 * g + i)) & 1u);
+            const int key = 16 * t + 4 * g + i;
+            const bool seen = kb + key >= row.lo && kb + key < row.hi && !((bad >> key) & 1u);
             x[t][i] = seen ? x[t][i] : -INFINITY;
           }
       }
       float top = x[0][0];
 #pragma unroll
-      for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i >> 2][i & 3]);
+      for (int i = 1; i < 4 * TILES; ++i) top = fmaxf(top, x[i >> 2][i & 3]);
       top = fmaxf(m, max_quarters(top) * c.scale);
       const float by = top == -INFINITY ? 0.f : top;
       const float less = exp2_(m - by);
       m = top;
       l = l * less;
-      float e[8];
+      float e[8] = {};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < 4 * TILES; ++i) {
         e[i] = exp2_(__builtin_fmaf(x[i >> 2][i & 3], c.scale, -by));
         l = l + e[i];
       }
@@ -366,39 +417,59 @@ __global__ __launch_bounds__(kThreads, FewTile<DP>::PER_CU) void attn_few_kernel
 #pragma unroll
       for (int t = 0; t < DT; ++t) acc[t] = acc[t] * less;
       // values: 16 rows at one chunk at a time
+      auto put_values = [&]() {
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < TILES; ++t)
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-          const int r = 16 * t + l16;
-          *reinterpret_cast<u32x4 *>(mine + r * T::PITCH + few_swizzle<DP>(r, 4 * s + g) * 16) = v[t][s];
-        }
-      asm volatile("" ::: "memory");  // the wave's LDS accesses are served in order
-      const int vr = 4 * g + (l16 >> 2);
-      const uint32_t v0 = mine_lds + vr * T::PITCH + few_swizzle<DP>(vr, (l16 & 3) >> 1) * 16 + 8 * (l16 & 1);
+          for (int s = 0; s < KS; ++s) {
+            const int r = 16 * t + l16;
+            *reinterpret_cast<u32x4 *>(mine + r * T::PITCH + few_swizzle<DP>(r, 4 * s + g) * 16) = v[t][s];
+          }
+        asm volatile("" ::: "memory");  // the wave's LDS accesses are served in order
+      };
+      put_values();
+      // a value that a row does not see must not reach it, whatever it is, and one that it sees must not meet the
+      // lower half of a weight, which may be 0: infinities and NaN go in one by one
+      uint32_t odd = 0;
 #pragma unroll
-      for (int t = 0; t < DT; ++t) {
-        const uint32_t at = (v0 ^ ((t & 7) * 32)) + (t >> 3) * 256;
-        const u32x2 a = read_transposed(at), b2 = read_transposed(at + 16 * T::PITCH);
-        u32x4 vt = {a[0], a[1], b2[0], b2[1]};
-        // a value that a row does not see must not reach it, whatever it is, and one that it sees must not meet the
-        // lower half of a weight, which may be 0: infinities and NaN go in one by one
-        const bool odd = pair_nonfinite(vt[0]) || pair_nonfinite(vt[1]) || pair_nonfinite(vt[2]) || pair_nonfinite(vt[3]);
-        if (__ballot(odd) != 0) {
+      for (int t = 0; t < TILES; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) vt[i] = pair_finite(vt[i]);
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) odd |= pair_exponents(v[t][s][i]);
+      if (__ballot((odd & 0x80008000u) != 0) != 0) {
 #pragma unroll 1
-          for (int r = 0; r < T::KEYS; ++r) {
-            const uint64_t w = *reinterpret_cast<const uint64_t *>(
+        for (int r = 0; r < T::KEYS; ++r) {
+          const bool seen = kb + r >= row.lo && kb + r < row.hi && !((bad >> r) & 1u);
+#pragma unroll
+          for (int t = 0; t < DT; ++t) {
+            const uint64_t four = *reinterpret_cast<const uint64_t *>(
                 mine + r * T::PITCH + few_swizzle<DP>(r, 2 * t + (g >> 1)) * 16 + 8 * (g & 1));
-            const bool seen = kb + r >= row.lo && kb + r < row.hi && !((bad[r >> 4] >> (r & 15)) & 1u);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const uint32_t h = (uint32_t)(w >> (16 * i)) & 0xFFFFu;
+              const uint32_t h = (uint32_t)(four >> (16 * i)) & 0xFFFFu;
               if (seen && (h & 0x7F80u) == 0x7F80u) acc[t][i] = acc[t][i] + as_float(h << 16);
             }
           }
         }
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+          for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[t][s][i] = pair_finite(v[t][s][i]);
+        put_values();
+      }
+      if (more) load(v, vc);
+      const int vr = 4 * g + (l16 >> 2);
+      const uint32_t v0 = mine_lds + vr * T::PITCH + few_swizzle<DP>(vr, (l16 & 3) >> 1) * 16 + 8 * (l16 & 1);
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        const uint32_t from = (v0 ^ ((t & 7) * 32)) + (t >> 3) * 256;
+        const u32x2 a = read_transposed(from);
+        u32x2 b2 = {0u, 0u};
+        if constexpr (TILES == 2) b2 = read_transposed(from + 16 * T::PITCH);
+        const u32x4 vt = {a[0], a[1], b2[0], b2[1]};
         acc[t] = mfma16(vt, hi, acc[t]);
         acc[t] = mfma16(vt, lo, acc[t]);
       }
@@ -412,92 +483,91 @@ __global__ __launch_bounds__(kThreads, FewTile<DP>::PER_CU) void attn_few_kernel
 #pragma unroll
     for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4 *>(o + l16 * T::O_PITCH + 16 * t + 4 * g) = acc[t];
     __syncthreads();
-    constexpr int CH = DP / 8;  // pieces of 8 values in a row
-    const int slots = (int)gridDim.x * 2;
-    const auto rs = rsrc_of(c.part, (uint32_t)(slots * T::PART * 4));
-    const int me = (int)xcd_remap(blockIdx.x, gridDim.x);
-    auto finish = [&](int r, int ch, const float (&v)[8], float top, float sum) {
-      const Row w = row_of(c, p, groups, r);
-      if (!w.valid) return;
-      const float by = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-      if (8 * ch < c.D) {
-        u32x4 h;
+    constexpr int CH = DP / 4;  // pieces of 4 values in a row
+    constexpr int PASSES = (16 * CH + T::THREADS - 1) / T::THREADS;
+    const auto rs = rsrc_of(c.part, gridDim.x * 2u * (uint32_t)(T::PART * 4));
+    f32x4 sum[PASSES];
+    f32x2 ms[PASSES];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = pack_bf16(v[2 * i] * by, v[2 * i + 1] * by);
-        *reinterpret_cast<u32x4 *>(c.out + (size_t)w.token * c.out_row + (size_t)w.head * c.out_head + 8 * ch) = h;
-      }
-      if (ch == 0 && c.lse != nullptr)
-        c.lse[(size_t)w.token * c.Hq + w.head] = sum > 0.f || sum != sum ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
-    };
-    for (int e = threadIdx.x; e < 16 * CH; e += kThreads) {
-      const int r = e / CH, ch = e % CH;
-      float top = -INFINITY;
+    for (int n = 0; n < PASSES; ++n) {
+      const int e = n * T::THREADS + (int)threadIdx.x, r = e / CH, ch = e % CH;
+      sum[n] = f32x4{0.f, 0.f, 0.f, 0.f}, ms[n] = f32x2{-INFINITY, 0.f};
+      if (r >= 16) continue;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w][0][r]);
-      const float by = top == -INFINITY ? 0.f : top;
-      float sum = 0.f, v[8] = {};
+      for (int w = 0; w < T::WAVES; ++w) ms[n][0] = fmaxf(ms[n][0], ml[w][0][r]);
+      const float by = ms[n][0] == -INFINITY ? 0.f : ms[n][0];
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
+      for (int w = 0; w < T::WAVES; ++w) {
         const float f = exp2_(ml[w][0][r] - by);
-        sum = __builtin_fmaf(ml[w][1][r], f, sum);
-        const float *ow = reinterpret_cast<const float *>(smem + w * T::WAVE_BYTES) + r * T::O_PITCH + 8 * ch;
+        ms[n][1] = __builtin_fmaf(ml[w][1][r], f, ms[n][1]);
+        const f32x4 ow = *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(smem + w * T::WAVE_BYTES) + r * T::O_PITCH + 4 * ch);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(ow[i], f, v[i]);
+        for (int i = 0; i < 4; ++i) sum[n][i] = __builtin_fmaf(ow[i], f, sum[n][i]);
       }
-      if (p.alone) {
-        finish(r, ch, v, top, sum);
-      } else {
-        const uint32_t slot = (uint32_t)(2 * me + (p.began ? 1 : 0)) * (T::PART * 4);
-        const uint32_t at = slot + (uint32_t)(r * DP + 8 * ch) * 4u;
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]}), rs, (int)at, 0, kDevice);
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]}), rs, (int)at + 16, 0, kDevice);
+      if (!p.alone) {
+        const uint32_t slot = place_of(me, p.began, T::PART);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, sum[n]), rs, (int)(slot + (uint32_t)(r * DP + 4 * ch) * 4u), 0, kDevice);
         if (ch == 0)
-          __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f32x2{top, sum}), rs,
-                                                (int)(slot + (uint32_t)(16 * DP + 2 * r) * 4u), 0, kDevice);
+          __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, ms[n]), rs, (int)(slot + (uint32_t)(16 * DP + 2 * r) * 4u), 0, kDevice);
       }
     }
+    bool write = true;
     if (!p.alone) {
-      stores_done();
-      const int parts = p.owners.to - p.owners.from;
-      if (threadIdx.x == 0) {
-        const bool last = add_device(c.joined + p.owners.from) + 1 == (uint32_t)parts;
-        if (last) put_device(c.joined + p.owners.from, 0u);  // for the next call
-        last_one = last;
-      }
-      __syncthreads();
-      if (last_one != 0u) {
-        for (int e = threadIdx.x; e < 16 * CH; e += kThreads) {
-          const int r = e / CH, ch = e % CH;
-          float top = -INFINITY, sum = 0.f, v[8] = {};
-          for (int w0 = 0; w0 < parts; w0 += 4) {
-            f32x4 a[4], b[4];
-            f32x2 t[4];
+      const AttnOwners o = attn_owners(c.cut, p.it, share);
+      const int from = uniform(o.from), parts = uniform(o.to) - from;
+      write = last_of(c, sh, AttnOwners{from, from + parts});
+      if (write) {
+        // the item's first part may be of the share that it begins in
+        const bool in_first = p.it.at >= (int64_t)from * share.units;
+#pragma unroll 1
+        for (int n = 0; n < PASSES; ++n) {
+          const int e = n * T::THREADS + (int)threadIdx.x, r = min(e / CH, 15), ch = e % CH;
+          f32x4 v4 = {0.f, 0.f, 0.f, 0.f};
+          f32x2 t2 = {-INFINITY, 0.f};
+#pragma unroll 1
+          for (int w0 = 0; w0 < parts; w0 += 8) {
+            f32x4 a[8];
+            f32x2 t[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int w = p.owners.from + min(w0 + j, parts - 1);
-              // the item's first part may be of a share that it begins in
-              const uint32_t slot = (uint32_t)(2 * w + (w == p.owners.from && p.first_began ? 1 : 0)) * (T::PART * 4);
-              const uint32_t at = slot + (uint32_t)(r * DP + 8 * ch) * 4u;
-              a[j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)at, 0, kDevice));
-              b[j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)at + 16, 0, kDevice));
+            for (int j = 0; j < 8; ++j) {
+              const int w = min(w0 + j, parts - 1);
+              const uint32_t slot = place_of(from + w, w == 0 && in_first, T::PART);
+              a[j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(slot + (uint32_t)(r * DP + 4 * ch) * 4u), 0, kDevice));
               t[j] = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, (int)(slot + (uint32_t)(16 * DP + 2 * r) * 4u), 0, kDevice));
             }
+            float now = t2[0];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              if (w0 + j >= parts) break;
-              const float now = fmaxf(top, t[j][0]), by = now == -INFINITY ? 0.f : now;
-              const float f0 = exp2_(top - by), f1 = exp2_(t[j][0] - by);
-              top = now;
-              sum = __builtin_fmaf(t[j][1], f1, sum * f0);
+            for (int j = 0; j < 8; ++j) now = fmaxf(now, t[j][0]);
+            const float by = now == -INFINITY ? 0.f : now, f0 = exp2_(t2[0] - by);
+            t2[0] = now, t2[1] = t2[1] * f0, v4 = v4 * f0;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                v[i] = __builtin_fmaf(a[j][i], f1, v[i] * f0);
-                v[4 + i] = __builtin_fmaf(b[j][i], f1, v[4 + i] * f0);
-              }
+            for (int j = 0; j < 8; ++j) {
+              const float f = w0 + j < parts ? exp2_(t[j][0] - by) : 0.f;
+              if (w0 + j >= parts) continue;
+              t2[1] = __builtin_fmaf(t[j][1], f, t2[1]);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) v4[i] = __builtin_fmaf(a[j][i], f, v4[i]);
             }
           }
-          finish(r, ch, v, top, sum);
+          if (PASSES == 1 || n == 0) sum[0] = v4, ms[0] = t2;
+          else sum[PASSES - 1] = v4, ms[PASSES - 1] = t2;
         }
+      }
+    }
+    if (write) {
+#pragma unroll
+      for (int n = 0; n < PASSES; ++n) {
+        const int e = n * T::THREADS + (int)threadIdx.x, r = e / CH, ch = e % CH;
+        const Row w = row_of(c, p, min(r, 15));
+        if (r >= 16 || !w.valid) continue;
+        const float total = ms[n][1];
+        const bool some = total > 0.f || total != total;
+        const float by = some ? 1.f / total : 0.f;
+        if (4 * ch < c.D)
+          *reinterpret_cast<u32x2 *>(c.out + (size_t)w.token * c.out_row + (size_t)w.head * c.out_head + 4 * ch) =
+              u32x2{pack_bf16(sum[n][0] * by, sum[n][1] * by), pack_bf16(sum[n][2] * by, sum[n][3] * by)};
+        if (ch == 0 && c.lse != nullptr)
+          c.lse[(size_t)w.token * c.Hq + w.head] = some ? (ms[n][0] + __builtin_amdgcn_logf(total)) * kLn2 : -INFINITY;
       }
     }
     __syncthreads();
@@ -514,13 +584,14 @@ __global__ __launch_bounds__(kThreads, FewTile<DP>::PER_CU) void attn_few_kernel
 // bits) is of the same size as the output's own; l sums them unrounded.
 template <int DP>
 struct ManyTile {
+  static constexpr int THREADS = 256;
   static constexpr int ROWS = 128, KEYS = 64;
   static constexpr int KS = DP / 16, DT = DP / 32;
   static constexpr int CH = DP / 8;                    // 16-byte chunks of a row
   static constexpr int PITCH = DP * 2;
   static constexpr int OPERAND = KEYS * PITCH;         // bytes of a tile of K, and of V
   static constexpr int STAGE = 2 * OPERAND;
-  static constexpr int PASS_ROWS = kThreads / CH, PASSES = KEYS / PASS_ROWS;
+  static constexpr int PASS_ROWS = THREADS / CH, PASSES = KEYS / PASS_ROWS;
   static constexpr int PART = ROWS * (DP + 2);
   static constexpr int PER_CU = DP > 128 ? 1 : 2;
 };
@@ -549,34 +620,30 @@ __device__ __forceinline__ void global_dma16(const void *from, uint32_t lds) {
 #pragma clang diagnostic pop
 
 template <int DP>
-__global__ __launch_bounds__(kThreads, ManyTile<DP>::PER_CU) void attn_many_kernel(AttnCall c) {
+__global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void attn_many_kernel(AttnCall c) {
   using T = ManyTile<DP>;
   constexpr int KS = T::KS, DT = T::DT;
   extern __shared__ __align__(256) unsigned char stages[];
-  __shared__ WalkShared sh;
+  __shared__ WalkShared<T::THREADS> sh;
   __shared__ uint32_t bad_rows[3][2];
-  __shared__ uint32_t last_one;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
   const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
   const uint32_t lds0 = lds_address(stages);
-  const int groups = c.cut.parts / c.Hkv;
-  const int slots = (int)gridDim.x * 2;
-  const auto rs = rsrc_of(c.part, (uint32_t)slots * (uint32_t)(T::PART * 4));
+  const auto rs = rsrc_of(c.part, gridDim.x * 2u * (uint32_t)(T::PART * 4));
   const int me = (int)xcd_remap(blockIdx.x, gridDim.x);
 
   // chunks that the heads do not have stay zero
   if (c.D < DP)
-    for (int i = threadIdx.x; i < 2 * T::STAGE / 16; i += kThreads) reinterpret_cast<u32x4 *>(stages)[i] = u32x4{0u, 0u, 0u, 0u};
+    for (int i = threadIdx.x; i < 2 * T::STAGE / 16; i += T::THREADS) reinterpret_cast<u32x4 *>(stages)[i] = u32x4{0u, 0u, 0u, 0u};
   if (threadIdx.x < 6) (&bad_rows[0][0])[threadIdx.x] = 0u;
   __syncthreads();
 
-  walk(c, sh, me, (int)gridDim.x, [&](const Piece &p) {
-    const int kv = p.part / groups;
-    const Row row = row_of(c, p, groups, wave * 32 + l32);
+  walk(c, sh, me, (int)gridDim.x, [&](const Piece &p, const AttnShare &share) {
+    const Row row = row_of(c, p, wave * 32 + l32);
     int all_lo, all_hi;
-    seen_by_all(c, p, wave * 32 / c.heads, (wave * 32 + 31) / c.heads + 1, all_lo, all_hi);
+    seen_by_all(c, p, c.by_heads(wave * 32), c.by_heads(wave * 32 + 31) + 1, all_lo, all_hi);
     const int32_t *table = c.table + (size_t)p.request * c.table_pitch;
-    const uint16_t *kc = c.k + (size_t)kv * c.cache_head, *vc = c.v + (size_t)kv * c.cache_head;
+    const uint16_t *kc = c.k + (size_t)p.kv * c.cache_head, *vc = c.v + (size_t)p.kv * c.cache_head;
     const int r_in = threadIdx.x / T::CH, chunk = threadIdx.x % T::CH;
 
     auto issue = [&](int b) {
@@ -585,7 +652,8 @@ __global__ __launch_bounds__(kThreads, ManyTile<DP>::PER_CU) void attn_many_kern
 #pragma unroll
       for (int i = 0; i < T::PASSES; ++i) {
         const int r = i * T::PASS_ROWS + r_in;
-        const KeyRow kr = key_row(c, table, min(p.first + b * T::KEYS + r, p.last - 1));
+        const int key = min(p.first + b * T::KEYS + r, p.last - 1);
+        const KeyRow kr = key_row(c, key, table[c.by_page(key)]);
         if (kr.bad && chunk == 0) atomicOr(&bad_rows[flags][r >> 5], 1u << (r & 31));
         const int ck = many_swizzle_k<DP>(r, chunk), cv = many_swizzle_v<DP>(r, chunk);
         if (8 * ck < c.D) global_dma16(kc + kr.at + 8 * ck, to + (uint32_t)i * 4096u);
@@ -707,8 +775,9 @@ __global__ __launch_bounds__(kThreads, ManyTile<DP>::PER_CU) void attn_many_kern
     l = sum_halves(l);
 
     const int r = wave * 32 + l32;
+    bool write = true;
     if (!p.alone) {
-      const uint32_t slot = (uint32_t)(2 * me + (p.began ? 1 : 0)) * (uint32_t)(T::PART * 4);
+      const uint32_t slot = place_of(me, p.began, T::PART);
 #pragma unroll
       for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -720,15 +789,11 @@ __global__ __launch_bounds__(kThreads, ManyTile<DP>::PER_CU) void attn_many_kern
       if (half == 0)
         __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f32x2{m, l}), rs,
                                               (int)(slot + (uint32_t)(T::ROWS * DP + 2 * r) * 4u), 0, kDevice);
-      stores_done();
-      const int parts = p.owners.to - p.owners.from;
-      if (threadIdx.x == 0) {
-        const bool last = add_device(c.joined + p.owners.from) + 1 == (uint32_t)parts;
-        if (last) put_device(c.joined + p.owners.from, 0u);  // for the next call
-        last_one = last;
-      }
-      __syncthreads();
-      if (last_one != 0u) {
+      const AttnOwners o = attn_owners(c.cut, p.it, share);
+      const int from = uniform(o.from), parts = uniform(o.to) - from;
+      write = last_of(c, sh, AttnOwners{from, from + parts});
+      if (write) {
+        const bool in_first = p.it.at >= (int64_t)from * share.units;
         m = -INFINITY, l = 0.f;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
@@ -736,8 +801,7 @@ __global__ __launch_bounds__(kThreads, ManyTile<DP>::PER_CU) void attn_many_kern
           for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
 #pragma unroll 1
         for (int s = 0; s < parts; ++s) {
-          const int from = p.owners.from + s;
-          const uint32_t slot = (uint32_t)(2 * from + (s == 0 && p.first_began ? 1 : 0)) * (uint32_t)(T::PART * 4);
+          const uint32_t slot = place_of(from + s, s == 0 && in_first, T::PART);
           const f32x2 t2 = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, (int)(slot + (uint32_t)(T::ROWS * DP + 2 * r) * 4u), 0, kDevice));
           const float now = fmaxf(m, t2[0]), by = now == -INFINITY ? 0.f : now;
           const float f0 = exp2_(m - by), f1 = exp2_(t2[0] - by);
@@ -755,7 +819,7 @@ __global__ __launch_bounds__(kThreads, ManyTile<DP>::PER_CU) void attn_many_kern
         }
       }
     }
-    if ((p.alone || last_one != 0u) && row.valid) {
+    if (write && row.valid) {
       const bool some = l > 0.f || l != l;
       const float by = some ? 1.f / l : 0.f;
       uint16_t *to = c.out + (size_t)row.token * c.out_row + (size_t)row.head * c.out_head;
@@ -790,7 +854,7 @@ int launch(const AttnCall &c, int grid, hipStream_t s) {
   void (*fn)(AttnCall);
   if constexpr (MANY) fn = attn_many_kernel<DP>;
   else fn = attn_few_kernel<DP>;
-  constexpr int lds = MANY ? 2 * ManyTile<DP>::STAGE : kWaves * FewTile<DP>::WAVE_BYTES;
+  constexpr int lds = MANY ? 2 * ManyTile<DP>::STAGE : FewTile<DP>::WAVES * FewTile<DP>::WAVE_BYTES;
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return OCC_ENODEV;
   static Once limit_set[kMaxDevices];
@@ -798,7 +862,7 @@ int launch(const AttnCall &c, int grid, hipStream_t s) {
         return hipFuncSetAttribute(reinterpret_cast<const void *>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
       }))
     return OCC_EHIP;
-  hipLaunchKernelGGL(fn, dim3(grid), dim3(kThreads), lds, s, c);
+  hipLaunchKernelGGL(fn, dim3(grid), dim3(MANY ? ManyTile<DP>::THREADS : FewTile<DP>::THREADS), lds, s, c);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
 }
 template <bool MANY>
@@ -841,12 +905,14 @@ int attn_launch(const occ_attn_args &a, hipStream_t s) {
     AttnCall k = c;
     const int rows = many ? ManyTile<128>::ROWS : FewTile<128>::ROWS;
     k.heads = std::min(c.group, rows);
-    k.cut.tokens = rows / k.heads;
-    k.cut.parts = a.Hkv * ((c.group + k.heads - 1) / k.heads);
-    k.cut.fixed = many ? 64 : 32, k.cut.block = many ? ManyTile<128>::KEYS : FewTile<128>::KEYS;
-    k.cut.window = a.window, k.cut.causal = a.causal != 0;
+    k.cut.tokens = rows / k.heads, k.cut.by_tokens = Divider(k.cut.tokens);
+    k.groups = (c.group + k.heads - 1) / k.heads;
+    k.by_heads = Divider(k.heads), k.by_groups = Divider(k.groups);
+    k.cut.parts = a.Hkv * k.groups;
+    k.cut.fixed = many ? 64 : 32, k.cut.block = many ? ManyTile<128>::KEYS : DP > 128 ? FewTile<256>::KEYS : FewTile<128>::KEYS;
+    k.cut.window = a.window < c.keys ? a.window : 0, k.cut.causal = a.causal != 0;
     k.least = least, k.most = most;
-    k.min_share = 256;
+    k.min_share = many ? 256 : 512;
     const int grid = workgroups_of(many, DP, cus);
     return many ? launch<true>(k, DP, grid, s) : launch<false>(k, DP, grid, s);
   };

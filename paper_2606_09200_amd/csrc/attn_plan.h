@@ -7,14 +7,9 @@
 // keys, many short ones are dealt out whole.
 #pragma once
 
-#include <stdint.h>
+#include "divider.h"
 
-#if defined(__HIPCC__)
-#include <hip/hip_runtime.h>
-#define OCC_PLAN __host__ __device__ __forceinline__
-#else
-#define OCC_PLAN inline
-#endif
+#define OCC_PLAN OCC_DIVIDE
 
 namespace occ {
 
@@ -22,9 +17,10 @@ struct AttnCut {
   int tokens;   // of a tile
   int parts;    // groups of heads
   int fixed;    // keys' worth of an item's beginning and end
-  int block;    // keys that a share is a multiple of
+  int block;    // keys that are computed at once, a power of two
   int window;   // 0: none
   int causal;
+  Divider by_tokens;
 };
 
 struct AttnSeq {
@@ -40,7 +36,7 @@ OCC_PLAN AttnSeq attn_seq(int start, int end, int len, int rows, int most) {
   return AttnSeq{a, b - a, len < 0 ? 0 : len > most ? most : len};
 }
 
-OCC_PLAN int attn_tiles(const AttnCut &c, const AttnSeq &s) { return (s.fresh + c.tokens - 1) / c.tokens; }
+OCC_PLAN int attn_tiles(const AttnCut &c, const AttnSeq &s) { return c.by_tokens(s.fresh + c.tokens - 1); }
 
 // Keys [first, last) that some token of tile m sees.
 OCC_PLAN int attn_last_key(const AttnCut &c, const AttnSeq &s, int m) {
@@ -56,10 +52,12 @@ OCC_PLAN int attn_first_key(const AttnCut &c, const AttnSeq &s, int m) {
   return at < 0 ? 0 : at > last ? last : (int)at;
 }
 
-// Sum over j < n of max(0, a + j step).
-OCC_PLAN int64_t attn_ramp(int64_t n, int64_t a, int64_t step) {
-  const int64_t skip = a < 0 ? (-a + step - 1) / step : 0;
-  if (n <= skip) return 0;
+// Sum over j < n of max(0, a + j tokens).
+OCC_PLAN int64_t attn_ramp(const AttnCut &c, int n, int64_t a) {
+  const int64_t step = c.tokens;
+  if (n <= 0 || a + (n - 1) * step <= 0) return 0;
+  // here -a < (n - 1) step, at most a request's rows
+  const int skip = a < 0 ? c.by_tokens((int)(-a + step - 1)) : 0;
   const int64_t count = n - skip;
   return count * (a + skip * step) + step * (count * (count - 1) / 2);
 }
@@ -69,14 +67,14 @@ OCC_PLAN int64_t attn_units_before(const AttnCut &c, const AttnSeq &s, int m) {
   const int64_t base = (int64_t)s.len - s.fresh;
   int64_t keys;
   if (c.causal) {
-    keys = attn_ramp(m, base + c.tokens, c.tokens);
+    keys = attn_ramp(c, m, base + c.tokens);
     // the last tile may have fewer tokens
     const int64_t over = base + (int64_t)m * c.tokens;
     if (m > 0 && (int64_t)m * c.tokens > s.fresh) keys -= (over > 0 ? over : 0) - s.len;
   } else {
     keys = (int64_t)m * s.len;
   }
-  if (c.window) keys -= attn_ramp(m, base - c.window + 1, c.tokens);
+  if (c.window) keys -= attn_ramp(c, m, base - c.window + 1);
   return keys + (int64_t)m * c.fixed;
 }
 
@@ -106,7 +104,27 @@ struct AttnItem {
 OCC_PLAN int attn_blocks_before(const AttnCut &c, const AttnItem &it, int64_t x) {
   int64_t k = x - it.at - c.fixed;
   k = k < 0 ? 0 : k > it.keys ? it.keys : k;
-  return ((int)k + c.block - 1) / c.block;
+  return (int)((k + c.block - 1) / c.block);
+}
+
+// The share that a unit lies in, below 2^53 units and 2^31 shares: a product in binary64 is off by less than one of them.
+struct AttnShare {
+  int64_t units;
+  double per_unit;
+  OCC_PLAN int operator()(int64_t x) const {
+    int q = (int)((double)x * per_unit);
+    const int64_t left = x - q * units;
+    if (left < 0) --q;
+    if (left >= units) ++q;
+    return q;
+  }
+};
+// `total` units in at most `shares` of them, of `least` units or more.
+OCC_PLAN AttnShare attn_share(int64_t total, int shares, int least) {
+  // rounded up, or one more
+  int64_t units = (int64_t)((double)total / shares) + 1;
+  if (units < least) units = least;
+  return AttnShare{units, 1.0 / (double)units};
 }
 
 // Who computes an item's blocks: shares [from, to), each of them some (a share is no shorter than a block); without
@@ -114,10 +132,10 @@ OCC_PLAN int attn_blocks_before(const AttnCut &c, const AttnItem &it, int64_t x)
 struct AttnOwners {
   int from, to;
 };
-OCC_PLAN AttnOwners attn_owners(const AttnCut &c, const AttnItem &it, int64_t share) {
-  if (it.keys == 0) return AttnOwners{(int)(it.at / share), (int)(it.at / share)};
+OCC_PLAN AttnOwners attn_owners(const AttnCut &c, const AttnItem &it, const AttnShare &share) {
+  if (it.keys == 0) return AttnOwners{share(it.at), share(it.at)};
   const int64_t last = (int64_t)(it.keys - 1) / c.block * c.block;
-  return AttnOwners{(int)((it.at + c.fixed) / share), (int)((it.at + c.fixed + last) / share) + 1};
+  return AttnOwners{share(it.at + c.fixed), share(it.at + c.fixed + last) + 1};
 }
 
 }  // namespace occ

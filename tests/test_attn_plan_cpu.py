@@ -46,13 +46,16 @@ static void line(const AttnCut &c, const std::vector<AttnSeq> &seqs, int workgro
       if (attn_units_before(c, s, tiles) != before) ++bad;
     }
   }
-  const int64_t total = at, share = std::max<int64_t>(min_share, (total + workgroups - 1) / workgroups);
-  if (share * workgroups < total) ++bad;
+  const int64_t total = at;
+  const AttnShare cutter = attn_share(total, workgroups, min_share);
+  const int64_t share = cutter.units;
+  if (share * workgroups < total || share < min_share) ++bad;
+  if (share > min_share && (share - 2) * workgroups > total) ++bad;
   std::set<int> counters;
   std::set<std::pair<int, int>> slots;
   for (const AttnItem &it : items) {
     ++items_seen;
-    const AttnOwners o = attn_owners(c, it, share);
+    const AttnOwners o = attn_owners(c, it, cutter);
     const int blocks = (it.keys + c.block - 1) / c.block;
     int next = 0;
     const int64_t end = it.at + c.fixed + it.keys;
@@ -80,6 +83,7 @@ int main() {
   for (int n = 0; n < 3000; ++n) {
     AttnCut c;
     c.tokens = pick({1, 2, 4, 16, 18, 128});
+    c.by_tokens = Divider(c.tokens);
     c.parts = pick({1, 2, 8});
     c.block = pick({32, 64});
     c.fixed = pick({0, 1, 32, 64, 300}) + (n % 2 ? 32 : 1);
@@ -95,13 +99,21 @@ int main() {
     line(c, seqs, pick({1, 2, 7, 256, 512}), pick({64, 256, 256}));
   }
   // sizes near the limits: no sum leaves 64 bits, no key 31
-  AttnCut c{2, 8, 32, 32, 0, 1};
+  AttnCut c{2, 8, 32, 32, 0, 1, Divider(2)};
   const AttnSeq big{0, 1 << 24, 2147418112};
   if (attn_units(c, big) <= 0 || attn_last_key(c, big, attn_tiles(c, big) - 1) != big.len) ++bad;
   c.window = 1 << 30;
   if (attn_units(c, big) <= 0 || attn_first_key(c, big, 0) != big.len - big.fresh - c.window + 1) ++bad;
   const AttnSeq s = attn_seq(-5, 2000000000, -7, 100, 1000), e = attn_seq(50, 20, 5000, 100, 1000);
   if (s.first != 0 || s.fresh != 100 || s.len != 0 || e.first != 50 || e.fresh != 0 || e.len != 1000) ++bad;
+  // shares of far units
+  for (int n = 0; n < 2000000; ++n) {
+    const int64_t total = ((int64_t)g() << 20 | g() >> 12) >> pick({0, 3, 10, 20, 30, 40});
+    const AttnShare by = attn_share(total, pick({1, 7, 256, 512}), pick({32, 256}));
+    const int64_t x = total == 0 ? 0 : (((int64_t)g() << 31 | g()) % total) / pick({1, 1, 1000});
+    const int64_t y = x / by.units * by.units;   // the first of its share
+    if (by(x) != x / by.units || by(y) != y / by.units || (y > 0 && by(y - 1) != (y - 1) / by.units)) ++bad;
+  }
   printf("bad %ld items %ld split %ld\n", bad, items_seen, split);
   return bad != 0 || split < 1000;
 }
