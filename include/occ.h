@@ -721,6 +721,7 @@ int occ_rope(const occ_rope_args *args, void *stream);
  * over j < lens[i], j <= pos (causal != 0) and j > pos - window (window > 0), but not keys whose page is not in [0, pages).
  * Where nothing is left, o is 0 and lse -inf; what is not seen has no influence, infinities and NaN neither.  lens[i] <= 0
  * leaves nothing; rows of no request keep what out and lse hold; lengths beyond width * page (or OCC_ATTN_MAX_KEYS) are cut.
+ * starts ascend; a row that two requests have all the same gets the result of either.
  * Logits, sums and o are fp32; weights p take part in the sum with v as bf16 (two of them where a request has few
  * rows), out is bf16 and lse (rows x Hq, null: not stored) fp32.
  * max_fresh: the most rows of a request; what the choice of kernels goes by (results hold for any).

@@ -99,7 +99,7 @@ struct AttnCall {
   float scale;         // of the exponent of 2
   AttnCut cut;
   int least, most;     // requests of `least` to `most` rows (tokens x heads of a group) are this launch's
-  int min_share;
+  int min_share, least_even, spare;
   uint32_t *joined;    // per share: finished parts of the item that begins in it
   float *part;
 };
@@ -124,7 +124,7 @@ __device__ __forceinline__ KeyRow key_row(const AttnCall &c, int key, int id) {
 
 template <int THREADS>
 struct WalkShared {
-  int64_t wave[THREADS / 64];
+  int64_t sums[2][THREADS / 64];
   int64_t at;
   int request;
   uint32_t last_one;
@@ -139,111 +139,220 @@ struct Piece {
   int first, last, b0, b1;
   bool began;  // the item begins in this share
   bool alone;  // nobody else has a part of it
+  int even;    // workgroups that have an even part of it, from `base` on; 0: the item is on the line
+  int base;
 };
 
-// Calls work(piece, share) for every item of share `me` of the line.
-template <int THREADS, class F>
-__device__ __forceinline__ void walk(const AttnCall &c, WalkShared<THREADS> &sh, int me, int shares, F work) {
-  const AttnCut &cut = c.cut;
-  // units of all requests before each thread's own
-  const int per = (c.n + THREADS - 1) / THREADS;
-  const int r0 = min((int)threadIdx.x * per, c.n), r1 = min(r0 + per, c.n);
-  int64_t own = 0;
-#pragma unroll 1
-  for (int i = r0; i < r1; ++i) {
-    const AttnSeq s = seq_of(c, i);
-    if (per == 1) sh.seq[threadIdx.x] = s;
-    own += attn_units(cut, s);
-  }
-  int64_t upto = own;
+// Sums of two numbers of each thread over the threads before it, and over all.
+template <int THREADS>
+__device__ __forceinline__ void block_sums(WalkShared<THREADS> &sh, int64_t (&v)[2], int64_t (&total)[2]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t upto[2] = {v[0], v[1]};
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
-    const int64_t v = __shfl_up(upto, d);
-    if ((int)(threadIdx.x & 63) >= d) upto += v;
+    const int64_t x = __shfl_up(upto[0], d), y = __shfl_up(upto[1], d);
+    if (lane >= d) upto[0] += x, upto[1] += y;
   }
-  if ((threadIdx.x & 63) == 63) sh.wave[threadIdx.x >> 6] = upto;
+  if (lane == 63) sh.sums[0][wave] = upto[0], sh.sums[1][wave] = upto[1];
   __syncthreads();
-  int64_t total = 0;
 #pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) {
-    if (w < (int)(threadIdx.x >> 6)) upto += sh.wave[w];
-    total += sh.wave[w];
-  }
-  total = uniform(total);
-  AttnShare share = attn_share(total, shares, c.min_share);
-  share.units = uniform(share.units);
-  const int64_t lo = me * share.units, hi = min(lo + share.units, total);
-  if (lo >= total) return;
-  if (upto - own <= lo && lo < upto) {
-    int64_t at = upto - own;
-    int i = r0;
-#pragma unroll 1
-    for (; i < r1 - 1; ++i) {
-      const int64_t u = attn_units(cut, seq_of(c, i));
-      if (lo < at + u) break;
-      at += u;
+  for (int n = 0; n < 2; ++n) {
+    total[n] = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+      if (w < wave) upto[n] += sh.sums[n][w];
+      total[n] += sh.sums[n][w];
     }
-    sh.request = i;
-    sh.at = at;
+    total[n] = uniform(total[n]);
+    v[n] = upto[n] - v[n];
   }
-  __syncthreads();
-  int i = uniform(sh.request), cached = 0;
-  int64_t at_request = uniform(sh.at);
-  bool filled = per == 1;
-#pragma unroll 1
-  for (; at_request < hi; ++i) {
-    if (!filled || i >= cached + THREADS) {  // the next requests' lengths, one a thread
+}
+
+// a / b for 0 <= a < 1024 and b >= 1: half a unit from a whole number, which is more than the reciprocal is off by.
+__device__ __forceinline__ int quotient(int a, int b) { return uniform((int)(((float)a + 0.5f) * __builtin_amdgcn_rcpf((float)b))); }
+
+// What workgroup `me` of `shares` has to do, piece by piece: the same in all its threads, which call together.
+template <int THREADS, bool FLAT>
+struct Walk {
+  const AttnCall &c;
+  WalkShared<THREADS> &sh;
+  AttnCut cut;
+  AttnShare share;
+  Piece p;
+  // on the line: the next item, of request p.request, and the end of the share
+  int64_t lo, hi, at, at_request, units, tile_units;
+  int per, cached, tiles, part;
+  bool left;  // something is left to do
+
+  __device__ __forceinline__ void request(int i) {
+    p.request = i;
+    if (per > 1 && (cached < 0 || i >= cached + THREADS)) {  // the next requests' lengths, one a thread
       __syncthreads();
       cached = i;
       if (cached + (int)threadIdx.x < c.n) sh.seq[threadIdx.x] = seq_of(c, cached + threadIdx.x);
       __syncthreads();
-      filled = true;
     }
-    Piece p;
-    p.s = sh.seq[i - cached];
+    p.s = sh.seq[per > 1 ? i - cached : i];
     p.s.first = uniform(p.s.first), p.s.fresh = uniform(p.s.fresh), p.s.len = uniform(p.s.len);
-    const int tiles = attn_tiles(cut, p.s);
-    if (tiles == 0) continue;
-    const int64_t units = attn_units_before(cut, p.s, tiles);
-    int part = 0, m = 0;
-    p.it.at = at_request;
-    if (lo > at_request) {  // the first request: from within it
-      while (p.it.at + units <= lo) p.it.at += units, ++part;
-      m = attn_tile_at(cut, p.s, lo - p.it.at);
-      if (m > 0) p.it.at += attn_units_before(cut, p.s, m);
-    }
-    p.request = i;
-#pragma unroll 1
-    while (p.it.at < hi && part < cut.parts) {
-      p.kv = c.by_groups(part), p.group = part - p.kv * c.groups, p.tile = m;
-      p.first = attn_first_key(cut, p.s, m), p.last = attn_last_key(cut, p.s, m);
-      p.it.keys = p.last - p.first;
-      p.b0 = attn_blocks_before(cut, p.it, lo), p.b1 = attn_blocks_before(cut, p.it, hi);
-      p.began = p.it.at >= lo;
-      p.alone = p.b0 == 0 && p.b1 * cut.block >= p.it.keys;
-      if (p.b0 < p.b1 || (p.it.keys == 0 && p.began)) work(p, share);
-      p.it.at += cut.fixed + p.it.keys;
-      if (++m == tiles) m = 0, ++part;
-    }
-    at_request += units * cut.parts;
+    tiles = attn_tiles(cut, p.s);
   }
+  __device__ __forceinline__ void item(int which, int tile) {
+    p.kv = c.by_groups(which), p.group = which - p.kv * c.groups, p.tile = tile;
+    p.first = attn_first_key(cut, p.s, tile), p.last = attn_last_key(cut, p.s, tile);
+    p.it.keys = p.last - p.first;
+  }
+
+  __device__ __forceinline__ Walk(const AttnCall &c_, WalkShared<THREADS> &sh_, int me, int shares) : c(c_), sh(sh_), cut(c_.cut) {
+    cut.flat = FLAT;
+    left = false, cached = -1, part = 0;
+    p.even = 0, p.base = 0, p.tile = 0;
+    // units and items of all requests before each thread's own
+    per = (c.n + THREADS - 1) / THREADS;
+    const int r0 = min((int)threadIdx.x * per, c.n), r1 = min(r0 + per, c.n);
+    int64_t own[2] = {0, 0}, before[2], total[2];
+#pragma unroll 1
+    for (int i = r0; i < r1; ++i) {
+      const AttnSeq s = seq_of(c, i);
+      if (per == 1) sh.seq[threadIdx.x] = s;
+      own[0] += attn_units(cut, s);
+      own[1] += (int64_t)cut.parts * attn_tiles(cut, s);
+    }
+    before[0] = own[0], before[1] = own[1];
+    block_sums(sh, before, total);
+    const int even = FLAT ? attn_even_units(total[0] - total[1] * cut.fixed, total[1], shares, c.least_even, c.spare) : 0;
+    // what a request counts as in the sums that its workgroups are found by
+    auto size = [&](const AttnSeq &s) {
+      return even == 0 ? attn_units(cut, s) : (int64_t)cut.parts * attn_tiles(cut, s) * attn_even_parts(attn_most_keys(cut, s), even);
+    };
+    if (even != 0) {
+      own[0] = 0;
+#pragma unroll 1
+      for (int i = r0; i < r1; ++i) own[0] += size(per == 1 ? sh.seq[threadIdx.x] : seq_of(c, i));
+      before[0] = own[0];
+      __syncthreads();  // the sums before have been read
+      block_sums(sh, before, total);
+      lo = me, hi = me + 1;
+    } else {
+      share = attn_share(total[0], shares, c.min_share);
+      share.units = uniform(share.units);
+      lo = me * share.units, hi = min(lo + share.units, total[0]);
+    }
+    if (lo >= total[0]) return;
+    if (before[0] <= lo && lo < before[0] + own[0]) {
+      int64_t from = before[0];
+      int i = r0;
+#pragma unroll 1
+      for (; i < r1 - 1; ++i) {
+        const int64_t u = size(seq_of(c, i));
+        if (lo < from + u) break;
+        from += u;
+      }
+      sh.request = i;
+      sh.at = from;
+    }
+    __syncthreads();
+    left = true;
+    at = at_request = uniform(sh.at);
+    request(uniform(sh.request));
+    if (even != 0) {
+      const int k = attn_even_parts(attn_most_keys(cut, p.s), even), in = (int)(lo - at);
+      const int which = quotient(in, k), j = in - which * k;
+      part = quotient(which, tiles);
+      item(part, which - part * tiles);
+      const int blocks = (p.it.keys + cut.block - 1) / cut.block;
+      p.b0 = attn_even_blocks(blocks, k, j), p.b1 = attn_even_blocks(blocks, k, j + 1);
+      p.even = k, p.base = me - j;
+      p.began = true, p.alone = min(blocks, k) <= 1;
+      left = p.b0 < p.b1 || (blocks == 0 && j == 0);
+      return;
+    }
+    units = attn_units_before(cut, p.s, tiles);
+    tile_units = attn_units_before(cut, p.s, 1);  // of every tile, where that is the same
+    if (lo > at) {  // from within the request
+      while (at + units <= lo) at += units, ++part;
+      if (FLAT) {
+        p.tile = AttnShare{tile_units, 1.0 / (double)tile_units}(lo - at);
+        at += p.tile * tile_units;
+      } else {
+        p.tile = attn_tile_at(cut, p.s, lo - at);
+        if (p.tile > 0) at += attn_units_before(cut, p.s, p.tile);
+      }
+    }
+  }
+
+  // The next piece in `p`; false where there is none.
+  __device__ __forceinline__ bool next() {
+    if (!left) return false;
+    if (p.even != 0) {
+      left = false;
+      return true;
+    }
+#pragma unroll 1
+    while (at < hi) {
+      if (part == cut.parts) {  // of the next request that has items
+        at_request += units * cut.parts;
+        do request(p.request + 1);
+        while (tiles == 0);
+        units = attn_units_before(cut, p.s, tiles);
+        tile_units = attn_units_before(cut, p.s, 1);
+        part = 0, p.tile = 0;
+      }
+      const int tile = p.tile;
+      item(part, tile);
+      p.it.at = at;
+      p.b0 = attn_blocks_before(cut, p.it, lo), p.b1 = attn_blocks_before(cut, p.it, hi);
+      p.began = at >= lo;
+      p.alone = p.b0 == 0 && p.b1 * cut.block >= p.it.keys;
+      at += FLAT ? tile_units : cut.fixed + p.it.keys;
+      following = tile + 1;
+      if (following == tiles) following = 0, ++part;
+      if (p.b0 < p.b1 || (p.it.keys == 0 && p.began)) return true;
+      p.tile = following;
+    }
+    return false;
+  }
+  __device__ __forceinline__ void done() { p.tile = following; }
+  int following = 0;
+};
+
+// The workgroups that have a part of an item: how many, and where the first keeps the item's counter.
+struct Joining {
+  int counter, parts;
+  bool even;
+  bool in_first;  // the line: the item begins in the first share that has blocks of it
+};
+__device__ __forceinline__ Joining joining(const AttnCall &c, const Piece &p, const AttnShare &share) {
+  Joining j;
+  j.even = p.even != 0, j.in_first = true;
+  if (p.even != 0) {
+    j.counter = p.base, j.parts = min((p.it.keys + c.cut.block - 1) / c.cut.block, p.even);
+  } else {
+    const AttnOwners o = attn_owners(c.cut, p.it, share);
+    j.counter = uniform(o.from), j.parts = uniform(o.to) - j.counter;
+    j.in_first = p.it.at >= (int64_t)j.counter * share.units;
+  }
+  return j;
 }
 
 // Whether this workgroup, its part of the item stored, is the last of those that have one (the same in all threads).
 template <int THREADS>
-__device__ __forceinline__ bool last_of(const AttnCall &c, WalkShared<THREADS> &sh, const AttnOwners &o) {
+__device__ __forceinline__ bool last_of(const AttnCall &c, WalkShared<THREADS> &sh, const Joining &j) {
   stores_done();
   if (threadIdx.x == 0) {
-    const bool last = add_device(c.joined + o.from) + 1 == (uint32_t)(o.to - o.from);
-    if (last) put_device(c.joined + o.from, 0u);  // for the next call
+    const bool last = add_device(c.joined + j.counter) + 1 == (uint32_t)j.parts;
+    if (last) put_device(c.joined + j.counter, 0u);  // for the next call
     sh.last_one = last;
   }
   __syncthreads();
   return sh.last_one != 0u;
 }
 
-// Places of partial results: two a share, for an item that began before it and for one that begins in it.
+// Places of partial results: two a workgroup, for an item that began before its share and for one that begins in it.
 __device__ __forceinline__ uint32_t place_of(int share, bool began, int floats) { return (uint32_t)(2 * share + (began ? 1 : 0)) * (uint32_t)(floats * 4); }
+
+__device__ __forceinline__ uint32_t place_of(const Joining &j, int part, int floats) {
+  return place_of(j.counter + part, j.even || (part == 0 && j.in_first), floats);
+}
 
 // A row of a tile: its token and head, and the keys [lo, hi) that it sees.
 struct Row {
@@ -310,9 +419,12 @@ __global__ __launch_bounds__(FewTile<DP>::THREADS, FewTile<DP>::PER_CU) void att
   const int l16 = lane & 15, g = lane >> 4;
   unsigned char *mine = smem + wave * T::WAVE_BYTES;
   const uint32_t mine_lds = lds_address(mine);
-  const int me = (int)xcd_remap(blockIdx.x, gridDim.x);
+  const int me = (int)blockIdx.x;
 
-  walk(c, sh, me, (int)gridDim.x, [&](const Piece &p, const AttnShare &share) {
+  Walk<T::THREADS, true> walk(c, sh, me, (int)gridDim.x);
+#pragma unroll 1
+  for (; walk.next(); walk.done()) {
+    const Piece &p = walk.p;
     const Row row = row_of(c, p, l16);
     int all_lo, all_hi;
     seen_by_all(c, p, 0, c.cut.tokens, all_lo, all_hi);
@@ -513,12 +625,10 @@ __global__ __launch_bounds__(FewTile<DP>::THREADS, FewTile<DP>::PER_CU) void att
     }
     bool write = true;
     if (!p.alone) {
-      const AttnOwners o = attn_owners(c.cut, p.it, share);
-      const int from = uniform(o.from), parts = uniform(o.to) - from;
-      write = last_of(c, sh, AttnOwners{from, from + parts});
+      const Joining join = joining(c, p, walk.share);
+      const int parts = join.parts;
+      write = last_of(c, sh, join);
       if (write) {
-        // the item's first part may be of the share that it begins in
-        const bool in_first = p.it.at >= (int64_t)from * share.units;
 #pragma unroll 1
         for (int n = 0; n < PASSES; ++n) {
           const int e = n * T::THREADS + (int)threadIdx.x, r = min(e / CH, 15), ch = e % CH;
@@ -531,7 +641,7 @@ __global__ __launch_bounds__(FewTile<DP>::THREADS, FewTile<DP>::PER_CU) void att
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               const int w = min(w0 + j, parts - 1);
-              const uint32_t slot = place_of(from + w, w == 0 && in_first, T::PART);
+              const uint32_t slot = place_of(join, w, T::PART);
               a[j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(slot + (uint32_t)(r * DP + 4 * ch) * 4u), 0, kDevice));
               t[j] = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, (int)(slot + (uint32_t)(16 * DP + 2 * r) * 4u), 0, kDevice));
             }
@@ -571,7 +681,7 @@ __global__ __launch_bounds__(FewTile<DP>::THREADS, FewTile<DP>::PER_CU) void att
       }
     }
     __syncthreads();
-  });
+  }
 }
 
 // ------------------------------------------------------------------ many rows
@@ -638,7 +748,10 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
   if (threadIdx.x < 6) (&bad_rows[0][0])[threadIdx.x] = 0u;
   __syncthreads();
 
-  walk(c, sh, me, (int)gridDim.x, [&](const Piece &p, const AttnShare &share) {
+  Walk<T::THREADS, false> walk(c, sh, me, (int)gridDim.x);
+#pragma unroll 1
+  for (; walk.next(); walk.done()) {
+    const Piece &p = walk.p;
     const Row row = row_of(c, p, wave * 32 + l32);
     int all_lo, all_hi;
     seen_by_all(c, p, c.by_heads(wave * 32), c.by_heads(wave * 32 + 31) + 1, all_lo, all_hi);
@@ -789,11 +902,10 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
       if (half == 0)
         __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f32x2{m, l}), rs,
                                               (int)(slot + (uint32_t)(T::ROWS * DP + 2 * r) * 4u), 0, kDevice);
-      const AttnOwners o = attn_owners(c.cut, p.it, share);
-      const int from = uniform(o.from), parts = uniform(o.to) - from;
-      write = last_of(c, sh, AttnOwners{from, from + parts});
+      const Joining join = joining(c, p, walk.share);
+      const int parts = join.parts;
+      write = last_of(c, sh, join);
       if (write) {
-        const bool in_first = p.it.at >= (int64_t)from * share.units;
         m = -INFINITY, l = 0.f;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
@@ -801,7 +913,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
           for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
 #pragma unroll 1
         for (int s = 0; s < parts; ++s) {
-          const uint32_t slot = place_of(from + s, s == 0 && in_first, T::PART);
+          const uint32_t slot = place_of(join, s, T::PART);
           const f32x2 t2 = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, (int)(slot + (uint32_t)(T::ROWS * DP + 2 * r) * 4u), 0, kDevice));
           const float now = fmaxf(m, t2[0]), by = now == -INFINITY ? 0.f : now;
           const float f0 = exp2_(m - by), f1 = exp2_(t2[0] - by);
@@ -838,7 +950,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
     __syncthreads();
     if (threadIdx.x < 6) (&bad_rows[0][0])[threadIdx.x] = 0u;
     __syncthreads();
-  });
+  }
 }
 
 // ------------------------------------------------------------------ launches
@@ -909,10 +1021,10 @@ int attn_launch(const occ_attn_args &a, hipStream_t s) {
     k.groups = (c.group + k.heads - 1) / k.heads;
     k.by_heads = Divider(k.heads), k.by_groups = Divider(k.groups);
     k.cut.parts = a.Hkv * k.groups;
-    k.cut.fixed = many ? 64 : 32, k.cut.block = many ? ManyTile<128>::KEYS : DP > 128 ? FewTile<256>::KEYS : FewTile<128>::KEYS;
+    k.cut.fixed = many ? 64 : 256, k.cut.block = many ? ManyTile<128>::KEYS : DP > 128 ? FewTile<256>::KEYS : FewTile<128>::KEYS;
     k.cut.window = a.window < c.keys ? a.window : 0, k.cut.causal = a.causal != 0;
     k.least = least, k.most = most;
-    k.min_share = many ? 256 : 512;
+    k.min_share = 256, k.least_even = 256, k.spare = 512;
     const int grid = workgroups_of(many, DP, cus);
     return many ? launch<true>(k, DP, grid, s) : launch<false>(k, DP, grid, s);
   };

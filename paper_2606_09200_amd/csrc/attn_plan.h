@@ -1,10 +1,12 @@
 // How the attention over a paged cache is cut into shares of equal work: arithmetic that the host can check.
 //
 // A request's new tokens are taken in tiles of `tokens` of them, once for each of `parts` groups of heads.  An item
-// (request, part, tile) costs what it reads, its keys, and `fixed` keys' worth beside.  All items in a row
-// are one line of units; a workgroup takes `share` units of it, which may begin and end within
-// an item.  Nothing but the lengths, which only the GPU knows, decides: a single long request is split along its
-// keys, many short ones are dealt out whole.
+// (request, part, tile) costs what it reads, its keys, and `fixed` keys' worth beside.  Nothing but the lengths, which only
+// the GPU knows, decides who does what:
+//  * The line.  All items in a row are one line of units; a workgroup takes a share of it, which may begin and end within an
+//    item.  Shares are equal, whatever the lengths; an item that several have a part of is joined.
+//  * Few items (attn_even): each item goes to as many workgroups as it is long for, in equal parts, and a workgroup has
+//    one part and no more.
 #pragma once
 
 #include "divider.h"
@@ -20,6 +22,7 @@ struct AttnCut {
   int block;    // keys that are computed at once, a power of two
   int window;   // 0: none
   int causal;
+  int flat;     // all tiles of a request count as its longest: no sums over tiles
   Divider by_tokens;
 };
 
@@ -62,8 +65,16 @@ OCC_PLAN int64_t attn_ramp(const AttnCut &c, int n, int64_t a) {
   return count * (a + skip * step) + step * (count * (count - 1) / 2);
 }
 
+// Keys that a tile has at most.
+OCC_PLAN int attn_most_keys(const AttnCut &c, const AttnSeq &s) {
+  // without causality the last key of all is every tile's last
+  const int64_t seen = (int64_t)c.window + (c.causal ? c.tokens : s.fresh) - 1;
+  return c.window && seen < s.len ? (int)seen : s.len;
+}
+
 // Units of a request's tiles before tile m (of one part).
 OCC_PLAN int64_t attn_units_before(const AttnCut &c, const AttnSeq &s, int m) {
+  if (c.flat) return (int64_t)m * (attn_most_keys(c, s) + c.fixed);
   const int64_t base = (int64_t)s.len - s.fresh;
   int64_t keys;
   if (c.causal) {
@@ -93,7 +104,7 @@ OCC_PLAN int attn_tile_at(const AttnCut &c, const AttnSeq &s, int64_t x) {
   return lo;
 }
 
-// An item on the line: units [at, at + fixed + keys), of which block b (keys first + b block ...) belongs to
+// An item on the line: units [at, at + fixed + keys) and, flat, some behind them, of which block b (keys first + b block ...) belongs to
 // the share that unit at + fixed + b block lies in.
 struct AttnItem {
   int64_t at;
@@ -136,6 +147,22 @@ OCC_PLAN AttnOwners attn_owners(const AttnCut &c, const AttnItem &it, const Attn
   if (it.keys == 0) return AttnOwners{share(it.at), share(it.at)};
   const int64_t last = (int64_t)(it.keys - 1) / c.block * c.block;
   return AttnOwners{share(it.at + c.fixed), share(it.at + c.fixed + last) + 1};
+}
+
+// Few items: parts of an item of at most `most` keys where a part has `units` of them, and whether that is better than
+// the line with `items` items of `total` units: if every part has a workgroup, and the longest is not so much longer
+// than a share that a second piece (and one more joining) would be cheaper, `spare` keys' worth.
+OCC_PLAN int attn_even_units(int64_t total, int64_t items, int shares, int least, int spare) {
+  if (items >= shares) return 0;
+  const double even = (double)total / (double)(shares - (int)items) + 1;  // the parts are less than `shares`
+  if (even > (double)total / shares + spare || even > 1e9) return 0;
+  return (int)even + 1 < least ? least : (int)even + 1;
+}
+OCC_PLAN int attn_even_parts(int most, int units) { return most <= units ? 1 : (int)((uint32_t)(most - 1) / (uint32_t)units) + 1; }
+// Blocks of an item before part j of k: the first parts have one more; if there are fewer blocks than parts, one each.
+OCC_PLAN int attn_even_blocks(int blocks, int k, int j) {
+  const int each = (int)((uint32_t)blocks / (uint32_t)k), more = blocks - each * k;
+  return j * each + (j < more ? j : more);
 }
 
 }  // namespace occ

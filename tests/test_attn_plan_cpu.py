@@ -16,11 +16,12 @@ PLAN = r"""
 
 using namespace occ;
 
-static long bad, items_seen, split;
+static long bad, items_seen, split, evened;
 
 static void line(const AttnCut &c, const std::vector<AttnSeq> &seqs, int workgroups, int min_share) {
   // the items as the definition has them
-  std::vector<AttnItem> items;
+  struct Placed { int64_t at; int keys, units; };
+  std::vector<Placed> items;
   int64_t at = 0;
   for (const AttnSeq &s : seqs) {
     const int tiles = attn_tiles(c, s);
@@ -38,10 +39,12 @@ static void line(const AttnCut &c, const std::vector<AttnSeq> &seqs, int workgro
         if (a < 0 || b < a || b > s.len) ++bad;
         if (last > 0 && (a > first || b < last || b != last)) ++bad;
         if (attn_units_before(c, s, m) != before) ++bad;
-        if (attn_tile_at(c, s, before) != m || attn_tile_at(c, s, before + c.fixed + (b - a) - 1) != m) ++bad;
-        items.push_back({at, b - a});
-        at += c.fixed + (b - a);
-        before += c.fixed + (b - a);
+        const int units = c.fixed + (c.flat ? attn_most_keys(c, s) : b - a);
+        if (b - a > attn_most_keys(c, s)) ++bad;
+        if (attn_tile_at(c, s, before) != m || attn_tile_at(c, s, before + units - 1) != m) ++bad;
+        items.push_back({at, b - a, units});
+        at += units;
+        before += units;
       }
       if (attn_units_before(c, s, tiles) != before) ++bad;
     }
@@ -53,12 +56,13 @@ static void line(const AttnCut &c, const std::vector<AttnSeq> &seqs, int workgro
   if (share > min_share && (share - 2) * workgroups > total) ++bad;
   std::set<int> counters;
   std::set<std::pair<int, int>> slots;
-  for (const AttnItem &it : items) {
+  for (const Placed &placed : items) {
+    const AttnItem it{placed.at, placed.keys};
     ++items_seen;
     const AttnOwners o = attn_owners(c, it, cutter);
     const int blocks = (it.keys + c.block - 1) / c.block;
     int next = 0;
-    const int64_t end = it.at + c.fixed + it.keys;
+    const int64_t end = it.at + placed.units;
     for (int w = (int)(it.at / share); w * share < end; ++w) {
       const int b0 = attn_blocks_before(c, it, w * share), b1 = attn_blocks_before(c, it, std::min((w + 1) * share, total));
       if (b0 != next) ++bad;
@@ -77,6 +81,34 @@ static void line(const AttnCut &c, const std::vector<AttnSeq> &seqs, int workgro
   }
 }
 
+// Items of these blocks in even parts: every block once, by parts that a joining workgroup finds in order.
+static void even(const std::vector<int> &keys, int shares, int least, int spare) {
+  int64_t total = 0;
+  for (int k : keys) total += k;
+  const int units = attn_even_units(total, keys.size(), shares, least, spare);
+  if (units == 0) return;
+  ++evened;
+  if (units < least) ++bad;
+  int64_t parts = 0;
+  for (int most : keys) {
+    const int k = attn_even_parts(most, units);
+    if (k < 1 || (int64_t)k * units < most) ++bad;
+    parts += k;
+    for (int n : {most, most / 2, most / 100, 1, 0}) {   // a tile may have fewer keys than its request's longest
+      const int blocks = (n + 31) / 32;
+      int have = 0;
+      if (attn_even_blocks(blocks, k, 0) != 0 || attn_even_blocks(blocks, k, k) != blocks) ++bad;
+      for (int j = 0; j < k; ++j) {
+        const int b0 = attn_even_blocks(blocks, k, j), b1 = attn_even_blocks(blocks, k, j + 1);
+        if (b1 < b0) ++bad;
+        if (b1 > b0 && have++ != j) ++bad;   // the parts that have any come first
+      }
+      if (have != std::min(blocks, k)) ++bad;
+    }
+  }
+  if (parts > shares) ++bad;
+}
+
 int main() {
   std::mt19937 g(1);
   auto pick = [&](std::vector<int> v) { return v[g() % v.size()]; };
@@ -89,6 +121,7 @@ int main() {
     c.fixed = pick({0, 1, 32, 64, 300}) + (n % 2 ? 32 : 1);
     c.window = pick({0, 0, 1, 5, 100, 1 << 30});
     c.causal = pick({1, 1, 0});
+    c.flat = pick({0, 1});
     std::vector<AttnSeq> seqs;
     const int count = pick({1, 3, 9});
     for (int i = 0; i < count; ++i) {
@@ -98,8 +131,14 @@ int main() {
     }
     line(c, seqs, pick({1, 2, 7, 256, 512}), pick({64, 256, 256}));
   }
+  for (int n = 0; n < 20000; ++n) {
+    std::vector<int> keys(pick({1, 2, 8, 40, 100, 200, 255, 256, 300}));
+    const int most = pick({1, 100, 700, 5000, 130000, 2000000000});
+    for (int &k : keys) k = pick({0, 1, 2}) ? g() % most + 1 : 0;
+    even(keys, pick({256, 256, 304, 8}), pick({128, 256}), pick({0, 512}));
+  }
   // sizes near the limits: no sum leaves 64 bits, no key 31
-  AttnCut c{2, 8, 32, 32, 0, 1, Divider(2)};
+  AttnCut c{2, 8, 32, 32, 0, 1, 0, Divider(2)};
   const AttnSeq big{0, 1 << 24, 2147418112};
   if (attn_units(c, big) <= 0 || attn_last_key(c, big, attn_tiles(c, big) - 1) != big.len) ++bad;
   c.window = 1 << 30;
@@ -115,7 +154,7 @@ int main() {
     if (by(x) != x / by.units || by(y) != y / by.units || (y > 0 && by(y - 1) != (y - 1) / by.units)) ++bad;
   }
   printf("bad %ld items %ld split %ld\n", bad, items_seen, split);
-  return bad != 0 || split < 1000;
+  return bad != 0 || split < 1000 || evened < 1000;
 }
 """
 
