@@ -72,11 +72,7 @@ __device__ __forceinline__ float sum_quarters(float v) {
   return sum_halves(as_float(s[0]) + as_float(s[1]));
 }
 
-// Whether one of two bf16 values is an infinity or a NaN, and the pair with such values zeroed.
-__device__ __forceinline__ bool pair_nonfinite(uint32_t w) {
-  return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
-}
-// Bits 0x80008000 are set where either is.
+// Bits 0x80008000 are set where one of two bf16 values is an infinity or a NaN; the pair with such values zeroed.
 __device__ __forceinline__ uint32_t pair_exponents(uint32_t w) { return (w & 0x7F807F80u) + 0x00800080u; }
 __device__ __forceinline__ uint32_t pair_finite(uint32_t w) {
   return ((w & 0x7F80u) == 0x7F80u ? 0u : w & 0xFFFFu) | ((w & 0x7F800000u) == 0x7F800000u ? 0u : w & 0xFFFF0000u);
@@ -219,18 +215,22 @@ struct Walk {
     }
     before[0] = own[0], before[1] = own[1];
     block_sums(sh, before, total);
-    const int even = FLAT ? attn_even_units(total[0] - total[1] * cut.fixed, total[1], shares, c.least_even, c.spare) : 0;
-    // what a request counts as in the sums that its workgroups are found by
+    // where even parts are better, the sums are of parts
+    int even = attn_even_units(total[0] - total[1] * cut.fixed, total[1], shares, c.least_even, c.spare);
     auto size = [&](const AttnSeq &s) {
       return even == 0 ? attn_units(cut, s) : (int64_t)cut.parts * attn_tiles(cut, s) * attn_even_parts(attn_most_keys(cut, s), even);
     };
     if (even != 0) {
-      own[0] = 0;
+      int64_t parts = 0, first[2] = {0, 0}, all[2];
 #pragma unroll 1
-      for (int i = r0; i < r1; ++i) own[0] += size(per == 1 ? sh.seq[threadIdx.x] : seq_of(c, i));
-      before[0] = own[0];
+      for (int i = r0; i < r1; ++i) parts += size(per == 1 ? sh.seq[threadIdx.x] : seq_of(c, i));
+      first[0] = parts;
       __syncthreads();  // the sums before have been read
-      block_sums(sh, before, total);
+      block_sums(sh, first, all);
+      if (all[0] <= shares) own[0] = parts, before[0] = first[0], total[0] = all[0];
+      else even = 0;  // tiles of a request may be shorter than its longest
+    }
+    if (even != 0) {
       lo = me, hi = me + 1;
     } else {
       share = attn_share(total[0], shares, c.min_share);
@@ -687,24 +687,29 @@ __global__ __launch_bounds__(FewTile<DP>::THREADS, FewTile<DP>::PER_CU) void att
 // ------------------------------------------------------------------ many rows
 //
 // Chunks of a prompt: 128 rows (tokens times heads that share keys) of a workgroup's 4 waves, 32 each, against
-// tiles of 64 keys that direct-to-LDS loads bring in while the tile before is multiplied.  S^T = K Q^T in 32x32x16
+// tiles of 32 or 64 keys in a ring of four that direct-to-LDS loads fill three tiles ahead.  S^T = K Q^T in 32x32x16
 // MFMAs leaves a lane 16 keys' scores of one row (the other half of the wave has the other 16), which,
 // rounded to bf16, are the second product's operand as they lie: O^T = V^T P^T over the keys in that order, values
 // read transposed.  m and l are one register a lane, and so is what o has to be scaled by.  The weights' rounding (8
 // bits) is of the same size as the output's own; l sums them unrounded.
+// Scaling o costs as much as half of a tile's exponentials: m stays behind the maximum until it would have to grow by
+// kSlack, so that weights are up to 2^kSlack and o is scaled once or twice in all.
 template <int DP>
 struct ManyTile {
   static constexpr int THREADS = 256;
-  static constexpr int ROWS = 128, KEYS = 64;
-  static constexpr int KS = DP / 16, DT = DP / 32;
+  static constexpr int ROWS = 128, KEYS = DP > 64 ? 32 : 64;
+  static constexpr int KS = DP / 16, DT = DP / 32, KT = KEYS / 32;
   static constexpr int CH = DP / 8;                    // 16-byte chunks of a row
   static constexpr int PITCH = DP * 2;
   static constexpr int OPERAND = KEYS * PITCH;         // bytes of a tile of K, and of V
-  static constexpr int STAGE = 2 * OPERAND;
+  static constexpr int STAGES = 4, STAGE = 2 * OPERAND;
   static constexpr int PASS_ROWS = THREADS / CH, PASSES = KEYS / PASS_ROWS;
+  static constexpr int DMAS = 2 * PASSES;              // of a wave for a tile
   static constexpr int PART = ROWS * (DP + 2);
   static constexpr int PER_CU = DP > 128 ? 1 : 2;
+  static constexpr int IDS = 512;                      // page numbers at hand
 };
+constexpr float kSlack = 8.f;
 
 // Physical chunk of chunk c in row r: a read of K sends 16 rows at one chunk, one of V, by 32 lanes, 4 rows at 4
 // chunks in a row.
@@ -732,10 +737,11 @@ __device__ __forceinline__ void global_dma16(const void *from, uint32_t lds) {
 template <int DP>
 __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void attn_many_kernel(AttnCall c) {
   using T = ManyTile<DP>;
-  constexpr int KS = T::KS, DT = T::DT;
+  constexpr int KS = T::KS, DT = T::DT, KT = T::KT;
   extern __shared__ __align__(256) unsigned char stages[];
   __shared__ WalkShared<T::THREADS> sh;
-  __shared__ uint32_t bad_rows[3][2];
+  __shared__ int32_t ids[T::IDS];
+  __shared__ uint32_t bad_rows[8][2];  // of tile b: [b % 8]
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
   const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
   const uint32_t lds0 = lds_address(stages);
@@ -744,9 +750,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
 
   // chunks that the heads do not have stay zero
   if (c.D < DP)
-    for (int i = threadIdx.x; i < 2 * T::STAGE / 16; i += T::THREADS) reinterpret_cast<u32x4 *>(stages)[i] = u32x4{0u, 0u, 0u, 0u};
-  if (threadIdx.x < 6) (&bad_rows[0][0])[threadIdx.x] = 0u;
-  __syncthreads();
+    for (int i = threadIdx.x; i < T::STAGES * T::STAGE / 16; i += T::THREADS) reinterpret_cast<u32x4 *>(stages)[i] = u32x4{0u, 0u, 0u, 0u};
 
   Walk<T::THREADS, false> walk(c, sh, me, (int)gridDim.x);
 #pragma unroll 1
@@ -759,21 +763,34 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
     const uint16_t *kc = c.k + (size_t)p.kv * c.cache_head, *vc = c.v + (size_t)p.kv * c.cache_head;
     const int r_in = threadIdx.x / T::CH, chunk = threadIdx.x % T::CH;
 
+    int ids_from = 0;
+    auto fill_ids = [&](int b) {  // page numbers from tile b's first on
+      ids_from = c.by_page(p.first + b * T::KEYS);
+      const int end = c.by_page(min(p.first + p.b1 * T::KEYS, p.last) - 1) + 1;
+      for (int i = threadIdx.x; i < T::IDS; i += T::THREADS)
+        if (ids_from + i < end) ids[i] = table[ids_from + i];
+    };
     auto issue = [&](int b) {
-      const int stage = b & 1, flags = b % 3;
-      const uint32_t to = lds0 + (uint32_t)stage * T::STAGE + (uint32_t)wave * 1024u;
+      if (c.by_page(min(p.first + (b + 1) * T::KEYS, p.last) - 1) >= ids_from + T::IDS) {
+        __syncthreads();
+        fill_ids(b);
+        __syncthreads();
+      }
+      const uint32_t to = lds0 + (uint32_t)(b % T::STAGES) * T::STAGE + (uint32_t)wave * 1024u;
 #pragma unroll
       for (int i = 0; i < T::PASSES; ++i) {
         const int r = i * T::PASS_ROWS + r_in;
         const int key = min(p.first + b * T::KEYS + r, p.last - 1);
-        const KeyRow kr = key_row(c, key, table[c.by_page(key)]);
-        if (kr.bad && chunk == 0) atomicOr(&bad_rows[flags][r >> 5], 1u << (r & 31));
+        const KeyRow kr = key_row(c, key, ids[c.by_page(key) - ids_from]);
+        if (kr.bad && chunk == 0) atomicOr(&bad_rows[b % 8][r >> 5], 1u << (r & 31));
         const int ck = many_swizzle_k<DP>(r, chunk), cv = many_swizzle_v<DP>(r, chunk);
         if (8 * ck < c.D) global_dma16(kc + kr.at + 8 * ck, to + (uint32_t)i * 4096u);
         if (8 * cv < c.D) global_dma16(vc + kr.at + 8 * cv, to + T::OPERAND + (uint32_t)i * 4096u);
       }
     };
 
+    if (threadIdx.x < 16) (&bad_rows[0][0])[threadIdx.x] = 0u;
+    if (p.b0 < p.b1) fill_ids(p.b0);
     u32x4 q[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
@@ -787,19 +804,21 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
     float m = -INFINITY, l = 0.f;
-
-    if (p.b0 < p.b1) issue(p.b0);
-    for (int b = p.b0; b < p.b1; ++b) {
-      wait_vmcnt<0>();
-      __syncthreads();  // tile b has landed, and nobody reads the one before any more
-      if (threadIdx.x < 2) bad_rows[(b + 2) % 3][threadIdx.x] = 0u;
-      if (b + 1 < p.b1) issue(b + 1);
-      const int kb = p.first + b * T::KEYS;
-      const uint32_t kt = lds0 + (uint32_t)(b & 1) * T::STAGE, vt0 = kt + T::OPERAND;
-      const uint32_t bad0 = bad_rows[b % 3][0], bad1 = bad_rows[b % 3][1];
-      f32x16 x[2];
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): from here on only direct loads to LDS are counted
+    __syncthreads();
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
+    for (int i = 0; i < T::STAGES - 1; ++i)
+      if (p.b0 + i < p.b1) issue(p.b0 + i);
+#pragma unroll 1
+    for (int b = p.b0; b < p.b1; ++b) {
+      wait_stages<T::STAGES - 2, T::DMAS>(min(T::STAGES - 2, p.b1 - 1 - b));
+      __syncthreads();  // tile b has landed, and nobody reads the one before any more
+      const int kb = p.first + b * T::KEYS;
+      const uint32_t kt = lds0 + (uint32_t)(b % T::STAGES) * T::STAGE, vt0 = kt + T::OPERAND;
+      const uint32_t bad0 = bad_rows[b % 8][0], bad1 = KT > 1 ? bad_rows[b % 8][KT - 1] : 0u;
+      f32x16 x[KT];
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[t][i] = 0.f;
         const uint32_t at = kt + (uint32_t)((32 * t + l32) * T::PITCH + many_swizzle_k<DP>(l32, half) * 16);
@@ -810,79 +829,90 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
           x[t] = mfma32(k, q[s], x[t]);
         }
       }
+      if (threadIdx.x < 2) bad_rows[(b + T::STAGES) % 8][threadIdx.x] = 0u;
+      if (b + T::STAGES - 1 < p.b1) issue(b + T::STAGES - 1);
       // a lane's scores are of keys 32 t + 8 (i / 4) + 4 half + i % 4
       const bool masked = kb < all_lo || kb + T::KEYS > all_hi || uniform((int)(bad0 | bad1)) != 0;
+      bool odd = false;
       if (masked) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < KT; ++t)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int at = 8 * (i >> 2) + 4 * half + (i & 3);
             const bool seen = kb + 32 * t + at >= row.lo && kb + 32 * t + at < row.hi && !(((t ? bad1 : bad0) >> at) & 1u);
             x[t][i] = seen ? x[t][i] : -INFINITY;
           }
+        // a value that a row does not see must not reach it, whatever it is: if there are infinities or NaN among the
+        // values, they go in one by one
+        uint32_t bits = 0;
+#pragma unroll
+        for (int i = 0; i < T::KEYS * T::CH / 64; ++i) {
+          const u32x4 w = *(__attribute__((address_space(3))) const u32x4 *)(size_t)(vt0 + (uint32_t)(i * 64 + lane) * 16u);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) bits |= pair_exponents(w[j]);
+        }
+        odd = __ballot((bits & 0x80008000u) != 0) != 0;
       }
       float top = x[0][0];
 #pragma unroll
-      for (int i = 1; i < 32; ++i) top = fmaxf(top, x[i >> 4][i & 15]);
-      top = fmaxf(m, max_halves(top) * c.scale);
-      const float by = top == -INFINITY ? 0.f : top;
-      const float less = exp2_(m - by);
-      m = top;
-      l = l * less;
-      u32x4 w[4];
+      for (int i = 1; i < 16 * KT; ++i) top = fmaxf(top, x[i >> 4][i & 15]);
+      top = max_halves(top) * c.scale;
+      if (__ballot(top > m + kSlack) != 0) {
+        const float now = fmaxf(m, top), less = now == -INFINITY ? 1.f : exp2_(m - now);
+        m = now;
+        l = l * less;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < DT; ++t) acc[t] = acc[t] * less;
+      }
+      const float by = m == -INFINITY ? 0.f : m;
+      u32x4 w[2 * KT];
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float e0 = exp2_(__builtin_fmaf(x[t][2 * i], c.scale, -by)), e1 = exp2_(__builtin_fmaf(x[t][2 * i + 1], c.scale, -by));
           l = l + (e0 + e1);
           w[2 * t + (i >> 2)][i & 3] = pack_bf16(e0, e1);
         }
+      if (odd) {
+#pragma unroll 1
+        for (int r = 0; r < T::KEYS; ++r) {
+          const bool seen = kb + r >= row.lo && kb + r < row.hi && !(((r & 32 ? bad1 : bad0) >> (r & 31)) & 1u);
 #pragma unroll
-      for (int t = 0; t < DT; ++t) acc[t] = acc[t] * less;
+          for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              // values 32 t + 8 i + 4 half .. + 3 of key r
+              const uint32_t a = vt0 + r * T::PITCH + many_swizzle_v<DP>(r, 4 * t + i) * 16 + 8 * half;
+              const u32x2 h = *(__attribute__((address_space(3))) const u32x2 *)(size_t)a;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const uint32_t f = (h[j >> 1] >> (16 * (j & 1))) & 0xFFFFu;
+                if (seen && (f & 0x7F80u) == 0x7F80u) acc[t][4 * i + j] = acc[t][4 * i + j] + as_float(f << 16);
+              }
+            }
+        }
+      }
       const int vr = 4 * half + (l16 >> 2);
       const uint32_t v0 = vt0 + vr * T::PITCH + many_swizzle_v<DP>(vr, 2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1)) * 16 + 8 * (l16 & 1);
 #pragma unroll
       for (int t = 0; t < DT; ++t) {
-        u32x4 vt[4];
+        u32x4 vt[2 * KT];
         const uint32_t at = (v0 ^ ((t & 3) * 64)) + (t >> 2) * 256;
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
+        for (int s = 0; s < 2 * KT; ++s) {
           const u32x2 a = read_transposed(at + 16 * s * T::PITCH), b2 = read_transposed(at + (16 * s + 8) * T::PITCH);
           vt[s] = u32x4{a[0], a[1], b2[0], b2[1]};
         }
-        if (masked) {
-          // a value that a row does not see must not reach it, whatever it is: infinities and NaN go in one by one
-          bool odd = false;
+        if (odd) {
 #pragma unroll
-          for (int s = 0; s < 4; ++s)
+          for (int s = 0; s < 2 * KT; ++s)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) odd = odd || pair_nonfinite(vt[s][i]);
-          if (__ballot(odd) != 0) {
-#pragma unroll
-            for (int s = 0; s < 4; ++s)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) vt[s][i] = pair_finite(vt[s][i]);
-#pragma unroll 1
-            for (int r = 0; r < T::KEYS; ++r) {
-              const bool seen = kb + r >= row.lo && kb + r < row.hi && !(((r & 32 ? bad1 : bad0) >> (r & 31)) & 1u);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                // values 32 t + 8 i + 4 half .. + 3 of key r
-                const uint32_t a = vt0 + r * T::PITCH + many_swizzle_v<DP>(r, 4 * t + i) * 16 + 8 * half;
-                const u32x2 h = *(__attribute__((address_space(3))) const u32x2 *)(size_t)a;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  const uint32_t f = ((j & 2 ? h[1] : h[0]) >> (16 * (j & 1))) & 0xFFFFu;
-                  if (seen && (f & 0x7F80u) == 0x7F80u) acc[t][4 * i + j] = acc[t][4 * i + j] + as_float(f << 16);
-                }
-              }
-            }
-          }
+            for (int i = 0; i < 4; ++i) vt[s][i] = pair_finite(vt[s][i]);
         }
 #pragma unroll
-        for (int s = 0; s < 4; ++s) acc[t] = mfma32(vt[s], w[s], acc[t]);
+        for (int s = 0; s < 2 * KT; ++s) acc[t] = mfma32(vt[s], w[s], acc[t]);
       }
     }
     l = sum_halves(l);
@@ -948,8 +978,6 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
         c.lse[(size_t)row.token * c.Hq + row.head] = some ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
     }
     __syncthreads();
-    if (threadIdx.x < 6) (&bad_rows[0][0])[threadIdx.x] = 0u;
-    __syncthreads();
   }
 }
 
@@ -966,7 +994,7 @@ int launch(const AttnCall &c, int grid, hipStream_t s) {
   void (*fn)(AttnCall);
   if constexpr (MANY) fn = attn_many_kernel<DP>;
   else fn = attn_few_kernel<DP>;
-  constexpr int lds = MANY ? 2 * ManyTile<DP>::STAGE : FewTile<DP>::WAVES * FewTile<DP>::WAVE_BYTES;
+  constexpr int lds = MANY ? ManyTile<DP>::STAGES * ManyTile<DP>::STAGE : FewTile<DP>::WAVES * FewTile<DP>::WAVE_BYTES;
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return OCC_ENODEV;
   static Once limit_set[kMaxDevices];
@@ -1021,10 +1049,10 @@ int attn_launch(const occ_attn_args &a, hipStream_t s) {
     k.groups = (c.group + k.heads - 1) / k.heads;
     k.by_heads = Divider(k.heads), k.by_groups = Divider(k.groups);
     k.cut.parts = a.Hkv * k.groups;
-    k.cut.fixed = many ? 64 : 256, k.cut.block = many ? ManyTile<128>::KEYS : DP > 128 ? FewTile<256>::KEYS : FewTile<128>::KEYS;
+    k.cut.fixed = many ? 128 : 256, k.cut.block = many ? (DP > 64 ? ManyTile<128>::KEYS : ManyTile<64>::KEYS) : DP > 128 ? FewTile<256>::KEYS : FewTile<128>::KEYS;
     k.cut.window = a.window < c.keys ? a.window : 0, k.cut.causal = a.causal != 0;
     k.least = least, k.most = most;
-    k.min_share = 256, k.least_even = 256, k.spare = 512;
+    k.min_share = 256, k.least_even = many ? 512 : 256, k.spare = 512;
     const int grid = workgroups_of(many, DP, cus);
     return many ? launch<true>(k, DP, grid, s) : launch<false>(k, DP, grid, s);
   };
