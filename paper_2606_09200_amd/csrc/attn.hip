@@ -734,14 +734,16 @@ __device__ __forceinline__ void global_dma16(const void *from, uint32_t lds) {
 }
 #pragma clang diagnostic pop
 
-template <int DP>
+// FULL: heads of DP values, no fewer.
+template <int DP, bool FULL>
 __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void attn_many_kernel(AttnCall c) {
   using T = ManyTile<DP>;
   constexpr int KS = T::KS, DT = T::DT, KT = T::KT;
   extern __shared__ __align__(256) unsigned char stages[];
   __shared__ WalkShared<T::THREADS> sh;
   __shared__ int32_t ids[T::IDS];
-  __shared__ uint32_t bad_rows[8][2];  // of tile b: [b % 8]
+  __shared__ uint32_t bad_rows[8][2];  // keys of tile b whose page is none: [b % 8]
+  __shared__ uint32_t bad_pages;       // whether some page at hand is none
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
   const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
   const uint32_t lds0 = lds_address(stages);
@@ -749,7 +751,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
   const int me = (int)xcd_remap(blockIdx.x, gridDim.x);
 
   // chunks that the heads do not have stay zero
-  if (c.D < DP)
+  if (!FULL)
     for (int i = threadIdx.x; i < T::STAGES * T::STAGE / 16; i += T::THREADS) reinterpret_cast<u32x4 *>(stages)[i] = u32x4{0u, 0u, 0u, 0u};
 
   Walk<T::THREADS, false> walk(c, sh, me, (int)gridDim.x);
@@ -764,32 +766,51 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
     const int r_in = threadIdx.x / T::CH, chunk = threadIdx.x % T::CH;
 
     int ids_from = 0;
+    bool some_bad = false;
     auto fill_ids = [&](int b) {  // page numbers from tile b's first on
       ids_from = c.by_page(p.first + b * T::KEYS);
       const int end = c.by_page(min(p.first + p.b1 * T::KEYS, p.last) - 1) + 1;
       for (int i = threadIdx.x; i < T::IDS; i += T::THREADS)
-        if (ids_from + i < end) ids[i] = table[ids_from + i];
+        if (ids_from + i < end) {
+          const int id = table[ids_from + i];
+          ids[i] = id;
+          if ((uint32_t)id >= (uint32_t)c.pages) bad_pages = 1u;
+        }
     };
     auto issue = [&](int b) {
       if (c.by_page(min(p.first + (b + 1) * T::KEYS, p.last) - 1) >= ids_from + T::IDS) {
         __syncthreads();
         fill_ids(b);
         __syncthreads();
+        some_bad = uniform((int)bad_pages) != 0;
       }
       const uint32_t to = lds0 + (uint32_t)(b % T::STAGES) * T::STAGE + (uint32_t)wave * 1024u;
+      int id[T::PASSES], key[T::PASSES];
+#pragma unroll
+      for (int i = 0; i < T::PASSES; ++i) {
+        key[i] = min(p.first + b * T::KEYS + i * T::PASS_ROWS + r_in, p.last - 1);
+        id[i] = ids[c.by_page(key[i]) - ids_from];
+      }
+      if (some_bad) {
+#pragma unroll
+        for (int i = 0; i < T::PASSES; ++i) {
+          const int r = i * T::PASS_ROWS + r_in;
+          if ((uint32_t)id[i] >= (uint32_t)c.pages && chunk == 0) atomicOr(&bad_rows[b % 8][r >> 5], 1u << (r & 31));
+        }
+      }
 #pragma unroll
       for (int i = 0; i < T::PASSES; ++i) {
         const int r = i * T::PASS_ROWS + r_in;
-        const int key = min(p.first + b * T::KEYS + r, p.last - 1);
-        const KeyRow kr = key_row(c, key, ids[c.by_page(key) - ids_from]);
-        if (kr.bad && chunk == 0) atomicOr(&bad_rows[b % 8][r >> 5], 1u << (r & 31));
+        const int64_t at = key_row(c, key[i], id[i]).at;
         const int ck = many_swizzle_k<DP>(r, chunk), cv = many_swizzle_v<DP>(r, chunk);
-        if (8 * ck < c.D) global_dma16(kc + kr.at + 8 * ck, to + (uint32_t)i * 4096u);
-        if (8 * cv < c.D) global_dma16(vc + kr.at + 8 * cv, to + T::OPERAND + (uint32_t)i * 4096u);
+        if (FULL || 8 * ck < c.D) global_dma16(kc + at + 8 * ck, to + (uint32_t)i * 4096u);
+        if (FULL || 8 * cv < c.D) global_dma16(vc + at + 8 * cv, to + T::OPERAND + (uint32_t)i * 4096u);
       }
     };
 
     if (threadIdx.x < 16) (&bad_rows[0][0])[threadIdx.x] = 0u;
+    if (threadIdx.x == 16) bad_pages = 0u;
+    __syncthreads();
     if (p.b0 < p.b1) fill_ids(p.b0);
     u32x4 q[KS];
 #pragma unroll
@@ -806,6 +827,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
     float m = -INFINITY, l = 0.f;
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): from here on only direct loads to LDS are counted
     __syncthreads();
+    some_bad = uniform((int)bad_pages) != 0;
 #pragma unroll
     for (int i = 0; i < T::STAGES - 1; ++i)
       if (p.b0 + i < p.b1) issue(p.b0 + i);
@@ -829,6 +851,19 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
           x[t] = mfma32(k, q[s], x[t]);
         }
       }
+      // values: 32 t + l % 32 of 16 keys at a time, on their way while the weights are made
+      const int vr = 4 * half + (l16 >> 2);
+      const uint32_t v0 = vt0 + vr * T::PITCH + many_swizzle_v<DP>(vr, 2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1)) * 16 + 8 * (l16 & 1);
+      u32x4 v[DT][2 * KT];
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        const uint32_t at = (v0 ^ ((t & 3) * 64)) + (t >> 2) * 256;
+#pragma unroll
+        for (int s = 0; s < 2 * KT; ++s) {
+          const u32x2 a = read_transposed(at + 16 * s * T::PITCH), b2 = read_transposed(at + (16 * s + 8) * T::PITCH);
+          v[t][s] = u32x4{a[0], a[1], b2[0], b2[1]};
+        }
+      }
       if (threadIdx.x < 2) bad_rows[(b + T::STAGES) % 8][threadIdx.x] = 0u;
       if (b + T::STAGES - 1 < p.b1) issue(b + T::STAGES - 1);
       // a lane's scores are of keys 32 t + 8 (i / 4) + 4 half + i % 4
@@ -847,11 +882,11 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
         // values, they go in one by one
         uint32_t bits = 0;
 #pragma unroll
-        for (int i = 0; i < T::KEYS * T::CH / 64; ++i) {
-          const u32x4 w = *(__attribute__((address_space(3))) const u32x4 *)(size_t)(vt0 + (uint32_t)(i * 64 + lane) * 16u);
+        for (int t = 0; t < DT; ++t)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) bits |= pair_exponents(w[j]);
-        }
+          for (int s = 0; s < 2 * KT; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bits |= pair_exponents(v[t][s][i]);
         odd = __ballot((bits & 0x80008000u) != 0) != 0;
       }
       float top = x[0][0];
@@ -893,27 +928,17 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
               }
             }
         }
-      }
-      const int vr = 4 * half + (l16 >> 2);
-      const uint32_t v0 = vt0 + vr * T::PITCH + many_swizzle_v<DP>(vr, 2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1)) * 16 + 8 * (l16 & 1);
 #pragma unroll
-      for (int t = 0; t < DT; ++t) {
-        u32x4 vt[2 * KT];
-        const uint32_t at = (v0 ^ ((t & 3) * 64)) + (t >> 2) * 256;
-#pragma unroll
-        for (int s = 0; s < 2 * KT; ++s) {
-          const u32x2 a = read_transposed(at + 16 * s * T::PITCH), b2 = read_transposed(at + (16 * s + 8) * T::PITCH);
-          vt[s] = u32x4{a[0], a[1], b2[0], b2[1]};
-        }
-        if (odd) {
+        for (int t = 0; t < DT; ++t)
 #pragma unroll
           for (int s = 0; s < 2 * KT; ++s)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) vt[s][i] = pair_finite(vt[s][i]);
-        }
-#pragma unroll
-        for (int s = 0; s < 2 * KT; ++s) acc[t] = mfma32(vt[s], w[s], acc[t]);
+            for (int i = 0; i < 4; ++i) v[t][s][i] = pair_finite(v[t][s][i]);
       }
+#pragma unroll
+      for (int s = 0; s < 2 * KT; ++s)
+#pragma unroll
+        for (int t = 0; t < DT; ++t) acc[t] = mfma32(v[t][s], w[s], acc[t]);
     }
     l = sum_halves(l);
 
@@ -989,10 +1014,10 @@ int workgroups_of(bool many, int DP, int cus) {
 }
 int padded_head(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
-template <int DP, bool MANY>
+template <int DP, bool MANY, bool FULL>
 int launch(const AttnCall &c, int grid, hipStream_t s) {
   void (*fn)(AttnCall);
-  if constexpr (MANY) fn = attn_many_kernel<DP>;
+  if constexpr (MANY) fn = attn_many_kernel<DP, FULL>;
   else fn = attn_few_kernel<DP>;
   constexpr int lds = MANY ? ManyTile<DP>::STAGES * ManyTile<DP>::STAGE : FewTile<DP>::WAVES * FewTile<DP>::WAVE_BYTES;
   int dev = -1;
@@ -1004,6 +1029,10 @@ int launch(const AttnCall &c, int grid, hipStream_t s) {
     return OCC_EHIP;
   hipLaunchKernelGGL(fn, dim3(grid), dim3(MANY ? ManyTile<DP>::THREADS : FewTile<DP>::THREADS), lds, s, c);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
+}
+template <int DP, bool MANY>
+int launch(const AttnCall &c, int grid, hipStream_t s) {
+  return MANY && c.D == DP ? launch<DP, MANY, true>(c, grid, s) : launch<DP, MANY, false>(c, grid, s);
 }
 template <bool MANY>
 int launch(const AttnCall &c, int DP, int grid, hipStream_t s) {
