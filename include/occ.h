@@ -656,6 +656,7 @@ size_t occ_moe_workspace_bytes(int tokens, int H, int I, int experts, int top_k)
 #define OCC_KV_MAX_REQUESTS 65536
 #define OCC_KV_MAX_PAGE 65536
 #define OCC_ATTN_MAX_KEYS 2147418112   /* keys of a request: 2^31 - 2^16 */
+#define OCC_ATTN_MAX_PITCH 2147483640  /* of pages and of rows, elements: 2^31 - 8 */
 
 /*
  * occ_kv_tables -- a step's block tables, slots and positions from the lengths of its requests.
@@ -726,7 +727,8 @@ int occ_rope(const occ_rope_args *args, void *stream);
  * rows), out is bf16 and lse (rows x Hq, null: not stored) fp32.
  * max_fresh: the most rows of a request; what the choice of kernels goes by (results hold for any).
  * D: a multiple of 8 up to 256; Hq a multiple of Hkv; pitches (elements) multiples of 8, buffers 16-byte aligned,
- * starts, lens, table and lse 4.  rows * Hq < 2^31.
+ * starts, lens, table and lse 4.  rows * Hq < 2^31, (rows + requests) * width * page * Hq < 2^50; cache_page and cache_row at
+ * most OCC_ATTN_MAX_PITCH.
  * workspace: occ_attn_paged_workspace_bytes(Hq, Hkv, D) bytes, 16-byte aligned, zeroed once before its first use (a
  * complete call leaves it ready for the next, of any sizes with this D); calls that share one must not overlap.
  * No workgroup waits for another.

@@ -330,6 +330,9 @@ int validate_attn(const occ_attn_args &a) {
   if (a.requests > 1 && a.ld_table < (size_t)a.width) return OCC_EINVAL;
   if (!apart(a.rows, a.q_row, a.Hq, a.q_head, a.D) || !apart(a.rows, a.out_row, a.Hq, a.out_head, a.D)) return OCC_EINVAL;
   if (!cache_apart(a.pages, a.cache_page, a.page, a.cache_row, a.Hkv, a.cache_head, a.D)) return OCC_EINVAL;
+  // pitches are 32-bit numbers in the kernels, units of work 64-bit ones with some bits to spare
+  if ((a.pages > 1 && a.cache_page > OCC_ATTN_MAX_PITCH) || (a.page > 1 && a.cache_row > OCC_ATTN_MAX_PITCH)) return OCC_EINVAL;
+  if ((double)(a.rows + a.requests) * a.width * a.page * a.Hq >= 0x1p50) return OCC_EINVAL;
   const size_t need = attn_workspace(a.D);
   if (a.workspace_bytes < need) return OCC_EINVAL;
   const size_t cached = (size_t)(a.pages - 1) * a.cache_page * 2 + span3(a.page, a.cache_row, a.Hkv, a.cache_head, a.D, 2);

@@ -35,6 +35,12 @@ __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+// Two values as bf16 in one instruction.
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+}
+
 // 4 rows x 16 columns of 16-bit values in LDS, transposed: lane l of 16 gives the address of row l / 4, columns 4 (l %
 // 4) .. + 3, and gets column l of the 4 rows.
 __device__ __forceinline__ u32x2 read_transposed(uint32_t lds) {
@@ -91,7 +97,8 @@ struct AttnCall {
   Divider by_page;
   size_t table_pitch;
   size_t q_row, q_head, out_row, out_head;           // elements
-  size_t cache_page, cache_row, cache_head;
+  size_t cache_head;
+  uint32_t page_bytes, row_bytes;                    // of the caches
   float scale;         // of the exponent of 2
   AttnCut cut;
   int least, most;     // requests of `least` to `most` rows (tokens x heads of a group) are this launch's
@@ -107,15 +114,34 @@ __device__ __forceinline__ AttnSeq seq_of(const AttnCall &c, int i) {
   return s;
 }
 
-// Where a key's row lies in the caches (elements), and whether its page does.
-struct KeyRow {
-  int64_t at;
-  bool bad;
+// A launch argument in registers of its own: one spilled with its neighbours costs a read of each.
+template <class V>
+__device__ __forceinline__ V own_register(V v) {
+  asm volatile("" : "+s"(v));
+  return v;
+}
+
+// Where keys' rows lie in the caches.
+struct KeyRows {
+  Divider by_page;
+  int page, pages;
+  uint32_t page_bytes, row_bytes;
+  __device__ __forceinline__ explicit KeyRows(const AttnCall &c)
+      : by_page(c.by_page), page(own_register(c.page)), pages(own_register(c.pages)), page_bytes(own_register(c.page_bytes)),
+        row_bytes(own_register(c.row_bytes)) {
+    by_page.mul = own_register(by_page.mul), by_page.shift = own_register(by_page.shift);
+  }
+  __device__ __forceinline__ int page_of(int key) const { return by_page(key); }
+  // A page that is none counts as the first: what is read there is not used.
+  __device__ __forceinline__ bool bad(int id) const { return (uint32_t)id >= (uint32_t)pages; }
+  // Bytes from a cache's beginning to row `off` of page `id`.
+  __device__ __forceinline__ uint64_t at(int id, int off) const {
+    return (uint64_t)(bad(id) ? 0u : (uint32_t)id) * page_bytes + (uint64_t)(uint32_t)off * row_bytes;
+  }
 };
-__device__ __forceinline__ KeyRow key_row(const AttnCall &c, int key, int id) {
-  const int index = c.by_page(key);
-  const bool bad = (uint32_t)id >= (uint32_t)c.pages;
-  return KeyRow{(int64_t)(bad ? 0 : id) * (int64_t)c.cache_page + (int64_t)(key - index * c.page) * (int64_t)c.cache_row, bad};
+template <class V>
+__device__ __forceinline__ const V *plus(const void *p, uint64_t bytes) {
+  return reinterpret_cast<const V *>(static_cast<const char *>(p) + bytes);
 }
 
 template <int THREADS>
@@ -419,6 +445,7 @@ __global__ __launch_bounds__(FewTile<DP>::THREADS, FewTile<DP>::PER_CU) void att
   const int l16 = lane & 15, g = lane >> 4;
   unsigned char *mine = smem + wave * T::WAVE_BYTES;
   const uint32_t mine_lds = lds_address(mine);
+  const KeyRows rows(c);
   const int me = (int)blockIdx.x;
 
   Walk<T::THREADS, true> walk(c, sh, me, (int)gridDim.x);
@@ -435,14 +462,15 @@ __global__ __launch_bounds__(FewTile<DP>::THREADS, FewTile<DP>::PER_CU) void att
     // set of registers each, and something in flight at all times.  The page numbers of the block after
     // are asked for before either, so that waiting for them does not wait for these.
     u32x4 k[TILES][KS], v[TILES][KS];
-    int ids[TILES], keys[TILES];
-    int64_t at[TILES];
+    int ids[TILES], keys[TILES], pages[TILES];
+    uint64_t at[TILES];
     uint32_t bad = 0, next_bad = 0;  // a bit for each key of the block whose page is none
     auto ask = [&](int b) {
 #pragma unroll
       for (int t = 0; t < TILES; ++t) {
         keys[t] = min(p.first + b * T::KEYS + 16 * t + l16, p.last - 1);
-        ids[t] = table[c.by_page(keys[t])];
+        pages[t] = rows.page_of(keys[t]);
+        ids[t] = table[pages[t]];
       }
     };
     auto load = [&](u32x4 (&to)[TILES][KS], const uint16_t *from) {
@@ -451,16 +479,15 @@ __global__ __launch_bounds__(FewTile<DP>::THREADS, FewTile<DP>::PER_CU) void att
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
           to[t][s] = u32x4{0u, 0u, 0u, 0u};
-          if (32 * s + 8 * g < c.D) to[t][s] = *reinterpret_cast<const u32x4 *>(from + at[t] + 32 * s);
+          if (32 * s + 8 * g < c.D) to[t][s] = *plus<u32x4>(from + 32 * s, at[t]);
         }
     };
     auto load_keys = [&](int b) {
       next_bad = 0;
 #pragma unroll
       for (int t = 0; t < TILES; ++t) {
-        const KeyRow r = key_row(c, keys[t], ids[t]);
-        at[t] = r.at;
-        next_bad |= ((uint32_t)__ballot(r.bad) & 0xFFFFu) << (16 * t);
+        at[t] = rows.at(ids[t], keys[t] - pages[t] * rows.page);
+        next_bad |= ((uint32_t)__ballot(rows.bad(ids[t])) & 0xFFFFu) << (16 * t);
       }
       if (b + T::WAVES < p.b1) ask(b + T::WAVES);
       load(k, kc);
@@ -523,8 +550,8 @@ __global__ __launch_bounds__(FewTile<DP>::THREADS, FewTile<DP>::PER_CU) void att
       u32x4 hi, lo;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        hi[i] = pack_bf16(e[2 * i], e[2 * i + 1]);
-        lo[i] = pack_bf16(e[2 * i] - bf16_lo(hi[i]), e[2 * i + 1] - bf16_hi(hi[i]));
+        hi[i] = pack2(e[2 * i], e[2 * i + 1]);
+        lo[i] = pack2(e[2 * i] - bf16_lo(hi[i]), e[2 * i + 1] - bf16_hi(hi[i]));
       }
 #pragma unroll
       for (int t = 0; t < DT; ++t) acc[t] = acc[t] * less;
@@ -675,7 +702,7 @@ __global__ __launch_bounds__(FewTile<DP>::THREADS, FewTile<DP>::PER_CU) void att
         const float by = some ? 1.f / total : 0.f;
         if (4 * ch < c.D)
           *reinterpret_cast<u32x2 *>(c.out + (size_t)w.token * c.out_row + (size_t)w.head * c.out_head + 4 * ch) =
-              u32x2{pack_bf16(sum[n][0] * by, sum[n][1] * by), pack_bf16(sum[n][2] * by, sum[n][3] * by)};
+              u32x2{pack2(sum[n][0] * by, sum[n][1] * by), pack2(sum[n][2] * by, sum[n][3] * by)};
         if (ch == 0 && c.lse != nullptr)
           c.lse[(size_t)w.token * c.Hq + w.head] = some ? (ms[n][0] + __builtin_amdgcn_logf(total)) * kLn2 : -INFINITY;
       }
@@ -686,28 +713,31 @@ __global__ __launch_bounds__(FewTile<DP>::THREADS, FewTile<DP>::PER_CU) void att
 
 // ------------------------------------------------------------------ many rows
 //
-// Chunks of a prompt: 128 rows (tokens times heads that share keys) of a workgroup's 4 waves, 32 each, against
-// tiles of 32 or 64 keys in a ring of four that direct-to-LDS loads fill three tiles ahead.  S^T = K Q^T in 32x32x16
-// MFMAs leaves a lane 16 keys' scores of one row (the other half of the wave has the other 16), which,
-// rounded to bf16, are the second product's operand as they lie: O^T = V^T P^T over the keys in that order, values
-// read transposed.  m and l are one register a lane, and so is what o has to be scaled by.  The weights' rounding (8
-// bits) is of the same size as the output's own; l sums them unrounded.
+// Chunks of a prompt: 256 rows (128 with heads beyond 128 values) of tokens times heads that share keys, 32 of each
+// wave, against tiles of keys in a ring of four that direct-to-LDS loads fill ahead.  S^T = K Q^T in 32x32x16 MFMAs leaves a lane
+// 16 of 32 keys' scores of one row (the other half of the wave has the other 16), which, rounded to bf16, are the
+// second product's operand as they lie: O^T = V^T P^T over the keys in that order, values read transposed.  m and l are
+// one register a lane, and so is what o has to be scaled by.  The weights' rounding (8 bits) is of the same size as the output's
+// own; l sums them unrounded.
 // Scaling o costs as much as half of a tile's exponentials: m stays behind the maximum until it would have to grow by
 // kSlack, so that weights are up to 2^kSlack and o is scaled once or twice in all.
 template <int DP>
 struct ManyTile {
-  static constexpr int THREADS = 256;
-  static constexpr int ROWS = 128, KEYS = DP > 64 ? 32 : 64;
+  static constexpr bool PAIRS = DP <= 128;             // two waves a SIMD that take turns, see attn_pairs_kernel
+  static constexpr int THREADS = PAIRS ? 512 : 256, WAVES = THREADS / 64;
+  static constexpr int ROWS = 32 * WAVES, KEYS = PAIRS ? 64 : 32;
   static constexpr int KS = DP / 16, DT = DP / 32, KT = KEYS / 32;
   static constexpr int CH = DP / 8;                    // 16-byte chunks of a row
   static constexpr int PITCH = DP * 2;
   static constexpr int OPERAND = KEYS * PITCH;         // bytes of a tile of K, and of V
   static constexpr int STAGES = 4, STAGE = 2 * OPERAND;
+  static constexpr int ZEROS = PAIRS ? OPERAND : 0;    // bytes of zeros behind the ring
+  static constexpr int LDS = STAGES * STAGE + ZEROS;
   static constexpr int PASS_ROWS = THREADS / CH, PASSES = KEYS / PASS_ROWS;
   static constexpr int DMAS = 2 * PASSES;              // of a wave for a tile
   static constexpr int PART = ROWS * (DP + 2);
-  static constexpr int PER_CU = DP > 128 ? 1 : 2;
-  static constexpr int IDS = 512;                      // page numbers at hand
+  static constexpr int PER_CU = 1;
+  static constexpr int IDS = 256;                      // page numbers that a wave has at hand
 };
 constexpr float kSlack = 8.f;
 
@@ -734,220 +764,247 @@ __device__ __forceinline__ void global_dma16(const void *from, uint32_t lds) {
 }
 #pragma clang diagnostic pop
 
+// What the workgroup shares beside the tiles.
+template <int DP>
+struct ManyShared {
+  WalkShared<ManyTile<DP>::THREADS> walk;
+  int32_t ids[ManyTile<DP>::WAVES][ManyTile<DP>::IDS];
+  uint32_t bad_rows[8][2];  // keys of tile b whose page is none: [b % 8]
+};
+
+// A wave's loads of an item's tiles: all waves load a part of each.
 // FULL: heads of DP values, no fewer.
 template <int DP, bool FULL>
-__global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void attn_many_kernel(AttnCall c) {
+struct TileLoads {
   using T = ManyTile<DP>;
-  constexpr int KS = T::KS, DT = T::DT, KT = T::KT;
-  extern __shared__ __align__(256) unsigned char stages[];
-  __shared__ WalkShared<T::THREADS> sh;
-  __shared__ int32_t ids[T::IDS];
-  __shared__ uint32_t bad_rows[8][2];  // keys of tile b whose page is none: [b % 8]
-  __shared__ uint32_t bad_pages;       // whether some page at hand is none
-  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
-  const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
-  const uint32_t lds0 = lds_address(stages);
-  const auto rs = rsrc_of(c.part, gridDim.x * 2u * (uint32_t)(T::PART * 4));
-  const int me = (int)xcd_remap(blockIdx.x, gridDim.x);
+  const KeyRows &rows;
+  const Piece &p;
+  ManyShared<DP> &sh;
+  const int32_t *table;
+  const uint16_t *k, *v;   // of the item's head
+  int D, wave, lane;
+  uint32_t lds;            // of the ring
+  int32_t *ids;
+  int ids_from, plain_until;
+  bool some_bad, ever_bad; // whether some page at hand, or of the item so far, is none
+  // page and row within it of this thread's keys of the tile that is issued next
+  int index[T::PASSES], off[T::PASSES], step_pages, step_rows;
 
-  // chunks that the heads do not have stay zero
-  if (!FULL)
-    for (int i = threadIdx.x; i < T::STAGES * T::STAGE / 16; i += T::THREADS) reinterpret_cast<u32x4 *>(stages)[i] = u32x4{0u, 0u, 0u, 0u};
-
-  Walk<T::THREADS, false> walk(c, sh, me, (int)gridDim.x);
-#pragma unroll 1
-  for (; walk.next(); walk.done()) {
-    const Piece &p = walk.p;
-    const Row row = row_of(c, p, wave * 32 + l32);
-    int all_lo, all_hi;
-    seen_by_all(c, p, c.by_heads(wave * 32), c.by_heads(wave * 32 + 31) + 1, all_lo, all_hi);
-    const int32_t *table = c.table + (size_t)p.request * c.table_pitch;
-    const uint16_t *kc = c.k + (size_t)p.kv * c.cache_head, *vc = c.v + (size_t)p.kv * c.cache_head;
-    const int r_in = threadIdx.x / T::CH, chunk = threadIdx.x % T::CH;
-
-    int ids_from = 0;
-    bool some_bad = false;
-    auto fill_ids = [&](int b) {  // page numbers from tile b's first on
-      ids_from = c.by_page(p.first + b * T::KEYS);
-      const int end = c.by_page(min(p.first + p.b1 * T::KEYS, p.last) - 1) + 1;
-      for (int i = threadIdx.x; i < T::IDS; i += T::THREADS)
-        if (ids_from + i < end) {
-          const int id = table[ids_from + i];
-          ids[i] = id;
-          if ((uint32_t)id >= (uint32_t)c.pages) bad_pages = 1u;
-        }
-    };
-    auto issue = [&](int b) {
-      if (c.by_page(min(p.first + (b + 1) * T::KEYS, p.last) - 1) >= ids_from + T::IDS) {
-        __syncthreads();
-        fill_ids(b);
-        __syncthreads();
-        some_bad = uniform((int)bad_pages) != 0;
-      }
-      const uint32_t to = lds0 + (uint32_t)(b % T::STAGES) * T::STAGE + (uint32_t)wave * 1024u;
-      int id[T::PASSES], key[T::PASSES];
+  __device__ __forceinline__ int row(int i) const { return i * T::PASS_ROWS + (wave * 64 + lane) / T::CH; }
+  __device__ __forceinline__ void find(int b) {
 #pragma unroll
-      for (int i = 0; i < T::PASSES; ++i) {
-        key[i] = min(p.first + b * T::KEYS + i * T::PASS_ROWS + r_in, p.last - 1);
-        id[i] = ids[c.by_page(key[i]) - ids_from];
-      }
-      if (some_bad) {
-#pragma unroll
-        for (int i = 0; i < T::PASSES; ++i) {
-          const int r = i * T::PASS_ROWS + r_in;
-          if ((uint32_t)id[i] >= (uint32_t)c.pages && chunk == 0) atomicOr(&bad_rows[b % 8][r >> 5], 1u << (r & 31));
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < T::PASSES; ++i) {
-        const int r = i * T::PASS_ROWS + r_in;
-        const int64_t at = key_row(c, key[i], id[i]).at;
-        const int ck = many_swizzle_k<DP>(r, chunk), cv = many_swizzle_v<DP>(r, chunk);
-        if (FULL || 8 * ck < c.D) global_dma16(kc + at + 8 * ck, to + (uint32_t)i * 4096u);
-        if (FULL || 8 * cv < c.D) global_dma16(vc + at + 8 * cv, to + T::OPERAND + (uint32_t)i * 4096u);
-      }
-    };
-
-    if (threadIdx.x < 16) (&bad_rows[0][0])[threadIdx.x] = 0u;
-    if (threadIdx.x == 16) bad_pages = 0u;
-    __syncthreads();
-    if (p.b0 < p.b1) fill_ids(p.b0);
-    u32x4 q[KS];
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      q[s] = u32x4{0u, 0u, 0u, 0u};
-      if (row.valid && 16 * s + 8 * half < c.D)
-        q[s] = *reinterpret_cast<const u32x4 *>(c.q + (size_t)row.token * c.q_row + (size_t)row.head * c.q_head + 16 * s + 8 * half);
+    for (int i = 0; i < T::PASSES; ++i) {
+      const int key = min(p.first + b * T::KEYS + row(i), p.last - 1);
+      index[i] = rows.page_of(key), off[i] = key - index[i] * rows.page;
     }
-    f32x16 acc[DT];
+  }
+  __device__ __forceinline__ void fill(int b) {  // page numbers from tile b's first on
+    ids_from = rows.page_of(p.first + b * T::KEYS);
+    const int end = rows.page_of(min(p.first + p.b1 * T::KEYS, p.last) - 1) + 1;
+    bool bad = false;
+#pragma unroll 1
+    for (int i = lane; i < T::IDS; i += 64)
+      if (ids_from + i < end) {
+        const int id = table[ids_from + i];
+        ids[i] = id;
+        bad = bad || rows.bad(id);
+      }
+    some_bad = __ballot(bad) != 0;
+    asm volatile("" ::: "memory");  // the wave's LDS accesses are served in order
+    // whole tiles, and those whose page numbers are at hand
+    const int64_t known = (int64_t)(ids_from + T::IDS) * rows.page - p.first;
+    plain_until = some_bad ? 0 : (int)(min((int64_t)(p.last - p.first), known) / T::KEYS);
+  }
+  // What the loads of tiles from plain_until on need beside the others': where keys lie, if the tile is not whole (or past
+  // the last one), page numbers that are not at hand, a note of pages that are none.
+  __device__ __forceinline__ void prepare(int b) {
+    asm volatile("" : "+s"(b));  // a branch: none of this is made for the others
+    const int end = p.first + (b + 1) * T::KEYS;
+    if (end > p.last) find(b);
+    if (rows.page_of(min(end, p.last) - 1) >= ids_from + T::IDS) fill(b);
+    if (some_bad) {
+      ever_bad = true;
 #pragma unroll
-    for (int t = 0; t < DT; ++t)
+      for (int i = 0; i < T::PASSES; ++i)
+        if (rows.bad(ids[index[i] - ids_from]) && lane % T::CH == 0) atomicOr(&sh.bad_rows[b % 8][row(i) >> 5], 1u << (row(i) & 31));
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): there for the barrier
+    }
+  }
+  // The page numbers of tile b, then its loads, which are on their way after this; the stage's earlier tile has been
+  // read.  Past the last tile the last key is loaded, which nobody reads: every wave has as many loads in every slot.
+  __device__ __forceinline__ void pages(int (&id)[T::PASSES]) const {
+#pragma unroll
+    for (int i = 0; i < T::PASSES; ++i) id[i] = ids[index[i] - ids_from];
+  }
+  __device__ __forceinline__ void issue(int b, const int (&id)[T::PASSES]) {
+    const uint32_t to = lds + (uint32_t)(b % T::STAGES) * T::STAGE + (uint32_t)wave * 1024u;
+#pragma unroll
+    for (int i = 0; i < T::PASSES; ++i) {
+      const int r = row(i), chunk = lane % T::CH;
+      const uint64_t at = rows.at(id[i], off[i]);
+      const int ck = many_swizzle_k<DP>(r, chunk), cv = many_swizzle_v<DP>(r, chunk);
+      if (FULL || 8 * ck < D) global_dma16(plus<uint16_t>(k + 8 * ck, at), to + (uint32_t)(i * T::THREADS * 16));
+      if (FULL || 8 * cv < D) global_dma16(plus<uint16_t>(v + 8 * cv, at), to + T::OPERAND + (uint32_t)(i * T::THREADS * 16));
+      index[i] += step_pages, off[i] += step_rows;
+      const bool over = off[i] >= rows.page;
+      off[i] -= over ? rows.page : 0, index[i] += over ? 1 : 0;
+    }
+  }
+  __device__ __forceinline__ void all(int b) {
+    int id[T::PASSES];
+    if (b >= plain_until) prepare(b);
+    pages(id);
+    issue(b, id);
+  }
+};
+
+// The operands' fragments as a wave reads them from a tile.
+template <int DP>
+struct Fragments {
+  using T = ManyTile<DP>;
+  uint32_t k0, v0, vt0;
+  __device__ __forceinline__ Fragments(uint32_t lds, int lane) {
+    const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15, r = 4 * half + (l16 >> 2);
+    k0 = lds + (uint32_t)(l32 * T::PITCH + many_swizzle_k<DP>(l32, half) * 16);
+    vt0 = lds + T::OPERAND;
+    v0 = vt0 + r * T::PITCH + many_swizzle_v<DP>(r, 2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1)) * 16 + 8 * (l16 & 1);
+  }
+  // Key 32 t + l % 32, values 16 s + 8 (l / 32) .. + 7.
+  __device__ __forceinline__ void keys(int b, int t, u32x4 (&k)[T::KS]) const {
+    const uint32_t from = k0 + (uint32_t)(b % T::STAGES) * T::STAGE;
+#pragma unroll
+    for (int s = 0; s < T::KS; ++s)
+      k[s] = *(__attribute__((address_space(3))) const u32x4 *)(size_t)((from ^ ((s & 7) * 32)) + (s >> 3) * 256 + 32 * t * T::PITCH);
+  }
+  // Values 32 (t0 + t) + l % 32 of the 8 keys of 16 s .. that the lane's weights are of.
+  __device__ __forceinline__ uint32_t stage(int b) const { return (uint32_t)(b % T::STAGES) * T::STAGE; }
+  template <int N>
+  __device__ __forceinline__ void values(uint32_t stage, int t0, u32x4 (&v)[N][2 * T::KT]) const {
+    const uint32_t from = v0 + stage;
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+      const uint32_t at = (from ^ (((t0 + t) & 3) * 64)) + ((t0 + t) >> 2) * 256;
+#pragma unroll
+      for (int s = 0; s < 2 * T::KT; ++s) {
+        const u32x2 a = read_transposed(at + 16 * s * T::PITCH), b2 = read_transposed(at + (16 * s + 8) * T::PITCH);
+        v[t][s] = u32x4{a[0], a[1], b2[0], b2[1]};
+      }
+    }
+  }
+};
+
+// A wave's rows, their running maximum and sum (in powers of 2) and o.
+template <int DP>
+struct RowState {
+  using T = ManyTile<DP>;
+  f32x16 acc[T::DT];
+  float m, l;
+  __device__ __forceinline__ void clear() {
+    m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int t = 0; t < T::DT; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
-    float m = -INFINITY, l = 0.f;
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): from here on only direct loads to LDS are counted
-    __syncthreads();
-    some_bad = uniform((int)bad_pages) != 0;
-#pragma unroll
-    for (int i = 0; i < T::STAGES - 1; ++i)
-      if (p.b0 + i < p.b1) issue(p.b0 + i);
-#pragma unroll 1
-    for (int b = p.b0; b < p.b1; ++b) {
-      wait_stages<T::STAGES - 2, T::DMAS>(min(T::STAGES - 2, p.b1 - 1 - b));
-      __syncthreads();  // tile b has landed, and nobody reads the one before any more
-      const int kb = p.first + b * T::KEYS;
-      const uint32_t kt = lds0 + (uint32_t)(b % T::STAGES) * T::STAGE, vt0 = kt + T::OPERAND;
-      const uint32_t bad0 = bad_rows[b % 8][0], bad1 = KT > 1 ? bad_rows[b % 8][KT - 1] : 0u;
-      f32x16 x[KT];
-#pragma unroll
-      for (int t = 0; t < KT; ++t) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[t][i] = 0.f;
-        const uint32_t at = kt + (uint32_t)((32 * t + l32) * T::PITCH + many_swizzle_k<DP>(l32, half) * 16);
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-          const uint32_t a = (at ^ ((s & 7) * 32)) + (s >> 3) * 256;
-          const u32x4 k = *(__attribute__((address_space(3))) const u32x4 *)(size_t)a;
-          x[t] = mfma32(k, q[s], x[t]);
-        }
-      }
-      // values: 32 t + l % 32 of 16 keys at a time, on their way while the weights are made
-      const int vr = 4 * half + (l16 >> 2);
-      const uint32_t v0 = vt0 + vr * T::PITCH + many_swizzle_v<DP>(vr, 2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1)) * 16 + 8 * (l16 & 1);
-      u32x4 v[DT][2 * KT];
-#pragma unroll
-      for (int t = 0; t < DT; ++t) {
-        const uint32_t at = (v0 ^ ((t & 3) * 64)) + (t >> 2) * 256;
-#pragma unroll
-        for (int s = 0; s < 2 * KT; ++s) {
-          const u32x2 a = read_transposed(at + 16 * s * T::PITCH), b2 = read_transposed(at + (16 * s + 8) * T::PITCH);
-          v[t][s] = u32x4{a[0], a[1], b2[0], b2[1]};
-        }
-      }
-      if (threadIdx.x < 2) bad_rows[(b + T::STAGES) % 8][threadIdx.x] = 0u;
-      if (b + T::STAGES - 1 < p.b1) issue(b + T::STAGES - 1);
+  }
+  // Scores of the keys from kb on (tile b) to weights.  `masked`: not all are seen by all rows.  True if there are
+  // infinities or NaN among such a tile's values: they must not reach rows that do not see them, and have gone into o
+  // one by one.
+  __device__ __forceinline__ bool weigh(f32x16 (&x)[T::KT], u32x4 (&w)[2 * T::KT], float scale, bool masked, int b, int kb, const Row &row,
+                                        uint32_t bad0, uint32_t bad1, const Fragments<DP> &from, int lane) {
+    const int half = lane >> 5;
+    const uint32_t vt0 = from.vt0 + (uint32_t)(b % T::STAGES) * T::STAGE;
+    bool odd = false;
+    if (masked) {
       // a lane's scores are of keys 32 t + 8 (i / 4) + 4 half + i % 4
-      const bool masked = kb < all_lo || kb + T::KEYS > all_hi || uniform((int)(bad0 | bad1)) != 0;
-      bool odd = false;
-      if (masked) {
+      const int lo = row.lo - kb - 4 * half, hi = row.hi - kb - 4 * half;
 #pragma unroll
-        for (int t = 0; t < KT; ++t)
+      for (int t = 0; t < T::KT; ++t) {
+        const uint32_t bad = (t ? bad1 : bad0) >> (4 * half);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int at = 8 * (i >> 2) + 4 * half + (i & 3);
-            const bool seen = kb + 32 * t + at >= row.lo && kb + 32 * t + at < row.hi && !(((t ? bad1 : bad0) >> at) & 1u);
-            x[t][i] = seen ? x[t][i] : -INFINITY;
-          }
-        // a value that a row does not see must not reach it, whatever it is: if there are infinities or NaN among the
-        // values, they go in one by one
-        uint32_t bits = 0;
-#pragma unroll
-        for (int t = 0; t < DT; ++t)
-#pragma unroll
-          for (int s = 0; s < 2 * KT; ++s)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) bits |= pair_exponents(v[t][s][i]);
-        odd = __ballot((bits & 0x80008000u) != 0) != 0;
-      }
-      float top = x[0][0];
-#pragma unroll
-      for (int i = 1; i < 16 * KT; ++i) top = fmaxf(top, x[i >> 4][i & 15]);
-      top = max_halves(top) * c.scale;
-      if (__ballot(top > m + kSlack) != 0) {
-        const float now = fmaxf(m, top), less = now == -INFINITY ? 1.f : exp2_(m - now);
-        m = now;
-        l = l * less;
-#pragma unroll
-        for (int t = 0; t < DT; ++t) acc[t] = acc[t] * less;
-      }
-      const float by = m == -INFINITY ? 0.f : m;
-      u32x4 w[2 * KT];
-#pragma unroll
-      for (int t = 0; t < KT; ++t)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float e0 = exp2_(__builtin_fmaf(x[t][2 * i], c.scale, -by)), e1 = exp2_(__builtin_fmaf(x[t][2 * i + 1], c.scale, -by));
-          l = l + (e0 + e1);
-          w[2 * t + (i >> 2)][i & 3] = pack_bf16(e0, e1);
+        for (int i = 0; i < 16; ++i) {
+          const int at = 8 * (i >> 2) + (i & 3);
+          x[t][i] = 32 * t + at >= lo && 32 * t + at < hi && !((bad >> at) & 1u) ? x[t][i] : -INFINITY;
         }
-      if (odd) {
-#pragma unroll 1
-        for (int r = 0; r < T::KEYS; ++r) {
-          const bool seen = kb + r >= row.lo && kb + r < row.hi && !(((r & 32 ? bad1 : bad0) >> (r & 31)) & 1u);
-#pragma unroll
-          for (int t = 0; t < DT; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              // values 32 t + 8 i + 4 half .. + 3 of key r
-              const uint32_t a = vt0 + r * T::PITCH + many_swizzle_v<DP>(r, 4 * t + i) * 16 + 8 * half;
-              const u32x2 h = *(__attribute__((address_space(3))) const u32x2 *)(size_t)a;
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const uint32_t f = (h[j >> 1] >> (16 * (j & 1))) & 0xFFFFu;
-                if (seen && (f & 0x7F80u) == 0x7F80u) acc[t][4 * i + j] = acc[t][4 * i + j] + as_float(f << 16);
-              }
-            }
-        }
-#pragma unroll
-        for (int t = 0; t < DT; ++t)
-#pragma unroll
-          for (int s = 0; s < 2 * KT; ++s)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[t][s][i] = pair_finite(v[t][s][i]);
       }
+      uint32_t bits = 0;
+#pragma unroll 4
+      for (int i = 0; i < T::OPERAND / 1024; ++i) {
+        const u32x4 four = *(__attribute__((address_space(3))) const u32x4 *)(size_t)(vt0 + (uint32_t)(i * 64 + lane) * 16u);
 #pragma unroll
-      for (int s = 0; s < 2 * KT; ++s)
-#pragma unroll
-        for (int t = 0; t < DT; ++t) acc[t] = mfma32(v[t][s], w[s], acc[t]);
+        for (int j = 0; j < 4; ++j) bits |= pair_exponents(four[j]);
+      }
+      odd = __ballot((bits & 0x80008000u) != 0) != 0;
     }
-    l = sum_halves(l);
+    float top = x[0][0];
+#pragma unroll
+    for (int i = 1; i < 16 * T::KT; ++i) top = fmaxf(top, x[i >> 4][i & 15]);
+    top = max_halves(top) * scale;
+    if (__ballot(top > m + kSlack) != 0) {
+      const float now = fmaxf(m, top), less = now == -INFINITY ? 1.f : exp2_(m - now);
+      m = now;
+      l = l * less;
+#pragma unroll
+      for (int t = 0; t < T::DT; ++t) acc[t] = acc[t] * less;
+    }
+    if (odd) {
+#pragma unroll 1
+      for (int r = 0; r < T::KEYS; ++r) {
+        const bool seen = kb + r >= row.lo && kb + r < row.hi && !(((r & 32 ? bad1 : bad0) >> (r & 31)) & 1u);
+#pragma unroll
+        for (int t = 0; t < T::DT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            // values 32 t + 8 i + 4 half .. + 3 of key r
+            const uint32_t a = vt0 + r * T::PITCH + many_swizzle_v<DP>(r, 4 * t + i) * 16 + 8 * half;
+            const u32x2 h = *(__attribute__((address_space(3))) const u32x2 *)(size_t)a;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t f = (h[j >> 1] >> (16 * (j & 1))) & 0xFFFFu;
+              if (seen && (f & 0x7F80u) == 0x7F80u) acc[t][4 * i + j] = acc[t][4 * i + j] + as_float(f << 16);
+            }
+          }
+      }
+    }
+    const float by = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int t = 0; t < T::KT; ++t)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float e0 = exp2_(__builtin_fmaf(x[t][2 * i], scale, -by)), e1 = exp2_(__builtin_fmaf(x[t][2 * i + 1], scale, -by));
+        l = l + (e0 + e1);
+        w[2 * t + (i >> 2)][i & 3] = pack2(e0, e1);
+      }
+    return odd;
+  }
+  // Infinities and NaN that weigh() has seen to, out of the values.
+  template <int N>
+  __device__ __forceinline__ static void only_finite(u32x4 (&v)[N][2 * T::KT]) {
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+      for (int s = 0; s < 2 * T::KT; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[t][s][i] = pair_finite(v[t][s][i]);
+  }
+  // o of the values 32 t0 and on.
+  template <int N>
+  __device__ __forceinline__ void multiply(const u32x4 (&v)[N][2 * T::KT], const u32x4 (&w)[2 * T::KT], int t0) {
+#pragma unroll
+    for (int s = 0; s < 2 * T::KT; ++s)
+#pragma unroll
+      for (int t = 0; t < N; ++t) acc[t0 + t] = mfma32(v[t][s], w[s], acc[t0 + t]);
+  }
 
-    const int r = wave * 32 + l32;
+  // The item's part is whole: to the output, or beside the others' and, if it is the last of them, joined.
+  __device__ __forceinline__ void finish(const AttnCall &c, WalkShared<T::THREADS> &sh, const Piece &p, const AttnShare &share, const Row &row,
+                                         int me, int r, int half) {
+    const auto rs = rsrc_of(c.part, gridDim.x * 2u * (uint32_t)(T::PART * 4));
+    l = sum_halves(l);
     bool write = true;
     if (!p.alone) {
       const uint32_t slot = place_of(me, p.began, T::PART);
 #pragma unroll
-      for (int t = 0; t < DT; ++t)
+      for (int t = 0; t < T::DT; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const f32x4 v = {acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]};
@@ -957,15 +1014,11 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
       if (half == 0)
         __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f32x2{m, l}), rs,
                                               (int)(slot + (uint32_t)(T::ROWS * DP + 2 * r) * 4u), 0, kDevice);
-      const Joining join = joining(c, p, walk.share);
+      const Joining join = joining(c, p, share);
       const int parts = join.parts;
       write = last_of(c, sh, join);
       if (write) {
-        m = -INFINITY, l = 0.f;
-#pragma unroll
-        for (int t = 0; t < DT; ++t)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
+        clear();
 #pragma unroll 1
         for (int s = 0; s < parts; ++s) {
           const uint32_t slot = place_of(join, s, T::PART);
@@ -975,7 +1028,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
           m = now;
           l = __builtin_fmaf(t2[1], f1, l * f0);
 #pragma unroll
-          for (int t = 0; t < DT; ++t)
+          for (int t = 0; t < T::DT; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const f32x4 v = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
@@ -991,35 +1044,254 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
       const float by = some ? 1.f / l : 0.f;
       uint16_t *to = c.out + (size_t)row.token * c.out_row + (size_t)row.head * c.out_head;
 #pragma unroll
-      for (int t = 0; t < DT; ++t)
+      for (int t = 0; t < T::DT; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int d = 32 * t + 8 * i + 4 * half;
           if (d < c.D)
-            *reinterpret_cast<u32x2 *>(to + d) = u32x2{pack_bf16(acc[t][4 * i] * by, acc[t][4 * i + 1] * by),
-                                                       pack_bf16(acc[t][4 * i + 2] * by, acc[t][4 * i + 3] * by)};
+            *reinterpret_cast<u32x2 *>(to + d) = u32x2{pack2(acc[t][4 * i] * by, acc[t][4 * i + 1] * by),
+                                                       pack2(acc[t][4 * i + 2] * by, acc[t][4 * i + 3] * by)};
         }
       if (half == 0 && c.lse != nullptr)
         c.lse[(size_t)row.token * c.Hq + row.head] = some ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
     }
+  }
+};
+
+// The schedule of what precedes: N matrix instructions, each followed by reads of LDS and vector instructions.
+template <int N, int READS, int VALU>
+__device__ __forceinline__ void interleave() {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if constexpr (READS > 0) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    if constexpr (VALU > 0) __builtin_amdgcn_sched_group_barrier(0x002, VALU, 0);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Heads up to 128 values.  Two waves share a SIMD, one of waves 0-3 and one of waves 4-7, and take turns at the matrix
+// pipe: in every slot one multiplies (o of the tile before, then the scores of this one: 32 MFMAs, 1024 cycles, with heads of
+// 128) while the other makes weights (about as long), waves 4-7 one slot behind.  A barrier ends a slot.
+//   Scores of tile b are made by waves 0-3 in slot 2 b and by waves 4-7 in slot 2 b + 1, o of it two slots later: its place in
+// the ring is free from slot 2 b + 4 on.  All waves ask for their part of tile b + 3 in the slot that has scores of
+// tile b + 1 (2 b + 2, 2 b + 3), in the time that the matrix instructions leave.  Each waits for its loads of tile b + 1 before the
+// barrier that ends slot 2 b + 1, after which waves 0-3 read it: later ones, of tile b + 2, may be outstanding.
+template <int DP, bool FULL>
+__global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void attn_pairs_kernel(AttnCall c) {
+  using T = ManyTile<DP>;
+  constexpr int KS = T::KS, DT = T::DT, KT = T::KT;
+  extern __shared__ __align__(256) unsigned char ring[];
+  __shared__ ManyShared<DP> sh;
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
+  const bool behind = wave >= 4;
+  const uint32_t lds = lds_address(ring);
+  const KeyRows rows(c);
+  const float scale = own_register(c.scale);
+  const Fragments<DP> from(lds, lane);
+  const int me = (int)xcd_remap(blockIdx.x, gridDim.x);
+
+  // chunks that the heads do not have stay zero, and what lies behind the ring
+  for (int i = (FULL ? T::STAGES * T::STAGE / 16 : 0) + threadIdx.x; i < T::LDS / 16; i += T::THREADS)
+    reinterpret_cast<u32x4 *>(ring)[i] = u32x4{0u, 0u, 0u, 0u};
+  auto barrier = [&]() {  // nothing moves across it
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  Walk<T::THREADS, false> walk(c, sh.walk, me, (int)gridDim.x);
+#pragma unroll 1
+  for (; walk.next(); walk.done()) {
+    const Piece &p = walk.p;
+    const Row row = row_of(c, p, wave * 32 + (lane & 31));
+    int all_lo, all_hi;
+    seen_by_all(c, p, c.by_heads(wave * 32), c.by_heads(wave * 32 + 31) + 1, all_lo, all_hi);
+    // tiles whose keys all rows see
+    const int clear_from = uniform((max(all_lo - p.first, 0) + T::KEYS - 1) / T::KEYS), clear_to = uniform(max(all_hi - p.first, 0) / T::KEYS);
+    TileLoads<DP, FULL> loads{rows, p, sh, c.table + (size_t)p.request * c.table_pitch, c.k + (size_t)p.kv * c.cache_head,
+                              c.v + (size_t)p.kv * c.cache_head, c.D, wave, lane, lds, sh.ids[wave]};
+    loads.ever_bad = false;
+    loads.step_pages = rows.page_of(T::KEYS), loads.step_rows = T::KEYS - loads.step_pages * rows.page;
+    if (threadIdx.x < 16) (&sh.bad_rows[0][0])[threadIdx.x] = 0u;
+    if (p.b0 < p.b1) loads.fill(p.b0), loads.find(p.b0);
+    u32x4 q[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      q[s] = u32x4{0u, 0u, 0u, 0u};
+      if (row.valid && (FULL || 16 * s + 8 * half < c.D))
+        q[s] = *reinterpret_cast<const u32x4 *>(c.q + (size_t)row.token * c.q_row + (size_t)row.head * c.q_head + 16 * s + 8 * half);
+    }
+    RowState<DP> state;
+    state.clear();
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): from here on only direct loads to LDS are counted
+    __syncthreads();
+    if (p.b0 < p.b1) {
+      for (int i = 0; i < 3; ++i) loads.all(p.b0 + i);
+      wait_vmcnt<2 * T::DMAS>();
+      barrier();
+      if (behind) barrier();
+      f32x16 x[KT];
+      auto score = [&](const u32x4 (&k)[KS], f32x16 &to) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) to[i] = 0.f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) to = mfma32(k[s], q[s], to);
+      };
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+        u32x4 k[KS];
+        from.keys(p.b0, t, k);
+        score(k, x[t]);
+      }
+      if (behind) wait_vmcnt<T::DMAS>();
+      barrier();
+#pragma unroll 1
+      for (int b = p.b0; b < p.b1; ++b) {
+        // weigh
+        u32x4 v0[DT / 2][2 * KT], v1[DT / 2][2 * KT], w[2 * KT];
+        uint32_t bad0 = 0, bad1 = 0;
+        if (loads.ever_bad) {
+          bad0 = sh.bad_rows[b % 8][0], bad1 = sh.bad_rows[b % 8][1];
+          if (threadIdx.x < 2) sh.bad_rows[(b + T::STAGES) % 8][threadIdx.x] = 0u;
+        }
+        const int kb = p.first + b * T::KEYS;
+        const bool masked = b < clear_from || b >= clear_to || loads.ever_bad;
+        uint32_t stage = from.stage(b);
+        const int odd = uniform(state.weigh(x, w, scale, masked, b, kb, row, bad0, bad1, from, lane) ? 1 : 0);
+#pragma unroll
+        for (int s = 0; s < 2 * KT; ++s) asm volatile("" : "+v"(w[s]), "+v"(state.l));  // made here: the scores' registers are free
+        if (odd != 0) {
+          // o of this tile here and now; the slot that is to come adds zeros
+#pragma unroll
+          for (int t = 0; t < DT; ++t) {
+            u32x4 v[1][2 * KT];
+            from.values(stage, t, v);
+            RowState<DP>::only_finite(v);
+            state.multiply(v, w, t);
+          }
+#pragma unroll
+          for (int s = 0; s < 2 * KT; ++s) w[s] = u32x4{0u, 0u, 0u, 0u};
+          stage = T::STAGES * T::STAGE - T::OPERAND;  // where zeros are, as a tile's values
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        from.values(stage, 0, v0);
+        if (!behind) wait_vmcnt<T::DMAS>();
+        barrier();
+        // multiply: o, then the next tile's scores (past the last tile they are not used).  Each part's operands are read
+        // while the part before runs: no more than two at a time have registers.
+        if (b + 3 >= loads.plain_until) loads.prepare(b + 3);
+        int id[T::PASSES];
+        u32x4 k0[KS], k1[KS];
+        constexpr int HALF = DT * KT;  // matrix instructions of half of o
+        loads.pages(id);
+        from.values(stage, DT / 2, v1);
+        state.multiply(v0, w, 0);
+        interleave<HALF, 2, 0>();
+        from.keys(b + 1, 0, k0);
+        loads.issue(b + 3, id);
+        state.multiply(v1, w, DT / 2);
+        interleave<HALF, KS / HALF, 6>();
+        from.keys(b + 1, 1, k1);
+        score(k0, x[0]);
+        interleave<KS, 1, 0>();
+        score(k1, x[1]);
+        if (behind) wait_vmcnt<T::DMAS>();
+        barrier();
+      }
+      if (!behind) barrier();
+    }
+    state.finish(c, sh.walk, p, walk.share, row, me, wave * 32 + (lane & 31), half);
+    __syncthreads();
+  }
+}
+
+// Heads beyond 128 values, whose o and q fill half of a SIMD's registers: one wave each, tiles of 32 keys that are loaded
+// three ahead, values read from LDS while the weights are made.
+template <int DP, bool FULL>
+__global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void attn_wide_kernel(AttnCall c) {
+  using T = ManyTile<DP>;
+  constexpr int KS = T::KS, DT = T::DT, KT = T::KT;
+  extern __shared__ __align__(256) unsigned char ring[];
+  __shared__ ManyShared<DP> sh;
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
+  const uint32_t lds = lds_address(ring);
+  const KeyRows rows(c);
+  const float scale = own_register(c.scale);
+  const Fragments<DP> from(lds, lane);
+  const int me = (int)xcd_remap(blockIdx.x, gridDim.x);
+
+  if (!FULL)
+    for (int i = threadIdx.x; i < T::STAGES * T::STAGE / 16; i += T::THREADS) reinterpret_cast<u32x4 *>(ring)[i] = u32x4{0u, 0u, 0u, 0u};
+
+  Walk<T::THREADS, false> walk(c, sh.walk, me, (int)gridDim.x);
+#pragma unroll 1
+  for (; walk.next(); walk.done()) {
+    const Piece &p = walk.p;
+    const Row row = row_of(c, p, wave * 32 + (lane & 31));
+    int all_lo, all_hi;
+    seen_by_all(c, p, c.by_heads(wave * 32), c.by_heads(wave * 32 + 31) + 1, all_lo, all_hi);
+    // tiles whose keys all rows see
+    const int clear_from = uniform((max(all_lo - p.first, 0) + T::KEYS - 1) / T::KEYS), clear_to = uniform(max(all_hi - p.first, 0) / T::KEYS);
+    TileLoads<DP, FULL> loads{rows, p, sh, c.table + (size_t)p.request * c.table_pitch, c.k + (size_t)p.kv * c.cache_head,
+                              c.v + (size_t)p.kv * c.cache_head, c.D, wave, lane, lds, sh.ids[wave]};
+    loads.ever_bad = false;
+    loads.step_pages = rows.page_of(T::KEYS), loads.step_rows = T::KEYS - loads.step_pages * rows.page;
+    if (threadIdx.x < 16) (&sh.bad_rows[0][0])[threadIdx.x] = 0u;
+    if (p.b0 < p.b1) loads.fill(p.b0), loads.find(p.b0);
+    u32x4 q[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      q[s] = u32x4{0u, 0u, 0u, 0u};
+      if (row.valid && (FULL || 16 * s + 8 * half < c.D))
+        q[s] = *reinterpret_cast<const u32x4 *>(c.q + (size_t)row.token * c.q_row + (size_t)row.head * c.q_head + 16 * s + 8 * half);
+    }
+    RowState<DP> state;
+    state.clear();
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): from here on only direct loads to LDS are counted
+    __syncthreads();
+    if (p.b0 < p.b1)
+      for (int i = 0; i < T::STAGES - 1; ++i) loads.all(p.b0 + i);
+#pragma unroll 1
+    for (int b = p.b0; b < p.b1; ++b) {
+      wait_vmcnt<(T::STAGES - 2) * T::DMAS>();
+      __syncthreads();  // tile b has landed, and nobody reads the one before any more
+      f32x16 x[KT];
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+        u32x4 k[KS];
+        from.keys(b, t, k);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[t][i] = 0.f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) x[t] = mfma32(k[s], q[s], x[t]);
+      }
+      u32x4 v[DT][2 * KT], w[2 * KT];
+      from.values(from.stage(b), 0, v);
+      const uint32_t bad0 = sh.bad_rows[b % 8][0], bad1 = sh.bad_rows[b % 8][KT - 1];
+      if (threadIdx.x < 2) sh.bad_rows[(b + T::STAGES) % 8][threadIdx.x] = 0u;
+      loads.all(b + T::STAGES - 1);
+      const int kb = p.first + b * T::KEYS;
+      const bool masked = b < clear_from || b >= clear_to || loads.ever_bad;
+      if (state.weigh(x, w, scale, masked, b, kb, row, bad0, bad1, from, lane)) RowState<DP>::only_finite(v);
+      state.multiply(v, w, 0);
+    }
+    state.finish(c, sh.walk, p, walk.share, row, me, wave * 32 + (lane & 31), half);
     __syncthreads();
   }
 }
 
 // ------------------------------------------------------------------ launches
 
-// Workgroups of a launch: what the chip holds at once.
-int workgroups_of(bool many, int DP, int cus) {
-  return cus * (many ? (DP > 128 ? ManyTile<256>::PER_CU : ManyTile<128>::PER_CU) : (DP > 128 ? FewTile<256>::PER_CU : FewTile<128>::PER_CU));
-}
 int padded_head(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
 template <int DP, bool MANY, bool FULL>
 int launch(const AttnCall &c, int grid, hipStream_t s) {
   void (*fn)(AttnCall);
-  if constexpr (MANY) fn = attn_many_kernel<DP, FULL>;
-  else fn = attn_few_kernel<DP>;
-  constexpr int lds = MANY ? ManyTile<DP>::STAGES * ManyTile<DP>::STAGE : FewTile<DP>::WAVES * FewTile<DP>::WAVE_BYTES;
+  if constexpr (!MANY) fn = attn_few_kernel<DP>;
+  else if constexpr (ManyTile<DP>::PAIRS) fn = attn_pairs_kernel<DP, FULL>;
+  else fn = attn_wide_kernel<DP, FULL>;
+  constexpr int lds = MANY ? ManyTile<DP>::LDS : FewTile<DP>::WAVES * FewTile<DP>::WAVE_BYTES;
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return OCC_ENODEV;
   static Once limit_set[kMaxDevices];
@@ -1039,15 +1311,17 @@ int launch(const AttnCall &c, int DP, int grid, hipStream_t s) {
   return DP == 64 ? launch<64, MANY>(c, grid, s) : DP == 128 ? launch<128, MANY>(c, grid, s) : launch<256, MANY>(c, grid, s);
 }
 
-constexpr int kJoined = 2 * kCus;  // shares, at most
+constexpr int kJoined = kCus;  // counters, a workgroup
+int many_rows(int DP) { return DP > 128 ? ManyTile<256>::ROWS : ManyTile<128>::ROWS; }
+int many_keys(int DP) { return DP > 128 ? ManyTile<256>::KEYS : ManyTile<128>::KEYS; }
+int few_keys(int DP) { return DP > 128 ? FewTile<256>::KEYS : FewTile<128>::KEYS; }
 
 }  // namespace
 
 size_t attn_workspace(int D) {
   const int DP = padded_head(D);
-  const size_t few = (size_t)workgroups_of(false, DP, kCus) * 2 * FewTile<128>::ROWS * (DP + 2) * 4;
-  const size_t many = (size_t)workgroups_of(true, DP, kCus) * 2 * ManyTile<128>::ROWS * (DP + 2) * 4;
-  return (size_t)kJoined * 4 + std::max(few, many);
+  // two partial results a workgroup, one workgroup a CU; those of many rows are the larger
+  return (size_t)kJoined * 4 + (size_t)kCus * 2 * many_rows(DP) * (DP + 2) * 4;
 }
 
 int attn_launch(const occ_attn_args &a, hipStream_t s) {
@@ -1065,25 +1339,24 @@ int attn_launch(const occ_attn_args &a, hipStream_t s) {
   c.by_page = Divider(a.page);
   c.table_pitch = a.ld_table;
   c.q_row = a.q_row, c.q_head = a.q_head, c.out_row = a.out_row, c.out_head = a.out_head;
-  c.cache_page = a.cache_page, c.cache_row = a.cache_row, c.cache_head = a.cache_head;
+  c.page_bytes = (uint32_t)a.cache_page * 2u, c.row_bytes = (uint32_t)a.cache_row * 2u, c.cache_head = a.cache_head;
   c.scale = a.scale * kLog2e;
   c.joined = static_cast<uint32_t *>(a.workspace);
   c.part = reinterpret_cast<float *>(static_cast<unsigned char *>(a.workspace) + (size_t)kJoined * 4);
   const int DP = padded_head(a.D), cus = std::min(di->num_cus, kCus);
   auto go = [&](bool many, int least, int most) {
     AttnCall k = c;
-    const int rows = many ? ManyTile<128>::ROWS : FewTile<128>::ROWS;
+    const int rows = many ? many_rows(DP) : FewTile<128>::ROWS;
     k.heads = std::min(c.group, rows);
     k.cut.tokens = rows / k.heads, k.cut.by_tokens = Divider(k.cut.tokens);
     k.groups = (c.group + k.heads - 1) / k.heads;
     k.by_heads = Divider(k.heads), k.by_groups = Divider(k.groups);
     k.cut.parts = a.Hkv * k.groups;
-    k.cut.fixed = many ? 128 : 256, k.cut.block = many ? (DP > 64 ? ManyTile<128>::KEYS : ManyTile<64>::KEYS) : DP > 128 ? FewTile<256>::KEYS : FewTile<128>::KEYS;
+    k.cut.fixed = many ? 128 : 256, k.cut.block = many ? many_keys(DP) : few_keys(DP);
     k.cut.window = a.window < c.keys ? a.window : 0, k.cut.causal = a.causal != 0;
     k.least = least, k.most = most;
     k.min_share = 256, k.least_even = many ? 512 : 256, k.spare = 512;
-    const int grid = workgroups_of(many, DP, cus);
-    return many ? launch<true>(k, DP, grid, s) : launch<false>(k, DP, grid, s);
+    return many ? launch<true>(k, DP, cus, s) : launch<false>(k, DP, cus, s);
   };
   const int most_rows = (int)std::min<int64_t>((int64_t)std::min(a.max_fresh, a.rows) * c.group, INT32_MAX);
   if (most_rows <= kFewRows) return go(false, 0, INT32_MAX);

@@ -108,6 +108,8 @@ def test_rope_accepts(L):
     (EINVAL, dict(v_cache=None)), (EINVAL, dict(table=None)), (EINVAL, dict(starts=None)), (EINVAL, dict(lens=place(6) + 2)),
     (EINVAL, dict(lse=place(8) + 2)), (EINVAL, dict(workspace=None)), (EINVAL, dict(workspace_bytes=4096)), (EINVAL, dict(q_row=516)),
     (EINVAL, dict(q_head=68)), (EINVAL, dict(out_row=64)), (EINVAL, dict(cache_row=64)), (EINVAL, dict(cache_page=1024)),
+    (EINVAL, dict(cache_page=1 << 31)), (EINVAL, dict(cache_row=1 << 31, cache_page=1 << 36)), (EINVAL, dict(width=1 << 30, ld_table=1 << 30,
+                                                                                                     page=65536, pages=5, cache_page=1 << 23, rows=1 << 10)),
     (EINVAL, dict(ld_table=4)), (EALIAS, dict(out=place(1))), (EALIAS, dict(lse=place(7))), (EALIAS, dict(out=place(2) + 64)),
     (EALIAS, dict(workspace=place(3))), (EALIAS, dict(lse=place(5))), (EALIAS, dict(out=place(9) + 4096)),
 ])

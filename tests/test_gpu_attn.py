@@ -127,7 +127,7 @@ def workspace_for(D, fresh=False):
 def teardown_module():
     torch.cuda.synchronize()
     for w in _workspaces.values():
-        assert int(w[:2048].view(torch.int32).abs().sum()) == 0, "counters are left"
+        assert int(w[:1024].view(torch.int32).abs().sum()) == 0, "counters are left"
     _workspaces.clear()
 
 
