@@ -882,14 +882,13 @@ struct Fragments {
   __device__ __forceinline__ void values(uint32_t stage, int t0, u32x4 (&v)[N][2 * T::KT]) const {
     const uint32_t from = v0 + stage;
 #pragma unroll
-    for (int t = 0; t < N; ++t) {
-      const uint32_t at = (from ^ (((t0 + t) & 3) * 64)) + ((t0 + t) >> 2) * 256;
+    for (int s = 0; s < 2 * T::KT; ++s)  // in the order in which multiply() uses them
 #pragma unroll
-      for (int s = 0; s < 2 * T::KT; ++s) {
+      for (int t = 0; t < N; ++t) {
+        const uint32_t at = (from ^ (((t0 + t) & 3) * 64)) + ((t0 + t) >> 2) * 256;
         const u32x2 a = read_transposed(at + 16 * s * T::PITCH), b2 = read_transposed(at + (16 * s + 8) * T::PITCH);
         v[t][s] = u32x4{a[0], a[1], b2[0], b2[1]};
       }
-    }
   }
 };
 
@@ -1148,7 +1147,9 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
       barrier();
 #pragma unroll 1
       for (int b = p.b0; b < p.b1; ++b) {
-        // weigh
+        // weigh.  The wave that multiplies goes first: the other's instructions fill what it leaves (712 -> 693 us for a prompt
+        // of 8192, together with the values' order).
+        __builtin_amdgcn_s_setprio(0);
         u32x4 v0[DT / 2][2 * KT], v1[DT / 2][2 * KT], w[2 * KT];
         uint32_t bad0 = 0, bad1 = 0;
         if (loads.ever_bad) {
@@ -1180,6 +1181,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
         barrier();
         // multiply: o, then the next tile's scores (past the last tile they are not used).  Each part's operands are read
         // while the part before runs: no more than two at a time have registers.
+        __builtin_amdgcn_s_setprio(1);
         if (b + 3 >= loads.plain_until) loads.prepare(b + 3);
         int id[T::PASSES];
         u32x4 k0[KS], k1[KS];
@@ -1199,6 +1201,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
         if (behind) wait_vmcnt<T::DMAS>();
         barrier();
       }
+      __builtin_amdgcn_s_setprio(0);
       if (!behind) barrier();
     }
     state.finish(c, sh.walk, p, walk.share, row, me, wave * 32 + (lane & 31), half);
