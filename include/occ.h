@@ -673,8 +673,8 @@ size_t occ_moe_workspace_bytes(int tokens, int H, int I, int experts, int top_k)
  *               rows behind the last token
  *   positions : rows; cached + 0, 1, ..; 0 for rows without a served request
  *   free_after: as free, for the next call; pages that come back are behind the others, and are not given out by this call
- * Only `table` and `ring` are read and written; the others must not overlap.  A program keeps lens as the next step's
- * cached and free_after as its free.  Everything is exact; int32 buffers, 4-byte aligned.  No workspace.
+ * Only `table` and `ring` are read and written; the others must not overlap.  A program keeps lens, where it is not -1, as the
+ * next step's cached and free_after as its free.  Everything is exact; int32 buffers, 4-byte aligned.  No workspace.
  */
 typedef struct occ_kv_tables_args {
   int requests, rows, width, page, pages, ring_size;

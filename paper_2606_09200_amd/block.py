@@ -1,7 +1,8 @@
 """The block operators as a model uses them.
 
-``Decoder`` serves: layers of norms and a mixture of experts with 4-bit weights, one
-step of a few tokens, which a HIP graph can hold.  ``Trainee`` trains: a block's norms
+``Decoder`` serves: layers of norms and a mixture of experts with 4-bit weights, with a
+``Cache`` each of them after attention, one step of new tokens, which a HIP graph can hold.
+``Trainee`` trains: a block's norms
 with their gate and a linear layer whose products, forward and backward, are 4-bit.
 
     python paper_2606_09200_amd/block.py            # both, with their times
@@ -29,11 +30,41 @@ def quantize_experts(w):
     return q
 
 
+class Cache:
+    """Keys and values of ``layers`` layers in pages, and the tables of a step: up to ``requests`` requests that bring up to
+    ``tokens`` new tokens, each of ``width`` pages at most.  Write ``fresh`` before a step: a request's new tokens (0: none,
+    -1: it is over); their rows follow each other in the requests' order.  ``most``: the new tokens that one request brings at
+    most, all of them if not given."""
+
+    def __init__(self, layers, requests, tokens, width, pages, page, kv_heads, head, most=None, device="cuda"):
+        def zeros(*shape):
+            return torch.zeros(*shape, dtype=torch.int32, device=device)
+
+        self.page, self.pages, self.most = page, pages, tokens if most is None else most
+        self.k, self.v = (torch.zeros(layers, pages, page, kv_heads, head, dtype=BF16, device=device) for _ in range(2))
+        self.cached, self.fresh, self.lens, self.starts = (zeros(n) for n in (requests, requests, requests, requests + 1))
+        self.table, self.ring = zeros(requests, width), torch.arange(pages, dtype=torch.int32, device=device)
+        self.free, self.free_after = torch.tensor([0, pages], dtype=torch.int32, device=device), zeros(2)
+        self.slots, self.positions = zeros(tokens), zeros(tokens)
+
+    def tables(self):
+        """Pages for what ``fresh`` brings; the same again if nothing has moved on."""
+        occ.occ_kv_tables(self.cached, self.fresh, self.table, self.ring, self.free, page=self.page, pages=self.pages,
+                          lens=self.lens, starts=self.starts, slots=self.slots, positions=self.positions,
+                          free_after=self.free_after)
+
+    def advance(self):
+        """The step is taken: what it brought is cached.  Requests that had no room (``lens`` -1) are where they were."""
+        self.cached.copy_(torch.where(self.lens < 0, self.cached, self.lens))
+        self.free.copy_(self.free_after)
+
+
 class Decoder:
     """``layers`` times: the residual takes the last block's output, normed, and what it
-    then is goes, normed, through the experts.  Weights are random."""
+    then is goes, normed, through the experts.  Weights are random.  With ``heads`` query heads over a ``cache``, each layer
+    has a block of attention before that of its experts."""
 
-    def __init__(self, layers, tokens, hidden, inner, experts, top_k, device="cuda", seed=0):
+    def __init__(self, layers, tokens, hidden, inner, experts, top_k, device="cuda", seed=0, heads=0, cache=None, window=0):
         g = torch.Generator(device=device).manual_seed(seed)
 
         def rand(*shape, scale):
@@ -49,6 +80,18 @@ class Decoder:
                 gate=quantize_experts(rand(experts, inner, hidden, **up)),
                 up=quantize_experts(rand(experts, inner, hidden, **up)),
                 down=quantize_experts(rand(experts, hidden, inner, scale=inner ** -0.5))))
+        self.cache, self.window = cache, window
+        if cache is not None:
+            kv_heads, head = cache.k.shape[3:]
+            self.split = (heads, kv_heads, kv_heads)
+            for w in self.layers:
+                w.update(w_attn_post=1 + rand(hidden, scale=0.1), w_attn_pre=1 + rand(hidden, scale=0.1),
+                         qkv=rand((heads + 2 * kv_heads) * head, hidden, scale=hidden ** -0.5),
+                         proj=rand(hidden, heads * head, scale=(heads * head) ** -0.5))
+            self.turns = occ.rope_turns(head // 2, device=device)
+            self.qkv, self.attended = (torch.zeros(tokens, n, head, dtype=BF16, device=device) for n in (heads + 2 * kv_heads, heads))
+            self.attn_workspace = torch.zeros(occ.occ_attn_paged_workspace_bytes(heads, kv_heads, head), dtype=torch.uint8,
+                                              device=device)
         # what a step reads, writes and passes on; the experts' workspace is zeroed once
         self.embedded = torch.zeros(tokens, hidden, dtype=BF16, device=device)
         self.live = torch.ones(tokens, dtype=torch.bool, device=device)  # slots that hold a request
@@ -58,18 +101,42 @@ class Decoder:
         self.workspace = torch.zeros(occ.occ_moe_workspace_bytes(tokens, hidden, inner, experts, top_k),
                                      dtype=torch.uint8, device=device)
 
+    def attend(self, w, i):
+        """Layer i's attention of ``h`` into ``f``; its keys and values go into the cache."""
+        occ.occ_gemm_bt(self.h, w["qkv"], self.qkv.flatten(1))
+        q, k, v = self.qkv.split(self.split, 1)
+        keys, values = self.cache.k[i], self.cache.v[i]
+        occ.occ_rope(q, k, self.cache.positions, self.turns, v=v, k_cache=keys, v_cache=values, slots=self.cache.slots)
+        occ.occ_attn_paged(q, keys, values, self.cache.table, self.cache.starts, self.cache.lens, self.attended,
+                           max_fresh=self.cache.most, window=self.window, workspace=self.attn_workspace)
+        occ.occ_gemm_bt(self.attended.flatten(1), w["proj"], self.f)
+
     def step(self):
-        """``out`` from ``embedded`` and ``live``, on the current stream."""
+        """``out`` from ``embedded`` and ``live``, on the current stream.  With a cache, ``live`` is what its ``fresh``
+        brings; the step can be taken again until the cache advances."""
+        if self.cache is not None:
+            self.cache.tables()
+            torch.ge(self.cache.slots, 0, out=self.live)
+        post = None  # the norm of what the last block put out
         for i, w in enumerate(self.layers):
-            if i == 0:  # nothing to add yet: the embedding is the residual, and only the norm before the block runs
-                self.f.zero_()
-                occ.occ_norm_gate(self.f, self.embedded, self.x, self.h, w_pre=w["w_pre"], post=False)
-            else:
-                occ.occ_norm_gate(self.f, self.x, self.x, self.h, w_post=self.layers[i - 1]["w_post"], w_pre=w["w_pre"])
+            if self.cache is not None:
+                self.norm(post, w["w_attn_pre"])
+                self.attend(w, i)
+                post = w["w_attn_post"]
+            self.norm(post, w["w_pre"])
             occ.occ_moe(self.h, w["router"], w["gate"], w["up"], w["down"], self.f, top_k=self.top_k,
                         workspace=self.workspace, ids=self.ids[i], mask=self.live)
-        occ.occ_norm_gate(self.f, self.x, self.out, w_post=self.layers[-1]["w_post"])
+            post = w["w_post"]
+        occ.occ_norm_gate(self.f, self.x, self.out, w_post=post)
         return self.out
+
+    def norm(self, post, pre):
+        """The residual takes ``f``; ``h`` is its norm."""
+        if post is None:  # nothing to add yet: the embedding is the residual, and only the norm before the block runs
+            self.f.zero_()
+            occ.occ_norm_gate(self.f, self.embedded, self.x, self.h, w_pre=pre, post=False)
+        else:
+            occ.occ_norm_gate(self.f, self.x, self.x, self.h, w_post=post, w_pre=pre)
 
     def graph(self):
         """The step as a graph: ``replay()`` it after writing ``embedded`` and ``live``."""
@@ -151,18 +218,33 @@ def timed(fn, n):
 def main(argv=None):
     p = argparse.ArgumentParser(description="a decode step and a training step of the block operators")
     for name, value in (("layers", 4), ("tokens", 8), ("hidden", 4096), ("inner", 2048), ("experts", 32), ("top-k", 4),
-                        ("rows", 4096), ("out", 4096), ("steps", 20)):
+                        ("rows", 4096), ("out", 4096), ("steps", 20), ("heads", 0), ("kv-heads", 8), ("head", 128),
+                        ("page", 16), ("context", 1000), ("window", 0)):
         p.add_argument("--" + name, type=int, default=value)
     a = p.parse_args(argv)
     g = torch.Generator(device="cuda").manual_seed(1)
-    d = Decoder(a.layers, a.tokens, a.hidden, a.inner, a.experts, a.top_k)
-    d.embedded.copy_(torch.randn(a.tokens, a.hidden, generator=g, device="cuda"))
-    eager = d.step().clone()
-    graph = d.graph()
-    graph.replay()
-    assert torch.equal(d.out, eager), "the graph's step differs"
-    print("decode: %d layers, %d tokens: %.0f us a step, %.0f from a graph"
-          % (a.layers, a.tokens, timed(d.step, 50), timed(graph.replay, 50)), flush=True)
+
+    def decode(what, d):
+        d.embedded.copy_(torch.randn(a.tokens, a.hidden, generator=g, device="cuda"))
+        eager = d.step().clone()
+        graph = d.graph()
+        graph.replay()
+        assert torch.equal(d.out, eager), "the graph's step differs"
+        print("%s: %d layers, %d tokens: %.0f us a step, %.0f from a graph"
+              % (what, a.layers, a.tokens, timed(d.step, 50), timed(graph.replay, 50)), flush=True)
+
+    decode("decode", Decoder(a.layers, a.tokens, a.hidden, a.inner, a.experts, a.top_k))
+    if a.heads:  # each token a request of its own, after `context` others
+        width = a.context // a.page + 1
+        cache = Cache(a.layers, a.tokens, a.tokens, width, a.tokens * width, a.page, a.kv_heads, a.head, most=1)
+        for t in (cache.k, cache.v):
+            t.normal_(generator=g)
+        cache.fresh.fill_(a.context)
+        cache.tables()
+        cache.advance()
+        cache.fresh.fill_(1)
+        decode("decode with attention over %d keys" % (a.context + 1),
+               Decoder(a.layers, a.tokens, a.hidden, a.inner, a.experts, a.top_k, heads=a.heads, cache=cache, window=a.window))
     t = Trainee(a.rows, a.hidden, a.out)
     f, x = (torch.randn(a.rows, a.hidden, generator=g, device="cuda").to(BF16) for _ in range(2))
     teacher = torch.randn(a.out, a.hidden, generator=g, device="cuda") * a.hidden ** -0.5
