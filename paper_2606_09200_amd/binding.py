@@ -921,12 +921,13 @@ def _cache_arg(k_cache, v_cache, dtype, heads, D):
     """(addresses, pages, page, pitches) of two caches (pages, page, heads, D) of the same strides."""
     if k_cache.dtype != dtype or v_cache.dtype != dtype or not k_cache.is_cuda or not v_cache.is_cuda:
         raise ValueError("k_cache and v_cache must be %s GPU tensors" % dtype)
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.shape[2:] != (heads, D):
+    shape, strides = k_cache.shape, k_cache.stride()
+    if len(shape) != 4 or shape[2] != heads or shape[3] != D or v_cache.shape != shape:
         raise ValueError("k_cache and v_cache must have one shape (pages, page, %d, %d)" % (heads, D))
-    if k_cache.stride() != v_cache.stride() or (D > 1 and k_cache.stride(3) != 1):
+    if v_cache.stride() != strides or (D > 1 and strides[3] != 1):
         raise ValueError("k_cache and v_cache must have the same strides, and contiguous heads")
-    pages, page = k_cache.shape[:2]
-    by_page, by_row, by_head, _ = k_cache.stride()
+    pages, page, _, _ = shape
+    by_page, by_row, by_head, _ = strides
     by_head = by_head if heads > 1 else D
     by_row = by_row if page > 1 else heads * by_head
     return k_cache.data_ptr(), v_cache.data_ptr(), pages, page, by_page if pages > 1 else page * by_row, by_row, by_head

@@ -24,7 +24,7 @@ struct TablesCall {
   int32_t *table, *ring;
   size_t ld;
   int32_t *lens, *starts, *slots, *positions, *free_after;
-  int requests, tokens;      // of a workgroup
+  int requests, each;        // of a workgroup, tokens of a thread
 };
 
 // A request by itself: its tokens, its pages before and after, whether it is over.
@@ -60,6 +60,28 @@ __device__ __forceinline__ void pass(const TablesCall &c, Before &b, const Asked
   b.back += a.back;
 }
 
+// The value of a lane before, 0 where there is none; of rows of 16 lanes, then of their last ones.
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ int64_t lane_before(int64_t v) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CONTROL, ROWS, 0xF, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)((uint64_t)v >> 32), CONTROL, ROWS, 0xF, false);
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+// The sum of the lanes up to one's own.
+__device__ __forceinline__ int64_t sum_upto(int64_t v) {
+  v += lane_before<0x111, 0xF>(v);
+  v += lane_before<0x112, 0xF>(v);
+  v += lane_before<0x114, 0xF>(v);
+  v += lane_before<0x118, 0xF>(v);
+  v += lane_before<0x142, 0xA>(v);
+  return v + lane_before<0x143, 0xC>(v);
+}
+
+// STAGED: up to kStaged requests lie in LDS, with what those before them have asked for, so that the passes over them and
+// the search for a token's request wait for nothing but LDS.
+constexpr int kStaged = 2048;
+
+template <bool STAGED>
 __global__ __launch_bounds__(kThreads) void kv_tables_kernel(TablesCall c) {
   __shared__ int64_t sums[3][kWaves];
   __shared__ Before before[kThreads + 1];   // of each thread's requests
@@ -68,55 +90,128 @@ __global__ __launch_bounds__(kThreads) void kv_tables_kernel(TablesCall c) {
     int have, need, back;
   };
   __shared__ Share shares[64];
+  __shared__ int lds_cached[STAGED ? kStaged : 1], lds_fresh[STAGED ? kStaged : 1];
+  __shared__ int lds_start[STAGED ? kStaged + 1 : 1], lds_need[STAGED ? kStaged : 1];  // sums before; what passes 31 bits cut
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int per = (c.n + kThreads - 1) / kThreads;
   const int r0 = min((int)threadIdx.x * per, c.n), r1 = min(r0 + per, c.n);
   const int size = c.size;
-  const int count = min(max(c.free[1], 0), size);
-  const int head = c.free[0] < 0 || c.free[0] >= size ? 0 : c.free[0];
+  const int given[2] = {c.free[0], c.free[1]};
+  if constexpr (STAGED) {
+    for (int i = threadIdx.x; i < c.n; i += kThreads) lds_cached[i] = c.cached[i], lds_fresh[i] = c.fresh[i];
+    __syncthreads();
+  }
+  const int count = min(max(given[1], 0), size);
+  const int head = given[0] < 0 || given[0] >= size ? 0 : given[0];
+  auto cached_of = [&](int i) { return STAGED ? lds_cached[i] : c.cached[i]; };
+  auto fresh_of = [&](int i) { return STAGED ? lds_fresh[i] : c.fresh[i]; };
+  auto short31 = [](int64_t v) { return (int)min(v, (int64_t)0x7FFFFFFF); };
 
   // Sums before each thread's requests: tokens first, for which requests need pages depends on them.
-  auto scan = [&](int64_t own, int which) {
-    int64_t upto = own;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int64_t v = __shfl_up(upto, d);
-      if (lane >= d) upto += v;
-    }
+  auto within_wave = [&](int64_t own, int which) {
+    const int64_t upto = sum_upto(own);
     if (lane == 63) sums[which][wave] = upto;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) upto += sums[which][w];
     return upto - own;
   };
+  auto waves_before = [&](int which) {
+    int64_t sum = 0;
+    for (int w = 0; w < wave; ++w) sum += sums[which][w];
+    return sum;
+  };
   Before own{0, 0, 0};
-  for (int i = r0; i < r1; ++i) own.tokens += max(c.fresh[i], 0);
-  Before b{scan(own.tokens, 0), 0, 0};
+  for (int i = r0; i < r1; ++i) own.tokens += max(fresh_of(i), 0);
+  Before b{within_wave(own.tokens, 0), 0, 0};
+  __syncthreads();
+  b.tokens += waves_before(0);
   Before mine = b;
-  for (int i = r0; i < r1; ++i) pass(c, mine, asked(c, c.cached[i], c.fresh[i]));
+  for (int i = r0; i < r1; ++i) pass(c, mine, asked(c, cached_of(i), fresh_of(i)));
   own = mine;
-  b.need = scan(own.need, 1);
-  b.back = scan(own.back, 2);
+  b.need = within_wave(own.need, 1);
+  b.back = within_wave(own.back, 2);
+  __syncthreads();
+  b.need += waves_before(1);
+  b.back += waves_before(2);
   before[threadIdx.x] = b;
   if (threadIdx.x == kThreads - 1) before[kThreads] = Before{own.tokens, b.need + own.need, b.back + own.back};
-  __syncthreads();
 
   // the workgroup's requests: lengths, and what their pages need
   const int first = min((int)blockIdx.x * c.requests, c.n), last = min(first + c.requests, c.n);
+  __shared__ int64_t taken;   // pages: the sum up to the last request that gets its own
+  if (threadIdx.x == 0) taken = 0;
+  __syncthreads();
   {
     Before at = b;
+    int64_t most = 0;
     for (int i = r0; i < r1; ++i) {
-      const Asked a = asked(c, c.cached[i], c.fresh[i]);
+      const Asked a = asked(c, cached_of(i), fresh_of(i));
+      const bool room = at.need + a.need <= count, ok = within(c, a, at) && (a.need == 0 || room);
+      if (ok && a.need > 0) most = at.need + a.need;
       if (i >= first && i < last) {
-        const bool ok = within(c, a, at) && (a.need == 0 || at.need + a.need <= count);
-        c.lens[i] = c.fresh[i] < 0 ? 0 : ok ? (int)(c.cached[i] + a.tokens) : -1;
+        c.lens[i] = fresh_of(i) < 0 ? 0 : ok ? (int)(cached_of(i) + a.tokens) : -1;
         c.starts[i] = (int)min(at.tokens, (int64_t)c.T);
         if (i == c.n - 1) c.starts[c.n] = (int)min(at.tokens + a.tokens, (int64_t)c.T);
         shares[i - first] = Share{a.back ? at.back : at.need, a.have, ok ? a.need : 0, a.back};
       }
+      if constexpr (STAGED) lds_start[i] = short31(at.tokens), lds_need[i] = short31(at.need);
       pass(c, at, a);
     }
+    if (blockIdx.x == 0 && most > 0) atomicMax(reinterpret_cast<long long *>(&taken), (long long)most);
   }
   __syncthreads();
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    const int64_t next = head + taken, back = before[kThreads].back;
+    c.free_after[0] = (int)(next < size ? next : next - size);
+    c.free_after[1] = (int)min(count - taken + back, size - taken);
+  }
+
+  // the workgroup's tokens, c.each that follow each other a thread
+  const int64_t all = before[kThreads].tokens;
+  const int64_t base = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * c.each, end = min(base + c.each, (int64_t)c.T);
+  if (base < end) {
+    // the last request that begins at or before the first: of several that begin there, the others have no tokens
+    int i = 0;
+    Before at{0, 0, 0};
+    if (base < all) {
+      int lo = 0, hi = STAGED ? c.n - 1 : kThreads - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if ((STAGED ? (int64_t)lds_start[mid] : before[mid].tokens) <= base) lo = mid;
+        else hi = mid - 1;
+      }
+      i = lo;
+      // threads behind the requests' end begin at the sum of all, which is past any token
+      if constexpr (!STAGED) at = before[lo], i = lo * per;
+    }
+#pragma unroll 1
+    for (int64_t t = base; t < end; ++t) {
+      int slot = -1, position = 0;
+      if (t < all) {
+        Asked a;
+        if constexpr (STAGED) {
+          while (i + 1 < c.n && lds_start[i + 1] <= t) ++i;
+          a = asked(c, lds_cached[i], lds_fresh[i]);
+          at = Before{lds_start[i], lds_need[i], 0};
+        } else {
+          a = asked(c, c.cached[i], c.fresh[i]);
+          while (at.tokens + a.tokens <= t) {
+            pass(c, at, a);
+            ++i;
+            a = asked(c, c.cached[i], c.fresh[i]);
+          }
+        }
+        if (within(c, a, at) && (a.need == 0 || at.need + a.need <= count)) {
+          position = cached_of(i) + (int)(t - at.tokens);
+          const int index = c.by_page(position);
+          const int64_t from = head + at.need + (index - a.have);
+          const int id = *(index < a.have ? c.table + (size_t)i * c.ld + index : c.ring + (from < size ? from : from - size));
+          if ((uint32_t)id < (uint32_t)c.pages) slot = id * c.page + (position - index * c.page);
+        }
+      }
+      c.slots[t] = slot;
+      c.positions[t] = position;
+    }
+  }
+  // and its pages
   for (int i = first + wave; i < last; i += kWaves) {
     const Share s = shares[i - first];
     int32_t *row = c.table + (size_t)i * c.ld;
@@ -128,64 +223,6 @@ __global__ __launch_bounds__(kThreads) void kv_tables_kernel(TablesCall c) {
       const int64_t at = (int64_t)count + s.first + j;  // behind what was free, as far as the ring has room
       if (at < size) c.ring[head + at < size ? head + at : head + at - size] = row[j];
     }
-  }
-  if (blockIdx.x == 0) {
-    // pages taken: the sum up to the last request that got its own, which is the last whose sum the free pages cover
-    __shared__ int64_t taken;
-    if (threadIdx.x == 0) taken = 0;
-    __syncthreads();
-    Before at = b;
-    int64_t most = 0;
-    for (int i = r0; i < r1; ++i) {
-      const Asked a = asked(c, c.cached[i], c.fresh[i]);
-      if (within(c, a, at) && a.need > 0 && at.need + a.need <= count) most = at.need + a.need;
-      pass(c, at, a);
-    }
-    if (most > 0) atomicMax(reinterpret_cast<long long *>(&taken), (long long)most);
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      const int64_t next = head + taken, back = before[kThreads].back;
-      c.free_after[0] = (int)(next < size ? next : next - size);
-      c.free_after[1] = (int)min(count - taken + back, size - taken);
-    }
-  }
-
-  // the workgroup's tokens
-  const int64_t all = before[kThreads].tokens;
-  for (int64_t t = (int64_t)blockIdx.x * c.tokens + threadIdx.x; t < min((int64_t)(blockIdx.x + 1) * c.tokens, (int64_t)c.T); t += kThreads) {
-    int slot = -1, position = 0;
-    if (t < all) {
-      int lo = 0, hi = kThreads - 1;   // the last thread whose requests begin at or before t
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (before[mid].tokens <= t) lo = mid;
-        else hi = mid - 1;
-      }
-      // threads behind the requests' end begin at the sum of all, which is past t; of several that begin at t's
-      // request, the last has it
-      Before at = before[lo];
-      int i = lo * per;
-      Asked a = asked(c, c.cached[i], c.fresh[i]);
-      while (at.tokens + a.tokens <= t) {
-        pass(c, at, a);
-        ++i;
-        a = asked(c, c.cached[i], c.fresh[i]);
-      }
-      if (within(c, a, at) && (a.need == 0 || at.need + a.need <= count)) {
-        position = c.cached[i] + (int)(t - at.tokens);
-        const int index = c.by_page(position);
-        int id;
-        if (index < a.have) {
-          id = c.table[(size_t)i * c.ld + index];
-        } else {
-          const int64_t from = head + at.need + (index - a.have);
-          id = c.ring[from < size ? from : from - size];
-        }
-        if ((uint32_t)id < (uint32_t)c.pages) slot = id * c.page + (position - index * c.page);
-      }
-    }
-    c.slots[t] = slot;
-    c.positions[t] = position;
   }
 }
 
@@ -334,10 +371,11 @@ int kv_tables_launch(const occ_kv_tables_args &a, hipStream_t s) {
   c.by_page = Divider(a.page);
   c.cached = a.cached, c.fresh = a.fresh, c.free = a.free, c.table = a.table, c.ring = a.ring, c.ld = a.ld_table;
   c.lens = a.lens, c.starts = a.starts, c.slots = a.slots, c.positions = a.positions, c.free_after = a.free_after;
-  const int grid = std::max((a.rows + 1023) / 1024, (a.requests + 63) / 64);
+  // a token a thread while that takes no more than two workgroups a CU: each of them scans all requests
+  c.each = a.rows <= 2 * kThreads * di->num_cus ? 1 : 4;
+  const int grid = std::max((int)(((int64_t)a.rows + kThreads * c.each - 1) / (kThreads * c.each)), (a.requests + 63) / 64);
   c.requests = (a.requests + grid - 1) / grid;
-  c.tokens = (a.rows + grid - 1) / grid;
-  hipLaunchKernelGGL(kv_tables_kernel, dim3(grid), dim3(kThreads), 0, s, c);
+  hipLaunchKernelGGL(a.requests <= kStaged ? kv_tables_kernel<true> : kv_tables_kernel<false>, dim3(grid), dim3(kThreads), 0, s, c);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
 }
 

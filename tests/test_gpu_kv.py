@@ -61,7 +61,8 @@ def problem(n, page, seed, most=100, over=0.1, spare=5, chunk=20, holes=False):
 
 
 @pytest.mark.parametrize("n,page,spare,chunk", [(1, 1, 0, 2), (3, 16, 5, 20), (64, 16, 0, 2), (255, 3, -40, 9), (256, 48, 3, 40),
-                                                (257, 64, -30, 100), (700, 5, -200, 12), (1500, 16, 9, 30)])
+                                                (257, 64, -30, 100), (700, 5, -200, 12), (1500, 16, 9, 30), (2047, 2, -50, 7),
+                                                (2048, 8, 0, 3), (2049, 8, 0, 3), (5000, 3, -900, 11)])
 def test_tables(n, page, spare, chunk):
     for seed in range(3):
         p = problem(n, page, seed, spare=spare, chunk=chunk, holes=seed == 2)
