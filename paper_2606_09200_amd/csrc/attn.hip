@@ -373,6 +373,21 @@ __device__ __forceinline__ bool last_of(const AttnCall &c, WalkShared<THREADS> &
   return sh.last_one != 0u;
 }
 
+// Whether all others have theirs already, as it is where the item's end is a share's first piece and its beginning another's
+// last: then this one's need not be stored (8 us for 256 rows of 128, of 17 to 20 us that a join took with it).
+template <int THREADS>
+__device__ __forceinline__ bool others_done(const AttnCall &c, WalkShared<THREADS> &sh, const Joining &j) {
+  if (threadIdx.x == 0) {
+    const bool last = get_device(c.joined + j.counter) + 1 == (uint32_t)j.parts;
+    if (last) put_device(c.joined + j.counter, 0u);
+    sh.last_one = last;
+  }
+  __syncthreads();
+  const bool last = sh.last_one != 0u;
+  __syncthreads();
+  return last;
+}
+
 // Places of partial results: two a workgroup, for an item that began before its share and for one that begins in it.
 __device__ __forceinline__ uint32_t place_of(int share, bool began, int floats) { return (uint32_t)(2 * share + (began ? 1 : 0)) * (uint32_t)(floats * 4); }
 
@@ -994,47 +1009,69 @@ struct RowState {
       for (int t = 0; t < N; ++t) acc[t0 + t] = mfma32(v[t][s], w[s], acc[t0 + t]);
   }
 
-  // The item's part is whole: to the output, or beside the others' and, if it is the last of them, joined.
+  // The item's part is whole: to the output, or beside the others' and, if it is the last of them, joined, always in the
+  // parts' order.  A partial result lies as the lanes have it, 1 KB an instruction.
   __device__ __forceinline__ void finish(const AttnCall &c, WalkShared<T::THREADS> &sh, const Piece &p, const AttnShare &share, const Row &row,
                                          int me, int r, int half) {
     const auto rs = rsrc_of(c.part, gridDim.x * 2u * (uint32_t)(T::PART * 4));
     l = sum_halves(l);
     bool write = true;
     if (!p.alone) {
-      const uint32_t slot = place_of(me, p.began, T::PART);
-#pragma unroll
-      for (int t = 0; t < T::DT; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x4 v = {acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]};
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rs,
-                                                 (int)(slot + (uint32_t)(r * DP + 32 * t + 8 * i + 4 * half) * 4u), 0, kDevice);
-        }
-      if (half == 0)
-        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f32x2{m, l}), rs,
-                                              (int)(slot + (uint32_t)(T::ROWS * DP + 2 * r) * 4u), 0, kDevice);
+      const uint32_t at = (uint32_t)((r >> 5) * 32 * DP * 4 + (half * 32 + (r & 31)) * 16), at_sums = (uint32_t)(T::ROWS * DP + 2 * r) * 4u;
       const Joining join = joining(c, p, share);
-      const int parts = join.parts;
-      write = last_of(c, sh, join);
+      write = others_done(c, sh, join);
+      if (!write) {
+        const uint32_t slot = place_of(me, p.began, T::PART);
+#pragma unroll
+        for (int t = 0; t < T::DT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const f32x4 v = {acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]};
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rs, (int)(slot + at + (uint32_t)(4 * t + i) * 1024u), 0, kDevice);
+          }
+        if (half == 0)
+          __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f32x2{m, l}), rs, (int)(slot + at_sums), 0, kDevice);
+        write = last_of(c, sh, join);
+      }
       if (write) {
+        const RowState own = *this;
         clear();
 #pragma unroll 1
-        for (int s = 0; s < parts; ++s) {
+        for (int s = 0; s < join.parts; ++s) {
+          constexpr int ONCE = T::DT == 4 ? 4 : 2;  // so that loads and sums fit into the registers
+          const bool mine = join.counter + s == me;
           const uint32_t slot = place_of(join, s, T::PART);
-          const f32x2 t2 = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, (int)(slot + (uint32_t)(T::ROWS * DP + 2 * r) * 4u), 0, kDevice));
-          const float now = fmaxf(m, t2[0]), by = now == -INFINITY ? 0.f : now;
-          const float f0 = exp2_(m - by), f1 = exp2_(t2[0] - by);
-          m = now;
-          l = __builtin_fmaf(t2[1], f1, l * f0);
+          f32x2 sums = {own.m, own.l};
+          if (!mine) sums = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, (int)(slot + at_sums), 0, kDevice));
+          float f0 = 0.f, f1 = 0.f;
 #pragma unroll
-          for (int t = 0; t < T::DT; ++t)
+          for (int t0 = 0; t0 < T::DT; t0 += ONCE) {
+            f32x4 v[ONCE][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const f32x4 v = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                  rs, (int)(slot + (uint32_t)(r * DP + 32 * t + 8 * i + 4 * half) * 4u), 0, kDevice));
+            for (int t = 0; t < ONCE; ++t)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) acc[t][4 * i + j] = __builtin_fmaf(v[j], f1, acc[t][4 * i + j] * f0);
+              for (int i = 0; i < 4; ++i) {
+                const f32x16 &o = own.acc[t0 + t];
+                v[t][i] = f32x4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
+              }
+            if (!mine) {
+#pragma unroll
+              for (int t = 0; t < ONCE; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  v[t][i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(slot + at + (uint32_t)(4 * (t0 + t) + i) * 1024u), 0, kDevice));
             }
+            if (t0 == 0) {
+              const float now = fmaxf(m, sums[0]), by = now == -INFINITY ? 0.f : now;
+              f0 = exp2_(m - by), f1 = exp2_(sums[0] - by);
+              m = now;
+              l = __builtin_fmaf(sums[1], f1, l * f0);
+            }
+#pragma unroll
+            for (int t = 0; t < ONCE; ++t)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) acc[t0 + t][i] = __builtin_fmaf(v[t][i >> 2][i & 3], f1, acc[t0 + t][i] * f0);
+          }
         }
       }
     }

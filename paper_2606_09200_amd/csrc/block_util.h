@@ -200,6 +200,10 @@ template <class V>
 __device__ __forceinline__ void put_device(V *p, V v) {  // through the XCD's L2, for readers on other XCDs
   __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
+template <class V>
+__device__ __forceinline__ V get_device(V *p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 __device__ __forceinline__ uint32_t add_device(uint32_t *p) {
   return __hip_atomic_fetch_add(p, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
