@@ -1392,10 +1392,14 @@ int attn_launch(const occ_attn_args &a, hipStream_t s) {
     k.groups = (c.group + k.heads - 1) / k.heads;
     k.by_heads = Divider(k.heads), k.by_groups = Divider(k.groups);
     k.cut.parts = a.Hkv * k.groups;
-    k.cut.fixed = many ? 128 : 256, k.cut.block = many ? many_keys(DP) : few_keys(DP);
+    // Keys' worth of an item's beginning and end.  Many rows: 11 us (a piece's q, pages and first tiles, a masked tile, its
+    // output), a tile of 64 keys 1.8 us; with 128 in place of 512 a prompt of 8192 took 682 us instead of 565, whose short
+    // items fell to few workgroups, and with 1024 570.  Few rows: 128 and 512 make 64 requests 1 % slower.
+    k.cut.fixed = many ? (DP <= 128 ? 512 : 256) : 256, k.cut.block = many ? many_keys(DP) : few_keys(DP);
     k.cut.window = a.window < c.keys ? a.window : 0, k.cut.causal = a.causal != 0;
     k.least = least, k.most = most;
-    k.min_share = 256, k.least_even = many ? 512 : 256, k.spare = 512;
+    // (four chunks of 256 tokens: 57 us with 512 spare, 43 with 1024)
+    k.min_share = 256, k.least_even = many ? 512 : 256, k.spare = many ? 1024 : 512;
     return many ? launch<true>(k, DP, cus, s) : launch<false>(k, DP, cus, s);
   };
   const int most_rows = (int)std::min<int64_t>((int64_t)std::min(a.max_fresh, a.rows) * c.group, INT32_MAX);
