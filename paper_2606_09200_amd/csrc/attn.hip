@@ -169,12 +169,7 @@ struct Piece {
 template <int THREADS>
 __device__ __forceinline__ void block_sums(WalkShared<THREADS> &sh, int64_t (&v)[2], int64_t (&total)[2]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int64_t upto[2] = {v[0], v[1]};
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t x = __shfl_up(upto[0], d), y = __shfl_up(upto[1], d);
-    if (lane >= d) upto[0] += x, upto[1] += y;
-  }
+  int64_t upto[2] = {sum_upto(v[0]), sum_upto(v[1])};
   if (lane == 63) sh.sums[0][wave] = upto[0], sh.sums[1][wave] = upto[1];
   __syncthreads();
 #pragma unroll
@@ -1150,7 +1145,6 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
     loads.ever_bad = false;
     loads.step_pages = rows.page_of(T::KEYS), loads.step_rows = T::KEYS - loads.step_pages * rows.page;
     if (threadIdx.x < 16) (&sh.bad_rows[0][0])[threadIdx.x] = 0u;
-    if (p.b0 < p.b1) loads.fill(p.b0), loads.find(p.b0);
     u32x4 q[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
@@ -1158,6 +1152,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
       if (row.valid && (FULL || 16 * s + 8 * half < c.D))
         q[s] = *reinterpret_cast<const u32x4 *>(c.q + (size_t)row.token * c.q_row + (size_t)row.head * c.q_head + 16 * s + 8 * half);
     }
+    if (p.b0 < p.b1) loads.fill(p.b0), loads.find(p.b0);
     RowState<DP> state;
     state.clear();
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): from here on only direct loads to LDS are counted

@@ -215,6 +215,23 @@ __device__ __forceinline__ void stores_done() {
   __syncthreads();
 }
 
+// The value of a lane before, 0 where there is none; of rows of 16 lanes, then of their last ones.
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ int64_t lane_before(int64_t v) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CONTROL, ROWS, 0xF, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)((uint64_t)v >> 32), CONTROL, ROWS, 0xF, false);
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+// The sum of the lanes up to one's own.
+__device__ __forceinline__ int64_t sum_upto(int64_t v) {
+  v += lane_before<0x111, 0xF>(v);
+  v += lane_before<0x112, 0xF>(v);
+  v += lane_before<0x114, 0xF>(v);
+  v += lane_before<0x118, 0xF>(v);
+  v += lane_before<0x142, 0xA>(v);
+  return v + lane_before<0x143, 0xC>(v);
+}
+
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
   return as_float((uint32_t)__builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));

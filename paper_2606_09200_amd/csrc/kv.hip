@@ -60,23 +60,6 @@ __device__ __forceinline__ void pass(const TablesCall &c, Before &b, const Asked
   b.back += a.back;
 }
 
-// The value of a lane before, 0 where there is none; of rows of 16 lanes, then of their last ones.
-template <int CONTROL, int ROWS>
-__device__ __forceinline__ int64_t lane_before(int64_t v) {
-  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CONTROL, ROWS, 0xF, false);
-  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)((uint64_t)v >> 32), CONTROL, ROWS, 0xF, false);
-  return (int64_t)((uint64_t)hi << 32 | lo);
-}
-// The sum of the lanes up to one's own.
-__device__ __forceinline__ int64_t sum_upto(int64_t v) {
-  v += lane_before<0x111, 0xF>(v);
-  v += lane_before<0x112, 0xF>(v);
-  v += lane_before<0x114, 0xF>(v);
-  v += lane_before<0x118, 0xF>(v);
-  v += lane_before<0x142, 0xA>(v);
-  return v + lane_before<0x143, 0xC>(v);
-}
-
 // STAGED: up to kStaged requests lie in LDS, with what those before them have asked for, so that the passes over them and
 // the search for a token's request wait for nothing but LDS.
 constexpr int kStaged = 2048;
