@@ -423,7 +423,12 @@ __device__ __forceinline__ void seen_by_all(const AttnCall &c, const Piece &p, i
 // from memory to the registers of S^T = K Q^T as they are (16x16x32 MFMAs: a lane holds 8 keys' scores of one row, which
 // are what the second product wants of it), values pass through the wave's own LDS to be read transposed for O^T = V^T
 // P^T.  P goes in as the sum of two bf16 values: matrix instructions are in plenty here, and o then has
-// its own rounding alone.
+// its own rounding alone (off by 0.0016 of its size; 0.0023 with one).
+//   Heads of 256 take a register more than there are: it is spilled before the loop and read again behind it.
+//   One workgroup a CU, so that a share is long: 64 requests of 1 to 8191 keys, 64 heads over 8 of 128, 213 us (5.0 TB/s, a
+// copy's rate), 40 heads of their own 250 (5.3 TB/s); 130000 keys of one request 117 (4.55 TB/s: workgroups finish 70 to 96 us
+// after they begin, as their pages lie).  Four requests of 500 keys 14.5: 3.6 the plan, 1.4 pages and the first keys, 2 the
+// keys, 5 the parts' way through memory.
 template <int DP>
 struct FewTile {
   static constexpr int WAVES = 8, THREADS = 64 * WAVES;
@@ -1108,6 +1113,9 @@ __device__ __forceinline__ void interleave() {
 // the ring is free from slot 2 b + 4 on.  All waves ask for their part of tile b + 3 in the slot that has scores of
 // tile b + 1 (2 b + 2, 2 b + 3), in the time that the matrix instructions leave.  Each waits for its loads of tile b + 1 before the
 // barrier that ends slot 2 b + 1, after which waves 0-3 read it: later ones, of tile b + 2, may be outstanding.
+//   A causal prompt of 8192, 32 heads over 8 of 128: 530 us, 1040 TFLOP/s.  The matrix pipes are 55 % busy (LDS 29 %, no bank
+// conflicts), a slot about 1850 cycles, at a clock that the board's power lowers from 2.1 to 1.7 GHz; with four waves of 32
+// rows, one a SIMD, it took 722.  Heads of 64: half the products, as many exponentials: 355 us, pipes 33 % busy.
 template <int DP, bool FULL>
 __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void attn_pairs_kernel(AttnCall c) {
   using T = ManyTile<DP>;
@@ -1242,7 +1250,9 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
 }
 
 // Heads beyond 128 values, whose o and q fill half of a SIMD's registers: one wave each, tiles of 32 keys that are loaded
-// three ahead, values read from LDS while the weights are made.
+// three ahead, values read from LDS while the weights are made.  A prompt of 4096, 16 heads over 8 of 256: 232 us, 590 TFLOP/s,
+// pipes 25 % busy: a wave has nobody to make weights beside its products.  Making the next tile's scores right after o, its
+// keys read meanwhile, took 250.
 template <int DP, bool FULL>
 __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void attn_wide_kernel(AttnCall c) {
   using T = ManyTile<DP>;
@@ -1273,7 +1283,6 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
     loads.ever_bad = false;
     loads.step_pages = rows.page_of(T::KEYS), loads.step_rows = T::KEYS - loads.step_pages * rows.page;
     if (threadIdx.x < 16) (&sh.bad_rows[0][0])[threadIdx.x] = 0u;
-    if (p.b0 < p.b1) loads.fill(p.b0), loads.find(p.b0);
     u32x4 q[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
@@ -1281,6 +1290,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
       if (row.valid && (FULL || 16 * s + 8 * half < c.D))
         q[s] = *reinterpret_cast<const u32x4 *>(c.q + (size_t)row.token * c.q_row + (size_t)row.head * c.q_head + 16 * s + 8 * half);
     }
+    if (p.b0 < p.b1) loads.fill(p.b0), loads.find(p.b0);
     RowState<DP> state;
     state.clear();
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): from here on only direct loads to LDS are counted

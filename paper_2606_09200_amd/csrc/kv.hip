@@ -15,6 +15,8 @@ constexpr int kThreads = 256, kWaves = 4;
 // All sums are over requests: tokens, pages to get, pages that go back.  One launch: every workgroup makes the sums of all
 // requests for itself (8 bytes a request from the L2) and then does its share of the requests (pages) and of the tokens.
 // Pages come from the ring's head and go back behind its tail, so nothing that one workgroup reads is written by another.
+// What bounds it is latency: 64 requests 6.2 us, of which a launch is 2.3 (8.2 with sums through LDS lane by lane, requests
+// read again for each pass and twice the code, which is fetched cold); 1500 requests with 360000 tokens 13.
 struct TablesCall {
   int n, T, width, pages, size;
   int64_t keys;              // width * page
@@ -215,7 +217,8 @@ __global__ __launch_bounds__(kThreads) void kv_tables_kernel(TablesCall c) {
 //
 // for pair i of a head.  turns is a 64-bit fraction of a turn, so that position * turns modulo 2^64 is the exact
 // remainder of the angle, however far the position.  A workgroup makes its tokens' cosines and sines once, in LDS, and
-// passes over their heads: bound by reading and writing q, k and v once.
+// passes over their heads: bound by reading and writing q, k and v once.  8192 tokens, 64 heads over 8 of 128, into the cache:
+// 76 us, 4.4 TB/s (a copy 4.95); 16 tokens 3.4 us.
 struct RopeCall {
   int T, Hq, Hkv, D, half, interleaved;
   const void *q, *k, *v;

@@ -269,6 +269,34 @@ def test_long_requests_are_shared_and_joined():
         assert torch.equal(p.run(max_fresh=70)[0], first)
 
 
+@pytest.mark.parametrize("requests,D,window", [([(100, 300)] * 5, 64, 0), ([(40, 513), (0, 260), (900, 255)] * 2, 128, 0),
+                                                 ([(300, 700), (5, 90)] * 2, 80, 200), ([(7, 400)] * 3, 256, 0)])
+def test_more_items_than_workgroups(requests, D, window):
+    """Shares that begin and end within items, of chunks: the same bits every time, and what 64 bits give for the first and
+    the last head."""
+    heads = 32
+    p = Problem(requests, heads, heads, D, 16, seed=30)
+    out, lse = (t.clone() for t in p.run(window=window))
+    for _ in range(4):
+        again = p.run(window=window)
+        assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+    ends = [0, heads - 1]
+    k, v, q = (f64(t)[..., ends, :] for t in (p.dk, p.dv, p.dq))
+    want = ref.attention(q, k, v, p.table, p.starts, p.lens, D ** -0.5, True, window)
+    compare(f64(out)[:, ends], f64(lse)[:, ends], want, D)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_more_pages_than_are_at_hand(D):
+    """Pages of one row: a part of an item has more of them than a wave keeps, some of them none."""
+    p = Problem([(1500, 70), (700, 1)], 4, 2, D, 1, seed=31)
+    p.check()
+    for j in (300, 301, 511, 1040):
+        p.table[0][j] = -1 if j % 2 else p.pages
+    p.dtable = i32(p.table)
+    p.check()
+
+
 def test_many_requests():
     """More requests than a workgroup has threads, most of them short."""
     rng = np.random.default_rng(15)
