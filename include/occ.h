@@ -674,7 +674,8 @@ size_t occ_moe_workspace_bytes(int tokens, int H, int I, int experts, int top_k)
  *   positions : rows; cached + 0, 1, ..; 0 for rows without a served request
  *   free_after: as free, for the next call; pages that come back are behind the others, and are not given out by this call
  * Only `table` and `ring` are read and written; the others must not overlap.  A program keeps lens, where it is not -1, as the
- * next step's cached and free_after as its free.  Everything is exact; int32 buffers, 4-byte aligned.  No workspace.
+ * next step's cached and free_after as its free.  Everything is exact; int32 buffers, 4-byte aligned (requests
+ * == 0: cached, fresh, lens and table may be null).  No workspace.
  */
 typedef struct occ_kv_tables_args {
   int requests, rows, width, page, pages, ring_size;
@@ -698,7 +699,7 @@ int occ_kv_tables(const occ_kv_tables_args *args, void *stream);
  * heads, cache_page, cache_row, cache_head of both caches.  Values of a head are contiguous.  1 <= D <= OCC_ROPE_MAX_D,
  * even, 0 <= 2 pairs <= D; page * pages < 2^31; rows <= 2^24.  Pitches, D / 2 and pairs that are multiples of 8 (4 with
  * OCC_F32), on 16-byte aligned buffers, are the fast case.
- * Two rows with one slot: either may be what is kept.  A head's rows must not overlap another's.
+ * Two rows with one slot: each value that is kept is one of theirs.  A head's rows must not overlap another's.
  */
 #define OCC_ROPE_MAX_D 1024
 typedef struct occ_rope_args {

@@ -221,17 +221,17 @@ int validate_kv_tables(const occ_kv_tables_args &a) {
   if (a.requests < 0 || a.requests > OCC_KV_MAX_REQUESTS || a.rows < 0 || a.rows > (1 << 24)) return OCC_EINVAL;
   if (a.width < 0 || a.page < 1 || a.page > OCC_KV_MAX_PAGE || a.pages < 0 || a.ring_size < 1) return OCC_EINVAL;
   if ((long long)a.pages * a.page > INT32_MAX || a.ring_size > (1 << 30)) return OCC_EINVAL;
-  if (a.requests == 0) return OCC_OK;
   if (a.requests > 1 && a.ld_table < (size_t)a.width) return OCC_EINVAL;
-  const void *needed[] = {a.cached, a.fresh, a.free, a.ring, a.lens, a.starts, a.free_after};
-  for (const void *p : needed)
-    if (p == nullptr || !aligned(p, 4)) return OCC_EINVAL;
-  if ((a.width > 0 && a.table == nullptr) || !aligned(a.table, 4)) return OCC_EINVAL;
+  const void *all[] = {a.cached, a.fresh, a.lens, a.table, a.free, a.ring, a.starts, a.free_after};
+  for (const void *p : all)
+    if (!aligned(p, 4)) return OCC_EINVAL;
+  if (a.requests > 0 && (a.cached == nullptr || a.fresh == nullptr || a.lens == nullptr || (a.width > 0 && a.table == nullptr))) return OCC_EINVAL;
+  if (a.free == nullptr || a.ring == nullptr || a.starts == nullptr || a.free_after == nullptr) return OCC_EINVAL;
   if (a.rows > 0 && (a.slots == nullptr || a.positions == nullptr)) return OCC_EINVAL;
   if (!aligned(a.slots, 4) || !aligned(a.positions, 4)) return OCC_EINVAL;
   const size_t n = (size_t)a.requests * 4, t = (size_t)a.rows * 4;
   const Range in[] = {{a.cached, n}, {a.fresh, n}, {a.free, 8}};
-  const Range out[] = {{a.table, a.width == 0 ? 0 : ((size_t)(a.requests - 1) * a.ld_table + a.width) * 4},
+  const Range out[] = {{a.table, a.width == 0 || a.requests == 0 ? 0 : ((size_t)(a.requests - 1) * a.ld_table + a.width) * 4},
                        {a.ring, (size_t)a.ring_size * 4}, {a.lens, n}, {a.starts, n + 4}, {a.slots, t}, {a.positions, t},
                        {a.free_after, 8}};
   return disjoint(out, in) ? OCC_OK : OCC_EALIAS;

@@ -145,6 +145,7 @@ __global__ __launch_bounds__(kThreads) void kv_tables_kernel(TablesCall c) {
   __syncthreads();
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     const int64_t next = head + taken, back = before[kThreads].back;
+    if (c.n == 0) c.starts[0] = 0;
     c.free_after[0] = (int)(next < size ? next : next - size);
     c.free_after[1] = (int)min(count - taken + back, size - taken);
   }
@@ -350,7 +351,6 @@ int kv_tables_launch(const occ_kv_tables_args &a, hipStream_t s) {
   const DeviceInfo *di = nullptr;
   const int st = current_device_info(&di);
   if (st != OCC_OK) return st;
-  if (a.requests == 0) return OCC_OK;
   TablesCall c{};
   c.n = a.requests, c.T = a.rows, c.width = a.width, c.pages = a.pages, c.size = a.ring_size, c.page = a.page;
   c.keys = std::min<int64_t>((int64_t)a.width * a.page, OCC_ATTN_MAX_KEYS);
@@ -359,7 +359,7 @@ int kv_tables_launch(const occ_kv_tables_args &a, hipStream_t s) {
   c.lens = a.lens, c.starts = a.starts, c.slots = a.slots, c.positions = a.positions, c.free_after = a.free_after;
   // a token a thread while that takes no more than two workgroups a CU: each of them scans all requests
   c.each = a.rows <= 2 * kThreads * di->num_cus ? 1 : 4;
-  const int grid = std::max((int)(((int64_t)a.rows + kThreads * c.each - 1) / (kThreads * c.each)), (a.requests + 63) / 64);
+  const int grid = std::max({(int)(((int64_t)a.rows + kThreads * c.each - 1) / (kThreads * c.each)), (a.requests + 63) / 64, 1});
   c.requests = (a.requests + grid - 1) / grid;
   hipLaunchKernelGGL(a.requests <= kStaged ? kv_tables_kernel<true> : kv_tables_kernel<false>, dim3(grid), dim3(kThreads), 0, s, c);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;

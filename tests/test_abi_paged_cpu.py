@@ -57,7 +57,7 @@ def attn(**k):
     (EINVAL, dict(pages=1 << 27)), (EINVAL, dict(ring_size=(1 << 30) + 1)), (EINVAL, dict(ld_table=7)), (EINVAL, dict(cached=None)),
     (EINVAL, dict(fresh=place(2) + 2)), (EINVAL, dict(free=None)), (EINVAL, dict(table=None)), (EINVAL, dict(ring=None)),
     (EINVAL, dict(lens=None)), (EINVAL, dict(starts=None)), (EINVAL, dict(slots=None)), (EINVAL, dict(positions=place(9) + 1)),
-    (EINVAL, dict(free_after=None)), (EALIAS, dict(lens=place(1))), (EALIAS, dict(free_after=place(3))), (EALIAS, dict(ring=place(4) + 64)),
+    (EINVAL, dict(free_after=None)), (EINVAL, dict(requests=0, free=None)), (EINVAL, dict(requests=0, starts=None)), (EALIAS, dict(lens=place(1))), (EALIAS, dict(free_after=place(3))), (EALIAS, dict(ring=place(4) + 64)),
     (EALIAS, dict(starts=place(6) + 12)), (EALIAS, dict(slots=place(9))), (EALIAS, dict(table=place(2) - 100)),
 ])
 def test_tables_refusals(L, status, change):
@@ -66,7 +66,7 @@ def test_tables_refusals(L, status, change):
 
 def test_tables_accepts(L):
     assert L.occ_kv_tables(None, None) == EINVAL
-    for k in (dict(), dict(requests=0, cached=None), dict(rows=0, slots=None, positions=None), dict(width=0, table=None),
+    for k in (dict(), dict(requests=0, cached=None, fresh=None, lens=None, table=None), dict(rows=0, slots=None, positions=None), dict(width=0, table=None),
               dict(requests=1, ld_table=0), dict(pages=0)):
         expect_accepted(L, L.occ_kv_tables, tables(**k), None)
 

@@ -118,7 +118,7 @@ int main() {
     c.by_tokens = Divider(c.tokens);
     c.parts = pick({1, 2, 8});
     c.block = pick({32, 64});
-    c.fixed = pick({0, 1, 32, 64, 300}) + (n % 2 ? 32 : 1);
+    c.fixed = pick({0, 1, 32, 64, 300, 512, 2000}) + (n % 2 ? 32 : 1);
     c.window = pick({0, 0, 1, 5, 100, 1 << 30});
     c.causal = pick({1, 1, 0});
     c.flat = pick({0, 1});

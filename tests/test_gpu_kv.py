@@ -94,6 +94,18 @@ def test_tables_edges():
     check([0, 0], [0, 1], [[], []], [0], [0, 1], 4, 1, 1)
 
 
+def test_tables_without_requests():
+    """Nothing is asked: no token has a slot, and the free pages stay."""
+    empty = torch.empty((0, 5), dtype=torch.int32, device=DEV)
+    ring, free = i32([4, 5, 6, 7]), i32([3, 2])
+    for rows in (0, 300):
+        starts, slots, positions, after = (torch.full((m,), -99, dtype=torch.int32, device=DEV) for m in (1, rows, rows, 2))
+        occ.occ_kv_tables(empty[:, 0].contiguous(), empty[:, 0].contiguous(), empty, ring, free, page=4, pages=8, lens=empty[:, 0].contiguous(),
+                          starts=starts, slots=slots, positions=positions, free_after=after)
+        assert starts.tolist() == [0] and slots.tolist() == [-1] * rows and positions.tolist() == [0] * rows
+        assert after.tolist() == [3, 2] and ring.tolist() == [4, 5, 6, 7]
+
+
 def test_tables_long_requests():
     # more pages and tokens than a wave or a workgroup has lanes, of one request
     cached, fresh, page = [5000, 100000], [9000, -1], 16
