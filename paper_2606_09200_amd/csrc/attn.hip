@@ -728,25 +728,31 @@ __global__ __launch_bounds__(FewTile<DP>::THREADS, FewTile<DP>::PER_CU) void att
 
 // ------------------------------------------------------------------ many rows
 //
-// Chunks of a prompt: 256 rows (128 with heads beyond 128 values) of tokens times heads that share keys, 32 of each
-// wave, against tiles of keys in a ring of four that direct-to-LDS loads fill ahead.  S^T = K Q^T in 32x32x16 MFMAs leaves a lane
-// 16 of 32 keys' scores of one row (the other half of the wave has the other 16), which, rounded to bf16, are the
-// second product's operand as they lie: O^T = V^T P^T over the keys in that order, values read transposed.  m and l are
+// Chunks of a prompt: 256 rows of tokens times heads that share keys, 32 of each wave, against tiles of keys in a ring of
+// four that direct-to-LDS loads fill ahead.  S^T = K Q^T in 32x32x16 MFMAs leaves a lane 16 of 32 keys' scores of one row
+// (the other half of the wave has the other 16), which, rounded to bf16, are the second product's operand as they
+// lie: O^T = V^T P^T over the keys in that order, values read transposed.  Heads beyond 128 values, whose o and q would
+// fill the registers, have 16 rows a wave and 16x16x32 MFMAs (a lane has 4 of 16 keys): every wave reads the tile from LDS for half
+// as many rows, and two waves a SIMD fit (a prompt of 4096, heads of 256: 232 us with one wave of 32 rows, 203 so).  m and l are
 // one register a lane, and so is what o has to be scaled by.  The weights' rounding (8 bits) is of the same size as the output's
 // own; l sums them unrounded.
 // Scaling o costs as much as half of a tile's exponentials: m stays behind the maximum until it would have to grow by
 // kSlack, so that weights are up to 2^kSlack and o is scaled once or twice in all.
 template <int DP>
 struct ManyTile {
-  static constexpr bool PAIRS = DP <= 128;             // two waves a SIMD that take turns, see attn_pairs_kernel
-  static constexpr int THREADS = PAIRS ? 512 : 256, WAVES = THREADS / 64;
-  static constexpr int ROWS = 32 * WAVES, KEYS = PAIRS ? 64 : 32;
-  static constexpr int KS = DP / 16, DT = DP / 32, KT = KEYS / 32;
+  static constexpr int WAVES = 8, THREADS = 64 * WAVES;
+  static constexpr int R = DP <= 128 ? 32 : 16;        // rows of a wave, and side of its matrix instructions
+  static constexpr int P = 64 / R;                     // parts of a wave, each with a lane for every row
+  static constexpr int ROWS = R * WAVES, KEYS = 2 * R;
+  static constexpr int STEP = 8 * P;                   // of the products' inner index in an instruction
+  static constexpr int KS = DP / STEP, DT = DP / R, KT = 2, WT = KEYS / STEP;
+  static constexpr int N = R / P;                      // values of a result tile that a lane has: 4 of every 4 P rows
+  typedef float Acc __attribute__((ext_vector_type(N)));
   static constexpr int CH = DP / 8;                    // 16-byte chunks of a row
   static constexpr int PITCH = DP * 2;
   static constexpr int OPERAND = KEYS * PITCH;         // bytes of a tile of K, and of V
   static constexpr int STAGES = 4, STAGE = 2 * OPERAND;
-  static constexpr int ZEROS = PAIRS ? OPERAND : 0;    // bytes of zeros behind the ring
+  static constexpr int ZEROS = OPERAND;                // bytes of zeros behind the ring
   static constexpr int LDS = STAGES * STAGE + ZEROS;
   static constexpr int PASS_ROWS = THREADS / CH, PASSES = KEYS / PASS_ROWS;
   static constexpr int DMAS = 2 * PASSES;              // of a wave for a tile
@@ -765,7 +771,24 @@ __device__ __forceinline__ int many_swizzle_k(int r, int c) {
 }
 template <int DP>
 __device__ __forceinline__ int many_swizzle_v(int r, int c) {
-  return swz_kn<ManyTile<DP>::CH>(r, c);
+  if constexpr (DP > 128) return few_swizzle<DP>(r, c);  // 8 rows at 2 chunks in a row
+  else return swz_kn<ManyTile<DP>::CH>(r, c);
+}
+template <int DP>
+__device__ __forceinline__ typename ManyTile<DP>::Acc many_mfma(u32x4 a, u32x4 b, typename ManyTile<DP>::Acc c) {
+  if constexpr (ManyTile<DP>::R == 32) return mfma32(a, b, c);
+  else return mfma16(a, b, c);
+}
+// Over the lanes that have a row, the same bits in all of them.
+template <int DP>
+__device__ __forceinline__ float row_max(float v) {
+  if constexpr (ManyTile<DP>::R == 32) return max_halves(v);
+  else return max_quarters(v);
+}
+template <int DP>
+__device__ __forceinline__ float row_sum(float v) {
+  if constexpr (ManyTile<DP>::R == 32) return sum_halves(v);
+  else return sum_quarters(v);
 }
 
 // 16 bytes a lane from its own address to LDS at `lds` + 16 lane.
@@ -879,29 +902,31 @@ struct Fragments {
   using T = ManyTile<DP>;
   uint32_t k0, v0, vt0;
   __device__ __forceinline__ Fragments(uint32_t lds, int lane) {
-    const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15, r = 4 * half + (l16 >> 2);
-    k0 = lds + (uint32_t)(l32 * T::PITCH + many_swizzle_k<DP>(l32, half) * 16);
+    const int row = lane % T::R, part = lane / T::R, l16 = lane & 15, r = 4 * part + (l16 >> 2);
+    k0 = lds + (uint32_t)(row * T::PITCH + many_swizzle_k<DP>(row, part) * 16);
     vt0 = lds + T::OPERAND;
-    v0 = vt0 + r * T::PITCH + many_swizzle_v<DP>(r, 2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1)) * 16 + 8 * (l16 & 1);
+    v0 = vt0 + r * T::PITCH + many_swizzle_v<DP>(r, 2 * (row >> 4) + ((l16 & 3) >> 1)) * 16 + 8 * (l16 & 1);
   }
-  // Key 32 t + l % 32, values 16 s + 8 (l / 32) .. + 7.
+  // Key R t + l % R, values STEP s + 8 (l / R) .. + 7.
   __device__ __forceinline__ void keys(int b, int t, u32x4 (&k)[T::KS]) const {
+    constexpr int IN = 16 / T::P;  // steps in 256 bytes
     const uint32_t from = k0 + (uint32_t)(b % T::STAGES) * T::STAGE;
 #pragma unroll
     for (int s = 0; s < T::KS; ++s)
-      k[s] = *(__attribute__((address_space(3))) const u32x4 *)(size_t)((from ^ ((s & 7) * 32)) + (s >> 3) * 256 + 32 * t * T::PITCH);
+      k[s] = *(__attribute__((address_space(3))) const u32x4 *)(size_t)((from ^ ((s % IN) * 16 * T::P)) + (s / IN) * 256 + T::R * t * T::PITCH);
   }
-  // Values 32 (t0 + t) + l % 32 of the 8 keys of 16 s .. that the lane's weights are of.
+  // Values R (t0 + t) + l % R of the 8 keys of STEP s .. that the lane's weights are of.
   __device__ __forceinline__ uint32_t stage(int b) const { return (uint32_t)(b % T::STAGES) * T::STAGE; }
   template <int N>
-  __device__ __forceinline__ void values(uint32_t stage, int t0, u32x4 (&v)[N][2 * T::KT]) const {
+  __device__ __forceinline__ void values(uint32_t stage, int t0, u32x4 (&v)[N][T::WT]) const {
+    constexpr int IN = 128 / T::R;  // tiles of values in 256 bytes
     const uint32_t from = v0 + stage;
 #pragma unroll
-    for (int s = 0; s < 2 * T::KT; ++s)  // in the order in which multiply() uses them
+    for (int s = 0; s < T::WT; ++s)  // in the order in which multiply() uses them
 #pragma unroll
       for (int t = 0; t < N; ++t) {
-        const uint32_t at = (from ^ (((t0 + t) & 3) * 64)) + ((t0 + t) >> 2) * 256;
-        const u32x2 a = read_transposed(at + 16 * s * T::PITCH), b2 = read_transposed(at + (16 * s + 8) * T::PITCH);
+        const uint32_t at = (from ^ (((t0 + t) % IN) * 2 * T::R)) + ((t0 + t) / IN) * 256;
+        const u32x2 a = read_transposed(at + T::STEP * s * T::PITCH), b2 = read_transposed(at + (T::STEP * s + 4 * T::P) * T::PITCH);
         v[t][s] = u32x4{a[0], a[1], b2[0], b2[1]};
       }
   }
@@ -911,33 +936,34 @@ struct Fragments {
 template <int DP>
 struct RowState {
   using T = ManyTile<DP>;
-  f32x16 acc[T::DT];
+  using Acc = typename T::Acc;
+  Acc acc[T::DT];
   float m, l;
   __device__ __forceinline__ void clear() {
     m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int t = 0; t < T::DT; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
+      for (int i = 0; i < T::N; ++i) acc[t][i] = 0.f;
   }
   // Scores of the keys from kb on (tile b) to weights.  `masked`: not all are seen by all rows.  True if there are
   // infinities or NaN among such a tile's values: they must not reach rows that do not see them, and have gone into o
   // one by one.
-  __device__ __forceinline__ bool weigh(f32x16 (&x)[T::KT], u32x4 (&w)[2 * T::KT], float scale, bool masked, int b, int kb, const Row &row,
+  __device__ __forceinline__ bool weigh(Acc (&x)[T::KT], u32x4 (&w)[T::WT], float scale, bool masked, int b, int kb, const Row &row,
                                         uint32_t bad0, uint32_t bad1, const Fragments<DP> &from, int lane) {
-    const int half = lane >> 5;
+    const int part = lane / T::R;
     const uint32_t vt0 = from.vt0 + (uint32_t)(b % T::STAGES) * T::STAGE;
     bool odd = false;
     if (masked) {
-      // a lane's scores are of keys 32 t + 8 (i / 4) + 4 half + i % 4
-      const int lo = row.lo - kb - 4 * half, hi = row.hi - kb - 4 * half;
+      // a lane's scores are of keys R t + 4 P (i / 4) + 4 part + i % 4
+      const int lo = row.lo - kb - 4 * part, hi = row.hi - kb - 4 * part;
 #pragma unroll
       for (int t = 0; t < T::KT; ++t) {
-        const uint32_t bad = (t ? bad1 : bad0) >> (4 * half);
+        const uint32_t bad = (T::R * t >= 32 ? bad1 : bad0) >> (T::R * t % 32 + 4 * part);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int at = 8 * (i >> 2) + (i & 3);
-          x[t][i] = 32 * t + at >= lo && 32 * t + at < hi && !((bad >> at) & 1u) ? x[t][i] : -INFINITY;
+        for (int i = 0; i < T::N; ++i) {
+          const int at = 4 * T::P * (i >> 2) + (i & 3);
+          x[t][i] = T::R * t + at >= lo && T::R * t + at < hi && !((bad >> at) & 1u) ? x[t][i] : -INFINITY;
         }
       }
       uint32_t bits = 0;
@@ -951,8 +977,8 @@ struct RowState {
     }
     float top = x[0][0];
 #pragma unroll
-    for (int i = 1; i < 16 * T::KT; ++i) top = fmaxf(top, x[i >> 4][i & 15]);
-    top = max_halves(top) * scale;
+    for (int i = 1; i < T::N * T::KT; ++i) top = fmaxf(top, x[i / T::N][i % T::N]);
+    top = row_max<DP>(top) * scale;
     if (__ballot(top > m + kSlack) != 0) {
       const float now = fmaxf(m, top), less = now == -INFINITY ? 1.f : exp2_(m - now);
       m = now;
@@ -967,9 +993,9 @@ struct RowState {
 #pragma unroll
         for (int t = 0; t < T::DT; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            // values 32 t + 8 i + 4 half .. + 3 of key r
-            const uint32_t a = vt0 + r * T::PITCH + many_swizzle_v<DP>(r, 4 * t + i) * 16 + 8 * half;
+          for (int i = 0; i < T::N / 4; ++i) {
+            // values R t + 4 P i + 4 part .. + 3 of key r
+            const uint32_t a = vt0 + r * T::PITCH + many_swizzle_v<DP>(r, (T::R * t + 4 * T::P * i + 4 * part) >> 3) * 16 + 8 * (part & 1);
             const u32x2 h = *(__attribute__((address_space(3))) const u32x2 *)(size_t)a;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -983,41 +1009,42 @@ struct RowState {
 #pragma unroll
     for (int t = 0; t < T::KT; ++t)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float e0 = exp2_(__builtin_fmaf(x[t][2 * i], scale, -by)), e1 = exp2_(__builtin_fmaf(x[t][2 * i + 1], scale, -by));
+      for (int i = 0; i < T::N; i += 2) {
+        const float e0 = exp2_(__builtin_fmaf(x[t][i], scale, -by)), e1 = exp2_(__builtin_fmaf(x[t][i + 1], scale, -by));
         l = l + (e0 + e1);
-        w[2 * t + (i >> 2)][i & 3] = pack2(e0, e1);
+        w[(T::N * t + i) / 8][(T::N * t + i) % 8 / 2] = pack2(e0, e1);
       }
     return odd;
   }
   // Infinities and NaN that weigh() has seen to, out of the values.
   template <int N>
-  __device__ __forceinline__ static void only_finite(u32x4 (&v)[N][2 * T::KT]) {
+  __device__ __forceinline__ static void only_finite(u32x4 (&v)[N][T::WT]) {
 #pragma unroll
     for (int t = 0; t < N; ++t)
 #pragma unroll
-      for (int s = 0; s < 2 * T::KT; ++s)
+      for (int s = 0; s < T::WT; ++s)
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[t][s][i] = pair_finite(v[t][s][i]);
   }
-  // o of the values 32 t0 and on.
+  // o of the values R t0 and on.
   template <int N>
-  __device__ __forceinline__ void multiply(const u32x4 (&v)[N][2 * T::KT], const u32x4 (&w)[2 * T::KT], int t0) {
+  __device__ __forceinline__ void multiply(const u32x4 (&v)[N][T::WT], const u32x4 (&w)[T::WT], int t0) {
 #pragma unroll
-    for (int s = 0; s < 2 * T::KT; ++s)
+    for (int s = 0; s < T::WT; ++s)
 #pragma unroll
-      for (int t = 0; t < N; ++t) acc[t0 + t] = mfma32(v[t][s], w[s], acc[t0 + t]);
+      for (int t = 0; t < N; ++t) acc[t0 + t] = many_mfma<DP>(v[t][s], w[s], acc[t0 + t]);
   }
 
   // The item's part is whole: to the output, or beside the others' and, if it is the last of them, joined, always in the
   // parts' order.  A partial result lies as the lanes have it, 1 KB an instruction.
   __device__ __forceinline__ void finish(const AttnCall &c, WalkShared<T::THREADS> &sh, const Piece &p, const AttnShare &share, const Row &row,
-                                         int me, int r, int half) {
+                                         int me, int wave, int lane) {
     const auto rs = rsrc_of(c.part, gridDim.x * 2u * (uint32_t)(T::PART * 4));
-    l = sum_halves(l);
+    const int r = wave * T::R + lane % T::R, part = lane / T::R;
+    l = row_sum<DP>(l);
     bool write = true;
     if (!p.alone) {
-      const uint32_t at = (uint32_t)((r >> 5) * 32 * DP * 4 + (half * 32 + (r & 31)) * 16), at_sums = (uint32_t)(T::ROWS * DP + 2 * r) * 4u;
+      const uint32_t at = (uint32_t)(wave * T::R * DP * 4 + lane * 16), at_sums = (uint32_t)(T::ROWS * DP + 2 * r) * 4u;
       const Joining join = joining(c, p, share);
       write = others_done(c, sh, join);
       if (!write) {
@@ -1025,11 +1052,11 @@ struct RowState {
 #pragma unroll
         for (int t = 0; t < T::DT; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < T::N / 4; ++i) {
             const f32x4 v = {acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]};
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rs, (int)(slot + at + (uint32_t)(4 * t + i) * 1024u), 0, kDevice);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rs, (int)(slot + at + (uint32_t)(T::N / 4 * t + i) * 1024u), 0, kDevice);
           }
-        if (half == 0)
+        if (part == 0)
           __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f32x2{m, l}), rs, (int)(slot + at_sums), 0, kDevice);
         write = last_of(c, sh, join);
       }
@@ -1038,7 +1065,7 @@ struct RowState {
         clear();
 #pragma unroll 1
         for (int s = 0; s < join.parts; ++s) {
-          constexpr int ONCE = T::DT == 4 ? 4 : 2;  // so that loads and sums fit into the registers
+          constexpr int ONCE = T::DT < 4 ? T::DT : 4, Q = T::N / 4;  // so that loads and sums fit into the registers
           const bool mine = join.counter + s == me;
           const uint32_t slot = place_of(join, s, T::PART);
           f32x2 sums = {own.m, own.l};
@@ -1046,20 +1073,20 @@ struct RowState {
           float f0 = 0.f, f1 = 0.f;
 #pragma unroll
           for (int t0 = 0; t0 < T::DT; t0 += ONCE) {
-            f32x4 v[ONCE][4];
+            f32x4 v[ONCE][Q];
 #pragma unroll
             for (int t = 0; t < ONCE; ++t)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const f32x16 &o = own.acc[t0 + t];
+              for (int i = 0; i < Q; ++i) {
+                const Acc &o = own.acc[t0 + t];
                 v[t][i] = f32x4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
               }
             if (!mine) {
 #pragma unroll
               for (int t = 0; t < ONCE; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  v[t][i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(slot + at + (uint32_t)(4 * (t0 + t) + i) * 1024u), 0, kDevice));
+                for (int i = 0; i < Q; ++i)
+                  v[t][i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(slot + at + (uint32_t)(Q * (t0 + t) + i) * 1024u), 0, kDevice));
             }
             if (t0 == 0) {
               const float now = fmaxf(m, sums[0]), by = now == -INFINITY ? 0.f : now;
@@ -1070,7 +1097,7 @@ struct RowState {
 #pragma unroll
             for (int t = 0; t < ONCE; ++t)
 #pragma unroll
-              for (int i = 0; i < 16; ++i) acc[t0 + t][i] = __builtin_fmaf(v[t][i >> 2][i & 3], f1, acc[t0 + t][i] * f0);
+              for (int i = 0; i < T::N; ++i) acc[t0 + t][i] = __builtin_fmaf(v[t][i >> 2][i & 3], f1, acc[t0 + t][i] * f0);
           }
         }
       }
@@ -1082,13 +1109,13 @@ struct RowState {
 #pragma unroll
       for (int t = 0; t < T::DT; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int d = 32 * t + 8 * i + 4 * half;
+        for (int i = 0; i < T::N / 4; ++i) {
+          const int d = T::R * t + 4 * T::P * i + 4 * part;
           if (d < c.D)
             *reinterpret_cast<u32x2 *>(to + d) = u32x2{pack2(acc[t][4 * i] * by, acc[t][4 * i + 1] * by),
                                                        pack2(acc[t][4 * i + 2] * by, acc[t][4 * i + 3] * by)};
         }
-      if (half == 0 && c.lse != nullptr)
+      if (part == 0 && c.lse != nullptr)
         c.lse[(size_t)row.token * c.Hq + row.head] = some ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
     }
   }
@@ -1106,7 +1133,7 @@ __device__ __forceinline__ void interleave() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// Heads up to 128 values.  Two waves share a SIMD, one of waves 0-3 and one of waves 4-7, and take turns at the matrix
+// Two waves share a SIMD, one of waves 0-3 and one of waves 4-7, and take turns at the matrix
 // pipe: in every slot one multiplies (o of the tile before, then the scores of this one: 32 MFMAs, 1024 cycles, with heads of
 // 128) while the other makes weights (about as long), waves 4-7 one slot behind.  A barrier ends a slot.
 //   Scores of tile b are made by waves 0-3 in slot 2 b and by waves 4-7 in slot 2 b + 1, o of it two slots later: its place in
@@ -1115,14 +1142,15 @@ __device__ __forceinline__ void interleave() {
 // barrier that ends slot 2 b + 1, after which waves 0-3 read it: later ones, of tile b + 2, may be outstanding.
 //   A causal prompt of 8192, 32 heads over 8 of 128: 530 us, 1040 TFLOP/s.  The matrix pipes are 55 % busy (LDS 29 %, no bank
 // conflicts), a slot about 1850 cycles, at a clock that the board's power lowers from 2.1 to 1.7 GHz; with four waves of 32
-// rows, one a SIMD, it took 722.  Heads of 64: half the products, as many exponentials: 355 us, pipes 33 % busy.
+// rows, one a SIMD, it took 722.  Heads of 64: half the products, as many exponentials: 355 us, pipes 33 % busy.  128 tokens
+// over 30000 keys, 32 heads over 4 of 256: 158 us, 800 TFLOP/s.
 template <int DP, bool FULL>
 __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void attn_pairs_kernel(AttnCall c) {
   using T = ManyTile<DP>;
-  constexpr int KS = T::KS, DT = T::DT, KT = T::KT;
+  constexpr int KS = T::KS, DT = T::DT, KT = T::KT, WT = T::WT;
   extern __shared__ __align__(256) unsigned char ring[];
   __shared__ ManyShared<DP> sh;
-  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), part = lane / T::R;
   const bool behind = wave >= 4;
   const uint32_t lds = lds_address(ring);
   const KeyRows rows(c);
@@ -1143,9 +1171,9 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
 #pragma unroll 1
   for (; walk.next(); walk.done()) {
     const Piece &p = walk.p;
-    const Row row = row_of(c, p, wave * 32 + (lane & 31));
+    const Row row = row_of(c, p, wave * T::R + lane % T::R);
     int all_lo, all_hi;
-    seen_by_all(c, p, c.by_heads(wave * 32), c.by_heads(wave * 32 + 31) + 1, all_lo, all_hi);
+    seen_by_all(c, p, c.by_heads(wave * T::R), c.by_heads(wave * T::R + T::R - 1) + 1, all_lo, all_hi);
     // tiles whose keys all rows see
     const int clear_from = uniform((max(all_lo - p.first, 0) + T::KEYS - 1) / T::KEYS), clear_to = uniform(max(all_hi - p.first, 0) / T::KEYS);
     TileLoads<DP, FULL> loads{rows, p, sh, c.table + (size_t)p.request * c.table_pitch, c.k + (size_t)p.kv * c.cache_head,
@@ -1157,8 +1185,8 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       q[s] = u32x4{0u, 0u, 0u, 0u};
-      if (row.valid && (FULL || 16 * s + 8 * half < c.D))
-        q[s] = *reinterpret_cast<const u32x4 *>(c.q + (size_t)row.token * c.q_row + (size_t)row.head * c.q_head + 16 * s + 8 * half);
+      if (row.valid && (FULL || T::STEP * s + 8 * part < c.D))
+        q[s] = *reinterpret_cast<const u32x4 *>(c.q + (size_t)row.token * c.q_row + (size_t)row.head * c.q_head + T::STEP * s + 8 * part);
     }
     if (p.b0 < p.b1) loads.fill(p.b0), loads.find(p.b0);
     RowState<DP> state;
@@ -1170,12 +1198,12 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
       wait_vmcnt<2 * T::DMAS>();
       barrier();
       if (behind) barrier();
-      f32x16 x[KT];
-      auto score = [&](const u32x4 (&k)[KS], f32x16 &to) {
+      typename T::Acc x[KT];
+      auto score = [&](const u32x4 (&k)[KS], typename T::Acc &to) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) to[i] = 0.f;
+        for (int i = 0; i < T::N; ++i) to[i] = 0.f;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) to = mfma32(k[s], q[s], to);
+        for (int s = 0; s < KS; ++s) to = many_mfma<DP>(k[s], q[s], to);
       };
 #pragma unroll
       for (int t = 0; t < KT; ++t) {
@@ -1190,7 +1218,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
         // weigh.  The wave that multiplies goes first: the other's instructions fill what it leaves (712 -> 693 us for a prompt
         // of 8192, together with the values' order).
         __builtin_amdgcn_s_setprio(0);
-        u32x4 v0[DT / 2][2 * KT], v1[DT / 2][2 * KT], w[2 * KT];
+        u32x4 v0[DT / 2][WT], v1[DT / 2][WT], w[WT];
         uint32_t bad0 = 0, bad1 = 0;
         if (loads.ever_bad) {
           bad0 = sh.bad_rows[b % 8][0], bad1 = sh.bad_rows[b % 8][1];
@@ -1201,18 +1229,18 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
         uint32_t stage = from.stage(b);
         const int odd = uniform(state.weigh(x, w, scale, masked, b, kb, row, bad0, bad1, from, lane) ? 1 : 0);
 #pragma unroll
-        for (int s = 0; s < 2 * KT; ++s) asm volatile("" : "+v"(w[s]), "+v"(state.l));  // made here: the scores' registers are free
+        for (int s = 0; s < WT; ++s) asm volatile("" : "+v"(w[s]), "+v"(state.l));  // made here: the scores' registers are free
         if (odd != 0) {
           // o of this tile here and now; the slot that is to come adds zeros
 #pragma unroll
           for (int t = 0; t < DT; ++t) {
-            u32x4 v[1][2 * KT];
+            u32x4 v[1][WT];
             from.values(stage, t, v);
             RowState<DP>::only_finite(v);
             state.multiply(v, w, t);
           }
 #pragma unroll
-          for (int s = 0; s < 2 * KT; ++s) w[s] = u32x4{0u, 0u, 0u, 0u};
+          for (int s = 0; s < WT; ++s) w[s] = u32x4{0u, 0u, 0u, 0u};
           stage = T::STAGES * T::STAGE - T::OPERAND;  // where zeros are, as a tile's values
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -1225,7 +1253,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
         if (b + 3 >= loads.plain_until) loads.prepare(b + 3);
         int id[T::PASSES];
         u32x4 k0[KS], k1[KS];
-        constexpr int HALF = DT * KT;  // matrix instructions of half of o
+        constexpr int HALF = DT / 2 * WT;  // matrix instructions of half of o
         loads.pages(id);
         from.values(stage, DT / 2, v1);
         state.multiply(v0, w, 0);
@@ -1244,84 +1272,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
       __builtin_amdgcn_s_setprio(0);
       if (!behind) barrier();
     }
-    state.finish(c, sh.walk, p, walk.share, row, me, wave * 32 + (lane & 31), half);
-    __syncthreads();
-  }
-}
-
-// Heads beyond 128 values, whose o and q fill half of a SIMD's registers: one wave each, tiles of 32 keys that are loaded
-// three ahead, values read from LDS while the weights are made.  A prompt of 4096, 16 heads over 8 of 256: 232 us, 590 TFLOP/s,
-// pipes 25 % busy: a wave has nobody to make weights beside its products.  Making the next tile's scores right after o, its
-// keys read meanwhile, took 250.
-template <int DP, bool FULL>
-__global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void attn_wide_kernel(AttnCall c) {
-  using T = ManyTile<DP>;
-  constexpr int KS = T::KS, DT = T::DT, KT = T::KT;
-  extern __shared__ __align__(256) unsigned char ring[];
-  __shared__ ManyShared<DP> sh;
-  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
-  const uint32_t lds = lds_address(ring);
-  const KeyRows rows(c);
-  const float scale = own_register(c.scale);
-  const Fragments<DP> from(lds, lane);
-  const int me = (int)xcd_remap(blockIdx.x, gridDim.x);
-
-  if (!FULL)
-    for (int i = threadIdx.x; i < T::STAGES * T::STAGE / 16; i += T::THREADS) reinterpret_cast<u32x4 *>(ring)[i] = u32x4{0u, 0u, 0u, 0u};
-
-  Walk<T::THREADS, false> walk(c, sh.walk, me, (int)gridDim.x);
-#pragma unroll 1
-  for (; walk.next(); walk.done()) {
-    const Piece &p = walk.p;
-    const Row row = row_of(c, p, wave * 32 + (lane & 31));
-    int all_lo, all_hi;
-    seen_by_all(c, p, c.by_heads(wave * 32), c.by_heads(wave * 32 + 31) + 1, all_lo, all_hi);
-    // tiles whose keys all rows see
-    const int clear_from = uniform((max(all_lo - p.first, 0) + T::KEYS - 1) / T::KEYS), clear_to = uniform(max(all_hi - p.first, 0) / T::KEYS);
-    TileLoads<DP, FULL> loads{rows, p, sh, c.table + (size_t)p.request * c.table_pitch, c.k + (size_t)p.kv * c.cache_head,
-                              c.v + (size_t)p.kv * c.cache_head, c.D, wave, lane, lds, sh.ids[wave]};
-    loads.ever_bad = false;
-    loads.step_pages = rows.page_of(T::KEYS), loads.step_rows = T::KEYS - loads.step_pages * rows.page;
-    if (threadIdx.x < 16) (&sh.bad_rows[0][0])[threadIdx.x] = 0u;
-    u32x4 q[KS];
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      q[s] = u32x4{0u, 0u, 0u, 0u};
-      if (row.valid && (FULL || 16 * s + 8 * half < c.D))
-        q[s] = *reinterpret_cast<const u32x4 *>(c.q + (size_t)row.token * c.q_row + (size_t)row.head * c.q_head + 16 * s + 8 * half);
-    }
-    if (p.b0 < p.b1) loads.fill(p.b0), loads.find(p.b0);
-    RowState<DP> state;
-    state.clear();
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): from here on only direct loads to LDS are counted
-    __syncthreads();
-    if (p.b0 < p.b1)
-      for (int i = 0; i < T::STAGES - 1; ++i) loads.all(p.b0 + i);
-#pragma unroll 1
-    for (int b = p.b0; b < p.b1; ++b) {
-      wait_vmcnt<(T::STAGES - 2) * T::DMAS>();
-      __syncthreads();  // tile b has landed, and nobody reads the one before any more
-      f32x16 x[KT];
-#pragma unroll
-      for (int t = 0; t < KT; ++t) {
-        u32x4 k[KS];
-        from.keys(b, t, k);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[t][i] = 0.f;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) x[t] = mfma32(k[s], q[s], x[t]);
-      }
-      u32x4 v[DT][2 * KT], w[2 * KT];
-      from.values(from.stage(b), 0, v);
-      const uint32_t bad0 = sh.bad_rows[b % 8][0], bad1 = sh.bad_rows[b % 8][KT - 1];
-      if (threadIdx.x < 2) sh.bad_rows[(b + T::STAGES) % 8][threadIdx.x] = 0u;
-      loads.all(b + T::STAGES - 1);
-      const int kb = p.first + b * T::KEYS;
-      const bool masked = b < clear_from || b >= clear_to || loads.ever_bad;
-      if (state.weigh(x, w, scale, masked, b, kb, row, bad0, bad1, from, lane)) RowState<DP>::only_finite(v);
-      state.multiply(v, w, 0);
-    }
-    state.finish(c, sh.walk, p, walk.share, row, me, wave * 32 + (lane & 31), half);
+    state.finish(c, sh.walk, p, walk.share, row, me, wave, lane);
     __syncthreads();
   }
 }
@@ -1334,8 +1285,7 @@ template <int DP, bool MANY, bool FULL>
 int launch(const AttnCall &c, int grid, hipStream_t s) {
   void (*fn)(AttnCall);
   if constexpr (!MANY) fn = attn_few_kernel<DP>;
-  else if constexpr (ManyTile<DP>::PAIRS) fn = attn_pairs_kernel<DP, FULL>;
-  else fn = attn_wide_kernel<DP, FULL>;
+  else fn = attn_pairs_kernel<DP, FULL>;
   constexpr int lds = MANY ? ManyTile<DP>::LDS : FewTile<DP>::WAVES * FewTile<DP>::WAVE_BYTES;
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return OCC_ENODEV;
@@ -1399,8 +1349,9 @@ int attn_launch(const occ_attn_args &a, hipStream_t s) {
     k.cut.parts = a.Hkv * k.groups;
     // Keys' worth of an item's beginning and end.  Many rows: 11 us (a piece's q, pages and first tiles, a masked tile, its
     // output), a tile of 64 keys 1.8 us; with 128 in place of 512 a prompt of 8192 took 682 us instead of 565, whose short
-    // items fell to few workgroups, and with 1024 570.  Few rows: 128 and 512 make 64 requests 1 % slower.
-    k.cut.fixed = many ? (DP <= 128 ? 512 : 256) : 256, k.cut.block = many ? many_keys(DP) : few_keys(DP);
+    // items fell to few workgroups, and with 1024 570.  Heads of 256: 384 (prompts of 4096 and 8192 212 and 354 us, with 256 231 and
+    // 383, with 768 217 and 361).  Few rows: 128 and 512 make 64 requests 1 % slower.
+    k.cut.fixed = many ? (DP <= 128 ? 512 : 384) : 256, k.cut.block = many ? many_keys(DP) : few_keys(DP);
     k.cut.window = a.window < c.keys ? a.window : 0, k.cut.causal = a.causal != 0;
     k.least = least, k.most = most;
     // (four chunks of 256 tokens: 57 us with 512 spare, 43 with 1024)
