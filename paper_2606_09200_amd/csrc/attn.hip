@@ -751,9 +751,9 @@ struct ManyTile {
   static constexpr int CH = DP / 8;                    // 16-byte chunks of a row
   static constexpr int PITCH = DP * 2;
   static constexpr int OPERAND = KEYS * PITCH;         // bytes of a tile of K, and of V
-  static constexpr int STAGES = 4, STAGE = 2 * OPERAND;
-  static constexpr int ZEROS = OPERAND;                // bytes of zeros behind the ring
-  static constexpr int LDS = STAGES * STAGE + ZEROS;
+  static constexpr int STAGES = 4;                     // of the ring of tiles of K, and of that of V
+  static constexpr int ZEROS = OPERAND;                // bytes of zeros behind the rings
+  static constexpr int LDS = 2 * STAGES * OPERAND + ZEROS;
   static constexpr int PASS_ROWS = THREADS / CH, PASSES = KEYS / PASS_ROWS;
   static constexpr int DMAS = 2 * PASSES;              // of a wave for a tile
   static constexpr int PART = ROWS * (DP + 2);
@@ -827,6 +827,7 @@ struct TileLoads {
   bool some_bad, ever_bad; // whether some page at hand, or of the item so far, is none
   // page and row within it of this thread's keys of the tile that is issued next
   int index[T::PASSES], off[T::PASSES], step_pages, step_rows;
+  uint64_t at_before[T::PASSES];  // of the tile before
 
   __device__ __forceinline__ int row(int i) const { return i * T::PASS_ROWS + (wave * 64 + lane) / T::CH; }
   __device__ __forceinline__ void find(int b) {
@@ -868,31 +869,34 @@ struct TileLoads {
       __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): there for the barrier
     }
   }
-  // The page numbers of tile b, then its loads, which are on their way after this; the stage's earlier tile has been
-  // read.  Past the last tile the last key is loaded, which nobody reads: every wave has as many loads in every slot.
+  // The page numbers of tile b, then the loads of its keys and of the values of the tile before, which are on their way after
+  // this; what the stages held has been read.  Past the last tile the last key is loaded, which nobody reads: every wave has
+  // as many loads in every interval.
   __device__ __forceinline__ void pages(int (&id)[T::PASSES]) const {
 #pragma unroll
     for (int i = 0; i < T::PASSES; ++i) id[i] = ids[index[i] - ids_from];
   }
-  __device__ __forceinline__ void issue(int b, const int (&id)[T::PASSES]) {
-    const uint32_t to = lds + (uint32_t)(b % T::STAGES) * T::STAGE + (uint32_t)wave * 1024u;
+  __device__ __forceinline__ void issue(int b, const int (&id)[T::PASSES], bool values = true) {
+    const uint32_t to = lds + (uint32_t)wave * 1024u;
+    const uint32_t to_k = to + (uint32_t)(b % T::STAGES) * T::OPERAND, to_v = to + (uint32_t)(T::STAGES + (b - 1 + T::STAGES) % T::STAGES) * T::OPERAND;
 #pragma unroll
     for (int i = 0; i < T::PASSES; ++i) {
       const int r = row(i), chunk = lane % T::CH;
       const uint64_t at = rows.at(id[i], off[i]);
       const int ck = many_swizzle_k<DP>(r, chunk), cv = many_swizzle_v<DP>(r, chunk);
-      if (FULL || 8 * ck < D) global_dma16(plus<uint16_t>(k + 8 * ck, at), to + (uint32_t)(i * T::THREADS * 16));
-      if (FULL || 8 * cv < D) global_dma16(plus<uint16_t>(v + 8 * cv, at), to + T::OPERAND + (uint32_t)(i * T::THREADS * 16));
+      if (FULL || 8 * ck < D) global_dma16(plus<uint16_t>(k + 8 * ck, at), to_k + (uint32_t)(i * T::THREADS * 16));
+      if (values && (FULL || 8 * cv < D)) global_dma16(plus<uint16_t>(v + 8 * cv, at_before[i]), to_v + (uint32_t)(i * T::THREADS * 16));
+      at_before[i] = at;
       index[i] += step_pages, off[i] += step_rows;
       const bool over = off[i] >= rows.page;
       off[i] -= over ? rows.page : 0, index[i] += over ? 1 : 0;
     }
   }
-  __device__ __forceinline__ void all(int b) {
+  __device__ __forceinline__ void all(int b, bool values = true) {
     int id[T::PASSES];
     if (b >= plain_until) prepare(b);
     pages(id);
-    issue(b, id);
+    issue(b, id, values);
   }
 };
 
@@ -904,19 +908,19 @@ struct Fragments {
   __device__ __forceinline__ Fragments(uint32_t lds, int lane) {
     const int row = lane % T::R, part = lane / T::R, l16 = lane & 15, r = 4 * part + (l16 >> 2);
     k0 = lds + (uint32_t)(row * T::PITCH + many_swizzle_k<DP>(row, part) * 16);
-    vt0 = lds + T::OPERAND;
+    vt0 = lds + T::STAGES * T::OPERAND;
     v0 = vt0 + r * T::PITCH + many_swizzle_v<DP>(r, 2 * (row >> 4) + ((l16 & 3) >> 1)) * 16 + 8 * (l16 & 1);
   }
   // Key R t + l % R, values STEP s + 8 (l / R) .. + 7.
   __device__ __forceinline__ void keys(int b, int t, u32x4 (&k)[T::KS]) const {
     constexpr int IN = 16 / T::P;  // steps in 256 bytes
-    const uint32_t from = k0 + (uint32_t)(b % T::STAGES) * T::STAGE;
+    const uint32_t from = k0 + stage(b);
 #pragma unroll
     for (int s = 0; s < T::KS; ++s)
       k[s] = *(__attribute__((address_space(3))) const u32x4 *)(size_t)((from ^ ((s % IN) * 16 * T::P)) + (s / IN) * 256 + T::R * t * T::PITCH);
   }
   // Values R (t0 + t) + l % R of the 8 keys of STEP s .. that the lane's weights are of.
-  __device__ __forceinline__ uint32_t stage(int b) const { return (uint32_t)(b % T::STAGES) * T::STAGE; }
+  __device__ __forceinline__ uint32_t stage(int b) const { return (uint32_t)(b % T::STAGES) * T::OPERAND; }
   template <int N>
   __device__ __forceinline__ void values(uint32_t stage, int t0, u32x4 (&v)[N][T::WT]) const {
     constexpr int IN = 128 / T::R;  // tiles of values in 256 bytes
@@ -952,7 +956,7 @@ struct RowState {
   __device__ __forceinline__ bool weigh(Acc (&x)[T::KT], u32x4 (&w)[T::WT], float scale, bool masked, int b, int kb, const Row &row,
                                         uint32_t bad0, uint32_t bad1, const Fragments<DP> &from, int lane) {
     const int part = lane / T::R;
-    const uint32_t vt0 = from.vt0 + (uint32_t)(b % T::STAGES) * T::STAGE;
+    const uint32_t vt0 = from.vt0 + from.stage(b);
     bool odd = false;
     if (masked) {
       // a lane's scores are of keys R t + 4 P (i / 4) + 4 part + i % 4
@@ -1133,13 +1137,13 @@ __device__ __forceinline__ void interleave() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// Two waves share a SIMD, one of waves 0-3 and one of waves 4-7, and take turns at the matrix
-// pipe: in every slot one multiplies (o of the tile before, then the scores of this one: 32 MFMAs, 1024 cycles, with heads of
-// 128) while the other makes weights (about as long), waves 4-7 one slot behind.  A barrier ends a slot.
-//   Scores of tile b are made by waves 0-3 in slot 2 b and by waves 4-7 in slot 2 b + 1, o of it two slots later: its place in
-// the ring is free from slot 2 b + 4 on.  All waves ask for their part of tile b + 3 in the slot that has scores of
-// tile b + 1 (2 b + 2, 2 b + 3), in the time that the matrix instructions leave.  Each waits for its loads of tile b + 1 before the
-// barrier that ends slot 2 b + 1, after which waves 0-3 read it: later ones, of tile b + 2, may be outstanding.
+// Two waves share a SIMD, one of waves 0-3 and one of waves 4-7, and take turns at the matrix pipe: each makes a tile's
+// weights and then multiplies (o of the tile, then the scores of the next one: 32 MFMAs, 1024 cycles, with heads of 128), and one
+// barrier a tile, which waves 0-3 have after multiplying and waves 4-7 after the weights, keeps them half a tile apart.
+//   In interval b, between two barriers, waves 0-3 make weights of tile b and o of it and scores of b + 1, waves 4-7 o of
+// b - 1, scores of b and weights of b: keys of b and b + 1 are read, values of b - 1 and b.  All ask for keys of
+// b + 3 and values of b + 2, whose stages (of b - 1 and b - 2) nobody reads, in the time that the matrix instructions
+// leave, and before the barrier wait for what they asked for in the interval before: it is read from the next on.
 //   A causal prompt of 8192, 32 heads over 8 of 128: 530 us, 1040 TFLOP/s.  The matrix pipes are 55 % busy (LDS 29 %, no bank
 // conflicts), a slot about 1850 cycles, at a clock that the board's power lowers from 2.1 to 1.7 GHz; with four waves of 32
 // rows, one a SIMD, it took 722.  Heads of 64: half the products, as many exponentials: 355 us, pipes 33 % busy.  128 tokens
@@ -1159,7 +1163,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
   const int me = (int)xcd_remap(blockIdx.x, gridDim.x);
 
   // chunks that the heads do not have stay zero, and what lies behind the ring
-  for (int i = (FULL ? T::STAGES * T::STAGE / 16 : 0) + threadIdx.x; i < T::LDS / 16; i += T::THREADS)
+  for (int i = (FULL ? 2 * T::STAGES * T::OPERAND / 16 : 0) + threadIdx.x; i < T::LDS / 16; i += T::THREADS)
     reinterpret_cast<u32x4 *>(ring)[i] = u32x4{0u, 0u, 0u, 0u};
   auto barrier = [&]() {  // nothing moves across it
     __builtin_amdgcn_sched_barrier(0);
@@ -1194,10 +1198,9 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): from here on only direct loads to LDS are counted
     __syncthreads();
     if (p.b0 < p.b1) {
-      for (int i = 0; i < 3; ++i) loads.all(p.b0 + i);
+      for (int i = 0; i < 3; ++i) loads.all(p.b0 + i, i > 0);
       wait_vmcnt<2 * T::DMAS>();
       barrier();
-      if (behind) barrier();
       typename T::Acc x[KT];
       auto score = [&](const u32x4 (&k)[KS], typename T::Acc &to) {
 #pragma unroll
@@ -1211,8 +1214,10 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
         from.keys(p.b0, t, k);
         score(k, x[t]);
       }
-      if (behind) wait_vmcnt<T::DMAS>();
+      wait_vmcnt<T::DMAS>();
       barrier();
+      if (behind) loads.all(p.b0 + 3);
+      const int ahead = behind ? 4 : 3;
 #pragma unroll 1
       for (int b = p.b0; b < p.b1; ++b) {
         // weigh.  The wave that multiplies goes first: the other's instructions fill what it leaves (712 -> 693 us for a prompt
@@ -1241,16 +1246,15 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
           }
 #pragma unroll
           for (int s = 0; s < WT; ++s) w[s] = u32x4{0u, 0u, 0u, 0u};
-          stage = T::STAGES * T::STAGE - T::OPERAND;  // where zeros are, as a tile's values
+          stage = T::STAGES * T::OPERAND;  // where zeros are, as a tile's values
         }
         __builtin_amdgcn_sched_barrier(0);
         from.values(stage, 0, v0);
-        if (!behind) wait_vmcnt<T::DMAS>();
-        barrier();
+        if (behind) wait_vmcnt<T::DMAS>(), barrier();
         // multiply: o, then the next tile's scores (past the last tile they are not used).  Each part's operands are read
         // while the part before runs: no more than two at a time have registers.
         __builtin_amdgcn_s_setprio(1);
-        if (b + 3 >= loads.plain_until) loads.prepare(b + 3);
+        if (b + ahead >= loads.plain_until) loads.prepare(b + ahead);
         int id[T::PASSES];
         u32x4 k0[KS], k1[KS];
         constexpr int HALF = DT / 2 * WT;  // matrix instructions of half of o
@@ -1259,18 +1263,16 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
         state.multiply(v0, w, 0);
         interleave<HALF, 2, 0>();
         from.keys(b + 1, 0, k0);
-        loads.issue(b + 3, id);
+        loads.issue(b + ahead, id);
         state.multiply(v1, w, DT / 2);
         interleave<HALF, KS / HALF, 6>();
         from.keys(b + 1, 1, k1);
         score(k0, x[0]);
         interleave<KS, 1, 0>();
         score(k1, x[1]);
-        if (behind) wait_vmcnt<T::DMAS>();
-        barrier();
+        if (!behind) wait_vmcnt<T::DMAS>(), barrier();
       }
       __builtin_amdgcn_s_setprio(0);
-      if (!behind) barrier();
     }
     state.finish(c, sh.walk, p, walk.share, row, me, wave, lane);
     __syncthreads();
