@@ -825,9 +825,10 @@ struct TileLoads {
   int32_t *ids;
   int ids_from, plain_until;
   bool some_bad, ever_bad; // whether some page at hand, or of the item so far, is none
-  // page and row within it of this thread's keys of the tile that is issued next
+  // page and row within it of this thread's keys of the tile that is issued next; where such a row of page 0 is, and how
+  // far its values are from there; the keys of the tile before
   int index[T::PASSES], off[T::PASSES], step_pages, step_rows;
-  uint64_t at_before[T::PASSES];  // of the tile before
+  uint64_t base[T::PASSES], to_values, before[T::PASSES];
 
   __device__ __forceinline__ int row(int i) const { return i * T::PASS_ROWS + (wave * 64 + lane) / T::CH; }
   __device__ __forceinline__ void find(int b) {
@@ -835,6 +836,30 @@ struct TileLoads {
     for (int i = 0; i < T::PASSES; ++i) {
       const int key = min(p.first + b * T::KEYS + row(i), p.last - 1);
       index[i] = rows.page_of(key), off[i] = key - index[i] * rows.page;
+      place(i);
+    }
+  }
+  // A thread's chunks of K and of V are the same ones in all its rows.
+  static_assert(T::PASS_ROWS % 16 == 0, "");
+  __device__ __forceinline__ int chunk_k() const { return many_swizzle_k<DP>(row(0), lane % T::CH); }
+  __device__ __forceinline__ int chunk_v() const { return many_swizzle_v<DP>(row(0), lane % T::CH); }
+  __device__ __forceinline__ void place(int i) {
+    base[i] = (uint64_t)(size_t)(k + 8 * chunk_k()) + (uint64_t)(uint32_t)off[i] * rows.row_bytes;
+  }
+  __device__ __forceinline__ void start(int b) {
+    step_pages = rows.page_of(T::KEYS), step_rows = T::KEYS - step_pages * rows.page;
+    to_values = (uint64_t)(size_t)(v + 8 * chunk_v()) - (uint64_t)(size_t)(k + 8 * chunk_k());
+    fill(b), find(b);
+  }
+  // Rows of the next tile; in pages that a tile is a whole number of they stay (2 to 4 % of a prompt's time).
+  __device__ __forceinline__ void advance() {
+    if (step_rows == 0) return;
+#pragma unroll
+    for (int i = 0; i < T::PASSES; ++i) {
+      off[i] += step_rows;
+      const bool over = off[i] >= rows.page;
+      off[i] -= over ? rows.page : 0, index[i] += over ? 1 : 0;
+      place(i);
     }
   }
   __device__ __forceinline__ void fill(int b) {  // page numbers from tile b's first on
@@ -881,15 +906,12 @@ struct TileLoads {
     const uint32_t to_k = to + (uint32_t)(b % T::STAGES) * T::OPERAND, to_v = to + (uint32_t)(T::STAGES + (b - 1 + T::STAGES) % T::STAGES) * T::OPERAND;
 #pragma unroll
     for (int i = 0; i < T::PASSES; ++i) {
-      const int r = row(i), chunk = lane % T::CH;
-      const uint64_t at = rows.at(id[i], off[i]);
-      const int ck = many_swizzle_k<DP>(r, chunk), cv = many_swizzle_v<DP>(r, chunk);
-      if (FULL || 8 * ck < D) global_dma16(plus<uint16_t>(k + 8 * ck, at), to_k + (uint32_t)(i * T::THREADS * 16));
-      if (values && (FULL || 8 * cv < D)) global_dma16(plus<uint16_t>(v + 8 * cv, at_before[i]), to_v + (uint32_t)(i * T::THREADS * 16));
-      at_before[i] = at;
-      index[i] += step_pages, off[i] += step_rows;
-      const bool over = off[i] >= rows.page;
-      off[i] -= over ? rows.page : 0, index[i] += over ? 1 : 0;
+      const uint64_t at = (uint64_t)(rows.bad(id[i]) ? 0u : (uint32_t)id[i]) * rows.page_bytes + base[i];
+      if (FULL || 8 * chunk_k() < D) global_dma16(reinterpret_cast<const void *>(at), to_k + (uint32_t)(i * T::THREADS * 16));
+      if (values && (FULL || 8 * chunk_v() < D))
+        global_dma16(reinterpret_cast<const void *>(before[i] + to_values), to_v + (uint32_t)(i * T::THREADS * 16));
+      before[i] = at;
+      index[i] += step_pages;
     }
   }
   __device__ __forceinline__ void all(int b, bool values = true) {
@@ -897,6 +919,7 @@ struct TileLoads {
     if (b >= plain_until) prepare(b);
     pages(id);
     issue(b, id, values);
+    advance();
   }
 };
 
@@ -1183,7 +1206,6 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
     TileLoads<DP, FULL> loads{rows, p, sh, c.table + (size_t)p.request * c.table_pitch, c.k + (size_t)p.kv * c.cache_head,
                               c.v + (size_t)p.kv * c.cache_head, c.D, wave, lane, lds, sh.ids[wave]};
     loads.ever_bad = false;
-    loads.step_pages = rows.page_of(T::KEYS), loads.step_rows = T::KEYS - loads.step_pages * rows.page;
     if (threadIdx.x < 16) (&sh.bad_rows[0][0])[threadIdx.x] = 0u;
     u32x4 q[KS];
 #pragma unroll
@@ -1192,7 +1214,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
       if (row.valid && (FULL || T::STEP * s + 8 * part < c.D))
         q[s] = *reinterpret_cast<const u32x4 *>(c.q + (size_t)row.token * c.q_row + (size_t)row.head * c.q_head + T::STEP * s + 8 * part);
     }
-    if (p.b0 < p.b1) loads.fill(p.b0), loads.find(p.b0);
+    if (p.b0 < p.b1) loads.start(p.b0);
     RowState<DP> state;
     state.clear();
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): from here on only direct loads to LDS are counted
@@ -1271,6 +1293,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
         interleave<KS, 1, 0>();
         score(k1, x[1]);
         if (!behind) wait_vmcnt<T::DMAS>(), barrier();
+        loads.advance();
       }
       __builtin_amdgcn_s_setprio(0);
     }
