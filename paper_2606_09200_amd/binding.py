@@ -852,9 +852,12 @@ def occ_moe(x, router, w_gate, w_up, w_down, y, *, top_k, workspace, ids=None, w
 
 # ------------------------------------------------------------------ a paged cache and its attention
 
+_INT32 = torch.int32
+
+
 def _int_param(name, t, shape):
     """Address of a contiguous int32 GPU tensor of that shape."""
-    if t.dtype != torch.int32 or not t.is_cuda or t.shape != shape or not t.is_contiguous():
+    if t.dtype is not _INT32 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
         raise ValueError("%s must be a contiguous int32 GPU tensor of shape %s" % (name, tuple(shape)))
     return t.data_ptr()
 
@@ -905,21 +908,23 @@ def rope_turns(pairs, base=10000.0, *, linear=1.0, bands=None, device="cuda"):
     return torch.tensor(values, dtype=torch.int64, device=device)
 
 
-def _heads_arg(name, t, dtype, rows, heads, D):
-    """(address, row pitch, head pitch) of a (rows, heads, D) tensor whose heads are contiguous."""
-    if t.dtype != dtype or not t.is_cuda or t.shape != (rows, heads, D):
-        raise ValueError("%s must be a %s GPU tensor of shape (%d, %d, %d)" % (name, dtype, rows, heads, D))
+def _heads_arg(name, t, dtype, shape):
+    """(address, row pitch, head pitch) of a tensor of that shape (rows, heads, D) whose heads are contiguous."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
+        raise ValueError("%s must be a %s GPU tensor of shape %s" % (name, dtype, tuple(shape)))
     row, head, one = t.stride()
-    if D > 1 and one != 1:
+    rows, heads, D = shape
+    if one != 1 and D > 1:
         raise ValueError("%s must have contiguous heads" % name)
     # a dimension of one has any stride
-    head = head if heads > 1 else D
+    if heads == 1:
+        head = D
     return t.data_ptr(), row if rows > 1 else heads * head, head
 
 
 def _cache_arg(k_cache, v_cache, dtype, heads, D):
     """(addresses, pages, page, pitches) of two caches (pages, page, heads, D) of the same strides."""
-    if k_cache.dtype != dtype or v_cache.dtype != dtype or not k_cache.is_cuda or not v_cache.is_cuda:
+    if k_cache.dtype is not dtype or v_cache.dtype is not dtype or not k_cache.is_cuda or not v_cache.is_cuda:
         raise ValueError("k_cache and v_cache must be %s GPU tensors" % dtype)
     shape, strides = k_cache.shape, k_cache.stride()
     if len(shape) != 4 or shape[2] != heads or shape[3] != D or v_cache.shape != shape:
@@ -940,41 +945,47 @@ def occ_rope(q, k, positions, turns, *, q_out=None, k_out=None, interleaved=Fals
     inverse: the other way, the gradient.  q_out and k_out: where to, None for in place -- but with k_cache and v_cache
     (pages, page, Hkv, D), into whose slots (rows, int32) the turned k and v go, no k_out is written for None.
     bf16 or fp32.  Returns (q_out, k_out)."""
-    some = q if q is not None else k
-    if some is None or some.dim() != 3:
+    some = k if q is None else q
+    shape = () if some is None else some.shape
+    if len(shape) != 3:
         raise ValueError("q or k must be given, (rows, heads, D)")
-    dtype, (rows, _, D) = some.dtype, some.shape
+    dtype, (rows, _, D) = some.dtype, shape
     kind = _float_type("q or k", some)
-    if turns.dim() != 1 or turns.dtype != torch.int64 or not turns.is_cuda or not turns.is_contiguous():
+    turns_shape = turns.shape
+    if len(turns_shape) != 1 or turns.dtype is not torch.int64 or not turns.is_cuda or not turns.is_contiguous():
         raise ValueError("turns must be a contiguous int64 GPU tensor of one dimension")
     Hq = Hkv = q_ptr = q_row = q_head = qo_ptr = qo_row = qo_head = 0
     k_ptr = k_row = k_head = ko_ptr = ko_row = ko_head = v_ptr = v_row = v_head = 0
     kc = vc = pages = page = by_page = by_row = by_head = s_ptr = 0
     if q is not None:
-        Hq = q.shape[1]
-        q_out = q if q_out is None else q_out
-        q_ptr, q_row, q_head = _heads_arg("q", q, dtype, rows, Hq, D)
-        qo_ptr, qo_row, qo_head = _heads_arg("q_out", q_out, dtype, rows, Hq, D)
+        Hq = shape[1]
+        qo_ptr, qo_row, qo_head = q_ptr, q_row, q_head = _heads_arg("q", q, dtype, shape)
+        if q_out is None:
+            q_out = q
+        else:
+            qo_ptr, qo_row, qo_head = _heads_arg("q_out", q_out, dtype, shape)
     elif q_out is not None:
         raise ValueError("q_out needs q")
     if k is not None:
-        if k.dim() != 3:
+        k_shape = k.shape
+        if len(k_shape) != 3:
             raise ValueError("k must have shape (rows, heads, D)")
-        Hkv = k.shape[1]
-        if k_out is None and k_cache is None:
-            k_out = k
-        k_ptr, k_row, k_head = _heads_arg("k", k, dtype, rows, Hkv, D)
+        Hkv = k_shape[1]
+        k_ptr, k_row, k_head = _heads_arg("k", k, dtype, (rows, Hkv, D))
         if k_out is not None:
-            ko_ptr, ko_row, ko_head = _heads_arg("k_out", k_out, dtype, rows, Hkv, D)
+            ko_ptr, ko_row, ko_head = _heads_arg("k_out", k_out, dtype, k_shape)
+        elif k_cache is None:
+            k_out = k
+            ko_ptr, ko_row, ko_head = k_ptr, k_row, k_head
     elif k_out is not None:
         raise ValueError("k_out needs k")
     if k_cache is not None or v_cache is not None or v is not None or slots is not None:
         if k is None or v is None or k_cache is None or v_cache is None or slots is None:
             raise ValueError("a cache needs k, v, k_cache, v_cache and slots")
-        v_ptr, v_row, v_head = _heads_arg("v", v, dtype, rows, Hkv, D)
+        v_ptr, v_row, v_head = _heads_arg("v", v, dtype, k_shape)
         kc, vc, pages, page, by_page, by_row, by_head = _cache_arg(k_cache, v_cache, dtype, Hkv, D)
         s_ptr = _int_param("slots", slots, (rows,))
-    a = _pack_rope.pack(rows, Hq, Hkv, D, turns.shape[0], kind, 1 if interleaved else 0, 1 if inverse else 0, page, pages, scale,
+    a = _pack_rope.pack(rows, Hq, Hkv, D, turns_shape[0], kind, 1 if interleaved else 0, 1 if inverse else 0, page, pages, scale,
                         q_ptr, k_ptr, v_ptr, qo_ptr, ko_ptr, kc, vc, _int_param("positions", positions, (rows,)), s_ptr,
                         turns.data_ptr(), q_row, q_head, k_row, k_head, v_row, v_head, qo_row, qo_head, ko_row, ko_head,
                         by_page, by_row, by_head)
@@ -996,12 +1007,13 @@ def occ_attn_paged(q, k_cache, v_cache, table, starts, lens, out, *, max_fresh, 
     D), its last row being its last key's.  scale: D^-0.5 if None.  window: keys a row sees at most, 0 for all.
     max_fresh: the most rows a request has (for the choice of kernels).  lse (rows, Hq, fp32) receives the log of
     each row's sum.  workspace: a GPU tensor zeroed once.  Rows of no request are left alone.  Returns out."""
-    if q.dim() != 3:
+    shape = q.shape
+    if len(shape) != 3:
         raise ValueError("q must have shape (rows, heads, D)")
-    rows, Hq, D = q.shape
+    rows, Hq, D = shape
     bf16 = torch.bfloat16
-    q_ptr, q_row, q_head = _heads_arg("q", q, bf16, rows, Hq, D)
-    o_ptr, o_row, o_head = _heads_arg("out", out, bf16, rows, Hq, D)
+    q_ptr, q_row, q_head = _heads_arg("q", q, bf16, shape)
+    o_ptr, o_row, o_head = _heads_arg("out", out, bf16, shape)
     if k_cache.dim() != 4:
         raise ValueError("k_cache must have shape (pages, page, heads, D)")
     Hkv = k_cache.shape[2]
