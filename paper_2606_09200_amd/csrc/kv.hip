@@ -219,7 +219,7 @@ __global__ __launch_bounds__(kThreads) void kv_tables_kernel(TablesCall c) {
 // for pair i of a head.  turns is a 64-bit fraction of a turn, so that position * turns modulo 2^64 is the exact
 // remainder of the angle, however far the position.  A workgroup makes its tokens' cosines and sines once, in LDS, and
 // passes over their heads: bound by reading and writing q, k and v once.  8192 tokens, 64 heads over 8 of 128, into the cache:
-// 76 us, 4.4 TB/s (a copy 4.95); 16 tokens 3.4 us.
+// 50 us, 6.7 TB/s, the inputs partly in the last cache (a copy of 2 GiB 4.95); 16 tokens 3.4 us.
 struct RopeCall {
   int T, Hq, Hkv, D, half, interleaved;
   const void *q, *k, *v;
@@ -253,6 +253,7 @@ struct Piece {
       for (int i = 0; i < N; ++i) x[i] = v[i];
     }
   }
+  template <bool STREAM>
   __device__ static __forceinline__ void store(E *p, const E (&x)[N]) {
     if constexpr (N == 1) {
       *p = x[0];
@@ -260,56 +261,38 @@ struct Piece {
       V v;
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] = x[i];
-      *reinterpret_cast<V *>(p) = v;
+      if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<V *>(p));
+      else *reinterpret_cast<V *>(p) = v;
     }
   }
 };
 
-template <class E, int PAIRS>
-__global__ __launch_bounds__(kThreads) void rope_kernel(RopeCall c) {
-  extern __shared__ __align__(16) float2 angles[];  // [token][pair]: (cos, sin), scaled
-  const int t0 = blockIdx.x * c.tokens, tokens = min(c.tokens, c.T - t0);
-  for (int i = threadIdx.x; i < tokens * c.half; i += kThreads) {
-    const int t = i / c.half, pair = i - t * c.half;
-    const int64_t phase = (int64_t)((uint64_t)(int64_t)c.positions[t0 + t] * (uint64_t)c.turns[pair]);
-    float s, co;
-    sincospif((float)phase * 0x1p-63f, &s, &co);
-    angles[i] = float2{co * c.scale, s * c.scale * c.sign};
-  }
-  __syncthreads();
-  const int stride = kThreads * gridDim.y;
-  for (int e = blockIdx.y * kThreads + threadIdx.x; e < tokens * c.per_token; e += stride) {
-    const int t = c.by_item(e), in = e - t * c.per_token;
-    const int h = c.by_chunk(in), piece = in - h * c.per_head;
+// An item: a piece of a head of a token, of q, of k or (past both) of v.
+template <class E, int PAIRS, bool STREAM>
+struct RopeItem {
+  int t, h, first, a0, a1;  // first: of its pairs; a0, a1: elements
+  bool turned;
+  E x[2][PAIRS];
+  __device__ __forceinline__ void load(const RopeCall &c, int t0, int e) {
+    t = c.by_item(e);
+    const int in = e - t * c.per_token;
+    h = c.by_chunk(in);
+    first = (in - h * c.per_head) * PAIRS;
     const size_t token = (size_t)(t0 + t);
-    // the caches' row, where the token has one
-    const int slot = c.slots != nullptr && h >= c.Hq ? c.slots[token] : -1;
-    const bool kept = slot >= 0 && slot < c.slots_end;
-    const int index = kept ? c.by_page(slot) : 0;
-    const size_t row = (size_t)index * c.cache_page + (size_t)(slot - index * c.page) * c.cache_row;
-    // elements of a piece: pairs of the turned part, then plain ones
-    const int first = piece * PAIRS;
-    const bool turned = first < c.half;
-    const int a0 = turned && !c.interleaved ? first : 2 * first;
-    const int a1 = turned && !c.interleaved ? first + c.half : 2 * first + PAIRS;
-    E x[2][PAIRS], y[2][PAIRS];
-    if (h >= c.Hq + c.Hkv) {
-      if (!kept) continue;
-      const int head = h - c.Hq - c.Hkv;
-      const E *from = static_cast<const E *>(c.v) + token * c.v_row + (size_t)head * c.v_head + 2 * first;
-      E *to = static_cast<E *>(c.v_cache) + row + (size_t)head * c.cache_head + 2 * first;
-      Piece<E, PAIRS>::load(from, x[0]);
-      Piece<E, PAIRS>::load(from + PAIRS, x[1]);
-      Piece<E, PAIRS>::store(to, x[0]);
-      Piece<E, PAIRS>::store(to + PAIRS, x[1]);
-      continue;
-    }
-    const bool key = h >= c.Hq;
-    const int head = key ? h - c.Hq : h;
-    const E *from = key ? static_cast<const E *>(c.k) + token * c.k_row + (size_t)head * c.k_head
-                        : static_cast<const E *>(c.q) + token * c.q_row + (size_t)head * c.q_head;
+    // pairs of the turned part, then plain ones
+    const bool plain = h >= c.Hq + c.Hkv;
+    turned = !plain && first < c.half;
+    a0 = turned && !c.interleaved ? first : 2 * first;
+    a1 = turned && !c.interleaved ? first + c.half : 2 * first + PAIRS;
+    const E *from = plain ? static_cast<const E *>(c.v) + token * c.v_row + (size_t)(h - c.Hq - c.Hkv) * c.v_head
+                  : h >= c.Hq ? static_cast<const E *>(c.k) + token * c.k_row + (size_t)(h - c.Hq) * c.k_head
+                              : static_cast<const E *>(c.q) + token * c.q_row + (size_t)h * c.q_head;
     Piece<E, PAIRS>::load(from + a0, x[0]);
     Piece<E, PAIRS>::load(from + a1, x[1]);
+  }
+  __device__ __forceinline__ void turn_and_store(const RopeCall &c, int t0, const float2 *angles) {
+    const size_t token = (size_t)(t0 + t);
+    E y[2][PAIRS];
     if (turned) {
       const float2 *cs = angles + t * c.half + first;
 #pragma unroll
@@ -330,16 +313,44 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeCall c) {
 #pragma unroll
       for (int i = 0; i < PAIRS; ++i) y[0][i] = x[0][i], y[1][i] = x[1][i];
     }
-    auto put = [&](E *to) {
-      Piece<E, PAIRS>::store(to + a0, y[0]);
-      Piece<E, PAIRS>::store(to + a1, y[1]);
+    auto put = [&](void *rows, size_t at) {
+      E *to = static_cast<E *>(rows) + at;
+      Piece<E, PAIRS>::template store<STREAM>(to + a0, y[0]);
+      Piece<E, PAIRS>::template store<STREAM>(to + a1, y[1]);
     };
-    if (!key) {
-      put(static_cast<E *>(c.q_out) + token * c.qo_row + (size_t)head * c.qo_head);
-    } else {
-      if (c.k_out != nullptr) put(static_cast<E *>(c.k_out) + token * c.ko_row + (size_t)head * c.ko_head);
-      if (kept) put(static_cast<E *>(c.k_cache) + row + (size_t)head * c.cache_head);
+    if (h < c.Hq) {
+      put(c.q_out, token * c.qo_row + (size_t)h * c.qo_head);
+      return;
     }
+    const bool key = h < c.Hq + c.Hkv;
+    const int head = h - c.Hq - (key ? 0 : c.Hkv);
+    if (key && c.k_out != nullptr) put(c.k_out, token * c.ko_row + (size_t)head * c.ko_head);
+    // the caches' row, where the token has one
+    const int slot = c.slots != nullptr ? c.slots[token] : -1;
+    if (slot < 0 || slot >= c.slots_end) return;
+    const int index = c.by_page(slot);
+    put(key ? c.k_cache : c.v_cache,
+        (size_t)index * c.cache_page + (size_t)(slot - index * c.page) * c.cache_row + (size_t)head * c.cache_head);
+  }
+};
+
+template <class E, int PAIRS, bool STREAM>
+__global__ __launch_bounds__(512) void rope_kernel(RopeCall c) {
+  extern __shared__ __align__(16) float2 angles[];  // [token][pair]: (cos, sin), scaled
+  const int t0 = blockIdx.x * c.tokens, tokens = min(c.tokens, c.T - t0), all = tokens * c.per_token;
+  const int stride = blockDim.x * gridDim.y;
+  for (int i = threadIdx.x; i < tokens * c.half; i += blockDim.x) {
+    const int t = i / c.half, pair = i - t * c.half;
+    const int64_t phase = (int64_t)((uint64_t)(int64_t)c.positions[t0 + t] * (uint64_t)c.turns[pair]);
+    float s, co;
+    sincospif((float)phase * 0x1p-63f, &s, &co);
+    angles[i] = float2{co * c.scale, s * c.scale * c.sign};
+  }
+  __syncthreads();
+  for (int e = blockIdx.y * blockDim.x + threadIdx.x; e < all; e += stride) {
+    RopeItem<E, PAIRS, STREAM> item;
+    item.load(c, t0, e);
+    item.turn_and_store(c, t0, angles);
   }
 }
 
@@ -394,17 +405,24 @@ int rope_launch(const occ_rope_args &a, hipStream_t s) {
     return a.D % 2 == 0 && all % n == 0 && at % bytes == 0;
   };
   const int pairs = elem == 2 ? (fits(8) ? 8 : fits(4) ? 4 : 1) : (fits(4) ? 4 : 1);
-  RopeFn fn = elem == 2 ? (pairs == 8 ? rope_kernel<uint16_t, 8> : pairs == 4 ? rope_kernel<uint16_t, 4> : rope_kernel<uint16_t, 1>)
-                        : (pairs == 4 ? rope_kernel<float, 4> : rope_kernel<float, 1>);
   c.per_head = a.D / 2 / pairs;
   c.per_token = c.per_head * (Hq + Hkv + (cache ? Hkv : 0));
   c.by_item = Divider(c.per_token), c.by_chunk = Divider(c.per_head);
-  // several tokens share a workgroup where there are plenty, a token's heads are dealt out where there are few
-  c.tokens = a.rows >= 4 * 4 * di->num_cus ? 4 : 1;
-  const int x = (a.rows + c.tokens - 1) / c.tokens;
-  const int passes = (int)(((int64_t)c.tokens * c.per_token + kThreads - 1) / kThreads);
+  // A token a workgroup, an item or two a thread, where there are plenty of tokens (several tokens where they have few
+  // items), dealt out among workgroups where there are few.  More than the L2s hold is stored past them.  8192 tokens, 64
+  // heads over 8 of 128: 77 us with four tokens a workgroup of 256 threads and ordinary stores, 62 with one, 50 past the L2s.
+  const bool plenty = a.rows >= di->num_cus;
+  const int threads = plenty ? std::min(512, (c.per_token + 63) / 64 * 64) : kThreads;
+  c.tokens = a.rows >= 16 * di->num_cus ? std::max(1, kThreads / c.per_token) : 1;
+  const int64_t items = (int64_t)c.tokens * c.per_token;
+  const int block = c.tokens > 1 ? kThreads : threads;
+  const bool stream = (int64_t)a.rows * c.per_token * 2 * pairs * elem > (32 << 20);
+  RopeFn fn = elem == 2 ? (pairs == 8 ? (stream ? rope_kernel<uint16_t, 8, true> : rope_kernel<uint16_t, 8, false>)
+                           : pairs == 4 ? rope_kernel<uint16_t, 4, false> : rope_kernel<uint16_t, 1, false>)
+                        : (pairs == 4 ? (stream ? rope_kernel<float, 4, true> : rope_kernel<float, 4, false>) : rope_kernel<float, 1, false>);
+  const int x = (a.rows + c.tokens - 1) / c.tokens, passes = (int)((items + block - 1) / block);
   const int y = std::max(1, std::min({passes, 4 * di->num_cus / x, 64}));
-  hipLaunchKernelGGL(fn, dim3(x, y), dim3(kThreads), (size_t)c.tokens * c.half * sizeof(float2), s, c);
+  hipLaunchKernelGGL(fn, dim3(x, y), dim3(block), (size_t)c.tokens * c.half * sizeof(float2), s, c);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
 }
 

@@ -216,6 +216,28 @@ def test_rope_many_rows_is_row_by_row():
         assert torch.equal(x, qo[a:b]) and torch.equal(y, ko[a:b])
 
 
+@pytest.mark.parametrize("rows,Hq,Hkv,D,dtype", [(255, 20, 4, 80, BF16), (256, 20, 4, 80, BF16), (257, 64, 8, 128, BF16), (4500, 32, 8, 128, BF16),
+                                                 (3000, 32, 8, 96, torch.float32)])
+def test_rope_by_launches(rows, Hq, Hkv, D, dtype):
+    """Workgroups of other sizes, and outputs larger than the L2s hold: the bits of the same rows a few at a time, in the cache
+    and beside it."""
+    page, pages = 16, rows // 16 + 3
+    q, k, v = (rand((rows, h, D), dtype, 8 + i) for i, h in enumerate((Hq, Hkv, Hkv)))
+    pos, turns = torch.arange(rows, device=DEV, dtype=torch.int32) * 3, occ.rope_turns(D // 2)
+    slots = torch.randperm(pages * page, generator=torch.Generator().manual_seed(9))[:rows].to(torch.int32).to(DEV)
+    slots[5] = -1
+    kc, vc = (torch.full((pages, page, Hkv, D), 3.0, dtype=dtype, device=DEV) for _ in range(2))
+    qo, ko = occ.occ_rope(q, k, pos, turns, q_out=torch.empty_like(q), k_out=torch.empty_like(k), v=v, k_cache=kc, v_cache=vc, slots=slots)
+    here = slots >= 0
+    assert torch.equal(kc.flatten(0, 1)[slots[here].long()], ko[here]) and torch.equal(vc.flatten(0, 1)[slots[here].long()], v[here])
+    rest = torch.ones(pages * page, dtype=torch.bool, device=DEV)
+    rest[slots[here].long()] = False
+    assert bool((kc.flatten(0, 1)[rest] == 3).all()) and bool((vc.flatten(0, 1)[rest] == 3).all())
+    for a in (0, 100, rows - 3):
+        x, y = occ.occ_rope(q[a:a + 3].clone(), k[a:a + 3].clone(), pos[a:a + 3].clone(), turns)
+        assert torch.equal(x, qo[a:a + 3]) and torch.equal(y, ko[a:a + 3])
+
+
 @pytest.mark.parametrize("form", ["rows", "heads", "planes", "odd"])
 def test_rope_into_the_cache(form):
     """From a joint projection's rows into caches of several layouts; rows without a slot, or one past the cache, go nowhere."""
