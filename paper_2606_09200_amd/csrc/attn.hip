@@ -427,8 +427,8 @@ __device__ __forceinline__ void seen_by_all(const AttnCall &c, const Piece &p, i
 //   Heads of 256 take a register more than there are: it is spilled before the loop and read again behind it.
 //   One workgroup a CU, so that a share is long: 64 requests of 1 to 8191 keys, 64 heads over 8 of 128, 213 us (5.0 TB/s, a
 // copy's rate), 40 heads of their own 250 (5.3 TB/s); 130000 keys of one request 117 (4.55 TB/s: workgroups finish 70 to 96 us
-// after they begin, as their pages lie).  Four requests of 500 keys 14.5: 3.6 the plan, 1.4 pages and the first keys, 2 the
-// keys, 5 the parts' way through memory.
+// after they begin, as their pages lie).  Four requests of 500 keys 13: 3.6 the plan, 3 pages and keys, 4 the parts' way
+// through memory, 2.3 a launch.
 template <int DP>
 struct FewTile {
   static constexpr int WAVES = 8, THREADS = 64 * WAVES;
@@ -1381,8 +1381,9 @@ int attn_launch(const occ_attn_args &a, hipStream_t s) {
     k.cut.fixed = many ? (DP <= 128 ? 512 : 384) : 256, k.cut.block = many ? many_keys(DP) : few_keys(DP);
     k.cut.window = a.window < c.keys ? a.window : 0, k.cut.causal = a.causal != 0;
     k.least = least, k.most = most;
-    // (four chunks of 256 tokens: 57 us with 512 spare, 43 with 1024)
-    k.min_share = 256, k.least_even = many ? 512 : 256, k.spare = many ? 1024 : 512;
+    // (four chunks of 256 tokens: 57 us with 512 spare, 43 with 1024; four requests of 100 to 900 keys 13.0 us with parts of
+    // 128 keys or more, 14.6 with 256, 17.8 with 512; one of 4000 keys 16.6, 16.4, 17.8, but 18.1 with 64)
+    k.min_share = 256, k.least_even = many ? 512 : 128, k.spare = many ? 1024 : 512;
     return many ? launch<true>(k, DP, cus, s) : launch<false>(k, DP, cus, s);
   };
   const int most_rows = (int)std::min<int64_t>((int64_t)std::min(a.max_fresh, a.rows) * c.group, INT32_MAX);
