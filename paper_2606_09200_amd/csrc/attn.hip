@@ -1382,8 +1382,9 @@ int attn_launch(const occ_attn_args &a, hipStream_t s) {
     k.cut.window = a.window < c.keys ? a.window : 0, k.cut.causal = a.causal != 0;
     k.least = least, k.most = most;
     // (four chunks of 256 tokens: 57 us with 512 spare, 43 with 1024; four requests of 100 to 900 keys 13.0 us with parts of
-    // 128 keys or more, 14.6 with 256, 17.8 with 512; one of 4000 keys 16.6, 16.4, 17.8, but 18.1 with 64)
-    k.min_share = 256, k.least_even = many ? 512 : 128, k.spare = many ? 1024 : 512;
+    // 128 keys or more, 14.6 with 256, 17.8 with 512; one of 4000 keys 16.6, 16.4, 17.8, but 18.1 with 64;
+    // many rows, a prompt of 1024: 32.0 with 256, 33.2 with 512)
+    k.min_share = 256, k.least_even = many ? 256 : 128, k.spare = many ? 1024 : 512;
     return many ? launch<true>(k, DP, cus, s) : launch<false>(k, DP, cus, s);
   };
   const int most_rows = (int)std::min<int64_t>((int64_t)std::min(a.max_fresh, a.rows) * c.group, INT32_MAX);
