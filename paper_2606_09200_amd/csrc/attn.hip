@@ -748,8 +748,9 @@ struct ManyTile {
   static constexpr int KS = DP / STEP, DT = DP / R, KT = 2, WT = KEYS / STEP;
   static constexpr int N = R / P;                      // values of a result tile that a lane has: 4 of every 4 P rows
   typedef float Acc __attribute__((ext_vector_type(N)));
-  static constexpr int CH = DP / 8;                    // 16-byte chunks of a row
-  static constexpr int PITCH = DP * 2;
+  static constexpr int ROOM = DP == 96 ? 128 : DP;     // values that a row in LDS has room for
+  static constexpr int CH = ROOM / 8;                  // 16-byte chunks of a row
+  static constexpr int PITCH = ROOM * 2;
   static constexpr int OPERAND = KEYS * PITCH;         // bytes of a tile of K, and of V
   static constexpr int STAGES = 4;                     // of the ring of tiles of K, and of that of V
   static constexpr int ZEROS = OPERAND;                // bytes of zeros behind the rings
@@ -766,7 +767,7 @@ constexpr float kSlack = 8.f;
 // chunks in a row.
 template <int DP>
 __device__ __forceinline__ int many_swizzle_k(int r, int c) {
-  if constexpr (DP >= 128) return c ^ (r & 15);
+  if constexpr (ManyTile<DP>::CH >= 16) return c ^ (r & 15);
   else return swz<8>(r, c);
 }
 template <int DP>
@@ -1247,7 +1248,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
         // weigh.  The wave that multiplies goes first: the other's instructions fill what it leaves (712 -> 693 us for a prompt
         // of 8192, together with the values' order).
         __builtin_amdgcn_s_setprio(0);
-        u32x4 v0[DT / 2][WT], v1[DT / 2][WT], w[WT];
+        u32x4 v0[DT - DT / 2][WT], v1[DT / 2][WT], w[WT];
         uint32_t bad0 = 0, bad1 = 0;
         if (loads.ever_bad) {
           bad0 = sh.bad_rows[b % 8][0], bad1 = sh.bad_rows[b % 8][1];
@@ -1281,15 +1282,15 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
         if (b + ahead >= loads.plain_until) loads.prepare(b + ahead);
         int id[T::PASSES];
         u32x4 k0[KS], k1[KS];
-        constexpr int HALF = DT / 2 * WT;  // matrix instructions of half of o
+        constexpr int SECOND = DT / 2 * WT;  // matrix instructions of o's second part
         loads.pages(id);
-        from.values(stage, DT / 2, v1);
+        from.values(stage, DT - DT / 2, v1);
         state.multiply(v0, w, 0);
-        interleave<HALF, 2, 0>();
+        interleave<DT * WT - SECOND, 2, 0>();
         from.keys(b + 1, 0, k0);
         loads.issue(b + ahead, id);
-        state.multiply(v1, w, DT / 2);
-        interleave<HALF, KS / HALF, 6>();
+        state.multiply(v1, w, DT - DT / 2);
+        interleave<SECOND, (KS + SECOND - 1) / SECOND, 6>();
         from.keys(b + 1, 1, k1);
         score(k0, x[0]);
         interleave<KS, 1, 0>();
@@ -1311,8 +1312,8 @@ int padded_head(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 template <int DP, bool MANY, bool FULL>
 int launch(const AttnCall &c, int grid, hipStream_t s) {
   void (*fn)(AttnCall);
-  if constexpr (!MANY) fn = attn_few_kernel<DP>;
-  else fn = attn_pairs_kernel<DP, FULL>;
+  if constexpr (MANY) fn = attn_pairs_kernel<DP, FULL>;
+  else fn = attn_few_kernel<DP>;
   constexpr int lds = MANY ? ManyTile<DP>::LDS : FewTile<DP>::WAVES * FewTile<DP>::WAVE_BYTES;
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return OCC_ENODEV;
@@ -1326,6 +1327,8 @@ int launch(const AttnCall &c, int grid, hipStream_t s) {
 }
 template <int DP, bool MANY>
 int launch(const AttnCall &c, int grid, hipStream_t s) {
+  // tiles of rows as wide as 128 values, products of 96 (a prompt of 4096, 32 heads over 8 of 80: 126 us, 142 with products of 128)
+  if (MANY && DP == 128 && c.D <= 96) return launch<96, true, false>(c, grid, s);
   return MANY && c.D == DP ? launch<DP, MANY, true>(c, grid, s) : launch<DP, MANY, false>(c, grid, s);
 }
 template <bool MANY>

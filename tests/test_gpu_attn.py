@@ -146,7 +146,8 @@ CHUNKS = [(0, 1)], [(0, 129)], [(100, 70), (0, 200)], [(3, 64), (0, 65), (300, 1
 
 @pytest.mark.parametrize("requests", CHUNKS)
 @pytest.mark.parametrize("Hq,Hkv,D,page", [(1, 1, 64, 16), (4, 2, 128, 16), (7, 1, 64, 48), (5, 1, 128, 1), (2, 1, 256, 64), (2, 2, 8, 3),
-                                          (3, 1, 80, 16), (2, 2, 136, 5), (20, 1, 64, 16), (130, 1, 64, 16)])
+                                          (3, 1, 80, 16), (2, 2, 136, 5), (20, 1, 64, 16), (130, 1, 64, 16), (4, 2, 96, 48), (2, 1, 72, 16),
+                                          (2, 1, 104, 24), (2, 1, 40, 7)])
 def test_chunks(requests, Hq, Hkv, D, page):
     Problem(requests, Hq, Hkv, D, page, seed=3).check(max_fresh=500)   # a large bound: the kernels of many rows
 
@@ -179,10 +180,11 @@ def test_a_table_wider_apart_and_rows_behind():
     p.check(), p.check(max_fresh=400)
 
 
+@pytest.mark.parametrize("D", [64, 80, 128, 256])
 @pytest.mark.parametrize("max_fresh", [1, 400])
-def test_unseen_infinities_and_nan(max_fresh):
+def test_unseen_infinities_and_nan(max_fresh, D):
     """Later tokens' keys and values are NaN or infinite: rows before them have the bits they have without."""
-    p = Problem([(60, 12), (0, 90)], 4, 2, 64, 16, seed=9)
+    p = Problem([(60, 12), (0, 90)], 4, 2, D, 16, seed=9)
     clean, clean_lse = (t.clone() for t in p.run(max_fresh=max_fresh))
     for bad in (float("nan"), float("inf"), -float("inf")):
         for i, (c, f) in enumerate(p.requests):
@@ -195,7 +197,7 @@ def test_unseen_infinities_and_nan(max_fresh):
             assert torch.equal(out[a:b - 1], clean[a:b - 1]) and torch.equal(lse[a:b - 1], clean_lse[a:b - 1])
             assert bool(out[b - 1].isnan().all())
     # a window that has moved past them
-    p = Problem([(60, 90)], 4, 2, 64, 16, seed=9)
+    p = Problem([(60, 90)], 4, 2, D, 16, seed=9)
     p.check(window=8, max_fresh=max_fresh)
     clean = p.out.clone()
     for j in range(20):
@@ -205,17 +207,18 @@ def test_unseen_infinities_and_nan(max_fresh):
     assert torch.equal(out, clean)
 
 
+@pytest.mark.parametrize("D", [64, 80, 128, 256])
 @pytest.mark.parametrize("max_fresh", [1, 400])
-def test_seen_infinite_values(max_fresh):
+def test_seen_infinite_values(max_fresh, D):
     """An infinite value that a row sees makes that one output infinite, and NaN a NaN; the others stay."""
-    p = Problem([(50, 20)], 2, 1, 64, 16, seed=10)
+    p = Problem([(50, 20)], 2, 1, D, 16, seed=10)
     clean, _ = (t.clone() for t in p.run(max_fresh=max_fresh))
     at = p.table[0][10 // 16], 10
     p.dv[at][0, 3], p.dv[at][0, 17], p.dv[at][0, 40] = float("inf"), -float("inf"), float("nan")
     out, _ = p.run(max_fresh=max_fresh)
     assert bool((out[:, :, 3] == float("inf")).all()) and bool((out[:, :, 17] == -float("inf")).all())
     assert bool(out[:, :, 40].isnan().all())
-    keep = [d for d in range(64) if d not in (3, 17, 40)]
+    keep = [d for d in range(D) if d not in (3, 17, 40)]
     assert torch.equal(out[:, :, keep], clean[:, :, keep])
 
 

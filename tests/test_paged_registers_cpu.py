@@ -9,7 +9,7 @@ SPILLS = {"attn_few_kernelILi256E": 1}
 def test_spilled_vector_registers(built):  # noqa: F811
     found = [k for elf in code_objects(binding.LIB_PATH) for k in kernels(elf)]
     ours = [k for k in found if any(n in k[".name"] for n in ("kv_tables", "rope_kernel", "attn_few", "attn_pairs"))]
-    assert len(ours) == 2 + 7 + 3 + 6
+    assert len(ours) == 2 + 7 + 3 + 7
     for k in ours:
         allowed = sum(n for name, n in SPILLS.items() if name in k[".name"])
         assert k.get(".vgpr_spill_count", 0) <= allowed, (k[".name"], k[".vgpr_spill_count"])
