@@ -236,6 +236,7 @@ struct Walk {
     }
     before[0] = own[0], before[1] = own[1];
     block_sums(sh, before, total);
+    if (total[1] == 0) return;  // a launch that has none of a step's requests
     // where even parts are better, the sums are of parts
     int even = attn_even_units(total[0] - total[1] * cut.fixed, total[1], shares, c.least_even, c.spare);
     auto size = [&](const AttnSeq &s) {
