@@ -240,7 +240,7 @@ int validate_kv_tables(const occ_kv_tables_args &a) {
 int validate_rope(const occ_rope_args &a) {
   if (!float_type(a.dtype) || a.rows < 0 || a.rows > (1 << 24) || a.Hq < 0 || a.Hkv < 0) return OCC_EINVAL;
   if (a.Hq > 65536 || a.Hkv > 65536 || a.D < 2 || a.D > OCC_ROPE_MAX_D || a.D % 2 != 0) return OCC_EINVAL;
-  if (a.pairs < 0 || 2 * a.pairs > a.D || !(a.scale - a.scale == 0.f)) return OCC_EINVAL;
+  if (a.pairs < 0 || a.pairs > a.D / 2 || !(a.scale - a.scale == 0.f)) return OCC_EINVAL;
   const bool cache = a.k_cache != nullptr;
   if (cache != (a.v_cache != nullptr)) return OCC_EINVAL;
   if (a.rows == 0) return OCC_OK;
@@ -332,7 +332,7 @@ int validate_attn(const occ_attn_args &a) {
   if (!cache_apart(a.pages, a.cache_page, a.page, a.cache_row, a.Hkv, a.cache_head, a.D)) return OCC_EINVAL;
   // pitches are 32-bit numbers in the kernels, units of work 64-bit ones with some bits to spare
   if ((a.pages > 1 && a.cache_page > OCC_ATTN_MAX_PITCH) || (a.page > 1 && a.cache_row > OCC_ATTN_MAX_PITCH)) return OCC_EINVAL;
-  if ((double)(a.rows + a.requests) * a.width * a.page * a.Hq >= 0x1p50) return OCC_EINVAL;
+  if (((double)a.rows + a.requests) * a.width * a.page * a.Hq >= 0x1p50) return OCC_EINVAL;
   const size_t need = attn_workspace(a.D);
   if (a.workspace_bytes < need) return OCC_EINVAL;
   const size_t cached = (size_t)(a.pages - 1) * a.cache_page * 2 + span3(a.page, a.cache_row, a.Hkv, a.cache_head, a.D, 2);
