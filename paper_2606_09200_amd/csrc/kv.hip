@@ -2,6 +2,7 @@
 // with keys and values put into the cache (occ_rope).
 #include "block_util.h"
 #include "divider.h"
+#include "rope_plan.h"
 
 #include <algorithm>
 
@@ -408,21 +409,15 @@ int rope_launch(const occ_rope_args &a, hipStream_t s) {
   c.per_head = a.D / 2 / pairs;
   c.per_token = c.per_head * (Hq + Hkv + (cache ? Hkv : 0));
   c.by_item = Divider(c.per_token), c.by_chunk = Divider(c.per_head);
-  // A token a workgroup, an item or two a thread, where there are plenty of tokens (several tokens where they have few
-  // items), dealt out among workgroups where there are few.  More than the L2s hold is stored past them.  8192 tokens, 64
-  // heads over 8 of 128: 77 us with four tokens a workgroup of 256 threads and ordinary stores, 62 with one, 50 past the L2s.
-  const bool plenty = a.rows >= di->num_cus;
-  const int threads = plenty ? std::min(512, (c.per_token + 63) / 64 * 64) : kThreads;
-  c.tokens = a.rows >= 16 * di->num_cus ? std::max(1, kThreads / c.per_token) : 1;
-  const int64_t items = (int64_t)c.tokens * c.per_token;
-  const int block = c.tokens > 1 ? kThreads : threads;
+  // More than the L2s hold is stored past them.  8192 tokens, 64 heads over 8 of 128: 77 us with four tokens a workgroup of 256
+  // threads and ordinary stores, 62 with one, 50 past the L2s.
+  const RopeGrid grid = rope_grid(a.rows, c.per_token, di->num_cus);
+  c.tokens = grid.tokens;
   const bool stream = (int64_t)a.rows * c.per_token * 2 * pairs * elem > (32 << 20);
   RopeFn fn = elem == 2 ? (pairs == 8 ? (stream ? rope_kernel<uint16_t, 8, true> : rope_kernel<uint16_t, 8, false>)
                            : pairs == 4 ? rope_kernel<uint16_t, 4, false> : rope_kernel<uint16_t, 1, false>)
                         : (pairs == 4 ? (stream ? rope_kernel<float, 4, true> : rope_kernel<float, 4, false>) : rope_kernel<float, 1, false>);
-  const int x = (a.rows + c.tokens - 1) / c.tokens, passes = (int)((items + block - 1) / block);
-  const int y = std::max(1, std::min({passes, 4 * di->num_cus / x, 64}));
-  hipLaunchKernelGGL(fn, dim3(x, y), dim3(block), (size_t)c.tokens * c.half * sizeof(float2), s, c);
+  hipLaunchKernelGGL(fn, dim3(grid.x, grid.y), dim3(grid.threads), (size_t)c.tokens * c.half * sizeof(float2), s, c);
   return hipGetLastError() == hipSuccess ? OCC_OK : OCC_EHIP;
 }
 
