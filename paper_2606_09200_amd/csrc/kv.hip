@@ -218,7 +218,7 @@ __global__ __launch_bounds__(kThreads) void kv_tables_kernel(TablesCall c) {
 //   (y_0, y_1) = m (x_0 cos a - x_1 sin a, x_1 cos a + x_0 sin a),  a = 2 pi position turns_i
 //
 // for pair i of a head.  turns is a 64-bit fraction of a turn, so that position * turns modulo 2^64 is the exact
-// remainder of the angle, however far the position.  A workgroup makes its tokens' cosines and sines once, in LDS, and
+// remainder of the angle, however far the position, and all its bits count (cos_sin).  A workgroup makes its tokens' cosines and sines once, in LDS, and
 // passes over their heads: bound by reading and writing q, k and v once.  8192 tokens, 64 heads over 8 of 128, into the cache:
 // 50 us, 6.7 TB/s, the inputs partly in the last cache (a copy of 2 GiB 4.95); 16 tokens 3.4 us.
 struct RopeCall {
@@ -335,6 +335,18 @@ struct RopeItem {
   }
 };
 
+// (cos, sin) of 2 pi phase / 2^64.  Of the nearest whole number of 2^40 that a float holds, then of the rest d, below 2^-24 half
+// turns: sin (a + d) = sin a + d cos a, cos (a + d) = cos a - d sin a, d^2 / 2 being below 2^-45.  Rounded to a float as it is,
+// the angle would be off by up to 2^-26 of a turn, in small sines by a multiple of their own rounding.
+__device__ __forceinline__ float2 cos_sin(int64_t phase) {
+  const uint64_t near = (uint64_t)phase + (1ull << 39);   // of all 64 bits: 2^63 is half a turn from either side
+  const float whole = (float)((int32_t)(near >> 32) >> 8) * 0x1p-23f;
+  const float d = (float)((int64_t)(near & ((1ull << 40) - 1)) - (1ll << 39)) * (float)(3.14159265358979323846 * 0x1p-63);
+  float s, c;
+  sincospif(whole, &s, &c);
+  return float2{__builtin_fmaf(-s, d, c), __builtin_fmaf(c, d, s)};
+}
+
 template <class E, int PAIRS, bool STREAM>
 __global__ __launch_bounds__(512) void rope_kernel(RopeCall c) {
   extern __shared__ __align__(16) float2 angles[];  // [token][pair]: (cos, sin), scaled
@@ -343,9 +355,8 @@ __global__ __launch_bounds__(512) void rope_kernel(RopeCall c) {
   for (int i = threadIdx.x; i < tokens * c.half; i += blockDim.x) {
     const int t = i / c.half, pair = i - t * c.half;
     const int64_t phase = (int64_t)((uint64_t)(int64_t)c.positions[t0 + t] * (uint64_t)c.turns[pair]);
-    float s, co;
-    sincospif((float)phase * 0x1p-63f, &s, &co);
-    angles[i] = float2{co * c.scale, s * c.scale * c.sign};
+    const float2 w = cos_sin(phase);
+    angles[i] = float2{w.x * c.scale, w.y * c.scale * c.sign};
   }
   __syncthreads();
   for (int e = blockIdx.y * blockDim.x + threadIdx.x; e < all; e += stride) {
