@@ -227,6 +227,8 @@ def main(argv=None):
     def decode(what, d):
         d.embedded.copy_(torch.randn(a.tokens, a.hidden, generator=g, device="cuda"))
         eager = d.step().clone()
+        if d.cache is not None:
+            assert bool((d.cache.lens == a.context + 1).all()), "a request has not the keys it should have"
         graph = d.graph()
         graph.replay()
         assert torch.equal(d.out, eager), "the graph's step differs"
@@ -239,10 +241,10 @@ def main(argv=None):
         cache = Cache(a.layers, a.tokens, a.tokens, width, a.tokens * width, a.page, a.kv_heads, a.head, most=1)
         for t in (cache.k, cache.v):
             t.normal_(generator=g)
-        cache.fresh.fill_(a.context)
-        cache.tables()
-        cache.advance()
         cache.fresh.fill_(1)
+        for _ in range(a.context):  # a step has room for a token of each
+            cache.tables()
+            cache.advance()
         decode("decode with attention over %d keys" % (a.context + 1),
                Decoder(a.layers, a.tokens, a.hidden, a.inner, a.experts, a.top_k, heads=a.heads, cache=cache, window=a.window))
     t = Trainee(a.rows, a.hidden, a.out)
