@@ -398,25 +398,15 @@ struct Row {
 };
 __device__ __forceinline__ Row row_of(const AttnCall &c, const Piece &p, int r) {
   const int t = c.by_heads(r), h = r - t * c.heads;
-  const int token = p.tile * c.cut.tokens + t;
   const int in = p.group * c.heads + h;
+  const AttnRow of = attn_row(c.cut, p.s, p.tile, t);
   Row row;
-  row.valid = t < c.cut.tokens && token < p.s.fresh && in < c.group;
-  row.token = p.s.first + token;
+  row.valid = t < c.cut.tokens && of.valid && in < c.group;
+  row.token = p.s.first + of.token;
   row.head = p.kv * c.group + in;
-  const int pos = p.s.len - p.s.fresh + token;
-  row.hi = !row.valid ? 0 : c.cut.causal ? min(pos + 1, p.s.len) : p.s.len;
-  row.lo = c.cut.window ? pos - c.cut.window + 1 : 0;
+  row.lo = of.lo, row.hi = row.valid ? of.hi : 0;
   return row;
 }
-// Keys [all_lo, all_hi) that every row of a tile sees.
-__device__ __forceinline__ void seen_by_all(const AttnCall &c, const Piece &p, int t0, int t1, int &all_lo, int &all_hi) {
-  const int base = p.s.len - p.s.fresh + p.tile * c.cut.tokens;
-  const int left = p.s.fresh - p.tile * c.cut.tokens;  // a tile's last tokens may not exist
-  all_hi = c.cut.causal ? min(base + t0 + 1, p.s.len) : p.s.len;
-  all_lo = c.cut.window ? base + min(t1, left) - c.cut.window : 0;
-}
-
 // ------------------------------------------------------------------ few rows
 //
 // Decoding: up to 16 rows (heads that share keys, times tokens) and many keys.  What bounds it is reading keys and
@@ -469,8 +459,7 @@ __global__ __launch_bounds__(FewTile<DP>::THREADS, FewTile<DP>::PER_CU) void att
   for (; walk.next(); walk.done()) {
     const Piece &p = walk.p;
     const Row row = row_of(c, p, l16);
-    int all_lo, all_hi;
-    seen_by_all(c, p, 0, c.cut.tokens, all_lo, all_hi);
+    const auto [all_lo, all_hi] = attn_all_see(c.cut, p.s, p.tile, 0, c.cut.tokens);  // keys that every row sees
     const int32_t *table = c.table + (size_t)p.request * c.table_pitch;
     const uint16_t *kc = c.k + (size_t)p.kv * c.cache_head + 8 * g, *vc = c.v + (size_t)p.kv * c.cache_head + 8 * g;
 
@@ -1203,8 +1192,7 @@ __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void a
   for (; walk.next(); walk.done()) {
     const Piece &p = walk.p;
     const Row row = row_of(c, p, wave * T::R + lane % T::R);
-    int all_lo, all_hi;
-    seen_by_all(c, p, c.by_heads(wave * T::R), c.by_heads(wave * T::R + T::R - 1) + 1, all_lo, all_hi);
+    const auto [all_lo, all_hi] = attn_all_see(c.cut, p.s, p.tile, c.by_heads(wave * T::R), c.by_heads(wave * T::R + T::R - 1) + 1);
     // tiles whose keys all rows see
     const int clear_from = uniform((max(all_lo - p.first, 0) + T::KEYS - 1) / T::KEYS), clear_to = uniform(max(all_hi - p.first, 0) / T::KEYS);
     TileLoads<DP, FULL> loads{rows, p, sh, c.table + (size_t)p.request * c.table_pitch, c.k + (size_t)p.kv * c.cache_head,

@@ -39,7 +39,8 @@ OCC_PLAN AttnSeq attn_seq(int start, int end, int len, int rows, int most) {
   return AttnSeq{a, b - a, len < 0 ? 0 : len > most ? most : len};
 }
 
-OCC_PLAN int attn_tiles(const AttnCut &c, const AttnSeq &s) { return c.by_tokens(s.fresh + c.tokens - 1); }
+// Numbers of rows go up to 2^31 - 1: nothing is added to one before it is divided.
+OCC_PLAN int attn_tiles(const AttnCut &c, const AttnSeq &s) { return s.fresh == 0 ? 0 : c.by_tokens(s.fresh - 1) + 1; }
 
 // Keys [first, last) that some token of tile m sees.
 OCC_PLAN int attn_last_key(const AttnCut &c, const AttnSeq &s, int m) {
@@ -55,12 +56,35 @@ OCC_PLAN int attn_first_key(const AttnCut &c, const AttnSeq &s, int m) {
   return at < 0 ? 0 : at > last ? last : (int)at;
 }
 
+// Token t of tile m: whether there is one, which of the request's, and the keys [lo, hi) that it sees.
+struct AttnRow {
+  int token, lo, hi;
+  bool valid;
+};
+OCC_PLAN AttnRow attn_row(const AttnCut &c, const AttnSeq &s, int m, int t) {
+  const int before = m * c.tokens;
+  AttnRow r{0, 0, 0, t < s.fresh - before};
+  const int pos = s.len - s.fresh + before + t;  // negative where a request has more rows than keys
+  r.token = r.valid ? before + t : 0;
+  r.hi = !r.valid ? 0 : !c.causal ? s.len : pos < 0 ? 0 : pos + 1 < s.len ? pos + 1 : s.len;
+  r.lo = c.window != 0 && pos >= c.window ? pos - c.window + 1 : 0;
+  return r;
+}
+// Keys [lo, hi) that all of its tokens t0 .. t1 - 1 see, as far as these exist.
+struct AttnKeys {
+  int lo, hi;
+};
+OCC_PLAN AttnKeys attn_all_see(const AttnCut &c, const AttnSeq &s, int m, int t0, int t1) {
+  const int left = s.fresh - m * c.tokens;
+  return AttnKeys{attn_row(c, s, m, (t1 < left ? t1 : left) - 1).lo, t0 < left ? attn_row(c, s, m, t0).hi : s.len};
+}
+
 // Sum over j < n of max(0, a + j tokens).
 OCC_PLAN int64_t attn_ramp(const AttnCut &c, int n, int64_t a) {
   const int64_t step = c.tokens;
   if (n <= 0 || a + (n - 1) * step <= 0) return 0;
   // here -a < (n - 1) step, at most a request's rows
-  const int skip = a < 0 ? c.by_tokens((int)(-a + step - 1)) : 0;
+  const int skip = a < 0 ? c.by_tokens((int)(-a - 1)) + 1 : 0;
   const int64_t count = n - skip;
   return count * (a + skip * step) + step * (count * (count - 1) / 2);
 }
