@@ -84,6 +84,22 @@ __device__ __forceinline__ uint32_t pair_finite(uint32_t w) {
   return ((w & 0x7F80u) == 0x7F80u ? 0u : w & 0xFFFFu) | ((w & 0x7F800000u) == 0x7F800000u ? 0u : w & 0xFFFF0000u);
 }
 
+// Whether some row's maximum is one that exact_maximum is for.
+__device__ __forceinline__ bool large_maximum(float by) { return __ballot(fabsf(by) >= 0x1p24f && fabsf(by) < INFINITY) != 0; }
+// Scores of a row whose maximum is `by` (in powers of 2) as exponents, exp2 (scale x - by): the product goes into the difference
+// unrounded, the maximum is a rounded one.  From 2^24 on that is off by 1 and more, by 2^7 at 2^31, and no weight would be left, or an
+// infinite one: there x becomes what, times scale, is the difference of rounded products, 0 at the maximum, and `by` 0.
+template <int TILES, class Acc>
+__device__ __forceinline__ void exact_maximum(Acc (&x)[TILES], float scale, float &by) {
+  const bool large = fabsf(by) >= 0x1p24f;
+  const float back = 1.f / scale;  // of numbers above 2^24 / 2^128 where it is used
+#pragma unroll
+  for (int t = 0; t < TILES; ++t)
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(Acc) / 4); ++i) x[t][i] = large ? (x[t][i] * scale - by) * back : x[t][i];
+  by = large ? 0.f : by;
+}
+
 struct AttnCall {
   const uint16_t *q, *k, *v;
   const int32_t *table, *starts, *lens;
@@ -542,9 +558,10 @@ __global__ __launch_bounds__(FewTile<DP>::THREADS, FewTile<DP>::PER_CU) void att
 #pragma unroll
       for (int i = 1; i < 4 * TILES; ++i) top = fmaxf(top, x[i >> 2][i & 3]);
       top = fmaxf(m, max_quarters(top) * c.scale);
-      const float by = top == -INFINITY ? 0.f : top;
+      float by = top == -INFINITY ? 0.f : top;
       const float less = exp2_(m - by);
       m = top;
+      if (large_maximum(by)) exact_maximum(x, c.scale, by);
       l = l * less;
       float e[8] = {};
 #pragma unroll
@@ -957,8 +974,9 @@ struct RowState {
   using Acc = typename T::Acc;
   Acc acc[T::DT];
   float m, l;
+  int large;  // large_maximum of the rows' m
   __device__ __forceinline__ void clear() {
-    m = -INFINITY, l = 0.f;
+    m = -INFINITY, l = 0.f, large = 0;
 #pragma unroll
     for (int t = 0; t < T::DT; ++t)
 #pragma unroll
@@ -1000,6 +1018,7 @@ struct RowState {
     if (__ballot(top > m + kSlack) != 0) {
       const float now = fmaxf(m, top), less = now == -INFINITY ? 1.f : exp2_(m - now);
       m = now;
+      large = uniform(large_maximum(m) ? 1 : 0);
       l = l * less;
 #pragma unroll
       for (int t = 0; t < T::DT; ++t) acc[t] = acc[t] * less;
@@ -1023,7 +1042,8 @@ struct RowState {
           }
       }
     }
-    const float by = m == -INFINITY ? 0.f : m;
+    float by = m == -INFINITY ? 0.f : m;
+    if (large != 0) exact_maximum(x, scale, by);
 #pragma unroll
     for (int t = 0; t < T::KT; ++t)
 #pragma unroll
