@@ -727,7 +727,7 @@ int occ_rope(const occ_rope_args *args, void *stream);
  * Logits, sums and o are fp32; weights p take part in the sum with v as bf16 (two of them where a request has few
  * rows), out is bf16 and lse (rows x Hq, null: not stored) fp32.
  * max_fresh: the most rows of a request; what the choice of kernels goes by (results hold for any).
- * D: a multiple of 8 up to 256; Hq a multiple of Hkv; pitches (elements) multiples of 8, buffers 16-byte aligned,
+ * 0 < scale <= 2^127.  D: a multiple of 8 up to 256; Hq a multiple of Hkv; pitches (elements) multiples of 8, buffers 16-byte aligned,
  * starts, lens, table and lse 4.  rows * Hq < 2^31, (rows + requests) * width * page * Hq < 2^50; cache_page and cache_row at
  * most OCC_ATTN_MAX_PITCH.
  * workspace: occ_attn_paged_workspace_bytes(Hq, Hkv, D) bytes, 16-byte aligned, zeroed once before its first use (a

@@ -318,7 +318,7 @@ int validate_attn(const occ_attn_args &a) {
   if (!attn_heads(a.Hq, a.Hkv, a.D)) return OCC_EINVAL;
   if (a.requests < 0 || a.requests > OCC_KV_MAX_REQUESTS || a.rows < 0 || (long long)a.rows * a.Hq > INT32_MAX) return OCC_EINVAL;
   if (a.page < 1 || a.page > OCC_KV_MAX_PAGE || a.width < 0 || a.max_fresh < 0 || a.window < 0) return OCC_EINVAL;
-  if (!(a.scale > 0.f) || !(a.scale - a.scale == 0.f)) return OCC_EINVAL;
+  if (!(a.scale > 0.f && a.scale <= 0x1p127f)) return OCC_EINVAL;  // the kernels' is log2 e times that
   if (a.requests == 0 || a.rows == 0) return OCC_OK;
   if (a.pages < 1 || (long long)a.pages * a.page > INT32_MAX) return OCC_EINVAL;
   const void *wide[] = {a.q, a.k_cache, a.v_cache, a.out, a.workspace};

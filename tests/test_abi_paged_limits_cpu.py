@@ -2,6 +2,7 @@
 pointers)."""
 import pytest
 
+from test_abi_cpu import expect_accepted
 from test_abi_paged_cpu import EINVAL, L, attn, rope  # noqa: F401
 
 MOST = 2 ** 31 - 1
@@ -20,3 +21,12 @@ def test_more_work_than_units_count(L, rows, requests):  # noqa: F811
     # tensors of as many rows are further apart than the default places
     far = {n: (i + 1) << 44 for i, n in enumerate(("q", "k_cache", "v_cache", "table", "starts", "lens", "out", "lse", "workspace"))}
     assert L.occ_attn_paged(attn(rows=rows, requests=requests, **one, **far), None) == EINVAL
+
+
+# times log2 e it has to stay a number
+@pytest.mark.parametrize("scale,status", [(2.0 ** 127 * 1.5, EINVAL), (3.4028234e38, EINVAL), (2.0 ** 127, None), (2.0 ** -149, None)])
+def test_scales(L, scale, status):  # noqa: F811
+    if status is None:
+        expect_accepted(L, L.occ_attn_paged, attn(scale=scale), None)
+    else:
+        assert L.occ_attn_paged(attn(scale=scale), None) == status
