@@ -1015,8 +1015,10 @@ struct RowState {
 #pragma unroll
     for (int i = 1; i < T::N * T::KT; ++i) top = fmaxf(top, x[i / T::N][i % T::N]);
     top = row_max<DP>(top) * scale;
-    if (__ballot(top > m + kSlack) != 0) {
-      const float now = fmaxf(m, top), less = now == -INFINITY ? 1.f : exp2_(m - now);
+    const bool grows = top > m + kSlack;
+    if (__ballot(grows) != 0) {
+      // each row by itself: its bits do not depend on the others', nor on keys that only they see
+      const float now = grows ? top : m, less = grows ? exp2_(m - now) : 1.f;
       m = now;
       large = uniform(large_maximum(m) ? 1 : 0);
       l = l * less;
