@@ -693,7 +693,8 @@ int occ_kv_tables(const occ_kv_tables_args *args, void *stream);
  * passed through.  turns[i] is the i-th frequency over 2 pi as a fraction of 2^64 (int64, wrapping): angles
  * are exact to 2^-32 of a turn at every position, negative ones too.  inverse != 0 turns the other way: the
  * gradient of the same call.  Sums are fp32, outputs are rounded once.
- * q_out may be q and k_out k (the same pitches).  With caches (both or none; k is needed), row r's turned keys
+ * q_out may be q and k_out k (the same pitches); q, k and v, and the two caches, may lie among each other in one buffer where their
+ * pitches keep them apart (beside each other in each row, head or page).  With caches (both or none; k is needed), row r's turned keys
  * and its rows of v go to slot slots[r] of k_cache and v_cache, and to none where that is not in [0, pages * page);
  * k_out may then be null.  dtype, of all tensors: OCC_BF16 or OCC_F32.  *_row, *_head: pitches in elements of rows and
  * heads, cache_page, cache_row, cache_head of both caches.  Values of a head are contiguous.  1 <= D <= OCC_ROPE_MAX_D,

@@ -210,6 +210,34 @@ bool apart(int rows, size_t row, int heads, size_t head, int D) {
   if (heads <= 1 || rows <= 1) return true;
   return row >= (size_t)(heads - 1) * head + d || head >= (size_t)(rows - 1) * row + d;
 }
+// How many heads, rows and pages of D values there are, and how far apart (elements).
+struct Pitches {
+  int count[3];
+  size_t pitch[3];
+};
+// Whether the values of x and y, in one buffer, are not each other's because of a period, one of their pitches: of what lies within
+// it (heads in a row, say), x's begins behind y's end and ends within it, and all else is whole periods away.
+bool interleaved(const void *x, const Pitches &gx, const void *y, const Pitches &gy, int D, size_t elem) {
+  const uintptr_t px = reinterpret_cast<uintptr_t>(x), py = reinterpret_cast<uintptr_t>(y);
+  auto within = [&](const Pitches &g, size_t period, size_t &width) {
+    width = (size_t)D;
+    for (int i = 0; i < 3; ++i) {
+      if (g.count[i] <= 1) continue;
+      if (g.pitch[i] < period) width += (size_t)(g.count[i] - 1) * g.pitch[i];
+      else if (g.pitch[i] % period != 0) return false;
+    }
+    return true;
+  };
+  for (const Pitches *g : {&gx, &gy})
+    for (int i = 0; i < 3; ++i) {
+      if (g->count[i] <= 1 || g->pitch[i] == 0) continue;
+      size_t wx, wy;
+      if (!within(gx, g->pitch[i], wx) || !within(gy, g->pitch[i], wy)) continue;
+      const size_t period = g->pitch[i] * elem, off = px >= py ? (px - py) % period : (period - (py - px) % period) % period;
+      if (off >= wy * elem && off + wx * elem <= period) return true;
+    }
+  return false;
+}
 // The same of a cache's rows in pages; pages are outermost, then rows or heads.
 bool cache_apart(int pages, size_t cache_page, int page, size_t row, int heads, size_t head, int D) {
   return apart(page, row, heads, head, D) && (pages <= 1 || cache_page >= span3(page, row, heads, head, D, 1));
@@ -261,8 +289,6 @@ int validate_rope(const occ_rope_args &a) {
                 !apart(a.rows, a.v_row, a.Hkv, a.v_head, a.D) ||
                 !cache_apart(a.pages, a.cache_page, a.page, a.cache_row, a.Hkv, a.cache_head, a.D)))
     return OCC_EINVAL;
-  // rows of the joint projection interleave q, k and v: only tensors that begin within another's head overlap, so
-  // in place is told by the pointer and other overlaps of outputs with inputs by whole ranges where these are packed
   const Range rq{q ? a.q : nullptr, span3(a.rows, a.q_row, a.Hq, a.q_head, a.D, e)};
   const Range rk{k ? a.k : nullptr, span3(a.rows, a.k_row, a.Hkv, a.k_head, a.D, e)};
   const Range rv{cache ? a.v : nullptr, span3(a.rows, a.v_row, a.Hkv, a.v_head, a.D, e)};
@@ -271,32 +297,27 @@ int validate_rope(const occ_rope_args &a) {
   const size_t cached = cache ? ((size_t)(a.pages - 1) * a.cache_page) * e + span3(a.page, a.cache_row, a.Hkv, a.cache_head, a.D, e) : 0;
   const Range kc{a.k_cache, cached}, vc{a.v_cache, cached};
   const Range pos{a.positions, (size_t)a.rows * 4}, turns{a.turns, (size_t)a.pairs * 8}, slots{cache ? a.slots : nullptr, (size_t)a.rows * 4};
-  // Rows of one matrix (q, k and v side by side, as a joint projection leaves them): disjoint where their columns are.
-  auto beside = [&](const Range &x, size_t x_row, int hx, size_t x_head, const Range &y, size_t y_row, int hy, size_t y_head) {
-    if (!overlaps(x, y)) return true;
-    if (x_row != y_row || a.rows < 2) return false;
-    const size_t wx = ((size_t)(hx - 1) * x_head + a.D) * e, wy = ((size_t)(hy - 1) * y_head + a.D) * e, pitch = x_row * e;
-    const uintptr_t px = reinterpret_cast<uintptr_t>(x.p), py = reinterpret_cast<uintptr_t>(y.p);
-    const size_t off = (px > py ? px - py : pitch - (py - px) % pitch) % pitch;  // of x's columns behind y's
-    return off >= wy && off + wx <= pitch;
+  // q, k and v may lie among each other, as a joint projection leaves them, and so may keys and values of one cache
+  const Pitches gq{{a.Hq, a.rows, 1}, {a.q_head, a.q_row, 0}}, gk{{a.Hkv, a.rows, 1}, {a.k_head, a.k_row, 0}};
+  const Pitches gv{{a.Hkv, a.rows, 1}, {a.v_head, a.v_row, 0}}, gqo{{a.Hq, a.rows, 1}, {a.qo_head, a.qo_row, 0}};
+  const Pitches gko{{a.Hkv, a.rows, 1}, {a.ko_head, a.ko_row, 0}};
+  auto among = [&](const Range &x, const Pitches &gx, const Range &y, const Pitches &gy) {
+    return !overlaps(x, y) || interleaved(x.p, gx, y.p, gy, a.D, e);
   };
   const bool same_q = a.q_out == a.q && a.qo_row == a.q_row && a.qo_head == a.q_head;
   const bool same_k = a.k_out == a.k && a.ko_row == a.k_row && a.ko_head == a.k_head;
-  if (q && !same_q && !beside(qo, a.qo_row, a.Hq, a.qo_head, rq, a.q_row, a.Hq, a.q_head)) return OCC_EALIAS;
-  if (q && k && !beside(qo, a.qo_row, a.Hq, a.qo_head, rk, a.k_row, a.Hkv, a.k_head)) return OCC_EALIAS;
-  if (q && cache && !beside(qo, a.qo_row, a.Hq, a.qo_head, rv, a.v_row, a.Hkv, a.v_head)) return OCC_EALIAS;
+  if (q && !same_q && !among(qo, gqo, rq, gq)) return OCC_EALIAS;
+  if (q && k && !among(qo, gqo, rk, gk)) return OCC_EALIAS;
+  if (q && cache && !among(qo, gqo, rv, gv)) return OCC_EALIAS;
   if (k && a.k_out != nullptr) {
-    if (!same_k && !beside(ko, a.ko_row, a.Hkv, a.ko_head, rk, a.k_row, a.Hkv, a.k_head)) return OCC_EALIAS;
-    if (q && !beside(ko, a.ko_row, a.Hkv, a.ko_head, rq, a.q_row, a.Hq, a.q_head)) return OCC_EALIAS;
-    if (q && !beside(ko, a.ko_row, a.Hkv, a.ko_head, qo, a.qo_row, a.Hq, a.qo_head)) return OCC_EALIAS;
-    if (cache && !beside(ko, a.ko_row, a.Hkv, a.ko_head, rv, a.v_row, a.Hkv, a.v_head)) return OCC_EALIAS;
+    if (!same_k && !among(ko, gko, rk, gk)) return OCC_EALIAS;
+    if (q && !among(ko, gko, rq, gq)) return OCC_EALIAS;
+    if (q && !among(ko, gko, qo, gqo)) return OCC_EALIAS;
+    if (cache && !among(ko, gko, rv, gv)) return OCC_EALIAS;
   }
-  // keys and values may be planes of one cache: disjoint where their heads, rows or pages lie apart
-  if (cache && overlaps(kc, vc)) {
-    const size_t one = span3(a.page, a.cache_row, a.Hkv, a.cache_head, a.D, e), pitch = a.cache_page * e;
-    const uintptr_t pk = reinterpret_cast<uintptr_t>(a.k_cache), pv = reinterpret_cast<uintptr_t>(a.v_cache);
-    const size_t off = (pk > pv ? pk - pv : pv - pk);
-    if (a.pages < 2 || off < one || off + one > pitch) return OCC_EALIAS;
+  if (cache) {
+    const Pitches g{{a.Hkv, a.page, a.pages}, {a.cache_head, a.cache_row, a.cache_page}};
+    if (!among(kc, g, vc, g)) return OCC_EALIAS;
   }
   const Range in[] = {pos, turns, slots}, wide[] = {rq, rk, rv};
   const Range out[] = {kc};
