@@ -725,9 +725,11 @@ int occ_rope(const occ_rope_args *args, void *stream);
  * Where nothing is left, o is 0 and lse -inf; what is not seen has no influence, infinities and NaN neither.  lens[i] <= 0
  * leaves nothing; rows of no request keep what out and lse hold; lengths beyond width * page (or OCC_ATTN_MAX_KEYS) are cut.
  * starts ascend; a row that two requests have all the same gets the result of either.
- * Logits, sums and o are fp32; weights p take part in the sum with v as bf16 (two of them where a request has few
- * rows), out is bf16 and lse (rows x Hq, null: not stored) fp32.
- * max_fresh: the most rows of a request; what the choice of kernels goes by (results hold for any).
+ * Logits, sums and o are fp32, out is bf16 and lse (rows x Hq, null: not stored) fp32.  Weights p take part in the sum with v as
+ * bf16: as two of them, so that o has out's rounding alone, or as one, whose rounding (2^-8) comes to that.  They are two where
+ * max_fresh * Hq / Hkv <= 64, and beyond for the requests of as few rows, unless requests is 1 or requests * max_fresh is rows.  An
+ * infinite value whose weight is below what fp32 holds gives an infinity or NaN.
+ * max_fresh: the most rows of a request; what the choice of kernels goes by, and so the weights' form (results hold for any).
  * 0 < scale <= 2^127.  D: a multiple of 8 up to 256; Hq a multiple of Hkv; pitches (elements) multiples of 8, buffers 16-byte aligned,
  * starts, lens, table and lse 4.  rows * Hq < 2^31, (rows + requests) * width * page * Hq < 2^50; cache_page and cache_row at
  * most OCC_ATTN_MAX_PITCH.

@@ -432,8 +432,8 @@ __device__ __forceinline__ Row row_of(const AttnCall &c, const Piece &p, int r) 
 // P^T.  P goes in as the sum of two bf16 values: matrix instructions are in plenty here, and o then has
 // its own rounding alone (off by 0.0016 of its size; 0.0023 with one).
 //   Heads of 256 take a register more than there are: it is spilled before the loop and read again behind it.
-//   One workgroup a CU, so that a share is long: 64 requests of 1 to 8191 keys, 64 heads over 8 of 128, 213 us (5.0 TB/s, a
-// copy's rate), 40 heads of their own 250 (5.3 TB/s); 130000 keys of one request 117 (4.55 TB/s: workgroups finish 70 to 96 us
+//   One workgroup a CU, so that a share is long: 64 requests of 1 to 8191 keys, 64 heads over 8 of 128, 214 us (5.0 TB/s; a
+// copy has 4.95, mostly reads 5.8), 40 heads of their own 250 (5.3 TB/s); 130000 keys of one request 117 (4.55 TB/s: workgroups finish 70 to 96 us
 // after they begin, as their pages lie).  Four requests of 500 keys 13: 3.6 the plan, 3 pages and keys, 4 the parts' way
 // through memory, 2.3 a launch.
 template <int DP>
@@ -740,7 +740,7 @@ __global__ __launch_bounds__(FewTile<DP>::THREADS, FewTile<DP>::PER_CU) void att
 // (the other half of the wave has the other 16), which, rounded to bf16, are the second product's operand as they
 // lie: O^T = V^T P^T over the keys in that order, values read transposed.  Heads beyond 128 values, whose o and q would
 // fill the registers, have 16 rows a wave and 16x16x32 MFMAs (a lane has 4 of 16 keys): every wave reads the tile from LDS for half
-// as many rows, and two waves a SIMD fit (a prompt of 4096, heads of 256: 232 us with one wave of 32 rows, 203 so, now 185).  m and l are
+// as many rows, and two waves a SIMD fit (a prompt of 4096, heads of 256: 232 us with one wave of 32 rows, 203 so, now 175).  m and l are
 // one register a lane, and so is what o has to be scaled by.  The weights' rounding (8 bits) is of the same size as the output's
 // own; l sums them unrounded.
 // Scaling o costs as much as half of a tile's exponentials: m stays behind the maximum until it would have to grow by
@@ -1180,11 +1180,11 @@ __device__ __forceinline__ void interleave() {
 // b - 1, scores of b and weights of b: keys of b and b + 1 are read, values of b - 1 and b.  All ask for keys of
 // b + 3 and values of b + 2, whose stages (of b - 1 and b - 2) nobody reads, in the time that the matrix instructions
 // leave, and before the barrier wait for what they asked for in the interval before: it is read from the next on.
-//   A causal prompt of 8192, 32 heads over 8 of 128: 514 to 545 us, 1010 to 1070 TFLOP/s.  The matrix pipes are 56 % busy (LDS 29 %,
+//   A causal prompt of 8192, 32 heads over 8 of 128: 505 to 547 us, 1000 to 1085 TFLOP/s.  The matrix pipes are 56 % busy (LDS 29 %,
 // no bank conflicts), a tile takes about 3300 cycles for two waves' 2086 of products, at a clock that the board's power
 // lowers from 2.1 to 1.8 GHz (2.2 on constant operands); without exponentials it takes 9 % fewer cycles, without loads to LDS 12,
 // without reads of LDS 12.  With four waves of 32 rows, one a SIMD, it took 722 us, with two barriers a tile 523.  Heads of 64: half
-// the products, as many exponentials: 334 to 360 us, pipes 37 % busy.  128 tokens over 30000 keys, 32 heads over 4 of 256: 152 us,
+// the products, as many exponentials: 325 to 360 us, pipes 37 % busy.  128 tokens over 30000 keys, 32 heads over 4 of 256: 152 us,
 // 830 TFLOP/s.
 template <int DP, bool FULL>
 __global__ __launch_bounds__(ManyTile<DP>::THREADS, ManyTile<DP>::PER_CU) void attn_pairs_kernel(AttnCall c) {

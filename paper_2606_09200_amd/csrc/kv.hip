@@ -64,7 +64,8 @@ __device__ __forceinline__ void pass(const TablesCall &c, Before &b, const Asked
 }
 
 // STAGED: up to kStaged requests lie in LDS, with what those before them have asked for, so that the passes over them and
-// the search for a token's request wait for nothing but LDS.
+// the search for a token's request wait for nothing but LDS.  Beyond, every workgroup reads them from memory for each pass, in
+// pieces that a thread takes one by one: single tokens of 2048 requests 12 us, of 2049 14, of 5000 25, of 16384 92, of 65536 930.
 constexpr int kStaged = 2048;
 
 template <bool STAGED>
@@ -220,7 +221,7 @@ __global__ __launch_bounds__(kThreads) void kv_tables_kernel(TablesCall c) {
 // for pair i of a head.  turns is a 64-bit fraction of a turn, so that position * turns modulo 2^64 is the exact
 // remainder of the angle, however far the position, and all its bits count (cos_sin).  A workgroup makes its tokens' cosines and sines once, in LDS, and
 // passes over their heads: bound by reading and writing q, k and v once.  8192 tokens, 64 heads over 8 of 128, into the cache:
-// 50 us, 6.7 TB/s, the inputs partly in the last cache (a copy of 2 GiB 4.95); 16 tokens 3.4 us.
+// 58 us, 5.75 TB/s, and 50 where the inputs are partly in the last cache (a copy of 2 GiB 4.95 TB/s); 16 tokens 3.6 us.
 struct RopeCall {
   int T, Hq, Hkv, D, half, interleaved;
   const void *q, *k, *v;
@@ -421,7 +422,7 @@ int rope_launch(const occ_rope_args &a, hipStream_t s) {
   c.per_token = c.per_head * (Hq + Hkv + (cache ? Hkv : 0));
   c.by_item = Divider(c.per_token), c.by_chunk = Divider(c.per_head);
   // More than the L2s hold is stored past them.  8192 tokens, 64 heads over 8 of 128: 77 us with four tokens a workgroup of 256
-  // threads and ordinary stores, 62 with one, 50 past the L2s.
+  // threads and ordinary stores, 62 with one, 50 past the L2s (all with inputs partly in the last cache).
   const RopeGrid grid = rope_grid(a.rows, c.per_token, di->num_cus);
   c.tokens = grid.tokens;
   const bool stream = (int64_t)a.rows * c.per_token * 2 * pairs * elem > (32 << 20);
